@@ -319,6 +319,177 @@ CLEAVE_API int cleave_last_kernel_ms(cleave_plan_t* p, float* exec_ms, float* as
 CLEAVE_API int cleave_assemble_static(cleave_plan_t* p, const float* partials, float* const* C, void* stream);
 
 CLEAVE_API void cleave_destroy(cleave_plan_t* p);
+
+/* ---- operators around the GEMMs ------------------------------------------------------------
+ *
+ * What the paper's server computes itself around the distributed GEMMs of a training step (Section
+ * 3.2: normalisation, activations and the Adam update stay on the server; Section 4.1: the
+ * optimizer's cost C_opt), plus the GEMMs that a server keeps for itself, with everything that
+ * follows the product fused into its write-out.
+ *
+ *   - Matrices are row-major with a leading dimension in elements (ld >= columns).  Element types
+ *     are CLEAVE_T_*; "type 0" means the operand is absent (and its pointer NULL).
+ *   - A pointer is aligned to its element size at least; 16-byte aligned bases with rows that are a
+ *     multiple of 16 bytes apart take the wide loads.  Any number of columns is accepted.
+ *   - Inputs and outputs may be the same buffer where a call says so, and must not overlap otherwise.
+ *   - Zero rows are accepted and compute nothing (sums over rows become 0).
+ *   - All sums, statistics and states are held in fp32; a narrower output is rounded once, to nearest
+ *     even, unless a call says otherwise.
+ *   - The calls check every argument before anything is launched (E_INVAL, E_UNSUPPORTED) and are
+ *     asynchronous on `stream`; results do not depend on the launch (no floating-point atomics).
+ *   - `workspace` [device, 16-byte aligned] holds at least what the matching ..._workspace call
+ *     returns, is written and read by the call's kernels only and may be reused in stream order. */
+#define CLEAVE_T_NONE 0u
+#define CLEAVE_T_BF16 1u
+#define CLEAVE_T_F32  2u
+#define CLEAVE_T_E4M3 3u      /* 8-bit float: 4 exponent bits, 3 mantissa bits, largest value 448, no infinity */
+
+/* Activations: z; max(z, 0); z Phi(z); z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; z / (1 + exp(-z)) */
+#define CLEAVE_ACT_NONE      0u
+#define CLEAVE_ACT_RELU      1u
+#define CLEAVE_ACT_GELU      2u
+#define CLEAVE_ACT_GELU_TANH 3u
+#define CLEAVE_ACT_SILU      4u
+
+/* AdamW over many tensors at once (Section 4.1: the server applies the optimizer to every weight at
+ * the end of a batch).  Per element, with g the gradient times grad_scale and t = step >= 1:
+ *   m = beta1 m + (1 - beta1) g          v = beta2 v + (1 - beta2) g^2
+ *   p = (1 - lr wd) p - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * and the copy w (bf16, optional: what the next step's GEMMs read) is p rounded to nearest even.
+ * Every product, sum, quotient and root is rounded to fp32 by itself (no fused multiply-add), so that
+ * the stored bits are the same wherever the same formula is evaluated in fp32.
+ *
+ * state_type CLEAVE_T_F32: m and v hold fp32.
+ * state_type CLEAVE_T_E4M3: m and v hold one 8-bit code per element and a fp32 scale per 256
+ *   consecutive elements (the last block may be short): m = code * scale; v holds the codes of
+ *   sqrt(v), whose range is half of v's in octaves.  scale = (largest magnitude of the block) / 448, or 0
+ *   (all codes 0) when that magnitude is below 2^-100.  Codes are rounded stochastically: nearest
+ *   rounding would hold v still, because one step moves it by a fraction 1 - beta2 while neighbouring
+ *   codes lie 6 to 12 % apart.  Rounding away from zero happens when the 16 random bits u of the
+ *   element, taken as a fraction, plus the part that is cut off reach 1.  With mix() = SplitMix64's
+ *   output function, key = mix(mix(seed + (step << 32) + tensor index)): word = mix(key + e / 2) for
+ *   element e; u = bits 0-15 (m) and 16-31 (v) of the word for even e, 32-47 and 48-63 for odd e.  A
+ *   root that is not zero is never stored as zero (the next step would divide by eps alone). */
+typedef struct {
+    uint64_t numel;
+    float*       p;            /* [device] fp32 weights, updated in place                                 */
+    void*        w;            /* [device] bf16 copy or NULL                                              */
+    const void*  g;            /* [device] gradient, g_type                                               */
+    void*        m;            /* [device] fp32 or 8-bit codes, updated in place                          */
+    void*        v;
+    float*       m_scale;      /* [device, ceil(numel / 256)] for 8-bit states, else NULL                 */
+    float*       v_scale;
+    double       weight_decay;
+} cleave_adamw_tensor_t;       /* 72 bytes */
+typedef struct {
+    double lr, beta1, beta2, eps, grad_scale;
+    uint64_t step, seed;       /* step counts from 1; seed of the stochastic rounding                      */
+} cleave_adamw_step_t;
+typedef struct cleave_adamw_s cleave_adamw_t;
+/* t [host, n]; every record of one handle has the same state_type and g_type (bf16 or fp32).  The
+ * handle keeps a device table of the records (the only allocation); the buffers stay the caller's.
+ * Errors: E_INVAL, E_UNSUPPORTED, E_CUDA, E_NOMEM. */
+CLEAVE_API int cleave_adamw_create(const cleave_adamw_tensor_t* t, uint32_t n, uint32_t state_type, uint32_t g_type,
+                                   cleave_adamw_t** out);
+/* Other gradient buffers from the next step on.  g [host, n device pointers]. */
+CLEAVE_API int cleave_adamw_set_grads(cleave_adamw_t* h, const void* const* g, void* stream);
+CLEAVE_API int cleave_adamw_step(cleave_adamw_t* h, const cleave_adamw_step_t* s, void* stream);
+CLEAVE_API void cleave_adamw_destroy(cleave_adamw_t* h);
+
+/* Root-mean-square norm with the residual's addition.  Per row, in fp32:
+ *   h = x + r      rstd = (mean_j h_j^2 + eps)^(-1/2)      y_j = h_j rstd w_j
+ * r (and with it h) may be absent: then h = x.  h is stored in r's type and may be r's buffer; the norm is
+ * taken of the sum before it is rounded.  w (bf16 or fp32) may be absent (ones).  rstd may be NULL.
+ * y_type CLEAVE_T_E4M3: the row's codes y_j / scale rounded to nearest even, scale = max_j |y_j| / 448
+ * (a row of zeros has scale 0; a row that holds a NaN has scale NaN). */
+typedef struct {
+    uint64_t rows;
+    uint32_t cols;
+    uint32_t x_type, r_type, w_type, y_type;     /* x, r: bf16 or fp32; y: bf16, fp32 or E4M3 */
+    float eps;
+    const void* x;  uint64_t ldx;
+    const void* r;  uint64_t ldr;
+    void*       h;  uint64_t ldh;
+    const void* w;
+    void*       y;  uint64_t ldy;
+    float*      rstd;                            /* [device, rows] or NULL                    */
+    float*      scale;                           /* [device, rows], E4M3 only                 */
+} cleave_rmsnorm_t;
+CLEAVE_API int cleave_rmsnorm(const cleave_rmsnorm_t* d, void* stream);
+
+/* Its backward pass.  With xh = h rstd and q = w dy:
+ *   dx = rstd (q - xh mean_j(q_j xh_j)) + dres       dw_j = sum over the rows of dy_j xh_j
+ * dx is the gradient of x and of r alike (h = x + r).  dres, the gradient that reaches h from the residual
+ * stream, may be absent and may be dx's buffer; h, dres and dx share h_type.  dw [device, cols] fp32 may be
+ * NULL.  w may be absent. */
+typedef struct {
+    uint64_t rows;
+    uint32_t cols;
+    uint32_t dy_type, h_type, w_type, pad_;      /* dy, h: bf16 or fp32                       */
+    const void*  dy;   uint64_t lddy;
+    const void*  h;    uint64_t ldh;
+    const void*  w;
+    const float* rstd;
+    const void*  dres; uint64_t lddres;
+    void*        dx;   uint64_t lddx;
+    float*       dw;
+} cleave_rmsnorm_backward_t;
+CLEAVE_API uint64_t cleave_rmsnorm_backward_workspace(uint64_t rows, uint32_t cols);
+CLEAVE_API int cleave_rmsnorm_backward(const cleave_rmsnorm_backward_t* d, void* workspace, void* stream);
+
+/* Rows in 8 bits: scale_i = max_j |x_ij| / 448, y = x / scale as E4M3 to nearest even: weights and inputs for
+ * the E4M3 products of cleave_linear.  x: bf16 or fp32. */
+CLEAVE_API int cleave_quantize_rows(const void* x, uint32_t x_type, uint64_t rows, uint32_t cols, uint64_t ldx, void* y,
+                                    uint64_t ldy, float* scale, void* stream);
+
+/* Matrix product with everything that follows it in its write-out:
+ *   z = scale_a[i] scale_b[j] (op(A) op(B))_ij + bias[j]        C = act(z) * mul + res
+ * g gives the sizes, layouts and leading dimensions as in cleave_plan (level is ignored); M may be 0.
+ * in_type CLEAVE_T_BF16: all layouts, lda and ldb multiples of 8.  in_type CLEAVE_T_E4M3: both operands
+ * K-contiguous (transA = 0, transB = 1), lda and ldb multiples of 16.  A and B are 16-byte aligned.
+ * Optional: scale_a [M], scale_b [N] fp32; bias [N] (bf16 or fp32); z out (bf16 or fp32, what
+ * cleave_act_backward needs); mul (bf16 or fp32, the other half of a gated unit); res (bf16 or fp32, may be
+ * C's buffer when it has C's type and ldc: an accumulation).  C: bf16 or fp32.  Products are summed in fp32. */
+typedef struct {
+    cleave_gemm_t g;
+    uint32_t in_type, c_type, bias_type, z_type, mul_type, res_type, act, pad_;
+    const void*  A;
+    const void*  B;
+    const float* scale_a;
+    const float* scale_b;
+    const void*  bias;
+    void*        z;    uint64_t ldz;
+    const void*  mul;  uint64_t ldmul;
+    const void*  res;  uint64_t ldres;
+    void*        C;    uint64_t ldc;
+} cleave_linear_t;
+CLEAVE_API int cleave_linear(const cleave_linear_t* d, void* stream);
+
+/* Backward pass of that epilogue (the products' own gradients are products again):
+ *   dz = dy * mul * act'(z)        dmul = dy * act(z)        dbias_j = sum over the rows of dz (before it is rounded)
+ * z is absent for CLEAVE_ACT_NONE without mul.  dz, dmul and dbias (fp32) are optional; dz may be dy's or
+ * z's buffer when types and leading dimensions agree.  At z = 0 the derivative of RELU is 0. */
+typedef struct {
+    uint64_t rows;
+    uint32_t cols;
+    uint32_t act, dy_type, z_type, mul_type, dz_type, dmul_type, pad_;       /* each bf16 or fp32 */
+    const void* dy;   uint64_t lddy;
+    const void* z;    uint64_t ldz;
+    const void* mul;  uint64_t ldmul;
+    void*       dz;   uint64_t lddz;
+    void*       dmul; uint64_t lddmul;
+    float*      dbias;
+} cleave_act_backward_t;
+CLEAVE_API uint64_t cleave_act_backward_workspace(uint64_t rows, uint32_t cols);
+CLEAVE_API int cleave_act_backward(const cleave_act_backward_t* d, void* workspace, void* stream);
+
+/* Synchronises `stream` and returns 0, or E_TIMEOUT when a bounded wait inside a cleave_linear of this
+ * device ran out since the last call (its C is then incomplete); clears the verdict. */
+CLEAVE_API int cleave_linear_status(void* stream);
+/* Bound, in nanoseconds, of every wait inside cleave_linear's kernels (default 2 s), for all later calls of the
+ * process.  With 0 the first wait that is not satisfied at once gives up (for tests of that path). */
+CLEAVE_API void cleave_linear_set_wait_limit_ns(uint64_t ns);
+
 CLEAVE_API const char* cleave_strerror(int code);
 
 #ifdef __cplusplus

@@ -47,12 +47,6 @@ struct DeviceState {
     bool ev_exec = false, ev_asm = false;
 };
 
-namespace {
-
-typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
-                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
-                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-
 EncodeTiledFn encode_tiled_fn() {
     static EncodeTiledFn fn = nullptr;
     if (!fn) {
@@ -64,6 +58,8 @@ EncodeTiledFn encode_tiled_fn() {
     }
     return fn;
 }
+
+namespace {
 
 // 2-D bf16 tensor map over a row-major [rows x cols] matrix with row stride ld: boxes of
 // 64 (contiguous) x box_rows elements, 128-byte swizzle, zero fill outside the matrix.

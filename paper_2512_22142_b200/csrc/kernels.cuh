@@ -68,6 +68,12 @@ struct ArmParams {
     unsigned long long arena_elems;
 };
 
+// the driver's tensor-map encoder (looked up once; null without a driver)
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+EncodeTiledFn encode_tiled_fn();
+
 cudaError_t launch_arm_queue(const ArmParams& a, int clear_status, cudaStream_t st);
 cudaError_t exec_pair_kernel_prepare();
 cudaError_t launch_exec_pair(uint32_t clusters, const ExecParams& e, cudaStream_t st);

@@ -1,0 +1,190 @@
+// adamw_kernel: one optimizer step over the elements of many tensors (see cleave.h for the formula and the
+// 8-bit states).
+//
+// One warp per block of 256 elements, 8 blocks per CTA.  The work list (tensor, first block) is made once per
+// handle, so tensors of any number and size share one launch.  Lane l owns the elements 4 l .. 4 l + 3 of both
+// halves of the block: every fp32 access of a warp is 512 consecutive bytes, and a block's largest magnitude is
+// a shuffle reduction inside its warp, so an 8-bit state needs no second pass.
+// Bound by the HBM's bandwidth: 30 bytes an element with fp32 states (gradient 4, weight 8, states 16, copy 2),
+// 18 with 8-bit ones.
+#include "ops.cuh"
+
+namespace cleave {
+
+// SplitMix64's output function
+__device__ __forceinline__ uint64_t mix64(uint64_t x) {
+    x += 0x9E3779B97F4A7C15ull;
+    x = (x ^ (x >> 30)) * 0xBF58476D1CE4E5B9ull;
+    x = (x ^ (x >> 27)) * 0x94D049BB133111EBull;
+    return x ^ (x >> 31);
+}
+
+// E4M3 magnitude code of |q| <= 448, away from zero with the probability of what is cut off (u: 16 random bits).
+// From 2^-6 on three mantissa bits stay, so the random bits are added right below them and the rest is cut;
+// below, codes are multiples of 2^-9.
+__device__ __forceinline__ uint32_t stochastic_code(float q, uint32_t u) {
+    const float a = fabsf(q);
+    const uint32_t whole = ((__float_as_uint(a) + (u << 4)) >> 20) - 960u;          // exponent bias 127 - 7, 3 mantissa bits
+    const uint32_t small = (uint32_t)floorf(__fadd_rn(__fmul_rn(a, 512.f), __fmul_rn((float)u, 1.f / 65536.f)));
+    const uint32_t code = min(a >= 0.015625f ? whole : small, 0x7Eu);
+    return a != a ? 0x7Fu : code;
+}
+
+template <bool WIDE, typename T>
+__device__ __forceinline__ void load4(const T* src, uint64_t e, uint64_t n, float (&x)[4]) {
+    if constexpr (WIDE) {
+        if constexpr (sizeof(T) == 4) {
+            const float4 v = *reinterpret_cast<const float4*>(src + e);
+            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+        } else {
+            const uint2 v = *reinterpret_cast<const uint2*>(src + e);
+            const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.y));
+            x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = e + i < n ? to_f32<T>(src[e + i]) : 0.f;
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void load4_codes(const uint8_t* src, uint64_t e, uint64_t n, float (&x)[4]) {
+    if constexpr (WIDE) {
+        const uint32_t c = *reinterpret_cast<const uint32_t*>(src + e);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = e4m3_value((uint8_t)(c >> (8 * i)));
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = e + i < n ? e4m3_value(src[e + i]) : 0.f;
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ void store4(float* dst, uint64_t e, uint64_t n, const float (&x)[4]) {
+    if constexpr (WIDE) *reinterpret_cast<float4*>(dst + e) = make_float4(x[0], x[1], x[2], x[3]);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = x[i];
+}
+template <bool WIDE>
+__device__ __forceinline__ void store4(__nv_bfloat16* dst, uint64_t e, uint64_t n, const float (&x)[4]) {
+    if constexpr (WIDE) {
+        const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
+        *reinterpret_cast<uint2*>(dst + e) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+    } else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = __float2bfloat16_rn(x[i]);
+}
+template <bool WIDE>
+__device__ __forceinline__ void store4_codes(uint8_t* dst, uint64_t e, uint64_t n, const uint32_t (&c)[4]) {
+    if constexpr (WIDE) *reinterpret_cast<uint32_t*>(dst + e) = c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = (uint8_t)c[i];
+}
+
+__device__ __forceinline__ float warp_max_nan(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+}
+// scale of a block whose largest magnitude is `top`, and its reciprocal (both 0 when there is nothing to scale)
+__device__ __forceinline__ float2 block_scale(float top) {
+    const float s = top < 0x1p-100f ? 0.f : __fmul_rn(top, 1.f / kE4M3Max);
+    return make_float2(s, s == 0.f ? 0.f : __frcp_rn(s));
+}
+
+// One block of 256 elements; WIDE: the block is whole and its buffers are aligned.
+template <bool STATE8, typename G, bool WIDE>
+__device__ __forceinline__ void adamw_block(const AdamTensor& t, uint32_t tensor, uint64_t block, const AdamStep& s, uint32_t lane) {
+    const uint64_t n = t.numel, e0 = block * kStateBlock + lane * 4u;
+    float m[2][4], r[2][4], p[2][4], g[2][4];
+    float sm = 0.f, sv = 0.f;
+    if constexpr (STATE8) { sm = t.m_scale[block]; sv = t.v_scale[block]; }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint64_t e = e0 + j * 128u;
+        load4<WIDE>(static_cast<const G*>(t.g), e, n, g[j]);
+        load4<WIDE>(t.p, e, n, p[j]);
+        if constexpr (STATE8) { load4_codes<WIDE>(static_cast<const uint8_t*>(t.m), e, n, m[j]); load4_codes<WIDE>(static_cast<const uint8_t*>(t.v), e, n, r[j]); }
+        else                  { load4<WIDE>(static_cast<const float*>(t.m), e, n, m[j]); load4<WIDE>(static_cast<const float*>(t.v), e, n, r[j]); }
+    }
+    const float decay = (float)__dadd_rn(1.0, -__dmul_rn(s.lr, t.weight_decay));
+    float top_m = 0.f, top_r = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float gr = __fmul_rn(g[j][i], s.grad_scale);
+            float mo = m[j][i], vo = r[j][i];
+            if constexpr (STATE8) {
+                mo = __fmul_rn(mo, sm);
+                const float root = __fmul_rn(vo, sv);
+                vo = __fmul_rn(root, root);
+            }
+            mo = __fadd_rn(__fmul_rn(mo, s.beta1), __fmul_rn(gr, s.omb1));
+            vo = __fadd_rn(__fmul_rn(vo, s.beta2), __fmul_rn(__fmul_rn(gr, gr), s.omb2));
+            const float root = __fsqrt_rn(vo);
+            const float den = __fadd_rn(__fmul_rn(root, s.root), s.eps);
+            p[j][i] = __fsub_rn(__fmul_rn(p[j][i], decay), __fmul_rn(__fdiv_rn(mo, den), s.step_size));
+            m[j][i] = mo;
+            if constexpr (STATE8) { r[j][i] = root; top_m = max_nan(top_m, fabsf(mo)); top_r = max_nan(top_r, root); }
+            else r[j][i] = vo;
+        }
+        const uint64_t e = e0 + j * 128u;
+        store4<WIDE>(t.p, e, n, p[j]);
+        if (t.w) store4<WIDE>(t.w, e, n, p[j]);
+        if constexpr (!STATE8) { store4<WIDE>(static_cast<float*>(t.m), e, n, m[j]); store4<WIDE>(static_cast<float*>(t.v), e, n, r[j]); }
+    }
+    if constexpr (STATE8) {
+        const float2 bm = block_scale(warp_max_nan(top_m)), bv = block_scale(warp_max_nan(top_r));
+        const uint64_t key = mix64(mix64(s.base + tensor));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const uint64_t e = e0 + j * 128u;
+            uint32_t cm[4], cv[4];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint64_t word = mix64(key + (e >> 1) + h);
+#pragma unroll
+                for (int o = 0; o < 2; ++o) {
+                    const int i = 2 * h + o;
+                    const uint32_t bits = (uint32_t)(word >> (32 * o));
+                    const float qm = __fmul_rn(m[j][i], bm.y), qv = __fmul_rn(r[j][i], bv.y);
+                    cm[i] = stochastic_code(qm, bits & 0xFFFFu) | (qm < 0.f ? 0x80u : 0u);
+                    const uint32_t c = stochastic_code(qv, bits >> 16);
+                    cv[i] = c == 0u && qv > 0.f ? 1u : c;
+                }
+            }
+            store4_codes<WIDE>(static_cast<uint8_t*>(t.m), e, n, cm);
+            store4_codes<WIDE>(static_cast<uint8_t*>(t.v), e, n, cv);
+        }
+        if (lane == 0) { t.m_scale[block] = bm.x; t.v_scale[block] = bv.x; }
+    }
+}
+
+template <bool STATE8, typename G>
+__global__ void __launch_bounds__(32 * kChunkBlocks)
+adamw_kernel(const AdamTensor* __restrict__ tensors, const AdamChunk* __restrict__ chunks, const __grid_constant__ AdamStep s) {
+    const AdamChunk c = chunks[blockIdx.x];
+    const AdamTensor& t = tensors[c.tensor];
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint64_t block = (uint64_t)c.block0 + (threadIdx.x >> 5);
+    if (block * kStateBlock >= t.numel) return;
+    if (t.wide && (block + 1) * kStateBlock <= t.numel) adamw_block<STATE8, G, true>(t, c.tensor, block, s, lane);
+    else adamw_block<STATE8, G, false>(t, c.tensor, block, s, lane);
+}
+
+cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, const AdamStep& s, bool state8,
+                         bool g_bf16, cudaStream_t st) {
+    if (!n_chunks) return cudaSuccess;
+    const dim3 block(32 * kChunkBlocks);
+    if (state8) {
+        if (g_bf16) adamw_kernel<true, __nv_bfloat16><<<n_chunks, block, 0, st>>>(tensors, chunks, s);
+        else        adamw_kernel<true, float><<<n_chunks, block, 0, st>>>(tensors, chunks, s);
+    } else {
+        if (g_bf16) adamw_kernel<false, __nv_bfloat16><<<n_chunks, block, 0, st>>>(tensors, chunks, s);
+        else        adamw_kernel<false, float><<<n_chunks, block, 0, st>>>(tensors, chunks, s);
+    }
+    return cudaGetLastError();
+}
+
+}  // namespace cleave

@@ -1,0 +1,396 @@
+// Matrix product with an epilogue (see cleave.h): z = scale_a scale_b (op(A) op(B)) + bias, C = act(z) mul + res.
+//
+// linear_split_kernel: one 128 x 128 tile of C per cluster of S = 1, 2, 4 or 8 CTAs; each CTA runs a K-range of the
+// tile (TMA loads into a ring of 128-byte-swizzled stages, one thread issuing tcgen05.mma, the accumulator in tensor
+// memory), then the S accumulators are laid into the CTAs' own shared memory and CTA r adds columns r * 128 / S ... of
+// all of them, in the order of the K-ranges, through distributed shared memory.  So a product of few rows is spread
+// over the whole GPU -- its time is the weights' bytes, which need every SM's loads in flight -- without a
+// workspace, a second launch or an order that changes.  Two CTAs share an SM: the write-out of one runs beside the
+// products of the other.
+//
+// Operands: K-contiguous or M/N-contiguous bf16 through the descriptors' major bits (no transposed copies), or
+// K-contiguous E4M3 (kind::f8f6f4), 128 bytes of K a stage either way; TMA fills what lies outside a matrix with
+// zeros, and nothing outside C is written.
+//
+// Every wait is bounded (2 s by default): a wait that runs out records it in a status word of the library, the
+// CTA's roles leave, copies and MMAs in flight are given time to end, and the kernel returns.
+#include <atomic>
+
+#include "kernels.cuh"
+#include "ops.cuh"
+#include "ptx.cuh"
+
+namespace cleave {
+
+__device__ unsigned int g_linear_status;
+static std::atomic<uint64_t> g_linear_wait_limit{2000000000ull};
+
+constexpr uint32_t kLinTile = 128, kLinStages = 3, kLinOperand = 16384, kLinStage = 2 * kLinOperand;
+constexpr uint32_t kLinThreads = 192, kLinSmem = kLinStages * kLinStage + 1024;
+
+// What the write-out needs, the same for every kernel of this file.
+struct Epilogue {
+    uint32_t M, N;
+    uint32_t act, c_type, bias_type, z_type, mul_type, res_type;
+    uint32_t wide;                  // bit per operand: rows allow 16-byte accesses (kWide*)
+    const float* scale_a;
+    const float* scale_b;
+    const void* bias;
+    void* z;
+    const void* mul;
+    const void* res;
+    void* C;
+    uint64_t ldz, ldmul, ldres, ldc;
+};
+enum : uint32_t { kWideB = 1u, kWideBias = 2u, kWideZ = 4u, kWideMul = 8u, kWideRes = 16u, kWideC = 32u };
+
+struct LinearParams {
+    Epilogue e;
+    uint32_t K_blocks, splits, tiles_n;
+    uint32_t a_mn, b_mn;
+    unsigned long long wait_limit_ns;
+};
+
+// 16 consecutive elements of a row as fp32; `wide`: whole and aligned.
+__device__ __forceinline__ void load16(const void* p, uint32_t type, uint64_t at, uint32_t n, bool wide, float (&x)[16]) {
+    if (wide && n >= 16) {
+        if (type == CLEAVE_T_F32) {
+            const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) { const float4 v = s[q]; x[4 * q] = v.x; x[4 * q + 1] = v.y; x[4 * q + 2] = v.z; x[4 * q + 3] = v.w; }
+        } else {
+            const uint4* s = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + at);
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                const uint4 v = s[q];
+                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (int h = 0; h < 4; ++h) { x[8 * q + 2 * h] = __uint_as_float(w[h] << 16); x[8 * q + 2 * h + 1] = __uint_as_float(w[h] & 0xFFFF0000u); }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x[i] = (uint32_t)i < n ? load_as(p, type, at + i) : 0.f;
+    }
+}
+__device__ __forceinline__ void store16(void* p, uint32_t type, uint64_t at, uint32_t n, bool wide, const float (&x)[16]) {
+    if (wide && n >= 16) {
+        if (type == CLEAVE_T_F32) {
+            float4* d = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) d[q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
+        } else {
+            uint4* d = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p) + at);
+#pragma unroll
+            for (int q = 0; q < 2; ++q)
+                d[q] = make_uint4(pack_bf16(x[8 * q], x[8 * q + 1]), pack_bf16(x[8 * q + 2], x[8 * q + 3]), pack_bf16(x[8 * q + 4], x[8 * q + 5]), pack_bf16(x[8 * q + 6], x[8 * q + 7]));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) if ((uint32_t)i < n) store_as(p, type, at + i, x[i]);
+    }
+}
+
+// 16 accumulator values of one row, columns col .. col + 15, through the epilogue to C (and z).
+__device__ __forceinline__ void write_out16(const Epilogue& e, uint32_t row, uint32_t col, float (&v)[16]) {
+    if (row >= e.M || col >= e.N) return;
+    const uint32_t n = e.N - col;
+    float t[16];
+    if (e.scale_a) {
+        const float sa = e.scale_a[row];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= sa;
+    }
+    if (e.scale_b) {
+        load16(e.scale_b, CLEAVE_T_F32, col, n, e.wide & kWideB, t);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= t[i];
+    }
+    if (e.bias) {
+        load16(e.bias, e.bias_type, col, n, e.wide & kWideBias, t);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += t[i];
+    }
+    if (e.z) store16(e.z, e.z_type, row * e.ldz + col, n, e.wide & kWideZ, v);
+    if (e.act != CLEAVE_ACT_NONE) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] = act_value(v[i], e.act);
+    }
+    if (e.mul) {
+        load16(e.mul, e.mul_type, row * e.ldmul + col, n, e.wide & kWideMul, t);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] *= t[i];
+    }
+    if (e.res) {
+        load16(e.res, e.res_type, row * e.ldres + col, n, e.wide & kWideRes, t);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) v[i] += t[i];
+    }
+    store16(e.C, e.c_type, row * e.ldc + col, n, e.wide & kWideC, v);
+}
+
+// ---- PTX of one-CTA products ---------------------------------------------------------------------------
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint32_t bar, int32_t c0, int32_t c1) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1) : "memory");
+}
+template <bool E4M3>
+__device__ __forceinline__ void umma_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (E4M3)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void umma_commit_one(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, float (&v)[16]) {
+    uint32_t u[16];
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
+                   "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]) : "r"(taddr) : "memory");
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
+}
+// Instruction descriptor of kind::f8f6f4: fp32 accumulator (bits 4-5 = 1), E4M3 A and B (format 0), both K-contiguous.
+__device__ __forceinline__ uint32_t instr_desc_e4m3(uint32_t m, uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((m >> 4) << 24); }
+__device__ __forceinline__ float ld_dsmem(uint32_t cluster_addr) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
+    return v;
+}
+
+struct LinWait { volatile uint32_t* abort_flag; uint64_t limit_ns; };
+static __device__ __noinline__ bool lin_wait_slow(uint32_t bar, uint32_t parity, const LinWait& w) {
+    const uint64_t t0 = global_timer_ns();
+    uint32_t spins = 0;
+    while (!mbar_try_wait(bar, parity)) {
+        if ((spins++ & 255u) == 0) {                     // at the first unsuccessful poll, then every 256
+            if (*w.abort_flag) return false;
+            if (global_timer_ns() - t0 >= w.limit_ns) { *w.abort_flag = 1u; atomicOr(&g_linear_status, STATUS_TIMEOUT); return false; }
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, const LinWait& w) {
+    return mbar_try_wait(bar, parity) || lin_wait_slow(bar, parity, w);
+}
+
+struct __align__(16) LinShared {
+    uint64_t full[kLinStages], empty[kLinStages], acc_full, drain;
+    uint32_t tmem_base, abort_flag;
+};
+
+template <bool E4M3>
+__global__ void __launch_bounds__(kLinThreads, 2)
+linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ LinearParams P) {
+    extern __shared__ uint8_t dyn_smem[];
+    __shared__ LinShared sh;
+    constexpr uint32_t kBlk = E4M3 ? 128u : 64u;         // K per stage: 128 bytes
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
+    const uint32_t base = (smem_u32(dyn_smem) + 1023u) & ~1023u;
+    const uint32_t rank = blockIdx.x % P.splits, tile = blockIdx.x / P.splits;
+    const uint32_t m0 = (tile / P.tiles_n) * kLinTile, n0 = (tile % P.tiles_n) * kLinTile;
+    const uint32_t kb0 = (uint32_t)((uint64_t)P.K_blocks * rank / P.splits), kb1 = (uint32_t)((uint64_t)P.K_blocks * (rank + 1) / P.splits);
+    const LinWait W = {&sh.abort_flag, P.wait_limit_ns};
+
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < kLinStages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
+        mbar_init(smem_u32(&sh.acc_full), 1);
+        mbar_init(smem_u32(&sh.drain), 1);
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(kLinTile) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem_base;
+
+    if (warp == 0 && lane == 0) {
+        // ---- producer ----
+        for (uint32_t kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+            const uint32_t s = it % kLinStages, ph = (it / kLinStages) & 1u;
+            if (!lin_wait(smem_u32(&sh.empty[s]), ph ^ 1u, W)) break;
+            const uint32_t bar = smem_u32(&sh.full[s]), sa = base + s * kLinStage, sb = sa + kLinOperand;
+            mbar_arrive_expect_tx(bar, kLinStage);
+            const int32_t k = (int32_t)(kb * kBlk);
+            if (P.a_mn) { tma_load_2d(sa, &map_a, bar, (int32_t)m0, k); tma_load_2d(sa + kSubBytes, &map_a, bar, (int32_t)m0 + 64, k); }
+            else tma_load_2d(sa, &map_a, bar, k, (int32_t)m0);
+            if (P.b_mn) { tma_load_2d(sb, &map_b, bar, (int32_t)n0, k); tma_load_2d(sb + kSubBytes, &map_b, bar, (int32_t)n0 + 64, k); }
+            else tma_load_2d(sb, &map_b, bar, k, (int32_t)n0);
+        }
+    } else if (warp == 1 && lane == 0) {
+        // ---- MMA issuer ----
+        const uint32_t idesc = E4M3 ? instr_desc_e4m3(kLinTile, kLinTile) : instr_desc_bf16(kLinTile, kLinTile, P.a_mn, P.b_mn);
+        const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
+        const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
+        bool ok = true;
+        for (uint32_t kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
+            const uint32_t s = it % kLinStages, ph = (it / kLinStages) & 1u;
+            if (!lin_wait(smem_u32(&sh.full[s]), ph, W)) { ok = false; break; }
+            tc_fence_after();
+            const uint32_t sa = base + s * kLinStage, sb = sa + kLinOperand;
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q)              // 32 bytes of K each
+                umma_one<E4M3>(tmem, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, (it | q) != 0u);
+            umma_commit_one(smem_u32(&sh.empty[s]));
+        }
+        if (ok) umma_commit_one(smem_u32(&sh.acc_full));
+        // everything issued above has completed before tensor memory is released
+        umma_commit_one(smem_u32(&sh.drain));
+        const uint64_t t0 = global_timer_ns();
+        while (!mbar_try_wait(smem_u32(&sh.drain), 0u))
+            if (global_timer_ns() - t0 > 2000000000ull) { atomicOr(&g_linear_status, STATUS_TIMEOUT); break; }
+    }
+    __syncwarp();
+    // ---- write-out: warps 2..5, warp w owns the accumulator rows 32 (w % 4) ... ----
+    const uint32_t quad = warp & 3u, row = m0 + quad * 32u + lane;
+    bool ok = true;
+    if (warp >= 2) {
+        ok = __all_sync(0xFFFFFFFFu, lin_wait(smem_u32(&sh.acc_full), 0u, W));
+        tc_fence_after();
+        const uint32_t taddr = tmem + ((quad * 32u) << 16);
+        if (ok && P.splits == 1) {
+#pragma unroll 1
+            for (uint32_t c = 0; c < kLinTile; c += 16) {
+                float v[16];
+                tmem_ld_32x16(taddr + c, v);
+                write_out16(P.e, row, n0 + c, v);
+            }
+        } else if (ok) {
+            float* part = reinterpret_cast<float*>(dyn_smem + (base - smem_u32(dyn_smem)));      // the stages are read: column-major [128][128]
+#pragma unroll 1
+            for (uint32_t c = 0; c < kLinTile; c += 16) {
+                float v[16];
+                tmem_ld_32x16(taddr + c, v);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) part[(c + i) * kLinTile + quad * 32u + lane] = v[i];
+            }
+        }
+        tc_fence_before();
+    }
+    if (P.splits > 1) {
+        cluster_arrive_wait();
+        if (warp >= 2 && ok) {
+            const uint32_t cols = kLinTile / P.splits, c0 = rank * cols;
+#pragma unroll 1
+            for (uint32_t c = c0; c < c0 + cols; c += 16) {
+                float v[16];
+#pragma unroll
+                for (int i = 0; i < 16; ++i) v[i] = 0.f;
+#pragma unroll 1
+                for (uint32_t r = 0; r < P.splits; ++r) {              // K-ranges in order
+                    const uint32_t src = mapa_shared(base, r) + ((c * kLinTile) + quad * 32u + lane) * 4u;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] += ld_dsmem(src + i * kLinTile * 4u);
+                }
+                write_out16(P.e, row, n0 + c, v);
+            }
+        }
+        cluster_arrive_wait();                            // no CTA leaves while another reads its shared memory
+    }
+    __syncthreads();
+    if (sh.abort_flag) {                                  // a role gave up: copies may still be in flight towards this CTA
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 200000ull) { }
+        __syncthreads();
+    }
+    tc_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kLinTile) : "memory");
+}
+
+// ---- host --------------------------------------------------------------------------------------------
+namespace {
+
+// Boxes of 128 bytes along the contiguous dimension x `box_rows` rows of a row-major [rows x cols] matrix.
+int encode_operand(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows, bool e4m3) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return CLEAVE_E_CUDA;
+    const uint32_t es = e4m3 ? 1u : 2u;
+    cuuint64_t dims[2] = {cols, rows};
+    cuuint64_t strides[1] = {ld * es};
+    cuuint32_t box[2] = {128u / es, box_rows};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(out, e4m3 ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(base), dims,
+                          strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? 0 : CLEAVE_E_CUDA;
+}
+
+bool wide16(const void* p, uint64_t ld, uint32_t type) { return ((uintptr_t)p & 15) == 0 && (ld * type_bytes(type)) % 16 == 0; }
+
+// SM count of the current device, or a negative CLEAVE_E_* code
+int sm_count() {
+    int dev = 0, n = 0, major = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+    return major == 10 ? n : CLEAVE_E_UNSUPPORTED;
+}
+
+}  // namespace
+
+int launch_linear(const cleave_linear_t& d, cudaStream_t st) {
+    const int sms = sm_count();
+    if (sms < 0) return sms;
+    const bool e4m3 = d.in_type == CLEAVE_T_E4M3;
+    const cleave_gemm_t& g = d.g;
+    LinearParams P = {};
+    Epilogue& e = P.e;
+    e.M = g.M; e.N = g.N; e.act = d.act;
+    e.c_type = d.c_type; e.bias_type = d.bias_type; e.z_type = d.z_type; e.mul_type = d.mul_type; e.res_type = d.res_type;
+    e.scale_a = d.scale_a; e.scale_b = d.scale_b; e.bias = d.bias; e.z = d.z; e.mul = d.mul; e.res = d.res; e.C = d.C;
+    e.ldz = d.ldz; e.ldmul = d.ldmul; e.ldres = d.ldres; e.ldc = d.ldc;
+    e.wide = (wide16(d.scale_b, 0, CLEAVE_T_F32) ? kWideB : 0u) | (wide16(d.bias, 0, d.bias_type) ? kWideBias : 0u) |
+             (wide16(d.z, d.ldz, d.z_type) ? kWideZ : 0u) | (wide16(d.mul, d.ldmul, d.mul_type) ? kWideMul : 0u) |
+             (wide16(d.res, d.ldres, d.res_type) ? kWideRes : 0u) | (wide16(d.C, d.ldc, d.c_type) ? kWideC : 0u);
+    P.wait_limit_ns = g_linear_wait_limit.load(std::memory_order_relaxed);
+    P.a_mn = g.transA ? 1u : 0u;
+    P.b_mn = g.transB ? 0u : 1u;
+    const uint32_t kblk = e4m3 ? 128u : 64u;
+    P.K_blocks = (g.K + kblk - 1) / kblk;
+    CUtensorMap ma, mb;
+    int rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, 128, e4m3);
+    if (!rc) rc = g.transB ? encode_operand(&mb, d.B, g.N, g.K, g.ldb, 128, e4m3) : encode_operand(&mb, d.B, g.K, g.N, g.ldb, 64, e4m3);
+    if (rc) return rc;
+    const uint64_t tiles_m = (g.M + kLinTile - 1) / kLinTile, tiles_n = (g.N + kLinTile - 1) / kLinTile, tiles = tiles_m * tiles_n;
+    P.tiles_n = (uint32_t)tiles_n;
+    // K is split while every CTA still finds a place at once (two an SM) and keeps at least four stages of work
+    P.splits = 1;
+    while (P.splits < 8 && tiles * P.splits * 2 <= 2u * (uint32_t)sms && P.K_blocks / (P.splits * 2) >= 4) P.splits *= 2;
+    if (tiles * P.splits > 0x7FFFFFFFull) return CLEAVE_E_UNSUPPORTED;
+    auto kernel = e4m3 ? linear_split_kernel<true> : linear_split_kernel<false>;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(tiles * P.splits));
+    cfg.blockDim = dim3(kLinThreads);
+    cfg.dynamicSmemBytes = kLinSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = P.splits; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, ma, mb, P) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+    return 0;
+}
+
+int linear_status(cudaStream_t st) {
+    unsigned int s = 0;
+    const unsigned int zero = 0;
+    if (cudaMemcpyFromSymbolAsync(&s, g_linear_status, sizeof s, 0, cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaStreamSynchronize(st) != cudaSuccess ||
+        (s && (cudaMemcpyToSymbolAsync(g_linear_status, &zero, sizeof zero, 0, cudaMemcpyHostToDevice, st) != cudaSuccess ||
+               cudaStreamSynchronize(st) != cudaSuccess))) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+    return s & STATUS_TIMEOUT ? CLEAVE_E_TIMEOUT : 0;
+}
+void linear_set_wait_limit_ns(uint64_t ns) { g_linear_wait_limit.store(ns, std::memory_order_relaxed); }
+
+}  // namespace cleave

@@ -1,0 +1,122 @@
+// Shared pieces of the operators around the GEMMs: element types, activations, 8-bit codes, launcher
+// declarations (internal).
+#pragma once
+
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp8.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "cleave.h"
+
+namespace cleave {
+
+constexpr float kE4M3Max = 448.f;
+constexpr uint32_t kStateBlock = 256;            // elements that share a scale in an 8-bit optimizer state
+
+inline uint32_t type_bytes(uint32_t t) { return t == CLEAVE_T_F32 ? 4u : (t == CLEAVE_T_BF16 ? 2u : (t == CLEAVE_T_E4M3 ? 1u : 0u)); }
+
+// ---- elements ----------------------------------------------------------------------------------------
+template <typename T> __device__ __forceinline__ float to_f32(T v);
+template <> __device__ __forceinline__ float to_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_f32<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+template <typename T> __device__ __forceinline__ T from_f32(float v);
+template <> __device__ __forceinline__ float from_f32<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_f32<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+
+// element `i` of an operand whose type is only known at run time (edges; the wide paths are typed)
+__device__ __forceinline__ float load_as(const void* p, uint32_t type, uint64_t i) {
+    return type == CLEAVE_T_F32 ? static_cast<const float*>(p)[i] : __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+__device__ __forceinline__ void store_as(void* p, uint32_t type, uint64_t i, float v) {
+    if (type == CLEAVE_T_F32) static_cast<float*>(p)[i] = v;
+    else static_cast<__nv_bfloat16*>(p)[i] = __float2bfloat16_rn(v);
+}
+
+// largest of two values; a NaN in either stays (fmaxf would drop it)
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+
+__device__ __forceinline__ uint8_t e4m3_nearest(float v) { return (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
+__device__ __forceinline__ float e4m3_value(uint8_t code) {
+    return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+}
+
+// ---- activations ----------------------------------------------------------------------------------
+// The two forms with an exponential are z g with g = 1 / (1 + e), e = exp(-t): one exponential and one quotient.
+// Where e overflows g is 0 (the limit); no 1 - tanh cancellation on the negative side.  In the slopes 1 - g loses
+// relative accuracy only where g is close to 1 and the term it belongs to vanishes against g.
+__device__ __forceinline__ float gelu_tanh_arg(float z) { return z * fmaf(0.07135481627260025f, z * z, 1.5957691216057308f); }   // 2 sqrt(2/pi) (z + 0.044715 z^3)
+__device__ __forceinline__ float act_value(float z, uint32_t act) {
+    switch (act) {
+        case CLEAVE_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
+        case CLEAVE_ACT_GELU: return 0.5f * z * erfcf(-0.7071067811865476f * z);
+        case CLEAVE_ACT_GELU_TANH: return __fdividef(z, 1.f + __expf(-gelu_tanh_arg(z)));
+        case CLEAVE_ACT_SILU: return __fdividef(z, 1.f + __expf(-z));
+        default: return z;
+    }
+}
+// value and slope at once
+__device__ __forceinline__ float2 act_value_slope(float z, uint32_t act) {
+    switch (act) {
+        case CLEAVE_ACT_RELU: return make_float2(z > 0.f ? z : (z != z ? z : 0.f), z > 0.f ? 1.f : 0.f);
+        case CLEAVE_ACT_GELU: {
+            const float phi = 0.5f * erfcf(-0.7071067811865476f * z);
+            return make_float2(z * phi, fmaf(z * 0.3989422804014327f, __expf(-0.5f * z * z), phi));
+        }
+        case CLEAVE_ACT_GELU_TANH: {
+            const float g = __fdividef(1.f, 1.f + __expf(-gelu_tanh_arg(z))), zg = z * g;
+            const float du = fmaf(0.21406444881780074f, fminf(z * z, 1e30f), 1.5957691216057308f);      // finite: 0 * du is 0 far out
+            return make_float2(zg, fmaf(zg * (1.f - g), du, g));
+        }
+        case CLEAVE_ACT_SILU: {
+            const float g = __fdividef(1.f, 1.f + __expf(-z)), zg = z * g;
+            return make_float2(zg, fmaf(zg, 1.f - g, g));
+        }
+        default: return make_float2(z, 1.f);
+    }
+}
+
+// ---- AdamW -----------------------------------------------------------------------------------------
+struct AdamTensor {                 // device record of one tensor
+    uint64_t numel;
+    float* p;
+    __nv_bfloat16* w;
+    const void* g;
+    void* m;
+    void* v;
+    float* m_scale;
+    float* v_scale;
+    double weight_decay;
+    uint32_t wide;                  // every buffer allows the wide accesses
+    uint32_t pad;
+};
+struct AdamStep {
+    float beta1, omb1, beta2, omb2; // omb = 1 - beta, formed in 64 bits
+    float step_size, root, eps, grad_scale;
+    double lr;
+    uint64_t base;                  // seed + (step << 32)
+};
+struct AdamChunk { uint32_t tensor, block0; };   // kChunkBlocks blocks of 256 elements from block0 on
+constexpr uint32_t kChunkBlocks = 8;
+cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, const AdamStep& s, bool state8,
+                         bool g_bf16, cudaStream_t st);
+
+// ---- norm, rows in 8 bits, epilogue backward ---------------------------------------------------------
+cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, cudaStream_t st);
+uint32_t rmsnorm_backward_parts(uint64_t rows, uint32_t cols);          // rows of partial sums in the workspace
+cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, cudaStream_t st);
+uint32_t act_backward_parts(uint64_t rows, uint32_t cols);
+cudaError_t launch_act_backward(const cleave_act_backward_t& d, float* ws, cudaStream_t st);
+cudaError_t launch_sum_parts(const float* ws, uint32_t parts, uint32_t cols, float* out, cudaStream_t st);
+
+// ---- product with an epilogue --------------------------------------------------------------------------
+int launch_linear(const cleave_linear_t& d, cudaStream_t st);           // CLEAVE_* code
+int linear_status(cudaStream_t st);
+void linear_set_wait_limit_ns(uint64_t ns);
+
+}  // namespace cleave

@@ -1,0 +1,502 @@
+"""The operators around the GEMMs on the GPU against their 64-bit oracle (AdamW: against its exact fp32 definition,
+bit for bit).  Tolerances are the roundings of the stated arithmetic: U = 2^-24 is half a unit of fp32, a bf16
+result may be half a unit of its 8 significant bits (2^-8) off, sums of n terms in fp32 a modest multiple of sqrt(n) U of their
+terms' magnitudes (bounded here by a fixed 64 U, well above any order of up to 2^15 terms split over lanes)."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import ops as ref
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+SUM = 64 * U
+DT = {"bf16": torch.bfloat16, "f32": torch.float32}
+KINDS = ["none", "relu", "gelu", "gelu_tanh", "silu"]
+
+
+@pytest.fixture(scope="module")
+def cl():
+    import paper_2512_22142_b200 as cl
+    return cl
+
+
+def _dev():
+    return torch.device("cuda:0")
+
+
+def _rand(rng, shape, dtype, scale=1.0):
+    return torch.tensor(rng.normal(size=shape) * scale, dtype=torch.float32).to(dtype).to(_dev())
+
+
+def _f64(t):
+    return None if t is None else t.to(torch.float64).cpu().numpy()
+
+
+def _close(got, want, abs_tol, what=""):
+    """|got - want| <= abs_tol + the rounding of got's type."""
+    half = 2.0 ** -8 if got.dtype == torch.bfloat16 else U
+    g = _f64(got)
+    assert np.isfinite(g).all(), what
+    bad = np.abs(g - want) - (abs_tol + half * np.maximum(np.abs(want), np.abs(g)) * 1.001 + 1e-38)
+    assert bad.max(initial=-1.0) <= 0, f"{what}: {bad.max():.3e} over at {np.unravel_index(np.argmax(bad), bad.shape)}"
+
+
+def _strided(rng, rows, cols, dtype, pad, scale=1.0):
+    """A [rows, cols] view whose rows lie `cols + pad` apart."""
+    return _rand(rng, (max(rows, 1), cols + pad), dtype, scale)[:rows, :cols]
+
+
+# ---- AdamW ---------------------------------------------------------------------------------------------
+def _adam_state(rng, sizes, eight, grad, copies, shift=0):
+    """Tensors whose storage begins `shift` elements into an allocation (shift != 0: the narrow path)."""
+    out = dict(p=[], g=[], m=[], v=[], ms=[], vs=[], w=[])
+    for n in sizes:
+        cut = lambda t: t.to(_dev())[shift:]  # noqa: E731
+        N = n + shift
+        out["p"].append(cut(torch.tensor(rng.normal(size=N) * 0.02, dtype=torch.float32)))
+        out["g"].append(cut(torch.tensor(rng.normal(size=N) * 0.01, dtype=torch.float32).to(grad)))
+        m, v = rng.normal(size=N) * 0.003, (rng.normal(size=N) * 0.01) ** 2
+        if eight:
+            codes = torch.tensor(rng.integers(0, 0x7F, size=N), dtype=torch.uint8)
+            sign = torch.tensor(rng.integers(0, 2, size=N) * 0x80, dtype=torch.uint8)
+            out["m"].append(cut(codes | sign).view(torch.float8_e4m3fn))
+            out["v"].append(cut(torch.tensor(rng.integers(0, 0x7F, size=N), dtype=torch.uint8)).view(torch.float8_e4m3fn))
+            blocks = -(-n // 256)
+            out["ms"].append(torch.tensor(rng.uniform(1e-6, 1e-5, size=blocks), dtype=torch.float32).to(_dev()))
+            out["vs"].append(torch.tensor(rng.uniform(1e-6, 1e-4, size=blocks), dtype=torch.float32).to(_dev()))
+        else:
+            out["m"].append(cut(torch.tensor(m, dtype=torch.float32)))
+            out["v"].append(cut(torch.tensor(v, dtype=torch.float32)))
+        if copies:
+            out["w"].append(cut(torch.zeros(N, dtype=torch.bfloat16)))
+    return out
+
+
+def _make(cl, s, wd, eight, copies):
+    return cl.AdamW(s["p"], s["g"], s["m"], s["v"], copies=s["w"] if copies else None, m_scales=s["ms"] if eight else None,
+                    v_scales=s["vs"] if eight else None, weight_decay=wd)
+
+
+def _codes(t):
+    return t.view(torch.uint8).cpu().numpy()
+
+
+def _bits(t):
+    return t.cpu().view(torch.int32).numpy()
+
+
+def _check_step(s0, s, wd, eight, copies, hyper, step, seed):
+    for i in range(len(s["p"])):
+        if s["p"][i].numel() == 0:
+            continue
+        args = dict(lr=hyper["lr"], beta1=hyper["beta1"], beta2=hyper["beta2"], eps=hyper["eps"], step=step, weight_decay=wd[i],
+                    grad_scale=hyper.get("grad_scale", 1.0), seed=seed, tensor=i)
+        p, g = s0["p"][i].cpu().numpy(), s0["g"][i].float().cpu().numpy()
+        if eight:
+            want = ref.adamw(p, g, _codes(s0["m"][i]), _codes(s0["v"][i]), m_scale=s0["ms"][i].cpu().numpy(), v_scale=s0["vs"][i].cpu().numpy(), **args)
+            assert np.array_equal(_codes(s["m"][i]), want[1]), f"tensor {i}: codes of m"
+            assert np.array_equal(_codes(s["v"][i]), want[2]), f"tensor {i}: codes of v"
+            assert np.array_equal(_bits(s["ms"][i]), want[3].view(np.int32)) and np.array_equal(_bits(s["vs"][i]), want[4].view(np.int32))
+        else:
+            want = ref.adamw(p, g, s0["m"][i].cpu().numpy(), s0["v"][i].cpu().numpy(), **args)
+            assert np.array_equal(_bits(s["m"][i]), want[1].view(np.int32)) and np.array_equal(_bits(s["v"][i]), want[2].view(np.int32))
+        assert np.array_equal(_bits(s["p"][i]), want[0].astype(np.float32).view(np.int32)), f"tensor {i}: weights"
+        if copies:
+            assert torch.equal(s["w"][i].cpu(), torch.tensor(want[0]).to(torch.bfloat16))
+
+
+def _clone(s):
+    return {k: [t.clone() for t in v] for k, v in s.items()}
+
+
+@pytest.mark.parametrize("eight", [False, True])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_adamw_stored_bits_are_the_definitions(cl, eight, grad, shift):
+    rng = np.random.default_rng(10)
+    sizes = [1, 0, 255, 256, 257, 2048, 5000, 3, 2049]
+    wd = [0.1, 0.0, 0.3, 0.0, 0.1, 0.01, 0.0, 1.0, 0.1]
+    copies = grad == "bf16"
+    s = _adam_state(rng, sizes, eight, DT[grad], copies, shift)
+    opt = _make(cl, s, wd, eight, copies)
+    hyper = dict(lr=1e-2, beta1=0.9, beta2=0.95, eps=1e-6, grad_scale=0.5)
+    for step in (1, 2, 1000):
+        before = _clone(s)
+        opt.step(step=step, seed=2 ** 63 + 11, **hyper)
+        torch.cuda.synchronize()
+        _check_step(before, s, wd, eight, copies, hyper, step, 2 ** 63 + 11)
+    opt.close()
+
+
+def test_adamw_blocks_with_nothing_in_them_tiny_values_and_nan(cl):
+    rng = np.random.default_rng(11)
+    s = _adam_state(rng, [256 * 5 + 7], True, torch.float32, False)
+    g = s["g"][0]
+    s["m"][0].view(torch.uint8).zero_(); s["v"][0].view(torch.uint8).zero_()
+    s["ms"][0].zero_(); s["vs"][0].zero_()
+    g[:256] = 0.0                                  # nothing at all
+    g[256:512] = 1e-38                             # squares vanish, magnitudes below the smallest scale
+    g[512:768] *= 1e-15                            # (their squares are still above zero in fp32)
+    g[512] = 3.0                                   # one large value: the others' codes round to 0 or 1
+    g[800] = float("nan")                          # stays in its block
+    before = _clone(s)
+    opt = _make(cl, s, [0.0], True, False)
+    hyper = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8)
+    opt.step(step=1, seed=5, **hyper)
+    codes_v, m, p = _codes(s["v"][0]), s["m"][0].float(), s["p"][0]
+    assert np.all(codes_v[:512] == 0) and float(s["vs"][0][0]) == 0.0 and float(s["vs"][0][1]) == 0.0
+    assert np.all(codes_v[513:768] >= 1)           # a root that is not zero is not stored as zero
+    nan = torch.isnan(p).cpu().numpy()
+    assert nan.sum() == 1 and nan[800]
+    assert torch.isnan(m[768:1024]).all() and not torch.isnan(m[1024:]).any() and not torch.isnan(m[:768]).any()
+    keep = [k for k in range(256 * 5 + 7) if not 768 <= k < 1024]
+    want = ref.adamw(before["p"][0].cpu().numpy(), before["g"][0].cpu().numpy(), _codes(before["m"][0]), _codes(before["v"][0]),
+                     m_scale=before["ms"][0].cpu().numpy(), v_scale=before["vs"][0].cpu().numpy(), step=1, weight_decay=0.0, seed=5, **hyper)
+    assert np.array_equal(_codes(s["m"][0])[keep], want[1][keep]) and np.array_equal(codes_v[keep], want[2][keep])
+    assert np.array_equal(p.cpu().numpy()[keep], want[0][keep])
+
+
+def test_adamw_8_bit_states_follow_a_change_of_the_gradients(cl):
+    """Nearest rounding would leave v where it is; stochastic codes follow on average: after the gradients shrink to a
+    third for 1500 steps the mean of v is within 10 % of the 32-bit state's."""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    n = 1 << 16
+    z = lambda dt=torch.float32: torch.zeros(n, dtype=dt, device=_dev())  # noqa: E731
+    p8, p32, g = z(), z(), z()
+    m32, v32 = z(), z()
+    m8, v8 = z(torch.uint8).view(torch.float8_e4m3fn), z(torch.uint8).view(torch.float8_e4m3fn)
+    ms, vs = torch.zeros(n // 256, device=_dev()), torch.zeros(n // 256, device=_dev())
+    a = cl.AdamW([p8], [g], [m8], [v8], m_scales=[ms], v_scales=[vs])
+    b = cl.AdamW([p32], [g], [m32], [v32])
+    for t in range(1, 2001):
+        g.normal_(generator=gen)
+        g.mul_(1.0 if t <= 500 else 1 / 3)
+        a.step(step=t, lr=1e-3, seed=3)
+        b.step(step=t, lr=1e-3)
+    v = (v8.float().view(-1, 256) * vs[:, None]).square().mean()
+    assert abs(float(v / v32.mean()) - 1) < 0.1
+    m = m8.float().view(-1, 256) * ms[:, None]
+    assert float((m.view(-1) - m32).norm() / m32.norm()) < 0.2 and abs(float(m.mean() - m32.mean())) < 1e-3
+
+
+def test_adamw_other_gradients_other_stream_and_refusals(cl):
+    rng = np.random.default_rng(12)
+    s = _adam_state(rng, [1000, 300], False, torch.float32, False)
+    other = [t * 2 for t in s["g"]]
+    hyper = dict(lr=1e-2, beta1=0.9, beta2=0.95, eps=1e-6)
+    opt = _make(cl, s, [0.0, 0.1], False, False)
+    before = _clone(s)
+    before["g"] = [t.clone() for t in other]
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    opt.set_grads(other, stream=side)
+    opt.step(step=3, stream=side, **hyper)
+    side.synchronize()
+    _check_step(before, s, [0.0, 0.1], False, False, hyper, 3, 0)
+    for bad in (dict(beta1=1.0), dict(beta2=-0.1), dict(eps=-1.0), dict(lr=float("nan")), dict(grad_scale=float("inf"))):
+        with pytest.raises(cl.CleaveError) as e:
+            opt.step(step=1, **{**hyper, **bad})
+        assert e.value.code == -1
+    with pytest.raises(ValueError):
+        opt.step(step=0, **hyper)
+    with pytest.raises(ValueError):
+        opt.set_grads(other[:1])
+    with pytest.raises(ValueError):
+        cl.AdamW(s["p"], [t.to(torch.bfloat16) for t in s["g"][:1]] + s["g"][1:], s["m"], s["v"])
+    empty = torch.zeros(0, device=_dev())
+    cl.AdamW([empty], [empty], [empty], [empty]).step(step=1, lr=1.0)            # nothing to do
+
+
+# ---- norm -----------------------------------------------------------------------------------------------
+NORM_SIZES = [(1, 1), (3, 7), (5, 8), (1, 4096), (33, 771), (4, 5120), (2, 16384), (2, 20001), (300, 64), (7, 1000), (2, 32768)]
+
+
+@pytest.mark.parametrize("rows,cols", NORM_SIZES)
+@pytest.mark.parametrize("x,res,y", [("bf16", "bf16", "bf16"), ("f32", None, "f32"), ("bf16", "f32", "e4m3"), ("f32", "bf16", "e4m3"), ("bf16", None, "bf16")])
+def test_rmsnorm(cl, rows, cols, x, res, y):
+    rng = np.random.default_rng(rows * 7 + cols)
+    for pad in (0, 8, 3):
+        xt = _strided(rng, rows, cols, DT[x], pad)
+        rt = _strided(rng, rows, cols, DT[res], pad, 3.0) if res else None
+        w = _rand(rng, cols, torch.float32 if pad == 0 else torch.bfloat16, 0.2) + 1 if pad != 3 else None
+        yt = torch.zeros(rows, cols + pad, dtype=torch.float8_e4m3fn if y == "e4m3" else DT[y], device=_dev())[:, :cols]
+        ht = torch.empty(rows, cols + pad, dtype=DT[res], device=_dev())[:, :cols] if res else None
+        rstd = torch.empty(rows, device=_dev())
+        scale = torch.empty(rows, device=_dev()) if y == "e4m3" else None
+        cl.rmsnorm(xt, w, yt, residual=rt, h=ht, rstd=rstd, scale=scale, eps=1e-5)
+        h64, y64, r64 = ref.rmsnorm(_f64(xt), _f64(rt), _f64(w), 1e-5)
+        _close(rstd, r64, SUM * r64, "rstd")
+        if res:
+            _close(ht, h64, U * np.abs(h64), "h")
+        if y == "e4m3":
+            top = np.abs(y64).max(axis=1)
+            _close(scale, top / 448, 2 * SUM * top / 448, "scale")
+            q64 = y64 / _f64(scale)[:, None]
+            err = np.abs(_f64(yt.float()) - q64)
+            assert np.all(err <= 0.5 * ref.e4m3_step(q64) * (1 + 1e-3) + 2 * SUM * np.abs(q64))
+        else:
+            _close(yt, y64, 2 * SUM * np.abs(y64), "y")
+
+
+def test_rmsnorm_in_place_zero_rows_nan_infinity_and_streams(cl):
+    rng = np.random.default_rng(20)
+    for cols in (512, 771):
+        x, r = _rand(rng, (6, cols), torch.bfloat16), _rand(rng, (6, cols), torch.float32)
+        x[2] = 0; r[2] = 0                                  # a row of zeros
+        x[3, 5] = float("nan")
+        x[4, 7] = float("inf")
+        h64, y64, _ = ref.rmsnorm(_f64(x), _f64(r), None, 1e-5)
+        fresh_h, y0, y1 = torch.empty_like(r), torch.empty_like(x), torch.empty_like(x)
+        s0, q0 = torch.empty(6, device=_dev()), torch.zeros(6, cols, dtype=torch.float8_e4m3fn, device=_dev())
+        cl.rmsnorm(x, None, y0, residual=r, h=fresh_h)
+        cl.rmsnorm(x, None, q0, residual=r, scale=s0)
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        cl.rmsnorm(x, None, y1, residual=r, h=r, stream=side)            # the sum replaces the residual
+        side.synchronize()
+        assert torch.equal(y0.view(torch.int16), y1.view(torch.int16)) and torch.equal(fresh_h.view(torch.int32), r.view(torch.int32))
+        assert torch.all(y0[2] == 0) and float(s0[2]) == 0 and torch.all(q0[2].float() == 0)
+        assert torch.isnan(y0[3]).all() and torch.isnan(s0[3])
+        other = [c for c in range(cols) if c != 7]
+        assert torch.isnan(y0[4, 7]) and torch.all(y0[4, other] == 0) and torch.isnan(s0[4])
+        for i in (0, 1, 5):
+            _close(y0[i:i + 1], y64[i:i + 1], 2 * SUM * np.abs(y64[i:i + 1]), f"row {i}")
+    e = torch.empty(0, 8, dtype=torch.bfloat16, device=_dev())
+    cl.rmsnorm(e, None, e.clone())
+    big = torch.full((2, 256), 3e38, device=_dev())                       # h^2 overflows: rstd 0, y 0
+    out = torch.empty_like(big)
+    cl.rmsnorm(big, None, out)
+    assert torch.all(out == 0)
+
+
+@pytest.mark.parametrize("cols", [1, 8, 250, 4096, 20001])
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_quantize_rows(cl, cols, dt):
+    rng = np.random.default_rng(21)
+    x = _rand(rng, (9, cols), DT[dt], 0.02)
+    x[4] = 0
+    q, s = torch.zeros(9, cols, dtype=torch.float8_e4m3fn, device=_dev()), torch.empty(9, device=_dev())
+    cl.quantize_rows(x, q, s)
+    x64 = _f64(x)
+    _close(s, np.abs(x64).max(axis=1) / 448, 2 * U * np.abs(x64).max(axis=1) / 448, "scale")
+    live = np.arange(9) != 4
+    q64 = x64[live] / _f64(s)[live][:, None]
+    assert np.all(np.abs(_f64(q.float())[live] - q64) <= 0.5 * ref.e4m3_step(q64) * (1 + 1e-3) + 4 * U * np.abs(q64))
+    assert float(s[4]) == 0 and torch.all(q[4].float() == 0)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 4096), (5, 7), (400, 64), (33, 771), (1000, 1000), (6, 20001), (310, 5120), (3, 16384)])
+@pytest.mark.parametrize("h,dy", [("bf16", "bf16"), ("f32", "f32"), ("f32", "bf16"), ("bf16", "f32")])
+def test_rmsnorm_backward(cl, rows, cols, h, dy):
+    rng = np.random.default_rng(rows + cols)
+    for pad in (0, 8, 1):
+        ht, dyt = _strided(rng, rows, cols, DT[h], pad, 3.0), _strided(rng, rows, cols, DT[dy], pad)
+        w = _rand(rng, cols, torch.float32 if pad == 0 else torch.bfloat16, 0.2) + 1 if pad != 1 else None
+        dres = _strided(rng, rows, cols, DT[h], pad) if pad != 8 else None
+        rstd = torch.rsqrt(ht.float().square().mean(1) + 1e-5)
+        dx, dw = torch.empty(rows, cols + pad, dtype=DT[h], device=_dev())[:, :cols], torch.full((cols,), float("nan"), device=_dev())
+        cl.rmsnorm_backward(dyt, ht, w, rstd, dx, dw, dres=dres)
+        a = [_f64(t) for t in (dyt, ht, w, rstd, dres)]
+        dx64, dw64 = ref.rmsnorm_backward(*a)
+        q = np.abs(a[0] if a[2] is None else a[0] * a[2])
+        xh = np.abs(a[1] * a[3][:, None])
+        size = a[3][:, None] * (q + xh * np.mean(q * xh, axis=1, keepdims=True)) + (0 if dres is None else np.abs(a[4]))
+        _close(dx, dx64, SUM * size, "dx")
+        _close(dw, dw64, SUM * np.sum(np.abs(a[0]) * xh, axis=0), "dw")
+        again, dx2 = torch.empty_like(dw), dx if dres is None else dres
+        cl.rmsnorm_backward(dyt, ht, w, rstd, dx2, again, dres=dres)     # in place over dres; the same bits again
+        assert torch.equal(again.view(torch.int32), dw.view(torch.int32)) and torch.equal(dx2, dx)
+
+
+def test_rmsnorm_backward_without_rows_or_without_dw(cl):
+    e = torch.empty(0, 40, device=_dev())
+    dw = torch.ones(40, device=_dev())
+    cl.rmsnorm_backward(e, e, None, torch.empty(0, device=_dev()), e, dw)
+    assert torch.all(dw == 0)
+    rng = np.random.default_rng(30)
+    h, dy = _rand(rng, (9, 40), torch.float32), _rand(rng, (9, 40), torch.float32)
+    rstd = torch.rsqrt(h.square().mean(1) + 1e-5)
+    a, b = torch.empty_like(h), torch.empty_like(h)
+    cl.rmsnorm_backward(dy, h, None, rstd, a, None)
+    ws = torch.empty(cl.rmsnorm_backward_workspace(9, 40), dtype=torch.uint8, device=_dev())
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    cl.rmsnorm_backward(dy, h, None, rstd, b, dw, workspace=ws, stream=side)
+    side.synchronize()
+    assert torch.equal(a, b)
+    with pytest.raises(ValueError):
+        cl.rmsnorm_backward(dy, h, None, rstd, a, dw, workspace=ws[:8])
+
+
+# ---- product with an epilogue -------------------------------------------------------------------------------
+def _operands(rng, m, n, k, ta, tb, kind, pad, integer=True):
+    """Stored A and B (rows a multiple of 16 elements apart) and their fp64 views as the product sees them."""
+    dt = torch.float8_e4m3fn if kind == "e4m3" else torch.bfloat16
+
+    def store(rows, cols):
+        ld = -(-cols // 16) * 16 + pad
+        v = rng.integers(-4, 5, size=(rows, ld)) if integer else rng.normal(size=(rows, ld))
+        return torch.tensor(v, dtype=torch.float32).to(dt).to(_dev())[:, :cols]
+    A, B = store(k, m) if ta else store(m, k), store(n, k) if tb else store(k, n)
+    a, b = _f64(A.float()), _f64(B.float())
+    return A, B, (a.T if ta else a), (b.T if tb else b)
+
+
+LAYOUTS = [(False, False, "bf16"), (False, True, "bf16"), (True, False, "bf16"), (True, True, "bf16"), (False, True, "e4m3")]
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 4096, 512), (16, 512, 4096), (128, 128, 64), (129, 257, 65), (77, 33, 200), (300, 520, 1000),
+                                   (8, 136, 3000), (260, 24, 72), (640, 1000, 130), (1, 8, 16384), (513, 769, 385)])
+@pytest.mark.parametrize("ta,tb,kind", LAYOUTS)
+def test_linear_integer_products_are_exact(cl, m, n, k, ta, tb, kind):
+    """Integers in -4..4: every fp32 sum is exact, so every value has to be equal, in every layout and size."""
+    rng = np.random.default_rng(m + n + k)
+    A, B, a, b = _operands(rng, m, n, k, ta, tb, kind, 16 if m % 2 else 0)
+    out = torch.full((m, n), float("nan"), device=_dev())
+    cl.linear(A, B, out, transA=ta, transB=tb)
+    assert cl.linear_status() == 0
+    assert np.array_equal(_f64(out), a @ b)
+    wide = torch.full((m, n + 5), 7.0, device=_dev())                     # padded rows: nothing outside C is written
+    cl.linear(A, B, wide[:, :n], transA=ta, transB=tb, residual=out)
+    assert np.array_equal(_f64(wide[:, :n]), 2 * (a @ b)) and torch.all(wide[:, n:] == 7.0)
+
+
+@pytest.mark.parametrize("act", KINDS)
+@pytest.mark.parametrize("kind,c,side", [("bf16", "bf16", "f32"), ("bf16", "f32", "bf16"), ("e4m3", "bf16", "bf16")])
+@pytest.mark.parametrize("m,n,k", [(1, 72, 256), (200, 300, 320), (130, 129, 70), (16, 2048, 1024), (700, 512, 256)])
+def test_linear_epilogue(cl, act, kind, c, side, m, n, k):
+    rng = np.random.default_rng(m * n + k)
+    A, B, a, b = _operands(rng, m, n, k, False, True, kind, 0, integer=False)
+    sa = torch.tensor(rng.uniform(0.5, 1.5, size=m), dtype=torch.float32).to(_dev()) if kind == "e4m3" else None
+    sb = torch.tensor(rng.uniform(0.02, 0.06, size=n), dtype=torch.float32).to(_dev())
+    bias = _rand(rng, n, DT[side])
+    mul, res = _rand(rng, (m, n), DT[side]), _rand(rng, (m, n), DT[c])
+    z = torch.empty(m, n, dtype=DT[side], device=_dev())
+    out = res.clone()
+    for gate, add in ((mul, True), (None, True), (mul, False), (None, False)):
+        out.copy_(res)
+        cl.linear(A, B, out, transB=True, scale_a=sa, scale_b=sb, bias=bias, act=act, z=z, mul=gate, residual=out if add else None)
+        assert cl.linear_status() == 0
+        c64, z64 = ref.linear(a, b, scale_a=_f64(sa), scale_b=_f64(sb), bias=_f64(bias), kind=act, mul=_f64(gate), res=_f64(res) if add else None)
+        # the products' terms in fp32, and the scales' and the bias's roundings
+        size = (np.abs(a) @ np.abs(b)) * (1 if sa is None else _f64(sa)[:, None]) * _f64(sb) + np.abs(_f64(bias))
+        zerr = SUM * size
+        _close(z, z64, zerr, "z")
+        # a slope of at most 1.13, then a few units of the activation's own arithmetic (its exponential's argument
+        # is rounded at its own size)
+        cerr = 1.13 * zerr + 32 * U * (1 + np.abs(z64)) * np.abs(z64)
+        cerr = cerr if gate is None else cerr * np.abs(_f64(gate))
+        _close(out, c64, cerr + 2 * U * (np.abs(c64) + (np.abs(_f64(res)) if add else 0)), "C")
+
+
+def test_linear_nan_and_infinity_stay_in_their_rows_and_columns(cl):
+    rng = np.random.default_rng(40)
+    for m, n, k in ((150, 200, 128), (700, 600, 256)):
+        A, B, a, b = _operands(rng, m, n, k, False, False, "bf16", 0)
+        A[3, 5] = float("nan")
+        B[7, 11] = float("inf")
+        out = torch.empty(m, n, device=_dev())
+        cl.linear(A, B, out)
+        g = _f64(out)
+        rows, cols = np.arange(m) != 3, np.arange(n) != 11
+        assert np.isnan(g[3]).all() and np.array_equal(g[np.ix_(rows, cols)], (a @ b)[np.ix_(rows, cols)])
+        assert not np.isfinite(g[rows][:, 11]).any()
+
+
+def test_linear_extreme_preactivations(cl):
+    """Activations far out on either side: their limits, no NaN."""
+    n = 64
+    bias = torch.linspace(-1e4, 1e4, n, device=_dev())
+    bias[0], bias[-1] = -1e30, 1e30
+    A, B = torch.zeros(3, 8, dtype=torch.bfloat16, device=_dev()), torch.zeros(8, n, dtype=torch.bfloat16, device=_dev())
+    for act in ("relu", "gelu", "gelu_tanh", "silu"):
+        out = torch.empty(3, n, device=_dev())
+        cl.linear(A, B, out, bias=bias, act=act)
+        want = torch.clamp_min(bias, 0).expand(3, n)
+        assert torch.allclose(out, want, rtol=1e-6, atol=0), act
+        dz = torch.empty(3, n, device=_dev())
+        cl.act_backward(torch.ones(3, n, device=_dev()), bias.expand(3, n).contiguous(), dz, act=act)
+        assert torch.allclose(dz, (bias > 0).float().expand(3, n), rtol=1e-6, atol=1e-6), act
+
+
+def test_linear_repeats_its_bits_on_any_stream(cl):
+    rng = np.random.default_rng(41)
+    A, B, a, b = _operands(rng, 16, 1024, 4096, False, False, "bf16", 0, integer=False)
+    first, second = torch.empty(16, 1024, device=_dev()), torch.empty(16, 1024, device=_dev())
+    cl.linear(A, B, first)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        cl.linear(A, B, second, stream=side)
+    assert cl.linear_status(side) == 0
+    assert torch.equal(first.view(torch.int32), second.view(torch.int32))
+    e = torch.empty(0, 4096, dtype=torch.bfloat16, device=_dev())
+    cl.linear(e, B, torch.empty(0, 1024, device=_dev()))
+
+
+@pytest.mark.parametrize("m,n,k", [(16, 512, 4096), (3000, 2048, 1024)])
+def test_a_wait_that_runs_out_ends_the_product_in_order(cl, m, n, k):
+    """With a limit of 0 the first wait that is not satisfied at once gives up: the kernel returns, the status says
+    so once, and the next product is right."""
+    rng = np.random.default_rng(42)
+    A, B, a, b = _operands(rng, m, n, k, False, False, "bf16", 0)
+    out = torch.zeros(m, n, device=_dev())
+    assert cl.linear_status() == 0
+    try:
+        cl.ops.lib.cleave_linear_set_wait_limit_ns(0)
+        cl.linear(A, B, out)
+        assert cl.linear_status() == -7
+    finally:
+        cl.ops.lib.cleave_linear_set_wait_limit_ns(2_000_000_000)
+    assert cl.linear_status() == 0
+    cl.linear(A, B, out)
+    assert cl.linear_status() == 0
+    assert np.array_equal(_f64(out), a @ b)
+
+
+# ---- the epilogue's backward ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 4096), (65, 33), (1000, 72), (513, 1001), (64, 512), (5000, 8)])
+@pytest.mark.parametrize("act", KINDS)
+@pytest.mark.parametrize("t", ["bf16", "f32"])
+def test_act_backward(cl, rows, cols, act, t):
+    rng = np.random.default_rng(rows + cols)
+    for pad in (0, 3):
+        dy, z, mul = (_strided(rng, rows, cols, DT[t], pad, s) for s in (1.0, 2.0, 1.0))
+        dz, dmul = (torch.empty(rows, cols + pad, dtype=DT[t], device=_dev())[:, :cols] for _ in range(2))
+        db = torch.full((cols,), float("nan"), device=_dev())
+        for gate in (mul, None):
+            cl.act_backward(dy, z, dz, act=act, mul=gate, dmul=dmul, dbias=db)
+            y64, z64, g64 = _f64(dy), _f64(z), _f64(gate)
+            dz64, dmul64, db64 = ref.act_backward(y64, z64, act, g64)
+            # the exponential's argument is rounded at its own size (up to 2 |z| (1 + z^2 / 20)); slopes are at most 1.13
+            own = 32 * U * (1 + np.abs(z64)) ** 2 * np.abs(y64)
+            err = own if gate is None else own * np.abs(g64)
+            _close(dz, dz64, err, "dz")
+            _close(dmul, dmul64, own * np.abs(z64), "dmul")
+            _close(db, db64, err.sum(axis=0) + SUM * np.abs(dz64).sum(axis=0), "dbias")
+        again = torch.empty_like(db)
+        cl.act_backward(dy, z, None, act=act, dbias=again)                 # the bias gradient alone, the same bits
+        assert torch.equal(again.view(torch.int32), db.view(torch.int32))
+        kept = dz.clone()
+        cl.act_backward(dy, z, z, act=act)                                 # over z's buffer
+        assert torch.equal(z, kept)
+
+
+def test_act_backward_without_rows_and_plain_column_sums(cl):
+    e = torch.empty(0, 24, device=_dev())
+    db = torch.ones(24, device=_dev())
+    cl.act_backward(e, None, dbias=db)
+    assert torch.all(db == 0)
+    dy = torch.tensor(np.random.default_rng(50).integers(-8, 9, size=(2000, 24)), dtype=torch.float32).to(_dev())
+    cl.act_backward(dy, None, dbias=db)
+    assert torch.equal(db, dy.sum(0))                                       # integers: exact in any order
+    ws = torch.empty(cl.act_backward_workspace(2000, 24), dtype=torch.uint8, device=_dev())
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    cl.act_backward(dy, None, dbias=db, workspace=ws, stream=side)
+    side.synchronize()
+    assert torch.equal(db, dy.sum(0))
+    with pytest.raises(ValueError):
+        cl.act_backward(dy, None, dbias=db, workspace=ws[:16])

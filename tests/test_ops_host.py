@@ -1,0 +1,166 @@
+"""Host side of the operators around the GEMMs, no GPU: struct layouts, workspace sizes, and the refusals, which come
+before anything touches a device (the addresses below are never dereferenced)."""
+import ctypes
+import os
+import subprocess
+
+import pytest
+import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+INVAL, UNSUPPORTED, CUDA = -1, -2, -6
+
+
+@pytest.fixture(scope="module")
+def ops():
+    import paper_2512_22142_b200 as cl
+    return cl.ops
+
+
+def test_struct_layouts_match_the_header(ops, tmp_path):
+    names = {"adamw_tensor": ops._AdamwTensor, "adamw_step": ops._AdamwStep, "rmsnorm": ops._Rmsnorm, "rmsnorm_backward": ops._RmsnormBackward,
+             "linear": ops._Linear, "act_backward": ops._ActBackward}
+    lines = []
+    for name, cls in names.items():
+        lines.append(f'printf("%zu\\n", sizeof(cleave_{name}_t));')
+        lines += [f'printf("%zu\\n", offsetof(cleave_{name}_t, {f[0]}));' for f in cls._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "cleave.h"\nint main(void) {' + "".join(lines) + "return 0; }\n")
+    exe = tmp_path / "layout"
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    want = []
+    for cls in names.values():
+        want.append(ctypes.sizeof(cls))
+        want += [getattr(cls, f[0]).offset for f in cls._fields_]
+    assert got == want
+
+
+def _refused(rc, code=INVAL):
+    assert rc == code
+
+
+def _norm(ops, **kw):
+    d = ops._Rmsnorm()
+    base = dict(rows=4, cols=8, eps=1e-5, x_type=1, x=4096, ldx=8, y_type=1, y=8192, ldy=8)
+    for k, v in {**base, **kw}.items():
+        setattr(d, k, v)
+    return ops.lib.cleave_rmsnorm(ctypes.byref(d), None)
+
+
+@pytest.mark.parametrize("kw", [dict(cols=0), dict(x=None), dict(x_type=0), dict(x_type=3), dict(ldx=7), dict(x=4097), dict(y_type=3),
+                                dict(scale=4096), dict(y_type=3, scale=4097), dict(h=4096, ldh=8), dict(r=4096), dict(r_type=1, r=4096, ldr=4),
+                                dict(r_type=2, r=4098, ldr=8), dict(w=4096), dict(w_type=3, w=4096), dict(rstd=4098), dict(eps=-1.0),
+                                dict(eps=float("nan")), dict(y=None), dict(ldy=1 << 41), dict(r_type=1, r=4096, ldr=8, h=4097, ldh=8)])
+def test_rmsnorm_refuses(ops, kw):
+    _refused(_norm(ops, **kw))
+
+
+def test_rmsnorm_limits(ops):
+    assert _norm(ops, rows=0, x=None, y=None) == 0
+    _refused(_norm(ops, rows=1 << 31), UNSUPPORTED)
+    assert ops.lib.cleave_rmsnorm(None, None) == INVAL
+
+
+def _norm_bwd(ops, ws=4096, **kw):
+    d = ops._RmsnormBackward()
+    base = dict(rows=4, cols=8, dy_type=1, dy=4096, lddy=8, h_type=1, h=8192, ldh=8, rstd=4096, dx=16384, lddx=8, dw=4096)
+    for k, v in {**base, **kw}.items():
+        setattr(d, k, v)
+    return ops.lib.cleave_rmsnorm_backward(ctypes.byref(d), ws, None)
+
+
+@pytest.mark.parametrize("kw", [dict(cols=0), dict(dy=None), dict(dy_type=3), dict(lddy=4), dict(h_type=0), dict(h=8193), dict(dx=None), dict(lddx=7),
+                                dict(rstd=None), dict(rstd=4098), dict(ws=None), dict(ws=4100), dict(dres=4097, lddres=8), dict(dres=4096, lddres=2),
+                                dict(dw=4098), dict(w=4096)])
+def test_rmsnorm_backward_refuses(ops, kw):
+    _refused(_norm_bwd(ops, **kw))
+
+
+def _linear(ops, **kw):
+    d = ops._Linear()
+    base = dict(in_type=1, c_type=1, A=4096, B=8192, C=16384, ldc=32)
+    g = dict(M=8, N=32, K=64, lda=64, ldb=32, transA=0, transB=0)
+    for k, v in {**base, **kw}.items():
+        if k in g:
+            g[k] = v
+        else:
+            setattr(d, k, v)
+    for k, v in g.items():
+        setattr(d.g, k, v)
+    return ops.lib.cleave_linear(ctypes.byref(d), None)
+
+
+@pytest.mark.parametrize("kw", [dict(N=0), dict(K=0), dict(in_type=2), dict(in_type=0), dict(c_type=3), dict(c_type=0), dict(act=5), dict(A=None),
+                                dict(A=4104), dict(B=8200), dict(lda=60), dict(lda=56), dict(ldb=24), dict(transB=1), dict(transA=2), dict(C=None), dict(ldc=31),
+                                dict(C=16385), dict(bias=4096), dict(bias_type=1, bias=4097), dict(z_type=2, z=4096, ldz=16), dict(mul_type=3, mul=4096, ldmul=32),
+                                dict(res_type=1, ldres=32), dict(scale_a=4098), dict(scale_b=4097), dict(M=1 << 31)])
+def test_linear_refuses(ops, kw):
+    _refused(_linear(ops, **kw))
+
+
+def test_linear_limits(ops):
+    assert _linear(ops, M=0, A=None, C=None) == 0
+    _refused(_linear(ops, in_type=3), UNSUPPORTED)                                   # E4M3 needs both operands K-contiguous
+    _refused(_linear(ops, in_type=3, transB=1, ldb=72))                              # 16-byte rows
+
+
+def _act(ops, ws=4096, **kw):
+    d = ops._ActBackward()
+    base = dict(rows=4, cols=8, act=2, dy_type=1, dy=4096, lddy=8, z_type=1, z=8192, ldz=8, dz_type=1, dz=16384, lddz=8, dbias=4096)
+    for k, v in {**base, **kw}.items():
+        setattr(d, k, v)
+    return ops.lib.cleave_act_backward(ctypes.byref(d), ws, None)
+
+
+@pytest.mark.parametrize("kw", [dict(cols=0), dict(act=9), dict(dy=None), dict(dy_type=3), dict(lddy=7), dict(z=None), dict(z_type=0, z=None), dict(ldz=1),
+                                dict(dz_type=0), dict(dz=16385), dict(mul_type=1), dict(dmul_type=1, dmul=4096), dict(ws=None), dict(ws=4104), dict(dbias=4097),
+                                dict(act=0, z_type=0, z=None, dmul_type=1, dmul=4096, lddmul=8)])
+def test_act_backward_refuses(ops, kw):
+    _refused(_act(ops, **kw))
+
+
+def _create(ops, n=1, state=2, grad=2, **kw):
+    t = (ops._AdamwTensor * 1)()
+    base = dict(numel=512, p=4096, g=8192, m=16384, v=32768)
+    for k, v in {**base, **kw}.items():
+        setattr(t[0], k, v)
+    h = ctypes.c_void_p()
+    rc = ops.lib.cleave_adamw_create(t, n, state, grad, ctypes.byref(h))
+    assert rc != 0 and not h.value
+    return rc
+
+
+@pytest.mark.parametrize("kw", [dict(n=0), dict(state=1), dict(state=0), dict(grad=3), dict(grad=0), dict(p=None), dict(p=4098), dict(g=None), dict(g=8193),
+                                dict(m=None), dict(v=32770), dict(w=4097), dict(numel=1 << 41), dict(weight_decay=float("nan")),
+                                dict(state=3), dict(state=3, m_scale=4096), dict(state=3, m_scale=4096, v_scale=4098), dict(m_scale=4096, v_scale=4096)])
+def test_adamw_refuses(ops, kw):
+    _refused(_create(ops, **kw))
+
+
+def test_adamw_step_refuses_a_missing_handle(ops):
+    s = ops._AdamwStep()
+    assert ops.lib.cleave_adamw_step(None, ctypes.byref(s), None) == INVAL
+    assert ops.lib.cleave_adamw_set_grads(None, None, None) == INVAL
+    ops.lib.cleave_adamw_destroy(None)
+
+
+@pytest.mark.skipif(torch.cuda.is_available(), reason="what a machine without a GPU answers")
+def test_without_a_device_the_calls_say_so(ops):
+    assert _norm(ops) == CUDA and _norm_bwd(ops) == CUDA and _linear(ops) == CUDA and _act(ops) == CUDA and _create(ops) == CUDA
+
+
+def test_workspaces(ops):
+    for fn in (ops.rmsnorm_backward_workspace, ops.act_backward_workspace):
+        assert fn(0, 100) == 0 and fn(1, 100) >= 400
+        assert fn(1 << 31, 100) <= 100 * 4 * 4096              # bounded: partial sums, not rows
+
+
+def test_binding_refuses_what_the_library_cannot_see(ops):
+    x = torch.zeros(4, 8, dtype=torch.bfloat16)
+    w = torch.zeros(8)
+    for call in (lambda: ops.rmsnorm(x, w, x), lambda: ops.rmsnorm(x[0], w, x), lambda: ops.linear(x, x, x, transB=True),
+                 lambda: ops.act_backward(x, x, x, act="relu"), lambda: ops.quantize_rows(x, x, w), lambda: ops.rmsnorm_backward(x, x, w, w, x),
+                 lambda: ops.AdamW([], [], [], []), lambda: ops.AdamW([w], [w], [w], [w]), lambda: ops.AdamW([w], [x], [x], [w])):
+        with pytest.raises(ValueError):
+            call()
