@@ -34,7 +34,7 @@ def build_library(force: bool = False, verbose: bool = False) -> str:
         return LIB_PATH
     os.makedirs(LIB_DIR, exist_ok=True)
     cmd = [_nvcc(), "-std=c++17", "-O3", "-lineinfo", "-gencode", "arch=compute_100a,code=sm_100a",
-           "-shared", "-Xcompiler", "-fPIC,-fvisibility=hidden", "-cudart", "static",
+           "--threads", "0", "-shared", "-Xcompiler", "-fPIC,-fvisibility=hidden", "-cudart", "static",
            "-I", os.path.join(ROOT, "include"), "-I", CSRC, "-o", LIB_PATH]
     if verbose:
         cmd += ["-Xptxas", "-v"]

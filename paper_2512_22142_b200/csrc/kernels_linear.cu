@@ -327,19 +327,9 @@ int encode_operand(CUtensorMap* out, const void* base, uint64_t rows, uint64_t c
 
 bool wide16(const void* p, uint64_t ld, uint32_t type) { return ((uintptr_t)p & 15) == 0 && (ld * type_bytes(type)) % 16 == 0; }
 
-// SM count of the current device, or a negative CLEAVE_E_* code
-int sm_count() {
-    int dev = 0, n = 0, major = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
-        cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
-    return major == 10 ? n : CLEAVE_E_UNSUPPORTED;
-}
-
 }  // namespace
 
-int launch_linear(const cleave_linear_t& d, cudaStream_t st) {
-    const int sms = sm_count();
-    if (sms < 0) return sms;
+int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     const bool e4m3 = d.in_type == CLEAVE_T_E4M3;
     const cleave_gemm_t& g = d.g;
     LinearParams P = {};
@@ -367,7 +357,8 @@ int launch_linear(const cleave_linear_t& d, cudaStream_t st) {
     while (P.splits < 8 && tiles * P.splits * 2 <= 2u * (uint32_t)sms && P.K_blocks / (P.splits * 2) >= 4) P.splits *= 2;
     if (tiles * P.splits > 0x7FFFFFFFull) return CLEAVE_E_UNSUPPORTED;
     auto kernel = e4m3 ? linear_split_kernel<true> : linear_split_kernel<false>;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+    static SmemLimit limit[2];
+    if (limit[e4m3 ? 1 : 0].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(tiles * P.splits));
     cfg.blockDim = dim3(kLinThreads);

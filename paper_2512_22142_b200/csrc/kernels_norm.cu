@@ -1,15 +1,40 @@
 // Root-mean-square norm with the residual's addition, its backward pass, and rows in 8 bits (see cleave.h).
+//
+// All of it is bound by the HBM's bandwidth: each row is read once, kept in registers while its statistics are
+// formed, and written once.  Two forms of each pass:
+//   wide   rows of whole 16-byte groups: a thread owns groups of 8 columns.  Up to 1024 columns a warp takes a row
+//          (no barrier, rows in flight by occupancy); above, a CTA takes a row, the next rows come by cp.async
+//          into a ring in shared memory -- each thread copies and reads its own groups only, so the ring needs no
+//          barrier of its own and the bytes in flight do not depend on registers -- and one barrier a row joins
+//          the warps' sums.
+//   any    every other size, stride or alignment: neighbouring threads own neighbouring columns and take them
+//          again in each pass (the row stays in L1 / L2).
 #include "ops.cuh"
 
 namespace cleave {
 
 constexpr uint32_t kRowThreads = 256;
 
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    return v;
+}
 // Sum / NaN-keeping maximum over the CTA; every thread receives it.  `buf` holds one value per warp and may be
 // reused after the call (it ends with a barrier).
 __device__ __forceinline__ float cta_sum(float v, float* buf) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    v = warp_sum(v);
     if ((threadIdx.x & 31u) == 0) buf[threadIdx.x >> 5] = v;
     __syncthreads();
     float s = 0.f;
@@ -18,8 +43,7 @@ __device__ __forceinline__ float cta_sum(float v, float* buf) {
     return s;
 }
 __device__ __forceinline__ float cta_max_nan(float v, float* buf) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    v = warp_max(v);
     if ((threadIdx.x & 31u) == 0) buf[threadIdx.x >> 5] = v;
     __syncthreads();
     float s = buf[0];
@@ -34,7 +58,7 @@ __device__ __forceinline__ float2 row_scale(float top) {
     return make_float2(s, s < 0x1p-120f ? 0.f : 1.f / s);
 }
 
-// One CTA per row, any types, sizes and alignments: the row is read again in each pass (it stays in L1 / L2).
+// ---- forward, any shape ------------------------------------------------------------------------------
 template <bool NORM>
 __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_constant__ cleave_rmsnorm_t d) {
     __shared__ float buf[32];
@@ -69,8 +93,217 @@ __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_const
     }
 }
 
-cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, cudaStream_t st) {
+// ---- forward, wide -----------------------------------------------------------------------------------
+struct NoRes {};                    // no residual operand
+template <typename T> struct Bytes8 { static constexpr uint32_t value = sizeof(T) * 8; };
+template <> struct Bytes8<NoRes> { static constexpr uint32_t value = 0; };
+
+__device__ __forceinline__ void load_weight8(const cleave_rmsnorm_t& d, uint32_t col, float (&w)[8]) {
+    if (d.w_type == CLEAVE_T_F32) {
+        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(d.w) + col);
+        const float4 a = __ldg(p), b = __ldg(p + 1);
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+    } else if (d.w_type == CLEAVE_T_BF16) {
+        Raw8<__nv_bfloat16> r;
+        r.w[0] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(d.w) + col));
+        unpack8(r, w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = 1.f;
+    }
+}
+
+// V groups of 8 columns per thread.  WARP: blockDim (32, rows per CTA), a warp per row.  Otherwise a CTA per row
+// and a ring of `stages` rows in shared memory, [stage][operand][group] with a thread's groups blockDim.x apart.
+template <typename X, typename R, typename Y, int V, bool WARP, bool NORM>
+__global__ void __launch_bounds__(WARP ? 256 : 1024) row_wide_kernel(const __grid_constant__ cleave_rmsnorm_t d, uint32_t stages) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float2 parts[2][32];
+    constexpr bool RES = !(sizeof(R) == 1);
+    const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
+    const uint64_t first = WARP ? (uint64_t)blockIdx.x * blockDim.y + threadIdx.y : blockIdx.x;
+    const uint64_t stride = WARP ? (uint64_t)gridDim.x * blockDim.y : gridDim.x;
+    const uint32_t stage_bytes = groups * (Bytes8<X>::value + Bytes8<R>::value);
+    const uint32_t ring_base = (uint32_t)__cvta_generic_to_shared(ring);
+    auto fetch = [&](uint64_t row, uint32_t s) {                 // this thread's groups of a row into stage s
+        if (row < d.rows) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const uint32_t g = tid + v * nt;
+                if (g >= groups) continue;
+                const uint8_t* px = reinterpret_cast<const uint8_t*>(static_cast<const X*>(d.x) + row * d.ldx + g * 8);
+                const uint32_t at = ring_base + s * stage_bytes + g * Bytes8<X>::value;
+#pragma unroll
+                for (uint32_t b = 0; b < Bytes8<X>::value; b += 16) cp_async16(at + b, px + b);
+                if constexpr (RES) {
+                    const uint8_t* pr = reinterpret_cast<const uint8_t*>(static_cast<const R*>(d.r) + row * d.ldr + g * 8);
+                    const uint32_t ar = ring_base + s * stage_bytes + groups * Bytes8<X>::value + g * Bytes8<R>::value;
+#pragma unroll
+                    for (uint32_t b = 0; b < Bytes8<R>::value; b += 16) cp_async16(ar + b, pr + b);
+                }
+            }
+        }
+        cp_async_commit();                                       // (an empty group keeps the count when there is no such row)
+    };
+    if constexpr (!WARP)
+        for (uint32_t s = 0; s < stages; ++s) fetch(first + s * stride, s);
+
+    uint32_t it = 0, s = 0;
+    for (uint64_t row = first; row < d.rows; row += stride, ++it) {
+        float h[V][8];
+        if constexpr (!WARP) {
+            if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t g = tid + v * nt;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[v][i] = 0.f;
+            if (g >= groups) continue;
+            Raw8<X> rx;
+            if constexpr (WARP) rx = load_raw8(static_cast<const X*>(d.x) + row * d.ldx + g * 8);
+            else rx = *reinterpret_cast<const Raw8<X>*>(ring + s * stage_bytes + g * Bytes8<X>::value);
+            unpack8(rx, h[v]);
+            if constexpr (RES) {
+                Raw8<R> rr;
+                float r[8];
+                if constexpr (WARP) rr = load_raw8(static_cast<const R*>(d.r) + row * d.ldr + g * 8);
+                else rr = *reinterpret_cast<const Raw8<R>*>(ring + s * stage_bytes + groups * Bytes8<X>::value + g * Bytes8<R>::value);
+                unpack8(rr, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[v][i] += r[i];
+            }
+        }
+        // one reduction for both statistics: the sum of squares and, for codes, the largest |h w| (times rstd later)
+        float ss = 0.f, top = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t g = tid + v * nt;
+            if (g >= groups) continue;
+            if constexpr (NORM) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) ss = fmaf(h[v][i], h[v][i], ss);
+            }
+            if constexpr (sizeof(Y) == 1) {
+                float w[8];
+                load_weight8(d, g * 8, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(h[v][i] * w[i]));
+            }
+        }
+        if constexpr (NORM) ss = warp_sum(ss);
+        if constexpr (sizeof(Y) == 1) top = warp_max(top);
+        if constexpr (!WARP) {
+            float2* p = parts[it & 1];
+            if ((tid & 31u) == 0) p[tid >> 5] = make_float2(ss, top);
+            __syncthreads();                                     // also: every thread has read stage s
+            fetch(row + (uint64_t)stages * stride, s);
+            s = s + 1 == stages ? 0 : s + 1;
+            float2 q = (tid & 31u) < nt / 32 ? p[tid & 31u] : make_float2(0.f, 0.f);
+            if constexpr (NORM) ss = warp_sum(q.x);
+            if constexpr (sizeof(Y) == 1) top = warp_max(q.y);
+        }
+        float rstd = 1.f;
+        if constexpr (NORM) {
+            rstd = rsqrtf(ss / (float)d.cols + d.eps);
+            if (d.rstd && tid == 0) d.rstd[row] = rstd;
+        }
+        float inv = 1.f;
+        if constexpr (sizeof(Y) == 1) {
+            if (top == INFINITY) {                               // h w overflowed (rows of extreme weights): take h rstd w
+                float t = 0.f;
+#pragma unroll
+                for (int v = 0; v < V; ++v) {
+                    const uint32_t g = tid + v * nt;
+                    if (g >= groups) continue;
+                    float w[8];
+                    load_weight8(d, g * 8, w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) t = max_nan(t, fabsf(h[v][i] * rstd * w[i]));
+                }
+                t = warp_max(t);
+                if constexpr (!WARP) {
+                    float2* p = parts[it & 1];
+                    __syncthreads();
+                    if ((tid & 31u) == 0) p[tid >> 5].y = t;
+                    __syncthreads();
+                    t = warp_max((tid & 31u) < nt / 32 ? p[tid & 31u].y : 0.f);
+                }
+                top = t;
+            } else top *= rstd;
+            const float2 sc = row_scale(top);
+            inv = sc.y;
+            if (tid == 0) d.scale[row] = sc.x;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t g = tid + v * nt;
+            if (g >= groups) continue;
+            if constexpr (RES && NORM) if (d.h) store8(static_cast<R*>(d.h) + row * d.ldh + g * 8, h[v]);
+            float w[8], y[8];
+            load_weight8(d, g * 8, w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = h[v][i] * rstd * w[i] * (sizeof(Y) == 1 ? inv : 1.f);
+            store8(static_cast<Y*>(d.y) + row * d.ldy + g * 8, y);
+        }
+    }
+}
+
+constexpr uint32_t kWarpRowCols = 1024;         // up to here a warp holds a row (four groups a lane)
+constexpr uint32_t kRingBytes = 64 * 1024;      // per CTA; three CTAs an SM at most sizes
+constexpr uint32_t kRingMost = 160 * 1024;
+
+template <typename X, typename R, typename Y, int V, bool WARP, bool NORM>
+cudaError_t launch_row_wide(const cleave_rmsnorm_t& d, uint32_t threads, int sms, cudaStream_t st) {
+    auto kernel = row_wide_kernel<X, R, Y, V, WARP, NORM>;
+    if (WARP) {
+        const uint64_t ctas = (d.rows + 7) / 8;
+        kernel<<<(unsigned)ctas, dim3(32, 8), 0, st>>>(d, 0u);
+        return cudaGetLastError();
+    }
+    const uint32_t stage = d.cols / 8 * (Bytes8<X>::value + Bytes8<R>::value);
+    const uint32_t stages = max(1u, min(4u, kRingBytes / stage)), smem = stage * stages;
+    static SmemLimit limit;
+    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
+    if (e != cudaSuccess) return e;
+    // CTAs that fit an SM by shared memory and threads; each walks the rows in steps of the grid
+    const uint32_t fit = max(1u, min(min(220u * 1024u / (smem + 2048u), 2048u / threads), 4u));
+    const uint64_t ctas = min((uint64_t)d.rows, (uint64_t)sms * fit);
+    kernel<<<(unsigned)ctas, threads, smem, st>>>(d, stages);
+    return cudaGetLastError();
+}
+
+template <typename X, typename R, typename Y, bool NORM>
+cudaError_t launch_row_types(const cleave_rmsnorm_t& d, int sms, cudaStream_t st) {
+    const uint32_t groups = d.cols / 8;
+    if (d.cols <= kWarpRowCols) {
+        if (groups <= 32) return launch_row_wide<X, R, Y, 1, true, NORM>(d, 32, sms, st);
+        if (groups <= 64) return launch_row_wide<X, R, Y, 2, true, NORM>(d, 32, sms, st);
+        return launch_row_wide<X, R, Y, 4, true, NORM>(d, 32, sms, st);
+    }
+    if (groups <= 1024) return launch_row_wide<X, R, Y, 2, false, NORM>(d, (groups + 63) / 64 * 32, sms, st);
+    return launch_row_wide<X, R, Y, 4, false, NORM>(d, (groups + 127) / 128 * 32, sms, st);
+}
+template <typename X, typename R>
+cudaError_t launch_row_out(const cleave_rmsnorm_t& d, bool norm, int sms, cudaStream_t st) {
+    if constexpr (sizeof(R) == 1)
+        if (!norm) return launch_row_types<X, R, uint8_t, false>(d, sms, st);
+    if (d.y_type == CLEAVE_T_E4M3) return launch_row_types<X, R, uint8_t, true>(d, sms, st);
+    if (d.y_type == CLEAVE_T_F32) return launch_row_types<X, R, float, true>(d, sms, st);
+    return launch_row_types<X, R, __nv_bfloat16, true>(d, sms, st);
+}
+template <typename X>
+cudaError_t launch_row_res(const cleave_rmsnorm_t& d, bool norm, int sms, cudaStream_t st) {
+    if (!d.r) return launch_row_out<X, NoRes>(d, norm, sms, st);
+    return d.r_type == CLEAVE_T_F32 ? launch_row_out<X, float>(d, norm, sms, st) : launch_row_out<X, __nv_bfloat16>(d, norm, sms, st);
+}
+
+cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, int sms, cudaStream_t st) {
     if (!d.rows || !d.cols) return cudaSuccess;
+    const uint64_t stage = (uint64_t)d.cols * (type_bytes(d.x_type) + type_bytes(d.r_type));
+    const bool wide = d.cols % 8 == 0 && d.cols <= 32768 && stage <= kRingMost && rows_wide(d.x, d.ldx, d.x_type) && rows_wide(d.y, d.ldy, d.y_type) &&
+                      (!d.r || rows_wide(d.r, d.ldr, d.r_type)) && (!d.h || rows_wide(d.h, d.ldh, d.r_type)) && (!d.w || (uintptr_t)d.w % 16 == 0);
+    if (wide) return d.x_type == CLEAVE_T_F32 ? launch_row_res<float>(d, norm, sms, st) : launch_row_res<__nv_bfloat16>(d, norm, sms, st);
     if (norm) row_any_kernel<true><<<(unsigned)d.rows, kRowThreads, 0, st>>>(d);
     else      row_any_kernel<false><<<(unsigned)d.rows, kRowThreads, 0, st>>>(d);
     return cudaGetLastError();
@@ -108,13 +341,105 @@ __global__ void __launch_bounds__(kRowThreads) rmsnorm_backward_any_kernel(const
     }
 }
 
+// V groups of 8 columns a thread, a CTA per row, a ring of rows of (dy, h, dres) in shared memory; w and the CTA's
+// share of dw stay in registers over all its rows.
+template <typename D, typename H, int V, int T>
+__global__ void __launch_bounds__(T) rmsnorm_backward_wide_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float parts[2][32];
+    constexpr uint32_t BD = Bytes8<D>::value, BH = Bytes8<H>::value;
+    const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
+    const bool res = d.dres != nullptr;
+    const uint32_t off_h = groups * BD, off_res = off_h + groups * BH, stage_bytes = off_res + (res ? groups * BH : 0u);
+    const uint32_t ring_base = (uint32_t)__cvta_generic_to_shared(ring);
+    auto fetch = [&](uint64_t row, uint32_t s) {
+        if (row < d.rows) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const uint32_t g = tid + v * nt;
+                if (g >= groups) continue;
+                const uint32_t at = ring_base + s * stage_bytes;
+                const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + row * d.lddy + g * 8);
+                const uint8_t* ph = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.h) + row * d.ldh + g * 8);
+#pragma unroll
+                for (uint32_t b = 0; b < BD; b += 16) cp_async16(at + g * BD + b, pd + b);
+#pragma unroll
+                for (uint32_t b = 0; b < BH; b += 16) cp_async16(at + off_h + g * BH + b, ph + b);
+                if (res) {
+                    const uint8_t* pr = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.dres) + row * d.lddres + g * 8);
+#pragma unroll
+                    for (uint32_t b = 0; b < BH; b += 16) cp_async16(at + off_res + g * BH + b, pr + b);
+                }
+            }
+        }
+        cp_async_commit();
+    };
+    for (uint32_t s = 0; s < stages; ++s) fetch(blockIdx.x + (uint64_t)s * gridDim.x, s);
+    float w[V][8], dw[V][8];
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const uint32_t g = tid + v * nt;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) { dw[v][i] = 0.f; w[v][i] = d.w && g < groups ? load_as(d.w, d.w_type, g * 8 + i) : 1.f; }
+    }
+    uint32_t it = 0, s = 0;
+    for (uint64_t row = blockIdx.x; row < d.rows; row += gridDim.x, ++it) {
+        if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
+        const float rstd = __ldg(d.rstd + row);
+        const uint8_t* stage = ring + s * stage_bytes;
+        float q[V][8], xh[V][8], dot = 0.f;
+        Raw8<H> rr[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t g = tid + v * nt;
+            if (g >= groups) continue;
+            unpack8(*reinterpret_cast<const Raw8<D>*>(stage + g * BD), q[v]);
+            unpack8(*reinterpret_cast<const Raw8<H>*>(stage + off_h + g * BH), xh[v]);
+            if (res) rr[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_res + g * BH);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                xh[v][i] *= rstd;
+                dw[v][i] = fmaf(q[v][i], xh[v][i], dw[v][i]);
+                q[v][i] *= w[v][i];
+                dot = fmaf(q[v][i], xh[v][i], dot);
+            }
+        }
+        dot = warp_sum(dot);
+        float* p = parts[it & 1];
+        if ((tid & 31u) == 0) p[tid >> 5] = dot;
+        __syncthreads();                                         // also: every thread has read stage s
+        fetch(row + (uint64_t)stages * gridDim.x, s);
+        s = s + 1 == stages ? 0 : s + 1;
+        const float mean = warp_sum((tid & 31u) < nt / 32 ? p[tid & 31u] : 0.f) / (float)d.cols;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t g = tid + v * nt;
+            if (g >= groups) continue;
+            float dx[8], r[8];
+            if (res) unpack8(rr[v], r);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dx[i] = rstd * (q[v][i] - xh[v][i] * mean) + (res ? r[i] : 0.f);
+            store8(static_cast<H*>(d.dx) + row * d.lddx + g * 8, dx);
+        }
+    }
+    if (d.dw)
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const uint32_t g = tid + v * nt;
+            if (g < groups) store8(ws + (uint64_t)blockIdx.x * d.cols + g * 8, dw[v]);
+        }
+}
+
 // out[j] = sum over the parts of ws[part][j], in a fixed order.  32 columns per CTA; warp w adds the parts
 // w, w + 8, ... and the eight sums are added in warp order.
 __global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ ws, uint32_t parts, uint32_t cols, float* __restrict__ out) {
     __shared__ float s[8][32];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, j = blockIdx.x * 32u + lane;
     float v = 0.f;
-    if (j < cols) for (uint32_t p = warp; p < parts; p += 8) v += ws[(uint64_t)p * cols + j];
+    if (j < cols) {
+#pragma unroll 4
+        for (uint32_t p = warp; p < parts; p += 8) v += ws[(uint64_t)p * cols + j];
+    }
     s[warp][lane] = v;
     __syncthreads();
     if (warp == 0 && j < cols) {
@@ -128,11 +453,39 @@ cudaError_t launch_sum_parts(const float* ws, uint32_t parts, uint32_t cols, flo
     return cudaGetLastError();
 }
 
-cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, cudaStream_t st) {
+template <typename D, typename H, int V, int T>
+cudaError_t launch_backward_wide(const cleave_rmsnorm_backward_t& d, float* ws, uint32_t threads, uint32_t parts, uint32_t stage, cudaStream_t st) {
+    auto kernel = rmsnorm_backward_wide_kernel<D, H, V, T>;
+    static SmemLimit limit;
+    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
+    if (e != cudaSuccess) return e;
+    const uint32_t stages = max(1u, min(4u, 100u * 1024u / stage));
+    kernel<<<parts, threads, stage * stages, st>>>(d, ws, stages);
+    return cudaGetLastError();
+}
+template <typename D, typename H>
+cudaError_t launch_backward_types(const cleave_rmsnorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
+    const uint32_t groups = d.cols / 8;
+    if (groups <= 512) return launch_backward_wide<D, H, 1, 512>(d, ws, (groups + 31) / 32 * 32, parts, stage, st);
+    if (groups <= 1024) return launch_backward_wide<D, H, 2, 512>(d, ws, (groups + 63) / 64 * 32, parts, stage, st);
+    return launch_backward_wide<D, H, 2, 1024>(d, ws, (groups + 63) / 64 * 32, parts, stage, st);
+}
+
+cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, int sms, cudaStream_t st) {
     if (!d.cols) return cudaSuccess;
+    (void)sms;
     const uint32_t parts = rmsnorm_backward_parts(d.rows, d.cols);
-    if (parts) rmsnorm_backward_any_kernel<<<parts, kRowThreads, 0, st>>>(d, ws);
-    cudaError_t e = cudaGetLastError();
+    const uint64_t stage = (uint64_t)d.cols * (type_bytes(d.dy_type) + type_bytes(d.h_type) * (d.dres ? 2u : 1u));
+    const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && stage <= kRingMost && rows_wide(d.dy, d.lddy, d.dy_type) && rows_wide(d.h, d.ldh, d.h_type) &&
+                      rows_wide(d.dx, d.lddx, d.h_type) && (!d.dres || rows_wide(d.dres, d.lddres, d.h_type));
+    cudaError_t e = cudaSuccess;
+    if (parts && wide) {
+        if (d.dy_type == CLEAVE_T_F32) e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<float, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<float, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
+        else e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<__nv_bfloat16, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<__nv_bfloat16, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
+    } else if (parts) {
+        rmsnorm_backward_any_kernel<<<parts, kRowThreads, 0, st>>>(d, ws);
+        e = cudaGetLastError();
+    }
     if (e != cudaSuccess || !d.dw) return e;
     return launch_sum_parts(ws, parts, d.cols, d.dw, st);
 }

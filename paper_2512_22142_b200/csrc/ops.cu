@@ -38,11 +38,12 @@ int cuda_code(cudaError_t e) {
     cudaGetLastError();
     return CLEAVE_E_CUDA;
 }
+// SM count of the current device, or a negative CLEAVE_E_* code
 int need_device() {
-    int n = 0, dev = 0, major = 0;
-    if (cudaGetDeviceCount(&n) != cudaSuccess || n == 0 || cudaGetDevice(&dev) != cudaSuccess ||
+    int dev = 0, n = 0, major = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
         cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
-    return major == 10 ? 0 : CLEAVE_E_UNSUPPORTED;
+    return major == 10 ? n : CLEAVE_E_UNSUPPORTED;
 }
 
 bool adam_wide(const AdamTensor& t, uint32_t state_type, uint32_t g_type) {
@@ -72,7 +73,8 @@ int cleave_adamw_create(const cleave_adamw_tensor_t* t, uint32_t n, uint32_t sta
     }
     if (n_chunks > 0x7FFFFFFFull) return CLEAVE_E_UNSUPPORTED;
     int rc = need_device();
-    if (rc) return rc;
+    if (rc < 0) return rc;
+    rc = 0;
     cleave_adamw_s* h = new (std::nothrow) cleave_adamw_s();
     if (!h) return CLEAVE_E_NOMEM;
     try {
@@ -149,8 +151,8 @@ int cleave_rmsnorm(const cleave_rmsnorm_t* d, void* stream) {
     if (d->h && (!d->r || !matrix_ok(d->h, d->r_type, d->ldh, d->cols))) return CLEAVE_E_INVAL;
     if (!matrix_ok(d->y, d->y_type, d->ldy, d->cols) || !aligned(d->rstd, 4)) return CLEAVE_E_INVAL;
     if ((d->y_type == CLEAVE_T_E4M3) != (d->scale != nullptr) || !aligned(d->scale, 4)) return CLEAVE_E_INVAL;
-    const int rc = need_device();
-    return rc ? rc : cuda_code(launch_rmsnorm(*d, true, static_cast<cudaStream_t>(stream)));
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_rmsnorm(*d, true, sms, static_cast<cudaStream_t>(stream)));
 }
 
 int cleave_quantize_rows(const void* x, uint32_t x_type, uint64_t rows, uint32_t cols, uint64_t ldx, void* y, uint64_t ldy,
@@ -162,8 +164,8 @@ int cleave_quantize_rows(const void* x, uint32_t x_type, uint64_t rows, uint32_t
     cleave_rmsnorm_t d = {};
     d.rows = rows; d.cols = cols; d.x_type = x_type; d.y_type = CLEAVE_T_E4M3;
     d.x = x; d.ldx = ldx; d.y = y; d.ldy = ldy; d.scale = scale;
-    const int rc = need_device();
-    return rc ? rc : cuda_code(launch_rmsnorm(d, false, static_cast<cudaStream_t>(stream)));
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_rmsnorm(d, false, sms, static_cast<cudaStream_t>(stream)));
 }
 
 uint64_t cleave_rmsnorm_backward_workspace(uint64_t rows, uint32_t cols) {
@@ -178,8 +180,8 @@ int cleave_rmsnorm_backward(const cleave_rmsnorm_backward_t* d, void* workspace,
         if (!optional_ok(d->w, d->w_type, d->cols, d->cols) || (d->dres && !matrix_ok(d->dres, d->h_type, d->lddres, d->cols))) return CLEAVE_E_INVAL;
         if (!d->rstd || !aligned(d->rstd, 4) || (d->dw && (!workspace || !aligned(workspace, 16)))) return CLEAVE_E_INVAL;
     }
-    const int rc = need_device();
-    return rc ? rc : cuda_code(launch_rmsnorm_backward(*d, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_rmsnorm_backward(*d, static_cast<float*>(workspace), sms, static_cast<cudaStream_t>(stream)));
 }
 
 // ---- product and its epilogue's backward -------------------------------------------------------------------
@@ -198,8 +200,8 @@ int cleave_linear(const cleave_linear_t* d, void* stream) {
     if (!aligned(d->scale_a, 4) || !aligned(d->scale_b, 4) || !optional_ok(d->bias, d->bias_type, g.N, g.N)) return CLEAVE_E_INVAL;
     if (!optional_ok(d->z, d->z_type, d->ldz, g.N) || !optional_ok(d->mul, d->mul_type, d->ldmul, g.N) ||
         !optional_ok(d->res, d->res_type, d->ldres, g.N) || !matrix_ok(d->C, d->c_type, d->ldc, g.N)) return CLEAVE_E_INVAL;
-    const int rc = need_device();
-    return rc ? rc : launch_linear(*d, static_cast<cudaStream_t>(stream));
+    const int sms = need_device();
+    return sms < 0 ? sms : launch_linear(*d, sms, static_cast<cudaStream_t>(stream));
 }
 int cleave_linear_status(void* stream) { return linear_status(static_cast<cudaStream_t>(stream)); }
 void cleave_linear_set_wait_limit_ns(uint64_t ns) { linear_set_wait_limit_ns(ns); }
@@ -217,8 +219,8 @@ int cleave_act_backward(const cleave_act_backward_t* d, void* workspace, void* s
         if (!d->z && (d->act != CLEAVE_ACT_NONE || d->dmul)) return CLEAVE_E_INVAL;
         if (d->dbias && (!workspace || !aligned(workspace, 16))) return CLEAVE_E_INVAL;
     }
-    const int rc = need_device();
-    return rc ? rc : cuda_code(launch_act_backward(*d, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_act_backward(*d, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -8,6 +8,8 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+
 #include "cleave.h"
 
 namespace cleave {
@@ -16,6 +18,21 @@ constexpr float kE4M3Max = 448.f;
 constexpr uint32_t kStateBlock = 256;            // elements that share a scale in an 8-bit optimizer state
 
 inline uint32_t type_bytes(uint32_t t) { return t == CLEAVE_T_F32 ? 4u : (t == CLEAVE_T_BF16 ? 2u : (t == CLEAVE_T_E4M3 ? 1u : 0u)); }
+
+// Raises a kernel's dynamic shared memory limit, once per device.
+struct SmemLimit {
+    std::atomic<uint64_t> devices{0};
+    cudaError_t raise(const void* kernel, int bytes) {
+        int dev = 0;
+        cudaError_t e = cudaGetDevice(&dev);
+        if (e != cudaSuccess) return e;
+        const uint64_t bit = dev < 64 ? 1ull << dev : 0ull;
+        if (devices.load(std::memory_order_relaxed) & bit) return cudaSuccess;
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+        if (e == cudaSuccess) devices.fetch_or(bit, std::memory_order_relaxed);
+        return e;
+    }
+};
 
 // ---- elements ----------------------------------------------------------------------------------------
 template <typename T> __device__ __forceinline__ float to_f32(T v);
@@ -44,6 +61,55 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 __device__ __forceinline__ uint8_t e4m3_nearest(float v) { return (uint8_t)__nv_cvt_float_to_fp8(v, __NV_SATFINITE, __NV_E4M3); }
 __device__ __forceinline__ float e4m3_value(uint8_t code) {
     return __half2float(__half(__nv_cvt_fp8_to_halfraw((__nv_fp8_storage_t)code, __NV_E4M3)));
+}
+
+// ---- 8 consecutive elements: 16 bytes of bf16 or 32 of fp32, as raw words and as fp32 -----------------------
+template <typename T> struct Raw8;
+template <> struct Raw8<float> { uint4 w[2]; };
+template <> struct Raw8<__nv_bfloat16> { uint4 w[1]; };
+template <typename T>
+__device__ __forceinline__ Raw8<T> load_raw8(const T* p) {           // read once: the line need not stay in L1
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(r.w) / 16); ++i) r.w[i] = __ldcs(reinterpret_cast<const uint4*>(p) + i);
+    return r;
+}
+__device__ __forceinline__ void unpack8(const Raw8<float>& r, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        x[4 * i] = __uint_as_float(r.w[i].x); x[4 * i + 1] = __uint_as_float(r.w[i].y);
+        x[4 * i + 2] = __uint_as_float(r.w[i].z); x[4 * i + 3] = __uint_as_float(r.w[i].w);
+    }
+}
+__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16>& r, float (&x)[8]) {
+    const uint32_t w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(w[i] << 16); x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+__device__ __forceinline__ void store8(float* p, const float (&x)[8]) {
+    reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
+    reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
+}
+__device__ __forceinline__ void store8(__nv_bfloat16* p, const float (&x)[8]) {
+    *reinterpret_cast<uint4*>(p) = make_uint4(bf16x2(x[0], x[1]), bf16x2(x[2], x[3]), bf16x2(x[4], x[5]), bf16x2(x[6], x[7]));
+}
+// eight E4M3 codes (to nearest even, magnitudes above 448 become 448)
+__device__ __forceinline__ void store8(uint8_t* p, const float (&x)[8]) {
+    uint32_t w[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+        w[i] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[4 * i], x[4 * i + 1]), __NV_SATFINITE, __NV_E4M3) |
+               ((uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(x[4 * i + 2], x[4 * i + 3]), __NV_SATFINITE, __NV_E4M3) << 16);
+    *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
+}
+// the wide accesses apply: base and rows 16-byte aligned (8 bytes for rows of codes), whole groups of 8 columns
+inline bool rows_wide(const void* p, uint64_t ld, uint32_t type) {
+    const uint64_t unit = type == CLEAVE_T_E4M3 ? 8 : 16;
+    return (uintptr_t)p % unit == 0 && (ld * type_bytes(type)) % unit == 0;
 }
 
 // ---- activations ----------------------------------------------------------------------------------
@@ -107,15 +173,15 @@ cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uin
                          bool g_bf16, cudaStream_t st);
 
 // ---- norm, rows in 8 bits, epilogue backward ---------------------------------------------------------
-cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, cudaStream_t st);
+cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, int sms, cudaStream_t st);   // sms: the device's SM count
 uint32_t rmsnorm_backward_parts(uint64_t rows, uint32_t cols);          // rows of partial sums in the workspace
-cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, cudaStream_t st);
+cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, int sms, cudaStream_t st);
 uint32_t act_backward_parts(uint64_t rows, uint32_t cols);
 cudaError_t launch_act_backward(const cleave_act_backward_t& d, float* ws, cudaStream_t st);
 cudaError_t launch_sum_parts(const float* ws, uint32_t parts, uint32_t cols, float* out, cudaStream_t st);
 
 // ---- product with an epilogue --------------------------------------------------------------------------
-int launch_linear(const cleave_linear_t& d, cudaStream_t st);           // CLEAVE_* code
+int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st);           // CLEAVE_* code
 int linear_status(cudaStream_t st);
 void linear_set_wait_limit_ns(uint64_t ns);
 
