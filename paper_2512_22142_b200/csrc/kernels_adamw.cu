@@ -7,6 +7,8 @@
 // a shuffle reduction inside its warp, so an 8-bit state needs no second pass.
 // Bound by the HBM's bandwidth: 30 bytes an element with fp32 states (gradient 4, weight 8, states 16, copy 2),
 // 18 with 8-bit ones.
+#include <cuda_fp16.h>
+
 #include "ops.cuh"
 
 namespace cleave {
@@ -19,15 +21,14 @@ __device__ __forceinline__ uint64_t mix64(uint64_t x) {
     return x ^ (x >> 31);
 }
 
-// E4M3 magnitude code of |q| <= 448, away from zero with the probability of what is cut off (u: 16 random bits).
-// From 2^-6 on three mantissa bits stay, so the random bits are added right below them and the rest is cut;
-// below, codes are multiples of 2^-9.
+// E4M3 magnitude code of |q| <= 448 (rounding of the scale may leave it a unit above), away from zero with the
+// probability of what is cut off (u: 16 random bits).  From 2^-6 on three mantissa bits stay, so the random bits are
+// added right below them and the rest is cut; below (a few elements in ten thousand), codes are multiples of 2^-9.
 __device__ __forceinline__ uint32_t stochastic_code(float q, uint32_t u) {
     const float a = fabsf(q);
-    const uint32_t whole = ((__float_as_uint(a) + (u << 4)) >> 20) - 960u;          // exponent bias 127 - 7, 3 mantissa bits
-    const uint32_t small = (uint32_t)floorf(__fadd_rn(__fmul_rn(a, 512.f), __fmul_rn((float)u, 1.f / 65536.f)));
-    const uint32_t code = min(a >= 0.015625f ? whole : small, 0x7Eu);
-    return a != a ? 0x7Fu : code;
+    uint32_t code = ((__float_as_uint(a) + (u << 4)) >> 20) - 960u;                 // exponent bias 127 - 7, 3 mantissa bits
+    if (a < 0.015625f) code = (uint32_t)floorf(__fadd_rn(__fmul_rn(a, 512.f), __fmul_rn((float)u, 1.f / 65536.f)));
+    return min(code, 0x7Eu);
 }
 
 template <bool WIDE, typename T>
@@ -51,7 +52,11 @@ __device__ __forceinline__ void load4_codes(const uint8_t* src, uint64_t e, uint
     if constexpr (WIDE) {
         const uint32_t c = *reinterpret_cast<const uint32_t*>(src + e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = e4m3_value((uint8_t)(c >> (8 * i)));
+        for (int h = 0; h < 2; ++h) {
+            const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(h ? c >> 16 : c & 0xFFFFu), __NV_E4M3);
+            const float2 f = __half22float2(__half2(r));
+            x[2 * h] = f.x; x[2 * h + 1] = f.y;
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = e + i < n ? e4m3_value(src[e + i]) : 0.f;
@@ -135,7 +140,11 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, uint32_t tensor
         if constexpr (!STATE8) { store4<WIDE>(static_cast<float*>(t.m), e, n, m[j]); store4<WIDE>(static_cast<float*>(t.v), e, n, r[j]); }
     }
     if constexpr (STATE8) {
-        const float2 bm = block_scale(warp_max_nan(top_m)), bv = block_scale(warp_max_nan(top_r));
+        top_m = warp_max_nan(top_m);
+        top_r = warp_max_nan(top_r);
+        const float2 bm = block_scale(top_m), bv = block_scale(top_r);
+        // a block that holds a NaN or an infinity: its scale is one, so some codes have to be NaN
+        const bool nan_m = !(top_m < INFINITY), nan_v = !(top_r < INFINITY);
         const uint64_t key = mix64(mix64(s.base + tensor));
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
@@ -149,9 +158,12 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, uint32_t tensor
                     const int i = 2 * h + o;
                     const uint32_t bits = (uint32_t)(word >> (32 * o));
                     const float qm = __fmul_rn(m[j][i], bm.y), qv = __fmul_rn(r[j][i], bv.y);
-                    cm[i] = stochastic_code(qm, bits & 0xFFFFu) | (qm < 0.f ? 0x80u : 0u);
-                    const uint32_t c = stochastic_code(qv, bits >> 16);
-                    cv[i] = c == 0u && qv > 0.f ? 1u : c;
+                    cm[i] = stochastic_code(qm, bits & 0xFFFFu);
+                    if (nan_m && qm != qm) cm[i] = 0x7Fu;
+                    if (qm < 0.f) cm[i] |= 0x80u;
+                    cv[i] = stochastic_code(qv, bits >> 16);
+                    if (qv > 0.f) cv[i] = max(cv[i], 1u);
+                    if (nan_v && qv != qv) cv[i] = 0x7Fu;
                 }
             }
             store4_codes<WIDE>(static_cast<uint8_t*>(t.m), e, n, cm);

@@ -9,6 +9,8 @@
 //          the warps' sums.
 //   any    every other size, stride or alignment: neighbouring threads own neighbouring columns and take them
 //          again in each pass (the row stays in L1 / L2).
+#include <type_traits>
+
 #include "ops.cuh"
 
 namespace cleave {
@@ -98,7 +100,8 @@ struct NoRes {};                    // no residual operand
 template <typename T> struct Bytes8 { static constexpr uint32_t value = sizeof(T) * 8; };
 template <> struct Bytes8<NoRes> { static constexpr uint32_t value = 0; };
 
-__device__ __forceinline__ void load_weight8(const cleave_rmsnorm_t& d, uint32_t col, float (&w)[8]) {
+template <typename Desc>
+__device__ __forceinline__ void load_weight8(const Desc& d, uint32_t col, float (&w)[8]) {      // (the same for every row: L1)
     if (d.w_type == CLEAVE_T_F32) {
         const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(d.w) + col);
         const float4 a = __ldg(p), b = __ldg(p + 1);
@@ -115,111 +118,119 @@ __device__ __forceinline__ void load_weight8(const cleave_rmsnorm_t& d, uint32_t
 
 // V groups of 8 columns per thread.  WARP: blockDim (32, rows per CTA), a warp per row.  Otherwise a CTA per row
 // and a ring of `stages` rows in shared memory, [stage][operand][group] with a thread's groups blockDim.x apart.
-template <typename X, typename R, typename Y, int V, bool WARP, bool NORM>
-__global__ void __launch_bounds__(WARP ? 256 : 1024) row_wide_kernel(const __grid_constant__ cleave_rmsnorm_t d, uint32_t stages) {
+template <typename X, typename R, typename Y, int V, bool WARP, bool NORM, int T>
+__global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cleave_rmsnorm_t d, uint32_t stages) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 parts[2][32];
-    constexpr bool RES = !(sizeof(R) == 1);
+    constexpr bool RES = !(sizeof(R) == 1), CODES = sizeof(Y) == 1;
+    constexpr uint32_t BX = Bytes8<X>::value, BR = Bytes8<R>::value;
     const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
     const uint64_t first = WARP ? (uint64_t)blockIdx.x * blockDim.y + threadIdx.y : blockIdx.x;
     const uint64_t stride = WARP ? (uint64_t)gridDim.x * blockDim.y : gridDim.x;
-    const uint32_t stage_bytes = groups * (Bytes8<X>::value + Bytes8<R>::value);
-    const uint32_t ring_base = (uint32_t)__cvta_generic_to_shared(ring);
-    auto fetch = [&](uint64_t row, uint32_t s) {                 // this thread's groups of a row into stage s
-        if (row < d.rows) {
+    const uint32_t off_r = groups * BX, stage_bytes = off_r + groups * BR;
+    const float inv_cols = 1.f / (float)d.cols;
+    bool live[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) live[v] = tid + v * nt < groups;
+    // this thread's first group of a row of each operand; a row's step in bytes
+    const uint8_t* px = reinterpret_cast<const uint8_t*>(static_cast<const X*>(d.x) + first * d.ldx) + tid * BX;
+    const uint8_t* pr = reinterpret_cast<const uint8_t*>(d.r) + (RES ? first * d.ldr * (BR / 8) + tid * BR : 0);
+    const uint64_t step_x = stride * d.ldx * (BX / 8), step_r = stride * d.ldr * (BR / 8);
+    const uint8_t* slot = ring + tid * BX;
+    const uint32_t slot_at = (uint32_t)__cvta_generic_to_shared(ring) + tid * BX;
+    uint64_t ahead = first;                                      // the row that is fetched next
+    auto fetch = [&](uint32_t at) {                              // this thread's groups of the next row into the stage at byte `at`
+        if (ahead < d.rows) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const uint32_t g = tid + v * nt;
-                if (g >= groups) continue;
-                const uint8_t* px = reinterpret_cast<const uint8_t*>(static_cast<const X*>(d.x) + row * d.ldx + g * 8);
-                const uint32_t at = ring_base + s * stage_bytes + g * Bytes8<X>::value;
+                if (!live[v]) continue;
 #pragma unroll
-                for (uint32_t b = 0; b < Bytes8<X>::value; b += 16) cp_async16(at + b, px + b);
+                for (uint32_t b = 0; b < BX; b += 16) cp_async16(slot_at + at + v * nt * BX + b, px + v * nt * BX + b);
                 if constexpr (RES) {
-                    const uint8_t* pr = reinterpret_cast<const uint8_t*>(static_cast<const R*>(d.r) + row * d.ldr + g * 8);
-                    const uint32_t ar = ring_base + s * stage_bytes + groups * Bytes8<X>::value + g * Bytes8<R>::value;
 #pragma unroll
-                    for (uint32_t b = 0; b < Bytes8<R>::value; b += 16) cp_async16(ar + b, pr + b);
+                    for (uint32_t b = 0; b < BR; b += 16) cp_async16(slot_at - tid * BX + tid * BR + off_r + at + v * nt * BR + b, pr + v * nt * BR + b);
                 }
             }
+            ahead += stride; px += step_x; pr += step_r;
         }
         cp_async_commit();                                       // (an empty group keeps the count when there is no such row)
     };
     if constexpr (!WARP)
-        for (uint32_t s = 0; s < stages; ++s) fetch(first + s * stride, s);
+        for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
 
-    uint32_t it = 0, s = 0;
+    Y* py = static_cast<Y*>(d.y) + first * d.ldy + tid * 8;
+    R* ph = RES && d.h ? static_cast<R*>(d.h) + first * d.ldh + tid * 8 : nullptr;
+    uint32_t it = 0, at = 0;
     for (uint64_t row = first; row < d.rows; row += stride, ++it) {
-        float h[V][8];
+        float h[V][8], hw[V][8];
         if constexpr (!WARP) {
             if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
         }
+        Raw8<X> rx[V];
+        Raw8<typename std::conditional<RES, R, X>::type> rr[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t g = tid + v * nt;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) h[v][i] = 0.f;
-            if (g >= groups) continue;
-            Raw8<X> rx;
-            if constexpr (WARP) rx = load_raw8(static_cast<const X*>(d.x) + row * d.ldx + g * 8);
-            else rx = *reinterpret_cast<const Raw8<X>*>(ring + s * stage_bytes + g * Bytes8<X>::value);
-            unpack8(rx, h[v]);
-            if constexpr (RES) {
-                Raw8<R> rr;
-                float r[8];
-                if constexpr (WARP) rr = load_raw8(static_cast<const R*>(d.r) + row * d.ldr + g * 8);
-                else rr = *reinterpret_cast<const Raw8<R>*>(ring + s * stage_bytes + groups * Bytes8<X>::value + g * Bytes8<R>::value);
-                unpack8(rr, r);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] += r[i];
+            if (!live[v]) continue;
+            if constexpr (WARP) {
+                rx[v] = load_raw8(reinterpret_cast<const X*>(px + v * nt * BX));
+                if constexpr (RES) rr[v] = load_raw8(reinterpret_cast<const R*>(pr + v * nt * BR));
+            } else {
+                rx[v] = *reinterpret_cast<const Raw8<X>*>(slot + at + v * nt * BX);
+                if constexpr (RES) rr[v] = *reinterpret_cast<const Raw8<R>*>(ring + off_r + at + (tid + v * nt) * BR);
             }
         }
         // one reduction for both statistics: the sum of squares and, for codes, the largest |h w| (times rstd later)
         float ss = 0.f, top = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t g = tid + v * nt;
-            if (g >= groups) continue;
+            if (!live[v]) continue;
+            unpack8(rx[v], h[v]);
+            if constexpr (RES) {
+                float r[8];
+                unpack8(rr[v], r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) h[v][i] += r[i];
+            }
             if constexpr (NORM) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) ss = fmaf(h[v][i], h[v][i], ss);
             }
-            if constexpr (sizeof(Y) == 1) {
-                float w[8];
-                load_weight8(d, g * 8, w);
+            load_weight8(d, (tid + v * nt) * 8, hw[v]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(h[v][i] * w[i]));
+            for (int i = 0; i < 8; ++i) {
+                hw[v][i] *= h[v][i];
+                if constexpr (CODES) top = max_nan(top, fabsf(hw[v][i]));
             }
         }
         if constexpr (NORM) ss = warp_sum(ss);
-        if constexpr (sizeof(Y) == 1) top = warp_max(top);
+        if constexpr (CODES) top = warp_max(top);
         if constexpr (!WARP) {
             float2* p = parts[it & 1];
             if ((tid & 31u) == 0) p[tid >> 5] = make_float2(ss, top);
-            __syncthreads();                                     // also: every thread has read stage s
-            fetch(row + (uint64_t)stages * stride, s);
-            s = s + 1 == stages ? 0 : s + 1;
-            float2 q = (tid & 31u) < nt / 32 ? p[tid & 31u] : make_float2(0.f, 0.f);
+            __syncthreads();                                     // also: every thread has read this stage
+            fetch(at);
+            at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
+            const float2 q = (tid & 31u) < nt / 32 ? p[tid & 31u] : make_float2(0.f, 0.f);
             if constexpr (NORM) ss = warp_sum(q.x);
-            if constexpr (sizeof(Y) == 1) top = warp_max(q.y);
-        }
+            if constexpr (CODES) top = warp_max(q.y);
+        } else { px += step_x; pr += step_r; }
         float rstd = 1.f;
         if constexpr (NORM) {
-            rstd = rsqrtf(ss / (float)d.cols + d.eps);
+            rstd = rsqrtf(fmaf(ss, inv_cols, d.eps));
             if (d.rstd && tid == 0) d.rstd[row] = rstd;
         }
-        float inv = 1.f;
-        if constexpr (sizeof(Y) == 1) {
-            if (top == INFINITY) {                               // h w overflowed (rows of extreme weights): take h rstd w
+        bool wide_range = false;                                 // h w overflowed (rows of extreme weights): take h rstd w
+        float mult = rstd;
+        if constexpr (CODES) {
+            wide_range = top == INFINITY;
+            if (wide_range) {
                 float t = 0.f;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const uint32_t g = tid + v * nt;
-                    if (g >= groups) continue;
-                    float w[8];
-                    load_weight8(d, g * 8, w);
+                    if (!live[v]) continue;
+                    load_weight8(d, (tid + v * nt) * 8, hw[v]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) t = max_nan(t, fabsf(h[v][i] * rstd * w[i]));
+                    for (int i = 0; i < 8; ++i) { hw[v][i] *= h[v][i] * rstd; t = max_nan(t, fabsf(hw[v][i])); }
                 }
                 t = warp_max(t);
                 if constexpr (!WARP) {
@@ -232,20 +243,35 @@ __global__ void __launch_bounds__(WARP ? 256 : 1024) row_wide_kernel(const __gri
                 top = t;
             } else top *= rstd;
             const float2 sc = row_scale(top);
-            inv = sc.y;
+            mult = wide_range ? sc.y : rstd * sc.y;
             if (tid == 0) d.scale[row] = sc.x;
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t g = tid + v * nt;
-            if (g >= groups) continue;
-            if constexpr (RES && NORM) if (d.h) store8(static_cast<R*>(d.h) + row * d.ldh + g * 8, h[v]);
-            float w[8], y[8];
-            load_weight8(d, g * 8, w);
+            if (!live[v]) continue;
+            if constexpr (RES && NORM) if (ph) store8(ph + v * nt * 8, h[v]);
+            float y[8];
+            if constexpr (!CODES) {
+                // (h w may overflow where h rstd w does not: the product is formed the other way round then)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) y[i] = h[v][i] * rstd * w[i] * (sizeof(Y) == 1 ? inv : 1.f);
-            store8(static_cast<Y*>(d.y) + row * d.ldy + g * 8, y);
+                for (int i = 0; i < 8; ++i) y[i] = hw[v][i] * mult;
+                bool over = false;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) over |= fabsf(hw[v][i]) == INFINITY;
+                if (over) {
+                    float w[8];
+                    load_weight8(d, (tid + v * nt) * 8, w);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) y[i] = h[v][i] * rstd * w[i];
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) y[i] = hw[v][i] * mult;
+            }
+            store8(py + v * nt * 8, y);
         }
+        py += stride * d.ldy;
+        if (RES && ph) ph += stride * d.ldh;
     }
 }
 
@@ -253,9 +279,9 @@ constexpr uint32_t kWarpRowCols = 1024;         // up to here a warp holds a row
 constexpr uint32_t kRingBytes = 64 * 1024;      // per CTA; three CTAs an SM at most sizes
 constexpr uint32_t kRingMost = 160 * 1024;
 
-template <typename X, typename R, typename Y, int V, bool WARP, bool NORM>
+template <typename X, typename R, typename Y, int V, bool WARP, bool NORM, int T>
 cudaError_t launch_row_wide(const cleave_rmsnorm_t& d, uint32_t threads, int sms, cudaStream_t st) {
-    auto kernel = row_wide_kernel<X, R, Y, V, WARP, NORM>;
+    auto kernel = row_wide_kernel<X, R, Y, V, WARP, NORM, T>;
     if (WARP) {
         const uint64_t ctas = (d.rows + 7) / 8;
         kernel<<<(unsigned)ctas, dim3(32, 8), 0, st>>>(d, 0u);
@@ -277,12 +303,13 @@ template <typename X, typename R, typename Y, bool NORM>
 cudaError_t launch_row_types(const cleave_rmsnorm_t& d, int sms, cudaStream_t st) {
     const uint32_t groups = d.cols / 8;
     if (d.cols <= kWarpRowCols) {
-        if (groups <= 32) return launch_row_wide<X, R, Y, 1, true, NORM>(d, 32, sms, st);
-        if (groups <= 64) return launch_row_wide<X, R, Y, 2, true, NORM>(d, 32, sms, st);
-        return launch_row_wide<X, R, Y, 4, true, NORM>(d, 32, sms, st);
+        if (groups <= 32) return launch_row_wide<X, R, Y, 1, true, NORM, 256>(d, 32, sms, st);
+        if (groups <= 64) return launch_row_wide<X, R, Y, 2, true, NORM, 256>(d, 32, sms, st);
+        return launch_row_wide<X, R, Y, 4, true, NORM, 256>(d, 32, sms, st);
     }
-    if (groups <= 1024) return launch_row_wide<X, R, Y, 2, false, NORM>(d, (groups + 63) / 64 * 32, sms, st);
-    return launch_row_wide<X, R, Y, 4, false, NORM>(d, (groups + 127) / 128 * 32, sms, st);
+    if (groups <= 512) return launch_row_wide<X, R, Y, 2, false, NORM, 256>(d, (groups + 63) / 64 * 32, sms, st);
+    if (groups <= 1024) return launch_row_wide<X, R, Y, 2, false, NORM, 512>(d, (groups + 63) / 64 * 32, sms, st);
+    return launch_row_wide<X, R, Y, 4, false, NORM, 1024>(d, (groups + 127) / 128 * 32, sms, st);
 }
 template <typename X, typename R>
 cudaError_t launch_row_out(const cleave_rmsnorm_t& d, bool norm, int sms, cudaStream_t st) {
@@ -341,10 +368,10 @@ __global__ void __launch_bounds__(kRowThreads) rmsnorm_backward_any_kernel(const
     }
 }
 
-// V groups of 8 columns a thread, a CTA per row, a ring of rows of (dy, h, dres) in shared memory; w and the CTA's
-// share of dw stay in registers over all its rows.
-template <typename D, typename H, int V, int T>
-__global__ void __launch_bounds__(T) rmsnorm_backward_wide_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
+// V groups of 8 columns a thread, a CTA per row, a ring of rows of (dy, h, dres) in shared memory; the CTA's share of
+// dw stays in registers over all its rows (w comes from L1: keeping it too would cost a CTA an SM).
+template <typename D, typename H, int V, int T, int CTAS>
+__global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float parts[2][32];
     constexpr uint32_t BD = Bytes8<D>::value, BH = Bytes8<H>::value;
@@ -352,110 +379,120 @@ __global__ void __launch_bounds__(T) rmsnorm_backward_wide_kernel(const __grid_c
     const bool res = d.dres != nullptr;
     const uint32_t off_h = groups * BD, off_res = off_h + groups * BH, stage_bytes = off_res + (res ? groups * BH : 0u);
     const uint32_t ring_base = (uint32_t)__cvta_generic_to_shared(ring);
-    auto fetch = [&](uint64_t row, uint32_t s) {
-        if (row < d.rows) {
+    const float inv_cols = 1.f / (float)d.cols;
+    bool live[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) live[v] = tid + v * nt < groups;
+    const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + blockIdx.x * d.lddy) + tid * BD;
+    const uint8_t* ph = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.h) + blockIdx.x * d.ldh) + tid * BH;
+    const uint8_t* pr = res ? reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.dres) + blockIdx.x * d.lddres) + tid * BH : nullptr;
+    const uint64_t step_d = gridDim.x * d.lddy * (BD / 8), step_h = gridDim.x * d.ldh * (BH / 8), step_r = gridDim.x * d.lddres * (BH / 8);
+    uint64_t ahead = blockIdx.x;
+    auto fetch = [&](uint32_t at) {
+        if (ahead < d.rows) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const uint32_t g = tid + v * nt;
-                if (g >= groups) continue;
-                const uint32_t at = ring_base + s * stage_bytes;
-                const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + row * d.lddy + g * 8);
-                const uint8_t* ph = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.h) + row * d.ldh + g * 8);
+                if (!live[v]) continue;
+                const uint32_t to = ring_base + at;
 #pragma unroll
-                for (uint32_t b = 0; b < BD; b += 16) cp_async16(at + g * BD + b, pd + b);
+                for (uint32_t b = 0; b < BD; b += 16) cp_async16(to + (tid + v * nt) * BD + b, pd + v * nt * BD + b);
 #pragma unroll
-                for (uint32_t b = 0; b < BH; b += 16) cp_async16(at + off_h + g * BH + b, ph + b);
+                for (uint32_t b = 0; b < BH; b += 16) cp_async16(to + off_h + (tid + v * nt) * BH + b, ph + v * nt * BH + b);
                 if (res) {
-                    const uint8_t* pr = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.dres) + row * d.lddres + g * 8);
 #pragma unroll
-                    for (uint32_t b = 0; b < BH; b += 16) cp_async16(at + off_res + g * BH + b, pr + b);
+                    for (uint32_t b = 0; b < BH; b += 16) cp_async16(to + off_res + (tid + v * nt) * BH + b, pr + v * nt * BH + b);
                 }
             }
+            ahead += gridDim.x; pd += step_d; ph += step_h;
+            if (res) pr += step_r;
         }
         cp_async_commit();
     };
-    for (uint32_t s = 0; s < stages; ++s) fetch(blockIdx.x + (uint64_t)s * gridDim.x, s);
-    float w[V][8], dw[V][8];
+    for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
+    float dw[V][8];
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        const uint32_t g = tid + v * nt;
+    for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) { dw[v][i] = 0.f; w[v][i] = d.w && g < groups ? load_as(d.w, d.w_type, g * 8 + i) : 1.f; }
-    }
-    uint32_t it = 0, s = 0;
+        for (int i = 0; i < 8; ++i) dw[v][i] = 0.f;
+    H* pdx = static_cast<H*>(d.dx) + blockIdx.x * d.lddx + tid * 8;
+    uint32_t it = 0, at = 0;
     for (uint64_t row = blockIdx.x; row < d.rows; row += gridDim.x, ++it) {
         if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
         const float rstd = __ldg(d.rstd + row);
-        const uint8_t* stage = ring + s * stage_bytes;
-        float q[V][8], xh[V][8], dot = 0.f;
-        Raw8<H> rr[V];
+        const uint8_t* stage = ring + at;
+        float q[V][8], dot = 0.f;                                // q = w dy; dot = sum q h
+        Raw8<H> rh[V], rr[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
+            if (!live[v]) continue;
             const uint32_t g = tid + v * nt;
-            if (g >= groups) continue;
             unpack8(*reinterpret_cast<const Raw8<D>*>(stage + g * BD), q[v]);
-            unpack8(*reinterpret_cast<const Raw8<H>*>(stage + off_h + g * BH), xh[v]);
+            rh[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_h + g * BH);
             if (res) rr[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_res + g * BH);
+            float h[8], w[8];
+            unpack8(rh[v], h);
+            load_weight8(d, g * 8, w);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                xh[v][i] *= rstd;
-                dw[v][i] = fmaf(q[v][i], xh[v][i], dw[v][i]);
-                q[v][i] *= w[v][i];
-                dot = fmaf(q[v][i], xh[v][i], dot);
+                dw[v][i] = fmaf(q[v][i] * rstd, h[i], dw[v][i]);
+                q[v][i] *= w[i];
+                dot = fmaf(q[v][i], h[i], dot);
             }
         }
         dot = warp_sum(dot);
         float* p = parts[it & 1];
         if ((tid & 31u) == 0) p[tid >> 5] = dot;
-        __syncthreads();                                         // also: every thread has read stage s
-        fetch(row + (uint64_t)stages * gridDim.x, s);
-        s = s + 1 == stages ? 0 : s + 1;
-        const float mean = warp_sum((tid & 31u) < nt / 32 ? p[tid & 31u] : 0.f) / (float)d.cols;
+        __syncthreads();                                         // also: every thread has read this stage
+        fetch(at);
+        at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
+        const float mean = warp_sum((tid & 31u) < nt / 32 ? p[tid & 31u] : 0.f) * rstd * inv_cols;      // of q xh
+        const float along = rstd * rstd * mean;                  // rstd xh mean = along h
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const uint32_t g = tid + v * nt;
-            if (g >= groups) continue;
-            float dx[8], r[8];
-            if (res) unpack8(rr[v], r);
+            if (!live[v]) continue;
+            float dx[8], h[8];
+            unpack8(rh[v], h);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dx[i] = rstd * (q[v][i] - xh[v][i] * mean) + (res ? r[i] : 0.f);
-            store8(static_cast<H*>(d.dx) + row * d.lddx + g * 8, dx);
+            for (int i = 0; i < 8; ++i) dx[i] = rstd * q[v][i] - along * h[i];
+            if (res) {
+                unpack8(rr[v], h);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) dx[i] += h[i];
+            }
+            store8(pdx + v * nt * 8, dx);
         }
+        pdx += gridDim.x * d.lddx;
     }
     if (d.dw)
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const uint32_t g = tid + v * nt;
-            if (g < groups) store8(ws + (uint64_t)blockIdx.x * d.cols + g * 8, dw[v]);
-        }
+        for (int v = 0; v < V; ++v)
+            if (live[v]) store8(ws + (uint64_t)blockIdx.x * d.cols + (tid + v * nt) * 8, dw[v]);
 }
 
 // out[j] = sum over the parts of ws[part][j], in a fixed order.  32 columns per CTA; warp w adds the parts
-// w, w + 8, ... and the eight sums are added in warp order.
-__global__ void __launch_bounds__(256) sum_parts_kernel(const float* __restrict__ ws, uint32_t parts, uint32_t cols, float* __restrict__ out) {
-    __shared__ float s[8][32];
+// w, w + 32, ... and the 32 sums are added in warp order.
+__global__ void __launch_bounds__(1024) sum_parts_kernel(const float* __restrict__ ws, uint32_t parts, uint32_t cols, float* __restrict__ out) {
+    __shared__ float s[32][33];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, j = blockIdx.x * 32u + lane;
     float v = 0.f;
     if (j < cols) {
-#pragma unroll 4
-        for (uint32_t p = warp; p < parts; p += 8) v += ws[(uint64_t)p * cols + j];
+#pragma unroll 8
+        for (uint32_t p = warp; p < parts; p += 32) v += __ldcs(ws + (uint64_t)p * cols + j);
     }
     s[warp][lane] = v;
     __syncthreads();
-    if (warp == 0 && j < cols) {
-#pragma unroll
-        for (int w = 1; w < 8; ++w) v += s[w][lane];
-        out[j] = v;
-    }
+    // warp w adds column w's 32 sums (a shuffle tree: fixed order)
+    v = warp_sum(s[lane][warp]);
+    if (lane == 0 && blockIdx.x * 32u + warp < cols) out[blockIdx.x * 32u + warp] = v;
 }
 cudaError_t launch_sum_parts(const float* ws, uint32_t parts, uint32_t cols, float* out, cudaStream_t st) {
-    sum_parts_kernel<<<(cols + 31) / 32, 256, 0, st>>>(ws, parts, cols, out);
+    sum_parts_kernel<<<(cols + 31) / 32, 1024, 0, st>>>(ws, parts, cols, out);
     return cudaGetLastError();
 }
 
-template <typename D, typename H, int V, int T>
+template <typename D, typename H, int V, int T, int CTAS>
 cudaError_t launch_backward_wide(const cleave_rmsnorm_backward_t& d, float* ws, uint32_t threads, uint32_t parts, uint32_t stage, cudaStream_t st) {
-    auto kernel = rmsnorm_backward_wide_kernel<D, H, V, T>;
+    auto kernel = rmsnorm_backward_wide_kernel<D, H, V, T, CTAS>;
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
@@ -466,9 +503,11 @@ cudaError_t launch_backward_wide(const cleave_rmsnorm_backward_t& d, float* ws, 
 template <typename D, typename H>
 cudaError_t launch_backward_types(const cleave_rmsnorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
     const uint32_t groups = d.cols / 8;
-    if (groups <= 512) return launch_backward_wide<D, H, 1, 512>(d, ws, (groups + 31) / 32 * 32, parts, stage, st);
-    if (groups <= 1024) return launch_backward_wide<D, H, 2, 512>(d, ws, (groups + 63) / 64 * 32, parts, stage, st);
-    return launch_backward_wide<D, H, 2, 1024>(d, ws, (groups + 63) / 64 * 32, parts, stage, st);
+    const uint32_t threads = (groups + 63) / 64 * 32;
+    if (groups <= 512) return launch_backward_wide<D, H, 2, 256, 2>(d, ws, threads, parts, stage, st);
+    if (groups <= 640) return launch_backward_wide<D, H, 2, 320, 2>(d, ws, threads, parts, stage, st);
+    if (groups <= 1024) return launch_backward_wide<D, H, 2, 512, 1>(d, ws, threads, parts, stage, st);
+    return launch_backward_wide<D, H, 2, 1024, 1>(d, ws, threads, parts, stage, st);
 }
 
 cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, int sms, cudaStream_t st) {
@@ -477,7 +516,7 @@ cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* w
     const uint32_t parts = rmsnorm_backward_parts(d.rows, d.cols);
     const uint64_t stage = (uint64_t)d.cols * (type_bytes(d.dy_type) + type_bytes(d.h_type) * (d.dres ? 2u : 1u));
     const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && stage <= kRingMost && rows_wide(d.dy, d.lddy, d.dy_type) && rows_wide(d.h, d.ldh, d.h_type) &&
-                      rows_wide(d.dx, d.lddx, d.h_type) && (!d.dres || rows_wide(d.dres, d.lddres, d.h_type));
+                      rows_wide(d.dx, d.lddx, d.h_type) && (!d.dres || rows_wide(d.dres, d.lddres, d.h_type)) && (uintptr_t)d.w % 16 == 0;
     cudaError_t e = cudaSuccess;
     if (parts && wide) {
         if (d.dy_type == CLEAVE_T_F32) e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<float, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<float, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);

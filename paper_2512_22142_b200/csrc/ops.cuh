@@ -113,16 +113,32 @@ inline bool rows_wide(const void* p, uint64_t ld, uint32_t type) {
 }
 
 // ---- activations ----------------------------------------------------------------------------------
-// The two forms with an exponential are z g with g = 1 / (1 + e), e = exp(-t): one exponential and one quotient.
-// Where e overflows g is 0 (the limit); no 1 - tanh cancellation on the negative side.  In the slopes 1 - g loses
-// relative accuracy only where g is close to 1 and the term it belongs to vanishes against g.
-__device__ __forceinline__ float gelu_tanh_arg(float z) { return z * fmaf(0.07135481627260025f, z * z, 1.5957691216057308f); }   // 2 sqrt(2/pi) (z + 0.044715 z^3)
+// The two forms with an exponential are z g with g = 1 / (1 + e), e = exp(-t): one exponential (base 2, the factor
+// log2(e) in the argument's constants) and one reciprocal of a value of at least 1, both the hardware's
+// approximations (a few units in the last place; what they flush to zero is below 2^-126).  Where e overflows g is 0
+// (the limit); no 1 - tanh cancellation on the negative side.  In the slopes 1 - g loses relative accuracy only
+// where g is close to 1 and the term it belongs to vanishes against g.
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float rcp_fast(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// 1 / (1 + exp(-2 sqrt(2/pi) (z + 0.044715 z^3))) and 1 / (1 + exp(-z))
+__device__ __forceinline__ float gelu_tanh_gate(float z) {
+    return rcp_fast(1.f + exp2_fast(-z * fmaf(0.1029432407f, z * z, 2.3022081983f)));
+}
+__device__ __forceinline__ float silu_gate(float z) { return rcp_fast(1.f + exp2_fast(-1.4426950409f * z)); }
 __device__ __forceinline__ float act_value(float z, uint32_t act) {
     switch (act) {
         case CLEAVE_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
         case CLEAVE_ACT_GELU: return 0.5f * z * erfcf(-0.7071067811865476f * z);
-        case CLEAVE_ACT_GELU_TANH: return __fdividef(z, 1.f + __expf(-gelu_tanh_arg(z)));
-        case CLEAVE_ACT_SILU: return __fdividef(z, 1.f + __expf(-z));
+        case CLEAVE_ACT_GELU_TANH: return z * gelu_tanh_gate(z);
+        case CLEAVE_ACT_SILU: return z * silu_gate(z);
         default: return z;
     }
 }
@@ -135,12 +151,12 @@ __device__ __forceinline__ float2 act_value_slope(float z, uint32_t act) {
             return make_float2(z * phi, fmaf(z * 0.3989422804014327f, __expf(-0.5f * z * z), phi));
         }
         case CLEAVE_ACT_GELU_TANH: {
-            const float g = __fdividef(1.f, 1.f + __expf(-gelu_tanh_arg(z))), zg = z * g;
+            const float g = gelu_tanh_gate(z), zg = z * g;
             const float du = fmaf(0.21406444881780074f, fminf(z * z, 1e30f), 1.5957691216057308f);      // finite: 0 * du is 0 far out
             return make_float2(zg, fmaf(zg * (1.f - g), du, g));
         }
         case CLEAVE_ACT_SILU: {
-            const float g = __fdividef(1.f, 1.f + __expf(-z)), zg = z * g;
+            const float g = silu_gate(z), zg = z * g;
             return make_float2(zg, fmaf(zg, 1.f - g, g));
         }
         default: return make_float2(z, 1.f);
