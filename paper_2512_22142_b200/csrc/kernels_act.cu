@@ -10,13 +10,13 @@
 namespace cleave {
 
 constexpr uint32_t kActWarps = 8;
-constexpr uint32_t kActMaxParts = 256;
 
-// rows of partial bias gradients: one per band of rows (bands of 64 rows, longer when that would make too many)
+// Rows of partial bias gradients: one per band of rows.  As many bands as give each SM three CTAs of 256 columns
+// (the wide form's), so that a CTA's warps stream over many rows and the sums are joined once.
 uint32_t act_backward_parts(uint64_t rows, uint32_t cols) {
-    (void)cols;
-    const uint64_t bands = (rows + 63) / 64;
-    return (uint32_t)(bands < kActMaxParts ? bands : kActMaxParts);
+    const uint64_t tiles = (cols + 255) / 256, most = (rows + 2 * kActWarps - 1) / (2 * kActWarps);
+    const uint64_t bands = tiles < 444 ? 444 / tiles : 1;
+    return (uint32_t)(bands < most ? bands : most);
 }
 
 // U elements of an operand: raw (what stays in flight) and as fp32.  The wide form is typed; U = 1 takes the type
@@ -39,11 +39,12 @@ __device__ __forceinline__ void store_cells(void* p, uint32_t type, uint64_t at,
     else store8(static_cast<T*>(p) + at, x);
 }
 
-// D: type of dy; T: type of z, mul, dz and dmul (wide form: one type).  Rows in flight per warp and operand: 4.
+// D: type of dy; T: type of z, mul, dz and dmul (wide form: one type).  Rows in flight per warp and operand: two
+// batches of ROWS.
 template <int U, typename D, typename T, uint32_t ACT, bool MUL>
 __global__ void __launch_bounds__(32 * kActWarps, MUL ? 2 : 3) act_backward_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
     __shared__ float s[kActWarps][32 * U];
-    constexpr int ROWS = U > 1 && sizeof(T) == 4 ? 2 : 4;
+    constexpr int ROWS = U > 1 && sizeof(T) == 4 ? 1 : 2;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint64_t j = ((uint64_t)blockIdx.x * 32u + lane) * U;
     const uint64_t band = (d.rows + gridDim.y - 1) / gridDim.y, r0 = blockIdx.y * band, r1 = r0 + band < d.rows ? r0 + band : d.rows;
@@ -51,39 +52,51 @@ __global__ void __launch_bounds__(32 * kActWarps, MUL ? 2 : 3) act_backward_kern
     float sum[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) sum[i] = 0.f;
-    if (j < d.cols)
-        for (uint64_t row = r0 + warp; row < r1; row += kActWarps * ROWS) {
-            Cells<U, D> cdy[ROWS];
-            Cells<U, T> cz[ROWS], cm[ROWS];
+    // two batches of ROWS rows: the next one is asked for before the first is used
+    Cells<U, D> cdy[2][ROWS];
+    Cells<U, T> cz[2][ROWS], cm[2][ROWS];
+    auto fetch = [&](uint64_t row, int b) {
 #pragma unroll
-            for (int k = 0; k < ROWS; ++k) {
-                const uint64_t i = row + k * kActWarps;
-                if (i >= r1) break;
-                load_cells(cdy[k], d.dy, d.dy_type, i * d.lddy + j);
-                if (has_z) load_cells(cz[k], d.z, d.z_type, i * d.ldz + j);
-                if constexpr (MUL) load_cells(cm[k], d.mul, d.mul_type, i * d.ldmul + j);
-            }
-#pragma unroll
-            for (int k = 0; k < ROWS; ++k) {
-                const uint64_t i = row + k * kActWarps;
-                if (i >= r1) break;
-                float dy[U], z[U], mul[U], dz[U], dm[U];
-                unpack_cells(cdy[k], dy);
-                if (has_z) unpack_cells(cz[k], z);
-                if constexpr (MUL) unpack_cells(cm[k], mul);
-#pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const float2 f = act_value_slope(has_z ? z[u] : 0.f, ACT);
-                    // (rounded one by one: the sums' bits do not depend on which outputs are wanted)
-                    dm[u] = __fmul_rn(dy[u], f.x);
-                    dz[u] = __fmul_rn(dy[u], f.y);
-                    if constexpr (MUL) dz[u] = __fmul_rn(dz[u], mul[u]);
-                    sum[u] = __fadd_rn(sum[u], dz[u]);
-                }
-                if (d.dmul) store_cells<U, T>(d.dmul, d.dmul_type, i * d.lddmul + j, dm);
-                if (d.dz) store_cells<U, T>(d.dz, d.dz_type, i * d.lddz + j, dz);
-            }
+        for (int k = 0; k < ROWS; ++k) {
+            const uint64_t i = row + k * kActWarps;
+            if (i >= r1) break;
+            load_cells(cdy[b][k], d.dy, d.dy_type, i * d.lddy + j);
+            if (has_z) load_cells(cz[b][k], d.z, d.z_type, i * d.ldz + j);
+            if constexpr (MUL) load_cells(cm[b][k], d.mul, d.mul_type, i * d.ldmul + j);
         }
+    };
+    auto use = [&](uint64_t row, int b) {
+#pragma unroll
+        for (int k = 0; k < ROWS; ++k) {
+            const uint64_t i = row + k * kActWarps;
+            if (i >= r1) break;
+            float dy[U], z[U], mul[U], dz[U], dm[U];
+            unpack_cells(cdy[b][k], dy);
+            if (has_z) unpack_cells(cz[b][k], z);
+            if constexpr (MUL) unpack_cells(cm[b][k], mul);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const float2 f = act_value_slope(has_z ? z[u] : 0.f, ACT);
+                // (rounded one by one: the sums' bits do not depend on which outputs are wanted)
+                dm[u] = __fmul_rn(dy[u], f.x);
+                dz[u] = __fmul_rn(dy[u], f.y);
+                if constexpr (MUL) dz[u] = __fmul_rn(dz[u], mul[u]);
+                sum[u] = __fadd_rn(sum[u], dz[u]);
+            }
+            if (d.dmul) store_cells<U, T>(d.dmul, d.dmul_type, i * d.lddmul + j, dm);
+            if (d.dz) store_cells<U, T>(d.dz, d.dz_type, i * d.lddz + j, dz);
+        }
+    };
+    constexpr uint32_t kStep = kActWarps * ROWS;
+    if (j < d.cols) {
+        fetch(r0 + warp, 0);
+        for (uint64_t row = r0 + warp; row < r1; row += 2 * kStep) {
+            fetch(row + kStep, 1);
+            use(row, 0);
+            fetch(row + 2 * kStep, 0);
+            use(row + kStep, 1);
+        }
+    }
     if (!d.dbias) return;
 #pragma unroll
     for (int u = 0; u < U; ++u) s[warp][u * 32 + lane] = sum[u];

@@ -1,8 +1,8 @@
 // adamw_kernel: one optimizer step over the elements of many tensors (see cleave.h for the formula and the
 // 8-bit states).
 //
-// One warp per block of 256 elements, 8 blocks per CTA.  The work list (tensor, first block) is made once per
-// handle, so tensors of any number and size share one launch.  Lane l owns the elements 4 l .. 4 l + 3 of both
+// One warp per block of 256 elements, a CTA of 8 warps per chunk of up to 32 neighbouring blocks of one tensor.  The
+// work list (tensor, first block) is made once per handle, so tensors of any number and size share one launch.  Lane l owns the elements 4 l .. 4 l + 3 of both
 // halves of the block: every fp32 access of a warp is 512 consecutive bytes, and a block's largest magnitude is
 // a shuffle reduction inside its warp, so an 8-bit state needs no second pass.
 // Bound by the HBM's bandwidth: 30 bytes an element with fp32 states (gradient 4, weight 8, states 16, copy 2),
@@ -78,18 +78,20 @@ __device__ __forceinline__ void store4(__nv_bfloat16* dst, uint64_t e, uint64_t 
 #pragma unroll
         for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = __float2bfloat16_rn(x[i]);
 }
-template <bool WIDE>
+template <bool WIDE>                       // codes in the top bytes of c
 __device__ __forceinline__ void store4_codes(uint8_t* dst, uint64_t e, uint64_t n, const uint32_t (&c)[4]) {
-    if constexpr (WIDE) *reinterpret_cast<uint32_t*>(dst + e) = c[0] | (c[1] << 8) | (c[2] << 16) | (c[3] << 24);
+    if constexpr (WIDE)
+        *reinterpret_cast<uint32_t*>(dst + e) = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
     else
 #pragma unroll
-        for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = (uint8_t)c[i];
+        for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = (uint8_t)(c[i] >> 24);
 }
 
-__device__ __forceinline__ float warp_max_nan(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    return v;
+// largest magnitude of the warp's values; a NaN stays
+__device__ __forceinline__ float warp_abs_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
 }
 // scale of a block whose largest magnitude is `top`, and its reciprocal (both 0 when there is nothing to scale)
 __device__ __forceinline__ float2 block_scale(float top) {
@@ -97,9 +99,13 @@ __device__ __forceinline__ float2 block_scale(float top) {
     return make_float2(s, s == 0.f ? 0.f : __frcp_rn(s));
 }
 
+// What an element's code needs besides its value: 16 random bits of `word` moved to where the 20 cut bits begin.
+__device__ __forceinline__ uint32_t bits_low(uint32_t w) { return (w << 4) & 0xFFFF0u; }
+__device__ __forceinline__ uint32_t bits_high(uint32_t w) { return (w >> 12) & 0xFFFF0u; }
+
 // One block of 256 elements; WIDE: the block is whole and its buffers are aligned.
 template <bool STATE8, typename G, bool WIDE>
-__device__ __forceinline__ void adamw_block(const AdamTensor& t, uint32_t tensor, uint64_t block, const AdamStep& s, uint32_t lane) {
+__device__ __forceinline__ void adamw_block(const AdamTensor& t, float decay, uint64_t key, uint64_t block, const AdamStep& s, uint32_t lane) {
     const uint64_t n = t.numel, e0 = block * kStateBlock + lane * 4u;
     float m[2][4], r[2][4], p[2][4], g[2][4];
     float sm = 0.f, sv = 0.f;
@@ -112,7 +118,6 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, uint32_t tensor
         if constexpr (STATE8) { load4_codes<WIDE>(static_cast<const uint8_t*>(t.m), e, n, m[j]); load4_codes<WIDE>(static_cast<const uint8_t*>(t.v), e, n, r[j]); }
         else                  { load4<WIDE>(static_cast<const float*>(t.m), e, n, m[j]); load4<WIDE>(static_cast<const float*>(t.v), e, n, r[j]); }
     }
-    const float decay = (float)__dadd_rn(1.0, -__dmul_rn(s.lr, t.weight_decay));
     float top_m = 0.f, top_r = 0.f;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -140,30 +145,44 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, uint32_t tensor
         if constexpr (!STATE8) { store4<WIDE>(static_cast<float*>(t.m), e, n, m[j]); store4<WIDE>(static_cast<float*>(t.v), e, n, r[j]); }
     }
     if constexpr (STATE8) {
-        top_m = warp_max_nan(top_m);
-        top_r = warp_max_nan(top_r);
+        top_m = warp_abs_max(top_m);
+        top_r = warp_abs_max(top_r);
         const float2 bm = block_scale(top_m), bv = block_scale(top_r);
-        // a block that holds a NaN or an infinity: its scale is one, so some codes have to be NaN
-        const bool nan_m = !(top_m < INFINITY), nan_v = !(top_r < INFINITY);
-        const uint64_t key = mix64(mix64(s.base + tensor));
+        const bool odd = !(top_m < INFINITY) || !(top_r < INFINITY);       // NaN or infinity: some codes have to be NaN
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const uint64_t e = e0 + j * 128u;
-            uint32_t cm[4], cv[4];
+            float qm[4], qv[4];
+            uint32_t w[4], cm[4], cv[4];                                    // w: the element's 32 random bits
+            float least = INFINITY;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                qm[i] = __fmul_rn(m[j][i], bm.y);
+                qv[i] = __fmul_rn(r[j][i], bv.y);
+                least = fminf(fminf(least, fabsf(qm[i])), qv[i]);
+            }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const uint64_t word = mix64(key + (e >> 1) + h);
+                w[2 * h] = (uint32_t)word; w[2 * h + 1] = (uint32_t)(word >> 32);
+            }
+            if (least >= 0.015625f && !odd) {
+                // every value has three mantissa bits left: the code is bits 20-26 of its magnitude plus the random
+                // bits, less 960 << 20 (exponent bias 127 - 7).  448 and a few units above it stay below the next code.
 #pragma unroll
-                for (int o = 0; o < 2; ++o) {
-                    const int i = 2 * h + o;
-                    const uint32_t bits = (uint32_t)(word >> (32 * o));
-                    const float qm = __fmul_rn(m[j][i], bm.y), qv = __fmul_rn(r[j][i], bv.y);
-                    cm[i] = stochastic_code(qm, bits & 0xFFFFu);
-                    if (nan_m && qm != qm) cm[i] = 0x7Fu;
-                    if (qm < 0.f) cm[i] |= 0x80u;
-                    cv[i] = stochastic_code(qv, bits >> 16);
-                    if (qv > 0.f) cv[i] = max(cv[i], 1u);
-                    if (nan_v && qv != qv) cv[i] = 0x7Fu;
+                for (int i = 0; i < 4; ++i) {
+                    cm[i] = (((__float_as_uint(qm[i]) & 0x7FFFFFFFu) + bits_low(w[i]) - (960u << 20)) << 4 & 0x7F000000u) | (__float_as_uint(qm[i]) & 0x80000000u);
+                    cv[i] = (__float_as_uint(qv[i]) + bits_high(w[i]) - (960u << 20)) << 4;
+                }
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t a = stochastic_code(qm[i], w[i] & 0xFFFFu), b = stochastic_code(qv[i], w[i] >> 16);
+                    if (qm[i] < 0.f) a |= 0x80u;
+                    if (qv[i] > 0.f) b = max(b, 1u);
+                    if (qm[i] != qm[i]) a = 0x7Fu;
+                    if (qv[i] != qv[i]) b = 0x7Fu;
+                    cm[i] = a << 24; cv[i] = b << 24;
                 }
             }
             store4_codes<WIDE>(static_cast<uint8_t*>(t.m), e, n, cm);
@@ -174,27 +193,31 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, uint32_t tensor
 }
 
 template <bool STATE8, typename G>
-__global__ void __launch_bounds__(32 * kChunkBlocks)
-adamw_kernel(const AdamTensor* __restrict__ tensors, const AdamChunk* __restrict__ chunks, const __grid_constant__ AdamStep s) {
+__global__ void __launch_bounds__(32 * kChunkWarps, 3)
+adamw_kernel(const AdamTensor* __restrict__ tensors, const AdamChunk* __restrict__ chunks, uint32_t chunk_blocks, const __grid_constant__ AdamStep s) {
     const AdamChunk c = chunks[blockIdx.x];
-    const AdamTensor& t = tensors[c.tensor];
+    const AdamTensor t = tensors[c.tensor];
     const uint32_t lane = threadIdx.x & 31u;
-    const uint64_t block = (uint64_t)c.block0 + (threadIdx.x >> 5);
-    if (block * kStateBlock >= t.numel) return;
-    if (t.wide && (block + 1) * kStateBlock <= t.numel) adamw_block<STATE8, G, true>(t, c.tensor, block, s, lane);
-    else adamw_block<STATE8, G, false>(t, c.tensor, block, s, lane);
+    const uint64_t key = STATE8 ? mix64(mix64(s.base + c.tensor)) : 0ull;
+    const float decay = (float)__dadd_rn(1.0, -__dmul_rn(s.lr, t.weight_decay));
+    for (uint32_t k = threadIdx.x >> 5; k < chunk_blocks; k += kChunkWarps) {
+        const uint64_t block = (uint64_t)c.block0 + k;
+        if (block * kStateBlock >= t.numel) return;
+        if (t.wide && (block + 1) * kStateBlock <= t.numel) adamw_block<STATE8, G, true>(t, decay, key, block, s, lane);
+        else adamw_block<STATE8, G, false>(t, decay, key, block, s, lane);
+    }
 }
 
-cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, const AdamStep& s, bool state8,
-                         bool g_bf16, cudaStream_t st) {
+cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, uint32_t chunk_blocks, const AdamStep& s,
+                         bool state8, bool g_bf16, cudaStream_t st) {
     if (!n_chunks) return cudaSuccess;
-    const dim3 block(32 * kChunkBlocks);
+    const dim3 block(32 * kChunkWarps);
     if (state8) {
-        if (g_bf16) adamw_kernel<true, __nv_bfloat16><<<n_chunks, block, 0, st>>>(tensors, chunks, s);
-        else        adamw_kernel<true, float><<<n_chunks, block, 0, st>>>(tensors, chunks, s);
+        if (g_bf16) adamw_kernel<true, __nv_bfloat16><<<n_chunks, block, 0, st>>>(tensors, chunks, chunk_blocks, s);
+        else        adamw_kernel<true, float><<<n_chunks, block, 0, st>>>(tensors, chunks, chunk_blocks, s);
     } else {
-        if (g_bf16) adamw_kernel<false, __nv_bfloat16><<<n_chunks, block, 0, st>>>(tensors, chunks, s);
-        else        adamw_kernel<false, float><<<n_chunks, block, 0, st>>>(tensors, chunks, s);
+        if (g_bf16) adamw_kernel<false, __nv_bfloat16><<<n_chunks, block, 0, st>>>(tensors, chunks, chunk_blocks, s);
+        else        adamw_kernel<false, float><<<n_chunks, block, 0, st>>>(tensors, chunks, chunk_blocks, s);
     }
     return cudaGetLastError();
 }

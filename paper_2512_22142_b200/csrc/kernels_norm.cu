@@ -158,6 +158,12 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
     if constexpr (!WARP)
         for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
 
+    constexpr bool KEEP = !WARP && V <= 2;                       // a CTA takes many rows: its weights stay in registers
+    float w[KEEP ? V : 1][8];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) if (live[v]) load_weight8(d, (tid + v * nt) * 8, w[v]);
+    }
     Y* py = static_cast<Y*>(d.y) + first * d.ldy + tid * 8;
     R* ph = RES && d.h ? static_cast<R*>(d.h) + first * d.ldh + tid * 8 : nullptr;
     uint32_t it = 0, at = 0;
@@ -195,10 +201,10 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
 #pragma unroll
                 for (int i = 0; i < 8; ++i) ss = fmaf(h[v][i], h[v][i], ss);
             }
-            load_weight8(d, (tid + v * nt) * 8, hw[v]);
+            if constexpr (!KEEP) load_weight8(d, (tid + v * nt) * 8, hw[v]);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                hw[v][i] *= h[v][i];
+                hw[v][i] = h[v][i] * (KEEP ? w[KEEP ? v : 0][i] : hw[v][i]);
                 if constexpr (CODES) top = max_nan(top, fabsf(hw[v][i]));
             }
         }

@@ -10,7 +10,7 @@ using namespace cleave;
 
 struct cleave_adamw_s {
     int device = -1;
-    uint32_t state_type = 0, g_type = 0, n_chunks = 0;
+    uint32_t state_type = 0, g_type = 0, n_chunks = 0, chunk_blocks = 0;
     std::vector<AdamTensor> host;
     AdamTensor* tensors = nullptr;
     AdamChunk* chunks = nullptr;
@@ -61,7 +61,7 @@ int cleave_adamw_create(const cleave_adamw_tensor_t* t, uint32_t n, uint32_t sta
     *out = nullptr;
     if (!t || !n || !float_type(g_type) || (state_type != CLEAVE_T_F32 && state_type != CLEAVE_T_E4M3)) return CLEAVE_E_INVAL;
     const bool state8 = state_type == CLEAVE_T_E4M3;
-    uint64_t n_chunks = 0;
+    uint64_t n_blocks = 0;
     for (uint32_t i = 0; i < n; ++i) {
         if (t[i].numel == 0) continue;
         if (t[i].numel > (1ull << 40) || !std::isfinite(t[i].weight_decay)) return CLEAVE_E_INVAL;
@@ -69,26 +69,30 @@ int cleave_adamw_create(const cleave_adamw_tensor_t* t, uint32_t n, uint32_t sta
         if (!t[i].p || !aligned(t[i].p, 4) || !aligned(t[i].w, 2) || !t[i].g || !aligned(t[i].g, type_bytes(g_type)) || !t[i].m || !t[i].v ||
             !aligned(t[i].m, sb) || !aligned(t[i].v, sb)) return CLEAVE_E_INVAL;
         if (state8 != (t[i].m_scale != nullptr) || state8 != (t[i].v_scale != nullptr) || !aligned(t[i].m_scale, 4) || !aligned(t[i].v_scale, 4)) return CLEAVE_E_INVAL;
-        n_chunks += ((t[i].numel + kStateBlock - 1) / kStateBlock + kChunkBlocks - 1) / kChunkBlocks;
+        n_blocks += (t[i].numel + kStateBlock - 1) / kStateBlock;
     }
-    if (n_chunks > 0x7FFFFFFFull) return CLEAVE_E_UNSUPPORTED;
-    int rc = need_device();
-    if (rc < 0) return rc;
-    rc = 0;
+    if (n_blocks / kChunkWarps > 0x7FFFFFF0ull - n) return CLEAVE_E_UNSUPPORTED;
+    const int sms = need_device();
+    if (sms < 0) return sms;
+    int rc = 0;
+    // A warp takes up to four blocks (what is the same for a chunk is set up once), fewer when the blocks would
+    // not give every SM its three CTAs then.
+    const uint64_t full = (uint64_t)sms * 3 * kChunkWarps;
+    const uint32_t chunk_blocks = kChunkWarps * (uint32_t)(n_blocks / full < 1 ? 1 : (n_blocks / full > kChunkMost ? kChunkMost : n_blocks / full));
     cleave_adamw_s* h = new (std::nothrow) cleave_adamw_s();
     if (!h) return CLEAVE_E_NOMEM;
     try {
         std::vector<AdamChunk> chunks;
-        chunks.reserve(n_chunks);
+        chunks.reserve(n_blocks / chunk_blocks + n);
         h->host.resize(n);
         for (uint32_t i = 0; i < n; ++i) {
             AdamTensor& a = h->host[i];
             a = AdamTensor{t[i].numel, t[i].p, static_cast<__nv_bfloat16*>(t[i].w), t[i].g, t[i].m, t[i].v, t[i].m_scale, t[i].v_scale, t[i].weight_decay, 0u, 0u};
             a.wide = adam_wide(a, state_type, g_type) ? 1u : 0u;
             const uint64_t blocks = (t[i].numel + kStateBlock - 1) / kStateBlock;
-            for (uint64_t b = 0; b < blocks; b += kChunkBlocks) chunks.push_back(AdamChunk{i, (uint32_t)b});
+            for (uint64_t b = 0; b < blocks; b += chunk_blocks) chunks.push_back(AdamChunk{i, (uint32_t)b});
         }
-        h->state_type = state_type; h->g_type = g_type; h->n_chunks = (uint32_t)chunks.size();
+        h->state_type = state_type; h->g_type = g_type; h->n_chunks = (uint32_t)chunks.size(); h->chunk_blocks = chunk_blocks;
         if (cudaGetDevice(&h->device) != cudaSuccess) rc = CLEAVE_E_CUDA;
         if (!rc && (cudaMalloc(&h->tensors, n * sizeof(AdamTensor)) != cudaSuccess ||
                     cudaMalloc(&h->chunks, (chunks.empty() ? 1 : chunks.size()) * sizeof(AdamChunk)) != cudaSuccess)) rc = CLEAVE_E_NOMEM;
@@ -129,7 +133,7 @@ int cleave_adamw_step(cleave_adamw_t* h, const cleave_adamw_step_t* s, void* str
     k.eps = (float)s->eps; k.grad_scale = (float)s->grad_scale;
     k.lr = s->lr;
     k.base = s->seed + (s->step << 32);
-    return cuda_code(launch_adamw(h->tensors, h->chunks, h->n_chunks, k, h->state_type == CLEAVE_T_E4M3, h->g_type == CLEAVE_T_BF16,
+    return cuda_code(launch_adamw(h->tensors, h->chunks, h->n_chunks, h->chunk_blocks, k, h->state_type == CLEAVE_T_E4M3, h->g_type == CLEAVE_T_BF16,
                                   static_cast<cudaStream_t>(stream)));
 }
 

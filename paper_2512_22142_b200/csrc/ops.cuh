@@ -183,10 +183,10 @@ struct AdamStep {
     double lr;
     uint64_t base;                  // seed + (step << 32)
 };
-struct AdamChunk { uint32_t tensor, block0; };   // kChunkBlocks blocks of 256 elements from block0 on
-constexpr uint32_t kChunkBlocks = 8;
-cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, const AdamStep& s, bool state8,
-                         bool g_bf16, cudaStream_t st);
+struct AdamChunk { uint32_t tensor, block0; };   // a CTA's blocks of 256 elements, from block0 on
+constexpr uint32_t kChunkWarps = 8, kChunkMost = 4;      // warps of a CTA; blocks a warp takes at most
+cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, uint32_t chunk_blocks, const AdamStep& s,
+                         bool state8, bool g_bf16, cudaStream_t st);
 
 // ---- norm, rows in 8 bits, epilogue backward ---------------------------------------------------------
 cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, int sms, cudaStream_t st);   // sms: the device's SM count
