@@ -1,8 +1,9 @@
 // Backward pass of the product's epilogue (see cleave.h): dz, the multiplier's gradient, the bias gradient.
 //
-// Bound by the HBM's bandwidth (dy, z, mul read once; dz, dmul written once).  A warp takes U columns a lane (8
-// where rows are whole 16-byte groups, else 1: any size, stride or alignment) and, with the seven other warps of
-// its CTA, the rows of a band; several rows of each operand are asked for before the first is used.  The bias
+// Bound by the HBM's bandwidth (dy, z, mul read once; dz, dmul written once).  A warp takes 8 columns a lane (where
+// rows are whole 16-byte groups, else one) and, with the seven other warps of its CTA, the rows of a band.  In the
+// wide form the operands' next rows are on their way to shared memory while a row is used -- each thread copies and
+// reads its own groups only, so there is no barrier, and the bytes in flight do not cost registers.  The bias
 // gradient stays in registers over the band's rows, the CTA's warps are joined in shared memory, and a band's sums
 // are one row of the workspace, added in order by sum_parts_kernel.
 #include "ops.cuh"
@@ -19,114 +20,163 @@ uint32_t act_backward_parts(uint64_t rows, uint32_t cols) {
     return (uint32_t)(bands < most ? bands : most);
 }
 
-// U elements of an operand: raw (what stays in flight) and as fp32.  The wide form is typed; U = 1 takes the type
-// from the launch (a uniform branch).
-template <int U, typename T> struct Cells { Raw8<T> raw; };
-template <typename T> struct Cells<1, T> { float raw; };
-template <int U, typename T>
-__device__ __forceinline__ void load_cells(Cells<U, T>& c, const void* p, uint32_t type, uint64_t at) {
-    if constexpr (U == 1) c.raw = load_as(p, type, at);
-    else c.raw = load_raw8(static_cast<const T*>(p) + at);
-}
-template <int U, typename T>
-__device__ __forceinline__ void unpack_cells(const Cells<U, T>& c, float (&x)[U]) {
-    if constexpr (U == 1) x[0] = c.raw;
-    else unpack8(c.raw, x);
-}
-template <int U, typename T>
-__device__ __forceinline__ void store_cells(void* p, uint32_t type, uint64_t at, const float (&x)[U]) {
-    if constexpr (U == 1) store_as(p, type, at, x[0]);
-    else store8(static_cast<T*>(p) + at, x);
-}
-
-// D: type of dy; T: type of z, mul, dz and dmul (wide form: one type).  Rows in flight per warp and operand: two
-// batches of ROWS.
-template <int U, typename D, typename T, uint32_t ACT, bool MUL>
-__global__ void __launch_bounds__(32 * kActWarps, MUL ? 2 : 3) act_backward_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
-    __shared__ float s[kActWarps][32 * U];
-    constexpr int ROWS = U > 1 && sizeof(T) == 4 ? 1 : 2;
+// Column sums of a CTA's warps, joined in warp order into the band's row of the workspace.
+template <int U>
+__device__ __forceinline__ void join_sums(const float (&sum)[U], float (*s)[32 * U], float* __restrict__ ws, uint64_t cols) {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-    const uint64_t j = ((uint64_t)blockIdx.x * 32u + lane) * U;
-    const uint64_t band = (d.rows + gridDim.y - 1) / gridDim.y, r0 = blockIdx.y * band, r1 = r0 + band < d.rows ? r0 + band : d.rows;
-    const bool has_z = ACT != CLEAVE_ACT_NONE || d.z;
-    float sum[U];
-#pragma unroll
-    for (int i = 0; i < U; ++i) sum[i] = 0.f;
-    // two batches of ROWS rows: the next one is asked for before the first is used
-    Cells<U, D> cdy[2][ROWS];
-    Cells<U, T> cz[2][ROWS], cm[2][ROWS];
-    auto fetch = [&](uint64_t row, int b) {
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            const uint64_t i = row + k * kActWarps;
-            if (i >= r1) break;
-            load_cells(cdy[b][k], d.dy, d.dy_type, i * d.lddy + j);
-            if (has_z) load_cells(cz[b][k], d.z, d.z_type, i * d.ldz + j);
-            if constexpr (MUL) load_cells(cm[b][k], d.mul, d.mul_type, i * d.ldmul + j);
-        }
-    };
-    auto use = [&](uint64_t row, int b) {
-#pragma unroll
-        for (int k = 0; k < ROWS; ++k) {
-            const uint64_t i = row + k * kActWarps;
-            if (i >= r1) break;
-            float dy[U], z[U], mul[U], dz[U], dm[U];
-            unpack_cells(cdy[b][k], dy);
-            if (has_z) unpack_cells(cz[b][k], z);
-            if constexpr (MUL) unpack_cells(cm[b][k], mul);
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float2 f = act_value_slope(has_z ? z[u] : 0.f, ACT);
-                // (rounded one by one: the sums' bits do not depend on which outputs are wanted)
-                dm[u] = __fmul_rn(dy[u], f.x);
-                dz[u] = __fmul_rn(dy[u], f.y);
-                if constexpr (MUL) dz[u] = __fmul_rn(dz[u], mul[u]);
-                sum[u] = __fadd_rn(sum[u], dz[u]);
-            }
-            if (d.dmul) store_cells<U, T>(d.dmul, d.dmul_type, i * d.lddmul + j, dm);
-            if (d.dz) store_cells<U, T>(d.dz, d.dz_type, i * d.lddz + j, dz);
-        }
-    };
-    constexpr uint32_t kStep = kActWarps * ROWS;
-    if (j < d.cols) {
-        fetch(r0 + warp, 0);
-        for (uint64_t row = r0 + warp; row < r1; row += 2 * kStep) {
-            fetch(row + kStep, 1);
-            use(row, 0);
-            fetch(row + 2 * kStep, 0);
-            use(row + kStep, 1);
-        }
-    }
-    if (!d.dbias) return;
 #pragma unroll
     for (int u = 0; u < U; ++u) s[warp][u * 32 + lane] = sum[u];
     __syncthreads();
     for (uint32_t c = threadIdx.x; c < 32u * U; c += 32 * kActWarps) {         // column c of the CTA: lane c / U, cell c % U
         const uint32_t at = (c % U) * 32u + c / U;
         const uint64_t col = (uint64_t)blockIdx.x * 32u * U + c;
-        if (col >= d.cols) continue;
+        if (col >= cols) continue;
         float t = s[0][at];
 #pragma unroll
         for (int w = 1; w < (int)kActWarps; ++w) t += s[w][at];
-        ws[(uint64_t)blockIdx.y * d.cols + col] = t;
+        ws[(uint64_t)blockIdx.y * cols + col] = t;
     }
+}
+// dz and dmul of one element (rounded one by one: the sums' bits do not depend on which outputs are wanted)
+template <uint32_t ACT, bool MUL>
+__device__ __forceinline__ void act_cell(float dy, float z, float mul, float& dz, float& dm, float& sum) {
+    const float2 f = act_value_slope(z, ACT);
+    dm = __fmul_rn(dy, f.x);
+    dz = __fmul_rn(dy, f.y);
+    if constexpr (MUL) dz = __fmul_rn(dz, mul);
+    sum = __fadd_rn(sum, dz);
+}
+struct Band { uint64_t r0, r1; };
+__device__ __forceinline__ Band this_band(uint64_t rows) {
+    const uint64_t band = (rows + gridDim.y - 1) / gridDim.y, r0 = blockIdx.y * band;
+    return Band{r0, r0 + band < rows ? r0 + band : rows};
 }
 
-template <int U, typename D, typename T, bool MUL>
-void launch_act(const cleave_act_backward_t& d, float* ws, uint32_t parts, cudaStream_t st) {
-    const dim3 grid((d.cols + 32 * U - 1) / (32 * U), parts), block(32 * kActWarps);
-    switch (d.act) {
-        case CLEAVE_ACT_RELU: act_backward_kernel<U, D, T, CLEAVE_ACT_RELU, MUL><<<grid, block, 0, st>>>(d, ws); break;
-        case CLEAVE_ACT_GELU: act_backward_kernel<U, D, T, CLEAVE_ACT_GELU, MUL><<<grid, block, 0, st>>>(d, ws); break;
-        case CLEAVE_ACT_GELU_TANH: act_backward_kernel<U, D, T, CLEAVE_ACT_GELU_TANH, MUL><<<grid, block, 0, st>>>(d, ws); break;
-        case CLEAVE_ACT_SILU: act_backward_kernel<U, D, T, CLEAVE_ACT_SILU, MUL><<<grid, block, 0, st>>>(d, ws); break;
-        default: act_backward_kernel<U, D, T, CLEAVE_ACT_NONE, MUL><<<grid, block, 0, st>>>(d, ws); break;
-    }
+// Any size, stride and alignment: a lane's column, four rows asked for at a time.
+template <uint32_t ACT, bool MUL>
+__global__ void __launch_bounds__(32 * kActWarps) act_backward_any_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
+    __shared__ float s[kActWarps][32];
+    constexpr int ROWS = 4;
+    const uint64_t j = (uint64_t)blockIdx.x * 32u + (threadIdx.x & 31u);
+    const Band b = this_band(d.rows);
+    const bool has_z = ACT != CLEAVE_ACT_NONE || d.z;
+    float sum[1] = {0.f};
+    if (j < d.cols)
+        for (uint64_t row = b.r0 + (threadIdx.x >> 5); row < b.r1; row += kActWarps * ROWS) {
+            float dy[ROWS], z[ROWS], mul[ROWS];
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                const uint64_t i = row + k * kActWarps;
+                if (i >= b.r1) break;
+                dy[k] = load_as(d.dy, d.dy_type, i * d.lddy + j);
+                z[k] = has_z ? load_as(d.z, d.z_type, i * d.ldz + j) : 0.f;
+                mul[k] = MUL ? load_as(d.mul, d.mul_type, i * d.ldmul + j) : 1.f;
+            }
+#pragma unroll
+            for (int k = 0; k < ROWS; ++k) {
+                const uint64_t i = row + k * kActWarps;
+                if (i >= b.r1) break;
+                float dz, dm;
+                act_cell<ACT, MUL>(dy[k], z[k], mul[k], dz, dm, sum[0]);
+                if (d.dmul) store_as(d.dmul, d.dmul_type, i * d.lddmul + j, dm);
+                if (d.dz) store_as(d.dz, d.dz_type, i * d.lddz + j, dz);
+            }
+        }
+    if (d.dbias) join_sums<1>(sum, s, ws, d.cols);
 }
-template <int U, typename D, typename T>
-void launch_act(const cleave_act_backward_t& d, float* ws, uint32_t parts, cudaStream_t st) {
-    if (d.mul) launch_act<U, D, T, true>(d, ws, parts, st);
-    else launch_act<U, D, T, false>(d, ws, parts, st);
+
+// Rows of whole 16-byte groups: a lane's 8 columns; STAGES rows of each operand on their way to shared memory.
+// D: type of dy; T: the one type of z, mul, dz and dmul.
+template <typename D, typename T, uint32_t ACT, bool MUL, int STAGES>
+__global__ void __launch_bounds__(32 * kActWarps) act_backward_wide_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float s[kActWarps][32 * 8];
+    constexpr uint32_t BD = sizeof(D) * 8, BT = sizeof(T) * 8, NT = MUL ? 2 : 1, STAGE = 32 * (BD + NT * BT);
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint64_t j = ((uint64_t)blockIdx.x * 32u + lane) * 8u;
+    const Band b = this_band(d.rows);
+    const bool has_z = ACT != CLEAVE_ACT_NONE || d.z;
+    float sum[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+    if (j < d.cols) {
+        const uint64_t first = b.r0 + warp;
+        const D* pd = static_cast<const D*>(d.dy) + first * d.lddy + j;
+        const T* pz = has_z ? static_cast<const T*>(d.z) + first * d.ldz + j : nullptr;
+        const T* pm = MUL ? static_cast<const T*>(d.mul) + first * d.ldmul + j : nullptr;
+        T* odz = d.dz ? static_cast<T*>(d.dz) + first * d.lddz + j : nullptr;
+        T* odm = d.dmul ? static_cast<T*>(d.dmul) + first * d.lddmul + j : nullptr;
+        uint8_t* mine = ring + warp * (STAGES * STAGE);
+        const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+        uint64_t ahead = first;
+        auto fetch = [&](uint32_t at) {
+            if (ahead < b.r1) {
+#pragma unroll
+                for (uint32_t x = 0; x < BD; x += 16) cp_async<16>(mine_at + at + lane * BD + x, reinterpret_cast<const uint8_t*>(pd) + x);
+#pragma unroll
+                for (uint32_t x = 0; x < BT; x += 16) {
+                    if (has_z) cp_async<16>(mine_at + at + 32 * BD + lane * BT + x, reinterpret_cast<const uint8_t*>(pz) + x);
+                    if constexpr (MUL) cp_async<16>(mine_at + at + 32 * (BD + BT) + lane * BT + x, reinterpret_cast<const uint8_t*>(pm) + x);
+                }
+                ahead += kActWarps;
+                pd += kActWarps * d.lddy;
+                if (has_z) pz += kActWarps * d.ldz;
+                if constexpr (MUL) pm += kActWarps * d.ldmul;
+            }
+            cp_async_commit();
+        };
+#pragma unroll
+        for (int k = 0; k < STAGES; ++k) fetch(k * STAGE);
+        uint32_t at = 0;
+        for (uint64_t row = first; row < b.r1; row += kActWarps) {
+            cp_async_wait<STAGES - 1>();
+            float dy[8], z[8], mul[8], dz[8], dm[8];
+            unpack8(*reinterpret_cast<const Raw8<D>*>(mine + at + lane * BD), dy);
+            if (has_z) unpack8(*reinterpret_cast<const Raw8<T>*>(mine + at + 32 * BD + lane * BT), z);
+            if constexpr (MUL) unpack8(*reinterpret_cast<const Raw8<T>*>(mine + at + 32 * (BD + BT) + lane * BT), mul);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) act_cell<ACT, MUL>(dy[u], has_z ? z[u] : 0.f, MUL ? mul[u] : 1.f, dz[u], dm[u], sum[u]);
+            fetch(at);                                           // the stage's values have been used
+            at = at + STAGE == STAGES * STAGE ? 0 : at + STAGE;
+            if (odm) { store8(odm, dm); odm += kActWarps * d.lddmul; }
+            if (odz) { store8(odz, dz); odz += kActWarps * d.lddz; }
+        }
+    }
+    if (d.dbias) join_sums<8>(sum, s, ws, d.cols);
+}
+
+template <typename D, typename T, uint32_t ACT, bool MUL>
+cudaError_t launch_act_wide(const cleave_act_backward_t& d, float* ws, uint32_t parts, cudaStream_t st) {
+    // 64 to 72 KB a CTA: three CTAs an SM
+    constexpr uint32_t stage = 32 * (sizeof(D) * 8 + (MUL ? 2 : 1) * sizeof(T) * 8);
+    constexpr int STAGES = 64 * 1024 / (kActWarps * stage) > 8 ? 8 : 64 * 1024 / (kActWarps * stage);
+    auto kernel = act_backward_wide_kernel<D, T, ACT, MUL, STAGES>;
+    constexpr uint32_t smem = kActWarps * STAGES * stage;
+    static SmemLimit limit;
+    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<dim3((d.cols + 255) / 256, parts), 32 * kActWarps, smem, st>>>(d, ws);
+    return cudaGetLastError();
+}
+template <uint32_t ACT, bool MUL>
+cudaError_t launch_act(const cleave_act_backward_t& d, float* ws, uint32_t parts, bool wide, uint32_t type, cudaStream_t st) {
+    if (!wide) {
+        act_backward_any_kernel<ACT, MUL><<<dim3((d.cols + 31) / 32, parts), 32 * kActWarps, 0, st>>>(d, ws);
+        return cudaGetLastError();
+    }
+    if (d.dy_type == CLEAVE_T_F32)
+        return type == CLEAVE_T_F32 ? launch_act_wide<float, float, ACT, MUL>(d, ws, parts, st) : launch_act_wide<float, __nv_bfloat16, ACT, MUL>(d, ws, parts, st);
+    return type == CLEAVE_T_F32 ? launch_act_wide<__nv_bfloat16, float, ACT, MUL>(d, ws, parts, st) : launch_act_wide<__nv_bfloat16, __nv_bfloat16, ACT, MUL>(d, ws, parts, st);
+}
+template <bool MUL>
+cudaError_t launch_act(const cleave_act_backward_t& d, float* ws, uint32_t parts, bool wide, uint32_t type, cudaStream_t st) {
+    switch (d.act) {
+        case CLEAVE_ACT_RELU: return launch_act<CLEAVE_ACT_RELU, MUL>(d, ws, parts, wide, type, st);
+        case CLEAVE_ACT_GELU: return launch_act<CLEAVE_ACT_GELU, MUL>(d, ws, parts, wide, type, st);
+        case CLEAVE_ACT_GELU_TANH: return launch_act<CLEAVE_ACT_GELU_TANH, MUL>(d, ws, parts, wide, type, st);
+        case CLEAVE_ACT_SILU: return launch_act<CLEAVE_ACT_SILU, MUL>(d, ws, parts, wide, type, st);
+        default: return launch_act<CLEAVE_ACT_NONE, MUL>(d, ws, parts, wide, type, st);
+    }
 }
 
 cudaError_t launch_act_backward(const cleave_act_backward_t& d, float* ws, cudaStream_t st) {
@@ -137,11 +187,8 @@ cudaError_t launch_act_backward(const cleave_act_backward_t& d, float* ws, cudaS
     auto fits = [&](const void* p, uint32_t t, uint64_t ld) { return !p || (t == type && rows_wide(p, ld, t)); };
     const bool wide = d.cols % 8 == 0 && rows_wide(d.dy, d.lddy, d.dy_type) && fits(d.z, d.z_type, d.ldz) && fits(d.mul, d.mul_type, d.ldmul) &&
                       fits(d.dz, d.dz_type, d.lddz) && fits(d.dmul, d.dmul_type, d.lddmul);
-    if (!parts) { }
-    else if (!wide) launch_act<1, float, float>(d, ws, parts, st);
-    else if (d.dy_type == CLEAVE_T_F32) { if (type == CLEAVE_T_F32) launch_act<8, float, float>(d, ws, parts, st); else launch_act<8, float, __nv_bfloat16>(d, ws, parts, st); }
-    else { if (type == CLEAVE_T_F32) launch_act<8, __nv_bfloat16, float>(d, ws, parts, st); else launch_act<8, __nv_bfloat16, __nv_bfloat16>(d, ws, parts, st); }
-    cudaError_t e = cudaGetLastError();
+    cudaError_t e = cudaSuccess;
+    if (parts) e = d.mul ? launch_act<true>(d, ws, parts, wide, type, st) : launch_act<false>(d, ws, parts, wide, type, st);
     if (e != cudaSuccess || !d.dbias) return e;
     return launch_sum_parts(ws, parts, d.cols, d.dbias, st);
 }

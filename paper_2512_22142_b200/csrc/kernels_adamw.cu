@@ -9,6 +9,8 @@
 // 18 with 8-bit ones.
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "ops.cuh"
 
 namespace cleave {
@@ -31,68 +33,56 @@ __device__ __forceinline__ uint32_t stochastic_code(float q, uint32_t u) {
     return min(code, 0x7Eu);
 }
 
-template <bool WIDE, typename T>
-__device__ __forceinline__ void load4(const T* src, uint64_t e, uint64_t n, float (&x)[4]) {
-    if constexpr (WIDE) {
-        if constexpr (sizeof(T) == 4) {
-            const float4 v = *reinterpret_cast<const float4*>(src + e);
-            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-        } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(src + e);
-            const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&v.y));
-            x[0] = a.x; x[1] = a.y; x[2] = b.x; x[3] = b.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = e + i < n ? to_f32<T>(src[e + i]) : 0.f;
-    }
-}
-template <bool WIDE>
-__device__ __forceinline__ void load4_codes(const uint8_t* src, uint64_t e, uint64_t n, float (&x)[4]) {
-    if constexpr (WIDE) {
-        const uint32_t c = *reinterpret_cast<const uint32_t*>(src + e);
+// Four consecutive elements of a lane.  `whole`: all four exist and the buffer allows one wide access.
+template <typename T>
+__device__ __forceinline__ void unpack4(const T* p, float (&x)[4]) {
+    if constexpr (sizeof(T) == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
+    } else if constexpr (sizeof(T) == 2) {
+        const uint2 v = *reinterpret_cast<const uint2*>(p);
+        x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+        x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
+    } else {                                                          // E4M3 codes
+        const uint32_t c = *reinterpret_cast<const uint32_t*>(p);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const __half2_raw r = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(h ? c >> 16 : c & 0xFFFFu), __NV_E4M3);
             const float2 f = __half22float2(__half2(r));
             x[2 * h] = f.x; x[2 * h + 1] = f.y;
         }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = e + i < n ? e4m3_value(src[e + i]) : 0.f;
     }
 }
-template <bool WIDE>
-__device__ __forceinline__ void store4(float* dst, uint64_t e, uint64_t n, const float (&x)[4]) {
-    if constexpr (WIDE) *reinterpret_cast<float4*>(dst + e) = make_float4(x[0], x[1], x[2], x[3]);
+__device__ __forceinline__ float element(const float* p) { return *p; }
+__device__ __forceinline__ float element(const __nv_bfloat16* p) { return __bfloat162float(*p); }
+__device__ __forceinline__ float element(const uint8_t* p) { return e4m3_value(*p); }
+template <typename T>
+__device__ __forceinline__ void load4(const T* src, uint64_t e, uint64_t n, bool whole, float (&x)[4]) {
+    if (whole) unpack4(src + e, x);
+    else
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = e + i < n ? element(src + e + i) : 0.f;
+}
+__device__ __forceinline__ void store4(float* dst, uint64_t e, uint64_t n, bool whole, const float (&x)[4]) {
+    if (whole) *reinterpret_cast<float4*>(dst + e) = make_float4(x[0], x[1], x[2], x[3]);
     else
 #pragma unroll
         for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = x[i];
 }
-template <bool WIDE>
-__device__ __forceinline__ void store4(__nv_bfloat16* dst, uint64_t e, uint64_t n, const float (&x)[4]) {
-    if constexpr (WIDE) {
-        const __nv_bfloat162 a = __floats2bfloat162_rn(x[0], x[1]), b = __floats2bfloat162_rn(x[2], x[3]);
-        *reinterpret_cast<uint2*>(dst + e) = make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-    } else
+__device__ __forceinline__ void store4(__nv_bfloat16* dst, uint64_t e, uint64_t n, bool whole, const float (&x)[4]) {
+    if (whole) *reinterpret_cast<uint2*>(dst + e) = make_uint2(bf16x2(x[0], x[1]), bf16x2(x[2], x[3]));
+    else
 #pragma unroll
         for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = __float2bfloat16_rn(x[i]);
 }
-template <bool WIDE>                       // codes in the top bytes of c
-__device__ __forceinline__ void store4_codes(uint8_t* dst, uint64_t e, uint64_t n, const uint32_t (&c)[4]) {
-    if constexpr (WIDE)
-        *reinterpret_cast<uint32_t*>(dst + e) = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
+// codes in the top bytes of c
+__device__ __forceinline__ void store4(uint8_t* dst, uint64_t e, uint64_t n, bool whole, const uint32_t (&c)[4]) {
+    if (whole) *reinterpret_cast<uint32_t*>(dst + e) = __byte_perm(__byte_perm(c[0], c[1], 0x0073), __byte_perm(c[2], c[3], 0x0073), 0x5410);
     else
 #pragma unroll
         for (int i = 0; i < 4; ++i) if (e + i < n) dst[e + i] = (uint8_t)(c[i] >> 24);
 }
 
-// largest magnitude of the warp's values; a NaN stays
-__device__ __forceinline__ float warp_abs_max(float v) {
-    float r;
-    asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
-    return r;
-}
 // scale of a block whose largest magnitude is `top`, and its reciprocal (both 0 when there is nothing to scale)
 __device__ __forceinline__ float2 block_scale(float top) {
     const float s = top < 0x1p-100f ? 0.f : __fmul_rn(top, 1.f / kE4M3Max);
@@ -103,21 +93,13 @@ __device__ __forceinline__ float2 block_scale(float top) {
 __device__ __forceinline__ uint32_t bits_low(uint32_t w) { return (w << 4) & 0xFFFF0u; }
 __device__ __forceinline__ uint32_t bits_high(uint32_t w) { return (w >> 12) & 0xFFFF0u; }
 
-// One block of 256 elements; WIDE: the block is whole and its buffers are aligned.
-template <bool STATE8, typename G, bool WIDE>
-__device__ __forceinline__ void adamw_block(const AdamTensor& t, float decay, uint64_t key, uint64_t block, const AdamStep& s, uint32_t lane) {
+// The update of one block of 256 elements whose values the warp holds (lane: elements 4 lane .. + 3 of both halves),
+// and its stores.  WHOLE: the block is complete and its buffers are aligned.
+template <bool STATE8, bool WHOLE>
+__device__ __forceinline__ void adamw_block(const AdamTensor& t, float decay, uint64_t key, uint64_t block, const AdamStep& s, uint32_t lane,
+                                            float (&g)[2][4], float (&p)[2][4], float (&m)[2][4], float (&r)[2][4], float sm, float sv) {
     const uint64_t n = t.numel, e0 = block * kStateBlock + lane * 4u;
-    float m[2][4], r[2][4], p[2][4], g[2][4];
-    float sm = 0.f, sv = 0.f;
-    if constexpr (STATE8) { sm = t.m_scale[block]; sv = t.v_scale[block]; }
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const uint64_t e = e0 + j * 128u;
-        load4<WIDE>(static_cast<const G*>(t.g), e, n, g[j]);
-        load4<WIDE>(t.p, e, n, p[j]);
-        if constexpr (STATE8) { load4_codes<WIDE>(static_cast<const uint8_t*>(t.m), e, n, m[j]); load4_codes<WIDE>(static_cast<const uint8_t*>(t.v), e, n, r[j]); }
-        else                  { load4<WIDE>(static_cast<const float*>(t.m), e, n, m[j]); load4<WIDE>(static_cast<const float*>(t.v), e, n, r[j]); }
-    }
+    const bool whole[2] = {WHOLE || (t.wide && e0 + 4 <= n), WHOLE || (t.wide && e0 + 132 <= n)};
     float top_m = 0.f, top_r = 0.f;
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
@@ -140,9 +122,9 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, float decay, ui
             else r[j][i] = vo;
         }
         const uint64_t e = e0 + j * 128u;
-        store4<WIDE>(t.p, e, n, p[j]);
-        if (t.w) store4<WIDE>(t.w, e, n, p[j]);
-        if constexpr (!STATE8) { store4<WIDE>(static_cast<float*>(t.m), e, n, m[j]); store4<WIDE>(static_cast<float*>(t.v), e, n, r[j]); }
+        store4(t.p, e, n, whole[j], p[j]);
+        if (t.w) store4(t.w, e, n, whole[j], p[j]);
+        if constexpr (!STATE8) { store4(static_cast<float*>(t.m), e, n, whole[j], m[j]); store4(static_cast<float*>(t.v), e, n, whole[j], r[j]); }
     }
     if constexpr (STATE8) {
         top_m = warp_abs_max(top_m);
@@ -185,41 +167,120 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, float decay, ui
                     cm[i] = a << 24; cv[i] = b << 24;
                 }
             }
-            store4_codes<WIDE>(static_cast<uint8_t*>(t.m), e, n, cm);
-            store4_codes<WIDE>(static_cast<uint8_t*>(t.v), e, n, cv);
+            store4(static_cast<uint8_t*>(t.m), e, n, whole[j], cm);
+            store4(static_cast<uint8_t*>(t.v), e, n, whole[j], cv);
         }
         if (lane == 0) { t.m_scale[block] = bm.x; t.v_scale[block] = bv.x; }
     }
 }
 
+// A warp's ring of blocks on their way to shared memory: each lane copies and reads its own elements only.
+template <bool STATE8, typename G> struct AdamStage {
+    using S = typename std::conditional<STATE8, uint8_t, float>::type;
+    static constexpr uint32_t g = 256 * 4, m = g + 256 * sizeof(G), v = m + 256 * sizeof(S), scales = v + 256 * sizeof(S);
+    static constexpr uint32_t bytes = scales + (STATE8 ? 2 * 32 * 4 : 0);
+    static constexpr int stages = 3;
+};
+
 template <bool STATE8, typename G>
 __global__ void __launch_bounds__(32 * kChunkWarps, 3)
 adamw_kernel(const AdamTensor* __restrict__ tensors, const AdamChunk* __restrict__ chunks, uint32_t chunk_blocks, const __grid_constant__ AdamStep s) {
+    using Stage = AdamStage<STATE8, G>;
+    using S = typename Stage::S;
+    extern __shared__ __align__(16) uint8_t ring[];
     const AdamChunk c = chunks[blockIdx.x];
     const AdamTensor t = tensors[c.tensor];
-    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint64_t key = STATE8 ? mix64(mix64(s.base + c.tensor)) : 0ull;
     const float decay = (float)__dadd_rn(1.0, -__dmul_rn(s.lr, t.weight_decay));
-    for (uint32_t k = threadIdx.x >> 5; k < chunk_blocks; k += kChunkWarps) {
-        const uint64_t block = (uint64_t)c.block0 + k;
-        if (block * kStateBlock >= t.numel) return;
-        if (t.wide && (block + 1) * kStateBlock <= t.numel) adamw_block<STATE8, G, true>(t, decay, key, block, s, lane);
-        else adamw_block<STATE8, G, false>(t, decay, key, block, s, lane);
+    const uint64_t all = (t.numel + kStateBlock - 1) / kStateBlock;
+    const uint64_t end = min(all, (uint64_t)c.block0 + chunk_blocks);
+    const uint64_t whole_end = t.wide ? min(end, t.numel / kStateBlock) : c.block0;        // blocks below it go through the ring
+    uint64_t block = (uint64_t)c.block0 + warp, ahead = block;
+    const G* const tg = static_cast<const G*>(t.g);
+    const S* const tm = static_cast<const S*>(t.m);
+    const S* const tv = static_cast<const S*>(t.v);
+    uint8_t* const mine = ring + warp * (Stage::stages * Stage::bytes);
+    const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
+    auto fetch = [&](uint32_t at) {
+        if (ahead < whole_end) {
+            const uint64_t e = ahead * kStateBlock + lane * 4u;
+            const uint32_t to = mine_at + at;
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j) {
+                const uint32_t o = lane * 4u + j * 128u;
+                cp_async<16>(to + o * 4u, t.p + e + j * 128u);
+                cp_async<4 * sizeof(G)>(to + Stage::g + o * (uint32_t)sizeof(G), tg + e + j * 128u);
+                cp_async<4 * sizeof(S)>(to + Stage::m + o * (uint32_t)sizeof(S), tm + e + j * 128u);
+                cp_async<4 * sizeof(S)>(to + Stage::v + o * (uint32_t)sizeof(S), tv + e + j * 128u);
+            }
+            if constexpr (STATE8) {
+                cp_async<4>(to + Stage::scales + lane * 4u, t.m_scale + ahead);
+                cp_async<4>(to + Stage::scales + 128u + lane * 4u, t.v_scale + ahead);
+            }
+            ahead += kChunkWarps;
+        }
+        cp_async_commit();
+    };
+#pragma unroll
+    for (int k = 0; k < Stage::stages; ++k) fetch(k * Stage::bytes);
+    uint32_t at = 0;
+    float g[2][4], p[2][4], m[2][4], r[2][4], sm = 0.f, sv = 0.f;
+    for (; block < whole_end; block += kChunkWarps) {
+        cp_async_wait<Stage::stages - 1>();
+        const uint8_t* stage = mine + at;
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+            const uint32_t o = lane * 4u + j * 128u;
+            unpack4(reinterpret_cast<const float*>(stage) + o, p[j]);
+            unpack4(reinterpret_cast<const G*>(stage + Stage::g) + o, g[j]);
+            unpack4(reinterpret_cast<const S*>(stage + Stage::m) + o, m[j]);
+            unpack4(reinterpret_cast<const S*>(stage + Stage::v) + o, r[j]);
+        }
+        if constexpr (STATE8) {
+            sm = *reinterpret_cast<const float*>(stage + Stage::scales + lane * 4u);
+            sv = *reinterpret_cast<const float*>(stage + Stage::scales + 128u + lane * 4u);
+        }
+        adamw_block<STATE8, true>(t, decay, key, block, s, lane, g, p, m, r, sm, sv);
+        __syncwarp();
+        fetch(at);                                                    // the stage's values have been used
+        at = at + Stage::bytes == Stage::stages * Stage::bytes ? 0 : at + Stage::bytes;
     }
+    // a block that is not whole, or buffers that are not aligned: straight from global memory
+    for (; block < end; block += kChunkWarps) {
+        if constexpr (STATE8) { sm = t.m_scale[block]; sv = t.v_scale[block]; }
+#pragma unroll
+        for (uint32_t j = 0; j < 2; ++j) {
+            const uint64_t e = block * kStateBlock + lane * 4u + j * 128u;
+            const bool whole = t.wide && e + 4 <= t.numel;
+            load4(tg, e, t.numel, whole, g[j]);
+            load4(const_cast<const float*>(t.p), e, t.numel, whole, p[j]);
+            load4(tm, e, t.numel, whole, m[j]);
+            load4(tv, e, t.numel, whole, r[j]);
+        }
+        adamw_block<STATE8, false>(t, decay, key, block, s, lane, g, p, m, r, sm, sv);
+    }
+}
+
+template <bool STATE8, typename G>
+cudaError_t launch_adamw_as(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, uint32_t chunk_blocks, const AdamStep& s, cudaStream_t st) {
+    using Stage = AdamStage<STATE8, G>;
+    constexpr uint32_t smem = kChunkWarps * Stage::stages * Stage::bytes;
+    auto kernel = adamw_kernel<STATE8, G>;
+    static SmemLimit limit;
+    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), smem);
+    if (e != cudaSuccess) return e;
+    kernel<<<n_chunks, 32 * kChunkWarps, smem, st>>>(tensors, chunks, chunk_blocks, s);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, uint32_t chunk_blocks, const AdamStep& s,
                          bool state8, bool g_bf16, cudaStream_t st) {
     if (!n_chunks) return cudaSuccess;
-    const dim3 block(32 * kChunkWarps);
-    if (state8) {
-        if (g_bf16) adamw_kernel<true, __nv_bfloat16><<<n_chunks, block, 0, st>>>(tensors, chunks, chunk_blocks, s);
-        else        adamw_kernel<true, float><<<n_chunks, block, 0, st>>>(tensors, chunks, chunk_blocks, s);
-    } else {
-        if (g_bf16) adamw_kernel<false, __nv_bfloat16><<<n_chunks, block, 0, st>>>(tensors, chunks, chunk_blocks, s);
-        else        adamw_kernel<false, float><<<n_chunks, block, 0, st>>>(tensors, chunks, chunk_blocks, s);
-    }
-    return cudaGetLastError();
+    if (state8) return g_bf16 ? launch_adamw_as<true, __nv_bfloat16>(tensors, chunks, n_chunks, chunk_blocks, s, st)
+                              : launch_adamw_as<true, float>(tensors, chunks, n_chunks, chunk_blocks, s, st);
+    return g_bf16 ? launch_adamw_as<false, __nv_bfloat16>(tensors, chunks, n_chunks, chunk_blocks, s, st)
+                  : launch_adamw_as<false, float>(tensors, chunks, n_chunks, chunk_blocks, s, st);
 }
 
 }  // namespace cleave

@@ -17,22 +17,6 @@ namespace cleave {
 
 constexpr uint32_t kRowThreads = 256;
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
-__device__ __forceinline__ float warp_sum(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
-    return v;
-}
-__device__ __forceinline__ float warp_max(float v) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = max_nan(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    return v;
-}
 // Sum / NaN-keeping maximum over the CTA; every thread receives it.  `buf` holds one value per warp and may be
 // reused after the call (it ends with a barrier).
 __device__ __forceinline__ float cta_sum(float v, float* buf) {
@@ -45,7 +29,7 @@ __device__ __forceinline__ float cta_sum(float v, float* buf) {
     return s;
 }
 __device__ __forceinline__ float cta_max_nan(float v, float* buf) {
-    v = warp_max(v);
+    v = warp_abs_max(v);
     if ((threadIdx.x & 31u) == 0) buf[threadIdx.x >> 5] = v;
     __syncthreads();
     float s = buf[0];
@@ -145,10 +129,10 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
             for (int v = 0; v < V; ++v) {
                 if (!live[v]) continue;
 #pragma unroll
-                for (uint32_t b = 0; b < BX; b += 16) cp_async16(slot_at + at + v * nt * BX + b, px + v * nt * BX + b);
+                for (uint32_t b = 0; b < BX; b += 16) cp_async<16>(slot_at + at + v * nt * BX + b, px + v * nt * BX + b);
                 if constexpr (RES) {
 #pragma unroll
-                    for (uint32_t b = 0; b < BR; b += 16) cp_async16(slot_at - tid * BX + tid * BR + off_r + at + v * nt * BR + b, pr + v * nt * BR + b);
+                    for (uint32_t b = 0; b < BR; b += 16) cp_async<16>(slot_at - tid * BX + tid * BR + off_r + at + v * nt * BR + b, pr + v * nt * BR + b);
                 }
             }
             ahead += stride; px += step_x; pr += step_r;
@@ -158,17 +142,11 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
     if constexpr (!WARP)
         for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
 
-    constexpr bool KEEP = !WARP && V <= 2;                       // a CTA takes many rows: its weights stay in registers
-    float w[KEEP ? V : 1][8];
-    if constexpr (KEEP) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) if (live[v]) load_weight8(d, (tid + v * nt) * 8, w[v]);
-    }
     Y* py = static_cast<Y*>(d.y) + first * d.ldy + tid * 8;
     R* ph = RES && d.h ? static_cast<R*>(d.h) + first * d.ldh + tid * 8 : nullptr;
     uint32_t it = 0, at = 0;
     for (uint64_t row = first; row < d.rows; row += stride, ++it) {
-        float h[V][8], hw[V][8];
+        float h[V][8];
         if constexpr (!WARP) {
             if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
         }
@@ -196,20 +174,21 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
                 unpack8(rr[v], r);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) h[v][i] += r[i];
+                if constexpr (NORM) if (ph) store8(ph + v * nt * 8, h[v]);
             }
             if constexpr (NORM) {
 #pragma unroll
                 for (int i = 0; i < 8; ++i) ss = fmaf(h[v][i], h[v][i], ss);
             }
-            if constexpr (!KEEP) load_weight8(d, (tid + v * nt) * 8, hw[v]);
+            if constexpr (CODES) {
+                float w[8];
+                load_weight8(d, (tid + v * nt) * 8, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                hw[v][i] = h[v][i] * (KEEP ? w[KEEP ? v : 0][i] : hw[v][i]);
-                if constexpr (CODES) top = max_nan(top, fabsf(hw[v][i]));
+                for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(h[v][i] * w[i]));
             }
         }
         if constexpr (NORM) ss = warp_sum(ss);
-        if constexpr (CODES) top = warp_max(top);
+        if constexpr (CODES) top = warp_abs_max(top);
         if constexpr (!WARP) {
             float2* p = parts[it & 1];
             if ((tid & 31u) == 0) p[tid >> 5] = make_float2(ss, top);
@@ -218,61 +197,48 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
             at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
             const float2 q = (tid & 31u) < nt / 32 ? p[tid & 31u] : make_float2(0.f, 0.f);
             if constexpr (NORM) ss = warp_sum(q.x);
-            if constexpr (CODES) top = warp_max(q.y);
+            if constexpr (CODES) top = warp_abs_max(q.y);
         } else { px += step_x; pr += step_r; }
         float rstd = 1.f;
         if constexpr (NORM) {
             rstd = rsqrtf(fmaf(ss, inv_cols, d.eps));
             if (d.rstd && tid == 0) d.rstd[row] = rstd;
         }
-        bool wide_range = false;                                 // h w overflowed (rows of extreme weights): take h rstd w
-        float mult = rstd;
+        float inv = 1.f;
         if constexpr (CODES) {
-            wide_range = top == INFINITY;
-            if (wide_range) {
+            if (top == INFINITY) {                               // h w overflowed (rows of extreme weights): take h rstd w
                 float t = 0.f;
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     if (!live[v]) continue;
-                    load_weight8(d, (tid + v * nt) * 8, hw[v]);
+                    float w[8];
+                    load_weight8(d, (tid + v * nt) * 8, w);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) { hw[v][i] *= h[v][i] * rstd; t = max_nan(t, fabsf(hw[v][i])); }
+                    for (int i = 0; i < 8; ++i) t = max_nan(t, fabsf(h[v][i] * rstd * w[i]));
                 }
-                t = warp_max(t);
+                t = warp_abs_max(t);
                 if constexpr (!WARP) {
                     float2* p = parts[it & 1];
                     __syncthreads();
                     if ((tid & 31u) == 0) p[tid >> 5].y = t;
                     __syncthreads();
-                    t = warp_max((tid & 31u) < nt / 32 ? p[tid & 31u].y : 0.f);
+                    t = warp_abs_max((tid & 31u) < nt / 32 ? p[tid & 31u].y : 0.f);
                 }
                 top = t;
             } else top *= rstd;
             const float2 sc = row_scale(top);
-            mult = wide_range ? sc.y : rstd * sc.y;
+            inv = sc.y;
             if (tid == 0) d.scale[row] = sc.x;
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
-            if constexpr (RES && NORM) if (ph) store8(ph + v * nt * 8, h[v]);
-            float y[8];
-            if constexpr (!CODES) {
-                // (h w may overflow where h rstd w does not: the product is formed the other way round then)
+            float w[8], y[8];
+            load_weight8(d, (tid + v * nt) * 8, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = hw[v][i] * mult;
-                bool over = false;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) over |= fabsf(hw[v][i]) == INFINITY;
-                if (over) {
-                    float w[8];
-                    load_weight8(d, (tid + v * nt) * 8, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) y[i] = h[v][i] * rstd * w[i];
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) y[i] = hw[v][i] * mult;
+            for (int i = 0; i < 8; ++i) {
+                y[i] = h[v][i] * rstd * w[i];
+                if constexpr (CODES) y[i] *= inv;
             }
             store8(py + v * nt * 8, y);
         }
@@ -282,7 +248,7 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
 }
 
 constexpr uint32_t kWarpRowCols = 1024;         // up to here a warp holds a row (four groups a lane)
-constexpr uint32_t kRingBytes = 64 * 1024;      // per CTA; three CTAs an SM at most sizes
+constexpr uint32_t kRingBytes = 48 * 1024;      // per CTA; four CTAs an SM at most sizes
 constexpr uint32_t kRingMost = 160 * 1024;
 
 template <typename X, typename R, typename Y, int V, bool WARP, bool NORM, int T>
@@ -299,7 +265,7 @@ cudaError_t launch_row_wide(const cleave_rmsnorm_t& d, uint32_t threads, int sms
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
     // CTAs that fit an SM by shared memory and threads; each walks the rows in steps of the grid
-    const uint32_t fit = max(1u, min(min(220u * 1024u / (smem + 2048u), 2048u / threads), 4u));
+    const uint32_t fit = max(1u, min(min(224u * 1024u / (smem + 2048u), 65536u / (threads * 112u)), 5u));
     const uint64_t ctas = min((uint64_t)d.rows, (uint64_t)sms * fit);
     kernel<<<(unsigned)ctas, threads, smem, st>>>(d, stages);
     return cudaGetLastError();
@@ -313,9 +279,10 @@ cudaError_t launch_row_types(const cleave_rmsnorm_t& d, int sms, cudaStream_t st
         if (groups <= 64) return launch_row_wide<X, R, Y, 2, true, NORM, 256>(d, 32, sms, st);
         return launch_row_wide<X, R, Y, 4, true, NORM, 256>(d, 32, sms, st);
     }
-    if (groups <= 512) return launch_row_wide<X, R, Y, 2, false, NORM, 256>(d, (groups + 63) / 64 * 32, sms, st);
-    if (groups <= 1024) return launch_row_wide<X, R, Y, 2, false, NORM, 512>(d, (groups + 63) / 64 * 32, sms, st);
-    return launch_row_wide<X, R, Y, 4, false, NORM, 1024>(d, (groups + 127) / 128 * 32, sms, st);
+    const uint32_t threads = (groups + 127) / 128 * 32;
+    if (groups <= 512) return launch_row_wide<X, R, Y, 4, false, NORM, 128>(d, threads, sms, st);
+    if (groups <= 1024) return launch_row_wide<X, R, Y, 4, false, NORM, 256>(d, threads, sms, st);
+    return launch_row_wide<X, R, Y, 4, false, NORM, 1024>(d, threads, sms, st);
 }
 template <typename X, typename R>
 cudaError_t launch_row_out(const cleave_rmsnorm_t& d, bool norm, int sms, cudaStream_t st) {
@@ -401,12 +368,12 @@ __global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __
                 if (!live[v]) continue;
                 const uint32_t to = ring_base + at;
 #pragma unroll
-                for (uint32_t b = 0; b < BD; b += 16) cp_async16(to + (tid + v * nt) * BD + b, pd + v * nt * BD + b);
+                for (uint32_t b = 0; b < BD; b += 16) cp_async<16>(to + (tid + v * nt) * BD + b, pd + v * nt * BD + b);
 #pragma unroll
-                for (uint32_t b = 0; b < BH; b += 16) cp_async16(to + off_h + (tid + v * nt) * BH + b, ph + v * nt * BH + b);
+                for (uint32_t b = 0; b < BH; b += 16) cp_async<16>(to + off_h + (tid + v * nt) * BH + b, ph + v * nt * BH + b);
                 if (res) {
 #pragma unroll
-                    for (uint32_t b = 0; b < BH; b += 16) cp_async16(to + off_res + (tid + v * nt) * BH + b, pr + v * nt * BH + b);
+                    for (uint32_t b = 0; b < BH; b += 16) cp_async<16>(to + off_res + (tid + v * nt) * BH + b, pr + v * nt * BH + b);
                 }
             }
             ahead += gridDim.x; pd += step_d; ph += step_h;

@@ -75,10 +75,11 @@ int cleave_adamw_create(const cleave_adamw_tensor_t* t, uint32_t n, uint32_t sta
     const int sms = need_device();
     if (sms < 0) return sms;
     int rc = 0;
-    // A warp takes up to four blocks (what is the same for a chunk is set up once), fewer when the blocks would
-    // not give every SM its three CTAs then.
-    const uint64_t full = (uint64_t)sms * 3 * kChunkWarps;
-    const uint32_t chunk_blocks = kChunkWarps * (uint32_t)(n_blocks / full < 1 ? 1 : (n_blocks / full > kChunkMost ? kChunkMost : n_blocks / full));
+    // Blocks a warp takes, so that the chunks fill whole waves of three CTAs an SM (two where states of fp32 fill
+    // the shared memory): long runs keep a warp's copies in flight, and a wave that is not full is wasted.
+    const uint64_t slots = (uint64_t)sms * (state8 ? 3 : 2) * kChunkWarps;
+    const uint64_t waves = (n_blocks + slots * kChunkMost - 1) / (slots * kChunkMost);
+    const uint32_t chunk_blocks = kChunkWarps * (uint32_t)(waves ? (n_blocks + slots * waves - 1) / (slots * waves) : 1);
     cleave_adamw_s* h = new (std::nothrow) cleave_adamw_s();
     if (!h) return CLEAVE_E_NOMEM;
     try {

@@ -112,6 +112,29 @@ inline bool rows_wide(const void* p, uint64_t ld, uint32_t type) {
     return (uintptr_t)p % unit == 0 && (ld * type_bytes(type)) % unit == 0;
 }
 
+// ---- asynchronous copies into shared memory, and warp reductions ----------------------------------------
+// A thread copies only what it reads itself, so a ring of such copies needs no barrier: the thread's own group count
+// says when a stage has landed.
+template <int BYTES>
+__device__ __forceinline__ void cp_async(uint32_t dst, const void* src) {
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+// largest magnitude of the warp's values; a NaN stays
+__device__ __forceinline__ float warp_abs_max(float v) {
+    float r;
+    asm volatile("redux.sync.max.abs.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+
 // ---- activations ----------------------------------------------------------------------------------
 // The two forms with an exponential are z g with g = 1 / (1 + e), e = exp(-t): one exponential (base 2, the factor
 // log2(e) in the argument's constants) and one reciprocal of a value of at least 1, both the hardware's
@@ -184,7 +207,7 @@ struct AdamStep {
     uint64_t base;                  // seed + (step << 32)
 };
 struct AdamChunk { uint32_t tensor, block0; };   // a CTA's blocks of 256 elements, from block0 on
-constexpr uint32_t kChunkWarps = 8, kChunkMost = 4;      // warps of a CTA; blocks a warp takes at most
+constexpr uint32_t kChunkWarps = 8, kChunkMost = 32;     // warps of a CTA; blocks a warp takes at most
 cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, uint32_t chunk_blocks, const AdamStep& s,
                          bool state8, bool g_bf16, cudaStream_t st);
 
