@@ -1,7 +1,7 @@
 """CPU oracle of the operators around the GEMMs: AdamW with 32- and 8-bit states, root-mean-square norm and its
 backward pass, rows in 8 bits, the product with an epilogue and that epilogue's backward pass.
 
-NumPy only; test infrastructure.  Everything is computed in fp64 from the definitions, except `adamw`, whose
+NumPy and SciPy's erfc only; test infrastructure.  Everything is computed in fp64 from the definitions, except `adamw`, whose
 definition says how each operation is rounded to fp32: there the stored bits themselves are the result.
 """
 from __future__ import annotations
@@ -9,6 +9,7 @@ from __future__ import annotations
 import math
 
 import numpy as np
+from scipy import special
 
 M64 = (1 << 64) - 1
 BLOCK = 256
@@ -139,7 +140,7 @@ def rmsnorm_backward(dy, h, w, rstd, dres=None):
 
 # ---- product with an epilogue --------------------------------------------------------------------------------
 def _phi(z):
-    return 0.5 * np.vectorize(math.erfc, otypes=[float])(-z / math.sqrt(2.0))
+    return 0.5 * special.erfc(-z / math.sqrt(2.0))
 
 
 def act(z, kind):

@@ -26,6 +26,7 @@ __device__ unsigned int g_linear_status;
 static std::atomic<uint64_t> g_linear_wait_limit{2000000000ull};
 
 constexpr uint32_t kLinTile = 128, kLinStages = 3, kLinOperand = 16384, kLinStage = 2 * kLinOperand;
+constexpr uint32_t kLongK = 512;         // products an accumulator takes before its sum moves on, in fp32 results
 constexpr uint32_t kLinThreads = 192, kLinSmem = kLinStages * kLinStage + 1024;
 
 // What the write-out needs, the same for every kernel of this file.
@@ -154,6 +155,16 @@ __device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, float (&v)[16]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
 #pragma unroll
     for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
+}
+__device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const float* v) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+        ::"f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]), "f"(v[8]), "f"(v[9]), "f"(v[10]),
+          "f"(v[11]), "f"(v[12]), "f"(v[13]), "f"(v[14]), "f"(v[15]), "f"(v[16]), "f"(v[17]), "f"(v[18]), "f"(v[19]), "f"(v[20]),
+          "f"(v[21]), "f"(v[22]), "f"(v[23]), "f"(v[24]), "f"(v[25]), "f"(v[26]), "f"(v[27]), "f"(v[28]), "f"(v[29]), "f"(v[30]),
+          "f"(v[31]), "r"(taddr) : "memory");
 }
 // Instruction descriptor of kind::f8f6f4: fp32 accumulator (bits 4-5 = 1), E4M3 A and B (format 0), both K-contiguous.
 __device__ __forceinline__ uint32_t instr_desc_e4m3(uint32_t m, uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((m >> 4) << 24); }
@@ -307,6 +318,222 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kLinTile) : "memory");
 }
 
+// ---- large products: pairs of CTAs ---------------------------------------------------------------------
+// linear_pair_kernel: one persistent cluster of two CTAs per pair of SMs.  A tile is 256 rows x BN <= 256 columns; CTA
+// r loads rows 128 r ... of A and columns r BN / 2 ... of B, the leader's MMA thread issues M = 256 products over both
+// CTAs' shared memory (six stages of 32 KB each), and each CTA finds its 128 rows in its own tensor memory, in two
+// slots, so the write-out of a tile runs beside the products of the next.  Tiles go to clusters round robin, in bands
+// of eight row tiles so that tiles in flight share operands in L2.
+//
+// LONG (fp32 results of a long K): the tensor core adds products to its accumulator with truncation, which after
+// thousands of steps shows in fp32 (relative error 9e-6 at K = 8192, growing with K; a bf16 result hides it).  So the
+// accumulator is handed over every `chunk` K-blocks and the epilogue warps keep the sum in registers with ordinary
+// rounded additions; the two slots take turns by chunk instead of by tile.
+constexpr uint32_t kLpStages = 6, kLpThreads = 384, kLpEpiWarp0 = 4, kLpBand = 8;
+constexpr uint32_t kLpSmem = kLpStages * kLinStage + 1024;
+
+struct PairParams {
+    Epilogue e;
+    uint32_t K_blocks, chunk, bn, b_boxes, b_bytes;      // b_bytes: what one CTA loads of B per stage
+    uint32_t tiles_m, tiles_n;
+    uint32_t a_mn, b_mn;
+    unsigned long long wait_limit_ns;
+};
+// mbar_wait_cl without a call (a call would have to save the caller's sums)
+__device__ __forceinline__ bool pair_wait_inline(uint32_t bar, uint32_t parity, const WaitCtx& w) {
+    if (mbar_try_wait_cl(bar, parity)) return true;
+    const uint64_t t0 = global_timer_ns();
+    for (uint32_t spins = 0; !mbar_try_wait_cl(bar, parity); ++spins)
+        if ((spins & 255u) == 0) {
+            if (*w.abort_flag) return false;
+            if (global_timer_ns() - t0 >= w.limit_ns) { raise_abort(w); return false; }
+        }
+    return true;
+}
+struct __align__(16) LpShared {
+    uint64_t full[kLpStages], empty[kLpStages], acc_full[2], acc_empty[2], drain;
+    uint32_t tmem_base, abort_flag;
+};
+// tile number -> row and column tile: bands of kLpBand row tiles, column by column inside a band
+__device__ __forceinline__ uint2 pair_tile(const PairParams& P, uint32_t t) {
+    const uint32_t per_band = kLpBand * P.tiles_n, band = t / per_band, in = t - band * per_band;
+    const uint32_t rows = min(kLpBand, P.tiles_m - band * kLpBand);
+    return make_uint2(band * kLpBand + in % rows, in / rows);
+}
+template <bool E4M3>
+__device__ __forceinline__ void umma_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (E4M3)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+                     ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate) : "memory");
+    else umma_bf16_pair(d_tmem, a_desc, b_desc, idesc, accumulate);
+}
+
+template <bool E4M3, bool LONG>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLpThreads, 1)
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ PairParams P) {
+    extern __shared__ uint8_t dyn_smem[];
+    __shared__ LpShared sh;
+    constexpr uint32_t kBlk = E4M3 ? 128u : 64u;
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u, rank = cluster_ctarank();
+    const uint32_t base = (smem_u32(dyn_smem) + 1023u) & ~1023u;
+    const uint32_t tiles = P.tiles_m * P.tiles_n, cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
+    const WaitCtx W = {&sh.abort_flag, &g_linear_status, P.wait_limit_ns};
+
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < kLpStages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&sh.acc_full[a]), 1); mbar_init(smem_u32(&sh.acc_empty[a]), LONG ? 16 : 8); }
+        mbar_init(smem_u32(&sh.drain), 1);
+        sh.abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc_pair(smem_u32(&sh.tmem_base), 512);
+    tc_fence_before();
+    cluster_arrive_wait();                            // barriers of both CTAs are ready before any remote arrive
+    tc_fence_after();
+    const uint32_t tmem = sh.tmem_base;
+
+    if (warp < kLpEpiWarp0) {
+        if constexpr (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if (warp == 0 && lane == 0) {
+            // ---- producer (both CTAs) ----
+            const uint32_t full0 = mapa_shared(smem_u32(&sh.full[0]), 0u), tx = 2u * (kLinOperand + P.b_bytes);
+            uint32_t it = 0;
+            bool ok = true;
+            for (uint32_t t = cluster; ok && t < tiles; t += clusters) {
+                const uint2 at = pair_tile(P, t);
+                const int32_t m = (int32_t)(at.x * 256u + rank * 128u), n = (int32_t)(at.y * P.bn + rank * (P.bn / 2));
+                for (uint32_t kb = 0; kb < P.K_blocks; ++kb, ++it) {
+                    const uint32_t s = it % kLpStages, ph = (it / kLpStages) & 1u;
+                    if (!mbar_wait_cl(smem_u32(&sh.empty[s]), ph ^ 1u, W)) { ok = false; break; }
+                    if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full[s]), tx);
+                    const uint32_t bar = full0 + s * 8u, sa = base + s * kLinStage, sb = sa + kLinOperand;
+                    const int32_t k = (int32_t)(kb * kBlk);
+                    if (P.a_mn) { tma_load_2d_pair(sa, &map_a, bar, m, k); tma_load_2d_pair(sa + kSubBytes, &map_a, bar, m + 64, k); }
+                    else tma_load_2d_pair(sa, &map_a, bar, k, m);
+                    if (P.b_mn) for (uint32_t j = 0; j < P.b_boxes; ++j) tma_load_2d_pair(sb + j * kSubBytes, &map_b, bar, n + 64 * (int32_t)j, k);
+                    else tma_load_2d_pair(sb, &map_b, bar, k, n);
+                }
+            }
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            // ---- MMA issuer (leader) ----
+            const uint32_t idesc = E4M3 ? instr_desc_e4m3(256, P.bn) : instr_desc_bf16(256, P.bn, P.a_mn, P.b_mn);
+            const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
+            const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
+            uint32_t it = 0, use = 0;                 // stages and accumulator slots used so far
+            bool ok = true;
+            for (uint32_t t = cluster; ok && t < tiles; t += clusters) {
+                for (uint32_t k0 = 0; ok && k0 < P.K_blocks; k0 += P.chunk, ++use) {
+                    const uint32_t k1 = min(P.K_blocks, k0 + P.chunk), acc = use & 1u, d = tmem + acc * 256u;
+                    if (!mbar_wait_cl(smem_u32(&sh.acc_empty[acc]), ((use >> 1) & 1u) ^ 1u, W)) { ok = false; break; }
+                    tc_fence_after();
+                    for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
+                        const uint32_t s = it % kLpStages, ph = (it / kLpStages) & 1u;
+                        if (!mbar_wait_cl(smem_u32(&sh.full[s]), ph, W)) { ok = false; break; }
+                        tc_fence_after();
+                        const uint32_t sa = base + s * kLinStage, sb = sa + kLinOperand;
+#pragma unroll
+                        for (uint32_t q = 0; q < 4; ++q)
+                            umma_pair<E4M3>(d, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, (kb != k0) | (q != 0u));
+                        umma_commit_both(smem_u32(&sh.empty[s]));
+                    }
+                    if (ok) umma_commit_both(smem_u32(&sh.acc_full[acc]));
+                }
+            }
+            // every MMA issued above has completed before either CTA releases tensor memory
+            umma_commit_local_pair(smem_u32(&sh.drain));
+            const uint64_t t0 = global_timer_ns();
+            while (!mbar_try_wait_cl(smem_u32(&sh.drain), 0u))
+                if (global_timer_ns() - t0 > 2000000000ull) { atomicOr(&g_linear_status, STATUS_TIMEOUT); break; }
+        }
+    } else {
+        // ---- write-out (both CTAs) ----
+        if constexpr (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+        const uint32_t quad = warp & 3u, group = (warp - kLpEpiWarp0) >> 2;
+        const uint32_t lane_base = (quad * 32u) << 16;
+        if constexpr (!LONG) {
+            // group g drains slot g: every second tile of the cluster
+            const uint32_t empty = mapa_shared(smem_u32(&sh.acc_empty[group]), 0u), taddr = tmem + group * 256u + lane_base;
+            uint32_t use = 0;
+            for (uint32_t t = cluster + group * clusters; t < tiles; t += 2 * clusters, ++use) {
+                const uint2 at = pair_tile(P, t);
+                const uint32_t row = at.x * 256u + rank * 128u + quad * 32u + lane, col = at.y * P.bn;
+                if (!__all_sync(0xFFFFFFFFu, mbar_wait_cl(smem_u32(&sh.acc_full[group]), use & 1u, W))) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (uint32_t c = 0; c < P.bn; c += 32) {
+                    uint32_t u[32];
+                    tmem_ld_32x32(taddr + c, u);
+                    tmem_ld_wait();
+                    if (c + 32 >= P.bn) {             // the slot is read: hand it back
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster_read_done(empty);
+                    }
+                    float v[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
+                    write_out16(P.e, row, col + c, v);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[16 + i]);
+                    write_out16(P.e, row, col + c + 16, v);
+                }
+            }
+        } else {
+            // all eight warps on one tile: group g keeps columns 128 g ... of its rows; the finished sums go back into
+            // the last slot, from where they are written out piece by piece (registers hold nothing else meanwhile)
+            uint32_t use = 0;
+            bool ok = true;
+            for (uint32_t t = cluster; ok && t < tiles; t += clusters) {
+                const uint2 at = pair_tile(P, t);
+                const uint32_t row = at.x * 256u + rank * 128u + quad * 32u + lane, col = at.y * P.bn + group * 128u;
+                const uint32_t cols = P.bn > group * 128u ? min(128u, P.bn - group * 128u) : 0u;
+                float sum[128];
+#pragma unroll
+                for (int i = 0; i < 128; ++i) sum[i] = 0.f;
+                for (uint32_t k0 = 0; k0 < P.K_blocks; k0 += P.chunk, ++use) {
+                    const uint32_t acc = use & 1u, taddr = tmem + acc * 256u + group * 128u + lane_base;
+                    ok = __all_sync(0xFFFFFFFFu, pair_wait_inline(smem_u32(&sh.acc_full[acc]), (use >> 1) & 1u, W));
+                    if (!ok) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (uint32_t c = 0; c < 128; c += 32) {
+                        uint32_t u[32];
+                        tmem_ld_32x32(taddr + c, u);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sum[c + i] += __uint_as_float(u[i]);
+                    }
+                    if (k0 + P.chunk >= P.K_blocks) {
+#pragma unroll
+                        for (uint32_t c = 0; c < 128; c += 32) tmem_st_32x32(taddr + c, sum + c);
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+#pragma unroll 1
+                        for (uint32_t c = 0; c < cols; c += 16) {
+                            float v[16];
+                            tmem_ld_32x16(taddr + c, v);
+                            write_out16(P.e, row, col + c, v);
+                        }
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster_read_done(mapa_shared(smem_u32(&sh.acc_empty[acc]), 0u));
+                }
+            }
+        }
+        tc_fence_before();
+    }
+    __syncwarp();
+    cluster_arrive_wait();                            // both CTAs are done with both tensor memories and all barriers
+    if (sh.abort_flag) {                              // a role gave up: copies may still be in flight towards this CTA
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 200000ull) { }
+        cluster_arrive_wait();
+    }
+    tc_fence_after();
+    if (warp == 1) tmem_dealloc_pair(tmem, 512);
+}
+
 // ---- host --------------------------------------------------------------------------------------------
 namespace {
 
@@ -348,28 +575,60 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     P.K_blocks = (g.K + kblk - 1) / kblk;
     CUtensorMap ma, mb;
     int rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, 128, e4m3);
-    if (!rc) rc = g.transB ? encode_operand(&mb, d.B, g.N, g.K, g.ldb, 128, e4m3) : encode_operand(&mb, d.B, g.K, g.N, g.ldb, 64, e4m3);
     if (rc) return rc;
-    const uint64_t tiles_m = (g.M + kLinTile - 1) / kLinTile, tiles_n = (g.N + kLinTile - 1) / kLinTile, tiles = tiles_m * tiles_n;
-    P.tiles_n = (uint32_t)tiles_n;
-    // K is split while every CTA still finds a place at once (two an SM) and keeps at least four stages of work
-    P.splits = 1;
-    while (P.splits < 8 && tiles * P.splits * 2 <= 2u * (uint32_t)sms && P.K_blocks / (P.splits * 2) >= 4) P.splits *= 2;
-    if (tiles * P.splits > 0x7FFFFFFFull) return CLEAVE_E_UNSUPPORTED;
-    auto kernel = e4m3 ? linear_split_kernel<true> : linear_split_kernel<false>;
-    static SmemLimit limit[2];
-    if (limit[e4m3 ? 1 : 0].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+    auto encode_b = [&](uint32_t rows) { return g.transB ? encode_operand(&mb, d.B, g.N, g.K, g.ldb, rows, e4m3) : encode_operand(&mb, d.B, g.K, g.N, g.ldb, 64, e4m3); };
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(tiles * P.splits));
-    cfg.blockDim = dim3(kLinThreads);
-    cfg.dynamicSmemBytes = kLinSmem;
-    cfg.stream = st;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = P.splits; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, kernel, ma, mb, P) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+    cfg.stream = st;
+    cudaError_t err;
+    const uint64_t tiles_m = (g.M + kLinTile - 1) / kLinTile, tiles_n = (g.N + kLinTile - 1) / kLinTile, tiles = tiles_m * tiles_n;
+    const uint32_t pairs = (uint32_t)sms / 2;
+    if (tiles >= 2u * (uint32_t)sms) {
+        PairParams Q = {};
+        Q.e = P.e; Q.K_blocks = P.K_blocks; Q.a_mn = P.a_mn; Q.b_mn = P.b_mn; Q.wait_limit_ns = P.wait_limit_ns;
+        Q.tiles_m = (g.M + 255) / 256;
+        // the tile width whose waves cost the fewest columns a cluster
+        uint64_t best = ~0ull;
+        for (uint32_t bn = 256; bn >= 128; bn -= 32) {
+            const uint64_t n = (g.N + bn - 1) / bn, cost = ((uint64_t)Q.tiles_m * n + pairs - 1) / pairs * (bn + 16);
+            if (cost < best) { best = cost; Q.bn = bn; Q.tiles_n = (uint32_t)n; }
+        }
+        Q.b_boxes = (Q.bn / 2 + 63) / 64;
+        Q.b_bytes = Q.b_mn ? Q.b_boxes * kSubBytes : Q.bn / 2 * 128u;
+        const bool lng = (d.c_type == CLEAVE_T_F32 || d.z_type == CLEAVE_T_F32) && g.K > kLongK;
+        Q.chunk = lng ? kLongK / kblk : Q.K_blocks;
+        if ((rc = encode_b(Q.bn / 2))) return rc;
+        auto kernel = e4m3 ? (lng ? linear_pair_kernel<true, true> : linear_pair_kernel<true, false>)
+                           : (lng ? linear_pair_kernel<false, true> : linear_pair_kernel<false, false>);
+        static SmemLimit limit[4];
+        if (limit[(e4m3 ? 2 : 0) + (lng ? 1 : 0)].raise(reinterpret_cast<const void*>(kernel), kLpSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+        const uint64_t all = (uint64_t)Q.tiles_m * Q.tiles_n;
+        if (all > 0x7FFFFFFFull) return CLEAVE_E_UNSUPPORTED;
+        cfg.gridDim = dim3(2u * (unsigned)(all < pairs ? all : pairs));
+        cfg.blockDim = dim3(kLpThreads);
+        cfg.dynamicSmemBytes = kLpSmem;
+        cfg.numAttrs = 0;                                   // (the cluster size is the kernel's own)
+        err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, Q);
+    } else {
+        P.tiles_n = (uint32_t)tiles_n;
+        // K is split while every CTA still finds a place at once (two an SM) and keeps at least four stages of work
+        P.splits = 1;
+        while (P.splits < 8 && tiles * P.splits * 2 <= 2u * (uint32_t)sms && P.K_blocks / (P.splits * 2) >= 4) P.splits *= 2;
+        if ((rc = encode_b(kLinTile))) return rc;
+        auto kernel = e4m3 ? linear_split_kernel<true> : linear_split_kernel<false>;
+        static SmemLimit limit[2];
+        if (limit[e4m3 ? 1 : 0].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+        cfg.gridDim = dim3((unsigned)(tiles * P.splits));
+        cfg.blockDim = dim3(kLinThreads);
+        cfg.dynamicSmemBytes = kLinSmem;
+        attr[0].val.clusterDim.x = P.splits;
+        err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, P);
+    }
+    if (err != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
     return 0;
 }
 

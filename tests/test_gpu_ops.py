@@ -348,7 +348,8 @@ LAYOUTS = [(False, False, "bf16"), (False, True, "bf16"), (True, False, "bf16"),
 
 
 @pytest.mark.parametrize("m,n,k", [(1, 1, 1), (1, 4096, 512), (16, 512, 4096), (128, 128, 64), (129, 257, 65), (77, 33, 200), (300, 520, 1000),
-                                   (8, 136, 3000), (260, 24, 72), (640, 1000, 130), (1, 8, 16384), (513, 769, 385)])
+                                   (8, 136, 3000), (260, 24, 72), (640, 1000, 130), (1, 8, 16384), (513, 769, 385),
+                                   (4700, 1300, 200), (257, 20000, 72), (2500, 2500, 1100), (2600, 3080, 64), (1, 38000, 600)])
 @pytest.mark.parametrize("ta,tb,kind", LAYOUTS)
 def test_linear_integer_products_are_exact(cl, m, n, k, ta, tb, kind):
     """Integers in -4..4: every fp32 sum is exact, so every value has to be equal, in every layout and size."""
@@ -365,7 +366,7 @@ def test_linear_integer_products_are_exact(cl, m, n, k, ta, tb, kind):
 
 @pytest.mark.parametrize("act", KINDS)
 @pytest.mark.parametrize("kind,c,side", [("bf16", "bf16", "f32"), ("bf16", "f32", "bf16"), ("e4m3", "bf16", "bf16")])
-@pytest.mark.parametrize("m,n,k", [(1, 72, 256), (200, 300, 320), (130, 129, 70), (16, 2048, 1024), (700, 512, 256)])
+@pytest.mark.parametrize("m,n,k", [(1, 72, 256), (200, 300, 320), (130, 129, 70), (16, 2048, 1024), (700, 512, 256), (3, 37993, 72), (130, 19008, 40)])
 def test_linear_epilogue(cl, act, kind, c, side, m, n, k):
     rng = np.random.default_rng(m * n + k)
     A, B, a, b = _operands(rng, m, n, k, False, True, kind, 0, integer=False)
