@@ -15,6 +15,7 @@
 // Every wait is bounded (2 s by default): a wait that runs out records it in a status word of the library, the
 // CTA's roles leave, copies and MMAs in flight are given time to end, and the kernel returns.
 #include <atomic>
+#include <type_traits>
 
 #include "kernels.cuh"
 #include "ops.cuh"
@@ -32,8 +33,9 @@ constexpr uint32_t kLinThreads = 192, kLinSmem = kLinStages * kLinStage + 1024;
 // What the write-out needs, the same for every kernel of this file.
 struct Epilogue {
     uint32_t M, N;
-    uint32_t act, c_type, bias_type, z_type, mul_type, res_type;
-    uint32_t wide;                  // bit per operand: rows allow 16-byte accesses (kWide*)
+    uint32_t c_type, bias_type, z_type, mul_type, res_type;
+    uint32_t form;                  // 1, 2: C (bf16, fp32) and z (bf16) leave as bulk stores, mul and res allow 16-byte accesses; 0: any
+    uint32_t wide;                  // bit per operand: rows allow one access for four elements (kWide*)
     const float* scale_a;
     const float* scale_b;
     const void* bias;
@@ -52,82 +54,212 @@ struct LinearParams {
     unsigned long long wait_limit_ns;
 };
 
-// 16 consecutive elements of a row as fp32; `wide`: whole and aligned.
-__device__ __forceinline__ void load16(const void* p, uint32_t type, uint64_t at, uint32_t n, bool wide, float (&x)[16]) {
-    if (wide && n >= 16) {
+// Four consecutive elements of a row; `n` of them exist, `wide`: the rows allow one access for four.
+__device__ __forceinline__ void load_row4(const void* p, uint32_t type, uint64_t at, uint32_t n, bool wide, float (&x)[4]) {
+    if (wide && n >= 4) {
         if (type == CLEAVE_T_F32) {
-            const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) { const float4 v = s[q]; x[4 * q] = v.x; x[4 * q + 1] = v.y; x[4 * q + 2] = v.z; x[4 * q + 3] = v.w; }
+            const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
         } else {
-            const uint4* s = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + at);
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-                const uint4 v = s[q];
-                const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (int h = 0; h < 4; ++h) { x[8 * q + 2 * h] = __uint_as_float(w[h] << 16); x[8 * q + 2 * h + 1] = __uint_as_float(w[h] & 0xFFFF0000u); }
-            }
+            const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + at);
+            x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
+            x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = (uint32_t)i < n ? load_as(p, type, at + i) : 0.f;
+        for (int i = 0; i < 4; ++i) x[i] = (uint32_t)i < n ? load_as(p, type, at + i) : 0.f;
     }
 }
-__device__ __forceinline__ void store16(void* p, uint32_t type, uint64_t at, uint32_t n, bool wide, const float (&x)[16]) {
-    if (wide && n >= 16) {
-        if (type == CLEAVE_T_F32) {
-            float4* d = reinterpret_cast<float4*>(static_cast<float*>(p) + at);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) d[q] = make_float4(x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]);
-        } else {
-            uint4* d = reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p) + at);
-#pragma unroll
-            for (int q = 0; q < 2; ++q)
-                d[q] = make_uint4(pack_bf16(x[8 * q], x[8 * q + 1]), pack_bf16(x[8 * q + 2], x[8 * q + 3]), pack_bf16(x[8 * q + 4], x[8 * q + 5]), pack_bf16(x[8 * q + 6], x[8 * q + 7]));
-        }
+__device__ __forceinline__ void store_row4(void* p, uint32_t type, uint64_t at, uint32_t n, bool wide, const float (&x)[4]) {
+    if (wide && n >= 4) {
+        if (type == CLEAVE_T_F32) *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = make_float4(x[0], x[1], x[2], x[3]);
+        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p) + at) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
     } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) if ((uint32_t)i < n) store_as(p, type, at + i, x[i]);
+        for (int i = 0; i < 4; ++i) if ((uint32_t)i < n) store_as(p, type, at + i, x[i]);
+    }
+}
+// A warp's staging tile: 32 rows of COLS fp32, written by a lane a row (what tensor memory gives) and read 4 columns a
+// lane, so that 8 (or 4) lanes cover a row of the chunk: 128 (64) bytes of fp32, 64 (32) of bf16 in one piece.  The
+// 16-byte groups of row r stand at group ^ r, so neither direction has bank conflicts.
+template <int COLS>
+__device__ __forceinline__ void stage_write(float* tile, uint32_t row, const float* v) {
+    float4* base = reinterpret_cast<float4*>(tile) + row * (COLS / 4);
+#pragma unroll
+    for (uint32_t j = 0; j < COLS / 4; ++j) base[j ^ (row & (COLS / 4 - 1))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+}
+
+// The staged chunk (rows row0 ... + 31, columns col ... + COLS - 1 of the product) through the epilogue to C and z, any
+// types and edges.  Kept small and out of line: instructions that are fetched but seldom run cost the common form time.
+template <int COLS, uint32_t ACT>
+__device__ __noinline__ void write_chunk_any(const Epilogue& e, const float* tile, uint32_t row0, uint32_t col, uint32_t lane) {
+    constexpr uint32_t LANES = COLS / 4, STEP = 32 / LANES;          // lanes per row, rows per step
+    const uint32_t cc = lane % LANES, rr = lane / LANES;
+    col += cc * 4u;
+    if (col >= e.N) return;
+    const uint32_t n = e.N - col;
+#pragma unroll 1
+    for (uint32_t r = rr; r < 32 && row0 + r < e.M; r += STEP) {
+        const uint32_t row = row0 + r;
+        const float4 f = reinterpret_cast<const float4*>(tile)[r * LANES + (cc ^ (r & (LANES - 1)))];
+        float x[4] = {f.x, f.y, f.z, f.w}, t[4];
+        if (e.scale_a) { const float sa = e.scale_a[row]; for (int i = 0; i < 4; ++i) x[i] *= sa; }
+        if (e.scale_b) { load_row4(e.scale_b, CLEAVE_T_F32, col, n, e.wide & kWideB, t); for (int i = 0; i < 4; ++i) x[i] *= t[i]; }
+        if (e.bias) { load_row4(e.bias, e.bias_type, col, n, e.wide & kWideBias, t); for (int i = 0; i < 4; ++i) x[i] += t[i]; }
+        if (e.z) store_row4(e.z, e.z_type, row * e.ldz + col, n, e.wide & kWideZ, x);
+        for (int i = 0; i < 4; ++i) x[i] = act_value(x[i], ACT);
+        if (e.mul) { load_row4(e.mul, e.mul_type, row * e.ldmul + col, n, e.wide & kWideMul, t); for (int i = 0; i < 4; ++i) x[i] *= t[i]; }
+        if (e.res) { load_row4(e.res, e.res_type, row * e.ldres + col, n, e.wide & kWideRes, t); for (int i = 0; i < 4; ++i) x[i] += t[i]; }
+        store_row4(e.C, e.c_type, row * e.ldc + col, n, e.wide & kWideC, x);
+    }
+}
+// 32 consecutive elements of a row added to / multiplied into x; the row allows 16-byte accesses and holds them all.
+template <bool MUL>
+__device__ __forceinline__ void join_row32(const void* p, uint32_t type, uint64_t at, float (&x)[32]) {
+    auto join = [](float& a, float b) { if constexpr (MUL) a *= b; else a += b; };
+    if (type == CLEAVE_T_F32) {
+        const float4* s = reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
+        float4 v[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = s[q];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) { join(x[4 * q], v[q].x); join(x[4 * q + 1], v[q].y); join(x[4 * q + 2], v[q].z); join(x[4 * q + 3], v[q].w); }
+    } else {
+        const uint4* s = reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + at);
+        uint4 v[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = s[q];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t w[4] = {v[q].x, v[q].y, v[q].z, v[q].w};
+#pragma unroll
+            for (int h = 0; h < 4; ++h) { join(x[8 * q + 2 * h], __uint_as_float(w[h] << 16)); join(x[8 * q + 2 * h + 1], __uint_as_float(w[h] & 0xFFFF0000u)); }
+        }
+    }
+}
+// A row of a 32 x 32 chunk as a bulk tensor store wants it: fp32 rows of 128 bytes with the 128-byte swizzle, or bf16
+// rows of 64 bytes with the 64-byte swizzle.
+template <bool F32>
+__device__ __forceinline__ void stage_out(uint8_t* buf, uint32_t row, const float (&x)[32]) {
+    if constexpr (F32) stage_write<32>(reinterpret_cast<float*>(buf), row, x);
+    else {
+        uint4* base = reinterpret_cast<uint4*>(buf) + row * 4u;
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j)
+            base[j ^ ((row >> 1) & 3u)] = make_uint4(pack_bf16(x[8 * j], x[8 * j + 1]), pack_bf16(x[8 * j + 2], x[8 * j + 3]),
+                                                     pack_bf16(x[8 * j + 4], x[8 * j + 5]), pack_bf16(x[8 * j + 6], x[8 * j + 7]));
     }
 }
 
-// 16 accumulator values of one row, columns col .. col + 15, through the epilogue to C (and z).
-__device__ __forceinline__ void write_out16(const Epilogue& e, uint32_t row, uint32_t col, float (&v)[16]) {
-    if (row >= e.M || col >= e.N) return;
-    const uint32_t n = e.N - col;
-    float t[16];
+// A warp's output buffers: `count` of `bytes` each, taken in turn; a buffer is free again when the bulk store that read it
+// (the count-th last one) has finished reading.
+struct OutRing {
+    uint8_t* base;
+    uint32_t bytes, count, next;
+    __device__ __forceinline__ uint8_t* take(uint32_t lane) {
+        if (lane == 0) { if (count >= 3) asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory"); else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+        __syncwarp();
+        uint8_t* b = base + next * bytes;
+        next = next + 1 == count ? 0 : next + 1;
+        return b;
+    }
+    __device__ __forceinline__ void store(const CUtensorMap* map, const uint8_t* buf, uint32_t col, uint32_t row, uint32_t lane) {
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) { tma_store_2d(map, smem_u32(buf), (int32_t)col, (int32_t)row); bulk_commit(); }
+    }
+    __device__ __forceinline__ void finish(uint32_t lane) { if (lane == 0) bulk_wait_all(); __syncwarp(); }
+};
+
+// One chunk, 32 columns from `col` on, a lane a row (row0 + lane), from its fp32 sums x to C (and z) through bulk stores,
+// which leave out what lies beyond C's edges.
+template <uint32_t ACT, bool F32>
+__device__ __forceinline__ void write_rows(const Epilogue& e, const CUtensorMap* map_c, const CUtensorMap* map_z, OutRing& out, float (&x)[32], float sa,
+                                           uint32_t row0, uint32_t col, uint32_t lane) {
+    uint8_t* buf = out.take(lane);
+    const uint32_t mine = col + lane;
     if (e.scale_a) {
-        const float sa = e.scale_a[row];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] *= sa;
+        for (int i = 0; i < 32; ++i) x[i] *= sa;
     }
-    if (e.scale_b) {
-        load16(e.scale_b, CLEAVE_T_F32, col, n, e.wide & kWideB, t);
+    if (e.scale_b || e.bias) {
+        // the columns' scales and biases, a lane a column, through the (still empty) buffer to every lane
+        float* vec = reinterpret_cast<float*>(buf);
+        if (e.scale_b) vec[lane] = mine < e.N ? __ldg(e.scale_b + mine) : 0.f;
+        if (e.bias) vec[32 + lane] = mine < e.N ? load_as(e.bias, e.bias_type, mine) : 0.f;
+        __syncwarp();
+        if (e.scale_b) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] *= t[i];
-    }
-    if (e.bias) {
-        load16(e.bias, e.bias_type, col, n, e.wide & kWideBias, t);
+            for (int q = 0; q < 8; ++q) { const float4 v = reinterpret_cast<const float4*>(vec)[q]; x[4 * q] *= v.x; x[4 * q + 1] *= v.y; x[4 * q + 2] *= v.z; x[4 * q + 3] *= v.w; }
+        }
+        if (e.bias) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += t[i];
+            for (int q = 0; q < 8; ++q) { const float4 v = reinterpret_cast<const float4*>(vec + 32)[q]; x[4 * q] += v.x; x[4 * q + 1] += v.y; x[4 * q + 2] += v.z; x[4 * q + 3] += v.w; }
+        }
+        __syncwarp();
     }
-    if (e.z) store16(e.z, e.z_type, row * e.ldz + col, n, e.wide & kWideZ, v);
-    if (e.act != CLEAVE_ACT_NONE) {
+    if (e.z) {
+        stage_out<false>(buf, lane, x);
+        out.store(map_z, buf, col, row0, lane);
+        buf = out.take(lane);
+    }
+    if constexpr (ACT != CLEAVE_ACT_NONE) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] = act_value(v[i], e.act);
+        for (int i = 0; i < 32; ++i) x[i] = act_value(x[i], ACT);
     }
-    if (e.mul) {
-        load16(e.mul, e.mul_type, row * e.ldmul + col, n, e.wide & kWideMul, t);
+    const uint64_t row = row0 + lane;
+    if (row < e.M) {
+        if (col + 32 <= e.N) {
+            if (e.mul) join_row32<true>(e.mul, e.mul_type, row * e.ldmul + col, x);
+            if (e.res) join_row32<false>(e.res, e.res_type, row * e.ldres + col, x);
+        } else {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] *= t[i];
+            for (uint32_t i = 0; i < 32; ++i)
+                if (col + i < e.N) {
+                    if (e.mul) x[i] *= load_as(e.mul, e.mul_type, row * e.ldmul + col + i);
+                    if (e.res) x[i] += load_as(e.res, e.res_type, row * e.ldres + col + i);
+                }
+        }
     }
-    if (e.res) {
-        load16(e.res, e.res_type, row * e.ldres + col, n, e.wide & kWideRes, t);
+    stage_out<F32>(buf, lane, x);
+    out.store(map_c, buf, col, row0, lane);
+}
+// A warp's strip of the accumulator, 32 rows x `cols` columns from tensor-memory address taddr on, to its place in C.
+// `read` is called when the accumulator has been read for the last time.
+template <uint32_t ACT, typename Read>
+__device__ __forceinline__ void write_strip(const Epilogue& e, const CUtensorMap* map_c, const CUtensorMap* map_z, OutRing& out, uint32_t taddr, uint32_t row0,
+                                            uint32_t col, uint32_t cols, uint32_t lane, Read read) {
+    const float sa = e.scale_a && row0 + lane < e.M ? __ldg(e.scale_a + row0 + lane) : 1.f;
+#pragma unroll 1
+    for (uint32_t c = 0; c < cols; c += 32) {
+        float x[32];
+        {
+            uint32_t u[32];
+            tmem_ld_32x32(taddr + c, u);
+            tmem_ld_wait();
+            if (c + 32 >= cols) read();
 #pragma unroll
-        for (int i = 0; i < 16; ++i) v[i] += t[i];
+            for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(u[i]);
+        }
+        if (row0 >= e.M || col + c >= e.N) continue;
+        if (e.form == 1) write_rows<ACT, false>(e, map_c, map_z, out, x, sa, row0, col + c, lane);
+        else if (e.form == 2) write_rows<ACT, true>(e, map_c, map_z, out, x, sa, row0, col + c, lane);
+        else {
+            float* tile = reinterpret_cast<float*>(out.base);
+            stage_write<32>(tile, lane, x);
+            __syncwarp();
+            write_chunk_any<32, ACT>(e, tile, row0, col + c, lane);
+            __syncwarp();
+        }
     }
-    store16(e.C, e.c_type, row * e.ldc + col, n, e.wide & kWideC, v);
+}
+// The rows of mul and res that a strip of 32 rows x `cols` columns will need, brought into L2 ahead of time.
+__device__ __forceinline__ void prefetch_strip(const void* p, uint32_t type, uint64_t ld, const Epilogue& e, uint32_t row, uint32_t col, uint32_t cols) {
+    if (!p || row >= e.M || col >= e.N) return;
+    const uint32_t es = type == CLEAVE_T_F32 ? 4u : 2u;
+    const uint8_t* at = static_cast<const uint8_t*>(p) + (row * ld + col) * es;
+    const uint32_t bytes = min(cols, e.N - col) * es;
+    for (uint32_t b = 0; b < bytes; b += 128) asm volatile("prefetch.global.L2 [%0];" ::"l"(at + b));
 }
 
 // ---- PTX of one-CTA products ---------------------------------------------------------------------------
@@ -146,15 +278,6 @@ __device__ __forceinline__ void umma_one(uint32_t d_tmem, uint64_t a_desc, uint6
 }
 __device__ __forceinline__ void umma_commit_one(uint32_t bar) {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, float (&v)[16]) {
-    uint32_t u[16];
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(u[0]), "=r"(u[1]), "=r"(u[2]), "=r"(u[3]), "=r"(u[4]), "=r"(u[5]), "=r"(u[6]), "=r"(u[7]), "=r"(u[8]), "=r"(u[9]),
-                   "=r"(u[10]), "=r"(u[11]), "=r"(u[12]), "=r"(u[13]), "=r"(u[14]), "=r"(u[15]) : "r"(taddr) : "memory");
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-#pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
 }
 __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const float* v) {
     asm volatile(
@@ -195,9 +318,10 @@ struct __align__(16) LinShared {
     uint32_t tmem_base, abort_flag;
 };
 
-template <bool E4M3>
+template <bool E4M3, uint32_t ACT>
 __global__ void __launch_bounds__(kLinThreads, 2)
-linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ LinearParams P) {
+linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c,
+                    const __grid_constant__ CUtensorMap map_z, const __grid_constant__ LinearParams P) {
     extern __shared__ uint8_t dyn_smem[];
     __shared__ LinShared sh;
     constexpr uint32_t kBlk = E4M3 ? 128u : 64u;         // K per stage: 128 bytes
@@ -263,27 +387,25 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     }
     __syncwarp();
     // ---- write-out: warps 2..5, warp w owns the accumulator rows 32 (w % 4) ... ----
-    const uint32_t quad = warp & 3u, row = m0 + quad * 32u + lane;
+    const uint32_t quad = warp & 3u;
     bool ok = true;
     if (warp >= 2) {
         ok = __all_sync(0xFFFFFFFFu, lin_wait(smem_u32(&sh.acc_full), 0u, W));
         tc_fence_after();
         const uint32_t taddr = tmem + ((quad * 32u) << 16);
         if (ok && P.splits == 1) {
-#pragma unroll 1
-            for (uint32_t c = 0; c < kLinTile; c += 16) {
-                float v[16];
-                tmem_ld_32x16(taddr + c, v);
-                write_out16(P.e, row, n0 + c, v);
-            }
+            OutRing out = {dyn_smem + (base - smem_u32(dyn_smem)) + (warp - 2) * 12288, 4096u, 3u, 0u};        // the stages are read
+            write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, m0 + quad * 32u, n0, kLinTile, lane, [] {});
+            if (P.e.form) out.finish(lane);
         } else if (ok) {
             float* part = reinterpret_cast<float*>(dyn_smem + (base - smem_u32(dyn_smem)));      // the stages are read: column-major [128][128]
 #pragma unroll 1
-            for (uint32_t c = 0; c < kLinTile; c += 16) {
-                float v[16];
-                tmem_ld_32x16(taddr + c, v);
+            for (uint32_t c = 0; c < kLinTile; c += 32) {
+                uint32_t u[32];
+                tmem_ld_32x32(taddr + c, u);
+                tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 16; ++i) part[(c + i) * kLinTile + quad * 32u + lane] = v[i];
+                for (int i = 0; i < 32; ++i) part[(c + i) * kLinTile + quad * 32u + lane] = __uint_as_float(u[i]);
             }
         }
         tc_fence_before();
@@ -291,19 +413,33 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     if (P.splits > 1) {
         cluster_arrive_wait();
         if (warp >= 2 && ok) {
-            const uint32_t cols = kLinTile / P.splits, c0 = rank * cols;
+            // (of eight CTAs the first four add: a chunk of 32 columns is the least that is written at once)
+            const uint32_t cols = P.splits == 2 ? 64u : 32u, c0 = rank * cols, row0 = m0 + quad * 32u;
+            OutRing out = {dyn_smem + (base - smem_u32(dyn_smem)) + 65536 + (warp - 2) * 8192, 4096u, 2u, 0u};   // behind the accumulators
+            if (row0 < P.e.M) {
+                const float sa = P.e.scale_a && row0 + lane < P.e.M ? __ldg(P.e.scale_a + row0 + lane) : 1.f;
 #pragma unroll 1
-            for (uint32_t c = c0; c < c0 + cols; c += 16) {
-                float v[16];
+                for (uint32_t c = c0; c < min(c0 + cols, kLinTile) && n0 + c < P.e.N; c += 32) {
+                    float x[32];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) v[i] = 0.f;
+                    for (int i = 0; i < 32; ++i) x[i] = 0.f;
 #pragma unroll 1
-                for (uint32_t r = 0; r < P.splits; ++r) {              // K-ranges in order
-                    const uint32_t src = mapa_shared(base, r) + ((c * kLinTile) + quad * 32u + lane) * 4u;
+                    for (uint32_t r = 0; r < P.splits; ++r) {              // K-ranges in order
+                        const uint32_t src = mapa_shared(base, r) + ((c * kLinTile) + quad * 32u + lane) * 4u;
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] += ld_dsmem(src + i * kLinTile * 4u);
+                        for (int i = 0; i < 32; ++i) x[i] += ld_dsmem(src + i * kLinTile * 4u);
+                    }
+                    if (P.e.form == 1) write_rows<ACT, false>(P.e, &map_c, &map_z, out, x, sa, row0, n0 + c, lane);
+                    else if (P.e.form == 2) write_rows<ACT, true>(P.e, &map_c, &map_z, out, x, sa, row0, n0 + c, lane);
+                    else {
+                        float* tile = reinterpret_cast<float*>(out.base);
+                        stage_write<32>(tile, lane, x);
+                        __syncwarp();
+                        write_chunk_any<32, ACT>(P.e, tile, row0, n0 + c, lane);
+                        __syncwarp();
+                    }
                 }
-                write_out16(P.e, row, n0 + c, v);
+                if (P.e.form) out.finish(lane);
             }
         }
         cluster_arrive_wait();                            // no CTA leaves while another reads its shared memory
@@ -329,14 +465,15 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // thousands of steps shows in fp32 (relative error 9e-6 at K = 8192, growing with K; a bf16 result hides it).  So the
 // accumulator is handed over every `chunk` K-blocks and the epilogue warps keep the sum in registers with ordinary
 // rounded additions; the two slots take turns by chunk instead of by tile.
-constexpr uint32_t kLpStages = 6, kLpThreads = 384, kLpEpiWarp0 = 4, kLpBand = 8;
-constexpr uint32_t kLpSmem = kLpStages * kLinStage + 1024;
+constexpr uint32_t kLpMaxStages = 6, kLpThreads = 384, kLpEpiWarp0 = 4, kLpBand = 8;
+constexpr uint32_t kLpSmemMost = 227 * 1024 - 256;       // (what is declared statically comes on top)
 
 struct PairParams {
     Epilogue e;
     uint32_t K_blocks, chunk, bn, b_boxes, b_bytes;      // b_bytes: what one CTA loads of B per stage
     uint32_t tiles_m, tiles_n;
     uint32_t a_mn, b_mn;
+    uint32_t stages, out_bytes, out_count;               // operand ring; output buffers of a write-out warp
     unsigned long long wait_limit_ns;
 };
 // mbar_wait_cl without a call (a call would have to save the caller's sums)
@@ -351,7 +488,7 @@ __device__ __forceinline__ bool pair_wait_inline(uint32_t bar, uint32_t parity, 
     return true;
 }
 struct __align__(16) LpShared {
-    uint64_t full[kLpStages], empty[kLpStages], acc_full[2], acc_empty[2], drain;
+    uint64_t full[kLpMaxStages], empty[kLpMaxStages], acc_full[2], acc_empty[2], drain;
     uint32_t tmem_base, abort_flag;
 };
 // tile number -> row and column tile: bands of kLpBand row tiles, column by column inside a band
@@ -368,9 +505,10 @@ __device__ __forceinline__ void umma_pair(uint32_t d_tmem, uint64_t a_desc, uint
     else umma_bf16_pair(d_tmem, a_desc, b_desc, idesc, accumulate);
 }
 
-template <bool E4M3, bool LONG>
+template <bool E4M3, bool LONG, uint32_t ACT>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLpThreads, 1)
-linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ PairParams P) {
+linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c,
+                   const __grid_constant__ CUtensorMap map_z, const __grid_constant__ PairParams P) {
     extern __shared__ uint8_t dyn_smem[];
     __shared__ LpShared sh;
     constexpr uint32_t kBlk = E4M3 ? 128u : 64u;
@@ -380,7 +518,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const WaitCtx W = {&sh.abort_flag, &g_linear_status, P.wait_limit_ns};
 
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < kLpStages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
+        for (uint32_t s = 0; s < P.stages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&sh.acc_full[a]), 1); mbar_init(smem_u32(&sh.acc_empty[a]), LONG ? 16 : 8); }
         mbar_init(smem_u32(&sh.drain), 1);
         sh.abort_flag = 0;
@@ -398,13 +536,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         if (warp == 0 && lane == 0) {
             // ---- producer (both CTAs) ----
             const uint32_t full0 = mapa_shared(smem_u32(&sh.full[0]), 0u), tx = 2u * (kLinOperand + P.b_bytes);
-            uint32_t it = 0;
+            uint32_t s = 0, ph = 0;
             bool ok = true;
             for (uint32_t t = cluster; ok && t < tiles; t += clusters) {
                 const uint2 at = pair_tile(P, t);
                 const int32_t m = (int32_t)(at.x * 256u + rank * 128u), n = (int32_t)(at.y * P.bn + rank * (P.bn / 2));
-                for (uint32_t kb = 0; kb < P.K_blocks; ++kb, ++it) {
-                    const uint32_t s = it % kLpStages, ph = (it / kLpStages) & 1u;
+                for (uint32_t kb = 0; kb < P.K_blocks; ++kb) {
                     if (!mbar_wait_cl(smem_u32(&sh.empty[s]), ph ^ 1u, W)) { ok = false; break; }
                     if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full[s]), tx);
                     const uint32_t bar = full0 + s * 8u, sa = base + s * kLinStage, sb = sa + kLinOperand;
@@ -413,6 +550,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     else tma_load_2d_pair(sa, &map_a, bar, k, m);
                     if (P.b_mn) for (uint32_t j = 0; j < P.b_boxes; ++j) tma_load_2d_pair(sb + j * kSubBytes, &map_b, bar, n + 64 * (int32_t)j, k);
                     else tma_load_2d_pair(sb, &map_b, bar, k, n);
+                    if (++s == P.stages) { s = 0; ph ^= 1u; }
                 }
             }
         } else if (warp == 1 && lane == 0 && rank == 0) {
@@ -420,15 +558,14 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const uint32_t idesc = E4M3 ? instr_desc_e4m3(256, P.bn) : instr_desc_bf16(256, P.bn, P.a_mn, P.b_mn);
             const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
             const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
-            uint32_t it = 0, use = 0;                 // stages and accumulator slots used so far
+            uint32_t s = 0, ph = 0, use = 0;          // stage, its phase, accumulator slots used so far
             bool ok = true;
             for (uint32_t t = cluster; ok && t < tiles; t += clusters) {
                 for (uint32_t k0 = 0; ok && k0 < P.K_blocks; k0 += P.chunk, ++use) {
                     const uint32_t k1 = min(P.K_blocks, k0 + P.chunk), acc = use & 1u, d = tmem + acc * 256u;
                     if (!mbar_wait_cl(smem_u32(&sh.acc_empty[acc]), ((use >> 1) & 1u) ^ 1u, W)) { ok = false; break; }
                     tc_fence_after();
-                    for (uint32_t kb = k0; kb < k1; ++kb, ++it) {
-                        const uint32_t s = it % kLpStages, ph = (it / kLpStages) & 1u;
+                    for (uint32_t kb = k0; kb < k1; ++kb) {
                         if (!mbar_wait_cl(smem_u32(&sh.full[s]), ph, W)) { ok = false; break; }
                         tc_fence_after();
                         const uint32_t sa = base + s * kLinStage, sb = sa + kLinOperand;
@@ -436,6 +573,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                         for (uint32_t q = 0; q < 4; ++q)
                             umma_pair<E4M3>(d, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, (kb != k0) | (q != 0u));
                         umma_commit_both(smem_u32(&sh.empty[s]));
+                        if (++s == P.stages) { s = 0; ph ^= 1u; }
                     }
                     if (ok) umma_commit_both(smem_u32(&sh.acc_full[acc]));
                 }
@@ -451,33 +589,23 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         if constexpr (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         const uint32_t quad = warp & 3u, group = (warp - kLpEpiWarp0) >> 2;
         const uint32_t lane_base = (quad * 32u) << 16;
+        OutRing out = {dyn_smem + (base - smem_u32(dyn_smem)) + P.stages * kLinStage + (warp - kLpEpiWarp0) * (P.out_bytes * P.out_count), P.out_bytes, P.out_count, 0u};
         if constexpr (!LONG) {
             // group g drains slot g: every second tile of the cluster
             const uint32_t empty = mapa_shared(smem_u32(&sh.acc_empty[group]), 0u), taddr = tmem + group * 256u + lane_base;
             uint32_t use = 0;
             for (uint32_t t = cluster + group * clusters; t < tiles; t += 2 * clusters, ++use) {
                 const uint2 at = pair_tile(P, t);
-                const uint32_t row = at.x * 256u + rank * 128u + quad * 32u + lane, col = at.y * P.bn;
+                const uint32_t row0 = at.x * 256u + rank * 128u + quad * 32u, col = at.y * P.bn;
+                prefetch_strip(P.e.mul, P.e.mul_type, P.e.ldmul, P.e, row0 + lane, col, P.bn);
+                prefetch_strip(P.e.res, P.e.res_type, P.e.ldres, P.e, row0 + lane, col, P.bn);
                 if (!__all_sync(0xFFFFFFFFu, mbar_wait_cl(smem_u32(&sh.acc_full[group]), use & 1u, W))) break;
                 tc_fence_after();
-#pragma unroll 1
-                for (uint32_t c = 0; c < P.bn; c += 32) {
-                    uint32_t u[32];
-                    tmem_ld_32x32(taddr + c, u);
-                    tmem_ld_wait();
-                    if (c + 32 >= P.bn) {             // the slot is read: hand it back
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive_cluster_read_done(empty);
-                    }
-                    float v[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[i]);
-                    write_out16(P.e, row, col + c, v);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(u[16 + i]);
-                    write_out16(P.e, row, col + c + 16, v);
-                }
+                write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, row0, col, P.bn, lane, [&] {       // the slot is read: hand it back
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster_read_done(empty);
+                });
             }
         } else {
             // all eight warps on one tile: group g keeps columns 128 g ... of its rows; the finished sums go back into
@@ -486,7 +614,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             bool ok = true;
             for (uint32_t t = cluster; ok && t < tiles; t += clusters) {
                 const uint2 at = pair_tile(P, t);
-                const uint32_t row = at.x * 256u + rank * 128u + quad * 32u + lane, col = at.y * P.bn + group * 128u;
+                const uint32_t row0 = at.x * 256u + rank * 128u + quad * 32u, col = at.y * P.bn + group * 128u;
                 const uint32_t cols = P.bn > group * 128u ? min(128u, P.bn - group * 128u) : 0u;
                 float sum[128];
 #pragma unroll
@@ -508,12 +636,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 #pragma unroll
                         for (uint32_t c = 0; c < 128; c += 32) tmem_st_32x32(taddr + c, sum + c);
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-#pragma unroll 1
-                        for (uint32_t c = 0; c < cols; c += 16) {
-                            float v[16];
-                            tmem_ld_32x16(taddr + c, v);
-                            write_out16(P.e, row, col + c, v);
-                        }
+                        if (cols) write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, row0, col, cols, lane, [] {});
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -521,6 +644,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                 }
             }
         }
+        if (P.e.form) out.finish(lane);               // the last stores are complete, their buffers read
         tc_fence_before();
     }
     __syncwarp();
@@ -552,7 +676,48 @@ int encode_operand(CUtensorMap* out, const void* base, uint64_t rows, uint64_t c
     return r == CUDA_SUCCESS ? 0 : CLEAVE_E_CUDA;
 }
 
-bool wide16(const void* p, uint64_t ld, uint32_t type) { return ((uintptr_t)p & 15) == 0 && (ld * type_bytes(type)) % 16 == 0; }
+// four neighbouring elements from a multiple of four columns on can be had with one access
+// Boxes of 32 x 32 of a row-major [rows x cols] output, bf16 or fp32, for bulk stores.
+int encode_output(CUtensorMap* out, void* base, uint64_t rows, uint64_t cols, uint64_t ld, bool f32) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return CLEAVE_E_CUDA;
+    cuuint64_t dims[2] = {cols, rows};
+    cuuint64_t strides[1] = {ld * (f32 ? 4u : 2u)};
+    cuuint32_t box[2] = {32, 32};
+    cuuint32_t estr[2] = {1, 1};
+    const CUresult r = fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                          CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? 0 : CLEAVE_E_CUDA;
+}
+
+bool rows16(const void* p, uint64_t ld, uint32_t type) { return (uintptr_t)p % 16 == 0 && (ld * type_bytes(type)) % 16 == 0; }
+bool wide4(const void* p, uint64_t ld, uint32_t type) { return (uintptr_t)p % (4 * type_bytes(type) + !type_bytes(type)) == 0 && ld % 4 == 0; }
+
+constexpr uint32_t kActs = CLEAVE_ACT_SILU + 1;
+using PairKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const PairParams);
+using SplitKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const LinearParams);
+struct PickPair {
+    using Kernel = PairKernel;
+    template <uint32_t ACT> static Kernel get(bool e4m3, bool lng) {
+        if (e4m3) return lng ? linear_pair_kernel<true, true, ACT> : linear_pair_kernel<true, false, ACT>;
+        return lng ? linear_pair_kernel<false, true, ACT> : linear_pair_kernel<false, false, ACT>;
+    }
+};
+struct PickSplit {
+    using Kernel = SplitKernel;
+    template <uint32_t ACT> static Kernel get(bool e4m3, bool) { return e4m3 ? linear_split_kernel<true, ACT> : linear_split_kernel<false, ACT>; }
+};
+template <typename Pick>
+typename Pick::Kernel pick_act(uint32_t act, bool e4m3, bool lng) {
+    switch (act) {
+        case CLEAVE_ACT_RELU: return Pick::template get<CLEAVE_ACT_RELU>(e4m3, lng);
+        case CLEAVE_ACT_GELU: return Pick::template get<CLEAVE_ACT_GELU>(e4m3, lng);
+        case CLEAVE_ACT_GELU_TANH: return Pick::template get<CLEAVE_ACT_GELU_TANH>(e4m3, lng);
+        case CLEAVE_ACT_SILU: return Pick::template get<CLEAVE_ACT_SILU>(e4m3, lng);
+        default: return Pick::template get<CLEAVE_ACT_NONE>(e4m3, lng);
+    }
+}
 
 }  // namespace
 
@@ -561,20 +726,28 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     const cleave_gemm_t& g = d.g;
     LinearParams P = {};
     Epilogue& e = P.e;
-    e.M = g.M; e.N = g.N; e.act = d.act;
+    e.M = g.M; e.N = g.N;
     e.c_type = d.c_type; e.bias_type = d.bias_type; e.z_type = d.z_type; e.mul_type = d.mul_type; e.res_type = d.res_type;
     e.scale_a = d.scale_a; e.scale_b = d.scale_b; e.bias = d.bias; e.z = d.z; e.mul = d.mul; e.res = d.res; e.C = d.C;
     e.ldz = d.ldz; e.ldmul = d.ldmul; e.ldres = d.ldres; e.ldc = d.ldc;
-    e.wide = (wide16(d.scale_b, 0, CLEAVE_T_F32) ? kWideB : 0u) | (wide16(d.bias, 0, d.bias_type) ? kWideBias : 0u) |
-             (wide16(d.z, d.ldz, d.z_type) ? kWideZ : 0u) | (wide16(d.mul, d.ldmul, d.mul_type) ? kWideMul : 0u) |
-             (wide16(d.res, d.ldres, d.res_type) ? kWideRes : 0u) | (wide16(d.C, d.ldc, d.c_type) ? kWideC : 0u);
+    e.wide = (wide4(d.scale_b, 0, CLEAVE_T_F32) ? kWideB : 0u) | (wide4(d.bias, 0, d.bias_type) ? kWideBias : 0u) |
+             (wide4(d.z, d.ldz, d.z_type) ? kWideZ : 0u) | (wide4(d.mul, d.ldmul, d.mul_type) ? kWideMul : 0u) |
+             (wide4(d.res, d.ldres, d.res_type) ? kWideRes : 0u) | (wide4(d.C, d.ldc, d.c_type) ? kWideC : 0u);
+    // bulk stores want 16-byte rows, and so do the row loads of mul and res
+    const bool bulk = rows16(d.C, d.ldc, d.c_type) && d.ldc * type_bytes(d.c_type) < (1ull << 40) && (!d.z || (d.z_type == CLEAVE_T_BF16 && rows16(d.z, d.ldz, d.z_type) && d.ldz < (1ull << 39))) &&
+                      (!d.mul || rows16(d.mul, d.ldmul, d.mul_type)) && (!d.res || rows16(d.res, d.ldres, d.res_type));
+    e.form = !bulk ? 0u : (d.c_type == CLEAVE_T_BF16 ? 1u : 2u);
+    CUtensorMap mc = {}, mz = {};
+    int rc = 0;
+    if (e.form && (rc = encode_output(&mc, d.C, g.M, g.N, d.ldc, e.form == 2))) return rc;
+    if (e.form && d.z && (rc = encode_output(&mz, d.z, g.M, g.N, d.ldz, false))) return rc;
     P.wait_limit_ns = g_linear_wait_limit.load(std::memory_order_relaxed);
     P.a_mn = g.transA ? 1u : 0u;
     P.b_mn = g.transB ? 0u : 1u;
     const uint32_t kblk = e4m3 ? 128u : 64u;
     P.K_blocks = (g.K + kblk - 1) / kblk;
     CUtensorMap ma, mb;
-    int rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, 128, e4m3);
+    rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, 128, e4m3);
     if (rc) return rc;
     auto encode_b = [&](uint32_t rows) { return g.transB ? encode_operand(&mb, d.B, g.N, g.K, g.ldb, rows, e4m3) : encode_operand(&mb, d.B, g.K, g.N, g.ldb, 64, e4m3); };
     cudaLaunchConfig_t cfg = {};
@@ -602,31 +775,36 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         const bool lng = (d.c_type == CLEAVE_T_F32 || d.z_type == CLEAVE_T_F32) && g.K > kLongK;
         Q.chunk = lng ? kLongK / kblk : Q.K_blocks;
         if ((rc = encode_b(Q.bn / 2))) return rc;
-        auto kernel = e4m3 ? (lng ? linear_pair_kernel<true, true> : linear_pair_kernel<true, false>)
-                           : (lng ? linear_pair_kernel<false, true> : linear_pair_kernel<false, false>);
-        static SmemLimit limit[4];
-        if (limit[(e4m3 ? 2 : 0) + (lng ? 1 : 0)].raise(reinterpret_cast<const void*>(kernel), kLpSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+        // output buffers in turn: two, or three with a second output; what is left of the shared memory holds stages
+        Q.out_bytes = e.form == 2 || !e.form ? 4096u : 2048u;
+        Q.out_count = e.form ? (d.z ? 3u : 2u) : 1u;
+        const uint32_t out_smem = 8 * Q.out_bytes * Q.out_count;
+        Q.stages = min(kLpMaxStages, (kLpSmemMost - 1024u - out_smem) / kLinStage);
+        const uint32_t smem = Q.stages * kLinStage + 1024u + out_smem;
+        const PairKernel kernel = pick_act<PickPair>(d.act, e4m3, lng);
+        static SmemLimit limit[4 * kActs];
+        if (limit[((e4m3 ? 2 : 0) + (lng ? 1 : 0)) * kActs + d.act].raise(reinterpret_cast<const void*>(kernel), kLpSmemMost) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
         const uint64_t all = (uint64_t)Q.tiles_m * Q.tiles_n;
         if (all > 0x7FFFFFFFull) return CLEAVE_E_UNSUPPORTED;
         cfg.gridDim = dim3(2u * (unsigned)(all < pairs ? all : pairs));
         cfg.blockDim = dim3(kLpThreads);
-        cfg.dynamicSmemBytes = kLpSmem;
+        cfg.dynamicSmemBytes = smem;
         cfg.numAttrs = 0;                                   // (the cluster size is the kernel's own)
-        err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, Q);
+        err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, mc, mz, Q);
     } else {
         P.tiles_n = (uint32_t)tiles_n;
         // K is split while every CTA still finds a place at once (two an SM) and keeps at least four stages of work
         P.splits = 1;
         while (P.splits < 8 && tiles * P.splits * 2 <= 2u * (uint32_t)sms && P.K_blocks / (P.splits * 2) >= 4) P.splits *= 2;
         if ((rc = encode_b(kLinTile))) return rc;
-        auto kernel = e4m3 ? linear_split_kernel<true> : linear_split_kernel<false>;
-        static SmemLimit limit[2];
-        if (limit[e4m3 ? 1 : 0].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+        const SplitKernel kernel = pick_act<PickSplit>(d.act, e4m3, false);
+        static SmemLimit limit[2 * kActs];
+        if (limit[(e4m3 ? 1 : 0) * kActs + d.act].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
         cfg.gridDim = dim3((unsigned)(tiles * P.splits));
         cfg.blockDim = dim3(kLinThreads);
         cfg.dynamicSmemBytes = kLinSmem;
         attr[0].val.clusterDim.x = P.splits;
-        err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, P);
+        err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, mc, mz, P);
     }
     if (err != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
     return 0;
