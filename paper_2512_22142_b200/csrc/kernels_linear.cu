@@ -14,6 +14,7 @@
 //
 // Every wait is bounded (2 s by default): a wait that runs out records it in a status word of the library, the
 // CTA's roles leave, copies and MMAs in flight are given time to end, and the kernel returns.
+#include <algorithm>
 #include <atomic>
 #include <type_traits>
 
@@ -50,7 +51,7 @@ enum : uint32_t { kWideB = 1u, kWideBias = 2u, kWideZ = 4u, kWideMul = 8u, kWide
 struct LinearParams {
     Epilogue e;
     uint32_t K_blocks, splits, tiles_n;
-    uint32_t a_mn, b_mn;
+    uint32_t a_mn, b_mn, a_rows;    // a_rows: rows of a K-contiguous A that a stage brings
     unsigned long long wait_limit_ns;
 };
 
@@ -157,7 +158,7 @@ struct OutRing {
     uint8_t* base;
     uint32_t bytes, count, next;
     __device__ __forceinline__ uint8_t* take(uint32_t lane) {
-        if (lane == 0) { if (count >= 3) asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory"); else asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); }
+        if (lane == 0) { if (count >= 3) asm volatile("cp.async.bulk.wait_group.read 2;" ::: "memory"); else if (count == 2) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory"); else bulk_wait_read_all(); }
         __syncwarp();
         uint8_t* b = base + next * bytes;
         next = next + 1 == count ? 0 : next + 1;
@@ -171,22 +172,31 @@ struct OutRing {
     __device__ __forceinline__ void finish(uint32_t lane) { if (lane == 0) bulk_wait_all(); __syncwarp(); }
 };
 
+// A column's scale and bias, a lane a column: asked for one chunk ahead.
+struct ColumnPair { float scale, bias; };
+__device__ __forceinline__ ColumnPair load_columns(const Epilogue& e, uint32_t col) {
+    ColumnPair p = {0.f, 0.f};
+    if (col < e.N) {
+        if (e.scale_b) p.scale = __ldg(e.scale_b + col);
+        if (e.bias) p.bias = load_as(e.bias, e.bias_type, col);
+    }
+    return p;
+}
 // One chunk, 32 columns from `col` on, a lane a row (row0 + lane), from its fp32 sums x to C (and z) through bulk stores,
 // which leave out what lies beyond C's edges.
 template <uint32_t ACT, bool F32>
 __device__ __forceinline__ void write_rows(const Epilogue& e, const CUtensorMap* map_c, const CUtensorMap* map_z, OutRing& out, float (&x)[32], float sa,
-                                           uint32_t row0, uint32_t col, uint32_t lane) {
+                                           ColumnPair columns, uint32_t row0, uint32_t col, uint32_t lane) {
     uint8_t* buf = out.take(lane);
-    const uint32_t mine = col + lane;
     if (e.scale_a) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) x[i] *= sa;
     }
     if (e.scale_b || e.bias) {
-        // the columns' scales and biases, a lane a column, through the (still empty) buffer to every lane
+        // through the (still empty) buffer to every lane
         float* vec = reinterpret_cast<float*>(buf);
-        if (e.scale_b) vec[lane] = mine < e.N ? __ldg(e.scale_b + mine) : 0.f;
-        if (e.bias) vec[32 + lane] = mine < e.N ? load_as(e.bias, e.bias_type, mine) : 0.f;
+        vec[lane] = columns.scale;
+        vec[32 + lane] = columns.bias;
         __syncwarp();
         if (e.scale_b) {
 #pragma unroll
@@ -224,34 +234,46 @@ __device__ __forceinline__ void write_rows(const Epilogue& e, const CUtensorMap*
     stage_out<F32>(buf, lane, x);
     out.store(map_c, buf, col, row0, lane);
 }
-// A warp's strip of the accumulator, 32 rows x `cols` columns from tensor-memory address taddr on, to its place in C.
-// `read` is called when the accumulator has been read for the last time.
-template <uint32_t ACT, typename Read>
-__device__ __forceinline__ void write_strip(const Epilogue& e, const CUtensorMap* map_c, const CUtensorMap* map_z, OutRing& out, uint32_t taddr, uint32_t row0,
-                                            uint32_t col, uint32_t cols, uint32_t lane, Read read) {
+template <uint32_t ACT>
+__device__ __forceinline__ void write_piece(const Epilogue& e, const CUtensorMap* map_c, const CUtensorMap* map_z, OutRing& out, float (&x)[32], float sa,
+                                            ColumnPair columns, uint32_t row0, uint32_t col, uint32_t lane) {
+    if (row0 >= e.M || col >= e.N) return;
+    if (e.form == 1) write_rows<ACT, false>(e, map_c, map_z, out, x, sa, columns, row0, col, lane);
+    else if (e.form == 2) write_rows<ACT, true>(e, map_c, map_z, out, x, sa, columns, row0, col, lane);
+    else {
+        float* tile = reinterpret_cast<float*>(out.base);
+        stage_write<32>(tile, lane, x);
+        __syncwarp();
+        write_chunk_any<32, ACT>(e, tile, row0, col, lane);
+        __syncwarp();
+    }
+}
+// A warp's part of the accumulator, 32 rows from row0 on, to its place in C: the chunks of 32 columns at c, c + step, ... of
+// the `cols` columns that begin at tensor-memory address taddr and column col.  `ready` waits for the accumulator;
+// `read` is called when the warp has read it for the last time.
+template <uint32_t ACT, typename Ready, typename Read>
+__device__ __forceinline__ bool write_strip(const Epilogue& e, const CUtensorMap* map_c, const CUtensorMap* map_z, OutRing& out, uint32_t taddr, uint32_t row0,
+                                            uint32_t col, uint32_t c, uint32_t step, uint32_t cols, uint32_t lane, Ready ready, Read read) {
     const float sa = e.scale_a && row0 + lane < e.M ? __ldg(e.scale_a + row0 + lane) : 1.f;
+    ColumnPair next = load_columns(e, col + c + lane);
+    if (!ready()) return false;
+    if (c >= cols) read();
 #pragma unroll 1
-    for (uint32_t c = 0; c < cols; c += 32) {
+    for (; c < cols; c += step) {
+        const ColumnPair columns = next;
         float x[32];
         {
             uint32_t u[32];
             tmem_ld_32x32(taddr + c, u);
+            if (c + step < cols) next = load_columns(e, col + c + step + lane);
             tmem_ld_wait();
-            if (c + 32 >= cols) read();
+            if (c + step >= cols) read();
 #pragma unroll
             for (int i = 0; i < 32; ++i) x[i] = __uint_as_float(u[i]);
         }
-        if (row0 >= e.M || col + c >= e.N) continue;
-        if (e.form == 1) write_rows<ACT, false>(e, map_c, map_z, out, x, sa, row0, col + c, lane);
-        else if (e.form == 2) write_rows<ACT, true>(e, map_c, map_z, out, x, sa, row0, col + c, lane);
-        else {
-            float* tile = reinterpret_cast<float*>(out.base);
-            stage_write<32>(tile, lane, x);
-            __syncwarp();
-            write_chunk_any<32, ACT>(e, tile, row0, col + c, lane);
-            __syncwarp();
-        }
+        write_piece<ACT>(e, map_c, map_z, out, x, sa, columns, row0, col + c, lane);
     }
+    return true;
 }
 // The rows of mul and res that a strip of 32 rows x `cols` columns will need, brought into L2 ahead of time.
 __device__ __forceinline__ void prefetch_strip(const void* p, uint32_t type, uint64_t ld, const Epilogue& e, uint32_t row, uint32_t col, uint32_t cols) {
@@ -355,7 +377,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             const uint32_t s = it % kLinStages, ph = (it / kLinStages) & 1u;
             if (!lin_wait(smem_u32(&sh.empty[s]), ph ^ 1u, W)) break;
             const uint32_t bar = smem_u32(&sh.full[s]), sa = base + s * kLinStage, sb = sa + kLinOperand;
-            mbar_arrive_expect_tx(bar, kLinStage);
+            mbar_arrive_expect_tx(bar, kLinOperand + P.a_rows * 128u);
             const int32_t k = (int32_t)(kb * kBlk);
             if (P.a_mn) { tma_load_2d(sa, &map_a, bar, (int32_t)m0, k); tma_load_2d(sa + kSubBytes, &map_a, bar, (int32_t)m0 + 64, k); }
             else tma_load_2d(sa, &map_a, bar, k, (int32_t)m0);
@@ -393,9 +415,11 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         ok = __all_sync(0xFFFFFFFFu, lin_wait(smem_u32(&sh.acc_full), 0u, W));
         tc_fence_after();
         const uint32_t taddr = tmem + ((quad * 32u) << 16);
-        if (ok && P.splits == 1) {
+        if (m0 + quad * 32u >= P.e.M) {
+            // (no rows for this warp)
+        } else if (ok && P.splits == 1) {
             OutRing out = {dyn_smem + (base - smem_u32(dyn_smem)) + (warp - 2) * 12288, 4096u, 3u, 0u};        // the stages are read
-            write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, m0 + quad * 32u, n0, kLinTile, lane, [] {});
+            write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, m0 + quad * 32u, n0, 0u, 32u, kLinTile, lane, [] { return true; }, [] {});
             if (P.e.form) out.finish(lane);
         } else if (ok) {
             float* part = reinterpret_cast<float*>(dyn_smem + (base - smem_u32(dyn_smem)));      // the stages are read: column-major [128][128]
@@ -424,20 +448,18 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 #pragma unroll
                     for (int i = 0; i < 32; ++i) x[i] = 0.f;
 #pragma unroll 1
-                    for (uint32_t r = 0; r < P.splits; ++r) {              // K-ranges in order
-                        const uint32_t src = mapa_shared(base, r) + ((c * kLinTile) + quad * 32u + lane) * 4u;
+                    for (uint32_t r = 0; r < P.splits; r += 2) {           // K-ranges in order, two asked for at a time
+                        const uint32_t off = ((c * kLinTile) + quad * 32u + lane) * 4u, s0 = mapa_shared(base, r) + off, s1 = mapa_shared(base, r + 1) + off;
+                        float y[32];
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) x[i] += ld_dsmem(src + i * kLinTile * 4u);
+                        for (int i = 0; i < 32; ++i) y[i] = ld_dsmem(s0 + i * kLinTile * 4u);
+                        float w[32];
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) w[i] = ld_dsmem(s1 + i * kLinTile * 4u);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) x[i] = (x[i] + y[i]) + w[i];
                     }
-                    if (P.e.form == 1) write_rows<ACT, false>(P.e, &map_c, &map_z, out, x, sa, row0, n0 + c, lane);
-                    else if (P.e.form == 2) write_rows<ACT, true>(P.e, &map_c, &map_z, out, x, sa, row0, n0 + c, lane);
-                    else {
-                        float* tile = reinterpret_cast<float*>(out.base);
-                        stage_write<32>(tile, lane, x);
-                        __syncwarp();
-                        write_chunk_any<32, ACT>(P.e, tile, row0, n0 + c, lane);
-                        __syncwarp();
-                    }
+                    write_piece<ACT>(P.e, &map_c, &map_z, out, x, sa, load_columns(P.e, n0 + c + lane), row0, n0 + c, lane);
                 }
                 if (P.e.form) out.finish(lane);
             }
@@ -465,14 +487,19 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // thousands of steps shows in fp32 (relative error 9e-6 at K = 8192, growing with K; a bf16 result hides it).  So the
 // accumulator is handed over every `chunk` K-blocks and the epilogue warps keep the sum in registers with ordinary
 // rounded additions; the two slots take turns by chunk instead of by tile.
-constexpr uint32_t kLpMaxStages = 6, kLpThreads = 384, kLpEpiWarp0 = 4, kLpBand = 8;
+constexpr uint32_t kLpMaxStages = 6, kLpEpiWarp0 = 4, kLpBand = 8;
+// Write-out warps: 16 keep pace with the products of a short K (bias, activation and a second output: 55 -> 50 us at 8192 x 768
+// x 3072 against 8); LONG takes 8, whose threads hold 128 sums each (with 16, what else they need spills: 419 -> 544 us
+// at 8192 x 8192 x 4096).
+__host__ __device__ constexpr uint32_t pair_warps(bool lng) { return lng ? 8u : 16u; }
+__host__ __device__ constexpr uint32_t pair_threads(bool lng) { return 32u * (kLpEpiWarp0 + pair_warps(lng)); }
 constexpr uint32_t kLpSmemMost = 227 * 1024 - 256;       // (what is declared statically comes on top)
 
 struct PairParams {
     Epilogue e;
     uint32_t K_blocks, chunk, bn, b_boxes, b_bytes;      // b_bytes: what one CTA loads of B per stage
     uint32_t tiles_m, tiles_n;
-    uint32_t a_mn, b_mn;
+    uint32_t a_mn, b_mn;                                 // 0: K-contiguous, 1: M/N-contiguous in boxes of 64, 2: in double boxes
     uint32_t stages, out_bytes, out_count;               // operand ring; output buffers of a write-out warp
     unsigned long long wait_limit_ns;
 };
@@ -506,7 +533,7 @@ __device__ __forceinline__ void umma_pair(uint32_t d_tmem, uint64_t a_desc, uint
 }
 
 template <bool E4M3, bool LONG, uint32_t ACT>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLpThreads, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(pair_threads(LONG), 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c,
                    const __grid_constant__ CUtensorMap map_z, const __grid_constant__ PairParams P) {
     extern __shared__ uint8_t dyn_smem[];
@@ -519,7 +546,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < P.stages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&sh.acc_full[a]), 1); mbar_init(smem_u32(&sh.acc_empty[a]), LONG ? 16 : 8); }
+        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&sh.acc_full[a]), 1); mbar_init(smem_u32(&sh.acc_empty[a]), 16); }
         mbar_init(smem_u32(&sh.drain), 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -532,7 +559,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const uint32_t tmem = sh.tmem_base;
 
     if (warp < kLpEpiWarp0) {
-        if constexpr (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");
+        if constexpr (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");       // 128 x 40 + 256 x 216 <= 384 x 168 registers
         if (warp == 0 && lane == 0) {
             // ---- producer (both CTAs) ----
             const uint32_t full0 = mapa_shared(smem_u32(&sh.full[0]), 0u), tx = 2u * (kLinOperand + P.b_bytes);
@@ -546,16 +573,18 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
                     if (rank == 0) mbar_arrive_expect_tx(smem_u32(&sh.full[s]), tx);
                     const uint32_t bar = full0 + s * 8u, sa = base + s * kLinStage, sb = sa + kLinOperand;
                     const int32_t k = (int32_t)(kb * kBlk);
-                    if (P.a_mn) { tma_load_2d_pair(sa, &map_a, bar, m, k); tma_load_2d_pair(sa + kSubBytes, &map_a, bar, m + 64, k); }
+                    if (P.a_mn == 2) tma_load_3d_pair(sa, &map_a, bar, 0, k, m / 64);
+                    else if (P.a_mn) { tma_load_2d_pair(sa, &map_a, bar, m, k); tma_load_2d_pair(sa + kSubBytes, &map_a, bar, m + 64, k); }
                     else tma_load_2d_pair(sa, &map_a, bar, k, m);
-                    if (P.b_mn) for (uint32_t j = 0; j < P.b_boxes; ++j) tma_load_2d_pair(sb + j * kSubBytes, &map_b, bar, n + 64 * (int32_t)j, k);
+                    if (P.b_mn == 2) tma_load_3d_pair(sb, &map_b, bar, 0, k, n / 64);
+                    else if (P.b_mn) for (uint32_t j = 0; j < P.b_boxes; ++j) tma_load_2d_pair(sb + j * kSubBytes, &map_b, bar, n + 64 * (int32_t)j, k);
                     else tma_load_2d_pair(sb, &map_b, bar, k, n);
                     if (++s == P.stages) { s = 0; ph ^= 1u; }
                 }
             }
         } else if (warp == 1 && lane == 0 && rank == 0) {
             // ---- MMA issuer (leader) ----
-            const uint32_t idesc = E4M3 ? instr_desc_e4m3(256, P.bn) : instr_desc_bf16(256, P.bn, P.a_mn, P.b_mn);
+            const uint32_t idesc = E4M3 ? instr_desc_e4m3(256, P.bn) : instr_desc_bf16(256, P.bn, P.a_mn ? 1u : 0u, P.b_mn ? 1u : 0u);
             const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
             const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
             uint32_t s = 0, ph = 0, use = 0;          // stage, its phase, accumulator slots used so far
@@ -587,40 +616,47 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     } else {
         // ---- write-out (both CTAs) ----
         if constexpr (LONG) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
-        const uint32_t quad = warp & 3u, group = (warp - kLpEpiWarp0) >> 2;
+        const uint32_t quad = warp & 3u, part = (warp - kLpEpiWarp0) >> 2;      // four warps, one a quadrant of lanes, per part
         const uint32_t lane_base = (quad * 32u) << 16;
         OutRing out = {dyn_smem + (base - smem_u32(dyn_smem)) + P.stages * kLinStage + (warp - kLpEpiWarp0) * (P.out_bytes * P.out_count), P.out_bytes, P.out_count, 0u};
         if constexpr (!LONG) {
-            // group g drains slot g: every second tile of the cluster
+            // parts 0, 1 drain slot 0, parts 2, 3 slot 1 (every second tile of the cluster); the two parts of a slot
+            // take its chunks of 32 columns in turn
+            const uint32_t group = part >> 1, half = part & 1u;
             const uint32_t empty = mapa_shared(smem_u32(&sh.acc_empty[group]), 0u), taddr = tmem + group * 256u + lane_base;
             uint32_t use = 0;
             for (uint32_t t = cluster + group * clusters; t < tiles; t += 2 * clusters, ++use) {
                 const uint2 at = pair_tile(P, t);
                 const uint32_t row0 = at.x * 256u + rank * 128u + quad * 32u, col = at.y * P.bn;
-                prefetch_strip(P.e.mul, P.e.mul_type, P.e.ldmul, P.e, row0 + lane, col, P.bn);
-                prefetch_strip(P.e.res, P.e.res_type, P.e.ldres, P.e, row0 + lane, col, P.bn);
-                if (!__all_sync(0xFFFFFFFFu, mbar_wait_cl(smem_u32(&sh.acc_full[group]), use & 1u, W))) break;
-                tc_fence_after();
-                write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, row0, col, P.bn, lane, [&] {       // the slot is read: hand it back
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_cluster_read_done(empty);
-                });
+                if (half) prefetch_strip(P.e.mul, P.e.mul_type, P.e.ldmul, P.e, row0 + lane, col, P.bn);
+                else prefetch_strip(P.e.res, P.e.res_type, P.e.ldres, P.e, row0 + lane, col, P.bn);
+                const bool ok = write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, row0, col, half * 32u, 64u, P.bn, lane,
+                    [&] {
+                        const bool r = __all_sync(0xFFFFFFFFu, mbar_wait_cl(smem_u32(&sh.acc_full[group]), use & 1u, W));
+                        tc_fence_after();
+                        return r;
+                    },
+                    [&] {                             // the warp has read the slot: hand it back
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster_read_done(empty);
+                    });
+                if (!ok) break;
             }
         } else {
-            // all eight warps on one tile: group g keeps columns 128 g ... of its rows; the finished sums go back into
-            // the last slot, from where they are written out piece by piece (registers hold nothing else meanwhile)
+            // all eight warps on one tile: part p keeps columns 128 p ... of its rows; the finished sums go back into the last
+            // slot, from where they are written out piece by piece (registers hold nothing else meanwhile)
             uint32_t use = 0;
             bool ok = true;
             for (uint32_t t = cluster; ok && t < tiles; t += clusters) {
                 const uint2 at = pair_tile(P, t);
-                const uint32_t row0 = at.x * 256u + rank * 128u + quad * 32u, col = at.y * P.bn + group * 128u;
-                const uint32_t cols = P.bn > group * 128u ? min(128u, P.bn - group * 128u) : 0u;
+                const uint32_t row0 = at.x * 256u + rank * 128u + quad * 32u, col = at.y * P.bn + part * 128u;
+                const uint32_t cols = P.bn > part * 128u ? min(128u, P.bn - part * 128u) : 0u;
                 float sum[128];
 #pragma unroll
                 for (int i = 0; i < 128; ++i) sum[i] = 0.f;
                 for (uint32_t k0 = 0; k0 < P.K_blocks; k0 += P.chunk, ++use) {
-                    const uint32_t acc = use & 1u, taddr = tmem + acc * 256u + group * 128u + lane_base;
+                    const uint32_t acc = use & 1u, taddr = tmem + acc * 256u + part * 128u + lane_base;
                     ok = __all_sync(0xFFFFFFFFu, pair_wait_inline(smem_u32(&sh.acc_full[acc]), (use >> 1) & 1u, W));
                     if (!ok) break;
                     tc_fence_after();
@@ -636,7 +672,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
 #pragma unroll
                         for (uint32_t c = 0; c < 128; c += 32) tmem_st_32x32(taddr + c, sum + c);
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
-                        if (cols) write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, row0, col, cols, lane, [] {});
+                        if (cols) write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, row0, col, 0u, 32u, cols, lane, [] { return true; }, [] {});
                     }
                     tc_fence_before();
                     __syncwarp();
@@ -688,6 +724,20 @@ int encode_output(CUtensorMap* out, void* base, uint64_t rows, uint64_t cols, ui
     const CUresult r = fn(out, f32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, base, dims, strides, box, estr,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, f32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
                           CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? 0 : CLEAVE_E_CUDA;
+}
+
+// A row-major [rows x cols] bf16 matrix, cols a multiple of 64, as [cols / 64][rows][64]: a box of 64 x 64 x 2 brings two
+// neighbouring groups of 64 columns (8 KB each, one after the other) with one operation.
+int encode_groups(CUtensorMap* out, const void* base, uint64_t rows, uint64_t cols, uint64_t ld) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (!fn) return CLEAVE_E_CUDA;
+    cuuint64_t dims[3] = {64, rows, cols / 64};
+    cuuint64_t strides[2] = {ld * 2, 128};
+    cuuint32_t box[3] = {64, 64, 2};
+    cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? 0 : CLEAVE_E_CUDA;
 }
 
@@ -747,8 +797,6 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     const uint32_t kblk = e4m3 ? 128u : 64u;
     P.K_blocks = (g.K + kblk - 1) / kblk;
     CUtensorMap ma, mb;
-    rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, 128, e4m3);
-    if (rc) return rc;
     auto encode_b = [&](uint32_t rows) { return g.transB ? encode_operand(&mb, d.B, g.N, g.K, g.ldb, rows, e4m3) : encode_operand(&mb, d.B, g.K, g.N, g.ldb, 64, e4m3); };
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
@@ -764,21 +812,26 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         PairParams Q = {};
         Q.e = P.e; Q.K_blocks = P.K_blocks; Q.a_mn = P.a_mn; Q.b_mn = P.b_mn; Q.wait_limit_ns = P.wait_limit_ns;
         Q.tiles_m = (g.M + 255) / 256;
-        // the tile width whose waves cost the fewest columns a cluster
-        uint64_t best = ~0ull;
-        for (uint32_t bn = 256; bn >= 128; bn -= 32) {
-            const uint64_t n = (g.N + bn - 1) / bn, cost = ((uint64_t)Q.tiles_m * n + pairs - 1) / pairs * (bn + 16);
-            if (cost < best) { best = cost; Q.bn = bn; Q.tiles_n = (uint32_t)n; }
-        }
+        // 256 columns (the whole of a narrower C): narrower tiles fill the last wave better, but bring fewer products per
+        // byte from L2, about 62 bytes a cycle and SM, and lost at every size tried (8192 x 768 x 3072: 39 us with 256
+        // columns, 43 with 224 and 192, 56 with 128; 4096^3: 106, 127, 130, 160).
+        Q.bn = g.N >= 256 ? 256u : (g.N + 31) / 32 * 32;
+        Q.tiles_n = (g.N + Q.bn - 1) / Q.bn;
         Q.b_boxes = (Q.bn / 2 + 63) / 64;
         Q.b_bytes = Q.b_mn ? Q.b_boxes * kSubBytes : Q.bn / 2 * 128u;
         const bool lng = (d.c_type == CLEAVE_T_F32 || d.z_type == CLEAVE_T_F32) && g.K > kLongK;
         Q.chunk = lng ? kLongK / kblk : Q.K_blocks;
-        if ((rc = encode_b(Q.bn / 2))) return rc;
-        // output buffers in turn: two, or three with a second output; what is left of the shared memory holds stages
-        Q.out_bytes = e.form == 2 || !e.form ? 4096u : 2048u;
-        Q.out_count = e.form ? (d.z ? 3u : 2u) : 1u;
-        const uint32_t out_smem = 8 * Q.out_bytes * Q.out_count;
+        if (Q.a_mn && g.M % 64 == 0) { Q.a_mn = 2; rc = encode_groups(&ma, d.A, g.K, g.M, g.lda); }
+        else rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, 128, e4m3);
+        if (rc) return rc;
+        if (Q.b_mn && Q.bn == 256 && g.N % 64 == 0) { Q.b_mn = 2; rc = encode_groups(&mb, d.B, g.K, g.N, g.ldb); }
+        else rc = encode_b(Q.bn / 2);
+        if (rc) return rc;
+        // output buffers a warp takes in turn (one of 4 KB for the general form); the rest of the shared memory holds stages
+        const uint32_t out_warps = pair_warps(lng);
+        Q.out_bytes = e.form == 1 ? 2048u : 4096u;
+        Q.out_count = e.form == 1 ? 2u : (e.form == 2 && lng ? 2u : 1u);
+        const uint32_t out_smem = out_warps * Q.out_bytes * Q.out_count;
         Q.stages = min(kLpMaxStages, (kLpSmemMost - 1024u - out_smem) / kLinStage);
         const uint32_t smem = Q.stages * kLinStage + 1024u + out_smem;
         const PairKernel kernel = pick_act<PickPair>(d.act, e4m3, lng);
@@ -787,7 +840,7 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         const uint64_t all = (uint64_t)Q.tiles_m * Q.tiles_n;
         if (all > 0x7FFFFFFFull) return CLEAVE_E_UNSUPPORTED;
         cfg.gridDim = dim3(2u * (unsigned)(all < pairs ? all : pairs));
-        cfg.blockDim = dim3(kLpThreads);
+        cfg.blockDim = dim3(pair_threads(lng));
         cfg.dynamicSmemBytes = smem;
         cfg.numAttrs = 0;                                   // (the cluster size is the kernel's own)
         err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, mc, mz, Q);
@@ -796,7 +849,10 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         // K is split while every CTA still finds a place at once (two an SM) and keeps at least four stages of work
         P.splits = 1;
         while (P.splits < 8 && tiles * P.splits * 2 <= 2u * (uint32_t)sms && P.K_blocks / (P.splits * 2) >= 4) P.splits *= 2;
-        if ((rc = encode_b(kLinTile))) return rc;
+        // (K-contiguous rows of A beyond M need not even be zeros: they only reach accumulator rows that nobody reads)
+        P.a_rows = g.transA ? kLinTile : std::min(kLinTile, (g.M + 7) / 8 * 8);
+        rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, P.a_rows, e4m3);
+        if (rc || (rc = encode_b(kLinTile))) return rc;
         const SplitKernel kernel = pick_act<PickSplit>(d.act, e4m3, false);
         static SmemLimit limit[2 * kActs];
         if (limit[(e4m3 ? 1 : 0) * kActs + d.act].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
