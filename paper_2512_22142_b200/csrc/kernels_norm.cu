@@ -85,25 +85,31 @@ template <typename T> struct Bytes8 { static constexpr uint32_t value = sizeof(T
 template <> struct Bytes8<NoRes> { static constexpr uint32_t value = 0; };
 
 template <typename Desc>
-__device__ __forceinline__ void load_weight8(const Desc& d, uint32_t col, float (&w)[8]) {      // (the same for every row: L1)
+__device__ __forceinline__ void load_weight8(const Desc& d, uint32_t col, F2 (&w)[4]) {      // (the same for every row: L1)
     if (d.w_type == CLEAVE_T_F32) {
-        const float4* p = reinterpret_cast<const float4*>(static_cast<const float*>(d.w) + col);
-        const float4 a = __ldg(p), b = __ldg(p + 1);
-        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+        Raw8<float> r;
+        const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(d.w) + col);
+        r.w[0] = __ldg(p); r.w[1] = __ldg(p + 1);
+        unpack8(r, w);
     } else if (d.w_type == CLEAVE_T_BF16) {
         Raw8<__nv_bfloat16> r;
         r.w[0] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(d.w) + col));
         unpack8(r, w);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = 1.f;
+        for (int i = 0; i < 4; ++i) w[i] = f2(1.f, 1.f);
     }
+}
+// largest magnitude of a pair and `top`; a NaN stays
+__device__ __forceinline__ float top2(float top, F2 a) {
+    const float2 h = halves(a);
+    return max_nan(max_nan(top, fabsf(h.x)), fabsf(h.y));
 }
 
 // V groups of 8 columns per thread.  WARP: blockDim (32, rows per CTA), a warp per row.  Otherwise a CTA per row
 // and a ring of `stages` rows in shared memory, [stage][operand][group] with a thread's groups blockDim.x apart.
 template <typename X, typename R, typename Y, int V, bool WARP, bool NORM, int T>
-__global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cleave_rmsnorm_t d, uint32_t stages) {
+__global__ void __launch_bounds__(T, T == 128 ? 6 : (T == 256 ? 3 : 1)) row_wide_kernel(const __grid_constant__ cleave_rmsnorm_t d, uint32_t stages) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 parts[2][32];
     constexpr bool RES = !(sizeof(R) == 1), CODES = sizeof(Y) == 1;
@@ -146,47 +152,49 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
     R* ph = RES && d.h ? static_cast<R*>(d.h) + first * d.ldh + tid * 8 : nullptr;
     uint32_t it = 0, at = 0;
     for (uint64_t row = first; row < d.rows; row += stride, ++it) {
-        float h[V][8];
+        F2 h[V][4];
         if constexpr (!WARP) {
             if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
         }
-        Raw8<X> rx[V];
-        Raw8<typename std::conditional<RES, R, X>::type> rr[V];
+        Raw8<X> rx[WARP ? V : 1];
+        Raw8<typename std::conditional<RES, R, X>::type> rr[WARP ? V : 1];
+        if constexpr (WARP) {                                    // everything is asked for before anything is used
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            if (!live[v]) continue;
-            if constexpr (WARP) {
+            for (int v = 0; v < V; ++v) {
+                if (!live[v]) continue;
                 rx[v] = load_raw8(reinterpret_cast<const X*>(px + v * nt * BX));
                 if constexpr (RES) rr[v] = load_raw8(reinterpret_cast<const R*>(pr + v * nt * BR));
-            } else {
-                rx[v] = *reinterpret_cast<const Raw8<X>*>(slot + at + v * nt * BX);
-                if constexpr (RES) rr[v] = *reinterpret_cast<const Raw8<R>*>(ring + off_r + at + (tid + v * nt) * BR);
             }
         }
         // one reduction for both statistics: the sum of squares and, for codes, the largest |h w| (times rstd later)
-        float ss = 0.f, top = 0.f;
+        F2 squares = f2(0.f, 0.f);
+        float top = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
-            unpack8(rx[v], h[v]);
+            if constexpr (WARP) unpack8(rx[v], h[v]);
+            else unpack8(*reinterpret_cast<const Raw8<X>*>(slot + at + v * nt * BX), h[v]);
             if constexpr (RES) {
-                float r[8];
-                unpack8(rr[v], r);
+                F2 r[4];
+                if constexpr (WARP) unpack8(rr[v], r);
+                else unpack8(*reinterpret_cast<const Raw8<R>*>(ring + off_r + at + (tid + v * nt) * BR), r);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] += r[i];
+                for (int i = 0; i < 4; ++i) h[v][i] = add2(h[v][i], r[i]);
                 if constexpr (NORM) if (ph) store8(ph + v * nt * 8, h[v]);
             }
             if constexpr (NORM) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) ss = fmaf(h[v][i], h[v][i], ss);
+                for (int i = 0; i < 4; ++i) squares = fma2(h[v][i], h[v][i], squares);
             }
             if constexpr (CODES) {
-                float w[8];
+                F2 w[4];
                 load_weight8(d, (tid + v * nt) * 8, w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) top = max_nan(top, fabsf(h[v][i] * w[i]));
+                for (int i = 0; i < 4; ++i) top = top2(top, mul2(h[v][i], w[i]));
             }
         }
+        const float2 sq = halves(squares);
+        float ss = sq.x + sq.y;
         if constexpr (NORM) ss = warp_sum(ss);
         if constexpr (CODES) top = warp_abs_max(top);
         if constexpr (!WARP) {
@@ -211,10 +219,10 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
                     if (!live[v]) continue;
-                    float w[8];
+                    F2 w[4];
                     load_weight8(d, (tid + v * nt) * 8, w);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) t = max_nan(t, fabsf(h[v][i] * rstd * w[i]));
+                    for (int i = 0; i < 4; ++i) t = top2(t, mul2(mul2(h[v][i], f2(rstd, rstd)), w[i]));
                 }
                 t = warp_abs_max(t);
                 if constexpr (!WARP) {
@@ -233,12 +241,12 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
-            float w[8], y[8];
+            F2 w[4], y[4];
             load_weight8(d, (tid + v * nt) * 8, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                y[i] = h[v][i] * rstd * w[i];
-                if constexpr (CODES) y[i] *= inv;
+            for (int i = 0; i < 4; ++i) {
+                y[i] = mul2(mul2(h[v][i], f2(rstd, rstd)), w[i]);
+                if constexpr (CODES) y[i] = mul2(y[i], f2(inv, inv));
             }
             store8(py + v * nt * 8, y);
         }
@@ -248,7 +256,7 @@ __global__ void __launch_bounds__(T) row_wide_kernel(const __grid_constant__ cle
 }
 
 constexpr uint32_t kWarpRowCols = 1024;         // up to here a warp holds a row (four groups a lane)
-constexpr uint32_t kRingBytes = 48 * 1024;      // per CTA; four CTAs an SM at most sizes
+constexpr uint32_t kRingBytes = 36 * 1024;      // per CTA; five or six CTAs an SM at most sizes
 constexpr uint32_t kRingMost = 160 * 1024;
 
 template <typename X, typename R, typename Y, int V, bool WARP, bool NORM, int T>
@@ -265,7 +273,7 @@ cudaError_t launch_row_wide(const cleave_rmsnorm_t& d, uint32_t threads, int sms
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
     // CTAs that fit an SM by shared memory and threads; each walks the rows in steps of the grid
-    const uint32_t fit = max(1u, min(min(224u * 1024u / (smem + 2048u), 65536u / (threads * 112u)), 5u));
+    const uint32_t fit = max(1u, min(min(224u * 1024u / (smem + 2048u), 65536u / (threads * 80u)), 6u));
     const uint64_t ctas = min((uint64_t)d.rows, (uint64_t)sms * fit);
     kernel<<<(unsigned)ctas, threads, smem, st>>>(d, stages);
     return cudaGetLastError();
@@ -382,18 +390,18 @@ __global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __
         cp_async_commit();
     };
     for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
-    float dw[V][8];
+    F2 dw[V][4];
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dw[v][i] = 0.f;
+        for (int i = 0; i < 4; ++i) dw[v][i] = f2(0.f, 0.f);
     H* pdx = static_cast<H*>(d.dx) + blockIdx.x * d.lddx + tid * 8;
     uint32_t it = 0, at = 0;
     for (uint64_t row = blockIdx.x; row < d.rows; row += gridDim.x, ++it) {
         if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
         const float rstd = __ldg(d.rstd + row);
         const uint8_t* stage = ring + at;
-        float q[V][8], dot = 0.f;                                // q = w dy; dot = sum q h
+        F2 q[V][4], dots = f2(0.f, 0.f);                         // q = w dy; dots: sum q h
         Raw8<H> rh[V], rr[V];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -402,16 +410,18 @@ __global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __
             unpack8(*reinterpret_cast<const Raw8<D>*>(stage + g * BD), q[v]);
             rh[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_h + g * BH);
             if (res) rr[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_res + g * BH);
-            float h[8], w[8];
+            F2 h[4], w[4];
             unpack8(rh[v], h);
             load_weight8(d, g * 8, w);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                dw[v][i] = fmaf(q[v][i] * rstd, h[i], dw[v][i]);
-                q[v][i] *= w[i];
-                dot = fmaf(q[v][i], h[i], dot);
+            for (int i = 0; i < 4; ++i) {
+                dw[v][i] = fma2(mul2(q[v][i], f2(rstd, rstd)), h[i], dw[v][i]);
+                q[v][i] = mul2(q[v][i], w[i]);
+                dots = fma2(q[v][i], h[i], dots);
             }
         }
+        const float2 dd = halves(dots);
+        float dot = dd.x + dd.y;
         dot = warp_sum(dot);
         float* p = parts[it & 1];
         if ((tid & 31u) == 0) p[tid >> 5] = dot;
@@ -423,14 +433,14 @@ __global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
-            float dx[8], h[8];
+            F2 dx[4], h[4];
             unpack8(rh[v], h);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) dx[i] = rstd * q[v][i] - along * h[i];
+            for (int i = 0; i < 4; ++i) dx[i] = fma2(f2(-along, -along), h[i], mul2(f2(rstd, rstd), q[v][i]));
             if (res) {
                 unpack8(rr[v], h);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) dx[i] += h[i];
+                for (int i = 0; i < 4; ++i) dx[i] = add2(dx[i], h[i]);
             }
             store8(pdx + v * nt * 8, dx);
         }

@@ -38,12 +38,17 @@ int cuda_code(cudaError_t e) {
     cudaGetLastError();
     return CLEAVE_E_CUDA;
 }
-// SM count of the current device, or a negative CLEAVE_E_* code
+// SM count of the current device, or a negative CLEAVE_E_* code (asked for once per device)
 int need_device() {
+    static std::atomic<int> known[64];
     int dev = 0, n = 0, major = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+    if (cudaGetDevice(&dev) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+    if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) != 0) return n;
+    if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
         cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
-    return major == 10 ? n : CLEAVE_E_UNSUPPORTED;
+    if (major != 10) n = CLEAVE_E_UNSUPPORTED;
+    if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+    return n;
 }
 
 bool adam_wide(const AdamTensor& t, uint32_t state_type, uint32_t g_type) {

@@ -112,6 +112,41 @@ inline bool rows_wide(const void* p, uint64_t ld, uint32_t type) {
     return (uintptr_t)p % unit == 0 && (ld * type_bytes(type)) % unit == 0;
 }
 
+// ---- two fp32 values in one register pair: each instruction below rounds both halves by itself ---------------------
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 halves(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+    return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c)); return r; }
+__device__ __forceinline__ void unpack8(const Raw8<float>& r, F2 (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        x[2 * i] = f2(__uint_as_float(r.w[i].x), __uint_as_float(r.w[i].y));
+        x[2 * i + 1] = f2(__uint_as_float(r.w[i].z), __uint_as_float(r.w[i].w));
+    }
+}
+__device__ __forceinline__ void unpack8(const Raw8<__nv_bfloat16>& r, F2 (&x)[4]) {
+    const uint32_t w[4] = {r.w[0].x, r.w[0].y, r.w[0].z, r.w[0].w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = f2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const F2 (&x)[4]) {
+    float y[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) { const float2 h = halves(x[i]); y[2 * i] = h.x; y[2 * i + 1] = h.y; }
+    store8(p, y);
+}
+
 // ---- asynchronous copies into shared memory, and warp reductions ----------------------------------------
 // A thread copies only what it reads itself, so a ring of such copies needs no barrier: the thread's own group count
 // says when a stage has landed.

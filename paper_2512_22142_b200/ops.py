@@ -8,6 +8,7 @@ were made on another stream are the caller's to order, as with any launch.
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 import torch
 
@@ -17,6 +18,9 @@ _vp, _u32, _u64, _i, _f, _d = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int, C.c_f
 
 T_NONE, T_BF16, T_F32, T_E4M3 = 0, 1, 2, 3
 _TYPE = {torch.bfloat16: T_BF16, torch.float32: T_F32, torch.float8_e4m3fn: T_E4M3}
+_FLOATS = {torch.bfloat16: T_BF16, torch.float32: T_F32}
+_F32 = {torch.float32: T_F32}
+_CODES = {torch.float8_e4m3fn: T_E4M3}
 ACT = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
@@ -79,9 +83,33 @@ for _name, (_res, _args) in _sig.items():
     _fn.restype, _fn.argtypes = _res, _args
 
 
+def _packer(cls):
+    """A function that lays positional values out as the record `cls` (bytes): what a call that lasts microseconds can
+    afford, where setting a ctypes record's fields one by one takes as long as the launch."""
+    codes = {_u64: "Q", _u32: "I", _vp: "Q", _f: "f", _d: "d", C.c_uint8: "B", C.c_uint16: "H"}
+    flat = [f for name, kind in cls._fields_ for f in (kind._fields_ if hasattr(kind, "_fields_") else [(name, kind)])]
+    layout = struct.Struct("@" + "".join(codes[kind] for _, kind in flat))
+    assert layout.size == C.sizeof(cls)
+    return layout.pack
+
+
+def _record_call(name):
+    """The entry point with its record as bytes."""
+    fn = lib[name]
+    fn.restype, fn.argtypes = _i, [C.c_char_p] + _sig[name][1][1:]
+    return fn
+
+
+_pack_rmsnorm, _pack_rmsnorm_backward, _pack_linear, _pack_act_backward = (
+    _packer(c) for c in (_Rmsnorm, _RmsnormBackward, _Linear, _ActBackward))
+_call_rmsnorm, _call_rmsnorm_backward, _call_linear, _call_act_backward = (
+    _record_call("cleave_" + n) for n in ("rmsnorm", "rmsnorm_backward", "linear", "act_backward"))
+_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+
+
 def _raw_stream(stream) -> int:
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+        return _current_stream(_current_device())
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 
@@ -89,39 +117,37 @@ def _bad(what: str):
     raise ValueError(what)
 
 
-def _matrix(t, name: str, rows: int, cols: int, types) -> tuple:
-    """(type, address, leading dimension) of a row-major [rows, cols] tensor; (0, None, 0) for None."""
-    if t is None:
-        return 0, None, 0
-    kind = _TYPE.get(t.dtype, 0)
-    if kind not in types or not t.is_cuda:
+_ABSENT = (0, 0, 0)
+
+
+def _matrix(t, name: str, shape, types) -> tuple:
+    """(type, address, leading dimension) of a row-major tensor of that shape."""
+    kind = types.get(t.dtype)
+    if kind is None or not t.is_cuda:
         _bad(f"{name}: a GPU tensor of a supported type is wanted, got {t.dtype} on {t.device}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
-        _bad(f"{name}: shape ({rows}, {cols}) is wanted, got {tuple(t.shape)}")
+    if t.shape != shape:
+        _bad(f"{name}: shape {tuple(shape)} is wanted, got {tuple(t.shape)}")
     ld, inner = t.stride()
+    cols = shape[1]
     if inner != 1 and cols > 1:
         _bad(f"{name}: rows have to be contiguous")
-    if rows <= 1 or ld < cols:
-        if rows > 1:
+    if ld < cols or shape[0] == 1:
+        if shape[0] > 1:
             _bad(f"{name}: rows overlap")
-        ld = max(ld, cols)         # a single row: any stride
+        ld = cols                  # a single row: any stride
     return kind, t.data_ptr(), ld
 
 
 def _vector(t, name: str, n: int, types) -> tuple:
-    """(type, address) of a contiguous [n] tensor; (0, None) for None."""
+    """(type, address) of a contiguous [n] tensor; (0, 0) for None."""
     if t is None:
-        return 0, None
-    kind = _TYPE.get(t.dtype, 0)
-    if kind not in types or not t.is_cuda:
+        return 0, 0
+    kind = types.get(t.dtype)
+    if kind is None or not t.is_cuda:
         _bad(f"{name}: a GPU tensor of a supported type is wanted, got {t.dtype} on {t.device}")
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
         _bad(f"{name}: a contiguous tensor of {n} elements is wanted, got {tuple(t.shape)}")
     return kind, t.data_ptr()
-
-
-_FLOATS = (T_BF16, T_F32)
-_F32 = (T_F32,)
 
 
 def _workspace(given, nbytes: int, like, raw: int, stream):
@@ -153,7 +179,7 @@ class AdamW:
         if n == 0 or len(grads) != n or len(m) != n or len(v) != n:
             _bad("params, grads, m and v: one of each per tensor is wanted")
         state, grad = _TYPE.get(m[0].dtype, 0), _TYPE.get(grads[0].dtype, 0)
-        if state not in (T_F32, T_E4M3) or grad not in _FLOATS:
+        if state not in (T_F32, T_E4M3) or grads[0].dtype not in _FLOATS:
             _bad("states are float32 or float8_e4m3fn, gradients float32 or bfloat16")
         if (state == T_E4M3) != (m_scales is not None) or (state == T_E4M3) != (v_scales is not None):
             _bad("m_scales and v_scales go with 8-bit states")
@@ -224,21 +250,22 @@ def rmsnorm(x, weight, y, *, residual=None, h=None, rstd=None, scale=None, eps: 
 
     x, residual (and h, of its type): bf16 or fp32 [rows, cols]; weight [cols] or None; y: bf16, fp32, or
     float8_e4m3fn with `scale` fp32 [rows]; rstd fp32 [rows] or None (what the backward pass needs)."""
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         _bad("x: two dimensions are wanted")
-    rows, cols = x.shape
-    d = _Rmsnorm()
-    d.rows, d.cols, d.eps = rows, cols, eps
-    d.x_type, d.x, d.ldx = _matrix(x, "x", rows, cols, _FLOATS)
-    d.r_type, d.r, d.ldr = _matrix(residual, "residual", rows, cols, _FLOATS)
-    kind, d.h, d.ldh = _matrix(h, "h", rows, cols, _FLOATS)
-    if h is not None and kind != d.r_type:
+    rows, cols = shape
+    xt, xp, ldx = _matrix(x, "x", shape, _FLOATS)
+    rt, rp, ldr = _ABSENT if residual is None else _matrix(residual, "residual", shape, _FLOATS)
+    ht, hp, ldh = _ABSENT if h is None else _matrix(h, "h", shape, _FLOATS)
+    if h is not None and ht != rt:
         _bad("h: the residual's type is wanted")
-    d.w_type, d.w = _vector(weight, "weight", cols, _FLOATS)
-    d.y_type, d.y, d.ldy = _matrix(y, "y", rows, cols, (T_BF16, T_F32, T_E4M3))
-    d.rstd = _vector(rstd, "rstd", rows, _F32)[1]
-    d.scale = _vector(scale, "scale", rows, _F32)[1]
-    _check(lib.cleave_rmsnorm(C.byref(d), _raw_stream(stream)), "cleave_rmsnorm")
+    wt, wp = _vector(weight, "weight", cols, _FLOATS)
+    yt, yp, ldy = _matrix(y, "y", shape, _TYPE)
+    record = _pack_rmsnorm(rows, cols, xt, rt, wt, yt, eps, xp, ldx, rp, ldr, hp, ldh, wp, yp, ldy, _vector(rstd, "rstd", rows, _F32)[1],
+                           _vector(scale, "scale", rows, _F32)[1])
+    code = _call_rmsnorm(record, _raw_stream(stream))
+    if code:
+        _check(code, "cleave_rmsnorm")
 
 
 def rmsnorm_backward_workspace(rows: int, cols: int) -> int:
@@ -248,35 +275,39 @@ def rmsnorm_backward_workspace(rows: int, cols: int) -> int:
 def rmsnorm_backward(dy, h, weight, rstd, dx, dweight=None, *, dres=None, workspace=None, stream=None) -> None:
     """cleave_rmsnorm_backward: dx (the gradient of x and of the residual alike) and dweight (fp32, or None) from the
     saved h and rstd; `dres`, of h's type, is the gradient that reaches h from the residual stream."""
-    if h.dim() != 2:
+    shape = h.shape
+    if len(shape) != 2:
         _bad("h: two dimensions are wanted")
-    rows, cols = h.shape
-    d = _RmsnormBackward()
-    d.rows, d.cols = rows, cols
-    d.dy_type, d.dy, d.lddy = _matrix(dy, "dy", rows, cols, _FLOATS)
-    d.h_type, d.h, d.ldh = _matrix(h, "h", rows, cols, _FLOATS)
-    d.w_type, d.w = _vector(weight, "weight", cols, _FLOATS)
-    d.rstd = _vector(rstd, "rstd", rows, _F32)[1]
-    own = (d.h_type,)
-    _, d.dres, d.lddres = _matrix(dres, "dres", rows, cols, own)
-    _, d.dx, d.lddx = _matrix(dx, "dx", rows, cols, own)
-    d.dw = _vector(dweight, "dweight", cols, _F32)[1]
+    rows, cols = shape
+    dyt, dyp, lddy = _matrix(dy, "dy", shape, _FLOATS)
+    ht, hp, ldh = _matrix(h, "h", shape, _FLOATS)
+    wt, wp = _vector(weight, "weight", cols, _FLOATS)
+    own = {h.dtype: ht}
+    _, rp, ldr = _ABSENT if dres is None else _matrix(dres, "dres", shape, own)
+    _, dxp, lddx = _matrix(dx, "dx", shape, own)
+    record = _pack_rmsnorm_backward(rows, cols, dyt, ht, wt, 0, dyp, lddy, hp, ldh, wp, _vector(rstd, "rstd", rows, _F32)[1], rp, ldr, dxp, lddx,
+                                    _vector(dweight, "dweight", cols, _F32)[1])
     raw = _raw_stream(stream)
-    ws = None
-    if dweight is not None:
-        ws = _workspace(workspace, lib.cleave_rmsnorm_backward_workspace(rows, cols), h, raw, stream)
-    _check(lib.cleave_rmsnorm_backward(C.byref(d), ws.data_ptr() if ws is not None else None, raw), "cleave_rmsnorm_backward")
+    ws = None if dweight is None else _workspace(workspace, lib.cleave_rmsnorm_backward_workspace(rows, cols), h, raw, stream)
+    code = _call_rmsnorm_backward(record, None if ws is None else ws.data_ptr(), raw)
+    if code:
+        _check(code, "cleave_rmsnorm_backward")
 
 
 def quantize_rows(x, y, scale, *, stream=None) -> None:
     """cleave_quantize_rows: y (float8_e4m3fn) = x / scale, scale fp32 [rows] = largest magnitude of the row / 448."""
-    if x.dim() != 2:
+    shape = x.shape
+    if len(shape) != 2:
         _bad("x: two dimensions are wanted")
-    rows, cols = x.shape
-    kind, px, ldx = _matrix(x, "x", rows, cols, _FLOATS)
-    _, py, ldy = _matrix(y, "y", rows, cols, (T_E4M3,))
-    ps = _vector(scale, "scale", rows, _F32)[1]
-    _check(lib.cleave_quantize_rows(px, kind, rows, cols, ldx, py, ldy, ps, _raw_stream(stream)), "cleave_quantize_rows")
+    if scale is None:
+        _bad("scale: a tensor is wanted")
+    kind, px, ldx = _matrix(x, "x", shape, _FLOATS)
+    _, py, ldy = _matrix(y, "y", shape, _CODES)
+    ps = _vector(scale, "scale", shape[0], _F32)[1]
+    _check(lib.cleave_quantize_rows(px, kind, shape[0], shape[1], ldx, py, ldy, ps, _raw_stream(stream)), "cleave_quantize_rows")
+
+
+_IN = {torch.bfloat16: T_BF16, torch.float8_e4m3fn: T_E4M3}
 
 
 def linear(A, B, out, *, transA: bool = False, transB: bool = False, scale_a=None, scale_b=None, bias=None, act: str = "none", z=None,
@@ -286,32 +317,34 @@ def linear(A, B, out, *, transA: bool = False, transB: bool = False, scale_a=Non
     A: [M, K] ([K, M] with transA), B: [K, N] ([N, K] with transB), both bf16, or both float8_e4m3fn with
     transB.  scale_a [M], scale_b [N] fp32.  bias [N], z, mul, residual [M, N], out [M, N]: bf16 or fp32.
     `residual` may be `out` itself (an accumulation)."""
-    if A.dim() != 2 or B.dim() != 2:
+    shape_a, shape_b = A.shape, B.shape
+    if len(shape_a) != 2 or len(shape_b) != 2:
         _bad("A, B: two dimensions are wanted")
-    K, M = A.shape if transA else reversed(A.shape)
-    N = B.shape[0 if transB else 1]
-    d = _Linear()
-    kind, d.A, lda = _matrix(A, "A", A.shape[0], A.shape[1], (T_BF16, T_E4M3))
-    kind_b, d.B, ldb = _matrix(B, "B", *((N, K) if transB else (K, N)), (kind,))
+    K, M = shape_a if transA else (shape_a[1], shape_a[0])
+    N = shape_b[0 if transB else 1]
+    if shape_b[1 if transB else 0] != K:
+        _bad(f"B: {K} products are wanted, got shape {tuple(shape_b)}")
+    kind, ap, lda = _matrix(A, "A", shape_a, _IN)
+    _, bp, ldb = _matrix(B, "B", shape_b, {A.dtype: kind})
     unit = 16 if kind == T_E4M3 else 8
-    if A.shape[0] == 1:
-        lda = -(-A.shape[1] // unit) * unit                 # a single row has no second one
-    if B.shape[0] == 1:
-        ldb = -(-B.shape[1] // unit) * unit
-    g = d.g
-    g.M, g.N, g.K, g.lda, g.ldb, g.transA, g.transB = M, N, K, lda, ldb, transA, transB
-    d.in_type = kind
-    d.scale_a = _vector(scale_a, "scale_a", M, _F32)[1]
-    d.scale_b = _vector(scale_b, "scale_b", N, _F32)[1]
-    d.bias_type, d.bias = _vector(bias, "bias", N, _FLOATS)
-    d.z_type, d.z, d.ldz = _matrix(z, "z", M, N, _FLOATS)
-    d.mul_type, d.mul, d.ldmul = _matrix(mul, "mul", M, N, _FLOATS)
-    d.res_type, d.res, d.ldres = _matrix(residual, "residual", M, N, _FLOATS)
-    d.c_type, d.C, d.ldc = _matrix(out, "out", M, N, _FLOATS)
-    if act not in ACT:
+    if shape_a[0] == 1:
+        lda = -(-shape_a[1] // unit) * unit                 # a single row has no second one
+    if shape_b[0] == 1:
+        ldb = -(-shape_b[1] // unit) * unit
+    code = ACT.get(act)
+    if code is None:
         _bad(f"act: one of {', '.join(ACT)} is wanted")
-    d.act = ACT[act]
-    _check(lib.cleave_linear(C.byref(d), _raw_stream(stream)), "cleave_linear")
+    shape = (M, N)
+    ct, cp, ldc = _matrix(out, "out", shape, _FLOATS)
+    bt, biasp = _vector(bias, "bias", N, _FLOATS)
+    zt, zp, ldz = _ABSENT if z is None else _matrix(z, "z", shape, _FLOATS)
+    mt, mp, ldm = _ABSENT if mul is None else _matrix(mul, "mul", shape, _FLOATS)
+    rt, rp, ldr = _ABSENT if residual is None else _matrix(residual, "residual", shape, _FLOATS)
+    record = _pack_linear(M, N, K, lda, ldb, transA, transB, 0, kind, ct, bt, zt, mt, rt, code, 0, ap, bp,
+                          _vector(scale_a, "scale_a", M, _F32)[1], _vector(scale_b, "scale_b", N, _F32)[1], biasp, zp, ldz, mp, ldm, rp, ldr, cp, ldc)
+    code = _call_linear(record, _raw_stream(stream))
+    if code:
+        _check(code, "cleave_linear")
 
 
 def linear_status(stream=None) -> int:
@@ -325,22 +358,22 @@ def act_backward_workspace(rows: int, cols: int) -> int:
 
 def act_backward(dy, z, dz=None, *, act: str = "none", mul=None, dmul=None, dbias=None, workspace=None, stream=None) -> None:
     """cleave_act_backward: dz = dy mul act'(z), dmul = dy act(z), dbias (fp32) = column sums of dz before its rounding."""
-    if dy.dim() != 2:
+    shape = dy.shape
+    if len(shape) != 2:
         _bad("dy: two dimensions are wanted")
-    rows, cols = dy.shape
-    d = _ActBackward()
-    d.rows, d.cols = rows, cols
-    if act not in ACT:
+    rows, cols = shape
+    code = ACT.get(act)
+    if code is None:
         _bad(f"act: one of {', '.join(ACT)} is wanted")
-    d.act = ACT[act]
-    d.dy_type, d.dy, d.lddy = _matrix(dy, "dy", rows, cols, _FLOATS)
-    d.z_type, d.z, d.ldz = _matrix(z, "z", rows, cols, _FLOATS)
-    d.mul_type, d.mul, d.ldmul = _matrix(mul, "mul", rows, cols, _FLOATS)
-    d.dz_type, d.dz, d.lddz = _matrix(dz, "dz", rows, cols, _FLOATS)
-    d.dmul_type, d.dmul, d.lddmul = _matrix(dmul, "dmul", rows, cols, _FLOATS)
-    d.dbias = _vector(dbias, "dbias", cols, _F32)[1]
+    dyt, dyp, lddy = _matrix(dy, "dy", shape, _FLOATS)
+    zt, zp, ldz = _ABSENT if z is None else _matrix(z, "z", shape, _FLOATS)
+    mt, mp, ldm = _ABSENT if mul is None else _matrix(mul, "mul", shape, _FLOATS)
+    dzt, dzp, lddz = _ABSENT if dz is None else _matrix(dz, "dz", shape, _FLOATS)
+    dmt, dmp, lddm = _ABSENT if dmul is None else _matrix(dmul, "dmul", shape, _FLOATS)
+    record = _pack_act_backward(rows, cols, code, dyt, zt, mt, dzt, dmt, 0, dyp, lddy, zp, ldz, mp, ldm, dzp, lddz, dmp, lddm,
+                                _vector(dbias, "dbias", cols, _F32)[1])
     raw = _raw_stream(stream)
-    ws = None
-    if dbias is not None:
-        ws = _workspace(workspace, lib.cleave_act_backward_workspace(rows, cols), dy, raw, stream)
-    _check(lib.cleave_act_backward(C.byref(d), ws.data_ptr() if ws is not None else None, raw), "cleave_act_backward")
+    ws = None if dbias is None else _workspace(workspace, lib.cleave_act_backward_workspace(rows, cols), dy, raw, stream)
+    code = _call_act_backward(record, None if ws is None else ws.data_ptr(), raw)
+    if code:
+        _check(code, "cleave_act_backward")
