@@ -7,8 +7,9 @@
 //          into a ring in shared memory -- each thread copies and reads its own groups only, so the ring needs no
 //          barrier of its own and the bytes in flight do not depend on registers -- and one barrier a row joins
 //          the warps' sums.
-//   any    every other size, stride or alignment: neighbouring threads own neighbouring columns and take them
-//          again in each pass (the row stays in L1 / L2).
+//   own    any alignment, up to 8192 columns: neighbouring threads own neighbouring columns, held in registers.
+//   any    what is left: the row is taken again in each pass (it stays in L1 / L2).
+#include <algorithm>
 #include <type_traits>
 
 #include "ops.cuh"
@@ -79,6 +80,158 @@ __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_const
     }
 }
 
+// ---- any alignment, up to 8192 columns ------------------------------------------------------------------
+// A thread owns the columns tid, tid + T, ...: kOwn of them stay in registers, and the next row's are asked for before
+// this row's sums are joined.
+constexpr uint32_t kOwn = 8, kOwnCols = kOwn * 1024;
+
+// Raw words (a bf16's bits below), so that nothing waits for a load before all of them are on their way; columns that do
+// not exist repeat the last one and are cleared by own_values.
+__device__ __forceinline__ void load_own(const void* p, uint32_t type, uint64_t at, uint32_t cols, uint32_t (&x)[kOwn]) {
+    if (type == CLEAVE_T_F32) {
+        const uint32_t* s = static_cast<const uint32_t*>(p) + at;
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) x[k] = s[min(threadIdx.x + k * blockDim.x, cols - 1)];
+    } else {
+        const uint16_t* s = static_cast<const uint16_t*>(p) + at;
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) x[k] = s[min(threadIdx.x + k * blockDim.x, cols - 1)];
+    }
+}
+__device__ __forceinline__ void own_values(const uint32_t (&raw)[kOwn], uint32_t type, uint32_t cols, float (&x)[kOwn]) {
+    const uint32_t shift = type == CLEAVE_T_F32 ? 0u : 16u;
+#pragma unroll
+    for (uint32_t k = 0; k < kOwn; ++k) x[k] = threadIdx.x + k * blockDim.x < cols ? __uint_as_float(raw[k] << shift) : 0.f;
+}
+__device__ __forceinline__ void store_own(void* p, uint32_t type, uint64_t at, uint32_t cols, const float (&x)[kOwn]) {
+    if (type == CLEAVE_T_F32) {
+        float* s = static_cast<float*>(p) + at;
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) { const uint32_t j = threadIdx.x + k * blockDim.x; if (j < cols) s[j] = x[k]; }
+    } else if (type == CLEAVE_T_BF16) {
+        __nv_bfloat16* s = static_cast<__nv_bfloat16*>(p) + at;
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) { const uint32_t j = threadIdx.x + k * blockDim.x; if (j < cols) s[j] = __float2bfloat16_rn(x[k]); }
+    } else {
+        uint8_t* s = static_cast<uint8_t*>(p) + at;
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) { const uint32_t j = threadIdx.x + k * blockDim.x; if (j < cols) s[j] = e4m3_nearest(x[k]); }
+    }
+}
+// sum and NaN-keeping maximum over the CTA with one barrier; the buffers take turns
+__device__ __forceinline__ float2 cta_join(float sum, float top, float2* p) {
+    sum = warp_sum(sum);
+    top = warp_abs_max(top);
+    if (blockDim.x == 32) return make_float2(sum, top);
+    if ((threadIdx.x & 31u) == 0) p[threadIdx.x >> 5] = make_float2(sum, top);
+    __syncthreads();
+    const float2 q = (threadIdx.x & 31u) < blockDim.x / 32 ? p[threadIdx.x & 31u] : make_float2(0.f, 0.f);
+    return make_float2(warp_sum(q.x), warp_abs_max(q.y));
+}
+
+template <bool NORM, int T>
+__global__ void __launch_bounds__(T) row_own_kernel(const __grid_constant__ cleave_rmsnorm_t d) {
+    __shared__ float2 parts[3][32];
+    float w[kOwn];
+    uint32_t x[kOwn], r[kOwn];
+#pragma unroll
+    for (uint32_t k = 0; k < kOwn; ++k) { w[k] = 1.f; r[k] = 0u; }
+    if (d.w) { load_own(d.w, d.w_type, 0, d.cols, x); own_values(x, d.w_type, d.cols, w); }
+    const float inv_cols = 1.f / (float)d.cols;
+    uint64_t row = blockIdx.x;
+    load_own(d.x, d.x_type, row * d.ldx, d.cols, x);
+    if (d.r) load_own(d.r, d.r_type, row * d.ldr, d.cols, r);
+    const bool codes = d.y_type == CLEAVE_T_E4M3;
+    for (uint32_t it = 0; row < d.rows; row += gridDim.x, ++it) {
+        float h[kOwn], ss = 0.f, top = 0.f;
+        own_values(x, d.x_type, d.cols, h);
+        if (d.r) {
+            float t[kOwn];
+            own_values(r, d.r_type, d.cols, t);
+#pragma unroll
+            for (uint32_t k = 0; k < kOwn; ++k) h[k] += t[k];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) ss = fmaf(h[k], h[k], ss);
+        if (codes) {
+#pragma unroll
+            for (uint32_t k = 0; k < kOwn; ++k) top = max_nan(top, fabsf(h[k] * w[k]));
+        }
+        const uint64_t next = row + gridDim.x;
+        if (next < d.rows) {
+            load_own(d.x, d.x_type, next * d.ldx, d.cols, x);
+            if (d.r) load_own(d.r, d.r_type, next * d.ldr, d.cols, r);
+        }
+        if (NORM && d.h) store_own(d.h, d.r_type, row * d.ldh, d.cols, h);
+        const float2 both = cta_join(ss, top, parts[it & 1]);
+        float rstd = 1.f, inv = 1.f;
+        if (NORM) {
+            rstd = rsqrtf(fmaf(both.x, inv_cols, d.eps));
+            if (d.rstd && threadIdx.x == 0) d.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) h[k] = h[k] * rstd * w[k];
+        if (codes) {
+            float t = both.y * rstd;
+            if (both.y == INFINITY) {                            // h w overflowed: take h rstd w
+                float a = 0.f;
+#pragma unroll
+                for (uint32_t k = 0; k < kOwn; ++k) a = max_nan(a, fabsf(h[k]));
+                __syncthreads();
+                t = cta_join(0.f, a, parts[2]).y;
+            }
+            const float2 sc = row_scale(t);
+            inv = sc.y;
+            if (threadIdx.x == 0) d.scale[row] = sc.x;
+#pragma unroll
+            for (uint32_t k = 0; k < kOwn; ++k) h[k] *= inv;
+        }
+        store_own(d.y, d.y_type, row * d.ldy, d.cols, h);
+    }
+}
+
+template <int T>
+__global__ void __launch_bounds__(T) rmsnorm_backward_own_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws) {
+    __shared__ float2 parts[2][32];
+    float w[kOwn], dw[kOwn];
+    uint32_t ndy[kOwn], nh[kOwn], nres[kOwn];
+#pragma unroll
+    for (uint32_t k = 0; k < kOwn; ++k) { w[k] = 1.f; dw[k] = 0.f; }
+    if (d.w) { load_own(d.w, d.w_type, 0, d.cols, nh); own_values(nh, d.w_type, d.cols, w); }
+    const float inv_cols = 1.f / (float)d.cols;
+    uint64_t row = blockIdx.x;
+    load_own(d.dy, d.dy_type, row * d.lddy, d.cols, ndy);
+    load_own(d.h, d.h_type, row * d.ldh, d.cols, nh);
+    if (d.dres) load_own(d.dres, d.h_type, row * d.lddres, d.cols, nres);
+    for (uint32_t it = 0; row < d.rows; row += gridDim.x, ++it) {
+        const float rstd = __ldg(d.rstd + row);
+        float q[kOwn], g[kOwn], res[kOwn], dot = 0.f;
+        own_values(ndy, d.dy_type, d.cols, q);
+        own_values(nh, d.h_type, d.cols, g);
+        if (d.dres) own_values(nres, d.h_type, d.cols, res);
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) {
+            dw[k] = fmaf(q[k] * rstd, g[k], dw[k]);
+            q[k] *= w[k];
+            dot = fmaf(q[k], g[k], dot);
+        }
+        const uint64_t next = row + gridDim.x;
+        if (next < d.rows) {
+            load_own(d.dy, d.dy_type, next * d.lddy, d.cols, ndy);
+            load_own(d.h, d.h_type, next * d.ldh, d.cols, nh);
+            if (d.dres) load_own(d.dres, d.h_type, next * d.lddres, d.cols, nres);
+        }
+        const float along = rstd * rstd * (cta_join(dot, 0.f, parts[it & 1]).x * rstd * inv_cols);
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) { q[k] = rstd * q[k] - along * g[k]; if (d.dres) q[k] += res[k]; }
+        store_own(d.dx, d.h_type, row * d.lddx, d.cols, q);
+    }
+    if (d.dw)
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) { const uint32_t j = threadIdx.x + k * blockDim.x; if (j < d.cols) ws[(uint64_t)blockIdx.x * d.cols + j] = dw[k]; }
+}
+uint32_t own_threads(uint32_t cols) { return (cols + 32 * kOwn - 1) / (32 * kOwn) * 32; }
+
 // ---- forward, wide -----------------------------------------------------------------------------------
 struct NoRes {};                    // no residual operand
 template <typename T> struct Bytes8 { static constexpr uint32_t value = sizeof(T) * 8; };
@@ -109,7 +262,7 @@ __device__ __forceinline__ float top2(float top, F2 a) {
 // V groups of 8 columns per thread.  WARP: blockDim (32, rows per CTA), a warp per row.  Otherwise a CTA per row
 // and a ring of `stages` rows in shared memory, [stage][operand][group] with a thread's groups blockDim.x apart.
 template <typename X, typename R, typename Y, int V, bool WARP, bool NORM, int T>
-__global__ void __launch_bounds__(T, T == 128 ? 6 : (T == 256 ? 3 : 1)) row_wide_kernel(const __grid_constant__ cleave_rmsnorm_t d, uint32_t stages) {
+__global__ void __launch_bounds__(T, T == 128 ? 4 : (T == 256 ? 2 : 1)) row_wide_kernel(const __grid_constant__ cleave_rmsnorm_t d, uint32_t stages) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 parts[2][32];
     constexpr bool RES = !(sizeof(R) == 1), CODES = sizeof(Y) == 1;
@@ -148,6 +301,20 @@ __global__ void __launch_bounds__(T, T == 128 ? 6 : (T == 256 ? 3 : 1)) row_wide
     if constexpr (!WARP)
         for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
 
+    // a CTA takes many rows, so its weights stay in registers (from L1 they were two thirds of what the SM's load unit
+    // moved: 52 us -> 43 us at 8192 x 4096); a warp takes one row, and 1024 threads have no room
+    constexpr bool KEEP = !WARP && T <= 512;
+    F2 kept[KEEP ? V : 1][4];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) if (live[v]) load_weight8(d, (tid + v * nt) * 8, kept[v]);
+    }
+    auto weights = [&](int v, F2 (&w)[4]) {
+        if constexpr (KEEP) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) w[i] = kept[KEEP ? v : 0][i];
+        } else load_weight8(d, (tid + v * nt) * 8, w);
+    };
     Y* py = static_cast<Y*>(d.y) + first * d.ldy + tid * 8;
     R* ph = RES && d.h ? static_cast<R*>(d.h) + first * d.ldh + tid * 8 : nullptr;
     uint32_t it = 0, at = 0;
@@ -188,7 +355,7 @@ __global__ void __launch_bounds__(T, T == 128 ? 6 : (T == 256 ? 3 : 1)) row_wide
             }
             if constexpr (CODES) {
                 F2 w[4];
-                load_weight8(d, (tid + v * nt) * 8, w);
+                weights(v, w);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) top = top2(top, mul2(h[v][i], w[i]));
             }
@@ -220,7 +387,7 @@ __global__ void __launch_bounds__(T, T == 128 ? 6 : (T == 256 ? 3 : 1)) row_wide
                 for (int v = 0; v < V; ++v) {
                     if (!live[v]) continue;
                     F2 w[4];
-                    load_weight8(d, (tid + v * nt) * 8, w);
+                    weights(v, w);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) t = top2(t, mul2(mul2(h[v][i], f2(rstd, rstd)), w[i]));
                 }
@@ -242,7 +409,7 @@ __global__ void __launch_bounds__(T, T == 128 ? 6 : (T == 256 ? 3 : 1)) row_wide
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
             F2 w[4], y[4];
-            load_weight8(d, (tid + v * nt) * 8, w);
+            weights(v, w);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 y[i] = mul2(mul2(h[v][i], f2(rstd, rstd)), w[i]);
@@ -256,7 +423,7 @@ __global__ void __launch_bounds__(T, T == 128 ? 6 : (T == 256 ? 3 : 1)) row_wide
 }
 
 constexpr uint32_t kWarpRowCols = 1024;         // up to here a warp holds a row (four groups a lane)
-constexpr uint32_t kRingBytes = 36 * 1024;      // per CTA; five or six CTAs an SM at most sizes
+constexpr uint32_t kRingBytes = 50 * 1024;      // per CTA; four CTAs an SM at most sizes
 constexpr uint32_t kRingMost = 160 * 1024;
 
 template <typename X, typename R, typename Y, int V, bool WARP, bool NORM, int T>
@@ -273,7 +440,7 @@ cudaError_t launch_row_wide(const cleave_rmsnorm_t& d, uint32_t threads, int sms
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
     // CTAs that fit an SM by shared memory and threads; each walks the rows in steps of the grid
-    const uint32_t fit = max(1u, min(min(224u * 1024u / (smem + 2048u), 65536u / (threads * 80u)), 6u));
+    const uint32_t fit = max(1u, min(min(224u * 1024u / (smem + 2048u), 65536u / (threads * 128u)), 4u));
     const uint64_t ctas = min((uint64_t)d.rows, (uint64_t)sms * fit);
     kernel<<<(unsigned)ctas, threads, smem, st>>>(d, stages);
     return cudaGetLastError();
@@ -290,6 +457,7 @@ cudaError_t launch_row_types(const cleave_rmsnorm_t& d, int sms, cudaStream_t st
     const uint32_t threads = (groups + 127) / 128 * 32;
     if (groups <= 512) return launch_row_wide<X, R, Y, 4, false, NORM, 128>(d, threads, sms, st);
     if (groups <= 1024) return launch_row_wide<X, R, Y, 4, false, NORM, 256>(d, threads, sms, st);
+    if (groups <= 2048) return launch_row_wide<X, R, Y, 4, false, NORM, 512>(d, threads, sms, st);
     return launch_row_wide<X, R, Y, 4, false, NORM, 1024>(d, threads, sms, st);
 }
 template <typename X, typename R>
@@ -312,7 +480,12 @@ cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, int sms, cudaSt
     const bool wide = d.cols % 8 == 0 && d.cols <= 32768 && stage <= kRingMost && rows_wide(d.x, d.ldx, d.x_type) && rows_wide(d.y, d.ldy, d.y_type) &&
                       (!d.r || rows_wide(d.r, d.ldr, d.r_type)) && (!d.h || rows_wide(d.h, d.ldh, d.r_type)) && (!d.w || (uintptr_t)d.w % 16 == 0);
     if (wide) return d.x_type == CLEAVE_T_F32 ? launch_row_res<float>(d, norm, sms, st) : launch_row_res<__nv_bfloat16>(d, norm, sms, st);
-    if (norm) row_any_kernel<true><<<(unsigned)d.rows, kRowThreads, 0, st>>>(d);
+    if (d.cols <= kOwnCols) {
+        const uint32_t threads = own_threads(d.cols);
+        const unsigned ctas = (unsigned)std::min<uint64_t>(d.rows, (uint64_t)sms * std::min(24u, 1024u / threads));
+        if (threads <= 512) { if (norm) row_own_kernel<true, 512><<<ctas, threads, 0, st>>>(d); else row_own_kernel<false, 512><<<ctas, threads, 0, st>>>(d); }
+        else { if (norm) row_own_kernel<true, 1024><<<ctas, threads, 0, st>>>(d); else row_own_kernel<false, 1024><<<ctas, threads, 0, st>>>(d); }
+    } else if (norm) row_any_kernel<true><<<(unsigned)d.rows, kRowThreads, 0, st>>>(d);
     else      row_any_kernel<false><<<(unsigned)d.rows, kRowThreads, 0, st>>>(d);
     return cudaGetLastError();
 }
@@ -320,10 +493,13 @@ cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, int sms, cudaSt
 // ---- backward ----------------------------------------------------------------------------------------
 // A CTA takes the rows part, part + parts, ...; its share of dw goes to row `part` of the workspace (fp32
 // [parts x cols]; each element belongs to one thread), and sum_parts_kernel adds the parts in order.
-constexpr uint32_t kMaxParts = 2 * 148;
+// CTAs of the backward pass an SM: as many threads as registers allow
+uint32_t backward_ctas(uint32_t cols) {
+    const uint32_t threads = (cols / 8 + 63) / 64 * 32;          // of the wide form
+    return threads <= 256 ? std::min(16u, 768u / std::max(threads, 32u)) : (threads <= 320 ? 2u : 1u);
+}
 uint32_t rmsnorm_backward_parts(uint64_t rows, uint32_t cols) {
-    (void)cols;
-    return (uint32_t)(rows < kMaxParts ? rows : kMaxParts);
+    return (uint32_t)std::min<uint64_t>(rows, 148ull * backward_ctas(cols));
 }
 
 __global__ void __launch_bounds__(kRowThreads) rmsnorm_backward_any_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws) {
@@ -479,7 +655,7 @@ cudaError_t launch_backward_wide(const cleave_rmsnorm_backward_t& d, float* ws, 
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
-    const uint32_t stages = max(1u, min(4u, 100u * 1024u / stage));
+    const uint32_t stages = max(1u, min(4u, min(kRingMost, 216u * 1024u / backward_ctas(d.cols)) / stage));
     kernel<<<parts, threads, stage * stages, st>>>(d, ws, stages);
     return cudaGetLastError();
 }
@@ -487,7 +663,7 @@ template <typename D, typename H>
 cudaError_t launch_backward_types(const cleave_rmsnorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
     const uint32_t groups = d.cols / 8;
     const uint32_t threads = (groups + 63) / 64 * 32;
-    if (groups <= 512) return launch_backward_wide<D, H, 2, 256, 2>(d, ws, threads, parts, stage, st);
+    if (groups <= 512) return launch_backward_wide<D, H, 2, 256, 3>(d, ws, threads, parts, stage, st);
     if (groups <= 640) return launch_backward_wide<D, H, 2, 320, 2>(d, ws, threads, parts, stage, st);
     if (groups <= 1024) return launch_backward_wide<D, H, 2, 512, 1>(d, ws, threads, parts, stage, st);
     return launch_backward_wide<D, H, 2, 1024, 1>(d, ws, threads, parts, stage, st);
@@ -504,6 +680,11 @@ cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* w
     if (parts && wide) {
         if (d.dy_type == CLEAVE_T_F32) e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<float, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<float, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
         else e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<__nv_bfloat16, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<__nv_bfloat16, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
+    } else if (parts && d.cols <= kOwnCols) {
+        const uint32_t threads = own_threads(d.cols);
+        if (threads <= 512) rmsnorm_backward_own_kernel<512><<<parts, threads, 0, st>>>(d, ws);
+        else rmsnorm_backward_own_kernel<1024><<<parts, threads, 0, st>>>(d, ws);
+        e = cudaGetLastError();
     } else if (parts) {
         rmsnorm_backward_any_kernel<<<parts, kRowThreads, 0, st>>>(d, ws);
         e = cudaGetLastError();
