@@ -89,9 +89,17 @@ __device__ __forceinline__ float2 block_scale(float top) {
     return make_float2(s, s == 0.f ? 0.f : __frcp_rn(s));
 }
 
-// What an element's code needs besides its value: 16 random bits of `word` moved to where the 20 cut bits begin.
-__device__ __forceinline__ uint32_t bits_low(uint32_t w) { return (w << 4) & 0xFFFF0u; }
-__device__ __forceinline__ uint32_t bits_high(uint32_t w) { return (w >> 12) & 0xFFFF0u; }
+// three-input forms (one instruction)
+__device__ __forceinline__ float abs_max3(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float abs_min3(float a, float b, float c) {
+    float r;
+    asm("min.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 
 // The update of one block of 256 elements whose values the warp holds (lane: elements 4 lane .. + 3 of both halves),
 // and its stores.  WHOLE: the block is complete and its buffers are aligned.
@@ -118,8 +126,11 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, float decay, ui
             const float den = __fadd_rn(__fmul_rn(root, s.root), s.eps);
             p[j][i] = __fsub_rn(__fmul_rn(p[j][i], decay), __fmul_rn(__fdiv_rn(mo, den), s.step_size));
             m[j][i] = mo;
-            if constexpr (STATE8) { r[j][i] = root; top_m = max_nan(top_m, fabsf(mo)); top_r = max_nan(top_r, root); }
-            else r[j][i] = vo;
+            r[j][i] = STATE8 ? root : vo;
+        }
+        if constexpr (STATE8) {
+            top_m = abs_max3(abs_max3(top_m, m[j][0], m[j][1]), m[j][2], m[j][3]);
+            top_r = abs_max3(abs_max3(top_r, r[j][0], r[j][1]), r[j][2], r[j][3]);
         }
         const uint64_t e = e0 + j * 128u;
         store4(t.p, e, n, whole[j], p[j]);
@@ -141,7 +152,7 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, float decay, ui
             for (int i = 0; i < 4; ++i) {
                 qm[i] = __fmul_rn(m[j][i], bm.y);
                 qv[i] = __fmul_rn(r[j][i], bv.y);
-                least = fminf(fminf(least, fabsf(qm[i])), qv[i]);
+                least = abs_min3(least, qm[i], qv[i]);
             }
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
@@ -149,12 +160,16 @@ __device__ __forceinline__ void adamw_block(const AdamTensor& t, float decay, ui
                 w[2 * h] = (uint32_t)word; w[2 * h + 1] = (uint32_t)(word >> 32);
             }
             if (least >= 0.015625f && !odd) {
-                // every value has three mantissa bits left: the code is bits 20-26 of its magnitude plus the random
-                // bits, less 960 << 20 (exponent bias 127 - 7).  448 and a few units above it stay below the next code.
+                // Every value has three mantissa bits left: the code is bits 20-26 of its magnitude plus the random bits
+                // (moved to where the 20 cut bits begin), less 960 << 20 (exponent bias 127 - 7).  448 and a few units
+                // above it stay below the next code.  Written as products, sixteenfold, so that the code ends in the
+                // top byte: the integer multiply-add has a pipe of its own, shifts and masks share the busy one.
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    cm[i] = (((__float_as_uint(qm[i]) & 0x7FFFFFFFu) + bits_low(w[i]) - (960u << 20)) << 4 & 0x7F000000u) | (__float_as_uint(qm[i]) & 0x80000000u);
-                    cv[i] = (__float_as_uint(qv[i]) + bits_high(w[i]) - (960u << 20)) << 4;
+                    const uint32_t um = __byte_perm(w[i], 0, 0x4410), uv = __byte_perm(w[i], 0, 0x4432);
+                    const uint32_t am = (__float_as_uint(qm[i]) & 0x7FFFFFFFu) * 16u + (0u - (960u << 24)), av = __float_as_uint(qv[i]) * 16u + (0u - (960u << 24));
+                    cm[i] = ((um * 256u + am) & 0x7F000000u) | (__float_as_uint(qm[i]) & 0x80000000u);
+                    cv[i] = uv * 256u + av;
                 }
             } else {
 #pragma unroll

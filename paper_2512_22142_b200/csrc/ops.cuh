@@ -112,7 +112,8 @@ inline bool rows_wide(const void* p, uint64_t ld, uint32_t type) {
     return (uintptr_t)p % unit == 0 && (ld * type_bytes(type)) % unit == 0;
 }
 
-// ---- two fp32 values in one register pair: each instruction below rounds both halves by itself ---------------------
+// ---- two fp32 values in one register pair --------------------------------------------------------------------------
+// (A product and a sum of pairs may be contracted: not for what is defined to the bit.)
 typedef unsigned long long F2;
 __device__ __forceinline__ F2 f2(float lo, float hi) {
     F2 r;
@@ -238,6 +239,7 @@ struct AdamTensor {                 // device record of one tensor
 struct AdamStep {
     float beta1, omb1, beta2, omb2; // omb = 1 - beta, formed in 64 bits
     float step_size, root, eps, grad_scale;
+    uint32_t ordinary;              // root and eps are such that no quotient's divisor leaves the ordinary range
     double lr;
     uint64_t base;                  // seed + (step << 32)
 };
