@@ -46,10 +46,10 @@ __device__ __forceinline__ void act_cell(float dy, float z, float mul, float& dz
     if constexpr (MUL) dz = __fmul_rn(dz, mul);
     sum = __fadd_rn(sum, dz);
 }
-struct Band { uint64_t r0, r1; };
+struct Band { uint32_t r0, r1; };                     // (at most 2^31 - 1 rows)
 __device__ __forceinline__ Band this_band(uint64_t rows) {
-    const uint64_t band = (rows + gridDim.y - 1) / gridDim.y, r0 = blockIdx.y * band;
-    return Band{r0, r0 + band < rows ? r0 + band : rows};
+    const uint32_t n = (uint32_t)rows, band = (n + gridDim.y - 1) / gridDim.y, r0 = min(blockIdx.y * band, n);
+    return Band{r0, min(r0 + band, n)};
 }
 
 // Any size, stride and alignment: a lane's column, four rows asked for at a time.
@@ -62,7 +62,7 @@ __global__ void __launch_bounds__(32 * kActWarps) act_backward_any_kernel(const 
     const bool has_z = ACT != CLEAVE_ACT_NONE || d.z;
     float sum[1] = {0.f};
     if (j < d.cols)
-        for (uint64_t row = b.r0 + (threadIdx.x >> 5); row < b.r1; row += kActWarps * ROWS) {
+        for (uint32_t row = b.r0 + (threadIdx.x >> 5); row < b.r1; row += kActWarps * ROWS) {
             float dy[ROWS], z[ROWS], mul[ROWS];
 #pragma unroll
             for (int k = 0; k < ROWS; ++k) {
@@ -88,7 +88,7 @@ __global__ void __launch_bounds__(32 * kActWarps) act_backward_any_kernel(const 
 // Rows of whole 16-byte groups: a lane's 8 columns; STAGES rows of each operand on their way to shared memory.
 // D: type of dy; T: the one type of z, mul, dz and dmul.
 template <typename D, typename T, uint32_t ACT, bool MUL, int STAGES>
-__global__ void __launch_bounds__(32 * kActWarps) act_backward_wide_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
+__global__ void __launch_bounds__(32 * kActWarps, 3) act_backward_wide_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float s[kActWarps][32 * 8];
     constexpr uint32_t BD = sizeof(D) * 8, BT = sizeof(T) * 8, NT = MUL ? 2 : 1, STAGE = 32 * (BD + NT * BT);
@@ -100,46 +100,49 @@ __global__ void __launch_bounds__(32 * kActWarps) act_backward_wide_kernel(const
 #pragma unroll
     for (int i = 0; i < 8; ++i) sum[i] = 0.f;
     if (j < d.cols) {
-        const uint64_t first = b.r0 + warp;
-        const D* pd = static_cast<const D*>(d.dy) + first * d.lddy + j;
-        const T* pz = has_z ? static_cast<const T*>(d.z) + first * d.ldz + j : nullptr;
-        const T* pm = MUL ? static_cast<const T*>(d.mul) + first * d.ldmul + j : nullptr;
+        const uint32_t first = b.r0 + warp;
+        const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + first * d.lddy + j);
+        const uint8_t* pz = has_z ? reinterpret_cast<const uint8_t*>(static_cast<const T*>(d.z) + first * d.ldz + j) : nullptr;
+        const uint8_t* pm = MUL ? reinterpret_cast<const uint8_t*>(static_cast<const T*>(d.mul) + first * d.ldmul + j) : nullptr;
         T* odz = d.dz ? static_cast<T*>(d.dz) + first * d.lddz + j : nullptr;
         T* odm = d.dmul ? static_cast<T*>(d.dmul) + first * d.lddmul + j : nullptr;
         uint8_t* mine = ring + warp * (STAGES * STAGE);
         const uint32_t mine_at = (uint32_t)__cvta_generic_to_shared(mine);
-        uint64_t ahead = first;
+        uint32_t ahead = first;
         auto fetch = [&](uint32_t at) {
             if (ahead < b.r1) {
 #pragma unroll
-                for (uint32_t x = 0; x < BD; x += 16) cp_async<16>(mine_at + at + lane * BD + x, reinterpret_cast<const uint8_t*>(pd) + x);
+                for (uint32_t x = 0; x < BD; x += 16) cp_async<16>(mine_at + at + lane * BD + x, pd + x);
 #pragma unroll
                 for (uint32_t x = 0; x < BT; x += 16) {
-                    if (has_z) cp_async<16>(mine_at + at + 32 * BD + lane * BT + x, reinterpret_cast<const uint8_t*>(pz) + x);
-                    if constexpr (MUL) cp_async<16>(mine_at + at + 32 * (BD + BT) + lane * BT + x, reinterpret_cast<const uint8_t*>(pm) + x);
+                    if (has_z) cp_async<16>(mine_at + at + 32 * BD + lane * BT + x, pz + x);
+                    if constexpr (MUL) cp_async<16>(mine_at + at + 32 * (BD + BT) + lane * BT + x, pm + x);
                 }
                 ahead += kActWarps;
-                pd += kActWarps * d.lddy;
-                if (has_z) pz += kActWarps * d.ldz;
-                if constexpr (MUL) pm += kActWarps * d.ldmul;
+                pd += kActWarps * sizeof(D) * d.lddy;
+                if (has_z) pz += kActWarps * sizeof(T) * d.ldz;
+                if constexpr (MUL) pm += kActWarps * sizeof(T) * d.ldmul;
             }
             cp_async_commit();
         };
 #pragma unroll
         for (int k = 0; k < STAGES; ++k) fetch(k * STAGE);
-        uint32_t at = 0;
-        for (uint64_t row = first; row < b.r1; row += kActWarps) {
-            cp_async_wait<STAGES - 1>();
-            float dy[8], z[8], mul[8], dz[8], dm[8];
-            unpack8(*reinterpret_cast<const Raw8<D>*>(mine + at + lane * BD), dy);
-            if (has_z) unpack8(*reinterpret_cast<const Raw8<T>*>(mine + at + 32 * BD + lane * BT), z);
-            if constexpr (MUL) unpack8(*reinterpret_cast<const Raw8<T>*>(mine + at + 32 * (BD + BT) + lane * BT), mul);
+        for (uint32_t row = first; row < b.r1;) {
 #pragma unroll
-            for (int u = 0; u < 8; ++u) act_cell<ACT, MUL>(dy[u], has_z ? z[u] : 0.f, MUL ? mul[u] : 1.f, dz[u], dm[u], sum[u]);
-            fetch(at);                                           // the stage's values have been used
-            at = at + STAGE == STAGES * STAGE ? 0 : at + STAGE;
-            if (odm) { store8(odm, dm); odm += kActWarps * d.lddmul; }
-            if (odz) { store8(odz, dz); odz += kActWarps * d.lddz; }
+            for (int k = 0; k < STAGES; ++k, row += kActWarps) {      // once round the ring: stages at constant places
+                if (row >= b.r1) break;
+                const uint8_t* stage = mine + k * STAGE;
+                cp_async_wait<STAGES - 1>();
+                float dy[8], z[8], mul[8], dz[8], dm[8];
+                unpack8(*reinterpret_cast<const Raw8<D>*>(stage + lane * BD), dy);
+                if (has_z) unpack8(*reinterpret_cast<const Raw8<T>*>(stage + 32 * BD + lane * BT), z);
+                if constexpr (MUL) unpack8(*reinterpret_cast<const Raw8<T>*>(stage + 32 * (BD + BT) + lane * BT), mul);
+#pragma unroll
+                for (int u = 0; u < 8; ++u) act_cell<ACT, MUL>(dy[u], has_z ? z[u] : 0.f, MUL ? mul[u] : 1.f, dz[u], dm[u], sum[u]);
+                fetch(k * STAGE);                                    // the stage's values have been used
+                if (odm) { store8(odm, dm); odm += kActWarps * d.lddmul; }
+                if (odz) { store8(odz, dz); odz += kActWarps * d.lddz; }
+            }
         }
     }
     if (d.dbias) join_sums<8>(sum, s, ws, d.cols);
@@ -147,9 +150,9 @@ __global__ void __launch_bounds__(32 * kActWarps) act_backward_wide_kernel(const
 
 template <typename D, typename T, uint32_t ACT, bool MUL>
 cudaError_t launch_act_wide(const cleave_act_backward_t& d, float* ws, uint32_t parts, cudaStream_t st) {
-    // 64 to 72 KB a CTA: three CTAs an SM
+    // 32 to 60 KB a CTA: three or four CTAs an SM
     constexpr uint32_t stage = 32 * (sizeof(D) * 8 + (MUL ? 2 : 1) * sizeof(T) * 8);
-    constexpr int STAGES = 64 * 1024 / (kActWarps * stage) > 8 ? 8 : 64 * 1024 / (kActWarps * stage);
+    constexpr int STAGES = stage >= 2560 ? 3 : 4;
     auto kernel = act_backward_wide_kernel<D, T, ACT, MUL, STAGES>;
     constexpr uint32_t smem = kActWarps * STAGES * stage;
     static SmemLimit limit;
