@@ -56,6 +56,7 @@ __device__ __forceinline__ Band this_band(uint64_t rows) {
 template <uint32_t ACT, bool MUL>
 __global__ void __launch_bounds__(32 * kActWarps) act_backward_any_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
     __shared__ float s[kActWarps][32];
+    let_dependents_start();
     constexpr int ROWS = 4;
     const uint64_t j = (uint64_t)blockIdx.x * 32u + (threadIdx.x & 31u);
     const Band b = this_band(d.rows);
@@ -91,6 +92,7 @@ template <typename D, typename T, uint32_t ACT, bool MUL, int STAGES>
 __global__ void __launch_bounds__(32 * kActWarps, 3) act_backward_wide_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float s[kActWarps][32 * 8];
+    let_dependents_start();
     constexpr uint32_t BD = sizeof(D) * 8, BT = sizeof(T) * 8, NT = MUL ? 2 : 1, STAGE = 32 * (BD + NT * BT);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint64_t j = ((uint64_t)blockIdx.x * 32u + lane) * 8u;

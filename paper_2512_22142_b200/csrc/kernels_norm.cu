@@ -193,6 +193,7 @@ __global__ void __launch_bounds__(T) row_own_kernel(const __grid_constant__ clea
 template <int T>
 __global__ void __launch_bounds__(T) rmsnorm_backward_own_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws) {
     __shared__ float2 parts[2][32];
+    let_dependents_start();
     float w[kOwn], dw[kOwn];
     uint32_t ndy[kOwn], nh[kOwn], nres[kOwn];
 #pragma unroll
@@ -504,6 +505,7 @@ uint32_t rmsnorm_backward_parts(uint64_t rows, uint32_t cols) {
 
 __global__ void __launch_bounds__(kRowThreads) rmsnorm_backward_any_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws) {
     __shared__ float buf[32];
+    let_dependents_start();
     float* dw = ws + (uint64_t)blockIdx.x * d.cols;
     if (d.dw) for (uint32_t j = threadIdx.x; j < d.cols; j += blockDim.x) dw[j] = 0.f;
     for (uint64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
@@ -531,6 +533,7 @@ template <typename D, typename H, int V, int T, int CTAS>
 __global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float parts[2][32];
+    let_dependents_start();
     constexpr uint32_t BD = Bytes8<D>::value, BH = Bytes8<H>::value;
     const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
     const bool res = d.dres != nullptr;
@@ -634,6 +637,7 @@ __global__ void __launch_bounds__(1024) sum_parts_kernel(const float* __restrict
     __shared__ float s[32][33];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, j = blockIdx.x * 32u + lane;
     float v = 0.f;
+    wait_for_primary();
     if (j < cols) {
 #pragma unroll 8
         for (uint32_t p = warp; p < parts; p += 32) v += __ldcs(ws + (uint64_t)p * cols + j);
@@ -645,8 +649,16 @@ __global__ void __launch_bounds__(1024) sum_parts_kernel(const float* __restrict
     if (lane == 0 && blockIdx.x * 32u + warp < cols) out[blockIdx.x * 32u + warp] = v;
 }
 cudaError_t launch_sum_parts(const float* ws, uint32_t parts, uint32_t cols, float* out, cudaStream_t st) {
-    sum_parts_kernel<<<(cols + 31) / 32, 1024, 0, st>>>(ws, parts, cols, out);
-    return cudaGetLastError();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((cols + 31) / 32);
+    cfg.blockDim = dim3(1024);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, sum_parts_kernel, ws, parts, cols, out);
 }
 
 template <typename D, typename H, int V, int T, int CTAS>
