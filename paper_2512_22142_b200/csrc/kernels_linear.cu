@@ -36,7 +36,6 @@ struct Epilogue {
     uint32_t M, N;
     uint32_t c_type, bias_type, z_type, mul_type, res_type;
     uint32_t form;                  // 1, 2: C (bf16, fp32) and z (bf16) leave as bulk stores, mul and res allow 16-byte accesses; 0: any
-    uint32_t wide;                  // bit per operand: rows allow one access for four elements (kWide*)
     const float* scale_a;
     const float* scale_b;
     const void* bias;
@@ -46,7 +45,6 @@ struct Epilogue {
     void* C;
     uint64_t ldz, ldmul, ldres, ldc;
 };
-enum : uint32_t { kWideB = 1u, kWideBias = 2u, kWideZ = 4u, kWideMul = 8u, kWideRes = 16u, kWideC = 32u };
 
 struct LinearParams {
     Epilogue e;
@@ -55,65 +53,61 @@ struct LinearParams {
     unsigned long long wait_limit_ns;
 };
 
-// Four consecutive elements of a row; `n` of them exist, `wide`: the rows allow one access for four.
-__device__ __forceinline__ void load_row4(const void* p, uint32_t type, uint64_t at, uint32_t n, bool wide, float (&x)[4]) {
-    if (wide && n >= 4) {
-        if (type == CLEAVE_T_F32) {
-            const float4 v = *reinterpret_cast<const float4*>(static_cast<const float*>(p) + at);
-            x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w;
-        } else {
-            const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const __nv_bfloat16*>(p) + at);
-            x[0] = __uint_as_float(v.x << 16); x[1] = __uint_as_float(v.x & 0xFFFF0000u);
-            x[2] = __uint_as_float(v.y << 16); x[3] = __uint_as_float(v.y & 0xFFFF0000u);
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = (uint32_t)i < n ? load_as(p, type, at + i) : 0.f;
-    }
-}
-__device__ __forceinline__ void store_row4(void* p, uint32_t type, uint64_t at, uint32_t n, bool wide, const float (&x)[4]) {
-    if (wide && n >= 4) {
-        if (type == CLEAVE_T_F32) *reinterpret_cast<float4*>(static_cast<float*>(p) + at) = make_float4(x[0], x[1], x[2], x[3]);
-        else *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(p) + at) = make_uint2(pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]));
-    } else {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) if ((uint32_t)i < n) store_as(p, type, at + i, x[i]);
-    }
-}
-// A warp's staging tile: 32 rows of COLS fp32, written by a lane a row (what tensor memory gives) and read 4 columns a
-// lane, so that 8 (or 4) lanes cover a row of the chunk: 128 (64) bytes of fp32, 64 (32) of bf16 in one piece.  The
-// 16-byte groups of row r stand at group ^ r, so neither direction has bank conflicts.
-template <int COLS>
+// A warp's staging tile: 32 rows of 32 fp32, written by a lane a row (what tensor memory gives); the 16-byte groups of row r
+// stand at group ^ (r & 7), so that neither a row nor a column of lanes meets bank conflicts.
 __device__ __forceinline__ void stage_write(float* tile, uint32_t row, const float* v) {
-    float4* base = reinterpret_cast<float4*>(tile) + row * (COLS / 4);
+    float4* base = reinterpret_cast<float4*>(tile) + row * 8u;
 #pragma unroll
-    for (uint32_t j = 0; j < COLS / 4; ++j) base[j ^ (row & (COLS / 4 - 1))] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    for (uint32_t j = 0; j < 8; ++j) base[j ^ (row & 7u)] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
 }
 
-// The staged chunk (rows row0 ... + 31, columns col ... + COLS - 1 of the product) through the epilogue to C and z, any
-// types and edges.  Kept small and out of line: instructions that are fetched but seldom run cost the common form time.
-template <int COLS, uint32_t ACT>
-__device__ __noinline__ void write_chunk_any(const Epilogue& e, const float* tile, uint32_t row0, uint32_t col, uint32_t lane) {
-    constexpr uint32_t LANES = COLS / 4, STEP = 32 / LANES;          // lanes per row, rows per step
-    const uint32_t cc = lane % LANES, rr = lane / LANES;
-    col += cc * 4u;
-    if (col >= e.N) return;
-    const uint32_t n = e.N - col;
+// The staged chunk (rows row0 ... + 31, columns col ... + 31 of the product) through the epilogue to C and z, any types,
+// alignments and edges: a lane a column, so that a row's accesses are neighbours.
+template <uint32_t ACT>
+__device__ __forceinline__ void write_chunk_any(const Epilogue& e, const float* tile, uint32_t row0, uint32_t col, uint32_t lane) {
+    const uint64_t j = col + lane;
+    if (j >= e.N) return;
+    const float sb = e.scale_b ? __ldg(e.scale_b + j) : 1.f, bias = e.bias ? load_as(e.bias, e.bias_type, j) : 0.f;
+    const uint32_t rows = min(32u, e.M - row0);
+    constexpr uint32_t U = 8;                                            // rows asked for before the ones in hand are used
+    uint32_t mul[U], res[U];                                             // raw words: nothing waits for a load before all are on their way
+    auto column = [&](const void* p, uint32_t type, uint64_t ld, uint32_t r0, uint32_t (&x)[U]) {
+        if (type == CLEAVE_T_F32) {
+            const uint32_t* s = static_cast<const uint32_t*>(p) + j;
+#pragma unroll
+            for (uint32_t k = 0; k < U; ++k) x[k] = s[(row0 + min(r0 + k, rows - 1)) * ld];        // (rows beyond the last repeat it)
+        } else {
+            const uint16_t* s = static_cast<const uint16_t*>(p) + j;
+#pragma unroll
+            for (uint32_t k = 0; k < U; ++k) x[k] = (uint32_t)s[(row0 + min(r0 + k, rows - 1)) * ld];
+        }
+    };
+    const uint32_t mul_shift = e.mul_type == CLEAVE_T_F32 ? 0u : 16u, res_shift = e.res_type == CLEAVE_T_F32 ? 0u : 16u;
+    if (e.mul) column(e.mul, e.mul_type, e.ldmul, 0, mul);
+    if (e.res) column(e.res, e.res_type, e.ldres, 0, res);
 #pragma unroll 1
-    for (uint32_t r = rr; r < 32 && row0 + r < e.M; r += STEP) {
-        const uint32_t row = row0 + r;
-        const float4 f = reinterpret_cast<const float4*>(tile)[r * LANES + (cc ^ (r & (LANES - 1)))];
-        float x[4] = {f.x, f.y, f.z, f.w}, t[4];
-        if (e.scale_a) { const float sa = e.scale_a[row]; for (int i = 0; i < 4; ++i) x[i] *= sa; }
-        if (e.scale_b) { load_row4(e.scale_b, CLEAVE_T_F32, col, n, e.wide & kWideB, t); for (int i = 0; i < 4; ++i) x[i] *= t[i]; }
-        if (e.bias) { load_row4(e.bias, e.bias_type, col, n, e.wide & kWideBias, t); for (int i = 0; i < 4; ++i) x[i] += t[i]; }
-        if (e.z) store_row4(e.z, e.z_type, row * e.ldz + col, n, e.wide & kWideZ, x);
-        for (int i = 0; i < 4; ++i) x[i] = act_value(x[i], ACT);
-        if (e.mul) { load_row4(e.mul, e.mul_type, row * e.ldmul + col, n, e.wide & kWideMul, t); for (int i = 0; i < 4; ++i) x[i] *= t[i]; }
-        if (e.res) { load_row4(e.res, e.res_type, row * e.ldres + col, n, e.wide & kWideRes, t); for (int i = 0; i < 4; ++i) x[i] += t[i]; }
-        store_row4(e.C, e.c_type, row * e.ldc + col, n, e.wide & kWideC, x);
+    for (uint32_t r0 = 0; r0 < rows; r0 += U) {
+        float m[U], a[U];
+#pragma unroll
+        for (uint32_t k = 0; k < U; ++k) {
+            m[k] = e.mul ? __uint_as_float(mul[k] << mul_shift) : 1.f;
+            a[k] = e.res ? __uint_as_float(res[k] << res_shift) : 0.f;
+        }
+        if (e.mul) column(e.mul, e.mul_type, e.ldmul, r0 + U, mul);
+        if (e.res) column(e.res, e.res_type, e.ldres, r0 + U, res);
+#pragma unroll
+        for (uint32_t k = 0; k < U; ++k) {
+            const uint32_t r = r0 + k;
+            if (r >= rows) break;
+            const uint64_t row = row0 + r;
+            const float x = tile[r * 32u + ((((lane >> 2) ^ (r & 7u)) << 2) | (lane & 3u))];
+            const float z = x * (e.scale_a ? __ldg(e.scale_a + row) : 1.f) * sb + bias;
+            if (e.z) store_as(e.z, e.z_type, row * e.ldz + j, z);
+            store_as(e.C, e.c_type, row * e.ldc + j, fmaf(act_value(z, ACT), m[k], a[k]));
+        }
     }
 }
+
 // 32 consecutive elements of a row added to / multiplied into x; the row allows 16-byte accesses and holds them all.
 template <bool MUL>
 __device__ __forceinline__ void join_row32(const void* p, uint32_t type, uint64_t at, float (&x)[32]) {
@@ -142,7 +136,7 @@ __device__ __forceinline__ void join_row32(const void* p, uint32_t type, uint64_
 // rows of 64 bytes with the 64-byte swizzle.
 template <bool F32>
 __device__ __forceinline__ void stage_out(uint8_t* buf, uint32_t row, const float (&x)[32]) {
-    if constexpr (F32) stage_write<32>(reinterpret_cast<float*>(buf), row, x);
+    if constexpr (F32) stage_write(reinterpret_cast<float*>(buf), row, x);
     else {
         uint4* base = reinterpret_cast<uint4*>(buf) + row * 4u;
 #pragma unroll
@@ -242,9 +236,9 @@ __device__ __forceinline__ void write_piece(const Epilogue& e, const CUtensorMap
     else if (e.form == 2) write_rows<ACT, true>(e, map_c, map_z, out, x, sa, columns, row0, col, lane);
     else {
         float* tile = reinterpret_cast<float*>(out.base);
-        stage_write<32>(tile, lane, x);
+        stage_write(tile, lane, x);
         __syncwarp();
-        write_chunk_any<32, ACT>(e, tile, row0, col, lane);
+        write_chunk_any<ACT>(e, tile, row0, col, lane);
         __syncwarp();
     }
 }
@@ -412,6 +406,16 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t quad = warp & 3u;
     bool ok = true;
     if (warp >= 2) {
+        if (P.splits == 1) {                              // what the write-out reads is brought into L2 beside the products
+            prefetch_strip(P.e.mul, P.e.mul_type, P.e.ldmul, P.e, m0 + quad * 32u + lane, n0, kLinTile);
+            prefetch_strip(P.e.res, P.e.res_type, P.e.ldres, P.e, m0 + quad * 32u + lane, n0, kLinTile);
+        } else {
+            const uint32_t cols = P.splits == 2 ? 64u : 32u;
+            if (rank * cols < kLinTile) {
+                prefetch_strip(P.e.mul, P.e.mul_type, P.e.ldmul, P.e, m0 + quad * 32u + lane, n0 + rank * cols, cols);
+                prefetch_strip(P.e.res, P.e.res_type, P.e.ldres, P.e, m0 + quad * 32u + lane, n0 + rank * cols, cols);
+            }
+        }
         ok = __all_sync(0xFFFFFFFFu, lin_wait(smem_u32(&sh.acc_full), 0u, W));
         tc_fence_after();
         const uint32_t taddr = tmem + ((quad * 32u) << 16);
@@ -712,7 +716,6 @@ int encode_operand(CUtensorMap* out, const void* base, uint64_t rows, uint64_t c
     return r == CUDA_SUCCESS ? 0 : CLEAVE_E_CUDA;
 }
 
-// four neighbouring elements from a multiple of four columns on can be had with one access
 // Boxes of 32 x 32 of a row-major [rows x cols] output, bf16 or fp32, for bulk stores.
 int encode_output(CUtensorMap* out, void* base, uint64_t rows, uint64_t cols, uint64_t ld, bool f32) {
     EncodeTiledFn fn = encode_tiled_fn();
@@ -742,7 +745,6 @@ int encode_groups(CUtensorMap* out, const void* base, uint64_t rows, uint64_t co
 }
 
 bool rows16(const void* p, uint64_t ld, uint32_t type) { return (uintptr_t)p % 16 == 0 && (ld * type_bytes(type)) % 16 == 0; }
-bool wide4(const void* p, uint64_t ld, uint32_t type) { return (uintptr_t)p % (4 * type_bytes(type) + !type_bytes(type)) == 0 && ld % 4 == 0; }
 
 constexpr uint32_t kActs = CLEAVE_ACT_SILU + 1;
 using PairKernel = void (*)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const CUtensorMap, const PairParams);
@@ -780,9 +782,6 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     e.c_type = d.c_type; e.bias_type = d.bias_type; e.z_type = d.z_type; e.mul_type = d.mul_type; e.res_type = d.res_type;
     e.scale_a = d.scale_a; e.scale_b = d.scale_b; e.bias = d.bias; e.z = d.z; e.mul = d.mul; e.res = d.res; e.C = d.C;
     e.ldz = d.ldz; e.ldmul = d.ldmul; e.ldres = d.ldres; e.ldc = d.ldc;
-    e.wide = (wide4(d.scale_b, 0, CLEAVE_T_F32) ? kWideB : 0u) | (wide4(d.bias, 0, d.bias_type) ? kWideBias : 0u) |
-             (wide4(d.z, d.ldz, d.z_type) ? kWideZ : 0u) | (wide4(d.mul, d.ldmul, d.mul_type) ? kWideMul : 0u) |
-             (wide4(d.res, d.ldres, d.res_type) ? kWideRes : 0u) | (wide4(d.C, d.ldc, d.c_type) ? kWideC : 0u);
     // bulk stores want 16-byte rows, and so do the row loads of mul and res
     const bool bulk = rows16(d.C, d.ldc, d.c_type) && d.ldc * type_bytes(d.c_type) < (1ull << 40) && (!d.z || (d.z_type == CLEAVE_T_BF16 && rows16(d.z, d.ldz, d.z_type) && d.ldz < (1ull << 39))) &&
                       (!d.mul || rows16(d.mul, d.ldmul, d.mul_type)) && (!d.res || rows16(d.res, d.ldres, d.res_type));

@@ -198,10 +198,21 @@ __device__ __forceinline__ float gelu_tanh_gate(float z) {
     return rcp_fast(1.f + exp2_fast(-z * fmaf(0.1029432407f, z * z, 2.3022081983f)));
 }
 __device__ __forceinline__ float silu_gate(float z) { return rcp_fast(1.f + exp2_fast(-1.4426950409f * z)); }
+// Phi(z), the normal distribution, and exp(-z^2 / 2): erfc by Abramowitz and Stegun's formula 7.1.26, |error| <= 1.5e-7, one
+// reciprocal and one exponential (erfcf takes four times as long: 84 against 24 us in the write-out of 39 M elements)
+__device__ __forceinline__ float2 normal_cdf(float z) {
+    const float x = 0.7071067811865476f * fabsf(z), t = rcp_fast(fmaf(0.3275911f, x, 1.f));
+    float p = fmaf(1.061405429f, t, -1.453152027f);
+    p = fmaf(p, t, 1.421413741f);
+    p = fmaf(p, t, -0.284496736f);
+    p = fmaf(p, t, 0.254829592f);
+    const float e = exp2_fast(-1.4426950409f * x * x), tail = 0.5f * p * t * e;
+    return make_float2(z > 0.f ? 1.f - tail : tail, e);
+}
 __device__ __forceinline__ float act_value(float z, uint32_t act) {
     switch (act) {
         case CLEAVE_ACT_RELU: return z > 0.f ? z : (z != z ? z : 0.f);
-        case CLEAVE_ACT_GELU: return 0.5f * z * erfcf(-0.7071067811865476f * z);
+        case CLEAVE_ACT_GELU: return z * normal_cdf(z).x;
         case CLEAVE_ACT_GELU_TANH: return z * gelu_tanh_gate(z);
         case CLEAVE_ACT_SILU: return z * silu_gate(z);
         default: return z;
@@ -212,8 +223,8 @@ __device__ __forceinline__ float2 act_value_slope(float z, uint32_t act) {
     switch (act) {
         case CLEAVE_ACT_RELU: return make_float2(z > 0.f ? z : (z != z ? z : 0.f), z > 0.f ? 1.f : 0.f);
         case CLEAVE_ACT_GELU: {
-            const float phi = 0.5f * erfcf(-0.7071067811865476f * z);
-            return make_float2(z * phi, fmaf(z * 0.3989422804014327f, __expf(-0.5f * z * z), phi));
+            const float2 n = normal_cdf(z);
+            return make_float2(z * n.x, fmaf(z * n.y, 0.3989422804014327f, n.x));
         }
         case CLEAVE_ACT_GELU_TANH: {
             const float g = gelu_tanh_gate(z), zg = z * g;
