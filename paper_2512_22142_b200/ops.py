@@ -1,26 +1,23 @@
-"""ctypes binding of the operators around the GEMMs (second half of include/cleave.h).
+"""Binding of the operators around the GEMMs (second half of include/cleave.h).
 
 Arguments are torch tensors on the GPU; outputs are written into tensors that the caller passes.  The binding
-checks what the C library cannot see (types, shapes, strides, devices) and marshals; the library checks the rest
-and computes.  `stream` is a torch stream, a raw cudaStream_t or None for torch's current stream; tensors that
-were made on another stream are the caller's to order, as with any launch.
+checks what the C library cannot see (types, shapes, strides, devices) and marshals (csrc/marshal.cpp; the optimizer's
+handle by ctypes); the library checks the rest and computes.  `stream` is a torch stream, a raw cudaStream_t or None
+for torch's current stream; tensors that were made on another stream are the caller's to order, as with any launch.
 """
 from __future__ import annotations
 
 import ctypes as C
-import struct
 
 import torch
 
-from .binding import CleaveError, _check, lib
+from . import _marshal
+from .binding import _check, lib
 
 _vp, _u32, _u64, _i, _f, _d = C.c_void_p, C.c_uint32, C.c_uint64, C.c_int, C.c_float, C.c_double
 
 T_NONE, T_BF16, T_F32, T_E4M3 = 0, 1, 2, 3
 _TYPE = {torch.bfloat16: T_BF16, torch.float32: T_F32, torch.float8_e4m3fn: T_E4M3}
-_FLOATS = {torch.bfloat16: T_BF16, torch.float32: T_F32}
-_F32 = {torch.float32: T_F32}
-_CODES = {torch.float8_e4m3fn: T_E4M3}
 ACT = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
@@ -83,82 +80,34 @@ for _name, (_res, _args) in _sig.items():
     _fn.restype, _fn.argtypes = _res, _args
 
 
-def _packer(cls):
-    """A function that lays positional values out as the record `cls` (bytes): what a call that lasts microseconds can
-    afford, where setting a ctypes record's fields one by one takes as long as the launch."""
-    codes = {_u64: "Q", _u32: "I", _vp: "Q", _f: "f", _d: "d", C.c_uint8: "B", C.c_uint16: "H"}
-    flat = [f for name, kind in cls._fields_ for f in (kind._fields_ if hasattr(kind, "_fields_") else [(name, kind)])]
-    layout = struct.Struct("@" + "".join(codes[kind] for _, kind in flat))
-    assert layout.size == C.sizeof(cls)
-    return layout.pack
+def _raw(stream):
+    """What the marshalling takes: None for torch's current stream, else the raw stream."""
+    return None if stream is None else (stream if isinstance(stream, int) else stream.cuda_stream)
 
 
-def _record_call(name):
-    """The entry point with its record as bytes."""
-    fn = lib[name]
-    fn.restype, fn.argtypes = _i, [C.c_char_p] + _sig[name][1][1:]
-    return fn
-
-
-_pack_rmsnorm, _pack_rmsnorm_backward, _pack_linear, _pack_act_backward = (
-    _packer(c) for c in (_Rmsnorm, _RmsnormBackward, _Linear, _ActBackward))
-_call_rmsnorm, _call_rmsnorm_backward, _call_linear, _call_act_backward = (
-    _record_call("cleave_" + n) for n in ("rmsnorm", "rmsnorm_backward", "linear", "act_backward"))
-_current_stream, _current_device = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
-
-
-def _raw_stream(stream) -> int:
+def _raw_stream(stream, device=None) -> int:
     if stream is None:
-        return _current_stream(_current_device())
-    return stream if isinstance(stream, int) else stream.cuda_stream
+        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device is None else device)
+    return _raw(stream)
 
 
 def _bad(what: str):
     raise ValueError(what)
 
 
-_ABSENT = (0, 0, 0)
+def _act_code(act: str) -> int:
+    code = ACT.get(act)
+    if code is None:
+        _bad(f"act: one of {', '.join(ACT)} is wanted")
+    return code
 
 
-def _matrix(t, name: str, shape, types) -> tuple:
-    """(type, address, leading dimension) of a row-major tensor of that shape."""
-    kind = types.get(t.dtype)
-    if kind is None or not t.is_cuda:
-        _bad(f"{name}: a GPU tensor of a supported type is wanted, got {t.dtype} on {t.device}")
-    if t.shape != shape:
-        _bad(f"{name}: shape {tuple(shape)} is wanted, got {tuple(t.shape)}")
-    ld, inner = t.stride()
-    cols = shape[1]
-    if inner != 1 and cols > 1:
-        _bad(f"{name}: rows have to be contiguous")
-    if ld < cols or shape[0] == 1:
-        if shape[0] > 1:
-            _bad(f"{name}: rows overlap")
-        ld = cols                  # a single row: any stride
-    return kind, t.data_ptr(), ld
-
-
-def _vector(t, name: str, n: int, types) -> tuple:
-    """(type, address) of a contiguous [n] tensor; (0, 0) for None."""
-    if t is None:
-        return 0, 0
-    kind = types.get(t.dtype)
-    if kind is None or not t.is_cuda:
-        _bad(f"{name}: a GPU tensor of a supported type is wanted, got {t.dtype} on {t.device}")
-    if t.shape != (n,) or (n > 1 and t.stride(0) != 1):
-        _bad(f"{name}: a contiguous tensor of {n} elements is wanted, got {tuple(t.shape)}")
-    return kind, t.data_ptr()
-
-
-def _workspace(given, nbytes: int, like, raw: int, stream):
-    """The caller's workspace, or one from torch's allocator that outlives the launch on its stream."""
-    if given is not None:
-        if not given.is_cuda or not given.is_contiguous() or given.numel() * given.element_size() < nbytes:
-            _bad(f"workspace: {nbytes} contiguous bytes on the GPU are wanted")
+def _workspace(given, nbytes: int, like, stream):
+    """For a launch on another stream than torch's current one: a workspace that the allocator keeps for it."""
+    if given is not None or stream is None:
         return given
     ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
-    if stream is not None:
-        ws.record_stream(torch.cuda.ExternalStream(raw, device=like.device) if isinstance(stream, int) else stream)
+    ws.record_stream(torch.cuda.ExternalStream(stream, device=like.device) if isinstance(stream, int) else stream)
     return ws
 
 
@@ -179,7 +128,7 @@ class AdamW:
         if n == 0 or len(grads) != n or len(m) != n or len(v) != n:
             _bad("params, grads, m and v: one of each per tensor is wanted")
         state, grad = _TYPE.get(m[0].dtype, 0), _TYPE.get(grads[0].dtype, 0)
-        if state not in (T_F32, T_E4M3) or grads[0].dtype not in _FLOATS:
+        if state not in (T_F32, T_E4M3) or grad not in (T_BF16, T_F32):
             _bad("states are float32 or float8_e4m3fn, gradients float32 or bfloat16")
         if (state == T_E4M3) != (m_scales is not None) or (state == T_E4M3) != (v_scales is not None):
             _bad("m_scales and v_scales go with 8-bit states")
@@ -208,6 +157,7 @@ class AdamW:
         self._keep = (list(params), list(grads), list(m), list(v), lists)
         self._n, self._grad = n, grad
         self._step = _AdamwStep()
+        self._device = device.index
         h = _vp()
         with torch.cuda.device(device):
             _check(lib.cleave_adamw_create(table, n, state, grad, C.byref(h)), "cleave_adamw_create")
@@ -221,7 +171,7 @@ class AdamW:
             if not g.is_cuda or g.device != p.device or _TYPE.get(g.dtype, 0) != self._grad or g.numel() != p.numel() or not g.is_contiguous():
                 _bad(f"grads[{i}]: a contiguous GPU tensor of the same type and size as before is wanted")
         ptrs = (_vp * self._n)(*[g.data_ptr() for g in grads])
-        _check(lib.cleave_adamw_set_grads(self._h, ptrs, _raw_stream(stream)), "cleave_adamw_set_grads")
+        _check(lib.cleave_adamw_set_grads(self._h, ptrs, _raw_stream(stream, self._device)), "cleave_adamw_set_grads")
         self._keep = (self._keep[0], list(grads)) + self._keep[2:]
 
     def step(self, *, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
@@ -231,7 +181,9 @@ class AdamW:
             _bad("step counts from 1")
         s = self._step
         s.lr, s.beta1, s.beta2, s.eps, s.grad_scale, s.step, s.seed = lr, beta1, beta2, eps, grad_scale, step, seed & 0xFFFFFFFFFFFFFFFF
-        _check(lib.cleave_adamw_step(self._h, C.byref(s), _raw_stream(stream)), "cleave_adamw_step")
+        code = lib.cleave_adamw_step(self._h, C.byref(s), _raw_stream(stream, self._device))
+        if code:
+            _check(code, "cleave_adamw_step")
 
     def close(self) -> None:
         if self._h:
@@ -250,20 +202,7 @@ def rmsnorm(x, weight, y, *, residual=None, h=None, rstd=None, scale=None, eps: 
 
     x, residual (and h, of its type): bf16 or fp32 [rows, cols]; weight [cols] or None; y: bf16, fp32, or
     float8_e4m3fn with `scale` fp32 [rows]; rstd fp32 [rows] or None (what the backward pass needs)."""
-    shape = x.shape
-    if len(shape) != 2:
-        _bad("x: two dimensions are wanted")
-    rows, cols = shape
-    xt, xp, ldx = _matrix(x, "x", shape, _FLOATS)
-    rt, rp, ldr = _ABSENT if residual is None else _matrix(residual, "residual", shape, _FLOATS)
-    ht, hp, ldh = _ABSENT if h is None else _matrix(h, "h", shape, _FLOATS)
-    if h is not None and ht != rt:
-        _bad("h: the residual's type is wanted")
-    wt, wp = _vector(weight, "weight", cols, _FLOATS)
-    yt, yp, ldy = _matrix(y, "y", shape, _TYPE)
-    record = _pack_rmsnorm(rows, cols, xt, rt, wt, yt, eps, xp, ldx, rp, ldr, hp, ldh, wp, yp, ldy, _vector(rstd, "rstd", rows, _F32)[1],
-                           _vector(scale, "scale", rows, _F32)[1])
-    code = _call_rmsnorm(record, _raw_stream(stream))
+    code = _marshal.rmsnorm(x, weight, y, residual, h, rstd, scale, eps, _raw(stream))
     if code:
         _check(code, "cleave_rmsnorm")
 
@@ -275,39 +214,18 @@ def rmsnorm_backward_workspace(rows: int, cols: int) -> int:
 def rmsnorm_backward(dy, h, weight, rstd, dx, dweight=None, *, dres=None, workspace=None, stream=None) -> None:
     """cleave_rmsnorm_backward: dx (the gradient of x and of the residual alike) and dweight (fp32, or None) from the
     saved h and rstd; `dres`, of h's type, is the gradient that reaches h from the residual stream."""
-    shape = h.shape
-    if len(shape) != 2:
-        _bad("h: two dimensions are wanted")
-    rows, cols = shape
-    dyt, dyp, lddy = _matrix(dy, "dy", shape, _FLOATS)
-    ht, hp, ldh = _matrix(h, "h", shape, _FLOATS)
-    wt, wp = _vector(weight, "weight", cols, _FLOATS)
-    own = {h.dtype: ht}
-    _, rp, ldr = _ABSENT if dres is None else _matrix(dres, "dres", shape, own)
-    _, dxp, lddx = _matrix(dx, "dx", shape, own)
-    record = _pack_rmsnorm_backward(rows, cols, dyt, ht, wt, 0, dyp, lddy, hp, ldh, wp, _vector(rstd, "rstd", rows, _F32)[1], rp, ldr, dxp, lddx,
-                                    _vector(dweight, "dweight", cols, _F32)[1])
-    raw = _raw_stream(stream)
-    ws = None if dweight is None else _workspace(workspace, lib.cleave_rmsnorm_backward_workspace(rows, cols), h, raw, stream)
-    code = _call_rmsnorm_backward(record, None if ws is None else ws.data_ptr(), raw)
+    if dweight is not None and stream is not None:
+        workspace = _workspace(workspace, rmsnorm_backward_workspace(*h.shape), h, stream)
+    code = _marshal.rmsnorm_backward(dy, h, weight, rstd, dx, dweight, dres, workspace, _raw(stream))
     if code:
         _check(code, "cleave_rmsnorm_backward")
 
 
 def quantize_rows(x, y, scale, *, stream=None) -> None:
     """cleave_quantize_rows: y (float8_e4m3fn) = x / scale, scale fp32 [rows] = largest magnitude of the row / 448."""
-    shape = x.shape
-    if len(shape) != 2:
-        _bad("x: two dimensions are wanted")
-    if scale is None:
-        _bad("scale: a tensor is wanted")
-    kind, px, ldx = _matrix(x, "x", shape, _FLOATS)
-    _, py, ldy = _matrix(y, "y", shape, _CODES)
-    ps = _vector(scale, "scale", shape[0], _F32)[1]
-    _check(lib.cleave_quantize_rows(px, kind, shape[0], shape[1], ldx, py, ldy, ps, _raw_stream(stream)), "cleave_quantize_rows")
-
-
-_IN = {torch.bfloat16: T_BF16, torch.float8_e4m3fn: T_E4M3}
+    code = _marshal.quantize_rows(x, y, scale, _raw(stream))
+    if code:
+        _check(code, "cleave_quantize_rows")
 
 
 def linear(A, B, out, *, transA: bool = False, transB: bool = False, scale_a=None, scale_b=None, bias=None, act: str = "none", z=None,
@@ -317,32 +235,7 @@ def linear(A, B, out, *, transA: bool = False, transB: bool = False, scale_a=Non
     A: [M, K] ([K, M] with transA), B: [K, N] ([N, K] with transB), both bf16, or both float8_e4m3fn with
     transB.  scale_a [M], scale_b [N] fp32.  bias [N], z, mul, residual [M, N], out [M, N]: bf16 or fp32.
     `residual` may be `out` itself (an accumulation)."""
-    shape_a, shape_b = A.shape, B.shape
-    if len(shape_a) != 2 or len(shape_b) != 2:
-        _bad("A, B: two dimensions are wanted")
-    K, M = shape_a if transA else (shape_a[1], shape_a[0])
-    N = shape_b[0 if transB else 1]
-    if shape_b[1 if transB else 0] != K:
-        _bad(f"B: {K} products are wanted, got shape {tuple(shape_b)}")
-    kind, ap, lda = _matrix(A, "A", shape_a, _IN)
-    _, bp, ldb = _matrix(B, "B", shape_b, {A.dtype: kind})
-    unit = 16 if kind == T_E4M3 else 8
-    if shape_a[0] == 1:
-        lda = -(-shape_a[1] // unit) * unit                 # a single row has no second one
-    if shape_b[0] == 1:
-        ldb = -(-shape_b[1] // unit) * unit
-    code = ACT.get(act)
-    if code is None:
-        _bad(f"act: one of {', '.join(ACT)} is wanted")
-    shape = (M, N)
-    ct, cp, ldc = _matrix(out, "out", shape, _FLOATS)
-    bt, biasp = _vector(bias, "bias", N, _FLOATS)
-    zt, zp, ldz = _ABSENT if z is None else _matrix(z, "z", shape, _FLOATS)
-    mt, mp, ldm = _ABSENT if mul is None else _matrix(mul, "mul", shape, _FLOATS)
-    rt, rp, ldr = _ABSENT if residual is None else _matrix(residual, "residual", shape, _FLOATS)
-    record = _pack_linear(M, N, K, lda, ldb, transA, transB, 0, kind, ct, bt, zt, mt, rt, code, 0, ap, bp,
-                          _vector(scale_a, "scale_a", M, _F32)[1], _vector(scale_b, "scale_b", N, _F32)[1], biasp, zp, ldz, mp, ldm, rp, ldr, cp, ldc)
-    code = _call_linear(record, _raw_stream(stream))
+    code = _marshal.linear(A, B, out, transA, transB, scale_a, scale_b, bias, _act_code(act), z, mul, residual, _raw(stream))
     if code:
         _check(code, "cleave_linear")
 
@@ -358,22 +251,8 @@ def act_backward_workspace(rows: int, cols: int) -> int:
 
 def act_backward(dy, z, dz=None, *, act: str = "none", mul=None, dmul=None, dbias=None, workspace=None, stream=None) -> None:
     """cleave_act_backward: dz = dy mul act'(z), dmul = dy act(z), dbias (fp32) = column sums of dz before its rounding."""
-    shape = dy.shape
-    if len(shape) != 2:
-        _bad("dy: two dimensions are wanted")
-    rows, cols = shape
-    code = ACT.get(act)
-    if code is None:
-        _bad(f"act: one of {', '.join(ACT)} is wanted")
-    dyt, dyp, lddy = _matrix(dy, "dy", shape, _FLOATS)
-    zt, zp, ldz = _ABSENT if z is None else _matrix(z, "z", shape, _FLOATS)
-    mt, mp, ldm = _ABSENT if mul is None else _matrix(mul, "mul", shape, _FLOATS)
-    dzt, dzp, lddz = _ABSENT if dz is None else _matrix(dz, "dz", shape, _FLOATS)
-    dmt, dmp, lddm = _ABSENT if dmul is None else _matrix(dmul, "dmul", shape, _FLOATS)
-    record = _pack_act_backward(rows, cols, code, dyt, zt, mt, dzt, dmt, 0, dyp, lddy, zp, ldz, mp, ldm, dzp, lddz, dmp, lddm,
-                                _vector(dbias, "dbias", cols, _F32)[1])
-    raw = _raw_stream(stream)
-    ws = None if dbias is None else _workspace(workspace, lib.cleave_act_backward_workspace(rows, cols), dy, raw, stream)
-    code = _call_act_backward(record, None if ws is None else ws.data_ptr(), raw)
+    if dbias is not None and stream is not None:
+        workspace = _workspace(workspace, act_backward_workspace(*dy.shape), dy, stream)
+    code = _marshal.act_backward(dy, z, dz, _act_code(act), mul, dmul, dbias, workspace, _raw(stream))
     if code:
         _check(code, "cleave_act_backward")
