@@ -56,7 +56,7 @@ __device__ __forceinline__ Band this_band(uint64_t rows) {
 template <uint32_t ACT, bool MUL>
 __global__ void __launch_bounds__(32 * kActWarps) act_backward_any_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
     __shared__ float s[kActWarps][32];
-    let_dependents_start();
+    begin_chained();
     constexpr int ROWS = 4;
     const uint64_t j = (uint64_t)blockIdx.x * 32u + (threadIdx.x & 31u);
     const Band b = this_band(d.rows);
@@ -92,7 +92,7 @@ template <typename D, typename T, uint32_t ACT, bool MUL, int STAGES>
 __global__ void __launch_bounds__(32 * kActWarps, 3) act_backward_wide_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float s[kActWarps][32 * 8];
-    let_dependents_start();
+    begin_chained();
     constexpr uint32_t BD = sizeof(D) * 8, BT = sizeof(T) * 8, NT = MUL ? 2 : 1, STAGE = 32 * (BD + NT * BT);
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     const uint64_t j = ((uint64_t)blockIdx.x * 32u + lane) * 8u;
@@ -160,15 +160,11 @@ cudaError_t launch_act_wide(const cleave_act_backward_t& d, float* ws, uint32_t 
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
-    kernel<<<dim3((d.cols + 255) / 256, parts), 32 * kActWarps, smem, st>>>(d, ws);
-    return cudaGetLastError();
+    return launch_chained(kernel, dim3((d.cols + 255) / 256, parts), 32 * kActWarps, smem, st, d, ws);
 }
 template <uint32_t ACT, bool MUL>
 cudaError_t launch_act(const cleave_act_backward_t& d, float* ws, uint32_t parts, bool wide, uint32_t type, cudaStream_t st) {
-    if (!wide) {
-        act_backward_any_kernel<ACT, MUL><<<dim3((d.cols + 31) / 32, parts), 32 * kActWarps, 0, st>>>(d, ws);
-        return cudaGetLastError();
-    }
+    if (!wide) return launch_chained(act_backward_any_kernel<ACT, MUL>, dim3((d.cols + 31) / 32, parts), 32 * kActWarps, 0, st, d, ws);
     if (d.dy_type == CLEAVE_T_F32)
         return type == CLEAVE_T_F32 ? launch_act_wide<float, float, ACT, MUL>(d, ws, parts, st) : launch_act_wide<float, __nv_bfloat16, ACT, MUL>(d, ws, parts, st);
     return type == CLEAVE_T_F32 ? launch_act_wide<__nv_bfloat16, float, ACT, MUL>(d, ws, parts, st) : launch_act_wide<__nv_bfloat16, __nv_bfloat16, ACT, MUL>(d, ws, parts, st);

@@ -199,10 +199,11 @@ template <bool STATE8, typename G> struct AdamStage {
 
 template <bool STATE8, typename G>
 __global__ void __launch_bounds__(32 * kChunkWarps, 3)
-adamw_kernel(const AdamTensor* __restrict__ tensors, const AdamChunk* __restrict__ chunks, uint32_t chunk_blocks, const __grid_constant__ AdamStep s) {
+adamw_kernel(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t chunk_blocks, const __grid_constant__ AdamStep s) {
     using Stage = AdamStage<STATE8, G>;
     using S = typename Stage::S;
     extern __shared__ __align__(16) uint8_t ring[];
+    begin_chained();
     const AdamChunk c = chunks[blockIdx.x];
     const AdamTensor t = tensors[c.tensor];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
@@ -285,8 +286,7 @@ cudaError_t launch_adamw_as(const AdamTensor* tensors, const AdamChunk* chunks, 
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
-    kernel<<<n_chunks, 32 * kChunkWarps, smem, st>>>(tensors, chunks, chunk_blocks, s);
-    return cudaGetLastError();
+    return launch_chained(kernel, n_chunks, 32 * kChunkWarps, smem, st, tensors, chunks, chunk_blocks, s);
 }
 
 cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uint32_t n_chunks, uint32_t chunk_blocks, const AdamStep& s,

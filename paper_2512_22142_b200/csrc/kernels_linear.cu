@@ -67,7 +67,7 @@ template <uint32_t ACT>
 __device__ __forceinline__ void write_chunk_any(const Epilogue& e, const float* tile, uint32_t row0, uint32_t col, uint32_t lane) {
     const uint64_t j = col + lane;
     if (j >= e.N) return;
-    const float sb = e.scale_b ? __ldg(e.scale_b + j) : 1.f, bias = e.bias ? load_as(e.bias, e.bias_type, j) : 0.f;
+    const float sb = e.scale_b ? e.scale_b[j] : 1.f, bias = e.bias ? load_as(e.bias, e.bias_type, j) : 0.f;
     const uint32_t rows = min(32u, e.M - row0);
     constexpr uint32_t U = 8;                                            // rows asked for before the ones in hand are used
     uint32_t mul[U], res[U];                                             // raw words: nothing waits for a load before all are on their way
@@ -101,7 +101,7 @@ __device__ __forceinline__ void write_chunk_any(const Epilogue& e, const float* 
             if (r >= rows) break;
             const uint64_t row = row0 + r;
             const float x = tile[r * 32u + ((((lane >> 2) ^ (r & 7u)) << 2) | (lane & 3u))];
-            const float z = x * (e.scale_a ? __ldg(e.scale_a + row) : 1.f) * sb + bias;
+            const float z = x * (e.scale_a ? e.scale_a[row] : 1.f) * sb + bias;
             if (e.z) store_as(e.z, e.z_type, row * e.ldz + j, z);
             store_as(e.C, e.c_type, row * e.ldc + j, fmaf(act_value(z, ACT), m[k], a[k]));
         }
@@ -171,7 +171,7 @@ struct ColumnPair { float scale, bias; };
 __device__ __forceinline__ ColumnPair load_columns(const Epilogue& e, uint32_t col) {
     ColumnPair p = {0.f, 0.f};
     if (col < e.N) {
-        if (e.scale_b) p.scale = __ldg(e.scale_b + col);
+        if (e.scale_b) p.scale = e.scale_b[col];
         if (e.bias) p.bias = load_as(e.bias, e.bias_type, col);
     }
     return p;
@@ -248,7 +248,7 @@ __device__ __forceinline__ void write_piece(const Epilogue& e, const CUtensorMap
 template <uint32_t ACT, typename Ready, typename Read>
 __device__ __forceinline__ bool write_strip(const Epilogue& e, const CUtensorMap* map_c, const CUtensorMap* map_z, OutRing& out, uint32_t taddr, uint32_t row0,
                                             uint32_t col, uint32_t c, uint32_t step, uint32_t cols, uint32_t lane, Ready ready, Read read) {
-    const float sa = e.scale_a && row0 + lane < e.M ? __ldg(e.scale_a + row0 + lane) : 1.f;
+    const float sa = e.scale_a && row0 + lane < e.M ? e.scale_a[row0 + lane] : 1.f;
     ColumnPair next = load_columns(e, col + c + lane);
     if (!ready()) return false;
     if (c >= cols) read();
@@ -347,6 +347,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     const uint32_t m0 = (tile / P.tiles_n) * kLinTile, n0 = (tile % P.tiles_n) * kLinTile;
     const uint32_t kb0 = (uint32_t)((uint64_t)P.K_blocks * rank / P.splits), kb1 = (uint32_t)((uint64_t)P.K_blocks * (rank + 1) / P.splits);
     const LinWait W = {&sh.abort_flag, P.wait_limit_ns};
+    let_dependents_start();
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < kLinStages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
@@ -364,6 +365,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
+    wait_for_primary();
 
     if (warp == 0 && lane == 0) {
         // ---- producer ----
@@ -445,7 +447,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
             const uint32_t cols = P.splits == 2 ? 64u : 32u, c0 = rank * cols, row0 = m0 + quad * 32u;
             OutRing out = {dyn_smem + (base - smem_u32(dyn_smem)) + 65536 + (warp - 2) * 8192, 4096u, 2u, 0u};   // behind the accumulators
             if (row0 < P.e.M) {
-                const float sa = P.e.scale_a && row0 + lane < P.e.M ? __ldg(P.e.scale_a + row0 + lane) : 1.f;
+                const float sa = P.e.scale_a && row0 + lane < P.e.M ? P.e.scale_a[row0 + lane] : 1.f;
 #pragma unroll 1
                 for (uint32_t c = c0; c < min(c0 + cols, kLinTile) && n0 + c < P.e.N; c += 32) {
                     float x[32];
@@ -547,6 +549,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     const uint32_t base = (smem_u32(dyn_smem) + 1023u) & ~1023u;
     const uint32_t tiles = P.tiles_m * P.tiles_n, cluster = blockIdx.x >> 1, clusters = gridDim.x >> 1;
     const WaitCtx W = {&sh.abort_flag, &g_linear_status, P.wait_limit_ns};
+    let_dependents_start();
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < P.stages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
@@ -561,6 +564,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
     cluster_arrive_wait();                            // barriers of both CTAs are ready before any remote arrive
     tc_fence_after();
     const uint32_t tmem = sh.tmem_base;
+    wait_for_primary();
 
     if (warp < kLpEpiWarp0) {
         if constexpr (LONG) asm volatile("setmaxnreg.dec.sync.aligned.u32 40;");       // 128 x 40 + 256 x 216 <= 384 x 168 registers
@@ -798,11 +802,13 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     CUtensorMap ma, mb;
     auto encode_b = [&](uint32_t rows) { return g.transB ? encode_operand(&mb, d.B, g.N, g.K, g.ldb, rows, e4m3) : encode_operand(&mb, d.B, g.K, g.N, g.ldb, 64, e4m3); };
     cudaLaunchConfig_t cfg = {};
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     cfg.stream = st;
     cudaError_t err;
     const uint64_t tiles_m = (g.M + kLinTile - 1) / kLinTile, tiles_n = (g.N + kLinTile - 1) / kLinTile, tiles = tiles_m * tiles_n;
@@ -841,7 +847,7 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         cfg.gridDim = dim3(2u * (unsigned)(all < pairs ? all : pairs));
         cfg.blockDim = dim3(pair_threads(lng));
         cfg.dynamicSmemBytes = smem;
-        cfg.numAttrs = 0;                                   // (the cluster size is the kernel's own)
+        cfg.numAttrs = 1;                                   // (the cluster size is the kernel's own)
         err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, mc, mz, Q);
     } else {
         P.tiles_n = (uint32_t)tiles_n;
@@ -858,7 +864,7 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         cfg.gridDim = dim3((unsigned)(tiles * P.splits));
         cfg.blockDim = dim3(kLinThreads);
         cfg.dynamicSmemBytes = kLinSmem;
-        attr[0].val.clusterDim.x = P.splits;
+        attr[1].val.clusterDim.x = P.splits;
         err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, mc, mz, P);
     }
     if (err != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }

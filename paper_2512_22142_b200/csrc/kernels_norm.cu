@@ -49,6 +49,7 @@ __device__ __forceinline__ float2 row_scale(float top) {
 template <bool NORM>
 __global__ void __launch_bounds__(kRowThreads) row_any_kernel(const __grid_constant__ cleave_rmsnorm_t d) {
     __shared__ float buf[32];
+    begin_chained();
     const uint64_t row = blockIdx.x;
     const uint64_t ox = row * d.ldx, orr = row * d.ldr, oh = row * d.ldh, oy = row * d.ldy;
     // (h may be r's buffer: it is written in the last pass only, each element by the thread that has just read it)
@@ -132,6 +133,7 @@ __device__ __forceinline__ float2 cta_join(float sum, float top, float2* p) {
 template <bool NORM, int T>
 __global__ void __launch_bounds__(T) row_own_kernel(const __grid_constant__ cleave_rmsnorm_t d) {
     __shared__ float2 parts[3][32];
+    begin_chained();
     float w[kOwn];
     uint32_t x[kOwn], r[kOwn];
 #pragma unroll
@@ -193,7 +195,7 @@ __global__ void __launch_bounds__(T) row_own_kernel(const __grid_constant__ clea
 template <int T>
 __global__ void __launch_bounds__(T) rmsnorm_backward_own_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws) {
     __shared__ float2 parts[2][32];
-    let_dependents_start();
+    begin_chained();
     float w[kOwn], dw[kOwn];
     uint32_t ndy[kOwn], nh[kOwn], nres[kOwn];
 #pragma unroll
@@ -205,7 +207,7 @@ __global__ void __launch_bounds__(T) rmsnorm_backward_own_kernel(const __grid_co
     load_own(d.h, d.h_type, row * d.ldh, d.cols, nh);
     if (d.dres) load_own(d.dres, d.h_type, row * d.lddres, d.cols, nres);
     for (uint32_t it = 0; row < d.rows; row += gridDim.x, ++it) {
-        const float rstd = __ldg(d.rstd + row);
+        const float rstd = d.rstd[row];
         float q[kOwn], g[kOwn], res[kOwn], dot = 0.f;
         own_values(ndy, d.dy_type, d.cols, q);
         own_values(nh, d.h_type, d.cols, g);
@@ -243,11 +245,11 @@ __device__ __forceinline__ void load_weight8(const Desc& d, uint32_t col, F2 (&w
     if (d.w_type == CLEAVE_T_F32) {
         Raw8<float> r;
         const uint4* p = reinterpret_cast<const uint4*>(static_cast<const float*>(d.w) + col);
-        r.w[0] = __ldg(p); r.w[1] = __ldg(p + 1);
+        r.w[0] = p[0]; r.w[1] = p[1];
         unpack8(r, w);
     } else if (d.w_type == CLEAVE_T_BF16) {
         Raw8<__nv_bfloat16> r;
-        r.w[0] = __ldg(reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(d.w) + col));
+        r.w[0] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(d.w) + col);
         unpack8(r, w);
     } else {
 #pragma unroll
@@ -266,6 +268,7 @@ template <typename X, typename R, typename Y, int V, bool WARP, bool NORM, int T
 __global__ void __launch_bounds__(T, T == 128 ? 4 : (T == 256 ? 2 : 1)) row_wide_kernel(const __grid_constant__ cleave_rmsnorm_t d, uint32_t stages) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 parts[2][32];
+    begin_chained();
     constexpr bool RES = !(sizeof(R) == 1), CODES = sizeof(Y) == 1;
     constexpr uint32_t BX = Bytes8<X>::value, BR = Bytes8<R>::value;
     const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
@@ -432,8 +435,7 @@ cudaError_t launch_row_wide(const cleave_rmsnorm_t& d, uint32_t threads, int sms
     auto kernel = row_wide_kernel<X, R, Y, V, WARP, NORM, T>;
     if (WARP) {
         const uint64_t ctas = (d.rows + 7) / 8;
-        kernel<<<(unsigned)ctas, dim3(32, 8), 0, st>>>(d, 0u);
-        return cudaGetLastError();
+        return launch_chained(kernel, (unsigned)ctas, dim3(32, 8), 0, st, d, 0u);
     }
     const uint32_t stage = d.cols / 8 * (Bytes8<X>::value + Bytes8<R>::value);
     const uint32_t stages = max(1u, min(4u, kRingBytes / stage)), smem = stage * stages;
@@ -443,8 +445,7 @@ cudaError_t launch_row_wide(const cleave_rmsnorm_t& d, uint32_t threads, int sms
     // CTAs that fit an SM by shared memory and threads; each walks the rows in steps of the grid
     const uint32_t fit = max(1u, min(min(224u * 1024u / (smem + 2048u), 65536u / (threads * 128u)), 4u));
     const uint64_t ctas = min((uint64_t)d.rows, (uint64_t)sms * fit);
-    kernel<<<(unsigned)ctas, threads, smem, st>>>(d, stages);
-    return cudaGetLastError();
+    return launch_chained(kernel, (unsigned)ctas, threads, smem, st, d, stages);
 }
 
 template <typename X, typename R, typename Y, bool NORM>
@@ -484,11 +485,10 @@ cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, int sms, cudaSt
     if (d.cols <= kOwnCols) {
         const uint32_t threads = own_threads(d.cols);
         const unsigned ctas = (unsigned)std::min<uint64_t>(d.rows, (uint64_t)sms * std::min(24u, 1024u / threads));
-        if (threads <= 512) { if (norm) row_own_kernel<true, 512><<<ctas, threads, 0, st>>>(d); else row_own_kernel<false, 512><<<ctas, threads, 0, st>>>(d); }
-        else { if (norm) row_own_kernel<true, 1024><<<ctas, threads, 0, st>>>(d); else row_own_kernel<false, 1024><<<ctas, threads, 0, st>>>(d); }
-    } else if (norm) row_any_kernel<true><<<(unsigned)d.rows, kRowThreads, 0, st>>>(d);
-    else      row_any_kernel<false><<<(unsigned)d.rows, kRowThreads, 0, st>>>(d);
-    return cudaGetLastError();
+        auto kernel = threads <= 512 ? (norm ? row_own_kernel<true, 512> : row_own_kernel<false, 512>) : (norm ? row_own_kernel<true, 1024> : row_own_kernel<false, 1024>);
+        return launch_chained(kernel, ctas, threads, 0, st, d);
+    }
+    return launch_chained(norm ? row_any_kernel<true> : row_any_kernel<false>, (unsigned)d.rows, kRowThreads, 0, st, d);
 }
 
 // ---- backward ----------------------------------------------------------------------------------------
@@ -505,7 +505,7 @@ uint32_t rmsnorm_backward_parts(uint64_t rows, uint32_t cols) {
 
 __global__ void __launch_bounds__(kRowThreads) rmsnorm_backward_any_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws) {
     __shared__ float buf[32];
-    let_dependents_start();
+    begin_chained();
     float* dw = ws + (uint64_t)blockIdx.x * d.cols;
     if (d.dw) for (uint32_t j = threadIdx.x; j < d.cols; j += blockDim.x) dw[j] = 0.f;
     for (uint64_t row = blockIdx.x; row < d.rows; row += gridDim.x) {
@@ -533,7 +533,7 @@ template <typename D, typename H, int V, int T, int CTAS>
 __global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float parts[2][32];
-    let_dependents_start();
+    begin_chained();
     constexpr uint32_t BD = Bytes8<D>::value, BH = Bytes8<H>::value;
     const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
     const bool res = d.dres != nullptr;
@@ -578,7 +578,7 @@ __global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __
     uint32_t it = 0, at = 0;
     for (uint64_t row = blockIdx.x; row < d.rows; row += gridDim.x, ++it) {
         if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
-        const float rstd = __ldg(d.rstd + row);
+        const float rstd = d.rstd[row];
         const uint8_t* stage = ring + at;
         F2 q[V][4], dots = f2(0.f, 0.f);                         // q = w dy; dots: sum q h
         Raw8<H> rh[V], rr[V];
@@ -633,11 +633,12 @@ __global__ void __launch_bounds__(T, CTAS) rmsnorm_backward_wide_kernel(const __
 
 // out[j] = sum over the parts of ws[part][j], in a fixed order.  32 columns per CTA; warp w adds the parts
 // w, w + 32, ... and the 32 sums are added in warp order.
-__global__ void __launch_bounds__(1024) sum_parts_kernel(const float* __restrict__ ws, uint32_t parts, uint32_t cols, float* __restrict__ out) {
+__global__ void __launch_bounds__(1024) sum_parts_kernel(const float* ws, uint32_t parts, uint32_t cols, float* out) {
     __shared__ float s[32][33];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, j = blockIdx.x * 32u + lane;
     float v = 0.f;
-    wait_for_primary();
+    wait_for_primary();   // and no early start for what follows: the kernel whose sums these are still runs, and one
+                          // that shares the SMs with it lands on them unevenly (act_backward of 8192 x 3072: 30 -> 35 us)
     if (j < cols) {
 #pragma unroll 8
         for (uint32_t p = warp; p < parts; p += 32) v += __ldcs(ws + (uint64_t)p * cols + j);
@@ -649,16 +650,7 @@ __global__ void __launch_bounds__(1024) sum_parts_kernel(const float* __restrict
     if (lane == 0 && blockIdx.x * 32u + warp < cols) out[blockIdx.x * 32u + warp] = v;
 }
 cudaError_t launch_sum_parts(const float* ws, uint32_t parts, uint32_t cols, float* out, cudaStream_t st) {
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((cols + 31) / 32);
-    cfg.blockDim = dim3(1024);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, sum_parts_kernel, ws, parts, cols, out);
+    return launch_chained(sum_parts_kernel, (cols + 31) / 32, 1024, 0, st, ws, parts, cols, out);
 }
 
 template <typename D, typename H, int V, int T, int CTAS>
@@ -668,8 +660,7 @@ cudaError_t launch_backward_wide(const cleave_rmsnorm_backward_t& d, float* ws, 
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
     const uint32_t stages = max(1u, min(4u, min(kRingMost, 216u * 1024u / backward_ctas(d.cols)) / stage));
-    kernel<<<parts, threads, stage * stages, st>>>(d, ws, stages);
-    return cudaGetLastError();
+    return launch_chained(kernel, parts, threads, stage * stages, st, d, ws, stages);
 }
 template <typename D, typename H>
 cudaError_t launch_backward_types(const cleave_rmsnorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
@@ -694,12 +685,9 @@ cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* w
         else e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<__nv_bfloat16, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<__nv_bfloat16, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
     } else if (parts && d.cols <= kOwnCols) {
         const uint32_t threads = own_threads(d.cols);
-        if (threads <= 512) rmsnorm_backward_own_kernel<512><<<parts, threads, 0, st>>>(d, ws);
-        else rmsnorm_backward_own_kernel<1024><<<parts, threads, 0, st>>>(d, ws);
-        e = cudaGetLastError();
+        e = launch_chained(threads <= 512 ? rmsnorm_backward_own_kernel<512> : rmsnorm_backward_own_kernel<1024>, parts, threads, 0, st, d, ws);
     } else if (parts) {
-        rmsnorm_backward_any_kernel<<<parts, kRowThreads, 0, st>>>(d, ws);
-        e = cudaGetLastError();
+        e = launch_chained(rmsnorm_backward_any_kernel, parts, kRowThreads, 0, st, d, ws);
     }
     if (e != cudaSuccess || !d.dw) return e;
     return launch_sum_parts(ws, parts, d.cols, d.dw, st);

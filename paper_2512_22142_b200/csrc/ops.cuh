@@ -19,11 +19,28 @@ constexpr uint32_t kStateBlock = 256;            // elements that share a scale 
 
 inline uint32_t type_bytes(uint32_t t) { return t == CLEAVE_T_F32 ? 4u : (t == CLEAVE_T_BF16 ? 2u : (t == CLEAVE_T_E4M3 ? 1u : 0u)); }
 
-// A kernel that only adds up what the kernel before it leaves may be launched while that one still runs: the first lets
-// its dependents start (`let_dependents_start`, at its beginning), the second waits for it (`wait_for_primary`) before
-// it reads anything.  Hides the second launch (2 to 3 us).
+// The operators' kernels are launched so that a kernel may start while the one before it in the stream still runs: the
+// first lets its dependents start at its beginning, the second sets itself up and then waits until the first has
+// ended and its results are visible, before it touches any memory.  Stream order is what it always is; a launch's
+// own latency (2 to 3 us) passes beside the kernel before it.  No load here goes by the read-only path (ld.global.nc):
+// the memory may still change after the kernel has begun, before its wait ends.
 __device__ __forceinline__ void let_dependents_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 __device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+__device__ __forceinline__ void begin_chained() { let_dependents_start(); wait_for_primary(); }
+template <typename... P, typename... A>
+cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, uint32_t smem, cudaStream_t st, const A&... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
 
 // Raises a kernel's dynamic shared memory limit, once per device.
 struct SmemLimit {

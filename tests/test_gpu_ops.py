@@ -501,3 +501,50 @@ def test_act_backward_without_rows_and_plain_column_sums(cl):
     assert torch.equal(db, dy.sum(0))
     with pytest.raises(ValueError):
         cl.act_backward(dy, None, dbias=db, workspace=ws[:16])
+
+
+# ---- one operator after another ------------------------------------------------------------------------
+@pytest.mark.parametrize("rows,cols,ffn", [(3, 256, 512), (700, 768, 1536), (33, 130, 266)])
+def test_chained_calls_see_what_the_one_before_wrote(cl, rows, cols, ffn):
+    """Each call reads what the one before it writes, and buffers are written again two calls later; the same calls
+    with the device idle in between, and replayed from a CUDA graph, leave the same bits."""
+    rng = np.random.default_rng(rows)
+    w1, w2 = _strided(rng, cols, ffn, torch.bfloat16, -ffn % 8, cols ** -0.5), _strided(rng, ffn, cols, torch.bfloat16, -cols % 8, ffn ** -0.5)
+    norm, start, dy = _rand(rng, (cols,), torch.float32), _rand(rng, (rows, cols), torch.float32), _rand(rng, (rows, cols), torch.bfloat16)
+    bf = lambda r, c: torch.empty(r, c + -c % 8, dtype=torch.bfloat16, device=_dev())[:, :c]  # noqa: E731 (operands' rows: 16 bytes)
+    f32 = lambda *s: torch.empty(*s, device=_dev())  # noqa: E731
+    stream = torch.cuda.Stream()
+    spaces = [torch.empty(cl.rmsnorm_backward_workspace(rows, cols), dtype=torch.uint8, device=_dev()),
+              torch.empty(cl.act_backward_workspace(rows, ffn), dtype=torch.uint8, device=_dev())]
+
+    def buffers():
+        return dict(h=start.clone(), y=bf(rows, cols), z=bf(rows, ffn), a=bf(rows, ffn), out=bf(rows, cols).zero_(), rstd=f32(rows), dz=bf(rows, ffn),
+                    db=f32(ffn), da=bf(rows, ffn), dh=f32(rows, cols), dw=f32(cols), g=f32(rows, cols).zero_())
+
+    def chain(t, between):
+        for _ in range(3):
+            for call in (lambda: cl.rmsnorm(t["out"], norm, t["y"], residual=t["h"], h=t["h"], rstd=t["rstd"], stream=stream),
+                         lambda: cl.linear(t["y"], w1, t["a"], act="gelu_tanh", z=t["z"], stream=stream),
+                         lambda: cl.linear(t["a"], w2, t["out"], stream=stream),
+                         lambda: cl.linear(t["out"], w2, t["da"], transB=True, stream=stream),
+                         lambda: cl.act_backward(t["da"], t["z"], t["dz"], act="gelu_tanh", dbias=t["db"], workspace=spaces[1], stream=stream),
+                         lambda: cl.linear(t["dz"], w1, t["out"], transB=True, stream=stream),
+                         lambda: cl.rmsnorm_backward(dy, t["h"], norm, t["rstd"], t["dh"], t["dw"], dres=t["g"], workspace=spaces[0], stream=stream),
+                         lambda: cl.rmsnorm_backward(t["out"], t["h"], norm, t["rstd"], t["g"], t["dw"], dres=t["dh"], workspace=spaces[0], stream=stream)):
+                call()
+                between()
+
+    slow, fast, replayed = buffers(), buffers(), buffers()
+    torch.cuda.synchronize()
+    chain(slow, torch.cuda.synchronize)
+    chain(fast, lambda: None)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        chain(replayed, lambda: None)
+    graph.replay()
+    torch.cuda.synchronize()
+    for k, v in slow.items():
+        assert torch.isfinite(v.float()).all(), k
+        assert torch.equal(v, fast[k]), k
+        assert torch.equal(v, replayed[k]), k
