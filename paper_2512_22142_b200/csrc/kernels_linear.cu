@@ -27,9 +27,12 @@ namespace cleave {
 __device__ unsigned int g_linear_status;
 static std::atomic<uint64_t> g_linear_wait_limit{2000000000ull};
 
-constexpr uint32_t kLinTile = 128, kLinStages = 3, kLinOperand = 16384, kLinStage = 2 * kLinOperand;
+constexpr uint32_t kLinTile = 128, kLinMaxStages = 5, kLinOperand = 16384, kLinStage = 2 * kLinOperand;
 constexpr uint32_t kLongK = 512;         // products an accumulator takes before its sum moves on, in fp32 results
-constexpr uint32_t kLinThreads = 192, kLinSmem = kLinStages * kLinStage + 1024;
+// Blocks of B that a CTA of linear_split_kernel asks L2 for while the kernel before still runs (16 x 4096 x 4096 right after
+// another: none 13.0, three 12.5, eight 13.0 us).
+constexpr uint32_t kLinAhead = 3;
+constexpr uint32_t kLinThreads = 192, kLinSmem = 112 * 1024;        // two CTAs an SM
 
 // What the write-out needs, the same for every kernel of this file.
 struct Epilogue {
@@ -50,6 +53,10 @@ struct LinearParams {
     Epilogue e;
     uint32_t K_blocks, splits, tiles_n;
     uint32_t a_mn, b_mn, a_rows;    // a_rows: rows of a K-contiguous A that a stage brings
+    // A stage holds B's 16 KB, then A's rows, so few rows leave room for five stages, 128 for three (16 x 4096 x 4096: three
+    // stages 12.5, five 12.3 us; 1 x 11008 x 4096: 23.5, 22.3).  The product reads 128 rows of A; what stands behind those
+    // that were brought only reaches accumulator rows that nobody reads.
+    uint32_t stages, stage_bytes;
     unsigned long long wait_limit_ns;
 };
 
@@ -283,6 +290,10 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const void* tmap, uint
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
                  ::"r"(dst), "l"(tmap), "r"(bar), "r"(c0), "r"(c1) : "memory");
 }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
+__device__ __forceinline__ void tma_prefetch_2d(const void* tmap, int32_t c0, int32_t c1) {
+    asm volatile("cp.async.bulk.prefetch.tensor.2d.L2.global.tile [%0, {%1, %2}];" ::"l"(tmap), "r"(c0), "r"(c1) : "memory");
+}
 template <bool E4M3>
 __device__ __forceinline__ void umma_one(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
     if constexpr (E4M3)
@@ -330,7 +341,7 @@ __device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, const Li
 }
 
 struct __align__(16) LinShared {
-    uint64_t full[kLinStages], empty[kLinStages], acc_full, drain;
+    uint64_t full[kLinMaxStages], empty[kLinMaxStages], acc_full, drain;
     uint32_t tmem_base, abort_flag;
 };
 
@@ -350,12 +361,23 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
     let_dependents_start();
 
     if (threadIdx.x == 0) {
-        for (uint32_t s = 0; s < kLinStages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
+        for (uint32_t s = 0; s < P.stages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
         mbar_init(smem_u32(&sh.acc_full), 1);
         mbar_init(smem_u32(&sh.drain), 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (threadIdx.x == 64) {                              // (a thread of the write-out)
+        prefetch_map(&map_a); prefetch_map(&map_b);
+        if (P.e.form) { prefetch_map(&map_c); if (P.e.z) prefetch_map(&map_z); }
+        // B's first blocks are on their way to L2 (where a later write by the kernel before reaches them) while that
+        // kernel still runs
+        for (uint32_t kb = kb0; kb < min(kb1, kb0 + kLinAhead); ++kb) {
+            const int32_t k = (int32_t)(kb * kBlk);
+            if (P.b_mn) { tma_prefetch_2d(&map_b, (int32_t)n0, k); tma_prefetch_2d(&map_b, (int32_t)n0 + 64, k); }
+            else tma_prefetch_2d(&map_b, k, (int32_t)n0);
+        }
     }
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(kLinTile) : "memory");
@@ -369,16 +391,16 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 
     if (warp == 0 && lane == 0) {
         // ---- producer ----
-        for (uint32_t kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
-            const uint32_t s = it % kLinStages, ph = (it / kLinStages) & 1u;
+        for (uint32_t kb = kb0, s = 0, ph = 0; kb < kb1; ++kb) {
             if (!lin_wait(smem_u32(&sh.empty[s]), ph ^ 1u, W)) break;
-            const uint32_t bar = smem_u32(&sh.full[s]), sa = base + s * kLinStage, sb = sa + kLinOperand;
+            const uint32_t bar = smem_u32(&sh.full[s]), sb = base + s * P.stage_bytes, sa = sb + kLinOperand;
             mbar_arrive_expect_tx(bar, kLinOperand + P.a_rows * 128u);
             const int32_t k = (int32_t)(kb * kBlk);
             if (P.a_mn) { tma_load_2d(sa, &map_a, bar, (int32_t)m0, k); tma_load_2d(sa + kSubBytes, &map_a, bar, (int32_t)m0 + 64, k); }
             else tma_load_2d(sa, &map_a, bar, k, (int32_t)m0);
             if (P.b_mn) { tma_load_2d(sb, &map_b, bar, (int32_t)n0, k); tma_load_2d(sb + kSubBytes, &map_b, bar, (int32_t)n0 + 64, k); }
             else tma_load_2d(sb, &map_b, bar, k, (int32_t)n0);
+            if (++s == P.stages) { s = 0; ph ^= 1u; }
         }
     } else if (warp == 1 && lane == 0) {
         // ---- MMA issuer ----
@@ -386,15 +408,15 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
         const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
         bool ok = true;
-        for (uint32_t kb = kb0, it = 0; kb < kb1; ++kb, ++it) {
-            const uint32_t s = it % kLinStages, ph = (it / kLinStages) & 1u;
+        for (uint32_t kb = kb0, s = 0, ph = 0; kb < kb1; ++kb) {
             if (!lin_wait(smem_u32(&sh.full[s]), ph, W)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t sa = base + s * kLinStage, sb = sa + kLinOperand;
+            const uint32_t sb = base + s * P.stage_bytes, sa = sb + kLinOperand;
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q)              // 32 bytes of K each
-                umma_one<E4M3>(tmem, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, (it | q) != 0u);
+                umma_one<E4M3>(tmem, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, (kb != kb0) | (q != 0u));
             umma_commit_one(smem_u32(&sh.empty[s]));
+            if (++s == P.stages) { s = 0; ph ^= 1u; }
         }
         if (ok) umma_commit_one(smem_u32(&sh.acc_full));
         // everything issued above has completed before tensor memory is released
@@ -856,6 +878,8 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         while (P.splits < 8 && tiles * P.splits * 2 <= 2u * (uint32_t)sms && P.K_blocks / (P.splits * 2) >= 4) P.splits *= 2;
         // (K-contiguous rows of A beyond M need not even be zeros: they only reach accumulator rows that nobody reads)
         P.a_rows = g.transA ? kLinTile : std::min(kLinTile, (g.M + 7) / 8 * 8);
+        P.stage_bytes = kLinOperand + P.a_rows * 128u;
+        P.stages = std::min(kLinMaxStages, (kLinSmem - 1024u - (kLinOperand - P.a_rows * 128u)) / P.stage_bytes);
         rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, P.a_rows, e4m3);
         if (rc || (rc = encode_b(kLinTile))) return rc;
         const SplitKernel kernel = pick_act<PickSplit>(d.act, e4m3, false);

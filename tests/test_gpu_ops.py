@@ -364,6 +364,23 @@ def test_linear_integer_products_are_exact(cl, m, n, k, ta, tb, kind):
     assert np.array_equal(_f64(wide[:, :n]), 2 * (a @ b)) and torch.all(wide[:, n:] == 7.0)
 
 
+@pytest.mark.parametrize("m,n,k", [(2500, 2048, 200), (2560, 2000, 72), (2560, 1930, 1100), (2800, 2304, 136), (75 * 256, 256, 130), (256, 19000, 640)])
+@pytest.mark.parametrize("ta,tb,kind", LAYOUTS)
+def test_linear_last_wave_of_large_products(cl, m, n, k, ta, tb, kind):
+    """Tiles of 256 x 256 that do not divide over the GPU's 74 pairs of SMs: a few left over, many, ragged ones."""
+    rng = np.random.default_rng(m + n + k)
+    A, B, a, b = _operands(rng, m, n, k, ta, tb, kind, 0)
+    want = a @ b
+    for dt in (torch.float32, torch.bfloat16):
+        out = torch.full((m, n), float("nan"), dtype=dt, device=_dev())
+        z = torch.full((m, n), float("nan"), dtype=torch.bfloat16, device=_dev())
+        cl.linear(A, B, out, transA=ta, transB=tb, act="relu", z=z)
+        assert cl.linear_status() == 0
+        rounded = torch.tensor(want).to(_dev())
+        assert torch.equal(z, rounded.to(torch.bfloat16))
+        assert torch.equal(out, rounded.clamp(min=0).to(dt))
+
+
 @pytest.mark.parametrize("act", KINDS)
 @pytest.mark.parametrize("kind,c,side", [("bf16", "bf16", "f32"), ("bf16", "f32", "bf16"), ("e4m3", "bf16", "bf16")])
 @pytest.mark.parametrize("m,n,k", [(1, 72, 256), (200, 300, 320), (130, 129, 70), (16, 2048, 1024), (700, 512, 256), (3, 37993, 72), (130, 19008, 40)])
