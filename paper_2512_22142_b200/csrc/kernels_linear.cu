@@ -8,6 +8,13 @@
 // workspace, a second launch or an order that changes.  Two CTAs share an SM: the write-out of one runs beside the
 // products of the other.
 //
+// linear_pair_kernel: tiles of 256 x 256 on pairs of CTAs, persistent, for large products (its comment below).
+//
+// Bound by: the weights' bytes and the latency of one pass (few rows: 16 x 4096 x 4096 takes 11.8 us after another, its
+// 34 MB 5.2 us at the measured copy rate); the write-out beside the products (8192 x 768 x 3072 with bias, GELU and z: 42 us,
+// products alone 27, the write-out alone 28); the tensor cores under the power cap (8192 x 4096 x 11008 in E4M3 with
+// SwiGLU 305 to 390 us, 11008 x 8192 x 4096 into fp32 560 to 660, with the clock).
+//
 // Operands: K-contiguous or M/N-contiguous bf16 through the descriptors' major bits (no transposed copies), or
 // K-contiguous E4M3 (kind::f8f6f4), 128 bytes of K a stage either way; TMA fills what lies outside a matrix with
 // zeros, and nothing outside C is written.
@@ -507,7 +514,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // ---- large products: pairs of CTAs ---------------------------------------------------------------------
 // linear_pair_kernel: one persistent cluster of two CTAs per pair of SMs.  A tile is 256 rows x BN <= 256 columns; CTA
 // r loads rows 128 r ... of A and columns r BN / 2 ... of B, the leader's MMA thread issues M = 256 products over both
-// CTAs' shared memory (six stages of 32 KB each), and each CTA finds its 128 rows in its own tensor memory, in two
+// CTAs' shared memory (four to six stages of 32 KB each, what the output buffers leave), and each CTA finds its 128 rows in its own tensor memory, in two
 // slots, so the write-out of a tile runs beside the products of the next.  Tiles go to clusters round robin, in bands
 // of eight row tiles so that tiles in flight share operands in L2.
 //
@@ -651,18 +658,20 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
         OutRing out = {dyn_smem + (base - smem_u32(dyn_smem)) + P.stages * kLinStage + (warp - kLpEpiWarp0) * (P.out_bytes * P.out_count), P.out_bytes, P.out_count, 0u};
         if constexpr (!LONG) {
             // parts 0, 1 drain slot 0, parts 2, 3 slot 1 (every second tile of the cluster); the two parts of a slot
-            // take its chunks of 32 columns in turn
-            const uint32_t group = part >> 1, half = part & 1u;
-            const uint32_t empty = mapa_shared(smem_u32(&sh.acc_empty[group]), 0u), taddr = tmem + group * 256u + lane_base;
-            uint32_t use = 0;
-            for (uint32_t t = cluster + group * clusters; t < tiles; t += 2 * clusters, ++use) {
-                const uint2 at = pair_tile(P, t);
-                const uint32_t row0 = at.x * 256u + rank * 128u + quad * 32u, col = at.y * P.bn;
-                if (half) prefetch_strip(P.e.mul, P.e.mul_type, P.e.ldmul, P.e, row0 + lane, col, P.bn);
+            // take its chunks of 32 columns in turn, and all four those of the last tile
+            const uint32_t count = (tiles - cluster + clusters - 1) / clusters;
+            for (uint32_t k = 0; k < count; ++k) {
+                const bool last = k + 1 == count;
+                const uint32_t slot = k & 1u, sharers = last ? 4u : 2u;
+                if (!last && part >> 1 != slot) continue;
+                const uint2 at = pair_tile(P, cluster + k * clusters);
+                const uint32_t empty = mapa_shared(smem_u32(&sh.acc_empty[slot]), 0u), taddr = tmem + slot * 256u + lane_base;
+                const uint32_t row0 = at.x * 256u + rank * 128u + quad * 32u, col = at.y * P.bn, mine = part & (sharers - 1);
+                if (mine & 1u) prefetch_strip(P.e.mul, P.e.mul_type, P.e.ldmul, P.e, row0 + lane, col, P.bn);
                 else prefetch_strip(P.e.res, P.e.res_type, P.e.ldres, P.e, row0 + lane, col, P.bn);
-                const bool ok = write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, row0, col, half * 32u, 64u, P.bn, lane,
+                const bool ok = write_strip<ACT>(P.e, &map_c, &map_z, out, taddr, row0, col, mine * 32u, sharers * 32u, P.bn, lane,
                     [&] {
-                        const bool r = __all_sync(0xFFFFFFFFu, mbar_wait_cl(smem_u32(&sh.acc_full[group]), use & 1u, W));
+                        const bool r = __all_sync(0xFFFFFFFFu, mbar_wait_cl(smem_u32(&sh.acc_full[slot]), (k >> 1) & 1u, W));
                         tc_fence_after();
                         return r;
                     },
@@ -835,7 +844,17 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     cudaError_t err;
     const uint64_t tiles_m = (g.M + kLinTile - 1) / kLinTile, tiles_n = (g.N + kLinTile - 1) / kLinTile, tiles = tiles_m * tiles_n;
     const uint32_t pairs = (uint32_t)sms / 2;
-    if (tiles >= 2u * (uint32_t)sms) {
+    // Results of an fp32 output of a long K move on every kLongK products (linear_pair_kernel)
+    const bool lng = (d.c_type == CLEAVE_T_F32 || d.z_type == CLEAVE_T_F32) && g.K > kLongK;
+    // Pairs of CTAs bring half the operand bytes for a product, one CTA a tile starts and ends sooner and spreads few tiles
+    // wider.  With one row of tiles half of a pair's rows would be empty (16 x 50304 x 2048: 56 us by pairs, 42 by tiles);
+    // from two tiles a place on, pairs win at every K (4096 x 2048: K = 256 10.1 against 12.6 us, K = 4096 51 against 66);
+    // between one tile an SM and two, when the pairs take them in one go, from a K of 32 blocks on (1536 x 2048: K = 1024 10.8
+    // against 11.1 us, 2048 16.1 against 17.7, 4096 26.4 against 30.2; fp32 2048 19.0 against 18.6, 4096 30.8 against 31.0); with
+    // fewer tiles, K is split (1152 x 2048 x 4096: 26.3 against 21.4).
+    const uint64_t pair_tiles = (uint64_t)((g.M + 255) / 256) * ((g.N + 255) / 256);
+    const bool by_pairs = g.M > kLinTile && (tiles >= 2u * (uint32_t)sms || (tiles > (uint32_t)sms && pair_tiles <= pairs && !lng && P.K_blocks >= 32));
+    if (by_pairs) {
         PairParams Q = {};
         Q.e = P.e; Q.K_blocks = P.K_blocks; Q.a_mn = P.a_mn; Q.b_mn = P.b_mn; Q.wait_limit_ns = P.wait_limit_ns;
         Q.tiles_m = (g.M + 255) / 256;
@@ -846,8 +865,9 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         Q.tiles_n = (g.N + Q.bn - 1) / Q.bn;
         Q.b_boxes = (Q.bn / 2 + 63) / 64;
         Q.b_bytes = Q.b_mn ? Q.b_boxes * kSubBytes : Q.bn / 2 * 128u;
-        const bool lng = (d.c_type == CLEAVE_T_F32 || d.z_type == CLEAVE_T_F32) && g.K > kLongK;
         Q.chunk = lng ? kLongK / kblk : Q.K_blocks;
+        // (an M- or N-contiguous operand by one copy a stage instead of two, where its columns are whole groups of 64: 4096^3
+        // 98.8 us against 105.9, 11008 x 4096 x 4096 285 against 308)
         if (Q.a_mn && g.M % 64 == 0) { Q.a_mn = 2; rc = encode_groups(&ma, d.A, g.K, g.M, g.lda); }
         else rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, 128, e4m3);
         if (rc) return rc;
@@ -873,7 +893,8 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         err = cudaLaunchKernelEx(&cfg, kernel, ma, mb, mc, mz, Q);
     } else {
         P.tiles_n = (uint32_t)tiles_n;
-        // K is split while every CTA still finds a place at once (two an SM) and keeps at least four stages of work
+        // K is split while every CTA still finds a place at once (two an SM) and keeps at least four stages of work (16 x 4096 x
+        // 4096: 22.8 us whole, 15.7 in two, 11.5 in four, 11.2 in eight; 512 x 1024 x 1024: 9.6, 9.4, 10.6, 11.0)
         P.splits = 1;
         while (P.splits < 8 && tiles * P.splits * 2 <= 2u * (uint32_t)sms && P.K_blocks / (P.splits * 2) >= 4) P.splits *= 2;
         // (K-contiguous rows of A beyond M need not even be zeros: they only reach accumulator rows that nobody reads)
