@@ -18,4 +18,6 @@ Parity status of each part (what pins it besides itself):
                          rows/columns); optimality "parity unpinned" as above
   numerics.py  pinned  - assembled result == undecomposed GEMM (brute force, triple loop, on
                          tiny shapes; bit-exact on small-integer inputs; numpy float64 matmul)
+  ops.py       pinned  - AdamW, RMSNorm, the product's epilogue and its backward: 64-bit formulas against finite
+                         differences and closed forms; 8-bit AdamW as the exact fp32 definition
 """
