@@ -103,12 +103,12 @@ def _act_code(act: str) -> int:
 
 
 def _workspace(given, nbytes: int, like, stream):
-    """For a launch on another stream than torch's current one: a workspace that the allocator keeps for it."""
+    """For a launch on another stream than torch's current one: a workspace from that stream's own pool.  (A block of the
+    current stream's pool may still be in use by work queued there, which the launch does not wait for.)"""
     if given is not None or stream is None:
         return given
-    ws = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
-    ws.record_stream(torch.cuda.ExternalStream(stream, device=like.device) if isinstance(stream, int) else stream)
-    return ws
+    with torch.cuda.stream(torch.cuda.ExternalStream(stream, device=like.device) if isinstance(stream, int) else stream):
+        return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=like.device)
 
 
 class AdamW:

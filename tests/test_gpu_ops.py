@@ -565,3 +565,35 @@ def test_chained_calls_see_what_the_one_before_wrote(cl, rows, cols, ffn):
         assert torch.isfinite(v.float()).all(), k
         assert torch.equal(v, fast[k]), k
         assert torch.equal(v, replayed[k]), k
+
+
+def test_workspaces_of_calls_on_another_stream_are_not_memory_in_use(cl):
+    """A block of the workspace's size is freed on the current stream while work that reads and writes it is still
+    queued there; calls on another stream that bring no workspace compute as ever, and so does the queued work."""
+    rng = np.random.default_rng(60)
+    rows, cols = 600, 1024
+    h, dy = _rand(rng, (rows, cols), torch.float32), _rand(rng, (rows, cols), torch.float32)
+    rstd = torch.rsqrt(h.square().mean(1) + 1e-5)
+    dx, dw, want_dw = torch.empty_like(h), torch.zeros(cols, device=_dev()), torch.zeros(cols, device=_dev())
+    db, want_db = torch.zeros(cols, device=_dev()), torch.zeros(cols, device=_dev())
+    cl.rmsnorm_backward(dy, h, None, rstd, dx, want_dw)
+    cl.act_backward(dy, None, dbias=want_db)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    big = torch.randn(4096, 4096, device=_dev())
+    for size, call, got, want in (
+            (cl.rmsnorm_backward_workspace(rows, cols), lambda s: cl.rmsnorm_backward(dy, h, None, rstd, dx, dw, stream=s), dw, want_dw),
+            (cl.act_backward_workspace(rows, cols), lambda s: cl.act_backward(dy, None, dbias=db, stream=s), db, want_db)):
+        for stream in (side, side.cuda_stream):
+            got.zero_()
+            torch.cuda.synchronize()
+            for _ in range(3):
+                big @ big                                            # the current stream is busy for a few milliseconds
+            block = torch.full((size // 4,), 3.0, device=_dev())
+            kept = block + 1.0
+            del block                                                # free for the current stream, whose work has not begun
+            call(stream)
+            torch.cuda.synchronize()
+            assert torch.all(kept == 4.0) and torch.equal(got, want)
+    # the workspaces' blocks belong to the launch's stream
+    assert side.cuda_stream in {s["stream"] for s in torch.cuda.memory_snapshot()}

@@ -164,3 +164,40 @@ def test_binding_refuses_what_the_library_cannot_see(ops):
                  lambda: ops.AdamW([], [], [], []), lambda: ops.AdamW([w], [w], [w], [w]), lambda: ops.AdamW([w], [x], [x], [w])):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("raw", [False, True])
+def test_a_workspace_for_another_stream_comes_from_that_streams_pool(ops, monkeypatch, raw):
+    """The allocator hands out blocks in the order of the stream that is current when it is asked: a block for a launch on
+    another stream is asked for with that stream current, or work still pending on the first one may use it too."""
+    import contextlib
+
+    class Stream:
+        cuda_stream = 77
+
+    current, asked = [], []
+
+    @contextlib.contextmanager
+    def stream_context(s):
+        current.append(s)
+        yield
+        current.pop()
+
+    real = torch.empty
+
+    def empty(*size, **kw):
+        asked.append(current[-1].cuda_stream if current else None)
+        t = real(*size, **kw)
+        t.record_stream = lambda s: None
+        return t
+
+    def external(handle, device=None):
+        s = Stream()
+        s.cuda_stream = handle
+        return s
+    monkeypatch.setattr(torch.cuda, "stream", stream_context)
+    monkeypatch.setattr(torch.cuda, "ExternalStream", external)
+    monkeypatch.setattr(torch, "empty", empty)
+    ws = ops._workspace(None, 400, torch.zeros(1), 78 if raw else Stream())
+    assert ws.numel() == 400 and asked == [78 if raw else 77] and not current
+    assert ops._workspace(ws, 400, ws, Stream()) is ws and ops._workspace(None, 400, ws, None) is None and len(asked) == 1
