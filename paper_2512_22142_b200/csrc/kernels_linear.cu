@@ -35,7 +35,9 @@ __device__ unsigned int g_linear_status;
 static std::atomic<uint64_t> g_linear_wait_limit{2000000000ull};
 
 constexpr uint32_t kLinTile = 128, kLinMaxStages = 5, kLinOperand = 16384, kLinStage = 2 * kLinOperand;
-constexpr uint32_t kLongK = 512;         // products an accumulator takes before its sum moves on, in fp32 results
+// Products an accumulator takes before its sum moves on, in fp32 results: the tensor core cuts off when it adds, so one
+// accumulator over K = 8192 is 9.1e-6 off (operands of one sign: 2.5e-5), handed over 4.8e-7 at every K (5e-7).
+constexpr uint32_t kLongK = 512;
 // Blocks of B that a CTA of linear_split_kernel asks L2 for while the kernel before still runs (16 x 4096 x 4096 right after
 // another: none 13.0, three 12.5, eight 13.0 us).
 constexpr uint32_t kLinAhead = 3;
@@ -58,7 +60,7 @@ struct Epilogue {
 
 struct LinearParams {
     Epilogue e;
-    uint32_t K_blocks, splits, tiles_n;
+    uint32_t K_blocks, splits, tiles_n, chunk;   // chunk: K-blocks that an accumulator takes before it is handed over
     uint32_t a_mn, b_mn, a_rows;    // a_rows: rows of a K-contiguous A that a stage brings
     // A stage holds B's 16 KB, then A's rows, so few rows leave room for five stages, 128 for three (16 x 4096 x 4096: three
     // stages 12.5, five 12.3 us; 1 x 11008 x 4096: 23.5, 22.3).  The product reads 128 rows of A; what stands behind those
@@ -331,6 +333,14 @@ __device__ __forceinline__ float ld_dsmem(uint32_t cluster_addr) {
     return v;
 }
 
+__device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]),
+          "=r"(v[8]), "=r"(v[9]), "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr) : "memory");
+}
+
 struct LinWait { volatile uint32_t* abort_flag; uint64_t limit_ns; };
 static __device__ __noinline__ bool lin_wait_slow(uint32_t bar, uint32_t parity, const LinWait& w) {
     const uint64_t t0 = global_timer_ns();
@@ -347,18 +357,36 @@ __device__ __forceinline__ bool lin_wait(uint32_t bar, uint32_t parity, const Li
     return mbar_try_wait(bar, parity) || lin_wait_slow(bar, parity, w);
 }
 
+// the same without a call (a call would have to save the caller's sums)
+__device__ __forceinline__ bool lin_wait_inline(uint32_t bar, uint32_t parity, const LinWait& w) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const uint64_t t0 = global_timer_ns();
+    for (uint32_t spins = 0; !mbar_try_wait(bar, parity); ++spins)
+        if ((spins & 255u) == 0) {
+            if (*w.abort_flag) return false;
+            if (global_timer_ns() - t0 >= w.limit_ns) { *w.abort_flag = 1u; atomicOr(&g_linear_status, STATUS_TIMEOUT); return false; }
+        }
+    return true;
+}
+
 struct __align__(16) LinShared {
-    uint64_t full[kLinMaxStages], empty[kLinMaxStages], acc_full, drain;
+    uint64_t full[kLinMaxStages], empty[kLinMaxStages], acc_full[2], acc_empty[2], drain;
     uint32_t tmem_base, abort_flag;
 };
 
-template <bool E4M3, uint32_t ACT>
+// LONG: the accumulator is handed over every P.chunk K-blocks (see kLongK).  Two of them take turns, 256 columns of tensor
+// memory a CTA (two CTAs share an SM's 512); each of the four write-out warps keeps the sums of its 32 rows in registers,
+// adds a chunk while the next one's products run, and lays the sums into the last accumulator's place at the end.
+// Measured against one accumulator: 16 x 4096 x 11008 21.4 to 20.6 us, 1 x 50304 x 2048 43.7 to 41.1, 768 x 3072 x 8192
+// 41.2 to 39.7.  (Sums 16 columns a load: 24 bytes spilled at the 168 registers that two CTAs an SM leave.)
+template <bool E4M3, bool LONG, uint32_t ACT>
 __global__ void __launch_bounds__(kLinThreads, 2)
 linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ CUtensorMap map_c,
                     const __grid_constant__ CUtensorMap map_z, const __grid_constant__ LinearParams P) {
     extern __shared__ uint8_t dyn_smem[];
     __shared__ LinShared sh;
     constexpr uint32_t kBlk = E4M3 ? 128u : 64u;         // K per stage: 128 bytes
+    constexpr uint32_t kTmem = LONG ? 2 * kLinTile : kLinTile;
     const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31u;
     const uint32_t base = (smem_u32(dyn_smem) + 1023u) & ~1023u;
     const uint32_t rank = blockIdx.x % P.splits, tile = blockIdx.x / P.splits;
@@ -369,7 +397,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < P.stages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
-        mbar_init(smem_u32(&sh.acc_full), 1);
+        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&sh.acc_full[a]), 1); mbar_init(smem_u32(&sh.acc_empty[a]), 4); }
         mbar_init(smem_u32(&sh.drain), 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -387,7 +415,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         }
     }
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(kLinTile) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh.tmem_base)), "r"(kTmem) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
@@ -415,17 +443,24 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
         const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
         bool ok = true;
-        for (uint32_t kb = kb0, s = 0, ph = 0; kb < kb1; ++kb) {
-            if (!lin_wait(smem_u32(&sh.full[s]), ph, W)) { ok = false; break; }
+        const uint32_t chunk = LONG ? P.chunk : kb1 - kb0;
+        uint32_t s = 0, ph = 0, use = 0;                  // stage, its phase, accumulators used so far
+        for (uint32_t k0 = kb0; ok && k0 < kb1; k0 += chunk, ++use) {
+            const uint32_t acc = use & 1u, d = tmem + acc * kLinTile;
+            if (LONG && !lin_wait(smem_u32(&sh.acc_empty[acc]), ((use >> 1) & 1u) ^ 1u, W)) { ok = false; break; }
             tc_fence_after();
-            const uint32_t sb = base + s * P.stage_bytes, sa = sb + kLinOperand;
+            for (uint32_t kb = k0; kb < min(kb1, k0 + chunk); ++kb) {
+                if (!lin_wait(smem_u32(&sh.full[s]), ph, W)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t sb = base + s * P.stage_bytes, sa = sb + kLinOperand;
 #pragma unroll
-            for (uint32_t q = 0; q < 4; ++q)              // 32 bytes of K each
-                umma_one<E4M3>(tmem, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, (kb != kb0) | (q != 0u));
-            umma_commit_one(smem_u32(&sh.empty[s]));
-            if (++s == P.stages) { s = 0; ph ^= 1u; }
+                for (uint32_t q = 0; q < 4; ++q)          // 32 bytes of K each
+                    umma_one<E4M3>(d, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, (kb != k0) | (q != 0u));
+                umma_commit_one(smem_u32(&sh.empty[s]));
+                if (++s == P.stages) { s = 0; ph ^= 1u; }
+            }
+            if (ok) umma_commit_one(smem_u32(&sh.acc_full[acc]));
         }
-        if (ok) umma_commit_one(smem_u32(&sh.acc_full));
         // everything issued above has completed before tensor memory is released
         umma_commit_one(smem_u32(&sh.drain));
         const uint64_t t0 = global_timer_ns();
@@ -447,9 +482,42 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
                 prefetch_strip(P.e.res, P.e.res_type, P.e.ldres, P.e, m0 + quad * 32u + lane, n0 + rank * cols, cols);
             }
         }
-        ok = __all_sync(0xFFFFFFFFu, lin_wait(smem_u32(&sh.acc_full), 0u, W));
-        tc_fence_after();
-        const uint32_t taddr = tmem + ((quad * 32u) << 16);
+        uint32_t taddr = tmem + ((quad * 32u) << 16);
+        if constexpr (LONG) {
+            const bool rows = m0 + quad * 32u < P.e.M;
+            float sum[kLinTile];
+#pragma unroll
+            for (uint32_t i = 0; i < kLinTile; ++i) sum[i] = 0.f;
+            uint32_t use = 0;
+            for (uint32_t k0 = kb0; k0 < kb1; k0 += P.chunk, ++use) {
+                const uint32_t acc = use & 1u, at = taddr + acc * kLinTile;
+                ok = __all_sync(0xFFFFFFFFu, lin_wait_inline(smem_u32(&sh.acc_full[acc]), (use >> 1) & 1u, W));
+                if (!ok) break;
+                tc_fence_after();
+                if (rows) {
+#pragma unroll
+                    for (uint32_t c = 0; c < kLinTile; c += 16) {
+                        uint32_t u[16];
+                        tmem_ld_32x16(at + c, u);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) sum[c + i] += __uint_as_float(u[i]);
+                    }
+                    if (k0 + P.chunk >= kb1) {            // nothing is accumulated here any more
+#pragma unroll
+                        for (uint32_t c = 0; c < kLinTile; c += 32) tmem_st_32x32(at + c, sum + c);
+                        asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh.acc_empty[acc]));
+            }
+            taddr += ((use - 1u) & 1u) * kLinTile;
+        } else {
+            ok = __all_sync(0xFFFFFFFFu, lin_wait(smem_u32(&sh.acc_full[0]), 0u, W));
+            tc_fence_after();
+        }
         if (m0 + quad * 32u >= P.e.M) {
             // (no rows for this warp)
         } else if (ok && P.splits == 1) {
@@ -508,7 +576,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         __syncthreads();
     }
     tc_fence_after();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kLinTile) : "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmem) : "memory");
 }
 
 // ---- large products: pairs of CTAs ---------------------------------------------------------------------
@@ -518,10 +586,8 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // slots, so the write-out of a tile runs beside the products of the next.  Tiles go to clusters round robin, in bands
 // of eight row tiles so that tiles in flight share operands in L2.
 //
-// LONG (fp32 results of a long K): the tensor core adds products to its accumulator with truncation, which after
-// thousands of steps shows in fp32 (relative error 9e-6 at K = 8192, growing with K; a bf16 result hides it).  So the
-// accumulator is handed over every `chunk` K-blocks and the epilogue warps keep the sum in registers with ordinary
-// rounded additions; the two slots take turns by chunk instead of by tile.
+// LONG (fp32 results of a long K, see kLongK): the accumulator is handed over every `chunk` K-blocks and the write-out
+// warps keep the sum in registers with ordinary rounded additions; the two slots take turns by chunk instead of by tile.
 constexpr uint32_t kLpMaxStages = 6, kLpEpiWarp0 = 4, kLpBand = 8;
 // Write-out warps: 16 keep pace with the products of a short K (bias, activation and a second output: 55 -> 50 us at 8192 x 768
 // x 3072 against 8); LONG takes 8, whose threads hold 128 sums each (with 16, what else they need spills: 419 -> 544 us
@@ -793,7 +859,10 @@ struct PickPair {
 };
 struct PickSplit {
     using Kernel = SplitKernel;
-    template <uint32_t ACT> static Kernel get(bool e4m3, bool) { return e4m3 ? linear_split_kernel<true, ACT> : linear_split_kernel<false, ACT>; }
+    template <uint32_t ACT> static Kernel get(bool e4m3, bool lng) {
+        if (e4m3) return lng ? linear_split_kernel<true, true, ACT> : linear_split_kernel<true, false, ACT>;
+        return lng ? linear_split_kernel<false, true, ACT> : linear_split_kernel<false, false, ACT>;
+    }
 };
 template <typename Pick>
 typename Pick::Kernel pick_act(uint32_t act, bool e4m3, bool lng) {
@@ -844,16 +913,16 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     cudaError_t err;
     const uint64_t tiles_m = (g.M + kLinTile - 1) / kLinTile, tiles_n = (g.N + kLinTile - 1) / kLinTile, tiles = tiles_m * tiles_n;
     const uint32_t pairs = (uint32_t)sms / 2;
-    // Results of an fp32 output of a long K move on every kLongK products (linear_pair_kernel)
+    // Results of an fp32 output of a long K move on every kLongK products (both kernels)
     const bool lng = (d.c_type == CLEAVE_T_F32 || d.z_type == CLEAVE_T_F32) && g.K > kLongK;
     // Pairs of CTAs bring half the operand bytes for a product, one CTA a tile starts and ends sooner and spreads few tiles
     // wider.  With one row of tiles half of a pair's rows would be empty (16 x 50304 x 2048: 56 us by pairs, 42 by tiles);
     // from two tiles a place on, pairs win at every K (4096 x 2048: K = 256 10.1 against 12.6 us, K = 4096 51 against 66);
     // between one tile an SM and two, when the pairs take them in one go, from a K of 32 blocks on (1536 x 2048: K = 1024 10.8
-    // against 11.1 us, 2048 16.1 against 17.7, 4096 26.4 against 30.2; fp32 2048 19.0 against 18.6, 4096 30.8 against 31.0); with
-    // fewer tiles, K is split (1152 x 2048 x 4096: 26.3 against 21.4).
+    // against 11.1 us, 2048 16.1 against 17.7, 4096 26.4 against 30.2; fp32 weight gradients 2048 20.8 against 22.0,
+    // 4096 33 against 37); with fewer tiles, K is split (1152 x 2048 x 4096: 26.3 against 21.4).
     const uint64_t pair_tiles = (uint64_t)((g.M + 255) / 256) * ((g.N + 255) / 256);
-    const bool by_pairs = g.M > kLinTile && (tiles >= 2u * (uint32_t)sms || (tiles > (uint32_t)sms && pair_tiles <= pairs && !lng && P.K_blocks >= 32));
+    const bool by_pairs = g.M > kLinTile && (tiles >= 2u * (uint32_t)sms || (tiles > (uint32_t)sms && pair_tiles <= pairs && P.K_blocks >= 32));
     if (by_pairs) {
         PairParams Q = {};
         Q.e = P.e; Q.K_blocks = P.K_blocks; Q.a_mn = P.a_mn; Q.b_mn = P.b_mn; Q.wait_limit_ns = P.wait_limit_ns;
@@ -903,9 +972,11 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         P.stages = std::min(kLinMaxStages, (kLinSmem - 1024u - (kLinOperand - P.a_rows * 128u)) / P.stage_bytes);
         rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, P.a_rows, e4m3);
         if (rc || (rc = encode_b(kLinTile))) return rc;
-        const SplitKernel kernel = pick_act<PickSplit>(d.act, e4m3, false);
-        static SmemLimit limit[2 * kActs];
-        if (limit[(e4m3 ? 1 : 0) * kActs + d.act].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
+        P.chunk = kLongK / kblk;
+        const bool hand_over = lng && (P.K_blocks + P.splits - 1) / P.splits > P.chunk;      // (the cluster's sum is a rounded one)
+        const SplitKernel kernel = pick_act<PickSplit>(d.act, e4m3, hand_over);
+        static SmemLimit limit[4 * kActs];
+        if (limit[((e4m3 ? 2 : 0) + (hand_over ? 1 : 0)) * kActs + d.act].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }
         cfg.gridDim = dim3((unsigned)(tiles * P.splits));
         cfg.blockDim = dim3(kLinThreads);
         cfg.dynamicSmemBytes = kLinSmem;

@@ -423,6 +423,47 @@ def test_linear_nan_and_infinity_stay_in_their_rows_and_columns(cl):
         assert not np.isfinite(g[rows][:, 11]).any()
 
 
+# split form with 1, 2 and 4 CTAs a tile and with one row of tiles, pairs of CTAs
+LONG_K = [(2048, 1280, 1900), (2048, 1280, 8192), (1100, 1500, 16384), (700, 900, 16400), (128, 20480, 8192), (1, 19200, 9000), (600, 1030, 4700), (4096, 2560, 8192)]
+
+
+@pytest.mark.parametrize("m,n,k", LONG_K)
+@pytest.mark.parametrize("ta,tb,kind", [(False, False, "bf16"), (True, False, "bf16"), (False, True, "e4m3")])
+def test_linear_fp32_results_of_a_long_k_keep_their_accuracy(cl, m, n, k, ta, tb, kind):
+    """Operands of one sign, so that what the tensor core cuts off adds up.  It adds 16 (E4M3: 32) products a step and may cut
+    off a unit (2^-23) of the running sum; an accumulator takes 512 products, 32 steps, whose running sums are half of the last
+    one on average: 17 units of 2^-23.  The chunks' sums are rounded: half a unit of the running sum each, again half on
+    average, and a few more in the cluster's sum.  (One accumulator over 8192 products: 9e-6, about three times the bound.)"""
+    gen = torch.Generator(device=_dev()).manual_seed(m + n + k)
+    dt = torch.float8_e4m3fn if kind == "e4m3" else torch.bfloat16
+
+    def store(rows, cols):
+        return (torch.rand(rows, -(-cols // 16) * 16, generator=gen, device=_dev()) + 0.5).to(dt)[:, :cols]
+    A, B = store(k, m) if ta else store(m, k), store(n, k) if tb else store(k, n)
+    a, b = (A.double().t() if ta else A.double()), (B.double().t() if tb else B.double())
+    want = a @ b
+    bound = 17 * 2.0 ** -23 + (k / 512 / 2 + 8) * 2.0 ** -24
+    out, z = torch.full((m, n), float("nan"), device=_dev()), torch.full((m, n), float("nan"), device=_dev())
+    cl.linear(A, B, out, transA=ta, transB=tb)
+    assert cl.linear_status() == 0
+    assert float((out.double() / want - 1).abs().max()) <= bound
+    narrow = torch.empty(m, n, dtype=torch.bfloat16, device=_dev())
+    cl.linear(A, B, narrow, transA=ta, transB=tb, act="relu", z=z)        # an fp32 z alone asks for it too
+    assert torch.equal(z, out) and torch.equal(narrow, out.to(torch.bfloat16))
+
+
+@pytest.mark.parametrize("m,n,k", [(300, 700, 5000), (1900, 1300, 1100), (1900, 1300, 4100), (1, 8, 4200), (129, 1, 9000), (100, 19100, 513), (1100, 1500, 3333)])
+@pytest.mark.parametrize("ta,tb,kind", LAYOUTS)
+def test_linear_handed_over_sums_are_whole(cl, m, n, k, ta, tb, kind):
+    """Integers, exact in fp32: no chunk of K is lost or taken twice, whatever the number of chunks."""
+    rng = np.random.default_rng(m + n + k)
+    A, B, a, b = _operands(rng, m, n, k, ta, tb, kind, 0)
+    out = torch.full((m, n + 4), 7.0, device=_dev())
+    cl.linear(A, B, out[:, :n], transA=ta, transB=tb)
+    assert cl.linear_status() == 0
+    assert np.array_equal(_f64(out[:, :n]), a @ b) and torch.all(out[:, n:] == 7.0)
+
+
 def test_linear_extreme_preactivations(cl):
     """Activations far out on either side: their limits, no NaN."""
     n = 64
@@ -472,6 +513,12 @@ def test_a_wait_that_runs_out_ends_the_product_in_order(cl, m, n, k):
     cl.linear(A, B, out)
     assert cl.linear_status() == 0
     assert np.array_equal(_f64(out), a @ b)
+
+
+@pytest.mark.parametrize("m,n,k", [(16, 512, 16384), (1900, 1300, 4096)])
+def test_a_wait_that_runs_out_while_sums_are_handed_over(cl, m, n, k):
+    """The same with accumulators that take turns (fp32 results of a long K)."""
+    test_a_wait_that_runs_out_ends_the_product_in_order(cl, m, n, k)
 
 
 # ---- the epilogue's backward ------------------------------------------------------------------------------------
