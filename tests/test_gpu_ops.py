@@ -381,6 +381,25 @@ def test_linear_last_wave_of_large_products(cl, m, n, k, ta, tb, kind):
         assert torch.equal(out, rounded.clamp(min=0).to(dt))
 
 
+@pytest.mark.parametrize("m,n,k", [(10000, 200, 2050), (19100, 130, 72), (38000, 40, 130), (38000, 96, 640), (38000, 8, 64), (19000, 225, 1030)])
+@pytest.mark.parametrize("ta,tb,kind", LAYOUTS)
+def test_linear_by_pairs_with_narrow_tiles(cl, m, n, k, ta, tb, kind):
+    """Products of many rows and fewer than 256 columns: a pair's tile is as wide as C (in steps of 32 columns)."""
+    rng = np.random.default_rng(m + n + k)
+    A, B, a, b = _operands(rng, m, n, k, ta, tb, kind, 0)
+    want = torch.tensor(a @ b).to(_dev())
+    for dt in (torch.float32, torch.bfloat16):
+        out = torch.full((m, n + 3), 7.0, dtype=dt, device=_dev())
+        z = torch.full((m, n), float("nan"), dtype=torch.bfloat16, device=_dev())
+        cl.linear(A, B, out[:, :n], transA=ta, transB=tb, act="relu", z=z)
+        whole = torch.full((m, n), float("nan"), dtype=dt, device=_dev())
+        cl.linear(A, B, whole, transA=ta, transB=tb, act="relu")
+        assert cl.linear_status() == 0
+        assert torch.equal(z, want.to(torch.bfloat16))
+        assert torch.equal(whole, want.clamp(min=0).to(dt))
+        assert torch.equal(out[:, :n], whole) and torch.all(out[:, n:] == 7.0)
+
+
 @pytest.mark.parametrize("act", KINDS)
 @pytest.mark.parametrize("kind,c,side", [("bf16", "bf16", "f32"), ("bf16", "f32", "bf16"), ("e4m3", "bf16", "bf16")])
 @pytest.mark.parametrize("m,n,k", [(1, 72, 256), (200, 300, 320), (130, 129, 70), (16, 2048, 1024), (700, 512, 256), (3, 37993, 72), (130, 19008, 40)])
