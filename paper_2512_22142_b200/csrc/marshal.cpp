@@ -36,18 +36,20 @@ const at::Tensor& tensor(PyObject* o, const char* name) {
     if (!THPVariable_Check(o)) refuse(name, "a tensor is wanted");
     return THPVariable_Unpack(o);
 }
-uint32_t checked_type(const at::Tensor& t, const char* name, unsigned types) {
+// `like`: the call's leading operand, on whose device the launch goes
+uint32_t checked_type(const at::Tensor& t, const char* name, unsigned types, const at::Tensor& like) {
     const uint32_t kind = type_of(t);
     if (!kind || !(types >> kind & 1u) || !t.is_cuda()) refuse(name, "a GPU tensor of a supported type is wanted");
+    if (t.device() != like.device()) refuse(name, "the operands are on different devices");
     return kind;
 }
 
 struct Matrix { uint32_t type = 0; void* p = nullptr; uint64_t ld = 0; };
-Matrix matrix(PyObject* o, const char* name, int64_t rows, int64_t cols, unsigned types, bool optional = false) {
+Matrix matrix(PyObject* o, const char* name, const at::Tensor& like, int64_t rows, int64_t cols, unsigned types, bool optional = false) {
     Matrix m;
     if (optional && o == Py_None) return m;
     const at::Tensor& t = tensor(o, name);
-    m.type = checked_type(t, name, types);
+    m.type = checked_type(t, name, types, like);
     if (t.dim() != 2 || t.size(0) != rows || t.size(1) != cols) {
         PyErr_Format(PyExc_ValueError, "%s: shape (%lld, %lld) is wanted", name, (long long)rows, (long long)cols);
         throw Refused{};
@@ -61,11 +63,11 @@ Matrix matrix(PyObject* o, const char* name, int64_t rows, int64_t cols, unsigne
     return m;
 }
 struct Vector { uint32_t type = 0; void* p = nullptr; };
-Vector vector(PyObject* o, const char* name, int64_t n, unsigned types) {
+Vector vector(PyObject* o, const char* name, const at::Tensor& like, int64_t n, unsigned types) {
     Vector v;
     if (o == Py_None) return v;
     const at::Tensor& t = tensor(o, name);
-    v.type = checked_type(t, name, types);
+    v.type = checked_type(t, name, types, like);
     if (t.dim() != 1 || t.size(0) != n || (n > 1 && t.stride(0) != 1)) {
         PyErr_Format(PyExc_ValueError, "%s: a contiguous tensor of %lld elements is wanted", name, (long long)n);
         throw Refused{};
@@ -93,8 +95,8 @@ void* workspace(PyObject* o, uint64_t bytes, const at::Tensor& like, at::Tensor&
         return hold.data_ptr();
     }
     const at::Tensor& t = tensor(o, "workspace");
-    if (!t.is_cuda() || !t.is_contiguous() || (uint64_t)t.nbytes() < bytes) {
-        PyErr_Format(PyExc_ValueError, "workspace: %llu contiguous bytes on the GPU are wanted", (unsigned long long)bytes);
+    if (!t.is_cuda() || t.device() != like.device() || !t.is_contiguous() || (uint64_t)t.nbytes() < bytes) {
+        PyErr_Format(PyExc_ValueError, "workspace: %llu contiguous bytes on the operands' GPU are wanted", (unsigned long long)bytes);
         throw Refused{};
     }
     return t.data_ptr();
@@ -103,9 +105,9 @@ void* workspace(PyObject* o, uint64_t bytes, const at::Tensor& like, at::Tensor&
 PyObject* run_rmsnorm(PyObject* const* a) {                // x, weight, y, residual, h, rstd, scale, eps, stream
     const at::Tensor& x = leading(a[0], "x");
     const int64_t rows = x.size(0), cols = x.size(1);
-    const Matrix mx = matrix(a[0], "x", rows, cols, kFloats), my = matrix(a[2], "y", rows, cols, kFloats | kE4M3);
-    const Matrix mr = matrix(a[3], "residual", rows, cols, kFloats, true), mh = matrix(a[4], "h", rows, cols, kFloats, true);
-    const Vector w = vector(a[1], "weight", cols, kFloats);
+    const Matrix mx = matrix(a[0], "x", x, rows, cols, kFloats), my = matrix(a[2], "y", x, rows, cols, kFloats | kE4M3);
+    const Matrix mr = matrix(a[3], "residual", x, rows, cols, kFloats, true), mh = matrix(a[4], "h", x, rows, cols, kFloats, true);
+    const Vector w = vector(a[1], "weight", x, cols, kFloats);
     if (mh.p && mr.type && mh.type != mr.type) refuse("h", "the residual's type is wanted");
     cleave_rmsnorm_t d = {};
     d.rows = (uint64_t)rows; d.cols = (uint32_t)cols;
@@ -113,8 +115,8 @@ PyObject* run_rmsnorm(PyObject* const* a) {                // x, weight, y, resi
     d.eps = (float)PyFloat_AsDouble(a[7]);
     if (PyErr_Occurred()) throw Refused{};
     d.x = mx.p; d.ldx = mx.ld; d.r = mr.p; d.ldr = mr.ld; d.h = mh.p; d.ldh = mh.ld; d.w = w.p; d.y = my.p; d.ldy = my.ld;
-    d.rstd = static_cast<float*>(vector(a[5], "rstd", rows, kF32).p);
-    d.scale = static_cast<float*>(vector(a[6], "scale", rows, kF32).p);
+    d.rstd = static_cast<float*>(vector(a[5], "rstd", x, rows, kF32).p);
+    d.scale = static_cast<float*>(vector(a[6], "scale", x, rows, kF32).p);
     const c10::cuda::CUDAGuard guard(x.device());
     return PyLong_FromLong(cleave_rmsnorm(&d, stream_of(a[8], x)));
 }
@@ -122,27 +124,27 @@ PyObject* run_rmsnorm(PyObject* const* a) {                // x, weight, y, resi
 PyObject* run_rmsnorm_backward(PyObject* const* a) {       // dy, h, weight, rstd, dx, dweight, dres, workspace, stream
     const at::Tensor& h = leading(a[1], "h");
     const int64_t rows = h.size(0), cols = h.size(1);
-    const Matrix mh = matrix(a[1], "h", rows, cols, kFloats), mdy = matrix(a[0], "dy", rows, cols, kFloats);
-    const Matrix mdx = matrix(a[4], "dx", rows, cols, 1u << mh.type), mr = matrix(a[6], "dres", rows, cols, 1u << mh.type, true);
-    const Vector w = vector(a[2], "weight", cols, kFloats);
+    const Matrix mh = matrix(a[1], "h", h, rows, cols, kFloats), mdy = matrix(a[0], "dy", h, rows, cols, kFloats);
+    const Matrix mdx = matrix(a[4], "dx", h, rows, cols, 1u << mh.type), mr = matrix(a[6], "dres", h, rows, cols, 1u << mh.type, true);
+    const Vector w = vector(a[2], "weight", h, cols, kFloats);
     cleave_rmsnorm_backward_t d = {};
     d.rows = (uint64_t)rows; d.cols = (uint32_t)cols;
     d.dy_type = mdy.type; d.h_type = mh.type; d.w_type = w.type;
     d.dy = mdy.p; d.lddy = mdy.ld; d.h = mh.p; d.ldh = mh.ld; d.w = w.p; d.dres = mr.p; d.lddres = mr.ld; d.dx = mdx.p; d.lddx = mdx.ld;
-    d.rstd = static_cast<const float*>(vector(a[3], "rstd", rows, kF32).p);
-    d.dw = static_cast<float*>(vector(a[5], "dweight", cols, kF32).p);
-    const c10::cuda::CUDAGuard guard(h.device());
+    d.rstd = static_cast<const float*>(vector(a[3], "rstd", h, rows, kF32).p);
+    d.dw = static_cast<float*>(vector(a[5], "dweight", h, cols, kF32).p);
     at::Tensor hold;
     void* ws = d.dw ? workspace(a[7], cleave_rmsnorm_backward_workspace(d.rows, d.cols), h, hold) : nullptr;
+    const c10::cuda::CUDAGuard guard(h.device());
     return PyLong_FromLong(cleave_rmsnorm_backward(&d, ws, stream_of(a[8], h)));
 }
 
 PyObject* run_quantize_rows(PyObject* const* a) {          // x, y, scale, stream
     const at::Tensor& x = leading(a[0], "x");
     const int64_t rows = x.size(0), cols = x.size(1);
-    const Matrix mx = matrix(a[0], "x", rows, cols, kFloats), my = matrix(a[1], "y", rows, cols, kE4M3);
+    const Matrix mx = matrix(a[0], "x", x, rows, cols, kFloats), my = matrix(a[1], "y", x, rows, cols, kE4M3);
     if (a[2] == Py_None) refuse("scale", "a tensor is wanted");
-    float* scale = static_cast<float*>(vector(a[2], "scale", rows, kF32).p);
+    float* scale = static_cast<float*>(vector(a[2], "scale", x, rows, kF32).p);
     const c10::cuda::CUDAGuard guard(x.device());
     return PyLong_FromLong(cleave_quantize_rows(mx.p, mx.type, (uint64_t)rows, (uint32_t)cols, mx.ld, my.p, my.ld, scale, stream_of(a[3], x)));
 }
@@ -153,10 +155,10 @@ PyObject* run_linear(PyObject* const* a) {
     const int ta = PyObject_IsTrue(a[3]), tb = PyObject_IsTrue(a[4]);
     if (ta < 0 || tb < 0) throw Refused{};
     const int64_t M = A.size(ta ? 1 : 0), K = A.size(ta ? 0 : 1), N = B.size(tb ? 0 : 1);
-    const Matrix ma = matrix(a[0], "A", A.size(0), A.size(1), kBf16 | kE4M3), mb = matrix(a[1], "B", tb ? N : K, tb ? K : N, 1u << ma.type);
-    const Matrix mc = matrix(a[2], "out", M, N, kFloats), mz = matrix(a[9], "z", M, N, kFloats, true), mm = matrix(a[10], "mul", M, N, kFloats, true),
-                 mr = matrix(a[11], "residual", M, N, kFloats, true);
-    const Vector bias = vector(a[7], "bias", N, kFloats);
+    const Matrix ma = matrix(a[0], "A", A, A.size(0), A.size(1), kBf16 | kE4M3), mb = matrix(a[1], "B", A, tb ? N : K, tb ? K : N, 1u << ma.type);
+    const Matrix mc = matrix(a[2], "out", A, M, N, kFloats), mz = matrix(a[9], "z", A, M, N, kFloats, true), mm = matrix(a[10], "mul", A, M, N, kFloats, true),
+                 mr = matrix(a[11], "residual", A, M, N, kFloats, true);
+    const Vector bias = vector(a[7], "bias", A, N, kFloats);
     const uint64_t unit = ma.type == CLEAVE_T_E4M3 ? 16 : 8;
     auto ld = [&](const Matrix& m, const at::Tensor& t) -> uint32_t {
         const uint64_t l = t.size(0) == 1 ? (m.ld + unit - 1) / unit * unit : m.ld;          // a single row has no second one
@@ -170,8 +172,8 @@ PyObject* run_linear(PyObject* const* a) {
     d.act = (uint32_t)PyLong_AsUnsignedLong(a[8]);
     if (PyErr_Occurred()) throw Refused{};
     d.A = ma.p; d.B = mb.p; d.bias = bias.p;
-    d.scale_a = static_cast<const float*>(vector(a[5], "scale_a", M, kF32).p);
-    d.scale_b = static_cast<const float*>(vector(a[6], "scale_b", N, kF32).p);
+    d.scale_a = static_cast<const float*>(vector(a[5], "scale_a", A, M, kF32).p);
+    d.scale_b = static_cast<const float*>(vector(a[6], "scale_b", A, N, kF32).p);
     d.z = mz.p; d.ldz = mz.ld; d.mul = mm.p; d.ldmul = mm.ld; d.res = mr.p; d.ldres = mr.ld; d.C = mc.p; d.ldc = mc.ld;
     const c10::cuda::CUDAGuard guard(A.device());
     return PyLong_FromLong(cleave_linear(&d, stream_of(a[12], A)));
@@ -181,18 +183,18 @@ PyObject* run_linear(PyObject* const* a) {
 PyObject* run_act_backward(PyObject* const* a) {
     const at::Tensor& dy = leading(a[0], "dy");
     const int64_t rows = dy.size(0), cols = dy.size(1);
-    const Matrix mdy = matrix(a[0], "dy", rows, cols, kFloats), mz = matrix(a[1], "z", rows, cols, kFloats, true), mdz = matrix(a[2], "dz", rows, cols, kFloats, true),
-                 mm = matrix(a[4], "mul", rows, cols, kFloats, true), mdm = matrix(a[5], "dmul", rows, cols, kFloats, true);
+    const Matrix mdy = matrix(a[0], "dy", dy, rows, cols, kFloats), mz = matrix(a[1], "z", dy, rows, cols, kFloats, true), mdz = matrix(a[2], "dz", dy, rows, cols, kFloats, true),
+                 mm = matrix(a[4], "mul", dy, rows, cols, kFloats, true), mdm = matrix(a[5], "dmul", dy, rows, cols, kFloats, true);
     cleave_act_backward_t d = {};
     d.rows = (uint64_t)rows; d.cols = (uint32_t)cols;
     d.act = (uint32_t)PyLong_AsUnsignedLong(a[3]);
     if (PyErr_Occurred()) throw Refused{};
     d.dy_type = mdy.type; d.z_type = mz.type; d.mul_type = mm.type; d.dz_type = mdz.type; d.dmul_type = mdm.type;
     d.dy = mdy.p; d.lddy = mdy.ld; d.z = mz.p; d.ldz = mz.ld; d.mul = mm.p; d.ldmul = mm.ld; d.dz = mdz.p; d.lddz = mdz.ld; d.dmul = mdm.p; d.lddmul = mdm.ld;
-    d.dbias = static_cast<float*>(vector(a[6], "dbias", cols, kF32).p);
-    const c10::cuda::CUDAGuard guard(dy.device());
+    d.dbias = static_cast<float*>(vector(a[6], "dbias", dy, cols, kF32).p);
     at::Tensor hold;
     void* ws = d.dbias ? workspace(a[7], cleave_act_backward_workspace(d.rows, d.cols), dy, hold) : nullptr;
+    const c10::cuda::CUDAGuard guard(dy.device());
     return PyLong_FromLong(cleave_act_backward(&d, ws, stream_of(a[8], dy)));
 }
 

@@ -201,3 +201,36 @@ def test_a_workspace_for_another_stream_comes_from_that_streams_pool(ops, monkey
     ws = ops._workspace(None, 400, torch.zeros(1), 78 if raw else Stream())
     assert ws.numel() == 400 and asked == [78 if raw else 77] and not current
     assert ops._workspace(ws, 400, ws, Stream()) is ws and ops._workspace(None, 400, ws, None) is None and len(asked) == 1
+
+
+def test_binding_refuses_operands_of_different_devices(ops):
+    """Tensors without memory that say they are on one GPU or another: the refusal comes before anything else."""
+    from torch._subclasses.fake_tensor import FakeTensorMode
+
+    def at(device, *size, dtype=torch.float32):
+        with FakeTensorMode():
+            return torch.empty(*size, dtype=dtype, device=device)
+    here, there = (lambda *s, **k: at("cuda:0", *s, **k)), (lambda *s, **k: at("cuda:1", *s, **k))
+    x, w, v = here(8, 8), here(8), here(8)
+    code, bf = here(8, 8, dtype=torch.float8_e4m3fn), here(8, 8, dtype=torch.bfloat16)
+    far, fv, fbf = there(8, 8), there(8), there(8, 8, dtype=torch.bfloat16)
+    ws, fws = here(1 << 16, dtype=torch.uint8), there(1 << 16, dtype=torch.uint8)
+    for call in (lambda: ops.rmsnorm(x, fv, x, stream=1), lambda: ops.rmsnorm(x, w, far, stream=1), lambda: ops.rmsnorm(x, w, x, residual=far, stream=1),
+                 lambda: ops.rmsnorm(x, w, x, residual=x, h=far, stream=1), lambda: ops.rmsnorm(x, w, x, rstd=fv, stream=1),
+                 lambda: ops.rmsnorm(x, w, code, scale=fv, stream=1), lambda: ops.quantize_rows(far, code, v, stream=1),
+                 lambda: ops.quantize_rows(x, code, fv, stream=1), lambda: ops.rmsnorm_backward(far, x, w, v, x, stream=1),
+                 lambda: ops.rmsnorm_backward(x, x, w, fv, x, stream=1), lambda: ops.rmsnorm_backward(x, x, w, v, far, stream=1),
+                 lambda: ops.rmsnorm_backward(x, x, w, v, x, fv, workspace=ws, stream=1), lambda: ops.rmsnorm_backward(x, x, w, v, x, dres=far, stream=1),
+                 lambda: ops.linear(bf, fbf, x, stream=1), lambda: ops.linear(bf, bf, far, stream=1), lambda: ops.linear(bf, bf, x, bias=fv, stream=1),
+                 lambda: ops.linear(bf, bf, x, scale_a=fv, stream=1), lambda: ops.linear(bf, bf, x, scale_b=fv, stream=1),
+                 lambda: ops.linear(bf, bf, x, z=far, stream=1), lambda: ops.linear(bf, bf, x, mul=far, stream=1),
+                 lambda: ops.linear(bf, bf, x, residual=far, stream=1), lambda: ops.act_backward(x, far, x, act="relu", stream=1),
+                 lambda: ops.act_backward(x, x, far, act="relu", stream=1), lambda: ops.act_backward(x, x, x, act="relu", mul=far, stream=1),
+                 lambda: ops.act_backward(x, x, x, act="relu", dmul=far, stream=1),
+                 lambda: ops.act_backward(x, x, x, act="relu", dbias=fv, workspace=ws, stream=1)):
+        with pytest.raises(ValueError, match="different devices"):
+            call()
+    for call in (lambda: ops.act_backward(x, x, x, act="relu", dbias=v, workspace=fws, stream=1),
+                 lambda: ops.rmsnorm_backward(x, x, w, v, x, v, workspace=fws, stream=1)):
+        with pytest.raises(ValueError, match="operands' GPU"):
+            call()
