@@ -134,7 +134,7 @@ PyObject* run_rmsnorm_backward(PyObject* const* a) {       // dy, h, weight, rst
     d.rstd = static_cast<const float*>(vector(a[3], "rstd", h, rows, kF32).p);
     d.dw = static_cast<float*>(vector(a[5], "dweight", h, cols, kF32).p);
     at::Tensor hold;
-    void* ws = d.dw ? workspace(a[7], cleave_rmsnorm_backward_workspace(d.rows, d.cols), h, hold) : nullptr;
+    void* ws = a[5] != Py_None ? workspace(a[7], cleave_rmsnorm_backward_workspace(d.rows, d.cols), h, hold) : nullptr;
     const c10::cuda::CUDAGuard guard(h.device());
     return PyLong_FromLong(cleave_rmsnorm_backward(&d, ws, stream_of(a[8], h)));
 }
@@ -193,7 +193,7 @@ PyObject* run_act_backward(PyObject* const* a) {
     d.dy = mdy.p; d.lddy = mdy.ld; d.z = mz.p; d.ldz = mz.ld; d.mul = mm.p; d.ldmul = mm.ld; d.dz = mdz.p; d.lddz = mdz.ld; d.dmul = mdm.p; d.lddmul = mdm.ld;
     d.dbias = static_cast<float*>(vector(a[6], "dbias", dy, cols, kF32).p);
     at::Tensor hold;
-    void* ws = d.dbias ? workspace(a[7], cleave_act_backward_workspace(d.rows, d.cols), dy, hold) : nullptr;
+    void* ws = a[6] != Py_None ? workspace(a[7], cleave_act_backward_workspace(d.rows, d.cols), dy, hold) : nullptr;
     const c10::cuda::CUDAGuard guard(dy.device());
     return PyLong_FromLong(cleave_act_backward(&d, ws, stream_of(a[8], dy)));
 }
