@@ -163,6 +163,13 @@ class AdamW:
             _check(lib.cleave_adamw_create(table, n, state, grad, C.byref(h)), "cleave_adamw_create")
         self._h = h
 
+    def _call(self, fn, arg, stream) -> int:
+        """A library call with the handle's device current (its table lives there)."""
+        if torch.cuda.current_device() == self._device:
+            return fn(self._h, arg, _raw_stream(stream, self._device))
+        with torch.cuda.device(self._device):
+            return fn(self._h, arg, _raw_stream(stream, self._device))
+
     def set_grads(self, grads, stream=None) -> None:
         """Other gradient tensors (same type and sizes) from the next step on."""
         if len(grads) != self._n:
@@ -171,7 +178,7 @@ class AdamW:
             if not g.is_cuda or g.device != p.device or _TYPE.get(g.dtype, 0) != self._grad or g.numel() != p.numel() or not g.is_contiguous():
                 _bad(f"grads[{i}]: a contiguous GPU tensor of the same type and size as before is wanted")
         ptrs = (_vp * self._n)(*[g.data_ptr() for g in grads])
-        _check(lib.cleave_adamw_set_grads(self._h, ptrs, _raw_stream(stream, self._device)), "cleave_adamw_set_grads")
+        _check(self._call(lib.cleave_adamw_set_grads, ptrs, stream), "cleave_adamw_set_grads")
         self._keep = (self._keep[0], list(grads)) + self._keep[2:]
 
     def step(self, *, step: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, grad_scale: float = 1.0,
@@ -181,7 +188,7 @@ class AdamW:
             _bad("step counts from 1")
         s = self._step
         s.lr, s.beta1, s.beta2, s.eps, s.grad_scale, s.step, s.seed = lr, beta1, beta2, eps, grad_scale, step, seed & 0xFFFFFFFFFFFFFFFF
-        code = lib.cleave_adamw_step(self._h, C.byref(s), _raw_stream(stream, self._device))
+        code = self._call(lib.cleave_adamw_step, C.byref(s), stream)
         if code:
             _check(code, "cleave_adamw_step")
 

@@ -234,3 +234,43 @@ def test_binding_refuses_operands_of_different_devices(ops):
                  lambda: ops.rmsnorm_backward(x, x, w, v, x, v, workspace=fws, stream=1)):
         with pytest.raises(ValueError, match="operands' GPU"):
             call()
+
+
+def _bare_optimizer(ops, monkeypatch, device, calls, during=lambda: None):
+    """An AdamW of `device` without memory or library behind it; every library call is noted with its current device."""
+    import contextlib
+    from types import SimpleNamespace
+    current = [0]
+
+    @contextlib.contextmanager
+    def on(d):
+        current.append(d)
+        yield
+        current.pop()
+
+    def step(h, s, stream):
+        during()
+        r = s._obj
+        calls.append(("step", current[-1], stream, r.lr, r.step, r.seed))
+        return 0
+
+    def set_grads(h, ptrs, stream):
+        calls.append(("set_grads", current[-1], stream))
+        return 0
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[-1])
+    monkeypatch.setattr(torch.cuda, "device", on)
+    monkeypatch.setattr(ops, "lib", SimpleNamespace(cleave_adamw_step=step, cleave_adamw_set_grads=set_grads, cleave_adamw_destroy=lambda h: None))
+    opt = object.__new__(ops.AdamW)
+    opt.__dict__.update(_h=0, _n=0, _grad=2, _device=device, _keep=([], [], [], [], []))
+    opt._step = ops._AdamwStep()
+    return opt
+
+
+def test_adamw_steps_on_its_own_device(ops, monkeypatch):
+    """Like every other operator: whatever device is the current one."""
+    for device in (0, 1):
+        calls = []
+        opt = _bare_optimizer(ops, monkeypatch, device, calls)
+        opt.step(step=3, lr=0.5, seed=9, stream=5)
+        opt.set_grads([], stream=5)
+        assert calls == [("step", device, 5, 0.5, 3, 9), ("set_grads", device, 5)]
