@@ -156,7 +156,6 @@ class AdamW:
             r.weight_decay = float(decay[i])
         self._keep = (list(params), list(grads), list(m), list(v), lists)
         self._n, self._grad = n, grad
-        self._step = _AdamwStep()
         self._device = device.index
         h = _vp()
         with torch.cuda.device(device):
@@ -186,8 +185,7 @@ class AdamW:
         """One update; `step` counts from 1.  `seed` feeds the stochastic rounding of 8-bit states."""
         if step < 1:
             _bad("step counts from 1")
-        s = self._step
-        s.lr, s.beta1, s.beta2, s.eps, s.grad_scale, s.step, s.seed = lr, beta1, beta2, eps, grad_scale, step, seed & 0xFFFFFFFFFFFFFFFF
+        s = _AdamwStep(lr, beta1, beta2, eps, grad_scale, step, seed & 0xFFFFFFFFFFFFFFFF)
         code = self._call(lib.cleave_adamw_step, C.byref(s), stream)
         if code:
             _check(code, "cleave_adamw_step")

@@ -262,7 +262,6 @@ def _bare_optimizer(ops, monkeypatch, device, calls, during=lambda: None):
     monkeypatch.setattr(ops, "lib", SimpleNamespace(cleave_adamw_step=step, cleave_adamw_set_grads=set_grads, cleave_adamw_destroy=lambda h: None))
     opt = object.__new__(ops.AdamW)
     opt.__dict__.update(_h=0, _n=0, _grad=2, _device=device, _keep=([], [], [], [], []))
-    opt._step = ops._AdamwStep()
     return opt
 
 
@@ -274,3 +273,19 @@ def test_adamw_steps_on_its_own_device(ops, monkeypatch):
         opt.step(step=3, lr=0.5, seed=9, stream=5)
         opt.set_grads([], stream=5)
         assert calls == [("step", device, 5, 0.5, 3, 9), ("set_grads", device, 5)]
+
+
+def test_adamw_steps_from_two_threads_keep_their_arguments(ops, monkeypatch):
+    """A library call releases the interpreter: another thread's step of the same optimizer may begin while it runs."""
+    import threading
+    calls, inner = [], []
+
+    def during():
+        if not inner:                          # inside the first call, another thread steps
+            t = threading.Thread(target=lambda: opt.step(step=8, lr=0.25, seed=2, stream=6))
+            inner.append(t)
+            t.start()
+            t.join()
+    opt = _bare_optimizer(ops, monkeypatch, 0, calls, during)
+    opt.step(step=7, lr=0.5, seed=1, stream=5)
+    assert sorted(calls) == [("step", 0, 5, 0.5, 7, 1), ("step", 0, 6, 0.25, 8, 2)]
