@@ -330,7 +330,8 @@ CLEAVE_API void cleave_destroy(cleave_plan_t* p);
  *   - Matrices are row-major with a leading dimension in elements (ld >= columns).  Element types
  *     are CLEAVE_T_*; "type 0" means the operand is absent (and its pointer NULL).
  *   - A pointer is aligned to its element size at least; 16-byte aligned bases with rows that are a
- *     multiple of 16 bytes apart take the wide loads.  Any number of columns is accepted.
+ *     multiple of 16 bytes apart take the wide loads.  Any number of rows and columns up to 2^31 - 1 is
+ *     accepted.
  *   - Inputs and outputs may be the same buffer where a call says so, and must not overlap otherwise.
  *   - Zero rows are accepted and compute nothing (sums over rows become 0).
  *   - All sums, statistics and states are held in fp32; a narrower output is rounded once, to nearest

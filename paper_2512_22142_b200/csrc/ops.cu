@@ -19,7 +19,7 @@ struct cleave_adamw_s {
 
 namespace {
 
-constexpr uint64_t kMaxRows = 0x7FFFFFFFull, kMaxLd = 1ull << 40;
+constexpr uint64_t kMaxRows = 0x7FFFFFFFull, kMaxCols = 0x7FFFFFFFull, kMaxLd = 1ull << 40;     // (the kernels count columns in 32 bits)
 
 bool float_type(uint32_t t) { return t == CLEAVE_T_BF16 || t == CLEAVE_T_F32; }
 bool aligned(const void* p, uint64_t bytes) { return ((uintptr_t)p % bytes) == 0; }
@@ -158,7 +158,7 @@ void cleave_adamw_destroy(cleave_adamw_t* h) {
 int cleave_rmsnorm(const cleave_rmsnorm_t* d, void* stream) {
     if (!d || !d->cols || !(d->eps >= 0.f)) return CLEAVE_E_INVAL;
     if (d->rows == 0) return CLEAVE_OK;
-    if (d->rows > kMaxRows) return CLEAVE_E_UNSUPPORTED;
+    if (d->rows > kMaxRows || d->cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
     if (!float_type(d->x_type) || !matrix_ok(d->x, d->x_type, d->ldx, d->cols)) return CLEAVE_E_INVAL;
     if (!optional_ok(d->r, d->r_type, d->ldr, d->cols) || !optional_ok(d->w, d->w_type, d->cols, d->cols)) return CLEAVE_E_INVAL;
     if (d->h && (!d->r || !matrix_ok(d->h, d->r_type, d->ldh, d->cols))) return CLEAVE_E_INVAL;
@@ -172,7 +172,7 @@ int cleave_quantize_rows(const void* x, uint32_t x_type, uint64_t rows, uint32_t
                          float* scale, void* stream) {
     if (!cols) return CLEAVE_E_INVAL;
     if (rows == 0) return CLEAVE_OK;
-    if (rows > kMaxRows) return CLEAVE_E_UNSUPPORTED;
+    if (rows > kMaxRows || cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
     if (!float_type(x_type) || !matrix_ok(x, x_type, ldx, cols) || !matrix_ok(y, CLEAVE_T_E4M3, ldy, cols) || !scale || !aligned(scale, 4)) return CLEAVE_E_INVAL;
     cleave_rmsnorm_t d = {};
     d.rows = rows; d.cols = cols; d.x_type = x_type; d.y_type = CLEAVE_T_E4M3;
@@ -186,7 +186,7 @@ uint64_t cleave_rmsnorm_backward_workspace(uint64_t rows, uint32_t cols) {
 }
 int cleave_rmsnorm_backward(const cleave_rmsnorm_backward_t* d, void* workspace, void* stream) {
     if (!d || !d->cols || !aligned(d->dw, 4)) return CLEAVE_E_INVAL;
-    if (d->rows > kMaxRows) return CLEAVE_E_UNSUPPORTED;
+    if (d->rows > kMaxRows || d->cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
     if (d->rows) {
         if (!float_type(d->dy_type) || !float_type(d->h_type) || !matrix_ok(d->dy, d->dy_type, d->lddy, d->cols) ||
             !matrix_ok(d->h, d->h_type, d->ldh, d->cols) || !matrix_ok(d->dx, d->h_type, d->lddx, d->cols)) return CLEAVE_E_INVAL;
@@ -224,7 +224,7 @@ uint64_t cleave_act_backward_workspace(uint64_t rows, uint32_t cols) {
 }
 int cleave_act_backward(const cleave_act_backward_t* d, void* workspace, void* stream) {
     if (!d || !d->cols || d->act > CLEAVE_ACT_SILU || !aligned(d->dbias, 4)) return CLEAVE_E_INVAL;
-    if (d->rows > kMaxRows) return CLEAVE_E_UNSUPPORTED;
+    if (d->rows > kMaxRows || d->cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
     if (d->rows) {
         if (!float_type(d->dy_type) || !matrix_ok(d->dy, d->dy_type, d->lddy, d->cols)) return CLEAVE_E_INVAL;
         if (!optional_ok(d->z, d->z_type, d->ldz, d->cols) || !optional_ok(d->mul, d->mul_type, d->ldmul, d->cols) ||

@@ -289,3 +289,13 @@ def test_adamw_steps_from_two_threads_keep_their_arguments(ops, monkeypatch):
     opt = _bare_optimizer(ops, monkeypatch, 0, calls, during)
     opt.step(step=7, lr=0.5, seed=1, stream=5)
     assert sorted(calls) == [("step", 0, 5, 0.5, 7, 1), ("step", 0, 6, 0.25, 8, 2)]
+
+
+@pytest.mark.parametrize("cols", [1 << 31, (1 << 32) - 200, (1 << 32) - 1])
+def test_columns_beyond_31_bits_are_refused(ops, cols):
+    """The kernels count columns in 32 bits, in steps of a CTA's threads."""
+    ld = 1 << 33
+    _refused(_norm(ops, cols=cols, ldx=ld, ldy=ld), UNSUPPORTED)
+    _refused(_norm_bwd(ops, cols=cols, lddy=ld, ldh=ld, lddx=ld), UNSUPPORTED)
+    _refused(_act(ops, cols=cols, lddy=ld, ldz=ld, lddz=ld), UNSUPPORTED)
+    _refused(ops.lib.cleave_quantize_rows(4096, 1, 4, cols, ld, 8192, ld, 4096, None), UNSUPPORTED)
