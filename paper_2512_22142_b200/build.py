@@ -34,7 +34,19 @@ def is_stale() -> bool:
     return any(os.path.getmtime(d) > t for d in deps)
 
 
+def _marshal_torch() -> str:
+    """Path of the note of the torch version that the marshalling was built against (it binds torch's ABI)."""
+    return MARSHAL_PATH + ".torch"
+
+
 def _marshal_is_stale() -> bool:
+    import torch
+    try:
+        with open(_marshal_torch()) as f:
+            if f.read() != torch.__version__:
+                return True
+    except OSError:
+        return True
     deps = [MARSHAL_SOURCE, os.path.join(ROOT, "include", "cleave.h")]
     return not os.path.exists(MARSHAL_PATH) or any(os.path.getmtime(d) > os.path.getmtime(MARSHAL_PATH) for d in deps)
 
@@ -52,6 +64,8 @@ def _build_marshal() -> None:
     res = subprocess.run(cmd, capture_output=True, text=True)
     if res.returncode != 0:
         raise RuntimeError("g++ failed:\n" + res.stdout + res.stderr)
+    with open(_marshal_torch(), "w") as f:
+        f.write(torch.__version__)
 
 
 def build_library(force: bool = False, verbose: bool = False) -> str:

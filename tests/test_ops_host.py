@@ -299,3 +299,19 @@ def test_columns_beyond_31_bits_are_refused(ops, cols):
     _refused(_norm_bwd(ops, cols=cols, lddy=ld, ldh=ld, lddx=ld), UNSUPPORTED)
     _refused(_act(ops, cols=cols, lddy=ld, ldz=ld, lddz=ld), UNSUPPORTED)
     _refused(ops.lib.cleave_quantize_rows(4096, 1, 4, cols, ld, 8192, ld, 4096, None), UNSUPPORTED)
+
+
+def test_marshalling_is_rebuilt_for_another_torch(monkeypatch, tmp_path):
+    """The extension is bound to torch's binary interface: one built against another version is stale, whatever its date."""
+    from paper_2512_22142_b200 import build
+    path = tmp_path / "_marshal.so"
+    monkeypatch.setattr(build, "MARSHAL_PATH", str(path))
+    assert build._marshal_is_stale()
+    path.write_text("")
+    os.utime(path, (2 ** 31, 2 ** 31))
+    stamp = tmp_path / "_marshal.so.torch"
+    assert build._marshal_is_stale()
+    stamp.write_text(torch.__version__)
+    assert not build._marshal_is_stale()
+    stamp.write_text("2.0.0")
+    assert build._marshal_is_stale()
