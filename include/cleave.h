@@ -345,7 +345,9 @@ CLEAVE_API void cleave_destroy(cleave_plan_t* p);
 #define CLEAVE_T_F32  2u
 #define CLEAVE_T_E4M3 3u      /* 8-bit float: 4 exponent bits, 3 mantissa bits, largest value 448, no infinity */
 
-/* Activations: z; max(z, 0); z Phi(z); z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; z / (1 + exp(-z)) */
+/* Activations: z; max(z, 0); z Phi(z); z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; z / (1 + exp(-z)).  The last three
+ * are evaluated in fp32 with relative errors of at most 16 (1 + z^2), 8 + 4 |2 sqrt(2/pi) (z + 0.044715 z^3)| and
+ * 8 + 3 |z| times 2^-24, on the negative side too, down to where the result is no longer a normal fp32 number. */
 #define CLEAVE_ACT_NONE      0u
 #define CLEAVE_ACT_RELU      1u
 #define CLEAVE_ACT_GELU      2u

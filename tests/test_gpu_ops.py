@@ -499,6 +499,41 @@ def test_linear_extreme_preactivations(cl):
         assert torch.allclose(dz, (bias > 0).float().expand(3, n), rtol=1e-6, atol=1e-6), act
 
 
+def _activation64(z, act):
+    """Value, slope, and the size of the slope's terms, in 64 bits without cancellation on the negative side."""
+    if act == "gelu":
+        phi, bell = 0.5 * torch.special.erfc(-z * 0.5 ** 0.5), torch.exp(-0.5 * z * z) * (0.5 / np.pi) ** 0.5
+        return z * phi, phi + z * bell, phi + z.abs() * bell
+    u, du = (z, torch.ones_like(z)) if act == "silu" else (2 * (2 / np.pi) ** 0.5 * (z + 0.044715 * z ** 3), 2 * (2 / np.pi) ** 0.5 * (1 + 3 * 0.044715 * z * z))
+    g, rest = torch.special.expit(u), torch.special.expit(-u)
+    return z * g, g + z * g * rest * du, g + (z * g * rest * du).abs()
+
+
+@pytest.mark.parametrize("act,low,units", [("gelu", -12.5, lambda z: 16 * (1 + z * z)), ("silu", -80.0, lambda z: 8 + 3 * z.abs()),
+                                           ("gelu_tanh", -9.0, lambda z: 8 + 4 * 2 * (2 / np.pi) ** 0.5 * (z.abs() + 0.044715 * z.abs() ** 3))])
+def test_activations_keep_their_digits_on_the_negative_side(cl, act, low, units):
+    """Errors relative to the value itself, in fp32, for arguments put in through the bias.  GELU: the exponent -z^2 / 2 log2(e) takes
+    two roundings and its constant's, which makes z^2 times 1.25 units; the polynomial (8.4e-8), its eight steps, the reciprocal
+    (2 units, its effect at most doubled by the polynomial's slope) and the exponential (4 units) the rest.  The other
+    two: gate = 1 / (1 + exp(-u)), u with at most four roundings of its own size, then exponential, sum and reciprocal."""
+    n = 20000
+    z = torch.cat([torch.linspace(low, 12.0, n - 200), -torch.logspace(-20, 0, 100), torch.logspace(-20, 0, 100)]).to(_dev())
+    A, B = torch.zeros(2, 8, dtype=torch.bfloat16, device=_dev()), torch.zeros(8, n, dtype=torch.bfloat16, device=_dev())
+    out = torch.empty(2, n, device=_dev())
+    cl.linear(A, B, out, bias=z, act=act)
+    value, slope, size = _activation64(z.double(), act)
+    bound = units(z.double()) * U
+    assert torch.all((out[1].double() - value).abs() <= (bound + U) * value.abs())
+    for cols in (n, n - 1):                                   # the wide form and the one for any size
+        zz, one = z[:cols].expand(2, cols).contiguous(), torch.ones(2, cols, device=_dev())
+        dz, dmul = torch.empty_like(zz), torch.empty_like(zz)
+        cl.act_backward(one, zz, dz, act=act, dmul=dmul)
+        assert torch.all((dmul[1].double() - value[:cols]).abs() <= (bound + U)[:cols] * value[:cols].abs())
+        # (1 - gate keeps only its absolute digits where the gate is close to 1, on the positive side: a unit of the factor)
+        extra = 0 if act == "gelu" else 4 * U * (z[:cols].double().clamp_min(0) * (1 if act == "silu" else 2.0 + 0.3 * z[:cols].double() ** 2))
+        assert torch.all((dz[1].double() - slope[:cols]).abs() <= (2 * bound + 4 * U)[:cols] * size[:cols] + extra)
+
+
 def test_linear_repeats_its_bits_on_any_stream(cl):
     rng = np.random.default_rng(41)
     A, B, a, b = _operands(rng, 16, 1024, 4096, False, False, "bf16", 0, integer=False)
