@@ -18,7 +18,7 @@ constexpr uint32_t kActWarps = 8;
 // (the wide form's), so that a CTA's warps stream over many rows and the sums are joined once.
 uint32_t act_backward_parts(uint64_t rows, uint32_t cols) {
     const uint64_t tiles = (cols + 255) / 256, most = (rows + 2 * kActWarps - 1) / (2 * kActWarps);
-    const uint64_t bands = tiles < 444 ? 444 / tiles : 1;
+    const uint64_t bands = tiles < 3 * kPartSms ? 3 * kPartSms / tiles : 1;
     return (uint32_t)(bands < most ? bands : most);
 }
 

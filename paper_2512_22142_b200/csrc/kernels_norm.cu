@@ -502,7 +502,7 @@ uint32_t backward_ctas(uint32_t cols) {
     return threads <= 256 ? std::min(16u, 768u / std::max(threads, 32u)) : (threads <= 320 ? 2u : 1u);
 }
 uint32_t rmsnorm_backward_parts(uint64_t rows, uint32_t cols) {
-    return (uint32_t)std::min<uint64_t>(rows, 148ull * backward_ctas(cols));
+    return (uint32_t)std::min<uint64_t>(rows, (uint64_t)kPartSms * backward_ctas(cols));
 }
 
 __global__ void __launch_bounds__(kRowThreads) rmsnorm_backward_any_kernel(const __grid_constant__ cleave_rmsnorm_backward_t d, float* __restrict__ ws) {
@@ -674,9 +674,8 @@ cudaError_t launch_backward_types(const cleave_rmsnorm_backward_t& d, float* ws,
     return launch_backward_wide<D, H, 2, 1024, 1>(d, ws, threads, parts, stage, st);
 }
 
-cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, int sms, cudaStream_t st) {
+cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, cudaStream_t st) {
     if (!d.cols) return cudaSuccess;
-    (void)sms;
     const uint32_t parts = rmsnorm_backward_parts(d.rows, d.cols);
     const uint64_t stage = (uint64_t)d.cols * (type_bytes(d.dy_type) + type_bytes(d.h_type) * (d.dres ? 2u : 1u));
     const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && stage <= kRingMost && rows_wide(d.dy, d.lddy, d.dy_type) && rows_wide(d.h, d.ldh, d.h_type) &&

@@ -139,7 +139,6 @@ int cleave_adamw_step(cleave_adamw_t* h, const cleave_adamw_step_t* s, void* str
     k.step_size = (float)(s->lr / (1.0 - std::pow(s->beta1, (double)s->step)));
     k.root = (float)(1.0 / std::sqrt(1.0 - std::pow(s->beta2, (double)s->step)));
     k.eps = (float)s->eps; k.grad_scale = (float)s->grad_scale;
-    k.ordinary = k.root >= 1.f && k.root <= 0x1p+20f && k.eps <= 0x1p+60f;
     k.lr = s->lr;
     k.base = s->seed + (s->step << 32);
     return cuda_code(launch_adamw(h->tensors, h->chunks, h->n_chunks, h->chunk_blocks, k, h->state_type == CLEAVE_T_E4M3, h->g_type == CLEAVE_T_BF16,
@@ -194,7 +193,7 @@ int cleave_rmsnorm_backward(const cleave_rmsnorm_backward_t* d, void* workspace,
         if (!d->rstd || !aligned(d->rstd, 4) || (d->dw && (!workspace || !aligned(workspace, 16)))) return CLEAVE_E_INVAL;
     }
     const int sms = need_device();
-    return sms < 0 ? sms : cuda_code(launch_rmsnorm_backward(*d, static_cast<float*>(workspace), sms, static_cast<cudaStream_t>(stream)));
+    return sms < 0 ? sms : cuda_code(launch_rmsnorm_backward(*d, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
 }
 
 // ---- product and its epilogue's backward -------------------------------------------------------------------

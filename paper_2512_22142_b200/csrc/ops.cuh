@@ -280,7 +280,6 @@ struct AdamTensor {                 // device record of one tensor
 struct AdamStep {
     float beta1, omb1, beta2, omb2; // omb = 1 - beta, formed in 64 bits
     float step_size, root, eps, grad_scale;
-    uint32_t ordinary;              // root and eps are such that no quotient's divisor leaves the ordinary range
     double lr;
     uint64_t base;                  // seed + (step << 32)
 };
@@ -291,8 +290,11 @@ cudaError_t launch_adamw(const AdamTensor* tensors, const AdamChunk* chunks, uin
 
 // ---- norm, rows in 8 bits, epilogue backward ---------------------------------------------------------
 cudaError_t launch_rmsnorm(const cleave_rmsnorm_t& d, bool norm, int sms, cudaStream_t st);   // sms: the device's SM count
-uint32_t rmsnorm_backward_parts(uint64_t rows, uint32_t cols);          // rows of partial sums in the workspace
-cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, int sms, cudaStream_t st);
+// Rows of partial sums in the workspace: as many as keep kPartSms SMs busy.  A constant, a B200's number of SMs, because the
+// workspace queries ask no device; on another number of SMs the sums only spread a little worse.
+constexpr uint32_t kPartSms = 148;
+uint32_t rmsnorm_backward_parts(uint64_t rows, uint32_t cols);
+cudaError_t launch_rmsnorm_backward(const cleave_rmsnorm_backward_t& d, float* ws, cudaStream_t st);
 uint32_t act_backward_parts(uint64_t rows, uint32_t cols);
 cudaError_t launch_act_backward(const cleave_act_backward_t& d, float* ws, cudaStream_t st);
 cudaError_t launch_sum_parts(const float* ws, uint32_t parts, uint32_t cols, float* out, cudaStream_t st);
