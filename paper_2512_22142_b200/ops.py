@@ -118,7 +118,7 @@ class AdamW:
     grads    bf16 or fp32 tensors (one type), read at every step; set_grads gives others
     m, v     states, updated in place: fp32 tensors, or float8_e4m3fn codes with m_scales, v_scales (fp32, one per
              256 elements); all zero at the beginning
-    copies   bf16 tensors that receive the rounded weights, or None
+    copies   bf16 tensors that receive the rounded weights, or None (for all, or in a tensor's place)
     weight_decay   one number, or one per tensor
     Every tensor is contiguous."""
 
@@ -127,6 +127,9 @@ class AdamW:
         n = len(params)
         if n == 0 or len(grads) != n or len(m) != n or len(v) != n:
             _bad("params, grads, m and v: one of each per tensor is wanted")
+        for name, tensors in (("params", params), ("grads", grads), ("m", m), ("v", v), ("m_scales", m_scales or ()), ("v_scales", v_scales or ())):
+            if any(t is None for t in tensors):
+                _bad(f"{name}: a tensor in every place is wanted")
         state, grad = _TYPE.get(m[0].dtype, 0), _TYPE.get(grads[0].dtype, 0)
         if state not in (T_F32, T_E4M3) or grad not in (T_BF16, T_F32):
             _bad("states are float32 or float8_e4m3fn, gradients float32 or bfloat16")
@@ -150,7 +153,7 @@ class AdamW:
                     _bad(f"{name}[{i}]: a contiguous GPU tensor of {count} elements of the common type is wanted")
             r = table[i]
             r.numel, r.p, r.g, r.m, r.v = size, params[i].data_ptr(), grads[i].data_ptr(), m[i].data_ptr(), v[i].data_ptr()
-            r.w = copies[i].data_ptr() if copies is not None else None
+            r.w = copies[i].data_ptr() if copies is not None and copies[i] is not None else None
             r.m_scale = m_scales[i].data_ptr() if m_scales is not None and size else None
             r.v_scale = v_scales[i].data_ptr() if v_scales is not None and size else None
             r.weight_decay = float(decay[i])

@@ -209,6 +209,17 @@ def test_adamw_other_gradients_other_stream_and_refusals(cl):
     cl.AdamW([empty], [empty], [empty], [empty]).step(step=1, lr=1.0)            # nothing to do
 
 
+def test_adamw_tensors_without_a_copy(cl):
+    rng = np.random.default_rng(13)
+    s = _adam_state(rng, [700, 300], False, torch.float32, True)
+    opt = cl.AdamW(s["p"], s["g"], s["m"], s["v"], copies=[None, s["w"][1]])
+    hyper = dict(lr=1e-2, beta1=0.9, beta2=0.95, eps=1e-6)
+    before = _clone(s)
+    opt.step(step=1, **hyper)
+    _check_step(before, s, [0.0, 0.0], False, False, hyper, 1, 0)
+    assert torch.all(s["w"][0] == 0) and torch.equal(s["w"][1], s["p"][1].to(torch.bfloat16))
+
+
 # ---- norm -----------------------------------------------------------------------------------------------
 NORM_SIZES = [(1, 1), (3, 7), (5, 8), (1, 4096), (33, 771), (4, 5120), (2, 16384), (2, 20001), (300, 64), (7, 1000), (2, 32768)]
 

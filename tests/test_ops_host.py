@@ -315,3 +315,32 @@ def test_marshalling_is_rebuilt_for_another_torch(monkeypatch, tmp_path):
     assert not build._marshal_is_stale()
     stamp.write_text("2.0.0")
     assert build._marshal_is_stale()
+
+
+def test_adamw_tensors_that_are_missing(ops, monkeypatch):
+    """A tensor may go without a copy (None in its place); everything else is wanted for each tensor, and said so."""
+    from types import SimpleNamespace
+
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode():
+        f, code = (lambda n: torch.empty(n, device="cuda:0")), (lambda n: torch.empty(n, dtype=torch.float8_e4m3fn, device="cuda:0"))
+        p, q, w = f(300), f(5), torch.empty(5, dtype=torch.bfloat16, device="cuda:0")
+        made = []
+
+        def create(table, n, state, grad, h):
+            made.append([(r.numel, r.w) for r in table])
+            return -1
+        monkeypatch.setattr(ops, "lib", SimpleNamespace(cleave_adamw_create=create, cleave_strerror=lambda c: b"", cleave_adamw_destroy=lambda h: None))
+        import contextlib
+        monkeypatch.setattr(torch.cuda, "device", lambda d: contextlib.nullcontext())
+        import paper_2512_22142_b200 as cl
+        with pytest.raises(cl.CleaveError):
+            ops.AdamW([p, q], [p, q], [p, q], [p, q], copies=[None, w])
+        assert [n for n, _ in made[0]] == [300, 5] and made[0][0][1] is None
+        for bad in (lambda: ops.AdamW([p, None], [p, q], [p, q], [p, q]), lambda: ops.AdamW([p, q], [p, None], [p, q], [p, q]),
+                    lambda: ops.AdamW([p, q], [p, q], [p, None], [p, q]), lambda: ops.AdamW([p, q], [p, q], [p, q], [None, q]),
+                    lambda: ops.AdamW([None], [p], [p], [p]), lambda: ops.AdamW([p], [None], [p], [p]), lambda: ops.AdamW([p], [p], [None], [p]),
+                    lambda: ops.AdamW([p], [p], [code(300)], [code(300)], m_scales=[None], v_scales=[f(2)])):
+            with pytest.raises(ValueError):
+                bad()
+        assert len(made) == 1
