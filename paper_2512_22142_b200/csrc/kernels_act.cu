@@ -5,14 +5,23 @@
 // wide form the operands' next rows are on their way to shared memory while a row is used -- each thread copies and
 // reads its own groups only, so there is no barrier, and the bytes in flight do not cost registers.  The bias
 // gradient stays in registers over the band's rows, the CTA's warps are joined in shared memory, and a band's sums
-// are one row of the workspace, added in order by sum_parts_kernel.
+// are one row of the workspace, added in order by sum_parts_kernel.  Few rows (join_rows) make at most eight bands, a
+// cluster, whose sums are added in order through distributed shared memory: one launch.
 // Measured: 8192 x 3072 with GELU and the bias gradient 28 us (5.4 TB/s; the gate's arithmetic issues in 75 % of the
 // cycles), 8192 x 11008 with SwiGLU's two gradients 153 us (5.9 TB/s of 6.5).
+#include <algorithm>
+
 #include "ops.cuh"
+#include "ptx.cuh"
 
 namespace cleave {
 
 constexpr uint32_t kActWarps = 8;
+constexpr uint32_t kJoinBands = 8;
+// Rows up to which the bands are one cluster.  A call is a launch shorter (plain column sums of 656 x 237 5.7 against 7.5 us,
+// 1024 x 3072 6.7 against 7.5); beyond, eight bands are too few CTAs (2048 x 3072: 10.5 against 8.2), sooner so where an
+// activation is computed (kernels alone, with GELU: 256 x 768 3.8 against 3.7, 512 x 768 5.0 against 3.8).
+inline uint64_t join_rows(uint32_t act) { return act == CLEAVE_ACT_NONE ? 1024 : 256; }
 
 // Rows of partial bias gradients: one per band of rows.  As many bands as give each SM three CTAs of 256 columns
 // (the wide form's), so that a CTA's warps stream over many rows and the sums are joined once.
@@ -22,9 +31,10 @@ uint32_t act_backward_parts(uint64_t rows, uint32_t cols) {
     return (uint32_t)(bands < most ? bands : most);
 }
 
-// Column sums of a CTA's warps, joined in warp order into the band's row of the workspace.
+// Column sums of a CTA's warps, joined in warp order into the band's row of `out`; `joined`: the bands of these columns
+// are one cluster, and `out` receives their sum in band order.
 template <int U>
-__device__ __forceinline__ void join_sums(const float (&sum)[U], float (*s)[32 * U], float* __restrict__ ws, uint64_t cols) {
+__device__ __forceinline__ void join_sums(const float (&sum)[U], float (*s)[32 * U], float* __restrict__ out, uint64_t cols, bool joined) {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
 #pragma unroll
     for (int u = 0; u < U; ++u) s[warp][u * 32 + lane] = sum[u];
@@ -36,8 +46,24 @@ __device__ __forceinline__ void join_sums(const float (&sum)[U], float (*s)[32 *
         float t = s[0][at];
 #pragma unroll
         for (int w = 1; w < (int)kActWarps; ++w) t += s[w][at];
-        ws[(uint64_t)blockIdx.y * cols + col] = t;
+        if (joined) s[0][at] = t;
+        else out[(uint64_t)blockIdx.y * cols + col] = t;
     }
+    if (!joined) return;
+    cluster_arrive_wait();
+    const uint32_t first = (uint32_t)__cvta_generic_to_shared(&s[0][0]);
+    for (uint32_t c = blockIdx.y + gridDim.y * threadIdx.x; c < 32u * U; c += gridDim.y * 32 * kActWarps) {        // (rank in the cluster: blockIdx.y)
+        const uint32_t at = first + ((c % U) * 32u + c / U) * 4u;
+        const uint64_t col = (uint64_t)blockIdx.x * 32u * U + c;
+        if (col >= cols) continue;
+        float x[kJoinBands], t = 0.f;
+#pragma unroll
+        for (uint32_t b = 0; b < kJoinBands; ++b) x[b] = b < gridDim.y ? ld_dsmem(mapa_shared(at, b)) : 0.f;
+#pragma unroll
+        for (uint32_t b = 0; b < kJoinBands; ++b) if (b < gridDim.y) t += x[b];
+        out[col] = t;
+    }
+    cluster_arrive_wait();                                  // no CTA leaves while another reads its sums
 }
 // dz and dmul of one element (rounded one by one: the sums' bits do not depend on which outputs are wanted)
 template <uint32_t ACT, bool MUL>
@@ -56,7 +82,7 @@ __device__ __forceinline__ Band this_band(uint64_t rows) {
 
 // Any size, stride and alignment: a lane's column, four rows asked for at a time.
 template <uint32_t ACT, bool MUL>
-__global__ void __launch_bounds__(32 * kActWarps) act_backward_any_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
+__global__ void __launch_bounds__(32 * kActWarps) act_backward_any_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ sums, uint32_t joined) {
     __shared__ float s[kActWarps][32];
     begin_chained();
     constexpr int ROWS = 4;
@@ -85,13 +111,13 @@ __global__ void __launch_bounds__(32 * kActWarps) act_backward_any_kernel(const 
                 if (d.dz) store_as(d.dz, d.dz_type, i * d.lddz + j, dz);
             }
         }
-    if (d.dbias) join_sums<1>(sum, s, ws, d.cols);
+    if (d.dbias) join_sums<1>(sum, s, sums, d.cols, joined != 0);
 }
 
 // Rows of whole 16-byte groups: a lane's 8 columns; STAGES rows of each operand on their way to shared memory.
 // D: type of dy; T: the one type of z, mul, dz and dmul.
 template <typename D, typename T, uint32_t ACT, bool MUL, int STAGES>
-__global__ void __launch_bounds__(32 * kActWarps, 3) act_backward_wide_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ ws) {
+__global__ void __launch_bounds__(32 * kActWarps, 3) act_backward_wide_kernel(const __grid_constant__ cleave_act_backward_t d, float* __restrict__ sums, uint32_t joined) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float s[kActWarps][32 * 8];
     begin_chained();
@@ -149,11 +175,12 @@ __global__ void __launch_bounds__(32 * kActWarps, 3) act_backward_wide_kernel(co
             }
         }
     }
-    if (d.dbias) join_sums<8>(sum, s, ws, d.cols);
+    if (d.dbias) join_sums<8>(sum, s, sums, d.cols, joined != 0);
 }
 
+struct Sums { float* out; uint32_t bands, joined; };       // where the bands' sums go; joined: the bands are one cluster
 template <typename D, typename T, uint32_t ACT, bool MUL>
-cudaError_t launch_act_wide(const cleave_act_backward_t& d, float* ws, uint32_t parts, cudaStream_t st) {
+cudaError_t launch_act_wide(const cleave_act_backward_t& d, const Sums& b, cudaStream_t st) {
     // 32 to 60 KB a CTA: three or four CTAs an SM
     constexpr uint32_t stage = 32 * (sizeof(D) * 8 + (MUL ? 2 : 1) * sizeof(T) * 8);
     constexpr int STAGES = stage >= 2560 ? 3 : 4;
@@ -162,23 +189,25 @@ cudaError_t launch_act_wide(const cleave_act_backward_t& d, float* ws, uint32_t 
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), smem);
     if (e != cudaSuccess) return e;
-    return launch_chained(kernel, dim3((d.cols + 255) / 256, parts), 32 * kActWarps, smem, st, d, ws);
+    return launch_chained_clusters(kernel, dim3(1, b.joined ? b.bands : 1), dim3((d.cols + 255) / 256, b.bands), 32 * kActWarps, smem, st, d, b.out, b.joined);
 }
 template <uint32_t ACT, bool MUL>
-cudaError_t launch_act(const cleave_act_backward_t& d, float* ws, uint32_t parts, bool wide, uint32_t type, cudaStream_t st) {
-    if (!wide) return launch_chained(act_backward_any_kernel<ACT, MUL>, dim3((d.cols + 31) / 32, parts), 32 * kActWarps, 0, st, d, ws);
+cudaError_t launch_act(const cleave_act_backward_t& d, const Sums& b, bool wide, uint32_t type, cudaStream_t st) {
+    if (!wide)
+        return launch_chained_clusters(act_backward_any_kernel<ACT, MUL>, dim3(1, b.joined ? b.bands : 1), dim3((d.cols + 31) / 32, b.bands), 32 * kActWarps, 0, st, d,
+                                       b.out, b.joined);
     if (d.dy_type == CLEAVE_T_F32)
-        return type == CLEAVE_T_F32 ? launch_act_wide<float, float, ACT, MUL>(d, ws, parts, st) : launch_act_wide<float, __nv_bfloat16, ACT, MUL>(d, ws, parts, st);
-    return type == CLEAVE_T_F32 ? launch_act_wide<__nv_bfloat16, float, ACT, MUL>(d, ws, parts, st) : launch_act_wide<__nv_bfloat16, __nv_bfloat16, ACT, MUL>(d, ws, parts, st);
+        return type == CLEAVE_T_F32 ? launch_act_wide<float, float, ACT, MUL>(d, b, st) : launch_act_wide<float, __nv_bfloat16, ACT, MUL>(d, b, st);
+    return type == CLEAVE_T_F32 ? launch_act_wide<__nv_bfloat16, float, ACT, MUL>(d, b, st) : launch_act_wide<__nv_bfloat16, __nv_bfloat16, ACT, MUL>(d, b, st);
 }
 template <bool MUL>
-cudaError_t launch_act(const cleave_act_backward_t& d, float* ws, uint32_t parts, bool wide, uint32_t type, cudaStream_t st) {
+cudaError_t launch_act(const cleave_act_backward_t& d, const Sums& b, bool wide, uint32_t type, cudaStream_t st) {
     switch (d.act) {
-        case CLEAVE_ACT_RELU: return launch_act<CLEAVE_ACT_RELU, MUL>(d, ws, parts, wide, type, st);
-        case CLEAVE_ACT_GELU: return launch_act<CLEAVE_ACT_GELU, MUL>(d, ws, parts, wide, type, st);
-        case CLEAVE_ACT_GELU_TANH: return launch_act<CLEAVE_ACT_GELU_TANH, MUL>(d, ws, parts, wide, type, st);
-        case CLEAVE_ACT_SILU: return launch_act<CLEAVE_ACT_SILU, MUL>(d, ws, parts, wide, type, st);
-        default: return launch_act<CLEAVE_ACT_NONE, MUL>(d, ws, parts, wide, type, st);
+        case CLEAVE_ACT_RELU: return launch_act<CLEAVE_ACT_RELU, MUL>(d, b, wide, type, st);
+        case CLEAVE_ACT_GELU: return launch_act<CLEAVE_ACT_GELU, MUL>(d, b, wide, type, st);
+        case CLEAVE_ACT_GELU_TANH: return launch_act<CLEAVE_ACT_GELU_TANH, MUL>(d, b, wide, type, st);
+        case CLEAVE_ACT_SILU: return launch_act<CLEAVE_ACT_SILU, MUL>(d, b, wide, type, st);
+        default: return launch_act<CLEAVE_ACT_NONE, MUL>(d, b, wide, type, st);
     }
 }
 
@@ -190,9 +219,16 @@ cudaError_t launch_act_backward(const cleave_act_backward_t& d, float* ws, cudaS
     auto fits = [&](const void* p, uint32_t t, uint64_t ld) { return !p || (t == type && rows_wide(p, ld, t)); };
     const bool wide = d.cols % 8 == 0 && rows_wide(d.dy, d.lddy, d.dy_type) && fits(d.z, d.z_type, d.ldz) && fits(d.mul, d.mul_type, d.ldmul) &&
                       fits(d.dz, d.dz_type, d.lddz) && fits(d.dmul, d.dmul_type, d.lddmul);
+    Sums b = {ws, parts, 0u};
+    const bool one_launch = d.dbias && parts && (d.rows <= join_rows(d.act) || parts == 1);
+    if (one_launch) {
+        b.bands = std::min(parts, kJoinBands);
+        b.joined = b.bands > 1;
+        b.out = d.dbias;
+    }
     cudaError_t e = cudaSuccess;
-    if (parts) e = d.mul ? launch_act<true>(d, ws, parts, wide, type, st) : launch_act<false>(d, ws, parts, wide, type, st);
-    if (e != cudaSuccess || !d.dbias) return e;
+    if (parts) e = d.mul ? launch_act<true>(d, b, wide, type, st) : launch_act<false>(d, b, wide, type, st);
+    if (e != cudaSuccess || !d.dbias || one_launch) return e;
     return launch_sum_parts(ws, parts, d.cols, d.dbias, st);
 }
 

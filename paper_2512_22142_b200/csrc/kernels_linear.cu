@@ -327,11 +327,6 @@ __device__ __forceinline__ void tmem_st_32x32(uint32_t taddr, const float* v) {
 }
 // Instruction descriptor of kind::f8f6f4: fp32 accumulator (bits 4-5 = 1), E4M3 A and B (format 0), both K-contiguous.
 __device__ __forceinline__ uint32_t instr_desc_e4m3(uint32_t m, uint32_t n) { return (1u << 4) | ((n >> 3) << 17) | ((m >> 4) << 24); }
-__device__ __forceinline__ float ld_dsmem(uint32_t cluster_addr) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(cluster_addr) : "memory");
-    return v;
-}
 
 __device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&v)[16]) {
     asm volatile(

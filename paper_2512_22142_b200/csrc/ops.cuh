@@ -28,18 +28,24 @@ __device__ __forceinline__ void let_dependents_start() { asm volatile("griddepco
 __device__ __forceinline__ void wait_for_primary() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 __device__ __forceinline__ void begin_chained() { let_dependents_start(); wait_for_primary(); }
 template <typename... P, typename... A>
-cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, uint32_t smem, cudaStream_t st, const A&... args) {
+cudaError_t launch_chained_clusters(void (*kernel)(P...), dim3 cluster, dim3 grid, dim3 block, uint32_t smem, cudaStream_t st, const A&... args) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = block;
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
+    cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cluster.x; attr[1].val.clusterDim.y = cluster.y; attr[1].val.clusterDim.z = cluster.z;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster.x * cluster.y * cluster.z > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+template <typename... P, typename... A>
+cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, uint32_t smem, cudaStream_t st, const A&... args) {
+    return launch_chained_clusters(kernel, dim3(1), grid, block, smem, st, args...);
 }
 
 // Raises a kernel's dynamic shared memory limit, once per device.

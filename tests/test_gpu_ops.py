@@ -632,6 +632,22 @@ def test_act_backward_without_rows_and_plain_column_sums(cl):
         cl.act_backward(dy, None, dbias=db, workspace=ws[:16])
 
 
+@pytest.mark.parametrize("rows", [1, 2, 16, 17, 33, 100, 128, 129, 255, 256, 257, 600, 1023, 1024, 1025, 1500])
+def test_act_backward_column_sums_are_whole_whatever_the_bands(cl, rows):
+    """Integers, exact in any order: rows that make one band, a cluster of up to eight, more; any alignment; no row lost."""
+    rng = np.random.default_rng(51 + rows)
+    for cols in (1, 8, 33, 256, 300, 1032):
+        for dt in (torch.float32, torch.bfloat16):
+            dy = torch.tensor(rng.integers(-8, 9, size=(rows, cols)), dtype=torch.float32).to(dt).to(_dev())
+            z = torch.tensor(rng.integers(-1, 2, size=(rows, cols)), dtype=torch.float32).to(dt).to(_dev())
+            db, dz = torch.full((cols + 2,), 7.0, device=_dev()), torch.empty_like(dy)
+            cl.act_backward(dy, None, dbias=db[:cols])
+            assert torch.equal(db[:cols], dy.float().sum(0)) and torch.all(db[cols:] == 7.0)
+            cl.act_backward(dy, z, dz, act="relu", dbias=db[1:cols + 1])
+            want = torch.where(z > 0, dy, torch.zeros_like(dy))
+            assert torch.equal(dz, want) and torch.equal(db[1:cols + 1], want.float().sum(0)) and float(db[cols + 1]) == 7.0
+
+
 # ---- one operator after another ------------------------------------------------------------------------
 @pytest.mark.parametrize("rows,cols,ffn", [(3, 256, 512), (700, 768, 1536), (33, 130, 266)])
 def test_chained_calls_see_what_the_one_before_wrote(cl, rows, cols, ffn):
