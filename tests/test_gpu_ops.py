@@ -632,6 +632,23 @@ def test_act_backward_without_rows_and_plain_column_sums(cl):
         cl.act_backward(dy, None, dbias=db, workspace=ws[:16])
 
 
+@pytest.mark.parametrize("ty,tz,tm,tdz,tdm", [("f32", "bf16", "bf16", "bf16", "bf16"), ("bf16", "f32", "f32", "f32", "f32"), ("f32", "bf16", "f32", "f32", "bf16"),
+                                              ("bf16", "f32", "bf16", "bf16", "f32")])
+@pytest.mark.parametrize("rows,cols", [(7, 48), (300, 264), (1200, 40)])
+def test_act_backward_of_mixed_types(cl, ty, tz, tm, tdz, tdm, rows, cols):
+    rng = np.random.default_rng(rows + cols)
+    dy, z, mul = _rand(rng, (rows, cols), DT[ty]), _rand(rng, (rows, cols), DT[tz], 2.0), _rand(rng, (rows, cols), DT[tm])
+    dz, dmul, db = torch.empty(rows, cols, dtype=DT[tdz], device=_dev()), torch.empty(rows, cols, dtype=DT[tdm], device=_dev()), torch.empty(cols, device=_dev())
+    for act in ("relu", "silu"):
+        cl.act_backward(dy, z, dz, act=act, mul=mul, dmul=dmul, dbias=db)
+        y64, z64, m64 = _f64(dy), _f64(z), _f64(mul)
+        dz64, dmul64, _ = ref.act_backward(y64, z64, act, m64)
+        own = 32 * U * (1 + np.abs(z64)) ** 2 * np.abs(y64)                # (as above)
+        _close(dz, dz64, own * np.abs(m64), "dz")
+        _close(dmul, dmul64, own * np.abs(z64), "dmul")
+        _close(db, dz64.sum(axis=0), (own * np.abs(m64)).sum(axis=0) + SUM * np.abs(dz64).sum(axis=0), "dbias")
+
+
 @pytest.mark.parametrize("rows", [1, 2, 16, 17, 33, 100, 128, 129, 255, 256, 257, 600, 1023, 1024, 1025, 1500])
 def test_act_backward_column_sums_are_whole_whatever_the_bands(cl, rows):
     """Integers, exact in any order: rows that make one band, a cluster of up to eight, more; any alignment; no row lost."""
