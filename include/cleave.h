@@ -330,8 +330,8 @@ CLEAVE_API void cleave_destroy(cleave_plan_t* p);
  *   - Matrices are row-major with a leading dimension in elements (ld >= columns).  Element types
  *     are CLEAVE_T_*; "type 0" means the operand is absent (and its pointer NULL).
  *   - A pointer is aligned to its element size at least; 16-byte aligned bases with rows that are a
- *     multiple of 16 bytes apart take the wide loads.  Any number of rows and columns up to 2^31 - 1 is
- *     accepted.
+ *     multiple of 16 bytes apart take the wide loads.  Columns: any number from 1 to
+ *     2^31 - 1; rows: up to 2^31 - 1.
  *   - Inputs and outputs may be the same buffer where a call says so, and must not overlap otherwise.
  *   - Zero rows are accepted and compute nothing (sums over rows become 0).
  *   - All sums, statistics and states are held in fp32; a narrower output is rounded once, to nearest
@@ -447,7 +447,7 @@ CLEAVE_API int cleave_quantize_rows(const void* x, uint32_t x_type, uint64_t row
 
 /* Matrix product with everything that follows it in its write-out:
  *   z = scale_a[i] scale_b[j] (op(A) op(B))_ij + bias[j]        C = act(z) * mul + res
- * g gives the sizes, layouts and leading dimensions as in cleave_plan (level is ignored); M may be 0.
+ * g gives the sizes, layouts and leading dimensions as in cleave_plan (level is ignored); M may be 0, N and K at least 1.
  * in_type CLEAVE_T_BF16: all layouts, lda and ldb multiples of 8.  in_type CLEAVE_T_E4M3: both operands
  * K-contiguous (transA = 0, transB = 1), lda and ldb multiples of 16.  A and B are 16-byte aligned.
  * Optional: scale_a [M], scale_b [N] fp32; bias [N] (bf16 or fp32); z out (bf16 or fp32, what

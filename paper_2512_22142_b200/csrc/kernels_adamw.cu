@@ -8,8 +8,8 @@
 // blocks are on their way to shared memory (three stages of its own, no barrier) while one is used.
 // Bytes an element: 30 with fp32 states (gradient 4, weight 8, states 16, copy 2; 28 with bf16 gradients), 18 with 8-bit
 // ones.  fp32 states are bound by the HBM (a layer of width 768, 7.1 M elements: 35 us, 5.7 TB/s).  8-bit states are bound
-// by instruction issue (74 % of the cycles issue, 55 % of the HBM's): two roundings with random bits, a division and a
-// root an element; 202 M elements take 691 us, 5.3 TB/s.
+// by instruction issue (73 % of the cycles issue, 64 % of the HBM's): two roundings with random bits, a division and a
+// root an element; 202 M elements take 691 us a step of one optimizer after another (5.3 TB/s), 720 with three in turn.
 #include <cuda_fp16.h>
 
 #include <type_traits>

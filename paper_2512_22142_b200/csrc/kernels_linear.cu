@@ -10,10 +10,11 @@
 //
 // linear_pair_kernel: tiles of 256 x 256 on pairs of CTAs, persistent, for large products (its comment below).
 //
-// Bound by: the weights' bytes and the latency of one pass (few rows: 16 x 4096 x 4096 takes 11.8 us after another, its
-// 34 MB 5.2 us at the measured copy rate); the write-out beside the products (8192 x 768 x 3072 with bias, GELU and z: 42 us,
-// products alone 27, the write-out alone 28); the tensor cores under the power cap (8192 x 4096 x 11008 in E4M3 with
-// SwiGLU 305 to 390 us, 11008 x 8192 x 4096 into fp32 560 to 660, with the clock).
+// Bound by: the weights' bytes and the latency of one pass (few rows: 16 x 4096 x 4096 takes 12.3 us after another, 13.0 with
+// bias and residual, its 34 MB 5.2 us at the measured copy rate); the write-out beside the products (8192 x 768 x 3072 with
+// bias, GELU and z: 52 us with inputs in turn, 43 with them in L2; products alone 27, the write-out alone 28); operands from
+// L2 beside the tensor cores, and the clock that the power cap leaves (8192 x 4096 x 11008 in E4M3 with SwiGLU 305 us in short
+// runs, 375 to 390 in long ones, 11008 x 8192 x 4096 into fp32 560 and 650; the tensor pipe works in 60 to 66 % of the cycles).
 //
 // Operands: K-contiguous or M/N-contiguous bf16 through the descriptors' major bits (no transposed copies), or
 // K-contiguous E4M3 (kind::f8f6f4), 128 bytes of K a stage either way; TMA fills what lies outside a matrix with
@@ -585,8 +586,8 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // warps keep the sum in registers with ordinary rounded additions; the two slots take turns by chunk instead of by tile.
 constexpr uint32_t kLpMaxStages = 6, kLpEpiWarp0 = 4, kLpBand = 8;
 // Write-out warps: 16 keep pace with the products of a short K (bias, activation and a second output: 55 -> 50 us at 8192 x 768
-// x 3072 against 8); LONG takes 8, whose threads hold 128 sums each (with 16, what else they need spills: 419 -> 544 us
-// at 8192 x 8192 x 4096).
+// x 3072 against 8); LONG takes 8, whose threads hold 128 sums each (with 16 warps 96 registers a thread are left:
+// 419 -> 544 us at 8192 x 8192 x 4096; with 8 the instances still spill, 204 bytes a thread, 252 with ReLU).
 __host__ __device__ constexpr uint32_t pair_warps(bool lng) { return lng ? 8u : 16u; }
 __host__ __device__ constexpr uint32_t pair_threads(bool lng) { return 32u * (kLpEpiWarp0 + pair_warps(lng)); }
 constexpr uint32_t kLpSmemMost = 227 * 1024 - 256;       // (what is declared statically comes on top)

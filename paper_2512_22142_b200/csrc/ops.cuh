@@ -221,8 +221,9 @@ __device__ __forceinline__ float gelu_tanh_gate(float z) {
     return rcp_fast(1.f + exp2_fast(-z * fmaf(0.1029432407f, z * z, 2.3022081983f)));
 }
 __device__ __forceinline__ float silu_gate(float z) { return rcp_fast(1.f + exp2_fast(-1.4426950409f * z)); }
-// Phi(z), the normal distribution, and exp(-z^2 / 2), with one reciprocal and one exponential (erfcf takes four times as
-// long: 84 against 24 us in the write-out of 39 M elements; 8192 x 768 x 3072 with z takes 48.3 us, with the tanh form 43.4).  On the negative side Phi(z) = t P(t) exp(-z^2 / 2) with
+// Phi(z), the normal distribution, and exp(-z^2 / 2), with one reciprocal and one exponential (8192 x 768 x 3072 with z takes
+// 48.3 us, with the tanh form 43.4; erfcf takes far longer: 84 against 24 us where an earlier polynomial of degree 4
+// stood in the write-out of 39 M elements).  On the negative side Phi(z) = t P(t) exp(-z^2 / 2) with
 // t = 1 / (1 + 0.30405593 |z|): 0.5 erfcx(|z| / sqrt(2)) / t is smooth in t, and P is its polynomial of degree 7 with the
 // smallest largest relative error over |z| <= 13.3 (8.4e-8; fitted by reweighted least squares on Chebyshev points).
 // In fp32 Phi's relative error is at most 16 (1 + z^2) 2^-24, tail included (the exponent's rounding grows with z^2, as
