@@ -36,9 +36,10 @@ __device__ unsigned int g_linear_status;
 static std::atomic<uint64_t> g_linear_wait_limit{2000000000ull};
 
 constexpr uint32_t kLinTile = 128, kLinMaxStages = 5, kLinOperand = 16384, kLinStage = 2 * kLinOperand;
-// Products an accumulator takes before its sum moves on, in fp32 results: the tensor core cuts off when it adds, so one
-// accumulator over K = 8192 is 9.1e-6 off (operands of one sign: 2.5e-5), handed over 4.8e-7 at every K (5e-7).
-constexpr uint32_t kLongK = 512;
+// K-blocks an accumulator takes before its sum moves on, in fp32 results: 32 steps of the tensor core, 512 products of bf16
+// or 1024 of E4M3.  It cuts off when it adds, so one accumulator over K = 8192 (bf16) is 9.1e-6 off (operands of one
+// sign: 2.5e-5), handed over 4.8e-7 at every K (5e-7).
+constexpr uint32_t kLongBlocks = 8;
 // Blocks of B that a CTA of linear_split_kernel asks L2 for while the kernel before still runs (16 x 4096 x 4096 right after
 // another: none 13.0, three 12.5, eight 13.0 us).
 constexpr uint32_t kLinAhead = 3;
@@ -61,7 +62,7 @@ struct Epilogue {
 
 struct LinearParams {
     Epilogue e;
-    uint32_t K_blocks, splits, tiles_n, chunk;   // chunk: K-blocks that an accumulator takes before it is handed over
+    uint32_t K_blocks, splits, tiles_n;
     uint32_t a_mn, b_mn, a_rows;    // a_rows: rows of a K-contiguous A that a stage brings
     // A stage holds B's 16 KB, then A's rows, so few rows leave room for five stages, 128 for three (16 x 4096 x 4096: three
     // stages 12.5, five 12.3 us; 1 x 11008 x 4096: 23.5, 22.3).  The product reads 128 rows of A; what stands behind those
@@ -370,7 +371,7 @@ struct __align__(16) LinShared {
     uint32_t tmem_base, abort_flag;
 };
 
-// LONG: the accumulator is handed over every P.chunk K-blocks (see kLongK).  Two of them take turns, 256 columns of tensor
+// LONG: the accumulator is handed over every kLongBlocks K-blocks.  Two of them take turns, 256 columns of tensor
 // memory a CTA (two CTAs share an SM's 512); each of the four write-out warps keeps the sums of its 32 rows in registers,
 // adds a chunk while the next one's products run, and lays the sums into the last accumulator's place at the end.
 // Measured against one accumulator: 16 x 4096 x 11008 21.4 to 20.6 us, 1 x 50304 x 2048 43.7 to 41.1, 768 x 3072 x 8192
@@ -393,7 +394,8 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < P.stages; ++s) { mbar_init(smem_u32(&sh.full[s]), 1); mbar_init(smem_u32(&sh.empty[s]), 1); }
-        for (int a = 0; a < 2; ++a) { mbar_init(smem_u32(&sh.acc_full[a]), 1); mbar_init(smem_u32(&sh.acc_empty[a]), 4); }
+        mbar_init(smem_u32(&sh.acc_full[0]), 1);
+        if constexpr (LONG) { mbar_init(smem_u32(&sh.acc_full[1]), 1); mbar_init(smem_u32(&sh.acc_empty[0]), 4); mbar_init(smem_u32(&sh.acc_empty[1]), 4); }
         mbar_init(smem_u32(&sh.drain), 1);
         sh.abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -439,23 +441,29 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
         const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
         bool ok = true;
-        const uint32_t chunk = LONG ? P.chunk : kb1 - kb0;
-        uint32_t s = 0, ph = 0, use = 0;                  // stage, its phase, accumulators used so far
-        for (uint32_t k0 = kb0; ok && k0 < kb1; k0 += chunk, ++use) {
-            const uint32_t acc = use & 1u, d = tmem + acc * kLinTile;
-            if (LONG && !lin_wait(smem_u32(&sh.acc_empty[acc]), ((use >> 1) & 1u) ^ 1u, W)) { ok = false; break; }
+        uint32_t s = 0, ph = 0;                           // stage, its phase
+        auto block = [&](uint32_t d, uint32_t accumulate) {
+            if (!lin_wait(smem_u32(&sh.full[s]), ph, W)) { ok = false; return; }
             tc_fence_after();
-            for (uint32_t kb = k0; kb < min(kb1, k0 + chunk); ++kb) {
-                if (!lin_wait(smem_u32(&sh.full[s]), ph, W)) { ok = false; break; }
-                tc_fence_after();
-                const uint32_t sb = base + s * P.stage_bytes, sa = sb + kLinOperand;
+            const uint32_t sb = base + s * P.stage_bytes, sa = sb + kLinOperand;
 #pragma unroll
-                for (uint32_t q = 0; q < 4; ++q)          // 32 bytes of K each
-                    umma_one<E4M3>(d, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, (kb != k0) | (q != 0u));
-                umma_commit_one(smem_u32(&sh.empty[s]));
-                if (++s == P.stages) { s = 0; ph ^= 1u; }
+            for (uint32_t q = 0; q < 4; ++q)              // 32 bytes of K each
+                umma_one<E4M3>(d, smem_desc_sw128(sa + q * a_step, a_lbo, 1024u), smem_desc_sw128(sb + q * b_step, b_lbo, 1024u), idesc, accumulate | (q != 0u));
+            umma_commit_one(smem_u32(&sh.empty[s]));
+            if (++s == P.stages) { s = 0; ph ^= 1u; }
+        };
+        if constexpr (LONG) {
+            uint32_t use = 0;                             // accumulators used so far
+            for (uint32_t k0 = kb0; ok && k0 < kb1; k0 += kLongBlocks, ++use) {
+                const uint32_t acc = use & 1u;
+                if (!lin_wait(smem_u32(&sh.acc_empty[acc]), ((use >> 1) & 1u) ^ 1u, W)) { ok = false; break; }
+                tc_fence_after();
+                for (uint32_t kb = k0; ok && kb < min(kb1, k0 + kLongBlocks); ++kb) block(tmem + acc * kLinTile, kb != k0);
+                if (ok) umma_commit_one(smem_u32(&sh.acc_full[acc]));
             }
-            if (ok) umma_commit_one(smem_u32(&sh.acc_full[acc]));
+        } else {
+            for (uint32_t kb = kb0; ok && kb < kb1; ++kb) block(tmem, kb != kb0);
+            if (ok) umma_commit_one(smem_u32(&sh.acc_full[0]));
         }
         // everything issued above has completed before tensor memory is released
         umma_commit_one(smem_u32(&sh.drain));
@@ -485,7 +493,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 #pragma unroll
             for (uint32_t i = 0; i < kLinTile; ++i) sum[i] = 0.f;
             uint32_t use = 0;
-            for (uint32_t k0 = kb0; k0 < kb1; k0 += P.chunk, ++use) {
+            for (uint32_t k0 = kb0; k0 < kb1; k0 += kLongBlocks, ++use) {
                 const uint32_t acc = use & 1u, at = taddr + acc * kLinTile;
                 ok = __all_sync(0xFFFFFFFFu, lin_wait_inline(smem_u32(&sh.acc_full[acc]), (use >> 1) & 1u, W));
                 if (!ok) break;
@@ -499,7 +507,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 #pragma unroll
                         for (int i = 0; i < 16; ++i) sum[c + i] += __uint_as_float(u[i]);
                     }
-                    if (k0 + P.chunk >= kb1) {            // nothing is accumulated here any more
+                    if (k0 + kLongBlocks >= kb1) {        // nothing is accumulated here any more
 #pragma unroll
                         for (uint32_t c = 0; c < kLinTile; c += 32) tmem_st_32x32(at + c, sum + c);
                         asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
@@ -582,7 +590,7 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
 // slots, so the write-out of a tile runs beside the products of the next.  Tiles go to clusters round robin, in bands
 // of eight row tiles so that tiles in flight share operands in L2.
 //
-// LONG (fp32 results of a long K, see kLongK): the accumulator is handed over every `chunk` K-blocks and the write-out
+// LONG (fp32 results of a long K, see kLongBlocks): the accumulator is handed over every `chunk` K-blocks and the write-out
 // warps keep the sum in registers with ordinary rounded additions; the two slots take turns by chunk instead of by tile.
 constexpr uint32_t kLpMaxStages = 6, kLpEpiWarp0 = 4, kLpBand = 8;
 // Write-out warps: 16 keep pace with the products of a short K (bias, activation and a second output: 55 -> 50 us at 8192 x 768
@@ -909,8 +917,8 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
     cudaError_t err;
     const uint64_t tiles_m = (g.M + kLinTile - 1) / kLinTile, tiles_n = (g.N + kLinTile - 1) / kLinTile, tiles = tiles_m * tiles_n;
     const uint32_t pairs = (uint32_t)sms / 2;
-    // Results of an fp32 output of a long K move on every kLongK products (both kernels)
-    const bool lng = (d.c_type == CLEAVE_T_F32 || d.z_type == CLEAVE_T_F32) && g.K > kLongK;
+    // Results of an fp32 output of a long K move on every kLongBlocks K-blocks (both kernels)
+    const bool lng = (d.c_type == CLEAVE_T_F32 || d.z_type == CLEAVE_T_F32) && P.K_blocks > kLongBlocks;
     // Pairs of CTAs bring half the operand bytes for a product, one CTA a tile starts and ends sooner and spreads few tiles
     // wider.  With one row of tiles half of a pair's rows would be empty (16 x 50304 x 2048: 56 us by pairs, 42 by tiles);
     // from two tiles a place on, pairs win at every K (4096 x 2048: K = 256 10.1 against 12.6 us, K = 4096 51 against 66);
@@ -930,7 +938,7 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         Q.tiles_n = (g.N + Q.bn - 1) / Q.bn;
         Q.b_boxes = (Q.bn / 2 + 63) / 64;
         Q.b_bytes = Q.b_mn ? Q.b_boxes * kSubBytes : Q.bn / 2 * 128u;
-        Q.chunk = lng ? kLongK / kblk : Q.K_blocks;
+        Q.chunk = lng ? kLongBlocks : Q.K_blocks;
         // (an M- or N-contiguous operand by one copy a stage instead of two, where its columns are whole groups of 64: 4096^3
         // 98.8 us against 105.9, 11008 x 4096 x 4096 285 against 308)
         if (Q.a_mn && g.M % 64 == 0) { Q.a_mn = 2; rc = encode_groups(&ma, d.A, g.K, g.M, g.lda); }
@@ -968,8 +976,7 @@ int launch_linear(const cleave_linear_t& d, int sms, cudaStream_t st) {
         P.stages = std::min(kLinMaxStages, (kLinSmem - 1024u - (kLinOperand - P.a_rows * 128u)) / P.stage_bytes);
         rc = g.transA ? encode_operand(&ma, d.A, g.K, g.M, g.lda, 64, e4m3) : encode_operand(&ma, d.A, g.M, g.K, g.lda, P.a_rows, e4m3);
         if (rc || (rc = encode_b(kLinTile))) return rc;
-        P.chunk = kLongK / kblk;
-        const bool hand_over = lng && (P.K_blocks + P.splits - 1) / P.splits > P.chunk;      // (the cluster's sum is a rounded one)
+        const bool hand_over = lng && (P.K_blocks + P.splits - 1) / P.splits > kLongBlocks;      // (the cluster's sum is a rounded one)
         const SplitKernel kernel = pick_act<PickSplit>(d.act, e4m3, hand_over);
         static SmemLimit limit[4 * kActs];
         if (limit[((e4m3 ? 2 : 0) + (hand_over ? 1 : 0)) * kActs + d.act].raise(reinterpret_cast<const void*>(kernel), kLinSmem) != cudaSuccess) { cudaGetLastError(); return CLEAVE_E_CUDA; }

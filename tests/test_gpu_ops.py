@@ -461,7 +461,7 @@ LONG_K = [(2048, 1280, 1900), (2048, 1280, 8192), (1100, 1500, 16384), (700, 900
 @pytest.mark.parametrize("ta,tb,kind", [(False, False, "bf16"), (True, False, "bf16"), (False, True, "e4m3")])
 def test_linear_fp32_results_of_a_long_k_keep_their_accuracy(cl, m, n, k, ta, tb, kind):
     """Operands of one sign, so that what the tensor core cuts off adds up.  It adds 16 (E4M3: 32) products a step and may cut
-    off a unit (2^-23) of the running sum; an accumulator takes 512 products, 32 steps, whose running sums are half of the last
+    off a unit (2^-23) of the running sum; an accumulator takes 32 steps, whose running sums are half of the last
     one on average: 17 units of 2^-23.  The chunks' sums are rounded: half a unit of the running sum each, again half on
     average, and a few more in the cluster's sum.  (One accumulator over 8192 products: 9e-6, about three times the bound.)"""
     gen = torch.Generator(device=_dev()).manual_seed(m + n + k)
