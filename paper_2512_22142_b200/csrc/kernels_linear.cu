@@ -338,6 +338,17 @@ __device__ __forceinline__ void tmem_ld_32x16(uint32_t taddr, uint32_t (&v)[16])
         : "r"(taddr) : "memory");
 }
 
+// mbarrier.try_wait may hold the thread for microseconds, longer than many a wait here: with a limit of 0 the MMA issuer's
+// first wait is asked for without holding.
+__device__ __forceinline__ bool mbar_is_done(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
 struct LinWait { volatile uint32_t* abort_flag; uint64_t limit_ns; };
 static __device__ __noinline__ bool lin_wait_slow(uint32_t bar, uint32_t parity, const LinWait& w) {
     const uint64_t t0 = global_timer_ns();
@@ -440,7 +451,8 @@ linear_split_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         const uint32_t idesc = E4M3 ? instr_desc_e4m3(kLinTile, kLinTile) : instr_desc_bf16(kLinTile, kLinTile, P.a_mn, P.b_mn);
         const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
         const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
-        bool ok = true;
+        bool ok = W.limit_ns != 0 || mbar_is_done(smem_u32(&sh.full[0]), 0u);
+        if (!ok) { sh.abort_flag = 1u; atomicOr(&g_linear_status, STATUS_TIMEOUT); }
         uint32_t s = 0, ph = 0;                           // stage, its phase
         auto block = [&](uint32_t d, uint32_t accumulate) {
             if (!lin_wait(smem_u32(&sh.full[s]), ph, W)) { ok = false; return; }
@@ -695,7 +707,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_const
             const uint32_t a_lbo = P.a_mn ? kSubBytes : 16u, a_step = P.a_mn ? 2048u : 32u;
             const uint32_t b_lbo = P.b_mn ? kSubBytes : 16u, b_step = P.b_mn ? 2048u : 32u;
             uint32_t s = 0, ph = 0, use = 0;          // stage, its phase, accumulator slots used so far
-            bool ok = true;
+            bool ok = W.limit_ns != 0 || mbar_is_done(smem_u32(&sh.full[0]), 0u);
+            if (!ok) raise_abort(W);
             for (uint32_t t = cluster; ok && t < tiles; t += clusters) {
                 for (uint32_t k0 = 0; ok && k0 < P.K_blocks; k0 += P.chunk, ++use) {
                     const uint32_t k1 = min(P.K_blocks, k0 + P.chunk), acc = use & 1u, d = tmem + acc * 256u;
