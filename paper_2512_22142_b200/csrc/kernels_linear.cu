@@ -14,7 +14,7 @@
 // bias and residual, its 34 MB 5.2 us at the measured copy rate); the write-out beside the products (8192 x 768 x 3072 with
 // bias, GELU and z: 52 us with inputs in turn, 43 with them in L2; products alone 27, the write-out alone 28); operands from
 // L2 beside the tensor cores, and the clock that the power cap leaves (8192 x 4096 x 11008 in E4M3 with SwiGLU 305 us in short
-// runs, 375 to 390 in long ones, 11008 x 8192 x 4096 into fp32 560 and 650; the tensor pipe works in 60 to 66 % of the cycles).
+// runs, 375 to 400 in long ones, 11008 x 8192 x 4096 into fp32 560 and 650; the tensor pipe works in 60 to 66 % of the cycles).
 //
 // Operands: K-contiguous or M/N-contiguous bf16 through the descriptors' major bits (no transposed copies), or
 // K-contiguous E4M3 (kind::f8f6f4), 128 bytes of K a stage either way; TMA fills what lies outside a matrix with
