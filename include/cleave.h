@@ -344,6 +344,8 @@ CLEAVE_API void cleave_destroy(cleave_plan_t* p);
 #define CLEAVE_T_BF16 1u
 #define CLEAVE_T_F32  2u
 #define CLEAVE_T_E4M3 3u      /* 8-bit float: 4 exponent bits, 3 mantissa bits, largest value 448, no infinity */
+#define CLEAVE_T_I32  4u      /* token numbers */
+#define CLEAVE_T_I64  5u
 
 /* Activations: z; max(z, 0); z Phi(z); z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2; z / (1 + exp(-z)).  The last three
  * are evaluated in fp32 with relative errors of at most 16 (1 + z^2), 8 + 4 |2 sqrt(2/pi) (z + 0.044715 z^3)| and
@@ -492,6 +494,161 @@ CLEAVE_API int cleave_linear_status(void* stream);
 /* Bound, in nanoseconds, of every wait inside cleave_linear's kernels (default 2 s), for all later calls of the
  * process.  With 0 the first wait that is not satisfied at once gives up (for tests of that path). */
 CLEAVE_API void cleave_linear_set_wait_limit_ns(uint64_t ns);
+
+/* ---- the two ends of a step on tokens ----------------------------------------------------------
+ *
+ * Token numbers are CLEAVE_T_I32 or CLEAVE_T_I64; one outside of [0, vocab) is padding: it reads and changes nothing
+ * and what it would have contributed is 0.
+ *
+ * Rows of a table by token, in the order of the tokens:   out_i = scale table[ids_i]
+ * (zeros where ids_i is padding).  table, out: bf16 or fp32. */
+typedef struct {
+    uint64_t n;                                  /* tokens                                    */
+    uint32_t vocab, cols;                        /* rows of the table and their length        */
+    uint32_t id_type, table_type, out_type;
+    float    scale;
+    const void* ids;                             /* [device, n]                               */
+    const void* table; uint64_t ldt;
+    void*       out;   uint64_t ldo;
+} cleave_embedding_t;
+CLEAVE_API int cleave_embedding(const cleave_embedding_t* d, void* stream);
+
+/* Its gradient:   dtable[v] = scale * (sum over the i with ids_i = v of dy_i)   for every v of the table (rows of tokens that do
+ * not occur become 0); accumulate = 1 adds that to dtable and touches the rows of tokens that occur only.  Summed in fp32 in an
+ * order that follows from the tokens alone.  dy, dtable: bf16 or fp32. */
+typedef struct {
+    uint64_t n;
+    uint32_t vocab, cols;
+    uint32_t id_type, dy_type, dtable_type, accumulate;
+    float    scale;
+    uint32_t pad_;
+    const void* ids;
+    const void* dy;     uint64_t lddy;
+    void*       dtable; uint64_t lddt;
+} cleave_embedding_backward_t;
+CLEAVE_API uint64_t cleave_embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols);
+CLEAVE_API int cleave_embedding_backward(const cleave_embedding_backward_t* d, void* workspace, void* stream);
+
+/* Layer norm with the residual's addition.  Per row, in fp32:
+ *   h = x + r      mean = mean_j h_j      rstd = (mean_j (h_j - mean)^2 + eps)^(-1/2)      y_j = (h_j - mean) rstd w_j + b_j
+ * The variance is formed from differences to the mean, never as a difference of squares.  r, h, w, y, the E4M3 codes and their
+ * scale as in cleave_rmsnorm; b (bf16 or fp32) may be absent (zeros), mean and rstd [device, rows] may be NULL. */
+typedef struct {
+    uint64_t rows;
+    uint32_t cols;
+    uint32_t x_type, r_type, w_type, b_type, y_type;
+    float    eps;
+    uint32_t pad_;
+    const void* x;  uint64_t ldx;
+    const void* r;  uint64_t ldr;
+    void*       h;  uint64_t ldh;
+    const void* w;
+    const void* b;
+    void*       y;  uint64_t ldy;
+    float*      mean;
+    float*      rstd;
+    float*      scale;
+} cleave_layernorm_t;
+CLEAVE_API int cleave_layernorm(const cleave_layernorm_t* d, void* stream);
+
+/* Its backward pass.  With xh = (h - mean) rstd and q = w dy:
+ *   dx = rstd (q - mean_j q_j - xh mean_j(q_j xh_j)) + dres      dw_j = sum over the rows of dy_j xh_j      db_j = sum of dy_j
+ * Operands as in cleave_rmsnorm_backward; dw and db [device, cols] fp32 may each be NULL. */
+typedef struct {
+    uint64_t rows;
+    uint32_t cols;
+    uint32_t dy_type, h_type, w_type, pad_;
+    const void*  dy;   uint64_t lddy;
+    const void*  h;    uint64_t ldh;
+    const void*  w;
+    const float* mean;
+    const float* rstd;
+    const void*  dres; uint64_t lddres;
+    void*        dx;   uint64_t lddx;
+    float*       dw;
+    float*       db;
+} cleave_layernorm_backward_t;
+CLEAVE_API uint64_t cleave_layernorm_backward_workspace(uint64_t rows, uint32_t cols);
+CLEAVE_API int cleave_layernorm_backward(const cleave_layernorm_backward_t* d, void* workspace, void* stream);
+
+/* Log probabilities of given tokens, and what else one reading of the scores gives.  Per row, with s = scale > 0 (1 / temperature)
+ * and p = softmax(s x):
+ *   lse = log sum_j exp(s x_j)      logp = s x_t - lse for the token t      entropy = -sum_j p_j log p_j
+ *   top_index, top_values: the `top` places of the largest scores, largest first and of equal ones the lowest place first,
+ *   and their log probabilities s x - lse.
+ * Every output may be NULL, but not all.  x: bf16 or fp32.  top: 0 to CLEAVE_TOP_MOST and at most cols.
+ * A masked place (-infinity) has probability 0.  A row without a score above -2^126 (all places masked, by -infinity or the type's
+ * lowest value) has lse = -infinity, logp = -infinity, entropy 0, top_values -infinity, and no gradient.  A row
+ * that holds a NaN or +infinity has NaN for lse, logp, entropy and top_values (a NaN sorts above all).  The logp of padding is 0. */
+#define CLEAVE_TOP_MOST 64u
+typedef struct {
+    uint64_t rows;
+    uint32_t cols;
+    uint32_t x_type, id_type, top;
+    float    scale;
+    uint32_t pad_;
+    const void* x;   uint64_t ldx;
+    const void* ids;                             /* [device, rows]; type 0 when logp is NULL  */
+    float* logp;                                 /* [device, rows] each, or NULL              */
+    float* lse;
+    float* entropy;
+    float*   top_values; uint64_t ldtv;          /* [device, rows x top], or NULL             */
+    int32_t* top_index;  uint64_t ldti;
+} cleave_logprobs_t;
+CLEAVE_API int cleave_logprobs(const cleave_logprobs_t* d, void* stream);
+
+/* Its backward pass, from the scores and the saved lse (and entropy, where dentropy is given):
+ *   dx_j = s (dlogp ([j = t] - p_j) + dlse p_j - dentropy p_j (log p_j + entropy))
+ * dlogp, dlse, dentropy [device, rows] fp32: each may be NULL (zeros).  dx (bf16 or fp32) may be x's buffer when types and
+ * leading dimensions agree.  Cross entropy is dlogp = -1 / (number of tokens); what dlse carries is a penalty on lse. */
+typedef struct {
+    uint64_t rows;
+    uint32_t cols;
+    uint32_t x_type, id_type, dx_type;
+    float    scale;
+    uint32_t pad_;
+    const void*  x;   uint64_t ldx;
+    const void*  ids;                            /* type 0 when dlogp is NULL                 */
+    const float* lse;
+    const float* entropy;
+    const float* dlogp;
+    const float* dlse;
+    const float* dentropy;
+    void*        dx;  uint64_t lddx;
+} cleave_logprobs_backward_t;
+CLEAVE_API int cleave_logprobs_backward(const cleave_logprobs_backward_t* d, void* stream);
+
+/* Distillation from a teacher's top scores.  Row i of index and values [rows x k] names k places of the vocabulary and what the
+ * teacher gave them; a place outside of [0, cols) or a value of -infinity is empty (its q is 0), and a place may occur more than once.
+ *   q = softmax over the row of s values (normalize = 1), or exp(s values) (normalize = 0: log probabilities as they are)
+ *   loss = sum_k q_k (log q_k - log p_(index_k)), p = softmax(s x) over the whole vocabulary; terms with q_k = 0 are 0
+ *   lse as in cleave_logprobs (may be NULL)
+ * A row whose places are all empty has loss 0 and no gradient; one whose scores are all masked has loss +infinity, unless
+ * its places are empty too, and no gradient.  k: 1 to CLEAVE_DISTILL_MOST. */
+#define CLEAVE_DISTILL_MOST 256u
+typedef struct {
+    uint64_t rows;
+    uint32_t cols, k;
+    uint32_t x_type, index_type, values_type, normalize;
+    float    scale;
+    uint32_t pad_;
+    const void* x;      uint64_t ldx;
+    const void* index;  uint64_t ldindex;
+    const void* values; uint64_t ldvalues;
+    float* loss;
+    float* lse;
+} cleave_distill_t;
+CLEAVE_API int cleave_distill(const cleave_distill_t* d, void* stream);
+
+/* Its gradient:   dx_j = dloss s ((sum_k q_k) p_j - sum over the k with index_k = j of q_k).   The records' common fields mean
+ * the same (loss is not read, lse is); dx as in cleave_logprobs_backward. */
+typedef struct {
+    cleave_distill_t f;
+    const float* dloss;                          /* [device, rows]                            */
+    uint32_t dx_type, pad_;
+    void*        dx;    uint64_t lddx;
+} cleave_distill_backward_t;
+CLEAVE_API int cleave_distill_backward(const cleave_distill_backward_t* d, void* stream);
 
 CLEAVE_API const char* cleave_strerror(int code);
 

@@ -9,7 +9,8 @@ _BINDING_NAMES = ("CleaveError", "Plan", "default_opts", "lib", "lib_path", "pla
 
 
 _OPS_NAMES = ("AdamW", "rmsnorm", "rmsnorm_backward", "rmsnorm_backward_workspace", "quantize_rows", "linear", "linear_status",
-              "act_backward", "act_backward_workspace")
+              "act_backward", "act_backward_workspace", "embedding", "embedding_backward", "embedding_backward_workspace", "layernorm",
+              "layernorm_backward", "layernorm_backward_workspace", "token_logprobs", "token_logprobs_backward", "distill", "distill_backward")
 
 
 def __getattr__(name):

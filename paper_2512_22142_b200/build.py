@@ -13,8 +13,9 @@ CSRC = os.path.join(PKG, "csrc")
 LIB_DIR = os.path.join(PKG, "lib")
 LIB_PATH = os.path.join(LIB_DIR, "libcleave.so")
 SOURCES = ["planner.cpp", "kernels.cu", "kernels_pair.cu", "kernels_verify.cu", "kernels_simple.cu", "api.cu",
-           "kernels_adamw.cu", "kernels_norm.cu", "kernels_act.cu", "kernels_linear.cu", "ops.cu"]
-HEADERS = ["plan_internal.hpp", "kernels.cuh", "ptx.cuh", "ops.cuh", os.path.join(ROOT, "include", "cleave.h")]
+           "kernels_adamw.cu", "kernels_norm.cu", "kernels_act.cu", "kernels_linear.cu", "kernels_embedding.cu", "kernels_layernorm.cu",
+           "kernels_logprobs.cu", "ops.cu"]
+HEADERS = ["plan_internal.hpp", "kernels.cuh", "ptx.cuh", "ops.cuh", "rows.cuh", "tokens.cuh", os.path.join(ROOT, "include", "cleave.h")]
 
 
 MARSHAL_SOURCE = os.path.join(CSRC, "marshal.cpp")

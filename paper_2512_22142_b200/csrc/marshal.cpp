@@ -23,12 +23,15 @@ struct Refused {};          // a Python error is set
 }
 
 constexpr unsigned kBf16 = 1u << CLEAVE_T_BF16, kF32 = 1u << CLEAVE_T_F32, kE4M3 = 1u << CLEAVE_T_E4M3, kFloats = kBf16 | kF32;
+constexpr unsigned kI32 = 1u << CLEAVE_T_I32, kTokens = kI32 | 1u << CLEAVE_T_I64;
 
 uint32_t type_of(const at::Tensor& t) {
     switch (t.scalar_type()) {
         case at::kBFloat16: return CLEAVE_T_BF16;
         case at::kFloat: return CLEAVE_T_F32;
         case at::kFloat8_e4m3fn: return CLEAVE_T_E4M3;
+        case at::kInt: return CLEAVE_T_I32;
+        case at::kLong: return CLEAVE_T_I64;
         default: return CLEAVE_T_NONE;
     }
 }
@@ -198,6 +201,164 @@ PyObject* run_act_backward(PyObject* const* a) {
     return PyLong_FromLong(cleave_act_backward(&d, ws, stream_of(a[8], dy)));
 }
 
+float number(PyObject* o) {
+    const float v = (float)PyFloat_AsDouble(o);
+    if (PyErr_Occurred()) throw Refused{};
+    return v;
+}
+bool truth(PyObject* o) {
+    const int v = PyObject_IsTrue(o);
+    if (v < 0) throw Refused{};
+    return v != 0;
+}
+void* required(const Vector& v, const char* name) {
+    if (!v.type) refuse(name, "a tensor is wanted");
+    return v.p;
+}
+
+PyObject* run_embedding(PyObject* const* a) {              // tokens, table, out, scale, stream
+    const at::Tensor &table = leading(a[1], "table"), &out = leading(a[2], "out");
+    const int64_t n = out.size(0), cols = table.size(1);
+    const Matrix mt = matrix(a[1], "table", table, table.size(0), cols, kFloats), mo = matrix(a[2], "out", table, n, cols, kFloats);
+    const Vector ids = vector(a[0], "tokens", table, n, kTokens);
+    cleave_embedding_t d = {};
+    d.n = (uint64_t)n; d.vocab = (uint32_t)table.size(0); d.cols = (uint32_t)cols;
+    d.id_type = ids.type; d.table_type = mt.type; d.out_type = mo.type; d.scale = number(a[3]);
+    d.ids = required(ids, "tokens"); d.table = mt.p; d.ldt = mt.ld; d.out = mo.p; d.ldo = mo.ld;
+    const c10::cuda::CUDAGuard guard(table.device());
+    return PyLong_FromLong(cleave_embedding(&d, stream_of(a[4], table)));
+}
+
+PyObject* run_embedding_backward(PyObject* const* a) {     // dy, tokens, dtable, scale, accumulate, workspace, stream
+    const at::Tensor &dy = leading(a[0], "dy"), &dt = leading(a[2], "dtable");
+    const int64_t n = dy.size(0), cols = dt.size(1);
+    const Matrix mt = matrix(a[2], "dtable", dt, dt.size(0), cols, kFloats), my = matrix(a[0], "dy", dt, n, cols, kFloats);
+    const Vector ids = vector(a[1], "tokens", dt, n, kTokens);
+    cleave_embedding_backward_t d = {};
+    d.n = (uint64_t)n; d.vocab = (uint32_t)dt.size(0); d.cols = (uint32_t)cols;
+    d.id_type = ids.type; d.dy_type = my.type; d.dtable_type = mt.type; d.scale = number(a[3]); d.accumulate = truth(a[4]);
+    d.ids = required(ids, "tokens"); d.dy = my.p; d.lddy = my.ld; d.dtable = mt.p; d.lddt = mt.ld;
+    at::Tensor hold;
+    void* ws = workspace(a[5], cleave_embedding_backward_workspace(d.n, d.vocab, d.cols), dt, hold);
+    const c10::cuda::CUDAGuard guard(dt.device());
+    return PyLong_FromLong(cleave_embedding_backward(&d, ws, stream_of(a[6], dt)));
+}
+
+PyObject* run_layernorm(PyObject* const* a) {              // x, weight, bias, y, residual, h, mean, rstd, scale, eps, stream
+    const at::Tensor& x = leading(a[0], "x");
+    const int64_t rows = x.size(0), cols = x.size(1);
+    const Matrix mx = matrix(a[0], "x", x, rows, cols, kFloats), my = matrix(a[3], "y", x, rows, cols, kFloats | kE4M3);
+    const Matrix mr = matrix(a[4], "residual", x, rows, cols, kFloats, true), mh = matrix(a[5], "h", x, rows, cols, kFloats, true);
+    const Vector w = vector(a[1], "weight", x, cols, kFloats), b = vector(a[2], "bias", x, cols, kFloats);
+    if (mh.type && mr.type && mh.type != mr.type) refuse("h", "the residual's type is wanted");
+    cleave_layernorm_t d = {};
+    d.rows = (uint64_t)rows; d.cols = (uint32_t)cols;
+    d.x_type = mx.type; d.r_type = mr.type; d.w_type = w.type; d.b_type = b.type; d.y_type = my.type; d.eps = number(a[9]);
+    d.x = mx.p; d.ldx = mx.ld; d.r = mr.p; d.ldr = mr.ld; d.h = mh.p; d.ldh = mh.ld; d.w = w.p; d.b = b.p; d.y = my.p; d.ldy = my.ld;
+    d.mean = static_cast<float*>(vector(a[6], "mean", x, rows, kF32).p);
+    d.rstd = static_cast<float*>(vector(a[7], "rstd", x, rows, kF32).p);
+    d.scale = static_cast<float*>(vector(a[8], "scale", x, rows, kF32).p);
+    const c10::cuda::CUDAGuard guard(x.device());
+    return PyLong_FromLong(cleave_layernorm(&d, stream_of(a[10], x)));
+}
+
+PyObject* run_layernorm_backward(PyObject* const* a) {     // dy, h, weight, mean, rstd, dx, dweight, dbias, dres, workspace, stream
+    const at::Tensor& h = leading(a[1], "h");
+    const int64_t rows = h.size(0), cols = h.size(1);
+    const Matrix mh = matrix(a[1], "h", h, rows, cols, kFloats), mdy = matrix(a[0], "dy", h, rows, cols, kFloats);
+    const Matrix mdx = matrix(a[5], "dx", h, rows, cols, 1u << mh.type), mr = matrix(a[8], "dres", h, rows, cols, 1u << mh.type, true);
+    const Vector w = vector(a[2], "weight", h, cols, kFloats);
+    cleave_layernorm_backward_t d = {};
+    d.rows = (uint64_t)rows; d.cols = (uint32_t)cols;
+    d.dy_type = mdy.type; d.h_type = mh.type; d.w_type = w.type;
+    d.dy = mdy.p; d.lddy = mdy.ld; d.h = mh.p; d.ldh = mh.ld; d.w = w.p; d.dres = mr.p; d.lddres = mr.ld; d.dx = mdx.p; d.lddx = mdx.ld;
+    d.mean = static_cast<const float*>(vector(a[3], "mean", h, rows, kF32).p);
+    d.rstd = static_cast<const float*>(vector(a[4], "rstd", h, rows, kF32).p);
+    d.dw = static_cast<float*>(vector(a[6], "dweight", h, cols, kF32).p);
+    d.db = static_cast<float*>(vector(a[7], "dbias", h, cols, kF32).p);
+    at::Tensor hold;
+    void* ws = a[6] != Py_None || a[7] != Py_None ? workspace(a[9], cleave_layernorm_backward_workspace(d.rows, d.cols), h, hold) : nullptr;
+    const c10::cuda::CUDAGuard guard(h.device());
+    return PyLong_FromLong(cleave_layernorm_backward(&d, ws, stream_of(a[10], h)));
+}
+
+// logits, tokens, logp, lse, entropy, top_values, top_index, scale, stream
+PyObject* run_logprobs(PyObject* const* a) {
+    const at::Tensor& x = leading(a[0], "logits");
+    const int64_t rows = x.size(0), cols = x.size(1);
+    const Matrix mx = matrix(a[0], "logits", x, rows, cols, kFloats);
+    const Vector ids = vector(a[1], "tokens", x, rows, kTokens), logp = vector(a[2], "logp", x, rows, kF32);
+    if (logp.type && !ids.type) refuse("tokens", "a tensor is wanted");
+    PyObject* shaped = a[6] != Py_None ? a[6] : a[5];
+    const int64_t top = shaped == Py_None ? 0 : leading(shaped, a[6] != Py_None ? "top_index" : "top_values").size(1);
+    const Matrix tv = matrix(a[5], "top_values", x, rows, top, kF32, true), ti = matrix(a[6], "top_index", x, rows, top, kI32, true);
+    if ((tv.type || ti.type) && top == 0) refuse(ti.type ? "top_index" : "top_values", "at least one column is wanted");
+    cleave_logprobs_t d = {};
+    d.rows = (uint64_t)rows; d.cols = (uint32_t)cols; d.x_type = mx.type; d.top = (uint32_t)top; d.scale = number(a[7]);
+    if (logp.type) { d.ids = ids.p; d.id_type = ids.type; }
+    d.x = mx.p; d.ldx = mx.ld;
+    d.logp = static_cast<float*>(logp.p);
+    d.lse = static_cast<float*>(vector(a[3], "lse", x, rows, kF32).p);
+    d.entropy = static_cast<float*>(vector(a[4], "entropy", x, rows, kF32).p);
+    d.top_values = static_cast<float*>(tv.p); d.ldtv = tv.ld; d.top_index = static_cast<int32_t*>(ti.p); d.ldti = ti.ld;
+    if (rows == 0) return PyLong_FromLong(0);                // (empty tensors have no addresses)
+    const c10::cuda::CUDAGuard guard(x.device());
+    return PyLong_FromLong(cleave_logprobs(&d, stream_of(a[8], x)));
+}
+
+// logits, tokens, lse, dlogits, dlogp, dlse, dentropy, entropy, scale, stream
+PyObject* run_logprobs_backward(PyObject* const* a) {
+    const at::Tensor& x = leading(a[0], "logits");
+    const int64_t rows = x.size(0), cols = x.size(1);
+    const Matrix mx = matrix(a[0], "logits", x, rows, cols, kFloats), md = matrix(a[3], "dlogits", x, rows, cols, kFloats);
+    const Vector ids = vector(a[1], "tokens", x, rows, kTokens), dlogp = vector(a[4], "dlogp", x, rows, kF32), dh = vector(a[6], "dentropy", x, rows, kF32),
+                 entropy = vector(a[7], "entropy", x, rows, kF32);
+    if (dlogp.type && !ids.type) refuse("tokens", "a tensor is wanted");
+    if (dh.type && !entropy.type) refuse("entropy", "a tensor is wanted");
+    cleave_logprobs_backward_t d = {};
+    d.rows = (uint64_t)rows; d.cols = (uint32_t)cols; d.x_type = mx.type; d.dx_type = md.type; d.scale = number(a[8]);
+    if (dlogp.type) { d.ids = ids.p; d.id_type = ids.type; }
+    d.x = mx.p; d.ldx = mx.ld; d.dx = md.p; d.lddx = md.ld;
+    d.lse = static_cast<const float*>(required(vector(a[2], "lse", x, rows, kF32), "lse"));
+    d.dlogp = static_cast<const float*>(dlogp.p);
+    d.dlse = static_cast<const float*>(vector(a[5], "dlse", x, rows, kF32).p);
+    d.dentropy = static_cast<const float*>(dh.p);
+    d.entropy = dh.type ? static_cast<const float*>(entropy.p) : nullptr;
+    if (rows == 0) return PyLong_FromLong(0);
+    const c10::cuda::CUDAGuard guard(x.device());
+    return PyLong_FromLong(cleave_logprobs_backward(&d, stream_of(a[9], x)));
+}
+
+cleave_distill_t distill_record(PyObject* logits, PyObject* index, PyObject* values, PyObject* lse, PyObject* scale, PyObject* normalize) {
+    const at::Tensor &x = leading(logits, "logits"), &at = leading(index, "index");
+    const int64_t rows = x.size(0), cols = x.size(1), k = at.size(1);
+    const Matrix mx = matrix(logits, "logits", x, rows, cols, kFloats), mi = matrix(index, "index", x, rows, k, kTokens), mv = matrix(values, "values", x, rows, k, kFloats);
+    cleave_distill_t d = {};
+    d.rows = (uint64_t)rows; d.cols = (uint32_t)cols; d.k = (uint32_t)k;
+    d.x_type = mx.type; d.index_type = mi.type; d.values_type = mv.type; d.normalize = truth(normalize); d.scale = number(scale);
+    d.x = mx.p; d.ldx = mx.ld; d.index = mi.p; d.ldindex = mi.ld; d.values = mv.p; d.ldvalues = mv.ld;
+    d.lse = static_cast<float*>(vector(lse, "lse", x, rows, kF32).p);
+    return d;
+}
+PyObject* run_distill(PyObject* const* a) {                // logits, index, values, loss, lse, scale, normalize, stream
+    cleave_distill_t d = distill_record(a[0], a[1], a[2], a[4], a[5], a[6]);
+    const at::Tensor& x = tensor(a[0], "logits");
+    d.loss = static_cast<float*>(required(vector(a[3], "loss", x, x.size(0), kF32), "loss"));
+    const c10::cuda::CUDAGuard guard(x.device());
+    return PyLong_FromLong(cleave_distill(&d, stream_of(a[7], x)));
+}
+PyObject* run_distill_backward(PyObject* const* a) {       // logits, index, values, lse, dloss, dlogits, scale, normalize, stream
+    cleave_distill_backward_t d = {};
+    d.f = distill_record(a[0], a[1], a[2], a[3], a[6], a[7]);
+    const at::Tensor& x = tensor(a[0], "logits");
+    if (a[3] == Py_None) refuse("lse", "a tensor is wanted");
+    d.dloss = static_cast<const float*>(required(vector(a[4], "dloss", x, x.size(0), kF32), "dloss"));
+    const Matrix m = matrix(a[5], "dlogits", x, x.size(0), x.size(1), kFloats);
+    d.dx = m.p; d.dx_type = m.type; d.lddx = m.ld;
+    const c10::cuda::CUDAGuard guard(x.device());
+    return PyLong_FromLong(cleave_distill_backward(&d, stream_of(a[8], x)));
+}
+
 // No C++ exception leaves a call: the ones above have set a Python error, torch's become one.
 template <PyObject* (*RUN)(PyObject* const*), int N>
 PyObject* call(PyObject*, PyObject* const* args, Py_ssize_t n) {
@@ -216,7 +377,10 @@ PyMethodDef method(const char* name) {
     return {name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(call<RUN, N>)), METH_FASTCALL, nullptr};
 }
 PyMethodDef methods[] = {method<run_rmsnorm, 9>("rmsnorm"), method<run_rmsnorm_backward, 9>("rmsnorm_backward"), method<run_quantize_rows, 4>("quantize_rows"),
-                         method<run_linear, 13>("linear"), method<run_act_backward, 9>("act_backward"), {nullptr, nullptr, 0, nullptr}};
+                         method<run_linear, 13>("linear"), method<run_act_backward, 9>("act_backward"),
+                         method<run_embedding, 5>("embedding"), method<run_embedding_backward, 7>("embedding_backward"), method<run_layernorm, 11>("layernorm"),
+                         method<run_layernorm_backward, 11>("layernorm_backward"), method<run_logprobs, 9>("logprobs"), method<run_logprobs_backward, 10>("logprobs_backward"),
+                         method<run_distill, 8>("distill"), method<run_distill_backward, 9>("distill_backward"), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", "Argument marshalling of the operators (see ops.py).", -1, methods};
 
 }  // namespace

@@ -6,6 +6,7 @@
 #include <vector>
 
 #include "ops.cuh"
+#include "tokens.cuh"
 
 using namespace cleave;
 
@@ -39,6 +40,9 @@ int cuda_code(cudaError_t e) {
     cudaGetLastError();
     return CLEAVE_E_CUDA;
 }
+// token numbers: `n` of them, `ld` apart from row to row where they have rows
+bool ids_ok(const void* p, uint32_t type) { return id_bytes(type) && p && aligned(p, id_bytes(type)); }
+bool scale_ok(float s) { return std::isfinite(s) && s > 0.f; }
 // SM count of the current device, or a negative CLEAVE_E_* code (asked for once per device)
 int need_device() {
     static std::atomic<int> known[64];
@@ -233,6 +237,116 @@ int cleave_act_backward(const cleave_act_backward_t* d, void* workspace, void* s
     }
     const int sms = need_device();
     return sms < 0 ? sms : cuda_code(launch_act_backward(*d, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
+}
+
+// ---- embedding -------------------------------------------------------------------------------------------
+int cleave_embedding(const cleave_embedding_t* d, void* stream) {
+    if (!d || !d->cols || !d->vocab || !std::isfinite(d->scale)) return CLEAVE_E_INVAL;
+    if (d->n == 0) return CLEAVE_OK;
+    if (d->n > kMaxRows || d->vocab > kMaxRows || d->cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
+    if (!ids_ok(d->ids, d->id_type) || !float_type(d->table_type) || !float_type(d->out_type) || !matrix_ok(d->table, d->table_type, d->ldt, d->cols) ||
+        !matrix_ok(d->out, d->out_type, d->ldo, d->cols)) return CLEAVE_E_INVAL;
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_embedding(*d, sms, static_cast<cudaStream_t>(stream)));
+}
+
+uint64_t cleave_embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols) { return embedding_backward_workspace(n, vocab, cols); }
+int cleave_embedding_backward(const cleave_embedding_backward_t* d, void* workspace, void* stream) {
+    if (!d || !d->cols || !d->vocab || !std::isfinite(d->scale) || d->accumulate > 1) return CLEAVE_E_INVAL;
+    if (d->n > kMaxRows || d->vocab > kMaxRows || d->cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
+    if (!float_type(d->dtable_type) || !matrix_ok(d->dtable, d->dtable_type, d->lddt, d->cols) || !workspace || !aligned(workspace, 16)) return CLEAVE_E_INVAL;
+    if (d->n && (!ids_ok(d->ids, d->id_type) || !float_type(d->dy_type) || !matrix_ok(d->dy, d->dy_type, d->lddy, d->cols))) return CLEAVE_E_INVAL;
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_embedding_backward(*d, workspace, static_cast<cudaStream_t>(stream)));
+}
+
+// ---- layer norm --------------------------------------------------------------------------------------------
+int cleave_layernorm(const cleave_layernorm_t* d, void* stream) {
+    if (!d || !d->cols || !(d->eps >= 0.f)) return CLEAVE_E_INVAL;
+    if (d->rows == 0) return CLEAVE_OK;
+    if (d->rows > kMaxRows || d->cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
+    if (!float_type(d->x_type) || !matrix_ok(d->x, d->x_type, d->ldx, d->cols)) return CLEAVE_E_INVAL;
+    if (!optional_ok(d->r, d->r_type, d->ldr, d->cols) || !optional_ok(d->w, d->w_type, d->cols, d->cols) || !optional_ok(d->b, d->b_type, d->cols, d->cols)) return CLEAVE_E_INVAL;
+    if (d->h && (!d->r || !matrix_ok(d->h, d->r_type, d->ldh, d->cols))) return CLEAVE_E_INVAL;
+    if (!matrix_ok(d->y, d->y_type, d->ldy, d->cols) || !aligned(d->mean, 4) || !aligned(d->rstd, 4)) return CLEAVE_E_INVAL;
+    if ((d->y_type == CLEAVE_T_E4M3) != (d->scale != nullptr) || !aligned(d->scale, 4)) return CLEAVE_E_INVAL;
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_layernorm(*d, sms, static_cast<cudaStream_t>(stream)));
+}
+
+uint64_t cleave_layernorm_backward_workspace(uint64_t rows, uint32_t cols) {
+    return (uint64_t)layernorm_backward_parts(rows, cols) * 2 * cols * sizeof(float);
+}
+int cleave_layernorm_backward(const cleave_layernorm_backward_t* d, void* workspace, void* stream) {
+    if (!d || !d->cols || !aligned(d->dw, 4) || !aligned(d->db, 4)) return CLEAVE_E_INVAL;
+    if (d->rows > kMaxRows || d->cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
+    if (d->rows) {
+        if (!float_type(d->dy_type) || !float_type(d->h_type) || !matrix_ok(d->dy, d->dy_type, d->lddy, d->cols) ||
+            !matrix_ok(d->h, d->h_type, d->ldh, d->cols) || !matrix_ok(d->dx, d->h_type, d->lddx, d->cols)) return CLEAVE_E_INVAL;
+        if (!optional_ok(d->w, d->w_type, d->cols, d->cols) || (d->dres && !matrix_ok(d->dres, d->h_type, d->lddres, d->cols))) return CLEAVE_E_INVAL;
+        if (!d->mean || !aligned(d->mean, 4) || !d->rstd || !aligned(d->rstd, 4)) return CLEAVE_E_INVAL;
+        if ((d->dw || d->db) && (!workspace || !aligned(workspace, 16))) return CLEAVE_E_INVAL;
+    }
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_layernorm_backward(*d, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream)));
+}
+
+// ---- log probabilities and distillation ---------------------------------------------------------------------
+int cleave_logprobs(const cleave_logprobs_t* d, void* stream) {
+    if (!d || !d->cols || !scale_ok(d->scale)) return CLEAVE_E_INVAL;
+    if (!d->logp && !d->lse && !d->entropy && !d->top_values && !d->top_index) return CLEAVE_E_INVAL;
+    if ((d->top != 0) != (d->top_values || d->top_index) || d->top > d->cols) return CLEAVE_E_INVAL;
+    if (d->rows > kMaxRows || d->cols > kMaxCols || d->top > CLEAVE_TOP_MOST) return CLEAVE_E_UNSUPPORTED;
+    if (d->rows == 0) return CLEAVE_OK;
+    if (!float_type(d->x_type) || !matrix_ok(d->x, d->x_type, d->ldx, d->cols)) return CLEAVE_E_INVAL;
+    if (d->logp ? !ids_ok(d->ids, d->id_type) : (d->ids || d->id_type)) return CLEAVE_E_INVAL;
+    if (!aligned(d->logp, 4) || !aligned(d->lse, 4) || !aligned(d->entropy, 4)) return CLEAVE_E_INVAL;
+    if ((d->top_values && !matrix_ok(d->top_values, CLEAVE_T_F32, d->ldtv, d->top)) || (d->top_index && !matrix_ok(d->top_index, CLEAVE_T_F32, d->ldti, d->top))) return CLEAVE_E_INVAL;
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_logprobs(*d, sms, static_cast<cudaStream_t>(stream)));
+}
+int cleave_logprobs_backward(const cleave_logprobs_backward_t* d, void* stream) {
+    if (!d || !d->cols || !scale_ok(d->scale)) return CLEAVE_E_INVAL;
+    if (!d->dlogp && !d->dlse && !d->dentropy) return CLEAVE_E_INVAL;
+    if (d->rows > kMaxRows || d->cols > kMaxCols) return CLEAVE_E_UNSUPPORTED;
+    if (d->rows == 0) return CLEAVE_OK;
+    if (!float_type(d->x_type) || !matrix_ok(d->x, d->x_type, d->ldx, d->cols) || !float_type(d->dx_type) || !matrix_ok(d->dx, d->dx_type, d->lddx, d->cols)) return CLEAVE_E_INVAL;
+    if (d->dlogp ? !ids_ok(d->ids, d->id_type) : (d->ids || d->id_type)) return CLEAVE_E_INVAL;
+    if (!d->lse || !aligned(d->lse, 4) || !aligned(d->entropy, 4) || (d->dentropy != nullptr) != (d->entropy != nullptr)) return CLEAVE_E_INVAL;
+    if (!aligned(d->dlogp, 4) || !aligned(d->dlse, 4) || !aligned(d->dentropy, 4)) return CLEAVE_E_INVAL;
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_logprobs_backward(*d, sms, static_cast<cudaStream_t>(stream)));
+}
+
+}  // extern "C"
+
+static int distill_ok(const cleave_distill_t& d) {
+    if (!d.cols || !d.k || !scale_ok(d.scale) || d.normalize > 1) return CLEAVE_E_INVAL;
+    if (d.rows > kMaxRows || d.cols > kMaxCols || d.k > CLEAVE_DISTILL_MOST) return CLEAVE_E_UNSUPPORTED;
+    if (d.rows == 0) return CLEAVE_OK;
+    if (!float_type(d.x_type) || !matrix_ok(d.x, d.x_type, d.ldx, d.cols)) return CLEAVE_E_INVAL;
+    if (!ids_ok(d.index, d.index_type) || d.ldindex < d.k || d.ldindex > kMaxLd) return CLEAVE_E_INVAL;
+    if (!float_type(d.values_type) || !matrix_ok(d.values, d.values_type, d.ldvalues, d.k) || !aligned(d.loss, 4) || !aligned(d.lse, 4)) return CLEAVE_E_INVAL;
+    return CLEAVE_OK;
+}
+
+extern "C" {
+
+int cleave_distill(const cleave_distill_t* d, void* stream) {
+    if (!d) return CLEAVE_E_INVAL;
+    const int rc = distill_ok(*d);
+    if (rc != CLEAVE_OK || d->rows == 0) return rc;
+    if (!d->loss) return CLEAVE_E_INVAL;
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_distill(*d, sms, static_cast<cudaStream_t>(stream)));
+}
+int cleave_distill_backward(const cleave_distill_backward_t* d, void* stream) {
+    if (!d) return CLEAVE_E_INVAL;
+    const int rc = distill_ok(d->f);
+    if (rc != CLEAVE_OK || d->f.rows == 0) return rc;
+    if (!d->f.lse || !d->dloss || !aligned(d->dloss, 4) || !float_type(d->dx_type) || !matrix_ok(d->dx, d->dx_type, d->lddx, d->f.cols)) return CLEAVE_E_INVAL;
+    const int sms = need_device();
+    return sms < 0 ? sms : cuda_code(launch_distill_backward(*d, sms, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -60,6 +60,49 @@ class _ActBackward(C.Structure):
                 ("mul", _vp), ("ldmul", _u64), ("dz", _vp), ("lddz", _u64), ("dmul", _vp), ("lddmul", _u64), ("dbias", _vp)]
 
 
+class _Embedding(C.Structure):
+    _fields_ = [("n", _u64), ("vocab", _u32), ("cols", _u32), ("id_type", _u32), ("table_type", _u32), ("out_type", _u32), ("scale", _f),
+                ("ids", _vp), ("table", _vp), ("ldt", _u64), ("out", _vp), ("ldo", _u64)]
+
+
+class _EmbeddingBackward(C.Structure):
+    _fields_ = [("n", _u64), ("vocab", _u32), ("cols", _u32), ("id_type", _u32), ("dy_type", _u32), ("dtable_type", _u32),
+                ("accumulate", _u32), ("scale", _f), ("pad_", _u32), ("ids", _vp), ("dy", _vp), ("lddy", _u64), ("dtable", _vp), ("lddt", _u64)]
+
+
+class _Layernorm(C.Structure):
+    _fields_ = [("rows", _u64), ("cols", _u32), ("x_type", _u32), ("r_type", _u32), ("w_type", _u32), ("b_type", _u32), ("y_type", _u32),
+                ("eps", _f), ("pad_", _u32), ("x", _vp), ("ldx", _u64), ("r", _vp), ("ldr", _u64), ("h", _vp), ("ldh", _u64), ("w", _vp), ("b", _vp),
+                ("y", _vp), ("ldy", _u64), ("mean", _vp), ("rstd", _vp), ("scale", _vp)]
+
+
+class _LayernormBackward(C.Structure):
+    _fields_ = [("rows", _u64), ("cols", _u32), ("dy_type", _u32), ("h_type", _u32), ("w_type", _u32), ("pad_", _u32),
+                ("dy", _vp), ("lddy", _u64), ("h", _vp), ("ldh", _u64), ("w", _vp), ("mean", _vp), ("rstd", _vp), ("dres", _vp), ("lddres", _u64),
+                ("dx", _vp), ("lddx", _u64), ("dw", _vp), ("db", _vp)]
+
+
+class _Logprobs(C.Structure):
+    _fields_ = [("rows", _u64), ("cols", _u32), ("x_type", _u32), ("id_type", _u32), ("top", _u32), ("scale", _f), ("pad_", _u32), ("x", _vp),
+                ("ldx", _u64), ("ids", _vp), ("logp", _vp), ("lse", _vp), ("entropy", _vp), ("top_values", _vp), ("ldtv", _u64), ("top_index", _vp),
+                ("ldti", _u64)]
+
+
+class _LogprobsBackward(C.Structure):
+    _fields_ = [("rows", _u64), ("cols", _u32), ("x_type", _u32), ("id_type", _u32), ("dx_type", _u32), ("scale", _f), ("pad_", _u32), ("x", _vp),
+                ("ldx", _u64), ("ids", _vp), ("lse", _vp), ("entropy", _vp), ("dlogp", _vp), ("dlse", _vp), ("dentropy", _vp), ("dx", _vp), ("lddx", _u64)]
+
+
+class _Distill(C.Structure):
+    _fields_ = [("rows", _u64), ("cols", _u32), ("k", _u32), ("x_type", _u32), ("index_type", _u32), ("values_type", _u32), ("normalize", _u32),
+                ("scale", _f), ("pad_", _u32), ("x", _vp), ("ldx", _u64), ("index", _vp), ("ldindex", _u64), ("values", _vp), ("ldvalues", _u64),
+                ("loss", _vp), ("lse", _vp)]
+
+
+class _DistillBackward(C.Structure):
+    _fields_ = [("f", _Distill), ("dloss", _vp), ("dx_type", _u32), ("pad_", _u32), ("dx", _vp), ("lddx", _u64)]
+
+
 _sig = {
     "cleave_adamw_create": (_i, [C.POINTER(_AdamwTensor), _u32, _u32, _u32, C.POINTER(_vp)]),
     "cleave_adamw_set_grads": (_i, [_vp, _vp, _vp]),
@@ -74,6 +117,16 @@ _sig = {
     "cleave_linear_set_wait_limit_ns": (None, [_u64]),
     "cleave_act_backward_workspace": (_u64, [_u64, _u32]),
     "cleave_act_backward": (_i, [C.POINTER(_ActBackward), _vp, _vp]),
+    "cleave_embedding": (_i, [C.POINTER(_Embedding), _vp]),
+    "cleave_embedding_backward_workspace": (_u64, [_u64, _u32, _u32]),
+    "cleave_embedding_backward": (_i, [C.POINTER(_EmbeddingBackward), _vp, _vp]),
+    "cleave_layernorm": (_i, [C.POINTER(_Layernorm), _vp]),
+    "cleave_layernorm_backward_workspace": (_u64, [_u64, _u32]),
+    "cleave_layernorm_backward": (_i, [C.POINTER(_LayernormBackward), _vp, _vp]),
+    "cleave_logprobs": (_i, [C.POINTER(_Logprobs), _vp]),
+    "cleave_logprobs_backward": (_i, [C.POINTER(_LogprobsBackward), _vp]),
+    "cleave_distill": (_i, [C.POINTER(_Distill), _vp]),
+    "cleave_distill_backward": (_i, [C.POINTER(_DistillBackward), _vp]),
 }
 for _name, (_res, _args) in _sig.items():
     _fn = getattr(lib, _name)
@@ -264,3 +317,87 @@ def act_backward(dy, z, dz=None, *, act: str = "none", mul=None, dmul=None, dbia
     code = _marshal.act_backward(dy, z, dz, _act_code(act), mul, dmul, dbias, workspace, _raw(stream))
     if code:
         _check(code, "cleave_act_backward")
+
+
+def embedding(tokens, table, out, *, scale: float = 1.0, stream=None) -> None:
+    """cleave_embedding: out[i] = scale * table[tokens[i]]; a token outside of the table is padding and gives zeros.
+
+    tokens: int32 or int64 [n]; table [vocab, cols], out [n, cols]: bf16 or fp32."""
+    code = _marshal.embedding(tokens, table, out, scale, _raw(stream))
+    if code:
+        _check(code, "cleave_embedding")
+
+
+def embedding_backward_workspace(n: int, vocab: int, cols: int) -> int:
+    return lib.cleave_embedding_backward_workspace(n, vocab, cols)
+
+
+def embedding_backward(dy, tokens, dtable, *, scale: float = 1.0, accumulate: bool = False, workspace=None, stream=None) -> None:
+    """cleave_embedding_backward: dtable[v] = scale * (sum of the rows of dy whose token is v), rows of tokens that do not occur
+    become 0; with `accumulate` that is added to dtable and other rows are not touched (a table that is tied to the
+    output projection).  dy [n, cols], dtable [vocab, cols]: bf16 or fp32."""
+    if stream is not None:
+        workspace = _workspace(workspace, embedding_backward_workspace(dy.shape[0], *dtable.shape), dtable, stream)
+    code = _marshal.embedding_backward(dy, tokens, dtable, scale, accumulate, workspace, _raw(stream))
+    if code:
+        _check(code, "cleave_embedding_backward")
+
+
+def layernorm(x, weight, bias, y, *, residual=None, h=None, mean=None, rstd=None, scale=None, eps: float = 1e-5, stream=None) -> None:
+    """cleave_layernorm: h = x + residual, y = (h - mean(h)) / sqrt(var(h) + eps) * weight + bias, row by row.
+
+    Operands as in rmsnorm; bias [cols] or None; mean, rstd: fp32 [rows] or None (what the backward pass needs)."""
+    code = _marshal.layernorm(x, weight, bias, y, residual, h, mean, rstd, scale, eps, _raw(stream))
+    if code:
+        _check(code, "cleave_layernorm")
+
+
+def layernorm_backward_workspace(rows: int, cols: int) -> int:
+    return lib.cleave_layernorm_backward_workspace(rows, cols)
+
+
+def layernorm_backward(dy, h, weight, mean, rstd, dx, dweight=None, dbias=None, *, dres=None, workspace=None, stream=None) -> None:
+    """cleave_layernorm_backward: dx (the gradient of x and of the residual alike), dweight and dbias (fp32, or None) from the
+    saved h, mean and rstd; `dres`, of h's type, is the gradient that reaches h from the residual stream."""
+    if (dweight is not None or dbias is not None) and stream is not None:
+        workspace = _workspace(workspace, layernorm_backward_workspace(*h.shape), h, stream)
+    code = _marshal.layernorm_backward(dy, h, weight, mean, rstd, dx, dweight, dbias, dres, workspace, _raw(stream))
+    if code:
+        _check(code, "cleave_layernorm_backward")
+
+
+def token_logprobs(logits, tokens=None, logp=None, *, lse=None, entropy=None, top_values=None, top_index=None, scale: float = 1.0, stream=None) -> None:
+    """cleave_logprobs: from one reading of the rows of logits (bf16 or fp32 [rows, vocab]), with p = softmax(scale * logits):
+    logp = log p of each row's token (0 for a token outside of the vocabulary: padding), lse = log(sum(exp(scale * logits))),
+    entropy of p: fp32 [rows]; the best places top_index (int32) and their log p top_values (fp32), [rows, top], best first and
+    of equal ones the lowest place first.  tokens: int32 or int64 [rows]; logp needs them.  What is None is not computed."""
+    code = _marshal.logprobs(logits, tokens, logp, lse, entropy, top_values, top_index, scale, _raw(stream))
+    if code:
+        _check(code, "cleave_logprobs")
+
+
+def token_logprobs_backward(logits, tokens, lse, dlogits, *, dlogp=None, dlse=None, dentropy=None, entropy=None, scale: float = 1.0, stream=None) -> None:
+    """cleave_logprobs_backward: dlogits (bf16 or fp32, may be logits itself) from the gradients of logp, lse and entropy (fp32
+    [rows] each, or None); `entropy`, as token_logprobs gave it, goes with dentropy, tokens with dlogp.
+    The mean cross entropy of n tokens has dlogp = -1 / n."""
+    code = _marshal.logprobs_backward(logits, tokens, lse, dlogits, dlogp, dlse, dentropy, entropy, scale, _raw(stream))
+    if code:
+        _check(code, "cleave_logprobs_backward")
+
+
+def distill(logits, index, values, loss, *, lse=None, scale: float = 1.0, normalize: bool = True, stream=None) -> None:
+    """cleave_distill: loss[i] = sum_k q_k (log q_k - log p[index_k]), p = softmax(scale * logits[i]); q = softmax(scale * values[i])
+    over the row's k entries or, without `normalize`, exp(scale * values[i]).
+
+    logits: bf16 or fp32 [rows, vocab]; index: int32 or int64 [rows, k], entries outside of the vocabulary are empty; values:
+    bf16 or fp32 [rows, k]; loss, lse (what the backward pass needs): fp32 [rows]."""
+    code = _marshal.distill(logits, index, values, loss, lse, scale, normalize, _raw(stream))
+    if code:
+        _check(code, "cleave_distill")
+
+
+def distill_backward(logits, index, values, lse, dloss, dlogits, *, scale: float = 1.0, normalize: bool = True, stream=None) -> None:
+    """cleave_distill_backward: dlogits (bf16 or fp32, may be logits itself) from dloss (fp32 [rows]) and the saved lse."""
+    code = _marshal.distill_backward(logits, index, values, lse, dloss, dlogits, scale, normalize, _raw(stream))
+    if code:
+        _check(code, "cleave_distill_backward")
