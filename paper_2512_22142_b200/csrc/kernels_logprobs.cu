@@ -1,7 +1,16 @@
 // Log probabilities of given tokens with entropy and top alternatives, distillation from a teacher's top scores, and the
 // backward passes of both (see cleave.h).
+//
+// Forward: one reading of the scores.  A thread keeps a largest score m and, relative to it, s = sum 2^a and t = sum 2^a a
+// with a = scale log2(e) (x - m); a larger score rescales both.  lse = scale m + ln 2 log2(s), entropy = ln 2 (log2(s) - t / s).
+// The top places go through a threshold that only rises: a score below it is dropped after one comparison (shared by 16
+// bytes of scores), the others are collected by warp and cut to the best `top` when a warp's room is full.
+// A row goes to one CTA, or with few rows to a cluster of them, joined through distributed shared memory.
+// Backward: each element from its score and the row's lse; one reading, one writing.
 #include <algorithm>
+#include <type_traits>
 
+#include "ptx.cuh"
 #include "rows.cuh"
 #include "tokens.cuh"
 
@@ -9,84 +18,346 @@ namespace cleave {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMasked = -0x1p126f;             // a row whose largest score is not above this has nothing left
-constexpr uint32_t kScoreThreads = 256;
+constexpr uint32_t kScoreThreads = 256, kScoreWarps = kScoreThreads / 32;
 
+// ---- order of scores -----------------------------------------------------------------------------------
 // whole number that orders like a score: NaN above all, +0 and -0 alike
 __device__ __forceinline__ uint32_t score_order(float x) {
     const uint32_t b = __float_as_uint(x + 0.f);
     return x != x ? 0xFFFFFFFFu : (b & 0x80000000u ? ~b : b | 0x80000000u);
 }
+__device__ __forceinline__ float order_score(uint32_t o) { return __uint_as_float(o & 0x80000000u ? o & 0x7FFFFFFFu : ~o); }       // (NaN: some NaN)
 // score, then the lower place: larger is better, no two alike, none 0 or all ones
 __device__ __forceinline__ uint64_t candidate(float x, uint32_t j) { return (uint64_t)score_order(x) << 32 | (0x7FFFFFFFu - j); }
 __device__ __forceinline__ uint32_t place_of(uint64_t c) { return 0x7FFFFFFFu - (uint32_t)c; }
+__device__ __forceinline__ float score_of(uint64_t c) { return (uint32_t)(c >> 32) == 0xFFFFFFFFu ? __uint_as_float(0x7FFFFFFFu) : order_score((uint32_t)(c >> 32)); }
 
-struct RowSums { float top, sum, mean; };        // largest score; sum of e = exp(s (x - top)); sum of e s (x - top)
-
-template <typename F>
-__device__ __forceinline__ float cta_reduce(float v, float* buf, F&& f) {       // buf: one value a warp; ends with a barrier
-#pragma unroll
-    for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    if ((threadIdx.x & 31u) == 0) buf[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = buf[0];
-    for (uint32_t w = 1; w < blockDim.x / 32; ++w) v = f(v, buf[w]);
-    __syncthreads();
-    return v;
+// ---- sums of a row ---------------------------------------------------------------------------------------
+struct Sums {                       // m: largest score (a NaN stays); ref = c m of the exponents (0 while nothing is above kMasked)
+    float m, ref, s, t;
+};
+__device__ __forceinline__ float reference(float m, float c) { return m <= kMasked ? 0.f : m * c; }
+// the same sums relative to another largest score (which is not below the old one)
+__device__ __forceinline__ void raise(Sums& a, float m, float c) {
+    const float ref = reference(m, c), d = a.ref - ref, f = a.s == 0.f ? 0.f : exp2_fast(d);
+    a.t = a.s == 0.f ? 0.f : f * fmaf(d, a.s, a.t);
+    a.s *= f;
+    a.m = m;
+    a.ref = ref;
 }
-__device__ __forceinline__ RowSums row_sums_any(const void* x, uint32_t type, uint64_t at, uint32_t cols, float scale, float* buf) {
-    RowSums r = {-INFINITY, 0.f, 0.f};
-    for (uint32_t j = threadIdx.x; j < cols; j += blockDim.x) r.top = max_nan(r.top, load_as(x, type, at + j));
-    r.top = cta_reduce(r.top, buf, [](float a, float b) { return max_nan(a, b); });
-    if (r.top <= kMasked) return r;
-    for (uint32_t j = threadIdx.x; j < cols; j += blockDim.x) {
-        const float d = scale * (load_as(x, type, at + j) - r.top), e = exp2_fast(d * kLog2e);
-        r.sum += e;
-        if (e != 0.f) r.mean = fmaf(e, d, r.mean);
-    }
-    r.sum = cta_sum(r.sum, buf);
-    r.mean = cta_sum(r.mean, buf);
+__device__ __forceinline__ float warp_max_nan(float v) {
+    float r;
+    asm volatile("redux.sync.max.NaN.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
     return r;
 }
-__device__ __forceinline__ float row_lse(const RowSums& r, float scale) { return r.top <= kMasked ? -INFINITY : fmaf(scale, r.top, logf(r.sum)); }
-
-__global__ void __launch_bounds__(kScoreThreads) logprobs_any_kernel(const __grid_constant__ cleave_logprobs_t d) {
-    __shared__ float buf[32];
-    __shared__ unsigned long long best;
-    begin_chained();
-    const uint64_t row = blockIdx.x, at = row * d.ldx;
-    const RowSums r = row_sums_any(d.x, d.x_type, at, d.cols, d.scale, buf);
-    const float lse = row_lse(r, d.scale);
-    const bool nothing = r.top <= kMasked;
-    if (threadIdx.x == 0) {
-        if (d.lse) d.lse[row] = lse;
-        if (d.entropy) d.entropy[row] = nothing ? 0.f : logf(r.sum) - r.mean / r.sum;
-        if (d.logp) {
-            const int32_t t = load_token(d.ids, d.id_type, row, d.cols);
-            d.logp[row] = t < 0 ? 0.f : (nothing ? -INFINITY : fmaf(d.scale, load_as(d.x, d.x_type, at + t), -lse));
-        }
-    }
-    uint64_t last = ~0ull;                                       // the best candidate of each round is the best below the last one
-    for (uint32_t k = 0; k < d.top; ++k) {
-        if (threadIdx.x == 0) best = 0;
-        __syncthreads();
-        unsigned long long mine = 0;
-        for (uint32_t j = threadIdx.x; j < d.cols; j += blockDim.x) {
-            const uint64_t c = candidate(load_as(d.x, d.x_type, at + j), j);
-            if (c < last && c > mine) mine = c;
-        }
-        atomicMax(&best, mine);
-        __syncthreads();
-        last = best;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            const uint32_t j = place_of(last);
-            if (d.top_index) d.top_index[row * d.ldti + k] = (int32_t)j;
-            if (d.top_values) d.top_values[row * d.ldtv + k] = nothing ? -INFINITY : fmaf(d.scale, load_as(d.x, d.x_type, at + j), -lse);
-        }
-    }
+template <bool ENT>
+__device__ __forceinline__ Sums warp_join(Sums a, float c) {
+    raise(a, warp_max_nan(a.m), c);
+    a.s = warp_sum(a.s);
+    if (ENT) a.t = warp_sum(a.t);
+    return a;
 }
-cudaError_t launch_logprobs(const cleave_logprobs_t& d, int, cudaStream_t st) {
-    return launch_chained(logprobs_any_kernel, (unsigned)d.rows, kScoreThreads, 0, st, d);
+__device__ __forceinline__ Sums nothing() { return {-INFINITY, 0.f, 0.f, 0.f}; }
+// a row's results; `ok` is false for a row with a NaN or +infinity
+struct Stats { float lse, entropy; };
+__device__ __forceinline__ Stats stats_of(const Sums& a, float scale, float c) {
+    if (a.m <= kMasked) return {-INFINITY, 0.f};
+    if (!(a.m < INFINITY)) return {__uint_as_float(0x7FFFFFFFu), __uint_as_float(0x7FFFFFFFu)};
+    const float bits = log2f(a.s);
+    // (ref is c m rounded: what that left out goes to the sum)
+    return {fmaf(scale, a.m, kLn2 * (bits + fmaf(-a.m, c, a.ref))), fmaxf(kLn2 * (bits - a.t / a.s), 0.f)};
+}
+
+// ---- 16 bytes of scores ------------------------------------------------------------------------------------
+template <typename T> constexpr int kUnit = 16 / sizeof(T);
+__device__ __forceinline__ float2 pair_of(const uint4& w, int i, float) { return i == 0 ? make_float2(__uint_as_float(w.x), __uint_as_float(w.y)) : make_float2(__uint_as_float(w.z), __uint_as_float(w.w)); }
+__device__ __forceinline__ float2 pair_of(const uint4& w, int i, __nv_bfloat16) {
+    const uint32_t v = i == 0 ? w.x : (i == 1 ? w.y : (i == 2 ? w.z : w.w));
+    return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xFFFF0000u));
+}
+__device__ __forceinline__ float unit_max(const uint4& w, float) {
+    return max_nan(max_nan(__uint_as_float(w.x), __uint_as_float(w.y)), max_nan(__uint_as_float(w.z), __uint_as_float(w.w)));
+}
+__device__ __forceinline__ float unit_max(const uint4& w, __nv_bfloat16) {
+    auto two = [](uint32_t a, uint32_t b) { uint32_t r; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; };
+    const uint32_t m = two(two(w.x, w.y), two(w.z, w.w));
+    return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+}
+template <typename T> __device__ __forceinline__ uint4 masked_unit() {
+    const uint32_t v = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+    return make_uint4(v, v, v, v);
+}
+__device__ __forceinline__ uint4 load_unit(const void* p) {      // (not kept in L1; L2 may serve the backward pass)
+    uint4 r;
+    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
+    return r;
+}
+
+// ---- the best places -----------------------------------------------------------------------------------------
+constexpr uint32_t kRoom = 128;                  // candidates a warp collects before it cuts them to the best
+struct TopRoom {
+    alignas(16) uint32_t first[kScoreThreads];   // (read 16 bytes at a time)
+    uint64_t room[kScoreWarps][kRoom];
+    uint64_t pool[kScoreWarps * CLEAVE_TOP_MOST];
+    uint64_t best[CLEAVE_TOP_MOST];
+    unsigned long long bar;                      // no candidate up to this one is among the best
+};
+// the warp's n candidates cut to the best k, best first; returns how many there are
+__device__ __forceinline__ uint32_t cut(uint64_t* room, uint32_t n, uint32_t k) {
+    const uint32_t lane = threadIdx.x & 31u;
+    uint64_t c[kRoom / 32];
+    uint32_t rank[kRoom / 32];
+    __syncwarp();
+#pragma unroll
+    for (uint32_t i = 0; i < kRoom / 32; ++i) { c[i] = lane + 32 * i < n ? room[lane + 32 * i] : 0; rank[i] = 0; }
+    for (uint32_t j = 0; j < n; ++j) {
+        const uint64_t o = room[j];
+#pragma unroll
+        for (uint32_t i = 0; i < kRoom / 32; ++i) rank[i] += o > c[i];
+    }
+    __syncwarp();
+#pragma unroll
+    for (uint32_t i = 0; i < kRoom / 32; ++i)
+        if (c[i] && rank[i] < k) room[rank[i]] = c[i];
+    __syncwarp();
+    return min(n, k);
+}
+// the best k of a pool of n (zeros do not count) into best[0 .. k), zeros behind them; all threads of the CTA
+__device__ __forceinline__ void pick(const uint64_t* pool, uint32_t n, uint64_t* best, uint32_t k) {
+    if (threadIdx.x < k) best[threadIdx.x] = 0;
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < n; e += kScoreThreads) {
+        const uint64_t c = pool[e];
+        if (!c) continue;
+        uint32_t rank = 0;
+        for (uint32_t j = 0; j < n; ++j) rank += pool[j] > c;
+        if (rank < k) best[rank] = c;
+    }
+    __syncthreads();
+}
+
+// ---- forward ---------------------------------------------------------------------------------------------------
+constexpr int kSteps = 4;                        // units a thread has in flight
+
+// The CTA's part (rank `part` of `parts`) of a row: its sums, joined over the CTA (every thread receives them), and with TOP its
+// best `top` candidates in room->best.
+template <typename T, bool ENT, bool TOP>
+__device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uint32_t part, uint32_t parts, Sums* warps, TopRoom* top_room, uint32_t top) {
+    constexpr int V = kUnit<T>;
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
+    // the row's units stand on 16 bytes; what is before them and behind them (less than a unit each) goes to threads of
+    // the first and the last part
+    const uint32_t head = min(cols, (uint32_t)((0u - (uint32_t)(uintptr_t)x) % 16u) / (uint32_t)sizeof(T)), units = (cols - head) / V, tail = cols - head - units * V;
+    const uint32_t each = (units + parts - 1) / parts, begin = min(units, part * each), end = min(units, begin + each);
+    const T* body = x + head;
+    uint32_t edge = cols;                                        // the place of this thread's single score
+    if (part == 0 && tid < head) edge = tid;
+    if (part == parts - 1 && tid >= 32u && tid - 32u < tail) edge = cols - tail + (tid - 32u);
+    float lone = -INFINITY;
+    uint4 w[kSteps];
+    auto fetch = [&](uint32_t u) {
+#pragma unroll
+        for (int q = 0; q < kSteps; ++q) w[q] = u + q * kScoreThreads < end ? load_unit(body + (uint64_t)(u + q * kScoreThreads) * V) : masked_unit<T>();
+    };
+    fetch(begin + tid);
+    if (edge < cols) lone = to_f32(x[edge]);
+
+    Sums a = nothing();
+    F2 s2[2] = {f2(0.f, 0.f), f2(0.f, 0.f)}, t2[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+    const F2 c2 = f2(c, c);
+    uint32_t held = 0;                                           // TOP: candidates in the warp's room
+    uint64_t bar = 0;
+    float bar_score = -INFINITY;
+    uint64_t* room = TOP ? top_room->room[warp] : nullptr;
+    auto see_bar = [&](uint64_t b) { bar = b; bar_score = b ? score_of(b) : -INFINITY; };
+    auto offer = [&](bool live, float v, uint32_t j) {           // all lanes of the warp
+        const uint64_t k = candidate(v, j);
+        const bool good = live && k > bar;
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, good);
+        if (!some) return;
+        if (good) room[held + __popc(some & ((1u << lane) - 1u))] = k;
+        held += __popc(some);
+        if (held > kRoom - 32) {
+            held = cut(room, held, top);
+            if (held == top) {
+                if (lane == 0) atomicMax(&top_room->bar, (unsigned long long)(room[top - 1] - 1));
+                if (room[top - 1] - 1 > bar) see_bar(room[top - 1] - 1);
+            }
+            __syncwarp();
+        }
+    };
+    if (TOP) {
+        // A first threshold: every thread has a score that is not below its largest of the first units, so `top` threads with a
+        // largest one of at least v mean that nothing below v is among the best.
+        float v = lone;
+        bool any = edge < cols;
+#pragma unroll
+        for (int q = 0; q < kSteps; ++q) { v = max_nan(v, unit_max(w[q], T())); any = any || begin + tid + q * kScoreThreads < end; }
+        const uint32_t mine = any ? score_order(v) : 0u;
+        if (tid == 0) top_room->bar = 0;
+        top_room->first[tid] = mine;
+        __syncthreads();
+        uint32_t rank = 0;
+#pragma unroll 8
+        for (uint32_t i = 0; i < kScoreThreads; i += 4) {
+            const uint4 o = *reinterpret_cast<const uint4*>(top_room->first + i);
+            rank += (o.x > mine || (o.x == mine && i < tid)) + (o.y > mine || (o.y == mine && i + 1 < tid)) + (o.z > mine || (o.z == mine && i + 2 < tid)) +
+                    (o.w > mine || (o.w == mine && i + 3 < tid));
+        }
+        if (rank == top - 1) top_room->bar = (unsigned long long)mine << 32;     // (below every candidate of that score)
+        __syncthreads();
+        see_bar(top_room->bar);
+        offer(edge < cols, lone, edge);
+    }
+    if (edge < cols) {
+        raise(a, lone, c);
+        a.s = lone <= kMasked ? 0.f : 1.f;                       // 2^0 at its own reference
+    }
+    for (uint32_t u = begin; u < end; u += kScoreThreads * kSteps) {             // (the same number of steps for every thread)
+        uint4 now[kSteps];
+#pragma unroll
+        for (int q = 0; q < kSteps; ++q) now[q] = w[q];
+        if (u + kScoreThreads * kSteps < end) fetch(u + kScoreThreads * kSteps + tid);
+        float most[kSteps], m = -INFINITY;
+#pragma unroll
+        for (int q = 0; q < kSteps; ++q) { most[q] = unit_max(now[q], T()); m = max_nan(m, most[q]); }
+        if (!(m <= a.m)) {
+            const float2 s0 = halves(add2(s2[0], s2[1])), t0 = halves(add2(t2[0], t2[1]));
+            a.s += s0.x + s0.y;
+            a.t += t0.x + t0.y;
+            raise(a, max_nan(a.m, m), c);
+            s2[0] = s2[1] = t2[0] = t2[1] = f2(0.f, 0.f);
+        }
+        const F2 r2 = f2(-a.ref, -a.ref);
+#pragma unroll
+        for (int q = 0; q < kSteps; ++q)
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) {
+                const float2 p = pair_of(now[q], i, T());
+                F2 e2 = fma2(f2(p.x, p.y), c2, r2);
+                float2 e = halves(e2);
+                if (ENT) { e.x = fmaxf(e.x, -200.f); e.y = fmaxf(e.y, -200.f); e2 = f2(e.x, e.y); }      // (2^-200 is 0: a masked place adds 0 to t)
+                const F2 p2 = f2(exp2_fast(e.x), exp2_fast(e.y));
+                s2[i & 1] = add2(s2[i & 1], p2);
+                if (ENT) t2[i & 1] = fma2(p2, e2, t2[i & 1]);
+            }
+        if (TOP) {
+            const uint64_t b = *static_cast<volatile unsigned long long*>(&top_room->bar);
+            if (b > bar) see_bar(b);
+#pragma unroll
+            for (int q = 0; q < kSteps; ++q) {
+                const uint32_t at = u + tid + q * kScoreThreads;
+                if (!__any_sync(0xFFFFFFFFu, at < end && !(most[q] < bar_score))) continue;
+#pragma unroll
+                for (int i = 0; i < V / 2; ++i) {
+                    const float2 p = pair_of(now[q], i, T());
+                    offer(at < end, p.x, head + at * V + 2 * i);
+                    offer(at < end, p.y, head + at * V + 2 * i + 1);
+                }
+            }
+        }
+    }
+    const float2 s0 = halves(add2(s2[0], s2[1])), t0 = halves(add2(t2[0], t2[1]));
+    a.s += s0.x + s0.y;
+    a.t += t0.x + t0.y;
+    a = warp_join<ENT>(a, c);
+    if (lane == 0) warps[warp] = a;
+    if (TOP) {
+        held = cut(room, held, top);
+        for (uint32_t i = lane; i < top; i += 32) top_room->pool[warp * top + i] = i < held ? room[i] : 0;
+    }
+    __syncthreads();
+    a = lane < kScoreWarps ? warps[lane] : nothing();
+    a = warp_join<ENT>(a, c);
+    if (TOP) pick(top_room->pool, kScoreWarps * top, top_room->best, top);
+    return a;
+}
+
+// joins the parts of a row over its cluster; every thread of the CTA with rank 0 receives the sums
+template <bool ENT>
+__device__ __forceinline__ Sums cluster_join(Sums a, float c, uint32_t rank, uint32_t parts, Sums* shared) {
+    if (threadIdx.x == 0) *shared = a;
+    cluster_arrive_wait();
+    if (rank == 0) {
+        const uint32_t lane = threadIdx.x & 31u;
+        a = nothing();
+        if (lane < parts) {
+            const uint32_t at = mapa_shared((uint32_t)__cvta_generic_to_shared(shared), lane);
+            a = {ld_dsmem(at), ld_dsmem(at + 4), ld_dsmem(at + 8), ld_dsmem(at + 12)};
+        }
+        a = warp_join<ENT>(a, c);
+    }
+    return a;
+}
+__device__ __forceinline__ uint64_t ld_dsmem_u64(uint32_t at) {
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(at) : "memory");
+    return v;
+}
+
+template <typename T, bool ENT, bool TOP>
+__global__ void __launch_bounds__(kScoreThreads) logprobs_kernel(const __grid_constant__ cleave_logprobs_t d) {
+    __shared__ Sums warps[kScoreWarps], whole;
+    __shared__ typename std::conditional<TOP, TopRoom, int>::type top_room;
+    begin_chained();
+    const uint32_t part = blockIdx.x, parts = gridDim.x;
+    const uint64_t row = blockIdx.y + (uint64_t)gridDim.y * blockIdx.z;
+    if (row >= d.rows) return;                                   // (the whole cluster)
+    const float c = d.scale * kLog2e;
+    const T* x = static_cast<const T*>(d.x) + row * d.ldx;
+    TopRoom* top = nullptr;
+    if constexpr (TOP) top = &top_room;
+    Sums a = row_part<T, ENT, TOP>(x, d.cols, c, part, parts, warps, top, d.top);
+    if (parts > 1) a = cluster_join<ENT>(a, c, part, parts, &whole);
+    if (part == 0) {
+        if constexpr (TOP) {
+            if (parts > 1) {
+                const uint32_t at = (uint32_t)__cvta_generic_to_shared(top_room.best);
+                for (uint32_t e = threadIdx.x; e < parts * d.top; e += kScoreThreads) top_room.pool[e] = ld_dsmem_u64(mapa_shared(at, e / d.top) + (e % d.top) * 8);
+                __syncthreads();
+                pick(top_room.pool, parts * d.top, top_room.room[0], d.top);     // (its own `best` may still be read)
+            }
+        }
+        const Stats r = stats_of(a, d.scale, c);
+        if (threadIdx.x == 0) {
+            if (d.lse) d.lse[row] = r.lse;
+            if (ENT && d.entropy) d.entropy[row] = r.entropy;
+            if (d.logp) {
+                const int32_t t = load_token(d.ids, d.id_type, row, d.cols);
+                d.logp[row] = t < 0 ? 0.f : (r.lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[t]), -r.lse));
+            }
+        }
+        if constexpr (TOP) {
+            const uint64_t* best = parts > 1 ? top_room.room[0] : top_room.best;
+            if (threadIdx.x < d.top) {
+                if (d.top_index) d.top_index[row * d.ldti + threadIdx.x] = (int32_t)place_of(best[threadIdx.x]);
+                if (d.top_values) d.top_values[row * d.ldtv + threadIdx.x] = r.lse == -INFINITY ? -INFINITY : fmaf(d.scale, score_of(best[threadIdx.x]), -r.lse);
+            }
+        }
+    }
+    if (parts > 1) cluster_arrive_wait();                        // no CTA leaves while another reads its shared memory
+}
+
+// CTAs a row: enough to fill the GPU a few times over, each with 16 KB of scores at least
+uint32_t row_parts(uint64_t rows, uint64_t row_bytes, int sms) {
+    uint32_t parts = 1;
+    while (parts < 8 && rows * parts < (uint64_t)sms * 8 && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
+    return parts;
+}
+struct RowGrid { dim3 cluster, grid; };
+RowGrid row_grid(uint64_t rows, uint64_t row_bytes, int sms) {
+    const uint32_t parts = row_parts(rows, row_bytes, sms), y = (uint32_t)std::min<uint64_t>(rows, 32768);
+    return {dim3(parts), dim3(parts, y, (unsigned)((rows + y - 1) / y))};
+}
+template <typename T, bool ENT>
+cudaError_t launch_logprobs_types(const cleave_logprobs_t& d, const RowGrid& g, cudaStream_t st) {
+    return d.top ? launch_chained_clusters(logprobs_kernel<T, ENT, true>, g.cluster, g.grid, kScoreThreads, 0, st, d)
+                 : launch_chained_clusters(logprobs_kernel<T, ENT, false>, g.cluster, g.grid, kScoreThreads, 0, st, d);
+}
+cudaError_t launch_logprobs(const cleave_logprobs_t& d, int sms, cudaStream_t st) {
+    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms);
+    if (d.x_type == CLEAVE_T_F32) return d.entropy ? launch_logprobs_types<float, true>(d, g, st) : launch_logprobs_types<float, false>(d, g, st);
+    return d.entropy ? launch_logprobs_types<__nv_bfloat16, true>(d, g, st) : launch_logprobs_types<__nv_bfloat16, false>(d, g, st);
 }
 
 // ---- gradients -----------------------------------------------------------------------------------------
@@ -123,6 +394,17 @@ cudaError_t launch_logprobs_backward(const cleave_logprobs_backward_t& d, int, c
 }
 
 // ---- distillation ------------------------------------------------------------------------------------------
+template <typename F>
+__device__ __forceinline__ float cta_reduce(float v, float* buf, F&& f) {       // buf: one value a warp; ends with a barrier
+#pragma unroll
+    for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
+    if ((threadIdx.x & 31u) == 0) buf[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = buf[0];
+    for (uint32_t w = 1; w < blockDim.x / 32; ++w) v = f(v, buf[w]);
+    __syncthreads();
+    return v;
+}
 // The row's teacher: thread k < d.k has place k (or -1) and q_k; `log_q` where q_k > 0.  All threads of the CTA take part.
 struct Place { int32_t j; float q, log_q; };
 __device__ __forceinline__ Place teacher(const cleave_distill_t& d, uint64_t row, float* buf) {
@@ -146,23 +428,35 @@ __device__ __forceinline__ Place teacher(const cleave_distill_t& d, uint64_t row
     if (p.q == 0.f) p.j = -1;
     return p;
 }
-__global__ void __launch_bounds__(kScoreThreads) distill_any_kernel(const __grid_constant__ cleave_distill_t d) {
+template <typename T>
+__global__ void __launch_bounds__(kScoreThreads) distill_kernel(const __grid_constant__ cleave_distill_t d) {
+    __shared__ Sums warps[kScoreWarps], whole;
     __shared__ float buf[32];
     begin_chained();
-    const uint64_t row = blockIdx.x, at = row * d.ldx;
-    const RowSums r = row_sums_any(d.x, d.x_type, at, d.cols, d.scale, buf);
-    const float lse = row_lse(r, d.scale);
-    const Place p = teacher(d, row, buf);
-    float term = 0.f;
-    if (p.j >= 0) term = p.q * (p.log_q - (lse == -INFINITY ? -INFINITY : fmaf(d.scale, load_as(d.x, d.x_type, at + p.j), -lse)));
-    term = cta_sum(term, buf);
-    if (threadIdx.x == 0) {
-        d.loss[row] = term;
-        if (d.lse) d.lse[row] = lse;
+    const uint32_t part = blockIdx.x, parts = gridDim.x;
+    const uint64_t row = blockIdx.y + (uint64_t)gridDim.y * blockIdx.z;
+    if (row >= d.rows) return;
+    const float c = d.scale * kLog2e;
+    const T* x = static_cast<const T*>(d.x) + row * d.ldx;
+    Sums a = row_part<T, false, false>(x, d.cols, c, part, parts, warps, nullptr, 0);
+    if (parts > 1) a = cluster_join<false>(a, c, part, parts, &whole);
+    if (part == 0) {
+        const float lse = stats_of(a, d.scale, c).lse;
+        const Place p = teacher(d, row, buf);
+        float term = 0.f;
+        if (p.j >= 0) term = p.q * (p.log_q - (lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[p.j]), -lse)));
+        term = cta_sum(term, buf);
+        if (threadIdx.x == 0) {
+            d.loss[row] = term;
+            if (d.lse) d.lse[row] = lse;
+        }
     }
+    if (parts > 1) cluster_arrive_wait();
 }
-cudaError_t launch_distill(const cleave_distill_t& d, int, cudaStream_t st) {
-    return launch_chained(distill_any_kernel, (unsigned)d.rows, kScoreThreads, 0, st, d);
+cudaError_t launch_distill(const cleave_distill_t& d, int sms, cudaStream_t st) {
+    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms);
+    return d.x_type == CLEAVE_T_F32 ? launch_chained_clusters(distill_kernel<float>, g.cluster, g.grid, kScoreThreads, 0, st, d)
+                                    : launch_chained_clusters(distill_kernel<__nv_bfloat16>, g.cluster, g.grid, kScoreThreads, 0, st, d);
 }
 __global__ void __launch_bounds__(kScoreThreads) distill_backward_any_kernel(const __grid_constant__ cleave_distill_backward_t d) {
     __shared__ float buf[32];
