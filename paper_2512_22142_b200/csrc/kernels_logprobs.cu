@@ -346,7 +346,7 @@ uint32_t row_parts(uint64_t rows, uint64_t row_bytes, int sms) {
 }
 struct RowGrid { dim3 cluster, grid; };
 RowGrid row_grid(uint64_t rows, uint64_t row_bytes, int sms) {
-    const uint32_t parts = row_parts(rows, row_bytes, sms), y = (uint32_t)std::min<uint64_t>(rows, 32768);
+    const uint32_t parts = row_parts(rows, row_bytes, sms), y = (uint32_t)std::min<uint64_t>(rows, 65535);
     return {dim3(parts), dim3(parts, y, (unsigned)((rows + y - 1) / y))};
 }
 template <typename T, bool ENT>
@@ -361,70 +361,187 @@ cudaError_t launch_logprobs(const cleave_logprobs_t& d, int sms, cudaStream_t st
 }
 
 // ---- gradients -----------------------------------------------------------------------------------------
-// dx_j = s (a p_j + b p_j log p_j - [what the row's named places hold]): the whole row from the scores and lse, then the
-// named places once more, from scores that were read before the row was written (dx may be x's buffer).  A row of which
-// nothing is asked (a = b = 0 and no place) is zeros whatever stands in it: padded rows may hold anything.
-struct RowSlope { float a, b; };
-__device__ __forceinline__ float slope_at(float x, float scale, float lse, const RowSlope& g) {
-    const float t = fmaf(scale, x, -lse), p = exp2_fast(t * kLog2e);
-    return p == 0.f ? 0.f : fmaf(g.b, t, g.a) * p;
+// dx_j = s (a p_j + b p_j log p_j - [what the row's named places hold]).  A row of which nothing is asked (a = b = 0 and no
+// place) is zeros whatever stands in it: padded rows may hold anything.  Rows are taken from the last to the first: the last
+// ones are what L2 still holds of the forward pass.
+struct RowSlope { float lse, a, b; };            // a and b with the scale
+template <bool ENT>
+__device__ __forceinline__ float slope_at(float x, float scale, const RowSlope& g) {
+    float t = fmaf(scale, x, -g.lse);
+    if (ENT) { t = max_nan(t, -200.f); return fmaf(g.b, t, g.a) * exp2_fast(t * kLog2e); }      // (p is 0 there, and so is p log p)
+    return g.a * exp2_fast(t * kLog2e);
 }
-__device__ __forceinline__ void write_row_any(const void* x, uint32_t x_type, uint64_t ox, void* dx, uint32_t dx_type, uint64_t odx, uint32_t cols, float scale, float lse,
-                                              const RowSlope& g) {
-    const bool zeros = lse == -INFINITY || (g.a == 0.f && g.b == 0.f);
-    for (uint32_t j = threadIdx.x; j < cols; j += blockDim.x)
-        store_as(dx, dx_type, odx + j, zeros ? 0.f : scale * slope_at(load_as(x, x_type, ox + j), scale, lse, g));
+template <bool ENT>
+__device__ __forceinline__ F2 slope_at(F2 x, F2 scale, const RowSlope& g) {
+    F2 t = fma2(scale, x, f2(-g.lse, -g.lse));
+    if (ENT) { const float2 h = halves(t); t = f2(max_nan(h.x, -200.f), max_nan(h.y, -200.f)); }
+    const float2 e = halves(mul2(t, f2(kLog2e, kLog2e)));
+    const F2 p = f2(exp2_fast(e.x), exp2_fast(e.y));
+    return ENT ? mul2(fma2(f2(g.b, g.b), t, f2(g.a, g.a)), p) : mul2(f2(g.a, g.a), p);
 }
-__global__ void __launch_bounds__(kScoreThreads) logprobs_backward_any_kernel(const __grid_constant__ cleave_logprobs_backward_t d) {
+// The columns of a row that a CTA writes.  Wide: groups of 8 that stand on 16 bytes in x and in dx; what is before and behind
+// them (less than a group each) goes to the first and the last part.
+struct Part { uint32_t head, tail, begin, end; };        // wide: groups; else columns
+template <typename X, typename D, bool WIDE>
+__device__ __forceinline__ Part row_columns(const X* x, const D* dx, uint32_t cols, uint32_t part, uint32_t parts) {
+    if (!WIDE) {
+        const uint32_t each = (cols + parts - 1) / parts, begin = min(cols, part * each);
+        return {0u, 0u, begin, min(cols, begin + each)};
+    }
+    // (the operand of 2 bytes says where a group begins; the other one agrees, or the form would not have been chosen)
+    const uint32_t at = sizeof(X) == 2 ? (uint32_t)((uintptr_t)x / 2 % 8) : (sizeof(D) == 2 ? (uint32_t)((uintptr_t)dx / 2 % 8) : (uint32_t)((uintptr_t)x / 4 % 4));
+    const uint32_t head = min(cols, (0u - at) % (sizeof(X) == 2 || sizeof(D) == 2 ? 8u : 4u)), groups = (cols - head) / 8;
+    const uint32_t each = (groups + parts - 1) / parts, begin = min(groups, part * each);
+    return {part == 0 ? head : 0u, part == parts - 1 ? cols - head - groups * 8 : 0u, begin, min(groups, begin + each)};
+}
+// Writes a part.  `slope` is asked for once the first scores are on their way; it may hold barriers.  `fix(j, y)` may change what
+// is stored in column j.
+template <typename X, typename D, bool ENT, bool WIDE, typename SLOPE, typename FIX>
+__device__ __forceinline__ void write_part(const X* x, D* dx, uint32_t cols, float scale, uint32_t part, uint32_t parts, SLOPE&& slope, FIX&& fix) {
+    constexpr int N = WIDE ? (sizeof(X) == 2 ? 4 : 2) : 8;       // groups, or columns, that a thread has in flight
+    const uint32_t tid = threadIdx.x;
+    const Part p = row_columns<X, D, WIDE>(x, dx, cols, part, parts);
+    using Raw = typename std::conditional<WIDE, Raw8<X>, X>::type;
+    Raw next[N];
+    uint32_t edge = cols;
+    float lone = 0.f;
+    const uint32_t first = WIDE && p.head == 0 ? row_columns<X, D, WIDE>(x, dx, cols, 0, 1).head : p.head;       // where group 0 begins
+    auto fetch = [&](uint32_t at) {
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const uint32_t k = at + q * kScoreThreads;
+            if (k >= p.end) continue;
+            if constexpr (WIDE) {
+                const uint4* from = reinterpret_cast<const uint4*>(x + first + (uint64_t)k * 8);
+#pragma unroll
+                for (int i = 0; i < (int)(sizeof(Raw) / 16); ++i) next[q].w[i] = load_unit(from + i);
+            } else next[q] = x[k];
+        }
+    };
+    fetch(p.begin + tid);
+    if (WIDE) {
+        if (tid < p.head) edge = tid;
+        if (tid >= 32u && tid - 32u < p.tail) edge = cols - p.tail + (tid - 32u);
+        if (edge < cols) lone = to_f32(x[edge]);
+    }
+    const RowSlope g = slope();
+    const bool zeros = g.lse == -INFINITY || (g.a == 0.f && g.b == 0.f);
+    const F2 scale2 = f2(scale, scale);
+    if (edge < cols) dx[edge] = from_f32<D>(fix(edge, zeros ? 0.f : slope_at<ENT>(lone, scale, g)));
+    for (uint32_t u = p.begin + tid; u < p.end; u += N * kScoreThreads) {
+        Raw now[N];
+#pragma unroll
+        for (int q = 0; q < N; ++q) now[q] = next[q];
+        if (!zeros) fetch(u + N * kScoreThreads);
+#pragma unroll
+        for (int q = 0; q < N; ++q) {
+            const uint32_t k = u + q * kScoreThreads;
+            if (k >= p.end) continue;
+            if constexpr (WIDE) {
+                F2 v[4];
+                unpack8(now[q], v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = zeros ? f2(0.f, 0.f) : slope_at<ENT>(v[i], scale2, g);
+                const uint32_t j = first + k * 8;
+                fix(j, v);
+                store8(dx + j, v);
+            } else dx[k] = from_f32<D>(fix(k, zeros ? 0.f : slope_at<ENT>(to_f32(now[q]), scale, g)));
+        }
+    }
+}
+__device__ __forceinline__ uint64_t row_from_end(uint64_t rows) { return rows - 1 - (blockIdx.y + (uint64_t)gridDim.y * blockIdx.z); }      // (below 0: beyond rows)
+
+template <typename X, typename D, bool ENT, bool WIDE>
+__global__ void __launch_bounds__(kScoreThreads) logprobs_backward_kernel(const __grid_constant__ cleave_logprobs_backward_t d) {
     begin_chained();
-    const uint64_t row = blockIdx.x, ox = row * d.ldx, odx = row * d.lddx;
-    const float lse = d.lse[row];
-    const int32_t t = d.dlogp ? load_token(d.ids, d.id_type, row, d.cols) : -1;
-    const float up = t < 0 ? 0.f : d.dlogp[row], dh = d.dentropy ? d.dentropy[row] : 0.f;
-    const RowSlope g = {(d.dlse ? d.dlse[row] : 0.f) - up - (dh != 0.f ? dh * d.entropy[row] : 0.f), -dh};
-    const bool named = up != 0.f && lse != -INFINITY;            // (a NaN counts)
-    const float own = named ? slope_at(load_as(d.x, d.x_type, ox + t), d.scale, lse, g) : 0.f;
-    __syncthreads();                                             // every thread has its token's score
-    write_row_any(d.x, d.x_type, ox, d.dx, d.dx_type, odx, d.cols, d.scale, lse, g);
-    __syncthreads();
-    if (named && threadIdx.x == 0) store_as(d.dx, d.dx_type, odx + t, d.scale * (own + up));
+    const uint64_t row = row_from_end(d.rows);
+    if (row >= d.rows) return;
+    uint32_t named = 0xFFFFFFFFu;                                // the row's token
+    float up = 0.f;
+    auto slope = [&] {
+        const float lse = d.lse[row];
+        const int32_t t = d.dlogp ? load_token(d.ids, d.id_type, row, d.cols) : -1;
+        up = t < 0 ? 0.f : d.dlogp[row];
+        const float dh = ENT ? d.dentropy[row] : 0.f;
+        const float a = (d.dlse ? d.dlse[row] : 0.f) - up - (dh != 0.f ? dh * d.entropy[row] : 0.f);
+        if (up != 0.f && lse != -INFINITY) named = (uint32_t)t;  // (a NaN counts)
+        up *= d.scale;
+        return RowSlope{lse, a * d.scale, -dh * d.scale};
+    };
+    struct Fix {
+        const uint32_t& named;
+        const float& up;
+        __device__ float operator()(uint32_t j, float y) const { return j == named ? y + up : y; }
+        __device__ void operator()(uint32_t j, F2 (&v)[4]) const {
+            const uint32_t e = named - j;
+            if (e < 8u) {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) { const float2 h = halves(v[i]); v[i] = f2(e == 2 * i ? h.x + up : h.x, e == 2 * i + 1 ? h.y + up : h.y); }
+            }
+        }
+    };
+    write_part<X, D, ENT, WIDE>(static_cast<const X*>(d.x) + row * d.ldx, static_cast<D*>(d.dx) + row * d.lddx, d.cols, d.scale, blockIdx.x, gridDim.x, slope, Fix{named, up});
 }
-cudaError_t launch_logprobs_backward(const cleave_logprobs_backward_t& d, int, cudaStream_t st) {
-    return launch_chained(logprobs_backward_any_kernel, (unsigned)d.rows, kScoreThreads, 0, st, d);
+
+// whether rows of x and dx allow groups of 8 that stand on 16 bytes in both
+bool groups_agree(const void* x, uint64_t ldx, uint32_t x_type, const void* dx, uint64_t lddx, uint32_t dx_type) {
+    const uint32_t sx = type_bytes(x_type), sd = type_bytes(dx_type), unit = sx == 2 && sd == 2 ? 8 : 4;
+    return ((uintptr_t)x / sx - (uintptr_t)dx / sd) % unit == 0 && (ldx - lddx) % unit == 0;
+}
+// Parts of a row: 32768 columns each, less where there are too few rows to fill the GPU.
+dim3 backward_grid(uint64_t rows, uint32_t cols, int sms) {
+    const uint64_t most = (cols + 2047u) / 2048u, wanted = (8ull * sms + rows - 1) / rows;
+    const uint32_t parts = (uint32_t)std::max<uint64_t>((cols + 32767u) / 32768u, std::min(most, wanted)), y = (uint32_t)std::min<uint64_t>(rows, 65535);
+    return dim3(parts, y, (unsigned)((rows + y - 1) / y));
+}
+template <typename X, typename D>
+cudaError_t launch_logprobs_backward_types(const cleave_logprobs_backward_t& d, dim3 grid, cudaStream_t st) {
+    if (groups_agree(d.x, d.ldx, d.x_type, d.dx, d.lddx, d.dx_type))
+        return launch_chained(d.dentropy ? logprobs_backward_kernel<X, D, true, true> : logprobs_backward_kernel<X, D, false, true>, grid, kScoreThreads, 0, st, d);
+    return launch_chained(d.dentropy ? logprobs_backward_kernel<X, D, true, false> : logprobs_backward_kernel<X, D, false, false>, grid, kScoreThreads, 0, st, d);
+}
+cudaError_t launch_logprobs_backward(const cleave_logprobs_backward_t& d, int sms, cudaStream_t st) {
+    const dim3 grid = backward_grid(d.rows, d.cols, sms);
+    if (d.x_type == CLEAVE_T_F32) return d.dx_type == CLEAVE_T_F32 ? launch_logprobs_backward_types<float, float>(d, grid, st) : launch_logprobs_backward_types<float, __nv_bfloat16>(d, grid, st);
+    return d.dx_type == CLEAVE_T_F32 ? launch_logprobs_backward_types<__nv_bfloat16, float>(d, grid, st) : launch_logprobs_backward_types<__nv_bfloat16, __nv_bfloat16>(d, grid, st);
 }
 
 // ---- distillation ------------------------------------------------------------------------------------------
-template <typename F>
-__device__ __forceinline__ float cta_reduce(float v, float* buf, F&& f) {       // buf: one value a warp; ends with a barrier
+// The row's teacher: thread k < d.k has place k (or -1) and q_k; `log_q` where q_k > 0; `all`, the sum of q, in every thread.  Every
+// warp reads the whole row (at most 8 entries a lane), so nothing waits for another warp.
+struct Place { int32_t j; float q, log_q, all; };
+constexpr int kEntries = CLEAVE_DISTILL_MOST / 32;
+__device__ __forceinline__ Place teacher(const cleave_distill_t& d, uint64_t row) {
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    float v[kEntries], top = -INFINITY;
+    int32_t j[kEntries];
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v = f(v, __shfl_xor_sync(0xFFFFFFFFu, v, o));
-    if ((threadIdx.x & 31u) == 0) buf[threadIdx.x >> 5] = v;
-    __syncthreads();
-    v = buf[0];
-    for (uint32_t w = 1; w < blockDim.x / 32; ++w) v = f(v, buf[w]);
-    __syncthreads();
-    return v;
-}
-// The row's teacher: thread k < d.k has place k (or -1) and q_k; `log_q` where q_k > 0.  All threads of the CTA take part.
-struct Place { int32_t j; float q, log_q; };
-__device__ __forceinline__ Place teacher(const cleave_distill_t& d, uint64_t row, float* buf) {
-    Place p = {-1, 0.f, 0.f};
-    float v = -INFINITY;
-    if (threadIdx.x < d.k) {
-        p.j = load_token(d.index, d.index_type, row * d.ldindex + threadIdx.x, d.cols);
-        if (p.j >= 0) v = d.scale * load_as(d.values, d.values_type, row * d.ldvalues + threadIdx.x);
+    for (int i = 0; i < kEntries; ++i) {
+        const uint32_t k = lane + 32 * i;
+        j[i] = -1;
+        v[i] = -INFINITY;
+        if (k < d.k) {
+            j[i] = load_token(d.index, d.index_type, row * d.ldindex + k, d.cols);
+            v[i] = load_as(d.values, d.values_type, row * d.ldvalues + k);
+        }
     }
-    if (d.normalize) {
-        const float top = cta_reduce(v, buf, [](float a, float b) { return max_nan(a, b); });
-        v = top == -INFINITY ? -INFINITY : v - top;
-        p.q = v == -INFINITY ? 0.f : exp2_fast(v * kLog2e);
-        const float sum = cta_sum(p.q, buf);
-        p.log_q = v - logf(sum);
-        p.q = p.q == 0.f ? 0.f : p.q / sum;
-    } else {
-        p.log_q = v;
-        p.q = v == -INFINITY ? 0.f : exp2_fast(v * kLog2e);
+#pragma unroll
+    for (int i = 0; i < kEntries; ++i) {
+        v[i] = j[i] < 0 ? -INFINITY : d.scale * v[i];
+        top = max_nan(top, v[i]);
     }
+    Place p = {-1, 0.f, 0.f, 0.f};
+    top = d.normalize ? warp_max_nan(top) : 0.f;
+    if (top == -INFINITY) return p;                              // an empty row
+    float e[kEntries], sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEntries; ++i) { v[i] -= top; e[i] = exp2_fast(v[i] * kLog2e); sum += e[i]; }
+    sum = warp_sum(sum);
+    const float inv = d.normalize ? 1.f / sum : 1.f, log_sum = d.normalize ? logf(sum) : 0.f;
+    p.all = d.normalize ? sum * inv : sum;
+#pragma unroll
+    for (int i = 0; i < kEntries; ++i)
+        if (warp == i) { p.j = j[i]; p.q = e[i] * inv; p.log_q = v[i] - log_sum; }
     if (p.q == 0.f) p.j = -1;
     return p;
 }
@@ -442,7 +559,7 @@ __global__ void __launch_bounds__(kScoreThreads) distill_kernel(const __grid_con
     if (parts > 1) a = cluster_join<false>(a, c, part, parts, &whole);
     if (part == 0) {
         const float lse = stats_of(a, d.scale, c).lse;
-        const Place p = teacher(d, row, buf);
+        const Place p = teacher(d, row);
         float term = 0.f;
         if (p.j >= 0) term = p.q * (p.log_q - (lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[p.j]), -lse)));
         term = cta_sum(term, buf);
@@ -458,32 +575,57 @@ cudaError_t launch_distill(const cleave_distill_t& d, int sms, cudaStream_t st) 
     return d.x_type == CLEAVE_T_F32 ? launch_chained_clusters(distill_kernel<float>, g.cluster, g.grid, kScoreThreads, 0, st, d)
                                     : launch_chained_clusters(distill_kernel<__nv_bfloat16>, g.cluster, g.grid, kScoreThreads, 0, st, d);
 }
-__global__ void __launch_bounds__(kScoreThreads) distill_backward_any_kernel(const __grid_constant__ cleave_distill_backward_t d) {
-    __shared__ float buf[32];
+template <typename X, typename D, bool WIDE>
+__global__ void __launch_bounds__(kScoreThreads) distill_backward_kernel(const __grid_constant__ cleave_distill_backward_t d) {
     __shared__ int32_t places[CLEAVE_DISTILL_MOST];
     __shared__ float weights[CLEAVE_DISTILL_MOST];
     begin_chained();
-    const uint64_t row = blockIdx.x, ox = row * d.f.ldx, odx = row * d.lddx;
-    const float lse = d.f.lse[row], up = d.dloss[row];
-    const Place p = teacher(d.f, row, buf);
-    if (threadIdx.x < d.f.k) { places[threadIdx.x] = p.j; weights[threadIdx.x] = p.q; }
-    const float all = cta_sum(p.q, buf);                         // (its barriers show the places to all)
-    const RowSlope g = {up == 0.f || all == 0.f ? 0.f : up * all, 0.f};
-    bool named = p.j >= 0 && up != 0.f && lse != -INFINITY;
+    const uint64_t row = row_from_end(d.f.rows);
+    if (row >= d.f.rows) return;
+    const X* x = static_cast<const X*>(d.f.x) + row * d.f.ldx;
+    D* dx = static_cast<D*>(d.dx) + row * d.lddx;
+    // the columns of this CTA: it alone writes them, the named places among them once the rest is written, from scores that are read
+    // before (dx may be x's buffer)
+    const Part p = row_columns<X, D, WIDE>(x, dx, d.f.cols, blockIdx.x, gridDim.x);
+    const uint32_t first = WIDE ? row_columns<X, D, WIDE>(x, dx, d.f.cols, 0, 1).head : 0u, unit = WIDE ? 8u : 1u;
+    const uint32_t from = first + p.begin * unit - p.head, to = first + p.end * unit + p.tail;
+    bool named = false;
     float own = 0.f;
-    if (named) {
-        float q = 0.f;
-        for (uint32_t k = 0; k < d.f.k; ++k)
-            if (places[k] == p.j) { q += weights[k]; named = named && k >= threadIdx.x; }      // of entries with the same place the first writes
-        own = slope_at(load_as(d.f.x, d.f.x_type, ox + p.j), d.f.scale, lse, g) - up * q;
-    }
+    Place t = {-1, 0.f, 0.f, 0.f};
+    auto slope = [&] {
+        const float lse = d.f.lse[row], up = d.dloss[row];
+        t = teacher(d.f, row);
+        if (threadIdx.x < d.f.k) { places[threadIdx.x] = t.j; weights[threadIdx.x] = t.q; }
+        const RowSlope g = {lse, up == 0.f || t.all == 0.f ? 0.f : up * t.all * d.f.scale, 0.f};
+        named = t.j >= 0 && up != 0.f && lse != -INFINITY && (uint32_t)t.j >= from && (uint32_t)t.j < to;
+        float score = 0.f;
+        if (named) score = to_f32(x[t.j]);
+        __syncthreads();
+        if (named) {
+            float q = 0.f;
+            for (uint32_t k = 0; k < d.f.k; ++k)
+                if (places[k] == t.j) { q += weights[k]; named = named && k >= threadIdx.x; }      // of entries with the same place the first writes
+            own = slope_at<false>(score, d.f.scale, g) - up * d.f.scale * q;
+        }
+        return g;
+    };
+    struct Fix {
+        __device__ float operator()(uint32_t, float y) const { return y; }
+        __device__ void operator()(uint32_t, F2 (&)[4]) const {}
+    };
+    write_part<X, D, false, WIDE>(x, dx, d.f.cols, d.f.scale, blockIdx.x, gridDim.x, slope, Fix{});
     __syncthreads();
-    write_row_any(d.f.x, d.f.x_type, ox, d.dx, d.dx_type, odx, d.f.cols, d.f.scale, lse, g);
-    __syncthreads();
-    if (named) store_as(d.dx, d.dx_type, odx + p.j, d.f.scale * own);
+    if (named) dx[t.j] = from_f32<D>(own);
 }
-cudaError_t launch_distill_backward(const cleave_distill_backward_t& d, int, cudaStream_t st) {
-    return launch_chained(distill_backward_any_kernel, (unsigned)d.f.rows, kScoreThreads, 0, st, d);
+template <typename X, typename D>
+cudaError_t launch_distill_backward_types(const cleave_distill_backward_t& d, dim3 grid, cudaStream_t st) {
+    return launch_chained(groups_agree(d.f.x, d.f.ldx, d.f.x_type, d.dx, d.lddx, d.dx_type) ? distill_backward_kernel<X, D, true> : distill_backward_kernel<X, D, false>, grid,
+                          kScoreThreads, 0, st, d);
+}
+cudaError_t launch_distill_backward(const cleave_distill_backward_t& d, int sms, cudaStream_t st) {
+    const dim3 grid = backward_grid(d.f.rows, d.f.cols, sms);
+    if (d.f.x_type == CLEAVE_T_F32) return d.dx_type == CLEAVE_T_F32 ? launch_distill_backward_types<float, float>(d, grid, st) : launch_distill_backward_types<float, __nv_bfloat16>(d, grid, st);
+    return d.dx_type == CLEAVE_T_F32 ? launch_distill_backward_types<__nv_bfloat16, float>(d, grid, st) : launch_distill_backward_types<__nv_bfloat16, __nv_bfloat16>(d, grid, st);
 }
 
 }  // namespace cleave
