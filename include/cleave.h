@@ -571,8 +571,8 @@ typedef struct {
 CLEAVE_API uint64_t cleave_layernorm_backward_workspace(uint64_t rows, uint32_t cols);
 CLEAVE_API int cleave_layernorm_backward(const cleave_layernorm_backward_t* d, void* workspace, void* stream);
 
-/* Log probabilities of given tokens, and what else one reading of the scores gives.  Per row, with s = scale > 0 (1 / temperature)
- * and p = softmax(s x):
+/* Log probabilities of given tokens, and what else one reading of the scores gives.  Per row, with s = scale (1 / temperature,
+ * 2^-100 to 2^100) and p = softmax(s x):
  *   lse = log sum_j exp(s x_j)      logp = s x_t - lse for the token t      entropy = -sum_j p_j log p_j
  *   top_index, top_values: the `top` places of the largest scores, largest first and of equal ones the lowest place first,
  *   and their log probabilities s x - lse.

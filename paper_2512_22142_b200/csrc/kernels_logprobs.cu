@@ -2,7 +2,7 @@
 // backward passes of both (see cleave.h).
 //
 // Forward: one reading of the scores.  A thread keeps a largest score m and, relative to it, s = sum 2^a and t = sum 2^a a
-// with a = scale log2(e) (x - m); a larger score rescales both.  lse = scale m + ln 2 log2(s), entropy = ln 2 (log2(s) - t / s).
+// with a = c (x - m), c = scale log2(e); a larger score rescales both.  lse = scale m + ln 2 log2(s), entropy = ln 2 (log2(s) - t / s).
 // The top places go through a threshold that only rises: a score below it is dropped after one comparison (shared by 16
 // bytes of scores), the others are collected by warp and cut to the best `top` when a warp's room is full.
 // A row goes to one CTA, or with few rows to a cluster of them, joined through distributed shared memory.
@@ -18,7 +18,8 @@ namespace cleave {
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kMasked = -0x1p126f;             // a row whose largest score is not above this has nothing left
-constexpr uint32_t kScoreThreads = 256, kScoreWarps = kScoreThreads / 32;
+constexpr uint32_t kScoreThreads = 256;          // of a CTA that writes gradients
+constexpr uint32_t kPartsMost = 8;               // CTAs a row in the forward passes
 
 // ---- order of scores -----------------------------------------------------------------------------------
 // whole number that orders like a score: NaN above all, +0 and -0 alike
@@ -33,17 +34,16 @@ __device__ __forceinline__ uint32_t place_of(uint64_t c) { return 0x7FFFFFFFu - 
 __device__ __forceinline__ float score_of(uint64_t c) { return (uint32_t)(c >> 32) == 0xFFFFFFFFu ? __uint_as_float(0x7FFFFFFFu) : order_score((uint32_t)(c >> 32)); }
 
 // ---- sums of a row ---------------------------------------------------------------------------------------
-struct Sums {                       // m: largest score (a NaN stays); ref = c m of the exponents (0 while nothing is above kMasked)
-    float m, ref, s, t;
+struct Sums {                       // m: largest score (a NaN stays); base: what the exponents are relative to, not above m, or 0 while nothing is above kMasked
+    float m, base, s, t;
 };
-__device__ __forceinline__ float reference(float m, float c) { return m <= kMasked ? 0.f : m * c; }
-// the same sums relative to another largest score (which is not below the old one)
+// the same sums relative to a largest score that is not below the old one
 __device__ __forceinline__ void raise(Sums& a, float m, float c) {
-    const float ref = reference(m, c), d = a.ref - ref, f = a.s == 0.f ? 0.f : exp2_fast(d);
-    a.t = a.s == 0.f ? 0.f : f * fmaf(d, a.s, a.t);
+    const float base = m <= kMasked ? 0.f : m, d = c * (a.base - base), f = a.s == 0.f ? 0.f : exp2_fast(d);
+    a.t = f == 0.f ? 0.f : f * fmaf(d, a.s, a.t);
     a.s *= f;
     a.m = m;
-    a.ref = ref;
+    a.base = base;
 }
 __device__ __forceinline__ float warp_max_nan(float v) {
     float r;
@@ -58,14 +58,12 @@ __device__ __forceinline__ Sums warp_join(Sums a, float c) {
     return a;
 }
 __device__ __forceinline__ Sums nothing() { return {-INFINITY, 0.f, 0.f, 0.f}; }
-// a row's results; `ok` is false for a row with a NaN or +infinity
 struct Stats { float lse, entropy; };
 __device__ __forceinline__ Stats stats_of(const Sums& a, float scale, float c) {
     if (a.m <= kMasked) return {-INFINITY, 0.f};
     if (!(a.m < INFINITY)) return {__uint_as_float(0x7FFFFFFFu), __uint_as_float(0x7FFFFFFFu)};
     const float bits = log2f(a.s);
-    // (ref is c m rounded: what that left out goes to the sum)
-    return {fmaf(scale, a.m, kLn2 * (bits + fmaf(-a.m, c, a.ref))), fmaxf(kLn2 * (bits - a.t / a.s), 0.f)};
+    return {fmaf(scale, a.m, kLn2 * bits), fmaxf(kLn2 * (bits - a.t / a.s), 0.f)};
 }
 
 // ---- 16 bytes of scores ------------------------------------------------------------------------------------
@@ -78,10 +76,23 @@ __device__ __forceinline__ float2 pair_of(const uint4& w, int i, __nv_bfloat16) 
 __device__ __forceinline__ float unit_max(const uint4& w, float) {
     return max_nan(max_nan(__uint_as_float(w.x), __uint_as_float(w.y)), max_nan(__uint_as_float(w.z), __uint_as_float(w.w)));
 }
+__device__ __forceinline__ uint32_t max_nan_pair(uint32_t a, uint32_t b) { uint32_t r; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; }
 __device__ __forceinline__ float unit_max(const uint4& w, __nv_bfloat16) {
-    auto two = [](uint32_t a, uint32_t b) { uint32_t r; asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b)); return r; };
-    const uint32_t m = two(two(w.x, w.y), two(w.z, w.w));
+    const uint32_t m = max_nan_pair(max_nan_pair(w.x, w.y), max_nan_pair(w.z, w.w));
     return max_nan(__uint_as_float(m << 16), __uint_as_float(m & 0xFFFF0000u));
+}
+template <typename T, int N> __device__ __forceinline__ float units_max(const uint4 (&w)[N]) {
+    if constexpr (sizeof(T) == 4) {
+        float m = unit_max(w[0], T());
+#pragma unroll
+        for (int q = 1; q < N; ++q) m = max_nan(m, unit_max(w[q], T()));
+        return m;
+    } else {
+        uint4 m = w[0];
+#pragma unroll
+        for (int q = 1; q < N; ++q) m = make_uint4(max_nan_pair(m.x, w[q].x), max_nan_pair(m.y, w[q].y), max_nan_pair(m.z, w[q].z), max_nan_pair(m.w, w[q].w));
+        return unit_max(m, T());
+    }
 }
 template <typename T> __device__ __forceinline__ uint4 masked_unit() {
     const uint32_t v = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
@@ -93,14 +104,37 @@ __device__ __forceinline__ uint4 load_unit(const void* p) {      // (not kept in
     return r;
 }
 
+// A score lifted to where 2^a is 0 but a is finite: a masked place then adds 0 a = 0 to t.  The floor lies `far` = 250 / c below the
+// base, rounded down.  A NaN need not stay: the largest score has it.
+template <typename T> struct Floor;
+template <> struct Floor<float> {
+    float at;
+    __device__ __forceinline__ void set(float base, float far) { at = __fsub_rd(base, far); }
+    __device__ __forceinline__ uint4 lift(const uint4& w) const {
+        auto one = [&](uint32_t v) { return __float_as_uint(fmaxf(__uint_as_float(v), at)); };
+        return make_uint4(one(w.x), one(w.y), one(w.z), one(w.w));
+    }
+};
+template <> struct Floor<__nv_bfloat16> {
+    uint32_t at;
+    __device__ __forceinline__ void set(float base, float far) {
+        const uint32_t v = __bfloat16_as_ushort(__float2bfloat16_rd(__fsub_rd(base, far)));
+        at = v << 16 | v;
+    }
+    __device__ __forceinline__ uint4 lift(const uint4& w) const {
+        auto two = [&](uint32_t v) { uint32_t r; asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(v), "r"(at)); return r; };
+        return make_uint4(two(w.x), two(w.y), two(w.z), two(w.w));
+    }
+};
+
 // ---- the best places -----------------------------------------------------------------------------------------
 constexpr uint32_t kRoom = 128;                  // candidates a warp collects before it cuts them to the best
+template <int T>
 struct TopRoom {
-    alignas(16) uint32_t first[kScoreThreads];   // (read 16 bytes at a time)
-    uint64_t room[kScoreWarps][kRoom];
-    uint64_t pool[kScoreWarps * CLEAVE_TOP_MOST];
+    uint64_t room[T / 32][kRoom];
+    uint64_t pool[(T / 32 > kPartsMost ? T / 32 : kPartsMost) * CLEAVE_TOP_MOST];      // (each warp's best, or each part's)
     uint64_t best[CLEAVE_TOP_MOST];
-    unsigned long long bar;                      // no candidate up to this one is among the best
+    uint32_t pooled, held;
 };
 // the warp's n candidates cut to the best k, best first; returns how many there are
 __device__ __forceinline__ uint32_t cut(uint64_t* room, uint32_t n, uint32_t k) {
@@ -123,13 +157,15 @@ __device__ __forceinline__ uint32_t cut(uint64_t* room, uint32_t n, uint32_t k) 
     return min(n, k);
 }
 // the best k of a pool of n (zeros do not count) into best[0 .. k), zeros behind them; all threads of the CTA
+template <int T>
 __device__ __forceinline__ void pick(const uint64_t* pool, uint32_t n, uint64_t* best, uint32_t k) {
     if (threadIdx.x < k) best[threadIdx.x] = 0;
     __syncthreads();
-    for (uint32_t e = threadIdx.x; e < n; e += kScoreThreads) {
+    for (uint32_t e = threadIdx.x; e < n; e += T) {
         const uint64_t c = pool[e];
         if (!c) continue;
         uint32_t rank = 0;
+#pragma unroll 8
         for (uint32_t j = 0; j < n; ++j) rank += pool[j] > c;
         if (rank < k) best[rank] = c;
     }
@@ -137,13 +173,15 @@ __device__ __forceinline__ void pick(const uint64_t* pool, uint32_t n, uint64_t*
 }
 
 // ---- forward ---------------------------------------------------------------------------------------------------
-constexpr int kSteps = 4;                        // units a thread has in flight
+constexpr int kSteps = 2;                        // units a thread takes at once, and as many again under way
+constexpr float kSlack = 8.f;
 
 // The CTA's part (rank `part` of `parts`) of a row: its sums, joined over the CTA (every thread receives them), and with TOP its
 // best `top` candidates in room->best.
-template <typename T, bool ENT, bool TOP>
-__device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uint32_t part, uint32_t parts, Sums* warps, TopRoom* top_room, uint32_t top) {
+template <typename T, bool ENT, bool TOP, int THREADS>
+__device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uint32_t part, uint32_t parts, Sums* warps, TopRoom<THREADS>* top_room, uint32_t top) {
     constexpr int V = kUnit<T>;
+    constexpr uint32_t kScoreThreads = THREADS;
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
     // the row's units stand on 16 bytes; what is before them and behind them (less than a unit each) goes to threads of
     // the first and the last part
@@ -154,23 +192,53 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
     if (part == 0 && tid < head) edge = tid;
     if (part == parts - 1 && tid >= 32u && tid - 32u < tail) edge = cols - tail + (tid - 32u);
     float lone = -INFINITY;
-    uint4 w[kSteps];
-    auto fetch = [&](uint32_t u) {
+    constexpr uint32_t kStride = kScoreThreads * kSteps;         // units a step of the CTA
+    const uint32_t steps = (end - begin + kStride - 1) / kStride;                // (the same for every thread)
+    const uint32_t whole = (end - begin) / kStride;              // steps in which every thread has all of its units
+    const T* from = body + (uint64_t)(begin + tid) * V;
+    struct Step { uint4 w[kSteps]; };
+    auto fetch = [&](Step& b, uint32_t step) {
+        if (step < whole) {
 #pragma unroll
-        for (int q = 0; q < kSteps; ++q) w[q] = u + q * kScoreThreads < end ? load_unit(body + (uint64_t)(u + q * kScoreThreads) * V) : masked_unit<T>();
+            for (int q = 0; q < kSteps; ++q) b.w[q] = load_unit(from + q * kScoreThreads * V);
+        } else {
+#pragma unroll
+            for (int q = 0; q < kSteps; ++q) b.w[q] = begin + step * kStride + tid + q * kScoreThreads < end ? load_unit(from + q * kScoreThreads * V) : masked_unit<T>();
+        }
+        from += (uint64_t)kStride * V;
     };
-    fetch(begin + tid);
+    Step even, odd;
+    fetch(even, 0);
     if (edge < cols) lone = to_f32(x[edge]);
 
     Sums a = nothing();
-    F2 s2[2] = {f2(0.f, 0.f), f2(0.f, 0.f)}, t2[2] = {f2(0.f, 0.f), f2(0.f, 0.f)};
+    F2 s2 = f2(0.f, 0.f), t2 = f2(0.f, 0.f);
     const F2 c2 = f2(c, c);
-    uint32_t held = 0;                                           // TOP: candidates in the warp's room
-    uint64_t bar = 0;
+    // The base follows the largest score only when 2^kSlack is passed: after its first units a thread hardly ever rescales, and
+    // what t and log2(s) cancel of each other stays below log2 of a vocabulary's size.
+    const float far = ENT ? __fdiv_ru(250.f, c) : 0.f, slack = kSlack / c;
+    float limit = -INFINITY;                                     // what m may reach without a new base
+    Floor<T> floor;
+    floor.set(0.f, far);
+    // TOP.  When `top` threads have seen a score of at least v, nothing below v is among the best: the largest such v, to 16 bits, is
+    // the bar, found bit by bit from the threads' largest scores and raised each time the steps have doubled.  What reaches it goes to the
+    // warp's room; a room that would run over is cut to its best, the last of which is a bar of the warp's own.
+    uint32_t held = 0;
+    uint64_t bar = 0;                                            // (candidates above it may be among the best)
     float bar_score = -INFINITY;
     uint64_t* room = TOP ? top_room->room[warp] : nullptr;
-    auto see_bar = [&](uint64_t b) { bar = b; bar_score = b ? score_of(b) : -INFINITY; };
-    auto offer = [&](bool live, float v, uint32_t j) {           // all lanes of the warp
+    auto raise_bar = [&](uint64_t b) {
+        if (b > bar) { bar = b; bar_score = score_of(b); }
+    };
+    auto common_bar = [&](float most) {                          // all threads of the CTA
+        const uint32_t mine = score_order(most);                 // (a thread that has seen nothing has -infinity, below which nothing is)
+        uint32_t least = 0;
+#pragma unroll 1
+        for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+            if ((uint32_t)__syncthreads_count(mine >= (least | bit)) >= top) least |= bit;
+        raise_bar((uint64_t)least << 32);                        // (below every candidate of that score)
+    };
+    auto offer = [&](bool live, float v, uint32_t j) {           // one candidate a lane; all lanes of the warp
         const uint64_t k = candidate(v, j);
         const bool good = live && k > bar;
         const uint32_t some = __ballot_sync(0xFFFFFFFFu, good);
@@ -179,97 +247,139 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
         held += __popc(some);
         if (held > kRoom - 32) {
             held = cut(room, held, top);
-            if (held == top) {
-                if (lane == 0) atomicMax(&top_room->bar, (unsigned long long)(room[top - 1] - 1));
-                if (room[top - 1] - 1 > bar) see_bar(room[top - 1] - 1);
-            }
+            if (held == top) raise_bar(room[top - 1] - 1);
             __syncwarp();
         }
     };
-    if (TOP) {
-        // A first threshold: every thread has a score that is not below its largest of the first units, so `top` threads with a
-        // largest one of at least v mean that nothing below v is among the best.
-        float v = lone;
-        bool any = edge < cols;
+    // (an equal score counts only where it can stand before the bar's place: a row of few different scores, masked ones most of
+    // all, is not offered again and again)
+    auto ties = [&](uint32_t step) { return place_of(bar) >= head + (begin + step * kStride) * V; };
+    auto reaches = [&](float v, bool tie) { return !(v < bar_score) && (tie || v != bar_score); };           // (a NaN reaches every bar)
+    auto offer_step = [&](const Step& b, uint32_t step) {
+        const uint32_t at = begin + step * kStride + tid;
+        uint32_t hits, n, all;
+        auto count = [&] {
+            const bool tie = ties(step);
+            hits = 0;
 #pragma unroll
-        for (int q = 0; q < kSteps; ++q) { v = max_nan(v, unit_max(w[q], T())); any = any || begin + tid + q * kScoreThreads < end; }
-        const uint32_t mine = any ? score_order(v) : 0u;
-        if (tid == 0) top_room->bar = 0;
-        top_room->first[tid] = mine;
-        __syncthreads();
-        uint32_t rank = 0;
-#pragma unroll 8
-        for (uint32_t i = 0; i < kScoreThreads; i += 4) {
-            const uint4 o = *reinterpret_cast<const uint4*>(top_room->first + i);
-            rank += (o.x > mine || (o.x == mine && i < tid)) + (o.y > mine || (o.y == mine && i + 1 < tid)) + (o.z > mine || (o.z == mine && i + 2 < tid)) +
-                    (o.w > mine || (o.w == mine && i + 3 < tid));
+            for (int q = 0; q < kSteps; ++q)
+                if (at + q * kScoreThreads < end)
+#pragma unroll
+                    for (int i = 0; i < V / 2; ++i) {
+                        const float2 p = pair_of(b.w[q], i, T());
+                        hits |= (reaches(p.x, tie) ? 1u << (q * V + 2 * i) : 0u) | (reaches(p.y, tie) ? 2u << (q * V + 2 * i) : 0u);
+                    }
+            n = __popc(hits);
+            all = __reduce_add_sync(0xFFFFFFFFu, n);
+        };
+        count();
+        if (all > kRoom - 32 - held) {                           // more than the room takes: a bar from the step's own units first
+            uint32_t least = 0, most[kSteps];
+#pragma unroll
+            for (int q = 0; q < kSteps; ++q) most[q] = score_order(unit_max(b.w[q], T()));
+#pragma unroll 1
+            for (uint32_t bit = 1u << 31; bit >= 1u << 16; bit >>= 1) {
+                uint32_t many = 0;
+#pragma unroll
+                for (int q = 0; q < kSteps; ++q) many += __popc(__ballot_sync(0xFFFFFFFFu, most[q] >= (least | bit)));
+                if (many >= top) least |= bit;
+            }
+            raise_bar((uint64_t)least << 32);
+            count();
         }
-        if (rank == top - 1) top_room->bar = (unsigned long long)mine << 32;     // (below every candidate of that score)
-        __syncthreads();
-        see_bar(top_room->bar);
+        if (all <= kRoom - 32 - held) {
+            uint32_t to = n;
+#pragma unroll
+            for (uint32_t o = 1; o < 32; o <<= 1) { const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, to, o); if (lane >= o) to += up; }
+            to += held - n;
+            if (hits)
+#pragma unroll
+                for (int q = 0; q < kSteps; ++q)
+#pragma unroll
+                    for (int i = 0; i < V; ++i)
+                        if (hits >> (q * V + i) & 1u) {
+                            const float2 p = pair_of(b.w[q], i / 2, T());
+                            room[to++] = candidate(i & 1 ? p.y : p.x, head + (at + q * kScoreThreads) * V + i);
+                        }
+            held += all;
+            __syncwarp();
+        } else {
+#pragma unroll
+            for (int q = 0; q < kSteps; ++q)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const float2 p = pair_of(b.w[q], i / 2, T());
+                    offer(hits >> (q * V + i) & 1u, i & 1 ? p.y : p.x, head + (at + q * kScoreThreads) * V + i);
+                }
+        }
+    };
+    if (TOP) {
+        if (tid == 0) top_room->pooled = top_room->held = 0;
+        common_bar(max_nan(lone, units_max<T>(even.w)));
         offer(edge < cols, lone, edge);
     }
     if (edge < cols) {
         raise(a, lone, c);
-        a.s = lone <= kMasked ? 0.f : 1.f;                       // 2^0 at its own reference
+        a.s = lone <= kMasked ? 0.f : 1.f;                       // 2^0 at its own base
+        floor.set(a.base, far);
+        limit = lone <= kMasked ? kMasked : a.base + slack;
     }
-    for (uint32_t u = begin; u < end; u += kScoreThreads * kSteps) {             // (the same number of steps for every thread)
-        uint4 now[kSteps];
-#pragma unroll
-        for (int q = 0; q < kSteps; ++q) now[q] = w[q];
-        if (u + kScoreThreads * kSteps < end) fetch(u + kScoreThreads * kSteps + tid);
-        float most[kSteps], m = -INFINITY;
-#pragma unroll
-        for (int q = 0; q < kSteps; ++q) { most[q] = unit_max(now[q], T()); m = max_nan(m, most[q]); }
-        if (!(m <= a.m)) {
-            const float2 s0 = halves(add2(s2[0], s2[1])), t0 = halves(add2(t2[0], t2[1]));
+    auto take = [&](const Step& b, uint32_t step) {
+        const float most = units_max<T>(b.w), m = max_nan(a.m, most);
+        if (TOP && __any_sync(0xFFFFFFFFu, reaches(most, ties(step)))) offer_step(b, step);
+        if (!(m <= limit)) {
+            const float2 s0 = halves(s2), t0 = halves(t2);
             a.s += s0.x + s0.y;
             a.t += t0.x + t0.y;
-            raise(a, max_nan(a.m, m), c);
-            s2[0] = s2[1] = t2[0] = t2[1] = f2(0.f, 0.f);
+            raise(a, m, c);
+            s2 = t2 = f2(0.f, 0.f);
+            floor.set(a.base, far);
+            limit = m <= kMasked ? kMasked : a.base + slack;
         }
-        const F2 r2 = f2(-a.ref, -a.ref);
+        a.m = m;
+        const F2 b2 = f2(-a.base, -a.base);
 #pragma unroll
-        for (int q = 0; q < kSteps; ++q)
+        for (int q = 0; q < kSteps; ++q) {
+            if (step >= whole && begin + step * kStride + q * kScoreThreads + warp * 32 >= end) break;           // (the whole warp)
+            const uint4 w = ENT ? floor.lift(b.w[q]) : b.w[q];
 #pragma unroll
             for (int i = 0; i < V / 2; ++i) {
-                const float2 p = pair_of(now[q], i, T());
-                F2 e2 = fma2(f2(p.x, p.y), c2, r2);
-                float2 e = halves(e2);
-                if (ENT) { e.x = fmaxf(e.x, -200.f); e.y = fmaxf(e.y, -200.f); e2 = f2(e.x, e.y); }      // (2^-200 is 0: a masked place adds 0 to t)
+                const float2 p = pair_of(w, i, T());
+                const F2 e2 = mul2(add2(f2(p.x, p.y), b2), c2);
+                const float2 e = halves(e2);
                 const F2 p2 = f2(exp2_fast(e.x), exp2_fast(e.y));
-                s2[i & 1] = add2(s2[i & 1], p2);
-                if (ENT) t2[i & 1] = fma2(p2, e2, t2[i & 1]);
-            }
-        if (TOP) {
-            const uint64_t b = *static_cast<volatile unsigned long long*>(&top_room->bar);
-            if (b > bar) see_bar(b);
-#pragma unroll
-            for (int q = 0; q < kSteps; ++q) {
-                const uint32_t at = u + tid + q * kScoreThreads;
-                if (!__any_sync(0xFFFFFFFFu, at < end && !(most[q] < bar_score))) continue;
-#pragma unroll
-                for (int i = 0; i < V / 2; ++i) {
-                    const float2 p = pair_of(now[q], i, T());
-                    offer(at < end, p.x, head + at * V + 2 * i);
-                    offer(at < end, p.y, head + at * V + 2 * i + 1);
-                }
+                s2 = add2(s2, p2);
+                if (ENT) t2 = fma2(p2, e2, t2);
             }
         }
+        if (TOP && step && (step & (step + 1)) == 0 && step + 1 < steps) common_bar(a.m);          // behind the steps 1, 3, 7, ...
+    };
+    for (uint32_t step = 0; step < steps; step += 2) {
+        if (step + 1 < steps) fetch(odd, step + 1);
+        take(even, step);
+        if (step + 1 >= steps) break;
+        if (step + 2 < steps) fetch(even, step + 2);
+        take(odd, step + 1);
     }
-    const float2 s0 = halves(add2(s2[0], s2[1])), t0 = halves(add2(t2[0], t2[1]));
+    const float2 s0 = halves(s2), t0 = halves(t2);
     a.s += s0.x + s0.y;
     a.t += t0.x + t0.y;
+    const float seen = a.m;
     a = warp_join<ENT>(a, c);
     if (lane == 0) warps[warp] = a;
-    if (TOP) {
-        held = cut(room, held, top);
-        for (uint32_t i = lane; i < top; i += 32) top_room->pool[warp * top + i] = i < held ? room[i] : 0;
-    }
+    if (TOP && lane == 0) atomicAdd(&top_room->held, held);
     __syncthreads();
-    a = lane < kScoreWarps ? warps[lane] : nothing();
+    a = lane < THREADS / 32 ? warps[lane] : nothing();
     a = warp_join<ENT>(a, c);
-    if (TOP) pick(top_room->pool, kScoreWarps * top, top_room->best, top);
+    if (TOP) {
+        const uint32_t all = top_room->held;
+        if (all > kRoom) common_bar(seen);                       // (worth its barriers where it leaves less to sort)
+        if (all > THREADS / 32 * CLEAVE_TOP_MOST) held = cut(room, held, top);      // more than the pool has room for
+        for (uint32_t i = lane; i < held; i += 32)
+            if (room[i] > bar) top_room->pool[atomicAdd(&top_room->pooled, 1u)] = room[i];     // (in any order: none are alike)
+        __syncthreads();
+        pick<THREADS>(top_room->pool, top_room->pooled, top_room->best, top);
+    }
     return a;
 }
 
@@ -295,37 +405,36 @@ __device__ __forceinline__ uint64_t ld_dsmem_u64(uint32_t at) {
     return v;
 }
 
-template <typename T, bool ENT, bool TOP>
-__global__ void __launch_bounds__(kScoreThreads) logprobs_kernel(const __grid_constant__ cleave_logprobs_t d) {
-    __shared__ Sums warps[kScoreWarps], whole;
-    __shared__ typename std::conditional<TOP, TopRoom, int>::type top_room;
+template <typename T, bool ENT, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS, TOP ? 1024 / THREADS : 1536 / THREADS) logprobs_kernel(const __grid_constant__ cleave_logprobs_t d) {
+    __shared__ Sums warps[THREADS / 32], whole;
+    __shared__ typename std::conditional<TOP, TopRoom<THREADS>, int>::type top_room;
     begin_chained();
     const uint32_t part = blockIdx.x, parts = gridDim.x;
     const uint64_t row = blockIdx.y + (uint64_t)gridDim.y * blockIdx.z;
     if (row >= d.rows) return;                                   // (the whole cluster)
     const float c = d.scale * kLog2e;
     const T* x = static_cast<const T*>(d.x) + row * d.ldx;
-    TopRoom* top = nullptr;
+    int32_t token = -1;                                          // (asked for ahead of the scores)
+    if (d.logp && part == 0 && threadIdx.x == 0) token = load_token(d.ids, d.id_type, row, d.cols);
+    TopRoom<THREADS>* top = nullptr;
     if constexpr (TOP) top = &top_room;
-    Sums a = row_part<T, ENT, TOP>(x, d.cols, c, part, parts, warps, top, d.top);
+    Sums a = row_part<T, ENT, TOP, THREADS>(x, d.cols, c, part, parts, warps, top, d.top);
     if (parts > 1) a = cluster_join<ENT>(a, c, part, parts, &whole);
     if (part == 0) {
         if constexpr (TOP) {
             if (parts > 1) {
                 const uint32_t at = (uint32_t)__cvta_generic_to_shared(top_room.best);
-                for (uint32_t e = threadIdx.x; e < parts * d.top; e += kScoreThreads) top_room.pool[e] = ld_dsmem_u64(mapa_shared(at, e / d.top) + (e % d.top) * 8);
+                for (uint32_t e = threadIdx.x; e < parts * d.top; e += THREADS) top_room.pool[e] = ld_dsmem_u64(mapa_shared(at, e / d.top) + (e % d.top) * 8);
                 __syncthreads();
-                pick(top_room.pool, parts * d.top, top_room.room[0], d.top);     // (its own `best` may still be read)
+                pick<THREADS>(top_room.pool, parts * d.top, top_room.room[0], d.top);     // (its own `best` may still be read)
             }
         }
         const Stats r = stats_of(a, d.scale, c);
         if (threadIdx.x == 0) {
             if (d.lse) d.lse[row] = r.lse;
             if (ENT && d.entropy) d.entropy[row] = r.entropy;
-            if (d.logp) {
-                const int32_t t = load_token(d.ids, d.id_type, row, d.cols);
-                d.logp[row] = t < 0 ? 0.f : (r.lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[t]), -r.lse));
-            }
+            if (d.logp) d.logp[row] = token < 0 ? 0.f : (r.lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[token]), -r.lse));
         }
         if constexpr (TOP) {
             const uint64_t* best = parts > 1 ? top_room.room[0] : top_room.best;
@@ -341,18 +450,24 @@ __global__ void __launch_bounds__(kScoreThreads) logprobs_kernel(const __grid_co
 // CTAs a row: enough to fill the GPU a few times over, each with 16 KB of scores at least
 uint32_t row_parts(uint64_t rows, uint64_t row_bytes, int sms) {
     uint32_t parts = 1;
-    while (parts < 8 && rows * parts < (uint64_t)sms * 8 && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
+    while (parts < kPartsMost && rows * parts < (uint64_t)sms * 8 && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
     return parts;
 }
-struct RowGrid { dim3 cluster, grid; };
+// few: less than two CTAs an SM, which then have more threads (16 x 128000 fp32 8 us against 10 with 256); many rows go to
+// CTAs of 128, whose joins cost less (8192 x 50257 with entropy 143 us against 152 with 256).
+struct RowGrid { dim3 cluster, grid; bool few; };
 RowGrid row_grid(uint64_t rows, uint64_t row_bytes, int sms) {
     const uint32_t parts = row_parts(rows, row_bytes, sms), y = (uint32_t)std::min<uint64_t>(rows, 65535);
-    return {dim3(parts), dim3(parts, y, (unsigned)((rows + y - 1) / y))};
+    return {dim3(parts), dim3(parts, y, (unsigned)((rows + y - 1) / y)), rows * parts < 2 * (uint64_t)sms && row_bytes / parts >= 16 * 1024};
+}
+template <typename T, bool ENT, bool TOP>
+cudaError_t launch_logprobs_kernel(const cleave_logprobs_t& d, const RowGrid& g, cudaStream_t st) {
+    return g.few ? launch_chained_clusters(logprobs_kernel<T, ENT, TOP, 512>, g.cluster, g.grid, 512, 0, st, d)
+                 : launch_chained_clusters(logprobs_kernel<T, ENT, TOP, 128>, g.cluster, g.grid, 128, 0, st, d);
 }
 template <typename T, bool ENT>
 cudaError_t launch_logprobs_types(const cleave_logprobs_t& d, const RowGrid& g, cudaStream_t st) {
-    return d.top ? launch_chained_clusters(logprobs_kernel<T, ENT, true>, g.cluster, g.grid, kScoreThreads, 0, st, d)
-                 : launch_chained_clusters(logprobs_kernel<T, ENT, false>, g.cluster, g.grid, kScoreThreads, 0, st, d);
+    return d.top ? launch_logprobs_kernel<T, ENT, true>(d, g, st) : launch_logprobs_kernel<T, ENT, false>(d, g, st);
 }
 cudaError_t launch_logprobs(const cleave_logprobs_t& d, int sms, cudaStream_t st) {
     const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms);
@@ -507,11 +622,11 @@ cudaError_t launch_logprobs_backward(const cleave_logprobs_backward_t& d, int sm
 }
 
 // ---- distillation ------------------------------------------------------------------------------------------
-// The row's teacher: thread k < d.k has place k (or -1) and q_k; `log_q` where q_k > 0; `all`, the sum of q, in every thread.  Every
-// warp reads the whole row (at most 8 entries a lane), so nothing waits for another warp.
-struct Place { int32_t j; float q, log_q, all; };
+// The row's teacher: `take(k, j, q, log_q)` for the entries of this thread's share whose q is not 0, and the sum of q to every thread.
+// Every warp reads the whole row (at most 8 entries a lane), so nothing waits for another warp; the entries are shared out 32 by 32.
 constexpr int kEntries = CLEAVE_DISTILL_MOST / 32;
-__device__ __forceinline__ Place teacher(const cleave_distill_t& d, uint64_t row) {
+template <int THREADS, typename TAKE>
+__device__ __forceinline__ float teacher(const cleave_distill_t& d, uint64_t row, TAKE&& take) {
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     float v[kEntries], top = -INFINITY;
     int32_t j[kEntries];
@@ -530,24 +645,21 @@ __device__ __forceinline__ Place teacher(const cleave_distill_t& d, uint64_t row
         v[i] = j[i] < 0 ? -INFINITY : d.scale * v[i];
         top = max_nan(top, v[i]);
     }
-    Place p = {-1, 0.f, 0.f, 0.f};
     top = d.normalize ? warp_max_nan(top) : 0.f;
-    if (top == -INFINITY) return p;                              // an empty row
+    if (top == -INFINITY) return 0.f;                            // an empty row
     float e[kEntries], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < kEntries; ++i) { v[i] -= top; e[i] = exp2_fast(v[i] * kLog2e); sum += e[i]; }
     sum = warp_sum(sum);
     const float inv = d.normalize ? 1.f / sum : 1.f, log_sum = d.normalize ? logf(sum) : 0.f;
-    p.all = d.normalize ? sum * inv : sum;
 #pragma unroll
     for (int i = 0; i < kEntries; ++i)
-        if (warp == i) { p.j = j[i]; p.q = e[i] * inv; p.log_q = v[i] - log_sum; }
-    if (p.q == 0.f) p.j = -1;
-    return p;
+        if (i % (THREADS / 32) == warp && e[i] * inv != 0.f) take(lane + 32 * i, (uint32_t)j[i], e[i] * inv, v[i] - log_sum);
+    return sum * inv;
 }
-template <typename T>
-__global__ void __launch_bounds__(kScoreThreads) distill_kernel(const __grid_constant__ cleave_distill_t d) {
-    __shared__ Sums warps[kScoreWarps], whole;
+template <typename T, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const __grid_constant__ cleave_distill_t d) {
+    __shared__ Sums warps[THREADS / 32], whole;
     __shared__ float buf[32];
     begin_chained();
     const uint32_t part = blockIdx.x, parts = gridDim.x;
@@ -555,13 +667,14 @@ __global__ void __launch_bounds__(kScoreThreads) distill_kernel(const __grid_con
     if (row >= d.rows) return;
     const float c = d.scale * kLog2e;
     const T* x = static_cast<const T*>(d.x) + row * d.ldx;
-    Sums a = row_part<T, false, false>(x, d.cols, c, part, parts, warps, nullptr, 0);
+    Sums a = row_part<T, false, false, THREADS>(x, d.cols, c, part, parts, warps, nullptr, 0);
     if (parts > 1) a = cluster_join<false>(a, c, part, parts, &whole);
     if (part == 0) {
         const float lse = stats_of(a, d.scale, c).lse;
-        const Place p = teacher(d, row);
         float term = 0.f;
-        if (p.j >= 0) term = p.q * (p.log_q - (lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[p.j]), -lse)));
+        teacher<THREADS>(d, row, [&](uint32_t, uint32_t j, float q, float log_q) {
+            term = fmaf(q, log_q - (lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[j]), -lse)), term);
+        });
         term = cta_sum(term, buf);
         if (threadIdx.x == 0) {
             d.loss[row] = term;
@@ -570,14 +683,17 @@ __global__ void __launch_bounds__(kScoreThreads) distill_kernel(const __grid_con
     }
     if (parts > 1) cluster_arrive_wait();
 }
+template <typename T>
+cudaError_t launch_distill_types(const cleave_distill_t& d, const RowGrid& g, cudaStream_t st) {
+    return g.few ? launch_chained_clusters(distill_kernel<T, 512>, g.cluster, g.grid, 512, 0, st, d) : launch_chained_clusters(distill_kernel<T, 128>, g.cluster, g.grid, 128, 0, st, d);
+}
 cudaError_t launch_distill(const cleave_distill_t& d, int sms, cudaStream_t st) {
     const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms);
-    return d.x_type == CLEAVE_T_F32 ? launch_chained_clusters(distill_kernel<float>, g.cluster, g.grid, kScoreThreads, 0, st, d)
-                                    : launch_chained_clusters(distill_kernel<__nv_bfloat16>, g.cluster, g.grid, kScoreThreads, 0, st, d);
+    return d.x_type == CLEAVE_T_F32 ? launch_distill_types<float>(d, g, st) : launch_distill_types<__nv_bfloat16>(d, g, st);
 }
 template <typename X, typename D, bool WIDE>
 __global__ void __launch_bounds__(kScoreThreads) distill_backward_kernel(const __grid_constant__ cleave_distill_backward_t d) {
-    __shared__ int32_t places[CLEAVE_DISTILL_MOST];
+    __shared__ uint32_t places[CLEAVE_DISTILL_MOST];
     __shared__ float weights[CLEAVE_DISTILL_MOST];
     begin_chained();
     const uint64_t row = row_from_end(d.f.rows);
@@ -590,21 +706,25 @@ __global__ void __launch_bounds__(kScoreThreads) distill_backward_kernel(const _
     const uint32_t first = WIDE ? row_columns<X, D, WIDE>(x, dx, d.f.cols, 0, 1).head : 0u, unit = WIDE ? 8u : 1u;
     const uint32_t from = first + p.begin * unit - p.head, to = first + p.end * unit + p.tail;
     bool named = false;
+    uint32_t place = 0;
     float own = 0.f;
-    Place t = {-1, 0.f, 0.f, 0.f};
     auto slope = [&] {
         const float lse = d.f.lse[row], up = d.dloss[row];
-        t = teacher(d.f, row);
-        if (threadIdx.x < d.f.k) { places[threadIdx.x] = t.j; weights[threadIdx.x] = t.q; }
-        const RowSlope g = {lse, up == 0.f || t.all == 0.f ? 0.f : up * t.all * d.f.scale, 0.f};
-        named = t.j >= 0 && up != 0.f && lse != -INFINITY && (uint32_t)t.j >= from && (uint32_t)t.j < to;
+        if (threadIdx.x < d.f.k) places[threadIdx.x] = 0xFFFFFFFFu;
+        const float all = teacher<kScoreThreads>(d.f, row, [&](uint32_t k, uint32_t j, float q, float) {        // (k is threadIdx.x)
+            places[k] = place = j;
+            weights[k] = q;
+            named = j >= from && j < to;
+        });
+        const RowSlope g = {lse, up == 0.f || all == 0.f ? 0.f : up * all * d.f.scale, 0.f};
+        named = named && up != 0.f && lse != -INFINITY;
         float score = 0.f;
-        if (named) score = to_f32(x[t.j]);
+        if (named) score = to_f32(x[place]);
         __syncthreads();
         if (named) {
             float q = 0.f;
             for (uint32_t k = 0; k < d.f.k; ++k)
-                if (places[k] == t.j) { q += weights[k]; named = named && k >= threadIdx.x; }      // of entries with the same place the first writes
+                if (places[k] == place) { q += weights[k]; named = named && k >= threadIdx.x; }        // of entries with the same place the first writes
             own = slope_at<false>(score, d.f.scale, g) - up * d.f.scale * q;
         }
         return g;
@@ -615,7 +735,7 @@ __global__ void __launch_bounds__(kScoreThreads) distill_backward_kernel(const _
     };
     write_part<X, D, false, WIDE>(x, dx, d.f.cols, d.f.scale, blockIdx.x, gridDim.x, slope, Fix{});
     __syncthreads();
-    if (named) dx[t.j] = from_f32<D>(own);
+    if (named) dx[place] = from_f32<D>(own);
 }
 template <typename X, typename D>
 cudaError_t launch_distill_backward_types(const cleave_distill_backward_t& d, dim3 grid, cudaStream_t st) {

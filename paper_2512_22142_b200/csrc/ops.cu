@@ -42,7 +42,7 @@ int cuda_code(cudaError_t e) {
 }
 // token numbers: `n` of them, `ld` apart from row to row where they have rows
 bool ids_ok(const void* p, uint32_t type) { return id_bytes(type) && p && aligned(p, id_bytes(type)); }
-bool scale_ok(float s) { return std::isfinite(s) && s > 0.f; }
+bool scale_ok(float s) { return s >= 0x1p-100f && s <= 0x1p100f; }            // (false for NaN)
 // SM count of the current device, or a negative CLEAVE_E_* code (asked for once per device)
 int need_device() {
     static std::atomic<int> known[64];
