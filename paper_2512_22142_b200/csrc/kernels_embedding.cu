@@ -1,42 +1,89 @@
 // Embedding lookup and its gradient by sorted tokens (see cleave.h).
 //
-// Lookup: out_i = scale table[ids_i].
+// Lookup: out_i = scale table[ids_i].  A warp takes 1024 columns of a row, four 16-byte groups a lane, all of them asked for at
+// once; bound by the HBM (few rows: by one token's and one row's latency).
 //
 // Gradient.  The rows of dy have to be added by token, in an order that does not change from run to run, and a vocabulary's
 // tokens are far from evenly spread (a few make up half of a batch).  So:
 //   order    the tokens' places are sorted by (token, place): a counting sort without communication.  CTA c owns a
 //            range of the vocabulary and reads all tokens (n of them stand in L2): what is below its range is its offset,
-//            what is inside is counted per warp and value; a second reading puts each place where it belongs.
+//            what is inside is counted per warp and value; a second reading puts each place where it belongs.  Its time does
+//            not depend on the tokens' distribution.
 //   sum      the sorted places are cut into chunks of the same length, whatever the tokens; a CTA adds the rows of a
 //            chunk run by run.  A run that lies inside one chunk is a finished row; the ends of longer runs go to the workspace.
 //            Other CTAs of the launch write zeros into the rows of tokens that do not occur.
 //   join     the pieces of each longer run are added in order.
+// Bound by the HBM where the whole table is written, by the three launches' latencies where few rows are.
 #include <algorithm>
+#include <type_traits>
 
 #include "tokens.cuh"
 
 namespace cleave {
 
 // ---- lookup ------------------------------------------------------------------------------------------
-__global__ void __launch_bounds__(256) embedding_any_kernel(const __grid_constant__ cleave_embedding_t d) {
+// WIDE: an item is 1024 columns of a row, in groups of 8; else 256 columns, neighbouring lanes next to each other.
+template <typename X, typename D, bool WIDE>
+__global__ void __launch_bounds__(256) embedding_kernel(const __grid_constant__ cleave_embedding_t d, uint32_t row_items) {
     begin_chained();
-    const uint64_t row = blockIdx.x;
+    const uint64_t item = (uint64_t)blockIdx.x * 8 + (threadIdx.x >> 5), row = item / row_items;
+    if (row >= d.n) return;
+    const uint32_t lane = threadIdx.x & 31u, j0 = (uint32_t)(item % row_items) * (WIDE ? 1024u : 256u);
     const int32_t t = load_token(d.ids, d.id_type, row, d.vocab);
-    for (uint32_t j = threadIdx.x; j < d.cols; j += blockDim.x)
-        store_as(d.out, d.out_type, row * d.ldo + j, t < 0 ? 0.f : d.scale * load_as(d.table, d.table_type, (uint64_t)t * d.ldt + j));
+    const X* from = static_cast<const X*>(d.table) + (uint64_t)max(t, 0) * d.ldt;
+    D* to = static_cast<D*>(d.out) + row * d.ldo;
+    if constexpr (WIDE) {
+        Raw8<X> raw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t j = j0 + (lane + 32 * i) * 8;
+            if (j < d.cols && t >= 0) {
+#pragma unroll
+                for (int k = 0; k < (int)(sizeof(raw[i].w) / 16); ++k) raw[i].w[k] = reinterpret_cast<const uint4*>(from + j)[k];
+            }
+        }
+        const F2 scale = f2(d.scale, d.scale);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t j = j0 + (lane + 32 * i) * 8;
+            if (j >= d.cols) continue;
+            F2 v[4] = {f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f), f2(0.f, 0.f)};
+            if (t >= 0) {
+                unpack8(raw[i], v);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = mul2(v[k], scale);
+            }
+            store8(to + j, v);
+        }
+    } else {
+        X raw[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (j0 + lane + 32 * i < d.cols && t >= 0) raw[i] = from[j0 + lane + 32 * i];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) if (j0 + lane + 32 * i < d.cols) to[j0 + lane + 32 * i] = from_f32<D>(t < 0 ? 0.f : d.scale * to_f32(raw[i]));
+    }
 }
-cudaError_t launch_embedding(const cleave_embedding_t& d, int, cudaStream_t st) {
-    return launch_chained(embedding_any_kernel, (unsigned)d.n, 256, 0, st, d);
+template <typename X, typename D>
+cudaError_t launch_embedding_types(const cleave_embedding_t& d, bool wide, cudaStream_t st) {
+    const uint32_t items = wide ? (d.cols + 1023) / 1024 : (d.cols + 255) / 256;
+    const uint64_t ctas = (d.n * items + 7) / 8;
+    return launch_chained(wide ? embedding_kernel<X, D, true> : embedding_kernel<X, D, false>, (unsigned)ctas, 256, 0, st, d, items);
+}
+cudaError_t launch_embedding(const cleave_embedding_t& d, cudaStream_t st) {
+    const bool wide = d.cols % 8 == 0 && rows_wide(d.table, d.ldt, d.table_type) && rows_wide(d.out, d.ldo, d.out_type);
+    if (d.table_type == CLEAVE_T_F32) return d.out_type == CLEAVE_T_F32 ? launch_embedding_types<float, float>(d, wide, st) : launch_embedding_types<float, __nv_bfloat16>(d, wide, st);
+    return d.out_type == CLEAVE_T_F32 ? launch_embedding_types<__nv_bfloat16, float>(d, wide, st) : launch_embedding_types<__nv_bfloat16, __nv_bfloat16>(d, wide, st);
 }
 
 // ---- gradient: the tokens' order ------------------------------------------------------------------------
 constexpr uint32_t kOrderThreads = 512, kOrderWarps = kOrderThreads / 32, kOrderMost = 2 * kOrderThreads;     // values a CTA owns at most
+constexpr int kOrderAhead = 4;                   // loads of 32 tokens under way
 
 uint32_t order_values(uint32_t vocab) { return std::min(kOrderMost, std::max(32u, (vocab + kPartSms - 1) / kPartSms)); }
 
-// offsets[v] = number of tokens below v, for v <= vocab; order[offsets[v] ...] = the places of token v, ascending
+// offsets[v] = number of tokens below v, for v <= vocab; sorted[offsets[v] ...] = (place, v), places ascending
 template <typename ID>
-__global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* ids, uint32_t n, uint32_t vocab, uint32_t values, uint32_t* offsets, uint32_t* order) {
+__global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* ids, uint32_t n, uint32_t vocab, uint32_t values, uint32_t* offsets, uint2* sorted) {
     extern __shared__ uint32_t counts[];                         // [warp][value]
     __shared__ uint32_t sums[32], below_all;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, lo = blockIdx.x * values, hi = min(vocab, lo + values);
@@ -47,12 +94,20 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
     __syncthreads();
     const uint32_t part = ((n + kOrderWarps - 1) / kOrderWarps + 31) / 32 * 32;
     const uint64_t from = (uint64_t)warp * part, to = min((uint64_t)n, from + part);
+    auto load = [&](uint64_t i, ID (&t)[kOrderAhead]) {          // 32 tokens each, in order; -1 behind the warp's part
+#pragma unroll
+        for (int k = 0; k < kOrderAhead; ++k) t[k] = i + 32 * k + lane < to ? ids[i + 32 * k + lane] : (ID)-1;
+    };
     uint32_t below = 0;
-    for (uint64_t i = from + lane; i < to; i += 32) {
-        const ID t = ids[i];
-        if (t < 0) continue;
-        if ((uint64_t)t < lo) ++below;
-        else if ((uint64_t)t < hi) atomicAdd(mine + (uint32_t)(t - lo), 1u);
+    for (uint64_t i = from; i < to; i += 32 * kOrderAhead) {
+        ID t[kOrderAhead];
+        load(i, t);
+#pragma unroll
+        for (int k = 0; k < kOrderAhead; ++k) {
+            if (t[k] < 0) continue;
+            if ((uint64_t)t[k] < lo) ++below;
+            else if ((uint64_t)t[k] < hi) atomicAdd(mine + (uint32_t)(t[k] - lo), 1u);
+        }
     }
     below = __reduce_add_sync(0xFFFFFFFFu, below);
     if (lane == 0 && below) atomicAdd(&below_all, below);        // (whole numbers: any order)
@@ -63,7 +118,8 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
     for (uint32_t k = 0; k < 2; ++k) {
         const uint32_t v = 2 * threadIdx.x + k;
         if (v < values)
-            for (uint32_t w = 0; w < kOrderWarps; ++w) { const uint32_t c = counts[w * values + v]; counts[w * values + v] = total[k]; total[k] += c; }
+#pragma unroll 8
+            for (uint32_t w = 0; w < kOrderWarps; ++w) total[k] += counts[w * values + v];
     }
     uint32_t sum = total[0] + total[1], up = sum;
     for (uint32_t o = 1; o < 32; o <<= 1) { const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, up, o); if (lane >= o) up += x; }
@@ -76,25 +132,30 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
         const uint32_t v = 2 * threadIdx.x + k;
         if (v < values && lo + v < hi) {
             offsets[lo + v] = before;
-            for (uint32_t w = 0; w < kOrderWarps; ++w) counts[w * values + v] += before;
+            uint32_t at = before;
+#pragma unroll 8
+            for (uint32_t w = 0; w < kOrderWarps; ++w) { const uint32_t c = counts[w * values + v]; counts[w * values + v] = at; at += c; }
         }
         before += total[k];
         if (v < values && lo + v + 1 == vocab) offsets[vocab] = before;
     }
     __syncthreads();
-    for (uint64_t i = from; i < to; i += 32) {                   // in order: 32 places at a time
-        const uint64_t at = i + lane;
-        const int64_t t = at < to ? (int64_t)ids[at] : -1;
-        const bool in = t >= (int64_t)lo && t < (int64_t)hi;
-        const uint32_t some = __ballot_sync(0xFFFFFFFFu, in);
-        if (in) {
-            const uint32_t same = __match_any_sync(some, (uint32_t)(t - lo)), rank = __popc(same & ((1u << lane) - 1u));
-            const uint32_t base = mine[(uint32_t)(t - lo)];
-            order[base + rank] = (uint32_t)at;
-            __syncwarp(some);
-            if (rank == 0) mine[(uint32_t)(t - lo)] = base + __popc(same);
+    for (uint64_t i = from; i < to; i += 32 * kOrderAhead) {
+        ID t[kOrderAhead];
+        load(i, t);
+#pragma unroll
+        for (int k = 0; k < kOrderAhead; ++k) {
+            const bool in = t[k] >= 0 && (uint64_t)t[k] >= lo && (uint64_t)t[k] < hi;
+            const uint32_t some = __ballot_sync(0xFFFFFFFFu, in);
+            if (!some) continue;
+            if (in) {
+                const uint32_t v = (uint32_t)(t[k] - lo), same = __match_any_sync(some, v), rank = __popc(same & ((1u << lane) - 1u)), base = mine[v];
+                sorted[base + rank] = make_uint2((uint32_t)(i + 32 * k + lane), lo + v);
+                __syncwarp(some);
+                if (rank == 0) mine[v] = base + __popc(same);
+            }
+            __syncwarp();
         }
-        __syncwarp();
     }
 }
 
@@ -104,81 +165,210 @@ uint32_t sum_chunk(uint64_t n) { return (uint32_t)std::max<uint64_t>(kChunkLeast
 
 struct Ordered {                    // what the order kernel left
     const uint32_t* offsets;
-    const uint32_t* order;
-    float* parts;                   // [2 chunk + 0: the run that began before the chunk, 1: the run that goes on after it][cols]
+    const uint2* sorted;
+    float* parts;                   // [2 chunk + 0: the run that began before the chunk, 1: the run that begins in it and goes on][cols]
     uint32_t chunk, chunks;
 };
-constexpr uint32_t kSumThreads = 256;
+constexpr uint32_t kZeroRows = 32;               // rows that a CTA looks through for absent tokens
+constexpr int kRowsAhead = 4;                    // rows of dy under way
 
-__device__ __forceinline__ void finish_row(const cleave_embedding_backward_t& d, uint32_t v, uint32_t j, float sum) {
-    const uint64_t at = (uint64_t)v * d.lddt + j;
-    sum *= d.scale;
-    if (d.accumulate) sum += load_as(d.dtable, d.dtable_type, at);
-    store_as(d.dtable, d.dtable_type, at, sum);
-}
-__global__ void __launch_bounds__(kSumThreads) embedding_sum_any_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o, uint32_t zero_rows) {
+// what a thread holds of a row: 8 columns (wide) or one
+template <typename T, bool WIDE> struct Cols;
+template <typename T> struct Cols<T, true> {
+    Raw8<T> r;
+    __device__ __forceinline__ void load(const T* p) {
+#pragma unroll
+        for (int k = 0; k < (int)(sizeof(r.w) / 16); ++k) r.w[k] = reinterpret_cast<const uint4*>(p)[k];
+    }
+};
+template <typename T> struct Cols<T, false> {
+    T r;
+    __device__ __forceinline__ void load(const T* p) { r = *p; }
+};
+template <bool WIDE> struct Acc;
+template <> struct Acc<true> {
+    F2 v[4];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = f2(0.f, 0.f);
+    }
+    template <typename T> __device__ __forceinline__ void add(const Cols<T, true>& c) {
+        F2 x[4];
+        unpack8(c.r, x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = add2(v[i], x[i]);
+    }
+    __device__ __forceinline__ void scale(float s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], f2(s, s));
+    }
+    template <typename T> __device__ __forceinline__ void store(T* p) const { store8(p, v); }
+};
+template <> struct Acc<false> {
+    float v;
+    __device__ __forceinline__ void clear() { v = 0.f; }
+    template <typename T> __device__ __forceinline__ void add(const Cols<T, false>& c) { v += to_f32(c.r); }
+    __device__ __forceinline__ void scale(float s) { v *= s; }
+    template <typename T> __device__ __forceinline__ void store(T* p) const { *p = from_f32<T>(v); }
+};
+
+template <typename X, typename D, bool WIDE>
+__global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
+    constexpr uint32_t W = WIDE ? 8 : 1;
     begin_chained();
-    const uint32_t column = blockIdx.y * kSumThreads + threadIdx.x, columns = gridDim.y * kSumThreads;
+    const uint32_t lane = threadIdx.x & 31u, columns = gridDim.y * blockDim.x * W;
     if (blockIdx.x >= o.chunks) {                                // rows of tokens that do not occur
-        const uint64_t v0 = (uint64_t)(blockIdx.x - o.chunks) * zero_rows;
-        for (uint64_t v = v0; v < min((uint64_t)d.vocab, v0 + zero_rows); ++v)
-            if (o.offsets[v] == o.offsets[v + 1])
-                for (uint32_t j = column; j < d.cols; j += columns) store_as(d.dtable, d.dtable_type, v * d.lddt + j, 0.f);
+        const uint64_t v0 = (uint64_t)(blockIdx.x - o.chunks) * kZeroRows;
+        static_assert(kZeroRows == 32, "a lane looks at a row");
+        const bool absent = v0 + lane < d.vocab && o.offsets[v0 + lane] == o.offsets[v0 + lane + 1];
+        for (uint32_t rows = __ballot_sync(0xFFFFFFFFu, absent); rows; rows &= rows - 1) {
+            D* row = static_cast<D*>(d.dtable) + (v0 + (uint32_t)__ffs((int)rows) - 1) * d.lddt;
+            Acc<WIDE> zero;
+            zero.clear();
+            for (uint32_t j = (blockIdx.y * blockDim.x + threadIdx.x) * W; j < d.cols; j += columns) zero.store(row + j);
+        }
         return;
     }
     const uint32_t total = o.offsets[d.vocab], first = blockIdx.x * o.chunk, last = min(total, first + o.chunk);
-    for (uint32_t p = first; p < last;) {
-        const uint32_t v = (uint32_t)load_token(d.ids, d.id_type, o.order[p], d.vocab), begin = o.offsets[v], end = o.offsets[v + 1], stop = min(end, last);
-        for (uint32_t j = column; j < d.cols; j += columns) {
-            float sum = 0.f;
-            for (uint32_t i = p; i < stop; ++i) sum += load_as(d.dy, d.dy_type, (uint64_t)o.order[i] * d.lddy + j);
-            if (begin >= first && end <= last) finish_row(d, v, j, sum);
-            else o.parts[((uint64_t)blockIdx.x * 2 + (begin < first ? 0 : 1)) * d.cols + j] = sum;
+    if (first >= last) return;
+    for (uint32_t j = (blockIdx.y * blockDim.x + threadIdx.x) * W; j - lane * W < d.cols; j += columns) {       // (a warp stays together)
+        const bool live = j < d.cols;
+        const X* dy = static_cast<const X*>(d.dy) + j;
+        D* dt = static_cast<D*>(d.dtable) + j;
+        Acc<WIDE> acc;
+        acc.clear();
+        bool before = false, open = false;                       // the run began before the chunk; it goes on at the end of it
+        for (uint32_t base = first; base < last; base += 32) {
+            // a lane looks at a place: its row, its token, whether its run ends there
+            const uint32_t p = base + lane;
+            const uint2 here = p < last ? o.sorted[p] : make_uint2(0u, 0u);
+            const bool ends = p < last && (p + 1 >= total || o.sorted[p + 1].y != here.y);
+            if (base == first) before = first > 0 && o.sorted[first - 1].y == __shfl_sync(0xFFFFFFFFu, here.y, 0);
+            const uint32_t stops = __ballot_sync(0xFFFFFFFFu, ends), count = min(32u, last - base);
+            for (uint32_t i = 0; i < count; i += kRowsAhead) {
+                Cols<X, WIDE> x[kRowsAhead];
+                Cols<D, WIDE> old[kRowsAhead];
+#pragma unroll
+                for (int k = 0; k < kRowsAhead; ++k) {
+                    const uint32_t row = __shfl_sync(0xFFFFFFFFu, here.x, (i + k) & 31u), v = __shfl_sync(0xFFFFFFFFu, here.y, (i + k) & 31u);
+                    if (!live || i + k >= count) continue;
+                    x[k].load(dy + (uint64_t)row * d.lddy);
+                    if (d.accumulate && (stops >> (i + k) & 1u)) old[k].load(dt + (uint64_t)v * d.lddt);       // (not used where the run's other piece is missing)
+                }
+#pragma unroll
+                for (int k = 0; k < kRowsAhead; ++k) {
+                    const uint32_t v = __shfl_sync(0xFFFFFFFFu, here.y, (i + k) & 31u);
+                    if (i + k >= count) continue;
+                    open = !(stops >> (i + k) & 1u);
+                    if (live) {
+                        acc.add(x[k]);
+                        if (!open) {
+                            if (before) acc.store(o.parts + (uint64_t)blockIdx.x * 2 * d.cols + j);
+                            else {
+                                acc.scale(d.scale);
+                                if (d.accumulate) acc.add(old[k]);
+                                acc.store(dt + (uint64_t)v * d.lddt);
+                            }
+                            acc.clear();
+                        }
+                    }
+                    if (!open) before = false;
+                }
+            }
         }
-        p = stop;
-    }
-}
-__global__ void __launch_bounds__(kSumThreads) embedding_join_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
-    begin_chained();
-    const uint32_t total = o.offsets[d.vocab], first = blockIdx.x * o.chunk, after = first + o.chunk;
-    if (after >= total) return;                                  // nothing goes on behind the chunk
-    const uint32_t v = (uint32_t)load_token(d.ids, d.id_type, o.order[after - 1], d.vocab), begin = o.offsets[v], end = o.offsets[v + 1];
-    if (begin < first || end <= after) return;                   // the run began before the chunk, or ends with it
-    for (uint32_t j = blockIdx.y * kSumThreads + threadIdx.x; j < d.cols; j += gridDim.y * kSumThreads) {
-        float sum = o.parts[((uint64_t)blockIdx.x * 2 + 1) * d.cols + j];
-        for (uint32_t c = blockIdx.x + 1; c <= (end - 1) / o.chunk; ++c) sum += o.parts[(uint64_t)c * 2 * d.cols + j];
-        finish_row(d, v, j, sum);
+        if (open && live) acc.store(o.parts + ((uint64_t)blockIdx.x * 2 + (before ? 0 : 1)) * d.cols + j);
     }
 }
 
-static uint64_t order_bytes(uint64_t n, uint32_t vocab) { return ((uint64_t)vocab + 1 + n + 3) / 4 * 16; }
+// A CTA looks at 8 chunks; for each whose last run begins in it and goes on, its warps add the pieces w, w + 8, ... of 32 lanes'
+// columns, and the warps' sums are added in order.
+template <typename D, bool WIDE>
+__global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
+    constexpr uint32_t W = WIDE ? 8 : 1;
+    __shared__ __align__(16) float s[8][32 * W];
+    begin_chained();
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, total = o.offsets[d.vocab];
+    uint32_t v = 0;
+    bool starts = false;
+    if (lane < 8) {
+        const uint32_t c = blockIdx.x * 8 + lane;
+        const uint64_t first = (uint64_t)c * o.chunk, after = first + o.chunk;
+        if (after < total) {
+            v = o.sorted[after - 1].y;
+            starts = o.sorted[after].y == v && (o.sorted[first].y != v || first == 0 || o.sorted[first - 1].y != v);
+        }
+    }
+    for (uint32_t some = __ballot_sync(0xFFFFFFFFu, starts); some; some &= some - 1) {
+        const uint32_t k = (uint32_t)__ffs((int)some) - 1, c0 = blockIdx.x * 8 + k, token = __shfl_sync(0xFFFFFFFFu, v, k);
+        const uint32_t pieces = (o.offsets[token + 1] - 1) / o.chunk - c0 + 1;
+        for (uint32_t j0 = blockIdx.y * 32 * W; j0 < d.cols; j0 += gridDim.y * 32 * W) {
+            const uint32_t j = j0 + lane * W;
+            Acc<WIDE> acc;
+            acc.clear();
+            if (j < d.cols) {
+#pragma unroll 4
+                for (uint32_t c = warp; c < pieces; c += 8) {
+                    Cols<float, WIDE> x;
+                    x.load(o.parts + ((uint64_t)(c0 + c) * 2 + (c == 0 ? 1 : 0)) * d.cols + j);
+                    acc.add(x);
+                }
+            }
+            acc.store(&s[warp][lane * W]);
+            __syncthreads();
+            if (warp == 0 && j < d.cols) {
+                acc.clear();
+#pragma unroll
+                for (uint32_t w = 0; w < 8; ++w) { Cols<float, WIDE> x; x.load(&s[w][lane * W]); acc.add(x); }
+                D* dt = static_cast<D*>(d.dtable) + (uint64_t)token * d.lddt + j;
+                acc.scale(d.scale);
+                if (d.accumulate) { Cols<D, WIDE> old; old.load(dt); acc.add(old); }
+                acc.store(dt);
+            }
+            __syncthreads();
+        }
+    }
+}
+
+static uint64_t offsets_bytes(uint32_t vocab) { return ((uint64_t)vocab + 1 + 3) / 4 * 16; }
+static uint64_t order_bytes(uint64_t n, uint32_t vocab) { return offsets_bytes(vocab) + (n + 1) / 2 * 16; }
 uint64_t embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols) {
     const uint64_t chunks = n ? (n + sum_chunk(n) - 1) / sum_chunk(n) : 0;
     return order_bytes(n, vocab) + chunks * 2 * cols * sizeof(float);
 }
-cudaError_t launch_embedding_backward(const cleave_embedding_backward_t& d, void* ws, cudaStream_t st) {
-    const uint32_t values = order_values(d.vocab), n = (uint32_t)d.n;
-    uint32_t* offsets = static_cast<uint32_t*>(ws);
-    uint32_t* order = offsets + d.vocab + 1;
-    Ordered o = {offsets, order, reinterpret_cast<float*>(static_cast<uint8_t*>(ws) + order_bytes(n, d.vocab)), sum_chunk(n), 0};
-    o.chunks = (n + o.chunk - 1) / o.chunk;
-    const uint32_t smem = kOrderWarps * values * 4;
-    const unsigned ctas = (d.vocab + values - 1) / values;
-    static SmemLimit limits[2];
-    cudaError_t e;
-    if (d.id_type == CLEAVE_T_I64) {
-        e = limits[1].raise(reinterpret_cast<const void*>(token_order_kernel<int64_t>), kOrderWarps * kOrderMost * 4);
-        if (e == cudaSuccess) e = launch_chained(token_order_kernel<int64_t>, ctas, kOrderThreads, smem, st, static_cast<const int64_t*>(d.ids), n, d.vocab, values, offsets, order);
-    } else {
-        e = limits[0].raise(reinterpret_cast<const void*>(token_order_kernel<int32_t>), kOrderWarps * kOrderMost * 4);
-        if (e == cudaSuccess) e = launch_chained(token_order_kernel<int32_t>, ctas, kOrderThreads, smem, st, static_cast<const int32_t*>(d.ids), n, d.vocab, values, offsets, order);
-    }
+template <typename ID>
+cudaError_t launch_order(const cleave_embedding_backward_t& d, uint32_t* offsets, uint2* sorted, cudaStream_t st) {
+    const uint32_t values = order_values(d.vocab);
+    static SmemLimit limit;
+    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(token_order_kernel<ID>), kOrderWarps * kOrderMost * 4);
     if (e != cudaSuccess) return e;
-    const uint32_t zero_rows = 64, tiles = std::min(65535u, (d.cols + kSumThreads - 1) / kSumThreads);
-    const unsigned zeros = d.accumulate ? 0 : (d.vocab + zero_rows - 1) / zero_rows;
-    if (o.chunks + zeros) e = launch_chained(embedding_sum_any_kernel, dim3(o.chunks + zeros, tiles), kSumThreads, 0, st, d, o, zero_rows);
+    return launch_chained(token_order_kernel<ID>, (d.vocab + values - 1) / values, kOrderThreads, kOrderWarps * values * 4, st, static_cast<const ID*>(d.ids), (uint32_t)d.n, d.vocab, values,
+                          offsets, sorted);
+}
+template <typename X, typename D, bool WIDE>
+cudaError_t launch_sums(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
+    const uint32_t units = WIDE ? d.cols / 8 : d.cols, tiles = std::min(65535u, (units + 255) / 256), threads = std::min(256u, ((units + tiles - 1) / tiles + 31) / 32 * 32);
+    const unsigned zeros = d.accumulate ? 0 : (d.vocab + kZeroRows - 1) / kZeroRows;
+    cudaError_t e = cudaSuccess;
+    if (o.chunks + zeros) e = launch_chained(embedding_sum_kernel<X, D, WIDE>, dim3(o.chunks + zeros, tiles), threads, 0, st, d, o);
     if (e != cudaSuccess || o.chunks < 2) return e;
-    return launch_chained(embedding_join_kernel, dim3(o.chunks - 1, tiles), kSumThreads, 0, st, d, o);
+    return launch_chained(embedding_join_kernel<D, WIDE>, dim3((o.chunks + 7) / 8, std::min(65535u, (units + 31) / 32)), 256, 0, st, d, o);
+}
+template <typename X, typename D>
+cudaError_t launch_sums_types(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
+    // (the pieces in the workspace stand on 16 bytes with whole groups of 8 columns)
+    const bool wide = d.cols % 8 == 0 && rows_wide(d.dy, d.lddy, d.dy_type) && rows_wide(d.dtable, d.lddt, d.dtable_type);
+    return wide ? launch_sums<X, D, true>(d, o, st) : launch_sums<X, D, false>(d, o, st);
+}
+cudaError_t launch_embedding_backward(const cleave_embedding_backward_t& d, void* ws, cudaStream_t st) {
+    uint8_t* w = static_cast<uint8_t*>(ws);
+    uint32_t* offsets = reinterpret_cast<uint32_t*>(w);
+    uint2* sorted = reinterpret_cast<uint2*>(w + offsets_bytes(d.vocab));
+    Ordered o = {offsets, sorted, reinterpret_cast<float*>(w + order_bytes(d.n, d.vocab)), sum_chunk(d.n), 0};
+    o.chunks = (uint32_t)((d.n + o.chunk - 1) / o.chunk);
+    const cudaError_t e = d.id_type == CLEAVE_T_I64 ? launch_order<int64_t>(d, offsets, sorted, st) : launch_order<int32_t>(d, offsets, sorted, st);
+    if (e != cudaSuccess) return e;
+    if (d.dy_type == CLEAVE_T_F32) return d.dtable_type == CLEAVE_T_F32 ? launch_sums_types<float, float>(d, o, st) : launch_sums_types<float, __nv_bfloat16>(d, o, st);
+    return d.dtable_type == CLEAVE_T_F32 ? launch_sums_types<__nv_bfloat16, float>(d, o, st) : launch_sums_types<__nv_bfloat16, __nv_bfloat16>(d, o, st);
 }
 
 }  // namespace cleave

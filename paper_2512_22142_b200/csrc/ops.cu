@@ -247,7 +247,7 @@ int cleave_embedding(const cleave_embedding_t* d, void* stream) {
     if (!ids_ok(d->ids, d->id_type) || !float_type(d->table_type) || !float_type(d->out_type) || !matrix_ok(d->table, d->table_type, d->ldt, d->cols) ||
         !matrix_ok(d->out, d->out_type, d->ldo, d->cols)) return CLEAVE_E_INVAL;
     const int sms = need_device();
-    return sms < 0 ? sms : cuda_code(launch_embedding(*d, sms, static_cast<cudaStream_t>(stream)));
+    return sms < 0 ? sms : cuda_code(launch_embedding(*d, static_cast<cudaStream_t>(stream)));
 }
 
 uint64_t cleave_embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols) { return embedding_backward_workspace(n, vocab, cols); }

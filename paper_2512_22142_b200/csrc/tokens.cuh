@@ -13,7 +13,7 @@ __device__ __forceinline__ int32_t load_token(const void* ids, uint32_t type, ui
     return (uint64_t)t < vocab ? (int32_t)t : -1;
 }
 
-cudaError_t launch_embedding(const cleave_embedding_t& d, int sms, cudaStream_t st);
+cudaError_t launch_embedding(const cleave_embedding_t& d, cudaStream_t st);
 uint64_t embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols);
 cudaError_t launch_embedding_backward(const cleave_embedding_backward_t& d, void* ws, cudaStream_t st);
 
