@@ -8,10 +8,10 @@
 //   order    the tokens' places are sorted by (token, place): a counting sort without communication.  CTA c owns a
 //            range of the vocabulary and reads all tokens (n of them stand in L2): what is below its range is its offset,
 //            what is inside is counted per warp and value; a second reading puts each place where it belongs.  Its time does
-//            not depend on the tokens' distribution.
+//            not depend on the tokens' distribution.  Where the table is not added to, other CTAs of the launch fill it with
+//            zeros meanwhile (the rows of tokens that occur are written again: a twentieth of the bytes, for a launch's latency).
 //   sum      the sorted places are cut into chunks of the same length, whatever the tokens; a CTA adds the rows of a
 //            chunk run by run.  A run that lies inside one chunk is a finished row; the ends of longer runs go to the workspace.
-//            Other CTAs of the launch write zeros into the rows of tokens that do not occur.
 //   join     the pieces of each longer run are added in order.
 // Bound by the HBM where the whole table is written, by the three launches' latencies where few rows are.
 #include <algorithm>
@@ -76,14 +76,43 @@ cudaError_t launch_embedding(const cleave_embedding_t& d, cudaStream_t st) {
 }
 
 // ---- gradient: the tokens' order ------------------------------------------------------------------------
-constexpr uint32_t kOrderThreads = 512, kOrderWarps = kOrderThreads / 32, kOrderMost = 2 * kOrderThreads;     // values a CTA owns at most
-constexpr int kOrderAhead = 4;                   // loads of 32 tokens under way
+constexpr uint32_t kOrderThreads = 1024, kOrderWarps = kOrderThreads / 32, kOrderMost = kOrderThreads;        // values a CTA owns at most
+constexpr int kOrderAhead = 8;                   // loads of 32 tokens under way
 
 uint32_t order_values(uint32_t vocab) { return std::min(kOrderMost, std::max(32u, (vocab + kPartSms - 1) / kPartSms)); }
 
+struct Zeros {                      // rows to be filled with zeros, each cut into pieces of kZeroPiece bytes; a row after another is one row
+    uint8_t* p;
+    uint64_t pitch, row_bytes, pieces, tasks;
+    uint32_t element;
+};
+constexpr uint32_t kZeroPiece = 4096;
+// a warp fills [p, p + bytes): elements up to 16 bytes, 16 bytes, elements
+__device__ __forceinline__ void fill_zeros(uint8_t* p, uint32_t bytes, uint32_t element) {
+    const uint32_t lane = threadIdx.x & 31u, head = min(bytes, (0u - (uint32_t)(uintptr_t)p) % 16u), body = (bytes - head) / 16, tail = bytes - head - body * 16;
+    auto one = [&](uint8_t* q) {
+        if (element == 4) *reinterpret_cast<uint32_t*>(q) = 0;
+        else *reinterpret_cast<uint16_t*>(q) = 0;
+    };
+    if (lane * element < head) one(p + lane * element);
+    if (lane * element < tail) one(p + bytes - tail + lane * element);
+#pragma unroll 4
+    for (uint32_t i = lane; i < body; i += 32) reinterpret_cast<uint4*>(p + head)[i] = make_uint4(0u, 0u, 0u, 0u);
+}
+
 // offsets[v] = number of tokens below v, for v <= vocab; sorted[offsets[v] ...] = (place, v), places ascending
 template <typename ID>
-__global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* ids, uint32_t n, uint32_t vocab, uint32_t values, uint32_t* offsets, uint2* sorted) {
+__global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* ids, uint32_t n, uint32_t vocab, uint32_t values, uint32_t* offsets, uint2* sorted, uint32_t owners,
+                                                                    const __grid_constant__ Zeros z) {
+    if (blockIdx.x >= owners) {
+        begin_chained();
+        const uint64_t step = (uint64_t)(gridDim.x - owners) * kOrderWarps;
+        for (uint64_t t = (uint64_t)(blockIdx.x - owners) * kOrderWarps + (threadIdx.x >> 5); t < z.tasks; t += step) {
+            const uint64_t row = z.pieces == z.tasks ? 0 : t / z.pieces, at = (t - row * z.pieces) * kZeroPiece;
+            fill_zeros(z.p + row * z.pitch + at, (uint32_t)min((uint64_t)kZeroPiece, z.row_bytes - at), z.element);
+        }
+        return;
+    }
     extern __shared__ uint32_t counts[];                         // [warp][value]
     __shared__ uint32_t sums[32], below_all;
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, lo = blockIdx.x * values, hi = min(vocab, lo + values);
@@ -112,32 +141,23 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
     below = __reduce_add_sync(0xFFFFFFFFu, below);
     if (lane == 0 && below) atomicAdd(&below_all, below);        // (whole numbers: any order)
     __syncthreads();
-    // a thread owns the values 2 tid and 2 tid + 1: counts become offsets among the warps, then in the whole
-    uint32_t total[2] = {0, 0};
-#pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) {
-        const uint32_t v = 2 * threadIdx.x + k;
-        if (v < values)
+    // a thread owns a value: counts become offsets among the warps, then in the whole
+    const uint32_t own = threadIdx.x;
+    uint32_t total = 0;
+    if (own < values)
 #pragma unroll 8
-            for (uint32_t w = 0; w < kOrderWarps; ++w) total[k] += counts[w * values + v];
-    }
-    uint32_t sum = total[0] + total[1], up = sum;
+        for (uint32_t w = 0; w < kOrderWarps; ++w) total += counts[w * values + own];
+    uint32_t up = total;
+#pragma unroll
     for (uint32_t o = 1; o < 32; o <<= 1) { const uint32_t x = __shfl_up_sync(0xFFFFFFFFu, up, o); if (lane >= o) up += x; }
     if (lane == 31) sums[warp] = up;
     __syncthreads();
-    uint32_t before = below_all + up - sum;
-    for (uint32_t w = 0; w < warp; ++w) before += sums[w];
-#pragma unroll
-    for (uint32_t k = 0; k < 2; ++k) {
-        const uint32_t v = 2 * threadIdx.x + k;
-        if (v < values && lo + v < hi) {
-            offsets[lo + v] = before;
-            uint32_t at = before;
+    uint32_t before = below_all + up - total + __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sums[lane] : 0u);
+    if (own < values && lo + own < hi) {
+        offsets[lo + own] = before;
+        if (lo + own + 1 == vocab) offsets[vocab] = before + total;
 #pragma unroll 8
-            for (uint32_t w = 0; w < kOrderWarps; ++w) { const uint32_t c = counts[w * values + v]; counts[w * values + v] = at; at += c; }
-        }
-        before += total[k];
-        if (v < values && lo + v + 1 == vocab) offsets[vocab] = before;
+        for (uint32_t w = 0; w < kOrderWarps; ++w) { const uint32_t c = counts[w * values + own]; counts[w * values + own] = before; before += c; }
     }
     __syncthreads();
     for (uint64_t i = from; i < to; i += 32 * kOrderAhead) {
@@ -169,7 +189,6 @@ struct Ordered {                    // what the order kernel left
     float* parts;                   // [2 chunk + 0: the run that began before the chunk, 1: the run that begins in it and goes on][cols]
     uint32_t chunk, chunks;
 };
-constexpr uint32_t kZeroRows = 32;               // rows that a CTA looks through for absent tokens
 constexpr int kRowsAhead = 4;                    // rows of dy under way
 
 // what a thread holds of a row: 8 columns (wide) or one
@@ -217,18 +236,6 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
     constexpr uint32_t W = WIDE ? 8 : 1;
     begin_chained();
     const uint32_t lane = threadIdx.x & 31u, columns = gridDim.y * blockDim.x * W;
-    if (blockIdx.x >= o.chunks) {                                // rows of tokens that do not occur
-        const uint64_t v0 = (uint64_t)(blockIdx.x - o.chunks) * kZeroRows;
-        static_assert(kZeroRows == 32, "a lane looks at a row");
-        const bool absent = v0 + lane < d.vocab && o.offsets[v0 + lane] == o.offsets[v0 + lane + 1];
-        for (uint32_t rows = __ballot_sync(0xFFFFFFFFu, absent); rows; rows &= rows - 1) {
-            D* row = static_cast<D*>(d.dtable) + (v0 + (uint32_t)__ffs((int)rows) - 1) * d.lddt;
-            Acc<WIDE> zero;
-            zero.clear();
-            for (uint32_t j = (blockIdx.y * blockDim.x + threadIdx.x) * W; j < d.cols; j += columns) zero.store(row + j);
-        }
-        return;
-    }
     const uint32_t total = o.offsets[d.vocab], first = blockIdx.x * o.chunk, last = min(total, first + o.chunk);
     if (first >= last) return;
     for (uint32_t j = (blockIdx.y * blockDim.x + threadIdx.x) * W; j - lane * W < d.cols; j += columns) {       // (a warp stays together)
@@ -280,49 +287,61 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
     }
 }
 
-// A CTA looks at 8 chunks; for each whose last run begins in it and goes on, its warps add the pieces w, w + 8, ... of 32 lanes'
-// columns, and the warps' sums are added in order.
+// A CTA looks at 8 chunks for runs that begin in a chunk and go on.  A warp adds the pieces of its chunk's run in order; a run of
+// more than kLongRun pieces is left to all warps (each adds every eighth piece, and the warps' sums are added in order).
+constexpr uint32_t kLongRun = 16;
 template <typename D, bool WIDE>
 __global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
     constexpr uint32_t W = WIDE ? 8 : 1;
     __shared__ __align__(16) float s[8][32 * W];
     begin_chained();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, total = o.offsets[d.vocab];
-    uint32_t v = 0;
-    bool starts = false;
+    uint32_t v = 0, pieces = 0;                                  // of lane k < 8: the run that begins in chunk k
     if (lane < 8) {
-        const uint32_t c = blockIdx.x * 8 + lane;
-        const uint64_t first = (uint64_t)c * o.chunk, after = first + o.chunk;
+        const uint64_t first = (uint64_t)(blockIdx.x * 8 + lane) * o.chunk, after = first + o.chunk;
         if (after < total) {
             v = o.sorted[after - 1].y;
-            starts = o.sorted[after].y == v && (o.sorted[first].y != v || first == 0 || o.sorted[first - 1].y != v);
+            if (o.sorted[after].y == v && (o.sorted[first].y != v || first == 0 || o.sorted[first - 1].y != v))
+                pieces = (o.offsets[v + 1] - 1) / o.chunk - (blockIdx.x * 8 + lane) + 1;
         }
     }
-    for (uint32_t some = __ballot_sync(0xFFFFFFFFu, starts); some; some &= some - 1) {
-        const uint32_t k = (uint32_t)__ffs((int)some) - 1, c0 = blockIdx.x * 8 + k, token = __shfl_sync(0xFFFFFFFFu, v, k);
-        const uint32_t pieces = (o.offsets[token + 1] - 1) / o.chunk - c0 + 1;
+    auto add = [&](Acc<WIDE>& acc, uint32_t k, uint32_t begin, uint32_t step, uint32_t end, uint32_t j) {      // pieces of the run of chunk k
+        const float* from = o.parts + (uint64_t)(blockIdx.x * 8 + k) * 2 * d.cols + j;
+#pragma unroll 4
+        for (uint32_t c = begin; c < end; c += step) {
+            Cols<float, WIDE> x;
+            x.load(from + ((uint64_t)c * 2 + (c == 0 ? 1 : 0)) * d.cols);
+            acc.add(x);
+        }
+    };
+    auto finish = [&](Acc<WIDE>& acc, uint32_t token, uint32_t j) {
+        D* dt = static_cast<D*>(d.dtable) + (uint64_t)token * d.lddt + j;
+        acc.scale(d.scale);
+        if (d.accumulate) { Cols<D, WIDE> old; old.load(dt); acc.add(old); }
+        acc.store(dt);
+    };
+    const uint32_t mine = __shfl_sync(0xFFFFFFFFu, pieces, warp), token = __shfl_sync(0xFFFFFFFFu, v, warp);
+    if (mine && mine <= kLongRun)
+        for (uint32_t j = (blockIdx.y * 32 + lane) * W; j < d.cols; j += gridDim.y * 32 * W) {
+            Acc<WIDE> acc;
+            acc.clear();
+            add(acc, warp, 0, 1, mine, j);
+            finish(acc, token, j);
+        }
+    for (uint32_t some = __ballot_sync(0xFFFFFFFFu, pieces > kLongRun); some; some &= some - 1) {
+        const uint32_t k = (uint32_t)__ffs((int)some) - 1, many = __shfl_sync(0xFFFFFFFFu, pieces, k), token = __shfl_sync(0xFFFFFFFFu, v, k);
         for (uint32_t j0 = blockIdx.y * 32 * W; j0 < d.cols; j0 += gridDim.y * 32 * W) {
             const uint32_t j = j0 + lane * W;
             Acc<WIDE> acc;
             acc.clear();
-            if (j < d.cols) {
-#pragma unroll 4
-                for (uint32_t c = warp; c < pieces; c += 8) {
-                    Cols<float, WIDE> x;
-                    x.load(o.parts + ((uint64_t)(c0 + c) * 2 + (c == 0 ? 1 : 0)) * d.cols + j);
-                    acc.add(x);
-                }
-            }
+            if (j < d.cols) add(acc, k, warp, 8, many, j);
             acc.store(&s[warp][lane * W]);
             __syncthreads();
             if (warp == 0 && j < d.cols) {
                 acc.clear();
 #pragma unroll
                 for (uint32_t w = 0; w < 8; ++w) { Cols<float, WIDE> x; x.load(&s[w][lane * W]); acc.add(x); }
-                D* dt = static_cast<D*>(d.dtable) + (uint64_t)token * d.lddt + j;
-                acc.scale(d.scale);
-                if (d.accumulate) { Cols<D, WIDE> old; old.load(dt); acc.add(old); }
-                acc.store(dt);
+                finish(acc, token, j);
             }
             __syncthreads();
         }
@@ -337,19 +356,26 @@ uint64_t embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols)
 }
 template <typename ID>
 cudaError_t launch_order(const cleave_embedding_backward_t& d, uint32_t* offsets, uint2* sorted, cudaStream_t st) {
-    const uint32_t values = order_values(d.vocab);
+    const uint32_t values = order_values(d.vocab), owners = (d.vocab + values - 1) / values;
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(token_order_kernel<ID>), kOrderWarps * kOrderMost * 4);
     if (e != cudaSuccess) return e;
-    return launch_chained(token_order_kernel<ID>, (d.vocab + values - 1) / values, kOrderThreads, kOrderWarps * values * 4, st, static_cast<const ID*>(d.ids), (uint32_t)d.n, d.vocab, values,
-                          offsets, sorted);
+    Zeros z = {};
+    if (!d.accumulate) {
+        const uint64_t b = type_bytes(d.dtable_type), rows = d.lddt == d.cols ? 1 : d.vocab;
+        z = {static_cast<uint8_t*>(d.dtable), d.lddt * b, rows == 1 ? (uint64_t)d.vocab * d.cols * b : d.cols * b, 0, 0, (uint32_t)b};
+        z.pieces = (z.row_bytes + kZeroPiece - 1) / kZeroPiece;
+        z.tasks = z.pieces * rows;
+    }
+    const uint32_t zeros = (uint32_t)std::min<uint64_t>(2 * kPartSms, (z.tasks + kOrderWarps - 1) / kOrderWarps);
+    return launch_chained(token_order_kernel<ID>, owners + zeros, kOrderThreads, kOrderWarps * values * 4, st, static_cast<const ID*>(d.ids), (uint32_t)d.n, d.vocab, values, offsets,
+                          sorted, owners, z);
 }
 template <typename X, typename D, bool WIDE>
 cudaError_t launch_sums(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
+    if (!o.chunks) return cudaSuccess;
     const uint32_t units = WIDE ? d.cols / 8 : d.cols, tiles = std::min(65535u, (units + 255) / 256), threads = std::min(256u, ((units + tiles - 1) / tiles + 31) / 32 * 32);
-    const unsigned zeros = d.accumulate ? 0 : (d.vocab + kZeroRows - 1) / kZeroRows;
-    cudaError_t e = cudaSuccess;
-    if (o.chunks + zeros) e = launch_chained(embedding_sum_kernel<X, D, WIDE>, dim3(o.chunks + zeros, tiles), threads, 0, st, d, o);
+    const cudaError_t e = launch_chained(embedding_sum_kernel<X, D, WIDE>, dim3(o.chunks, tiles), threads, 0, st, d, o);
     if (e != cudaSuccess || o.chunks < 2) return e;
     return launch_chained(embedding_join_kernel<D, WIDE>, dim3((o.chunks + 7) / 8, std::min(65535u, (units + 31) / 32)), 256, 0, st, d, o);
 }
