@@ -5,10 +5,10 @@
 //
 // Gradient.  The rows of dy have to be added by token, in an order that does not change from run to run, and a vocabulary's
 // tokens are far from evenly spread (a few make up half of a batch).  So:
-//   order    the tokens' places are sorted by (token, place): a counting sort without communication.  CTA c owns a
-//            range of the vocabulary and reads all tokens (n of them stand in L2): what is below its range is its offset,
-//            what is inside is counted per warp and value; a second reading puts each place where it belongs.  Its time does
-//            not depend on the tokens' distribution.  Where the table is not added to, other CTAs of the launch fill it with
+//   order    the tokens' places are sorted by (token modulo a power of two, token, place): a counting sort without communication.
+//            CTA c owns the tokens v with v mod CTAs = c (neighbours, which are alike in frequency, go to different ones) and reads
+//            all tokens (n of them stand in L2): those of lower remainder are its offset, its own are counted per warp and
+//            token; a second reading puts each place where it belongs.  Where the table is not added to, other CTAs of the launch fill it with
 //            zeros meanwhile (the rows of tokens that occur are written again: a twentieth of the bytes, for a launch's latency).
 //   sum      the sorted places are cut into chunks of the same length, whatever the tokens; a CTA adds the rows of a
 //            chunk run by run.  A run that lies inside one chunk is a finished row; the ends of longer runs go to the workspace.
@@ -76,10 +76,15 @@ cudaError_t launch_embedding(const cleave_embedding_t& d, cudaStream_t st) {
 }
 
 // ---- gradient: the tokens' order ------------------------------------------------------------------------
-constexpr uint32_t kOrderThreads = 1024, kOrderWarps = kOrderThreads / 32, kOrderMost = kOrderThreads;        // values a CTA owns at most
+constexpr uint32_t kOrderThreads = 1024, kOrderWarps = kOrderThreads / 32, kOrderMost = kOrderThreads;        // tokens of the vocabulary a CTA owns at most
 constexpr int kOrderAhead = 8;                   // loads of 32 tokens under way
 
-uint32_t order_values(uint32_t vocab) { return std::min(kOrderMost, std::max(32u, (vocab + kPartSms - 1) / kPartSms)); }
+// log2 of the number of owners: a power of two near the number of SMs, more for a vocabulary beyond 131072
+uint32_t order_owners(uint32_t vocab) {
+    uint32_t bits = 7;
+    while ((uint64_t)kOrderMost << bits < vocab) ++bits;
+    return bits;
+}
 
 struct Zeros {                      // rows to be filled with zeros, each cut into pieces of kZeroPiece bytes; a row after another is one row
     uint8_t* p;
@@ -100,10 +105,11 @@ __device__ __forceinline__ void fill_zeros(uint8_t* p, uint32_t bytes, uint32_t 
     for (uint32_t i = lane; i < body; i += 32) reinterpret_cast<uint4*>(p + head)[i] = make_uint4(0u, 0u, 0u, 0u);
 }
 
-// offsets[v] = number of tokens below v, for v <= vocab; sorted[offsets[v] ...] = (place, v), places ascending
+// sorted = (place, v) by v mod owners, v, place; ends[v] = where the places of token v end in it; *count = how many there are
 template <typename ID>
-__global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* ids, uint32_t n, uint32_t vocab, uint32_t values, uint32_t* offsets, uint2* sorted, uint32_t owners,
+__global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* ids, uint32_t n, uint32_t vocab, uint32_t bits, uint32_t values, uint32_t* ends, uint32_t* count, uint2* sorted,
                                                                     const __grid_constant__ Zeros z) {
+    const uint32_t owners = 1u << bits, low = owners - 1;
     if (blockIdx.x >= owners) {
         begin_chained();
         const uint64_t step = (uint64_t)(gridDim.x - owners) * kOrderWarps;
@@ -115,7 +121,7 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
     }
     extern __shared__ uint32_t counts[];                         // [warp][value]
     __shared__ uint32_t sums[32], below_all;
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, lo = blockIdx.x * values, hi = min(vocab, lo + values);
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     uint32_t* mine = counts + warp * values;
     for (uint32_t i = threadIdx.x; i < kOrderWarps * values; i += kOrderThreads) counts[i] = 0;
     if (threadIdx.x == 0) below_all = 0;
@@ -133,9 +139,10 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
         load(i, t);
 #pragma unroll
         for (int k = 0; k < kOrderAhead; ++k) {
-            if (t[k] < 0) continue;
-            if ((uint64_t)t[k] < lo) ++below;
-            else if ((uint64_t)t[k] < hi) atomicAdd(mine + (uint32_t)(t[k] - lo), 1u);
+            const uint32_t v = (uint32_t)t[k], owner = v & low;
+            if (t[k] < 0 || t[k] >= (ID)vocab) continue;
+            if (owner < blockIdx.x) ++below;
+            else if (owner == blockIdx.x) atomicAdd(mine + (v >> bits), 1u);
         }
     }
     below = __reduce_add_sync(0xFFFFFFFFu, below);
@@ -153,11 +160,12 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
     if (lane == 31) sums[warp] = up;
     __syncthreads();
     uint32_t before = below_all + up - total + __reduce_add_sync(0xFFFFFFFFu, lane < warp ? sums[lane] : 0u);
-    if (own < values && lo + own < hi) {
-        offsets[lo + own] = before;
-        if (lo + own + 1 == vocab) offsets[vocab] = before + total;
+    if (own < values) {
 #pragma unroll 8
         for (uint32_t w = 0; w < kOrderWarps; ++w) { const uint32_t c = counts[w * values + own]; counts[w * values + own] = before; before += c; }
+        const uint64_t v = ((uint64_t)own << bits) + blockIdx.x;
+        if (v < vocab) ends[v] = before;
+        if (own == values - 1 && blockIdx.x == low) *count = before;
     }
     __syncthreads();
     for (uint64_t i = from; i < to; i += 32 * kOrderAhead) {
@@ -165,12 +173,12 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
         load(i, t);
 #pragma unroll
         for (int k = 0; k < kOrderAhead; ++k) {
-            const bool in = t[k] >= 0 && (uint64_t)t[k] >= lo && (uint64_t)t[k] < hi;
+            const bool in = t[k] >= 0 && t[k] < (ID)vocab && ((uint32_t)t[k] & low) == blockIdx.x;
             const uint32_t some = __ballot_sync(0xFFFFFFFFu, in);
             if (!some) continue;
             if (in) {
-                const uint32_t v = (uint32_t)(t[k] - lo), same = __match_any_sync(some, v), rank = __popc(same & ((1u << lane) - 1u)), base = mine[v];
-                sorted[base + rank] = make_uint2((uint32_t)(i + 32 * k + lane), lo + v);
+                const uint32_t v = (uint32_t)t[k] >> bits, same = __match_any_sync(some, v), rank = __popc(same & ((1u << lane) - 1u)), base = mine[v];
+                sorted[base + rank] = make_uint2((uint32_t)(i + 32 * k + lane), (uint32_t)t[k]);
                 __syncwarp(some);
                 if (rank == 0) mine[v] = base + __popc(same);
             }
@@ -180,16 +188,24 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
 }
 
 // ---- gradient: sums --------------------------------------------------------------------------------------
-constexpr uint32_t kChunkLeast = 16, kChunksMost = 16 * kPartSms;
-uint32_t sum_chunk(uint64_t n) { return (uint32_t)std::max<uint64_t>(kChunkLeast, (n + kChunksMost - 1) / kChunksMost); }      // places a chunk
+// Places a chunk: 16; 8 where those would make too few CTAs (8192 places of 768 columns 42.6 us against 46, 16384 of 4096 columns 84
+// against 77); more where there would be more than kChunksMost, which bounds the workspace.
+constexpr uint32_t kChunksMost = 16 * kPartSms;
+uint32_t sum_chunk(uint64_t n, uint32_t cols) {
+    const uint64_t least = n / 16 * ((cols + 2047u) / 2048u) < 8 * kPartSms ? 8 : 16;
+    return (uint32_t)std::max<uint64_t>(least, (n + kChunksMost - 1) / kChunksMost);
+}
 
 struct Ordered {                    // what the order kernel left
-    const uint32_t* offsets;
+    const uint32_t* ends;           // [token]
+    const uint32_t* count;
     const uint2* sorted;
+    uint2* runs;                    // [chunk]: token and number of pieces of the run that begins in the chunk and goes on (0 pieces: none)
     float* parts;                   // [2 chunk + 0: the run that began before the chunk, 1: the run that begins in it and goes on][cols]
     uint32_t chunk, chunks;
 };
-constexpr int kRowsAhead = 4;                    // rows of dy under way
+// rows of dy under way: 128 bytes a thread, and as much of the table's rows where they are added to
+template <typename X, bool ADD> constexpr int kRowsAhead = sizeof(X) == 2 && !ADD ? 8 : 4;
 
 // what a thread holds of a row: 8 columns (wide) or one
 template <typename T, bool WIDE> struct Cols;
@@ -231,41 +247,52 @@ template <> struct Acc<false> {
     template <typename T> __device__ __forceinline__ void store(T* p) const { *p = from_f32<T>(v); }
 };
 
-template <typename X, typename D, bool WIDE>
+template <typename X, typename D, bool WIDE, bool ADD>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
     constexpr uint32_t W = WIDE ? 8 : 1;
+    constexpr int N = kRowsAhead<X, ADD>;
     begin_chained();
-    const uint32_t lane = threadIdx.x & 31u, columns = gridDim.y * blockDim.x * W;
-    const uint32_t total = o.offsets[d.vocab], first = blockIdx.x * o.chunk, last = min(total, first + o.chunk);
-    if (first >= last) return;
+    const uint32_t lane = threadIdx.x & 31u, columns = gridDim.y * blockDim.x * W, n = (uint32_t)d.n, first = blockIdx.x * o.chunk, most = min(n, first + o.chunk);
+    // a lane looks at a place: its row, its token, the next place's token (behind the last token's place stands nothing in particular)
+    auto look = [&](uint32_t p, uint2& here, uint32_t& next) {
+        here = p < most ? o.sorted[p] : make_uint2(0u, 0u);
+        next = p + 1 < n ? o.sorted[p + 1].y : 0u;
+    };
+    uint2 here;
+    uint32_t next;
+    look(first + lane, here, next);
+    const uint32_t ahead = first ? o.sorted[first - 1].y : 0u, total = *o.count, last = min(total, most);
+    if (first >= last) {
+        if (blockIdx.y == 0 && threadIdx.x == 0) o.runs[blockIdx.x] = make_uint2(0u, 0u);
+        return;
+    }
+    const bool began = first > 0 && ahead == __shfl_sync(0xFFFFFFFFu, here.y, 0);            // the first run began before the chunk
     for (uint32_t j = (blockIdx.y * blockDim.x + threadIdx.x) * W; j - lane * W < d.cols; j += columns) {       // (a warp stays together)
         const bool live = j < d.cols;
         const X* dy = static_cast<const X*>(d.dy) + j;
         D* dt = static_cast<D*>(d.dtable) + j;
         Acc<WIDE> acc;
         acc.clear();
-        bool before = false, open = false;                       // the run began before the chunk; it goes on at the end of it
+        bool before = began, open = false;                       // open: the run goes on at the end of the chunk
+        uint32_t token = 0;
         for (uint32_t base = first; base < last; base += 32) {
-            // a lane looks at a place: its row, its token, whether its run ends there
-            const uint32_t p = base + lane;
-            const uint2 here = p < last ? o.sorted[p] : make_uint2(0u, 0u);
-            const bool ends = p < last && (p + 1 >= total || o.sorted[p + 1].y != here.y);
-            if (base == first) before = first > 0 && o.sorted[first - 1].y == __shfl_sync(0xFFFFFFFFu, here.y, 0);
-            const uint32_t stops = __ballot_sync(0xFFFFFFFFu, ends), count = min(32u, last - base);
-            for (uint32_t i = 0; i < count; i += kRowsAhead) {
-                Cols<X, WIDE> x[kRowsAhead];
-                Cols<D, WIDE> old[kRowsAhead];
+            if (o.chunk > 32) look(base + lane, here, next);
+            const uint32_t p = base + lane, count = min(32u, last - base), stops = __ballot_sync(0xFFFFFFFFu, p < last && (p + 1 >= total || next != here.y));
+            for (uint32_t i = 0; i < count; i += N) {
+                Cols<X, WIDE> x[N];
+                Cols<D, WIDE> old[ADD ? N : 1];
 #pragma unroll
-                for (int k = 0; k < kRowsAhead; ++k) {
+                for (int k = 0; k < N; ++k) {
                     const uint32_t row = __shfl_sync(0xFFFFFFFFu, here.x, (i + k) & 31u), v = __shfl_sync(0xFFFFFFFFu, here.y, (i + k) & 31u);
                     if (!live || i + k >= count) continue;
                     x[k].load(dy + (uint64_t)row * d.lddy);
-                    if (d.accumulate && (stops >> (i + k) & 1u)) old[k].load(dt + (uint64_t)v * d.lddt);       // (not used where the run's other piece is missing)
+                    if (ADD && (stops >> (i + k) & 1u)) old[ADD ? k : 0].load(dt + (uint64_t)v * d.lddt);      // (not used where the run's other piece is missing)
                 }
 #pragma unroll
-                for (int k = 0; k < kRowsAhead; ++k) {
+                for (int k = 0; k < N; ++k) {
                     const uint32_t v = __shfl_sync(0xFFFFFFFFu, here.y, (i + k) & 31u);
                     if (i + k >= count) continue;
+                    token = v;
                     open = !(stops >> (i + k) & 1u);
                     if (live) {
                         acc.add(x[k]);
@@ -273,7 +300,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
                             if (before) acc.store(o.parts + (uint64_t)blockIdx.x * 2 * d.cols + j);
                             else {
                                 acc.scale(d.scale);
-                                if (d.accumulate) acc.add(old[k]);
+                                if (ADD) acc.add(old[ADD ? k : 0]);
                                 acc.store(dt + (uint64_t)v * d.lddt);
                             }
                             acc.clear();
@@ -284,6 +311,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
             }
         }
         if (open && live) acc.store(o.parts + ((uint64_t)blockIdx.x * 2 + (before ? 0 : 1)) * d.cols + j);
+        if (j == 0) o.runs[blockIdx.x] = make_uint2(token, open && !before ? (o.ends[token] - 1) / o.chunk - blockIdx.x + 1 : 0u);
     }
 }
 
@@ -295,45 +323,46 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_consta
     constexpr uint32_t W = WIDE ? 8 : 1;
     __shared__ __align__(16) float s[8][32 * W];
     begin_chained();
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, total = o.offsets[d.vocab];
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     uint32_t v = 0, pieces = 0;                                  // of lane k < 8: the run that begins in chunk k
-    if (lane < 8) {
-        const uint64_t first = (uint64_t)(blockIdx.x * 8 + lane) * o.chunk, after = first + o.chunk;
-        if (after < total) {
-            v = o.sorted[after - 1].y;
-            if (o.sorted[after].y == v && (o.sorted[first].y != v || first == 0 || o.sorted[first - 1].y != v))
-                pieces = (o.offsets[v + 1] - 1) / o.chunk - (blockIdx.x * 8 + lane) + 1;
-        }
+    if (lane < 8 && blockIdx.x * 8 + lane < o.chunks) {
+        const uint2 run = o.runs[blockIdx.x * 8 + lane];
+        v = run.x;
+        pieces = run.y;
     }
     auto add = [&](Acc<WIDE>& acc, uint32_t k, uint32_t begin, uint32_t step, uint32_t end, uint32_t j) {      // pieces of the run of chunk k
         const float* from = o.parts + (uint64_t)(blockIdx.x * 8 + k) * 2 * d.cols + j;
-#pragma unroll 4
+#pragma unroll 8
         for (uint32_t c = begin; c < end; c += step) {
             Cols<float, WIDE> x;
             x.load(from + ((uint64_t)c * 2 + (c == 0 ? 1 : 0)) * d.cols);
             acc.add(x);
         }
     };
-    auto finish = [&](Acc<WIDE>& acc, uint32_t token, uint32_t j) {
-        D* dt = static_cast<D*>(d.dtable) + (uint64_t)token * d.lddt + j;
+    auto at = [&](uint32_t token, uint32_t j) { return static_cast<D*>(d.dtable) + (uint64_t)token * d.lddt + j; };
+    auto finish = [&](Acc<WIDE>& acc, const Cols<D, WIDE>& old, D* dt) {
         acc.scale(d.scale);
-        if (d.accumulate) { Cols<D, WIDE> old; old.load(dt); acc.add(old); }
+        if (d.accumulate) acc.add(old);
         acc.store(dt);
     };
     const uint32_t mine = __shfl_sync(0xFFFFFFFFu, pieces, warp), token = __shfl_sync(0xFFFFFFFFu, v, warp);
     if (mine && mine <= kLongRun)
         for (uint32_t j = (blockIdx.y * 32 + lane) * W; j < d.cols; j += gridDim.y * 32 * W) {
             Acc<WIDE> acc;
+            Cols<D, WIDE> old;
             acc.clear();
+            if (d.accumulate) old.load(at(token, j));
             add(acc, warp, 0, 1, mine, j);
-            finish(acc, token, j);
+            finish(acc, old, at(token, j));
         }
     for (uint32_t some = __ballot_sync(0xFFFFFFFFu, pieces > kLongRun); some; some &= some - 1) {
         const uint32_t k = (uint32_t)__ffs((int)some) - 1, many = __shfl_sync(0xFFFFFFFFu, pieces, k), token = __shfl_sync(0xFFFFFFFFu, v, k);
         for (uint32_t j0 = blockIdx.y * 32 * W; j0 < d.cols; j0 += gridDim.y * 32 * W) {
             const uint32_t j = j0 + lane * W;
             Acc<WIDE> acc;
+            Cols<D, WIDE> old;
             acc.clear();
+            if (d.accumulate && warp == 0 && j < d.cols) old.load(at(token, j));
             if (j < d.cols) add(acc, k, warp, 8, many, j);
             acc.store(&s[warp][lane * W]);
             __syncthreads();
@@ -341,22 +370,28 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_consta
                 acc.clear();
 #pragma unroll
                 for (uint32_t w = 0; w < 8; ++w) { Cols<float, WIDE> x; x.load(&s[w][lane * W]); acc.add(x); }
-                finish(acc, token, j);
+                finish(acc, old, at(token, j));
             }
             __syncthreads();
         }
     }
 }
 
-static uint64_t offsets_bytes(uint32_t vocab) { return ((uint64_t)vocab + 1 + 3) / 4 * 16; }
-static uint64_t order_bytes(uint64_t n, uint32_t vocab) { return offsets_bytes(vocab) + (n + 1) / 2 * 16; }
-uint64_t embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols) {
-    const uint64_t chunks = n ? (n + sum_chunk(n) - 1) / sum_chunk(n) : 0;
-    return order_bytes(n, vocab) + chunks * 2 * cols * sizeof(float);
+// the workspace: the count and the ends, sorted places, runs, pieces; each begins on 16 bytes
+struct Space { uint64_t sorted, runs, parts, bytes; };
+static Space space_of(uint64_t n, uint32_t vocab, uint32_t cols) {
+    const uint64_t chunk = sum_chunk(n, cols), chunks = (n + chunk - 1) / chunk;
+    Space s;
+    s.sorted = ((uint64_t)vocab + 1 + 3) / 4 * 16;
+    s.runs = s.sorted + (n + 1) / 2 * 16;
+    s.parts = s.runs + (chunks + 1) / 2 * 16;
+    s.bytes = s.parts + chunks * 2 * cols * sizeof(float);
+    return s;
 }
+uint64_t embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols) { return space_of(n, vocab, cols).bytes; }
 template <typename ID>
-cudaError_t launch_order(const cleave_embedding_backward_t& d, uint32_t* offsets, uint2* sorted, cudaStream_t st) {
-    const uint32_t values = order_values(d.vocab), owners = (d.vocab + values - 1) / values;
+cudaError_t launch_order(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
+    const uint32_t bits = order_owners(d.vocab), owners = 1u << bits, values = (uint32_t)(((uint64_t)d.vocab + owners - 1) >> bits);
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(token_order_kernel<ID>), kOrderWarps * kOrderMost * 4);
     if (e != cudaSuccess) return e;
@@ -368,14 +403,14 @@ cudaError_t launch_order(const cleave_embedding_backward_t& d, uint32_t* offsets
         z.tasks = z.pieces * rows;
     }
     const uint32_t zeros = (uint32_t)std::min<uint64_t>(2 * kPartSms, (z.tasks + kOrderWarps - 1) / kOrderWarps);
-    return launch_chained(token_order_kernel<ID>, owners + zeros, kOrderThreads, kOrderWarps * values * 4, st, static_cast<const ID*>(d.ids), (uint32_t)d.n, d.vocab, values, offsets,
-                          sorted, owners, z);
+    return launch_chained(token_order_kernel<ID>, owners + zeros, kOrderThreads, kOrderWarps * values * 4, st, static_cast<const ID*>(d.ids), (uint32_t)d.n, d.vocab, bits, values,
+                          const_cast<uint32_t*>(o.ends), const_cast<uint32_t*>(o.count), const_cast<uint2*>(o.sorted), z);
 }
 template <typename X, typename D, bool WIDE>
 cudaError_t launch_sums(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
     if (!o.chunks) return cudaSuccess;
     const uint32_t units = WIDE ? d.cols / 8 : d.cols, tiles = std::min(65535u, (units + 255) / 256), threads = std::min(256u, ((units + tiles - 1) / tiles + 31) / 32 * 32);
-    const cudaError_t e = launch_chained(embedding_sum_kernel<X, D, WIDE>, dim3(o.chunks, tiles), threads, 0, st, d, o);
+    const cudaError_t e = launch_chained(d.accumulate ? embedding_sum_kernel<X, D, WIDE, true> : embedding_sum_kernel<X, D, WIDE, false>, dim3(o.chunks, tiles), threads, 0, st, d, o);
     if (e != cudaSuccess || o.chunks < 2) return e;
     return launch_chained(embedding_join_kernel<D, WIDE>, dim3((o.chunks + 7) / 8, std::min(65535u, (units + 31) / 32)), 256, 0, st, d, o);
 }
@@ -386,12 +421,12 @@ cudaError_t launch_sums_types(const cleave_embedding_backward_t& d, const Ordere
     return wide ? launch_sums<X, D, true>(d, o, st) : launch_sums<X, D, false>(d, o, st);
 }
 cudaError_t launch_embedding_backward(const cleave_embedding_backward_t& d, void* ws, cudaStream_t st) {
+    const Space sp = space_of(d.n, d.vocab, d.cols);
     uint8_t* w = static_cast<uint8_t*>(ws);
-    uint32_t* offsets = reinterpret_cast<uint32_t*>(w);
-    uint2* sorted = reinterpret_cast<uint2*>(w + offsets_bytes(d.vocab));
-    Ordered o = {offsets, sorted, reinterpret_cast<float*>(w + order_bytes(d.n, d.vocab)), sum_chunk(d.n), 0};
+    uint32_t* head = reinterpret_cast<uint32_t*>(w);
+    Ordered o = {head + 1, head, reinterpret_cast<const uint2*>(w + sp.sorted), reinterpret_cast<uint2*>(w + sp.runs), reinterpret_cast<float*>(w + sp.parts), sum_chunk(d.n, d.cols), 0};
     o.chunks = (uint32_t)((d.n + o.chunk - 1) / o.chunk);
-    const cudaError_t e = d.id_type == CLEAVE_T_I64 ? launch_order<int64_t>(d, offsets, sorted, st) : launch_order<int32_t>(d, offsets, sorted, st);
+    const cudaError_t e = d.id_type == CLEAVE_T_I64 ? launch_order<int64_t>(d, o, st) : launch_order<int32_t>(d, o, st);
     if (e != cudaSuccess) return e;
     if (d.dy_type == CLEAVE_T_F32) return d.dtable_type == CLEAVE_T_F32 ? launch_sums_types<float, float>(d, o, st) : launch_sums_types<float, __nv_bfloat16>(d, o, st);
     return d.dtable_type == CLEAVE_T_F32 ? launch_sums_types<__nv_bfloat16, float>(d, o, st) : launch_sums_types<__nv_bfloat16, __nv_bfloat16>(d, o, st);

@@ -149,7 +149,7 @@ def test_workspaces(ops):
     fn = ops.embedding_backward_workspace
     assert fn(0, 1000, 64) >= 4 * 1001 and fn(100, 1000, 64) >= 4 * 1101
     for n in (1, 100, 10 ** 5, (1 << 31) - 1):
-        assert fn(n, 1000, 64) % 4 == 0 and fn(n, 1000, 64) <= 4 * (n + 1001) + 64 + 2 * 4 * 64 * min(n, 4096)
+        assert fn(n, 1000, 64) % 4 == 0 and fn(n, 1000, 64) <= 8 * n + 4 * 1001 + 64 + (8 + 2 * 4 * 64) * min(n, 4096)      # places with their tokens, offsets, pieces
 
 
 def test_binding_refuses_what_the_library_cannot_see(ops):
