@@ -1,10 +1,36 @@
 // Layer norm with the residual's addition, and its backward pass (see cleave.h).
+//
+// Bound by the HBM's bandwidth: each row is read once, kept in registers while its mean and then its variance (the sum of the
+// squared differences to that mean) are formed, and written once.  Forms as in the root-mean-square norm:
+//   wide   rows of whole 16-byte groups: a thread owns groups of 8 columns.  Up to 1024 columns a warp takes a row; above, a CTA
+//          takes a row, and the next rows come by cp.async into a ring in shared memory that needs no barrier of its own.
+//   own    any alignment, up to 8192 columns: neighbouring threads own neighbouring columns, held in registers.
+//   any    what is left: the row is taken again in each pass (it stays in L1 / L2).
 #include <algorithm>
+#include <type_traits>
 
 #include "rows.cuh"
 #include "tokens.cuh"
 
 namespace cleave {
+
+// 8 of a vector of weights or biases of columns, or `fill` where there is none
+__device__ __forceinline__ void load_vector8(const void* p, uint32_t type, uint32_t col, float fill, F2 (&v)[4]) {
+    if (type == CLEAVE_T_F32) {
+        Raw8<float> r;
+        const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + col);
+        r.w[0] = q[0]; r.w[1] = q[1];
+        unpack8(r, v);
+    } else if (type == CLEAVE_T_BF16) {
+        Raw8<__nv_bfloat16> r;
+        r.w[0] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + col);
+        unpack8(r, v);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = f2(fill, fill);
+    }
+}
+__device__ __forceinline__ float sum_of(F2 a) { const float2 h = halves(a); return h.x + h.y; }
 
 // ---- forward, any shape ------------------------------------------------------------------------------
 __global__ void __launch_bounds__(kRowThreads) layernorm_any_kernel(const __grid_constant__ cleave_layernorm_t d) {
@@ -40,14 +66,268 @@ __global__ void __launch_bounds__(kRowThreads) layernorm_any_kernel(const __grid
         else store_as(d.y, d.y_type, oy + j, y);
     }
 }
-cudaError_t launch_layernorm(const cleave_layernorm_t& d, int, cudaStream_t st) {
+
+// ---- forward, a row held by its CTA -------------------------------------------------------------------------
+template <int T>
+__global__ void __launch_bounds__(T) layernorm_own_kernel(const __grid_constant__ cleave_layernorm_t d) {
+    __shared__ float2 parts[3][32];
+    begin_chained();
+    float w[kOwn], b[kOwn];
+    uint32_t x[kOwn], r[kOwn];
+#pragma unroll
+    for (uint32_t k = 0; k < kOwn; ++k) { w[k] = 1.f; b[k] = 0.f; r[k] = 0u; }
+    if (d.w) { load_own(d.w, d.w_type, 0, d.cols, x); own_values(x, d.w_type, d.cols, w); }
+    if (d.b) { load_own(d.b, d.b_type, 0, d.cols, x); own_values(x, d.b_type, d.cols, b); }
+    const float inv_cols = 1.f / (float)d.cols;
+    uint64_t row = blockIdx.x;
+    load_own(d.x, d.x_type, row * d.ldx, d.cols, x);
+    if (d.r) load_own(d.r, d.r_type, row * d.ldr, d.cols, r);
+    for (; row < d.rows; row += gridDim.x) {
+        float h[kOwn], s = 0.f, ss = 0.f, top = 0.f;
+        own_values(x, d.x_type, d.cols, h);
+        if (d.r) {
+            float t[kOwn];
+            own_values(r, d.r_type, d.cols, t);
+#pragma unroll
+            for (uint32_t k = 0; k < kOwn; ++k) h[k] += t[k];
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) s += h[k];
+        const uint64_t next = row + gridDim.x;
+        if (next < d.rows) {
+            load_own(d.x, d.x_type, next * d.ldx, d.cols, x);
+            if (d.r) load_own(d.r, d.r_type, next * d.ldr, d.cols, r);
+        }
+        if (d.h) store_own(d.h, d.r_type, row * d.ldh, d.cols, h);
+        const float mean = cta_join(s, 0.f, parts[0]).x * inv_cols;
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) {
+            h[k] = threadIdx.x + k * blockDim.x < d.cols ? h[k] - mean : 0.f;
+            ss = fmaf(h[k], h[k], ss);
+        }
+        const float rstd = rsqrtf(fmaf(cta_join(ss, 0.f, parts[1]).x, inv_cols, d.eps));
+        if (threadIdx.x == 0) {
+            if (d.mean) d.mean[row] = mean;
+            if (d.rstd) d.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) { h[k] = fmaf(h[k] * rstd, w[k], b[k]); top = max_nan(top, fabsf(h[k])); }       // (columns that do not exist: 0)
+        if (d.y_type == CLEAVE_T_E4M3) {
+            const float2 sc = row_scale(cta_join(0.f, top, parts[2]).y);
+            if (threadIdx.x == 0) d.scale[row] = sc.x;
+#pragma unroll
+            for (uint32_t k = 0; k < kOwn; ++k) h[k] *= sc.y;
+        }
+        store_own(d.y, d.y_type, row * d.ldy, d.cols, h);
+    }
+}
+
+// ---- forward, wide -----------------------------------------------------------------------------------
+// V groups of 8 columns per thread.  WARP: blockDim (32, rows per CTA), a warp per row.  Otherwise a CTA per row and a ring of
+// `stages` rows in shared memory, [stage][operand][group] with a thread's groups blockDim.x apart; a CTA takes many rows, so
+// its weights and biases stay in registers where these allow it (up to 512 threads).
+template <typename X, typename R, typename Y, int V, bool WARP, int T>
+__global__ void __launch_bounds__(T, WARP && V > 2 ? 2 : (T <= 512 ? 768 / T : 1)) layernorm_wide_kernel(const __grid_constant__ cleave_layernorm_t d, uint32_t stages) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float parts[3][32];
+    begin_chained();
+    constexpr bool RES = !(sizeof(R) == 1), CODES = sizeof(Y) == 1, KEEP = !WARP && T <= 512;
+    constexpr uint32_t BX = Bytes8<X>::value, BR = Bytes8<R>::value;
+    const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
+    const uint64_t first = WARP ? (uint64_t)blockIdx.x * blockDim.y + threadIdx.y : blockIdx.x;
+    const uint64_t stride = WARP ? (uint64_t)gridDim.x * blockDim.y : gridDim.x;
+    const uint32_t off_r = groups * BX, stage_bytes = off_r + groups * BR;
+    const float inv_cols = 1.f / (float)d.cols;
+    bool live[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) live[v] = tid + v * nt < groups;
+    const uint8_t* px = reinterpret_cast<const uint8_t*>(static_cast<const X*>(d.x) + first * d.ldx) + tid * BX;
+    const uint8_t* pr = reinterpret_cast<const uint8_t*>(d.r) + (RES ? first * d.ldr * (BR / 8) + tid * BR : 0);
+    const uint64_t step_x = stride * d.ldx * (BX / 8), step_r = stride * d.ldr * (BR / 8);
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(ring);
+    uint64_t ahead = first;                                      // the row that is fetched next
+    auto fetch = [&](uint32_t at) {                              // this thread's groups of the next row into the stage at byte `at`
+        if (ahead < d.rows) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (!live[v]) continue;
+#pragma unroll
+                for (uint32_t b = 0; b < BX; b += 16) cp_async<16>(slot + at + (tid + v * nt) * BX + b, px + v * nt * BX + b);
+                if constexpr (RES) {
+#pragma unroll
+                    for (uint32_t b = 0; b < BR; b += 16) cp_async<16>(slot + off_r + at + (tid + v * nt) * BR + b, pr + v * nt * BR + b);
+                }
+            }
+            ahead += stride; px += step_x; pr += step_r;
+        }
+        cp_async_commit();                                       // (an empty group keeps the count when there is no such row)
+    };
+    if constexpr (!WARP)
+        for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
+    F2 kept_w[KEEP ? V : 1][4], kept_b[KEEP ? V : 1][4];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (live[v]) { load_vector8(d.w, d.w_type, (tid + v * nt) * 8, 1.f, kept_w[v]); load_vector8(d.b, d.b_type, (tid + v * nt) * 8, 0.f, kept_b[v]); }
+    }
+    auto join = [&](float v, float* p) {                         // sum over the row's threads
+        v = warp_sum(v);
+        if constexpr (!WARP) {
+            if ((tid & 31u) == 0) p[tid >> 5] = v;
+            __syncthreads();
+            v = warp_sum((tid & 31u) < nt / 32 ? p[tid & 31u] : 0.f);
+        }
+        return v;
+    };
+    Y* py = static_cast<Y*>(d.y) + first * d.ldy + tid * 8;
+    R* ph = RES && d.h ? static_cast<R*>(d.h) + first * d.ldh + tid * 8 : nullptr;
+    uint32_t at = 0;
+    for (uint64_t row = first; row < d.rows; row += stride) {
+        F2 h[V][4];
+        if constexpr (!WARP) {
+            if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
+        }
+        Raw8<X> rx[WARP ? V : 1];
+        Raw8<typename std::conditional<RES, R, X>::type> rr[WARP ? V : 1];
+        if constexpr (WARP) {                                    // everything is asked for before anything is used
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (!live[v]) continue;
+                rx[v] = load_raw8(reinterpret_cast<const X*>(px + v * nt * BX));
+                if constexpr (RES) rr[v] = load_raw8(reinterpret_cast<const R*>(pr + v * nt * BR));
+            }
+        }
+        F2 sum = f2(0.f, 0.f), squares = f2(0.f, 0.f);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!live[v]) continue;
+            if constexpr (WARP) unpack8(rx[v], h[v]);
+            else unpack8(*reinterpret_cast<const Raw8<X>*>(ring + at + (tid + v * nt) * BX), h[v]);
+            if constexpr (RES) {
+                F2 r[4];
+                if constexpr (WARP) unpack8(rr[v], r);
+                else unpack8(*reinterpret_cast<const Raw8<R>*>(ring + off_r + at + (tid + v * nt) * BR), r);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[v][i] = add2(h[v][i], r[i]);
+                if (ph) store8(ph + v * nt * 8, h[v]);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum = add2(sum, h[v][i]);
+        }
+        const float mean = join(sum_of(sum), parts[0]) * inv_cols;
+        if constexpr (!WARP) {                                   // (behind the barrier: every thread has read this stage)
+            fetch(at);
+            at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
+        } else { px += step_x; pr += step_r; }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!live[v]) continue;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) { h[v][i] = add2(h[v][i], f2(-mean, -mean)); squares = fma2(h[v][i], h[v][i], squares); }
+        }
+        const float rstd = rsqrtf(fmaf(join(sum_of(squares), parts[1]), inv_cols, d.eps));
+        if (tid == 0) {
+            if (d.mean) d.mean[row] = mean;
+            if (d.rstd) d.rstd[row] = rstd;
+        }
+        float top = 0.f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!live[v]) continue;
+            F2 w[4], b[4];
+            if constexpr (!KEEP) { load_vector8(d.w, d.w_type, (tid + v * nt) * 8, 1.f, w); load_vector8(d.b, d.b_type, (tid + v * nt) * 8, 0.f, b); }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                h[v][i] = fma2(mul2(h[v][i], f2(rstd, rstd)), KEEP ? kept_w[KEEP ? v : 0][i] : w[i], KEEP ? kept_b[KEEP ? v : 0][i] : b[i]);
+                if constexpr (CODES) top = top2(top, h[v][i]);
+            }
+            if constexpr (!CODES) store8(py + v * nt * 8, h[v]);
+        }
+        if constexpr (CODES) {
+            top = warp_abs_max(top);
+            if constexpr (!WARP) {
+                if ((tid & 31u) == 0) parts[2][tid >> 5] = top;
+                __syncthreads();
+                top = warp_abs_max((tid & 31u) < nt / 32 ? parts[2][tid & 31u] : 0.f);
+            }
+            const float2 sc = row_scale(top);
+            if (tid == 0) d.scale[row] = sc.x;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (!live[v]) continue;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) h[v][i] = mul2(h[v][i], f2(sc.y, sc.y));
+                store8(py + v * nt * 8, h[v]);
+            }
+        }
+        py += stride * d.ldy;
+        if (RES && ph) ph += stride * d.ldh;
+    }
+}
+
+constexpr uint32_t kWarpRowCols = 1024;         // up to here a warp holds a row (four groups a lane)
+constexpr uint32_t kRingBytes = 64 * 1024;      // per CTA; three CTAs of 256 threads an SM
+constexpr uint32_t kRingMost = 160 * 1024;
+
+template <typename X, typename R, typename Y, int V, bool WARP, int T>
+cudaError_t launch_wide(const cleave_layernorm_t& d, uint32_t threads, int sms, cudaStream_t st) {
+    auto kernel = layernorm_wide_kernel<X, R, Y, V, WARP, T>;
+    if (WARP) return launch_chained(kernel, (unsigned)((d.rows + 7) / 8), dim3(32, 8), 0, st, d, 0u);
+    const uint32_t stage = d.cols / 8 * (Bytes8<X>::value + Bytes8<R>::value);
+    const uint32_t stages = std::max(1u, std::min(4u, kRingBytes / stage)), smem = stage * stages;
+    static SmemLimit limit;
+    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
+    if (e != cudaSuccess) return e;
+    // CTAs that fit an SM by shared memory and threads; each walks the rows in steps of the grid
+    const uint32_t fit = std::max(1u, std::min(224u * 1024u / (smem + 2048u), T <= 512 ? 768u / threads : 1u));
+    const uint64_t ctas = std::min((uint64_t)d.rows, (uint64_t)sms * fit);
+    return launch_chained(kernel, (unsigned)ctas, threads, smem, st, d, stages);
+}
+template <typename X, typename R, typename Y>
+cudaError_t launch_sizes(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
+    const uint32_t groups = d.cols / 8;
+    if (d.cols <= kWarpRowCols) {
+        if (groups <= 32) return launch_wide<X, R, Y, 1, true, 256>(d, 32, sms, st);
+        if (groups <= 64) return launch_wide<X, R, Y, 2, true, 256>(d, 32, sms, st);
+        return launch_wide<X, R, Y, 4, true, 256>(d, 32, sms, st);
+    }
+    const uint32_t threads = (groups + 63) / 64 * 32;
+    if (groups <= 512) return launch_wide<X, R, Y, 2, false, 256>(d, threads, sms, st);
+    if (groups <= 768) return launch_wide<X, R, Y, 2, false, 384>(d, threads, sms, st);
+    return launch_wide<X, R, Y, 2, false, 1024>(d, threads, sms, st);
+}
+template <typename X, typename R>
+cudaError_t launch_out(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
+    if (d.y_type == CLEAVE_T_E4M3) return launch_sizes<X, R, uint8_t>(d, sms, st);
+    return d.y_type == CLEAVE_T_F32 ? launch_sizes<X, R, float>(d, sms, st) : launch_sizes<X, R, __nv_bfloat16>(d, sms, st);
+}
+template <typename X>
+cudaError_t launch_residual(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
+    if (!d.r) return launch_out<X, NoRes>(d, sms, st);
+    return d.r_type == CLEAVE_T_F32 ? launch_out<X, float>(d, sms, st) : launch_out<X, __nv_bfloat16>(d, sms, st);
+}
+cudaError_t launch_layernorm(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
+    const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && rows_wide(d.x, d.ldx, d.x_type) && rows_wide(d.y, d.ldy, d.y_type) && (!d.r || rows_wide(d.r, d.ldr, d.r_type)) &&
+                      (!d.h || rows_wide(d.h, d.ldh, d.r_type)) && (uintptr_t)d.w % 16 == 0 && (uintptr_t)d.b % 16 == 0;
+    if (wide) return d.x_type == CLEAVE_T_F32 ? launch_residual<float>(d, sms, st) : launch_residual<__nv_bfloat16>(d, sms, st);
+    if (d.cols <= kOwnCols) {
+        const uint32_t threads = own_threads(d.cols);
+        const unsigned ctas = (unsigned)std::min<uint64_t>(d.rows, (uint64_t)sms * std::min(24u, 1024u / threads));
+        return launch_chained(threads <= 512 ? layernorm_own_kernel<512> : layernorm_own_kernel<1024>, ctas, threads, 0, st, d);
+    }
     return launch_chained(layernorm_any_kernel, (unsigned)d.rows, kRowThreads, 0, st, d);
 }
 
 // ---- backward ----------------------------------------------------------------------------------------
 // A CTA takes the rows part, part + parts, ...; its shares of dw and db go to row `part` of the workspace (fp32
-// [parts x 2 cols], dw's columns first), and sum_parts_kernel adds the parts in order.
-uint32_t layernorm_backward_parts(uint64_t rows, uint32_t) { return (uint32_t)std::min<uint64_t>(rows, 2 * kPartSms); }
+// [parts x 2 cols], dw's columns first; each element belongs to one thread), and layernorm_sum_parts_kernel adds the parts in order.
+uint32_t backward_threads(uint32_t cols) { return (cols / 8 + 63) / 64 * 32; }      // of the wide form
+// CTAs an SM: as many threads as registers allow
+uint32_t backward_fit(uint32_t cols) {
+    const uint32_t threads = std::max(backward_threads(cols), 32u);
+    return threads <= 256 ? 512u / threads : (threads <= 320 ? 2u : 1u);
+}
+uint32_t layernorm_backward_parts(uint64_t rows, uint32_t cols) { return (uint32_t)std::min<uint64_t>(rows, (uint64_t)kPartSms * backward_fit(cols)); }
 
 __global__ void __launch_bounds__(kRowThreads) layernorm_backward_any_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws) {
     __shared__ float buf[32];
@@ -76,6 +356,177 @@ __global__ void __launch_bounds__(kRowThreads) layernorm_backward_any_kernel(con
         }
     }
 }
+
+// two sums over the CTA with one barrier; the buffers take turns
+__device__ __forceinline__ float2 cta_sums(float a, float b, float2* p) {
+    a = warp_sum(a);
+    b = warp_sum(b);
+    if (blockDim.x == 32) return make_float2(a, b);
+    if ((threadIdx.x & 31u) == 0) p[threadIdx.x >> 5] = make_float2(a, b);
+    __syncthreads();
+    const float2 q = (threadIdx.x & 31u) < blockDim.x / 32 ? p[threadIdx.x & 31u] : make_float2(0.f, 0.f);
+    return make_float2(warp_sum(q.x), warp_sum(q.y));
+}
+
+template <int T>
+__global__ void __launch_bounds__(T) layernorm_backward_own_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws) {
+    __shared__ float2 parts[2][32];
+    begin_chained();
+    float w[kOwn], dw[kOwn], db[kOwn];
+    uint32_t ndy[kOwn], nh[kOwn], nres[kOwn];
+#pragma unroll
+    for (uint32_t k = 0; k < kOwn; ++k) { w[k] = 1.f; dw[k] = db[k] = 0.f; }
+    if (d.w) { load_own(d.w, d.w_type, 0, d.cols, nh); own_values(nh, d.w_type, d.cols, w); }
+    const float inv_cols = 1.f / (float)d.cols;
+    uint64_t row = blockIdx.x;
+    load_own(d.dy, d.dy_type, row * d.lddy, d.cols, ndy);
+    load_own(d.h, d.h_type, row * d.ldh, d.cols, nh);
+    if (d.dres) load_own(d.dres, d.h_type, row * d.lddres, d.cols, nres);
+    for (uint32_t it = 0; row < d.rows; row += gridDim.x, ++it) {
+        const float rstd = d.rstd[row], mean = d.mean[row];
+        float q[kOwn], g[kOwn], res[kOwn], dot = 0.f, sum = 0.f;
+        own_values(ndy, d.dy_type, d.cols, q);
+        own_values(nh, d.h_type, d.cols, g);
+        if (d.dres) own_values(nres, d.h_type, d.cols, res);
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) {                    // (columns that do not exist: dy is 0)
+            g[k] = (g[k] - mean) * rstd;
+            dw[k] = fmaf(q[k], g[k], dw[k]);
+            db[k] += q[k];
+            q[k] *= w[k];
+            sum += q[k];
+            dot = fmaf(q[k], g[k], dot);
+        }
+        const uint64_t next = row + gridDim.x;
+        if (next < d.rows) {
+            load_own(d.dy, d.dy_type, next * d.lddy, d.cols, ndy);
+            load_own(d.h, d.h_type, next * d.ldh, d.cols, nh);
+            if (d.dres) load_own(d.dres, d.h_type, next * d.lddres, d.cols, nres);
+        }
+        const float2 both = cta_sums(sum, dot, parts[it & 1]);
+        const float shift = both.x * inv_cols, along = both.y * inv_cols;
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) { q[k] = rstd * (q[k] - shift - g[k] * along); if (d.dres) q[k] += res[k]; }
+        store_own(d.dx, d.h_type, row * d.lddx, d.cols, q);
+    }
+    if (d.dw || d.db)
+#pragma unroll
+        for (uint32_t k = 0; k < kOwn; ++k) {
+            const uint32_t j = threadIdx.x + k * blockDim.x;
+            if (j < d.cols) { ws[(uint64_t)blockIdx.x * 2 * d.cols + j] = dw[k]; ws[((uint64_t)blockIdx.x * 2 + 1) * d.cols + j] = db[k]; }
+        }
+}
+
+// Two groups of 8 columns a thread, a CTA per row, a ring of rows of (dy, h, dres) in shared memory; the CTA's shares of dw and db
+// stay in registers over all its rows (w comes from L1).
+template <typename D, typename H, int T, int CTAS>
+__global__ void __launch_bounds__(T, CTAS) layernorm_backward_wide_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
+    constexpr int V = 2;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float2 parts[2][32];
+    begin_chained();
+    constexpr uint32_t BD = Bytes8<D>::value, BH = Bytes8<H>::value;
+    const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
+    const bool res = d.dres != nullptr;
+    const uint32_t off_h = groups * BD, off_res = off_h + groups * BH, stage_bytes = off_res + (res ? groups * BH : 0u);
+    const uint32_t ring_base = (uint32_t)__cvta_generic_to_shared(ring);
+    const float inv_cols = 1.f / (float)d.cols;
+    bool live[V];
+#pragma unroll
+    for (int v = 0; v < V; ++v) live[v] = tid + v * nt < groups;
+    const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + blockIdx.x * d.lddy) + tid * BD;
+    const uint8_t* ph = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.h) + blockIdx.x * d.ldh) + tid * BH;
+    const uint8_t* pr = res ? reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.dres) + blockIdx.x * d.lddres) + tid * BH : nullptr;
+    const uint64_t step_d = gridDim.x * d.lddy * (BD / 8), step_h = gridDim.x * d.ldh * (BH / 8), step_r = gridDim.x * d.lddres * (BH / 8);
+    uint64_t ahead = blockIdx.x;
+    auto fetch = [&](uint32_t at) {
+        if (ahead < d.rows) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                if (!live[v]) continue;
+                const uint32_t to = ring_base + at;
+#pragma unroll
+                for (uint32_t b = 0; b < BD; b += 16) cp_async<16>(to + (tid + v * nt) * BD + b, pd + v * nt * BD + b);
+#pragma unroll
+                for (uint32_t b = 0; b < BH; b += 16) cp_async<16>(to + off_h + (tid + v * nt) * BH + b, ph + v * nt * BH + b);
+                if (res) {
+#pragma unroll
+                    for (uint32_t b = 0; b < BH; b += 16) cp_async<16>(to + off_res + (tid + v * nt) * BH + b, pr + v * nt * BH + b);
+                }
+            }
+            ahead += gridDim.x; pd += step_d; ph += step_h;
+            if (res) pr += step_r;
+        }
+        cp_async_commit();
+    };
+    for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
+    F2 dw[V][4], db[V][4];
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) dw[v][i] = db[v][i] = f2(0.f, 0.f);
+    H* pdx = static_cast<H*>(d.dx) + blockIdx.x * d.lddx + tid * 8;
+    uint32_t it = 0, at = 0;
+    float next_rstd = blockIdx.x < d.rows ? d.rstd[blockIdx.x] : 0.f, next_mean = blockIdx.x < d.rows ? d.mean[blockIdx.x] : 0.f;
+    for (uint64_t row = blockIdx.x; row < d.rows; row += gridDim.x, ++it) {
+        if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
+        const float rstd = next_rstd, mean = next_mean;
+        if (row + gridDim.x < d.rows) { next_rstd = d.rstd[row + gridDim.x]; next_mean = d.mean[row + gridDim.x]; }
+        const uint8_t* stage = ring + at;
+        F2 q[V][4], dots = f2(0.f, 0.f), sums = f2(0.f, 0.f);    // q = w dy; sums of q xh and of q
+        Raw8<H> rh[V], rr[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!live[v]) continue;
+            const uint32_t g = tid + v * nt;
+            unpack8(*reinterpret_cast<const Raw8<D>*>(stage + g * BD), q[v]);
+            rh[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_h + g * BH);
+            if (res) rr[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_res + g * BH);
+            F2 h[4], w[4];
+            unpack8(rh[v], h);
+            load_vector8(d.w, d.w_type, g * 8, 1.f, w);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const F2 xh = mul2(add2(h[i], f2(-mean, -mean)), f2(rstd, rstd));
+                dw[v][i] = fma2(q[v][i], xh, dw[v][i]);
+                db[v][i] = add2(db[v][i], q[v][i]);
+                q[v][i] = mul2(q[v][i], w[i]);
+                sums = add2(sums, q[v][i]);
+                dots = fma2(q[v][i], xh, dots);
+            }
+        }
+        const float2 both = cta_sums(sum_of(sums), sum_of(dots), parts[it & 1]);          // (its barrier: every thread has read this stage)
+        fetch(at);
+        at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
+        const float shift = both.x * inv_cols, along = both.y * inv_cols;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!live[v]) continue;
+            F2 dx[4], h[4];
+            unpack8(rh[v], h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const F2 xh = mul2(add2(h[i], f2(-mean, -mean)), f2(rstd, rstd));
+                dx[i] = mul2(f2(rstd, rstd), fma2(f2(-along, -along), xh, add2(q[v][i], f2(-shift, -shift))));
+            }
+            if (res) {
+                unpack8(rr[v], h);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dx[i] = add2(dx[i], h[i]);
+            }
+            store8(pdx + v * nt * 8, dx);
+        }
+        pdx += gridDim.x * d.lddx;
+    }
+    if (d.dw || d.db)
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (live[v]) {
+                store8(ws + (uint64_t)blockIdx.x * 2 * d.cols + (tid + v * nt) * 8, dw[v]);
+                store8(ws + ((uint64_t)blockIdx.x * 2 + 1) * d.cols + (tid + v * nt) * 8, db[v]);
+            }
+}
+
 // out[j] = sum over the parts of ws[part][j], 0 <= j < cols for dw and behind them for db, each in a fixed order: 32 columns
 // per CTA; warp w adds the parts w, w + 32, ... and the 32 sums are added by a shuffle tree.
 __global__ void __launch_bounds__(1024) layernorm_sum_parts_kernel(const float* ws, uint32_t parts, uint32_t cols, float* dw, float* db) {
@@ -95,10 +546,38 @@ __global__ void __launch_bounds__(1024) layernorm_sum_parts_kernel(const float* 
     if (lane == 0 && blockIdx.x * 32u + warp < cols) out[blockIdx.x * 32u + warp] = v;
 }
 
+template <typename D, typename H, int T, int CTAS>
+cudaError_t launch_backward_wide(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
+    auto kernel = layernorm_backward_wide_kernel<D, H, T, CTAS>;
+    static SmemLimit limit;
+    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
+    if (e != cudaSuccess) return e;
+    const uint32_t stages = std::max(1u, std::min(4u, std::min(kRingMost, 216u * 1024u / backward_fit(d.cols)) / stage));
+    return launch_chained(kernel, parts, backward_threads(d.cols), stage * stages, st, d, ws, stages);
+}
+template <typename D, typename H>
+cudaError_t launch_backward_types(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
+    const uint32_t groups = d.cols / 8;
+    if (groups <= 512) return launch_backward_wide<D, H, 256, 2>(d, ws, parts, stage, st);
+    if (groups <= 640) return launch_backward_wide<D, H, 320, 2>(d, ws, parts, stage, st);
+    if (groups <= 1024) return launch_backward_wide<D, H, 512, 1>(d, ws, parts, stage, st);
+    return launch_backward_wide<D, H, 1024, 1>(d, ws, parts, stage, st);
+}
 cudaError_t launch_layernorm_backward(const cleave_layernorm_backward_t& d, float* ws, cudaStream_t st) {
     const uint32_t parts = layernorm_backward_parts(d.rows, d.cols);
+    const uint64_t stage = (uint64_t)d.cols * (type_bytes(d.dy_type) + type_bytes(d.h_type) * (d.dres ? 2u : 1u));
+    const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && stage <= kRingMost && rows_wide(d.dy, d.lddy, d.dy_type) && rows_wide(d.h, d.ldh, d.h_type) &&
+                      rows_wide(d.dx, d.lddx, d.h_type) && (!d.dres || rows_wide(d.dres, d.lddres, d.h_type)) && (uintptr_t)d.w % 16 == 0;
     cudaError_t e = cudaSuccess;
-    if (parts) e = launch_chained(layernorm_backward_any_kernel, parts, kRowThreads, 0, st, d, ws);
+    if (parts && wide) {
+        if (d.dy_type == CLEAVE_T_F32) e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<float, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<float, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
+        else e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<__nv_bfloat16, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<__nv_bfloat16, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
+    } else if (parts && d.cols <= kOwnCols) {
+        const uint32_t threads = own_threads(d.cols);
+        e = launch_chained(threads <= 512 ? layernorm_backward_own_kernel<512> : layernorm_backward_own_kernel<1024>, parts, threads, 0, st, d, ws);
+    } else if (parts) {
+        e = launch_chained(layernorm_backward_any_kernel, parts, kRowThreads, 0, st, d, ws);
+    }
     if (e != cudaSuccess || (!d.dw && !d.db)) return e;
     return launch_chained(layernorm_sum_parts_kernel, dim3((d.cols + 31) / 32, 2), 1024, 0, st, ws, parts, d.cols, d.dw, d.db);
 }
