@@ -3,7 +3,8 @@
 // Bound by the HBM's bandwidth: each row is read once, kept in registers while its mean and then its variance (the sum of the
 // squared differences to that mean) are formed, and written once.  Forms as in the root-mean-square norm:
 //   wide   rows of whole 16-byte groups: a thread owns groups of 8 columns.  Up to 1024 columns a warp takes a row; above, a CTA
-//          takes a row, and the next rows come by cp.async into a ring in shared memory that needs no barrier of its own.
+//          takes a row.  The next rows come by cp.async into a ring in shared memory: each thread copies and reads its own groups
+//          only, so the ring needs no barrier of its own and the bytes in flight do not depend on registers.
 //   own    any alignment, up to 8192 columns: neighbouring threads own neighbouring columns, held in registers.
 //   any    what is left: the row is taken again in each pass (it stays in L1 / L2).
 #include <algorithm>
@@ -123,15 +124,17 @@ __global__ void __launch_bounds__(T) layernorm_own_kernel(const __grid_constant_
 }
 
 // ---- forward, wide -----------------------------------------------------------------------------------
-// V groups of 8 columns per thread.  WARP: blockDim (32, rows per CTA), a warp per row.  Otherwise a CTA per row and a ring of
-// `stages` rows in shared memory, [stage][operand][group] with a thread's groups blockDim.x apart; a CTA takes many rows, so
-// its weights and biases stay in registers where these allow it (up to 512 threads).
+// V groups of 8 columns per thread.  WARP: blockDim (32, 8), a warp per row; otherwise a CTA per row.  A row has a ring of `stages` of the
+// next ones in shared memory, [stage][operand][group] with a thread's groups blockDim.x apart, and weights and biases stay in registers
+// over all rows.  Warps an SM: 24 of two groups, 16 of four (8192 x 8192 into E4M3 80 us; with 1024 threads of two groups, whose
+// registers hold no weights, 133); 8 warps with a row each, all registers theirs (8192 x 768 17.0 us; a warp's row at a time without a ring 18.2).
+constexpr int row_warps(int V) { return V <= 2 ? 24 : 16; }
 template <typename X, typename R, typename Y, int V, bool WARP, int T>
-__global__ void __launch_bounds__(T, WARP && V > 2 ? 2 : (T <= 512 ? 768 / T : 1)) layernorm_wide_kernel(const __grid_constant__ cleave_layernorm_t d, uint32_t stages) {
+__global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm_wide_kernel(const __grid_constant__ cleave_layernorm_t d, uint32_t stages) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float parts[3][32];
     begin_chained();
-    constexpr bool RES = !(sizeof(R) == 1), CODES = sizeof(Y) == 1, KEEP = !WARP && T <= 512;
+    constexpr bool RES = !(sizeof(R) == 1), CODES = sizeof(Y) == 1;
     constexpr uint32_t BX = Bytes8<X>::value, BR = Bytes8<R>::value;
     const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
     const uint64_t first = WARP ? (uint64_t)blockIdx.x * blockDim.y + threadIdx.y : blockIdx.x;
@@ -144,7 +147,8 @@ __global__ void __launch_bounds__(T, WARP && V > 2 ? 2 : (T <= 512 ? 768 / T : 1
     const uint8_t* px = reinterpret_cast<const uint8_t*>(static_cast<const X*>(d.x) + first * d.ldx) + tid * BX;
     const uint8_t* pr = reinterpret_cast<const uint8_t*>(d.r) + (RES ? first * d.ldr * (BR / 8) + tid * BR : 0);
     const uint64_t step_x = stride * d.ldx * (BX / 8), step_r = stride * d.ldr * (BR / 8);
-    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(ring);
+    const uint8_t* mine = ring + (WARP ? threadIdx.y * stages * stage_bytes : 0u);
+    const uint32_t slot = (uint32_t)__cvta_generic_to_shared(mine);
     uint64_t ahead = first;                                      // the row that is fetched next
     auto fetch = [&](uint32_t at) {                              // this thread's groups of the next row into the stage at byte `at`
         if (ahead < d.rows) {
@@ -162,14 +166,11 @@ __global__ void __launch_bounds__(T, WARP && V > 2 ? 2 : (T <= 512 ? 768 / T : 1
         }
         cp_async_commit();                                       // (an empty group keeps the count when there is no such row)
     };
-    if constexpr (!WARP)
-        for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
-    F2 kept_w[KEEP ? V : 1][4], kept_b[KEEP ? V : 1][4];
-    if constexpr (KEEP) {
+    for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
+    F2 w[V][4], b[V][4];
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (live[v]) { load_vector8(d.w, d.w_type, (tid + v * nt) * 8, 1.f, kept_w[v]); load_vector8(d.b, d.b_type, (tid + v * nt) * 8, 0.f, kept_b[v]); }
-    }
+    for (int v = 0; v < V; ++v)
+        if (live[v]) { load_vector8(d.w, d.w_type, (tid + v * nt) * 8, 1.f, w[v]); load_vector8(d.b, d.b_type, (tid + v * nt) * 8, 0.f, b[v]); }
     auto join = [&](float v, float* p) {                         // sum over the row's threads
         v = warp_sum(v);
         if constexpr (!WARP) {
@@ -184,29 +185,15 @@ __global__ void __launch_bounds__(T, WARP && V > 2 ? 2 : (T <= 512 ? 768 / T : 1
     uint32_t at = 0;
     for (uint64_t row = first; row < d.rows; row += stride) {
         F2 h[V][4];
-        if constexpr (!WARP) {
-            if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
-        }
-        Raw8<X> rx[WARP ? V : 1];
-        Raw8<typename std::conditional<RES, R, X>::type> rr[WARP ? V : 1];
-        if constexpr (WARP) {                                    // everything is asked for before anything is used
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                if (!live[v]) continue;
-                rx[v] = load_raw8(reinterpret_cast<const X*>(px + v * nt * BX));
-                if constexpr (RES) rr[v] = load_raw8(reinterpret_cast<const R*>(pr + v * nt * BR));
-            }
-        }
+        if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
         F2 sum = f2(0.f, 0.f), squares = f2(0.f, 0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
-            if constexpr (WARP) unpack8(rx[v], h[v]);
-            else unpack8(*reinterpret_cast<const Raw8<X>*>(ring + at + (tid + v * nt) * BX), h[v]);
+            unpack8(*reinterpret_cast<const Raw8<X>*>(mine + at + (tid + v * nt) * BX), h[v]);
             if constexpr (RES) {
                 F2 r[4];
-                if constexpr (WARP) unpack8(rr[v], r);
-                else unpack8(*reinterpret_cast<const Raw8<R>*>(ring + off_r + at + (tid + v * nt) * BR), r);
+                unpack8(*reinterpret_cast<const Raw8<R>*>(mine + off_r + at + (tid + v * nt) * BR), r);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) h[v][i] = add2(h[v][i], r[i]);
                 if (ph) store8(ph + v * nt * 8, h[v]);
@@ -215,10 +202,8 @@ __global__ void __launch_bounds__(T, WARP && V > 2 ? 2 : (T <= 512 ? 768 / T : 1
             for (int i = 0; i < 4; ++i) sum = add2(sum, h[v][i]);
         }
         const float mean = join(sum_of(sum), parts[0]) * inv_cols;
-        if constexpr (!WARP) {                                   // (behind the barrier: every thread has read this stage)
-            fetch(at);
-            at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
-        } else { px += step_x; pr += step_r; }
+        fetch(at);                                               // (this thread has read its groups of this stage)
+        at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
@@ -234,11 +219,9 @@ __global__ void __launch_bounds__(T, WARP && V > 2 ? 2 : (T <= 512 ? 768 / T : 1
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
-            F2 w[4], b[4];
-            if constexpr (!KEEP) { load_vector8(d.w, d.w_type, (tid + v * nt) * 8, 1.f, w); load_vector8(d.b, d.b_type, (tid + v * nt) * 8, 0.f, b); }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                h[v][i] = fma2(mul2(h[v][i], f2(rstd, rstd)), KEEP ? kept_w[KEEP ? v : 0][i] : w[i], KEEP ? kept_b[KEEP ? v : 0][i] : b[i]);
+                h[v][i] = fma2(mul2(h[v][i], f2(rstd, rstd)), w[v][i], b[v][i]);
                 if constexpr (CODES) top = top2(top, h[v][i]);
             }
             if constexpr (!CODES) store8(py + v * nt * 8, h[v]);
@@ -267,21 +250,24 @@ __global__ void __launch_bounds__(T, WARP && V > 2 ? 2 : (T <= 512 ? 768 / T : 1
 
 constexpr uint32_t kWarpRowCols = 1024;         // up to here a warp holds a row (four groups a lane)
 constexpr uint32_t kRingBytes = 64 * 1024;      // per CTA; three CTAs of 256 threads an SM
-constexpr uint32_t kRingMost = 160 * 1024;
+constexpr uint32_t kRingMost = 208 * 1024;     // of all rings of a CTA
+constexpr uint32_t kWarpRing = 26 * 1024;       // of one of a CTA's eight warps
 
 template <typename X, typename R, typename Y, int V, bool WARP, int T>
 cudaError_t launch_wide(const cleave_layernorm_t& d, uint32_t threads, int sms, cudaStream_t st) {
     auto kernel = layernorm_wide_kernel<X, R, Y, V, WARP, T>;
-    if (WARP) return launch_chained(kernel, (unsigned)((d.rows + 7) / 8), dim3(32, 8), 0, st, d, 0u);
     const uint32_t stage = d.cols / 8 * (Bytes8<X>::value + Bytes8<R>::value);
-    const uint32_t stages = std::max(1u, std::min(4u, kRingBytes / stage)), smem = stage * stages;
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
-    // CTAs that fit an SM by shared memory and threads; each walks the rows in steps of the grid
-    const uint32_t fit = std::max(1u, std::min(224u * 1024u / (smem + 2048u), T <= 512 ? 768u / threads : 1u));
-    const uint64_t ctas = std::min((uint64_t)d.rows, (uint64_t)sms * fit);
-    return launch_chained(kernel, (unsigned)ctas, threads, smem, st, d, stages);
+    if (WARP) {                                                  // a ring a warp
+        const uint32_t stages = std::max(1u, std::min(4u, kWarpRing / stage));
+        return launch_chained(kernel, (unsigned)std::min<uint64_t>((d.rows + 7) / 8, (uint64_t)sms), dim3(32, 8), 8 * stages * stage, st, d, stages);
+    }
+    const uint32_t stages = std::max(1u, std::min(4u, kRingBytes / stage)), smem = stage * stages;
+    // CTAs that fit an SM by shared memory and registers; each walks the rows in steps of the grid
+    const uint32_t fit = std::max(1u, std::min(224u * 1024u / (smem + 2048u), (uint32_t)row_warps(V) * 32u / threads));
+    return launch_chained(kernel, (unsigned)std::min((uint64_t)d.rows, (uint64_t)sms * fit), threads, smem, st, d, stages);
 }
 template <typename X, typename R, typename Y>
 cudaError_t launch_sizes(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
@@ -289,12 +275,13 @@ cudaError_t launch_sizes(const cleave_layernorm_t& d, int sms, cudaStream_t st) 
     if (d.cols <= kWarpRowCols) {
         if (groups <= 32) return launch_wide<X, R, Y, 1, true, 256>(d, 32, sms, st);
         if (groups <= 64) return launch_wide<X, R, Y, 2, true, 256>(d, 32, sms, st);
+        if (groups <= 96) return launch_wide<X, R, Y, 3, true, 256>(d, 32, sms, st);
         return launch_wide<X, R, Y, 4, true, 256>(d, 32, sms, st);
     }
-    const uint32_t threads = (groups + 63) / 64 * 32;
-    if (groups <= 512) return launch_wide<X, R, Y, 2, false, 256>(d, threads, sms, st);
-    if (groups <= 768) return launch_wide<X, R, Y, 2, false, 384>(d, threads, sms, st);
-    return launch_wide<X, R, Y, 2, false, 1024>(d, threads, sms, st);
+    if (groups <= 512) return launch_wide<X, R, Y, 2, false, 256>(d, (groups + 63) / 64 * 32, sms, st);
+    const uint32_t threads = (groups + 127) / 128 * 32;
+    if (groups <= 1024) return launch_wide<X, R, Y, 4, false, 256>(d, threads, sms, st);
+    return launch_wide<X, R, Y, 4, false, 512>(d, threads, sms, st);
 }
 template <typename X, typename R>
 cudaError_t launch_out(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
@@ -321,13 +308,17 @@ cudaError_t launch_layernorm(const cleave_layernorm_t& d, int sms, cudaStream_t 
 // ---- backward ----------------------------------------------------------------------------------------
 // A CTA takes the rows part, part + parts, ...; its shares of dw and db go to row `part` of the workspace (fp32
 // [parts x 2 cols], dw's columns first; each element belongs to one thread), and layernorm_sum_parts_kernel adds the parts in order.
-uint32_t backward_threads(uint32_t cols) { return (cols / 8 + 63) / 64 * 32; }      // of the wide form
-// CTAs an SM: as many threads as registers allow
-uint32_t backward_fit(uint32_t cols) {
-    const uint32_t threads = std::max(backward_threads(cols), 32u);
-    return threads <= 256 ? 512u / threads : (threads <= 320 ? 2u : 1u);
+// The wide form's shape: threads a row, groups of 8 columns a thread, rows that a CTA works on at a time.  What counts is work between two
+// barriers: many groups a thread and few threads (16384 rows of 4096 columns: 4 groups and 128 threads 91 us, 2 groups and 256
+// threads 111, one group and 512 threads 164); up to 1024 columns a row is one warp's.  A CTA an SM, with as many warps as registers allow.
+struct Shape { uint32_t threads, groups, rows; };
+Shape backward_shape(uint32_t cols) {
+    const uint32_t units = (cols + 7) / 8;
+    const uint32_t threads = units <= 640 ? std::min(128u, (units + 127) / 128 * 32) : (units <= 1024 ? 256u : 512u), groups = (units + threads - 1) / threads;
+    const uint32_t warps = groups <= 2 ? 16 : (groups == 3 ? 12 : 8);
+    return {threads, groups, std::max(1u, warps * 32 / threads)};
 }
-uint32_t layernorm_backward_parts(uint64_t rows, uint32_t cols) { return (uint32_t)std::min<uint64_t>(rows, (uint64_t)kPartSms * backward_fit(cols)); }
+uint32_t layernorm_backward_parts(uint64_t rows, uint32_t cols) { return (uint32_t)std::min<uint64_t>(rows, kPartSms); }
 
 __global__ void __launch_bounds__(kRowThreads) layernorm_backward_any_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws) {
     __shared__ float buf[32];
@@ -357,20 +348,31 @@ __global__ void __launch_bounds__(kRowThreads) layernorm_backward_any_kernel(con
     }
 }
 
-// two sums over the CTA with one barrier; the buffers take turns
-__device__ __forceinline__ float2 cta_sums(float a, float b, float2* p) {
-    a = warp_sum(a);
-    b = warp_sum(b);
-    if (blockDim.x == 32) return make_float2(a, b);
-    if ((threadIdx.x & 31u) == 0) p[threadIdx.x >> 5] = make_float2(a, b);
-    __syncthreads();
-    const float2 q = (threadIdx.x & 31u) < blockDim.x / 32 ? p[threadIdx.x & 31u] : make_float2(0.f, 0.f);
-    return make_float2(warp_sum(q.x), warp_sum(q.y));
+// Two sums over a row's threads with one barrier; the buffers take turns.  The lower half of a warp carries on with the first sum, the upper
+// half with the second: half of the shuffles.
+__device__ __forceinline__ float half_sum(float v) {
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+__device__ __forceinline__ float2 row_sums(float a, float b, float (&p)[2][32]) {        // over the threads with this threadIdx.y
+    const uint32_t lane = threadIdx.x & 31u, half = lane >> 4, warps = blockDim.x / 32;
+    float v = half ? b : a;
+    v = half_sum(v + __shfl_xor_sync(0xFFFFFFFFu, half ? a : b, 16));
+    if (warps > 1) {
+        if ((lane & 15u) == 0) p[half][threadIdx.x >> 5] = v;
+        if (blockDim.y == 1) __syncthreads();
+        else asm volatile("bar.sync %0, %1;" ::"r"(threadIdx.y + 1), "r"(blockDim.x) : "memory");
+        v = (lane & 15u) < warps ? p[half][lane & 15u] : 0.f;
+        if (warps > 16 && (lane & 15u) + 16 < warps) v += p[half][(lane & 15u) + 16];
+        v = half_sum(v);
+    }
+    return make_float2(__shfl_sync(0xFFFFFFFFu, v, 0), __shfl_sync(0xFFFFFFFFu, v, 16));
 }
 
 template <int T>
 __global__ void __launch_bounds__(T) layernorm_backward_own_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws) {
-    __shared__ float2 parts[2][32];
+    __shared__ float parts[2][2][32];
     begin_chained();
     float w[kOwn], dw[kOwn], db[kOwn];
     uint32_t ndy[kOwn], nh[kOwn], nres[kOwn];
@@ -403,7 +405,7 @@ __global__ void __launch_bounds__(T) layernorm_backward_own_kernel(const __grid_
             load_own(d.h, d.h_type, next * d.ldh, d.cols, nh);
             if (d.dres) load_own(d.dres, d.h_type, next * d.lddres, d.cols, nres);
         }
-        const float2 both = cta_sums(sum, dot, parts[it & 1]);
+        const float2 both = row_sums(sum, dot, parts[it & 1]);
         const float shift = both.x * inv_cols, along = both.y * inv_cols;
 #pragma unroll
         for (uint32_t k = 0; k < kOwn; ++k) { q[k] = rstd * (q[k] - shift - g[k] * along); if (d.dres) q[k] += res[k]; }
@@ -417,28 +419,32 @@ __global__ void __launch_bounds__(T) layernorm_backward_own_kernel(const __grid_
         }
 }
 
-// Two groups of 8 columns a thread, a CTA per row, a ring of rows of (dy, h, dres) in shared memory; the CTA's shares of dw and db
-// stay in registers over all its rows (w comes from L1).
-template <typename D, typename H, int T, int CTAS>
-__global__ void __launch_bounds__(T, CTAS) layernorm_backward_wide_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
-    constexpr int V = 2;
-    extern __shared__ __align__(16) uint8_t ring[];
-    __shared__ float2 parts[2][32];
+// V groups of 8 columns a thread, blockDim.y rows at a time, each with a ring of the next rows of (dy, h, dres) in shared memory; the
+// weights (where registers hold them) and the shares of dw and db stay in registers over all rows, and the
+// CTA's rows add theirs at the end.
+template <typename D, typename H, int V, int T>
+__global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
+    extern __shared__ __align__(16) uint8_t rings[];
+    __shared__ float buffers[16][2][2][32];
     begin_chained();
     constexpr uint32_t BD = Bytes8<D>::value, BH = Bytes8<H>::value;
+    constexpr bool KEEP = V < 4 || (V == 4 && T < 512) || (V == 5 && sizeof(H) == 2);
+    float (&parts)[2][2][32] = buffers[threadIdx.y];
     const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
     const bool res = d.dres != nullptr;
     const uint32_t off_h = groups * BD, off_res = off_h + groups * BH, stage_bytes = off_res + (res ? groups * BH : 0u);
+    uint8_t* ring = rings + threadIdx.y * stages * stage_bytes;
     const uint32_t ring_base = (uint32_t)__cvta_generic_to_shared(ring);
     const float inv_cols = 1.f / (float)d.cols;
+    const uint64_t first = blockIdx.x + (uint64_t)gridDim.x * threadIdx.y, stride = (uint64_t)gridDim.x * blockDim.y;
     bool live[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) live[v] = tid + v * nt < groups;
-    const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + blockIdx.x * d.lddy) + tid * BD;
-    const uint8_t* ph = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.h) + blockIdx.x * d.ldh) + tid * BH;
-    const uint8_t* pr = res ? reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.dres) + blockIdx.x * d.lddres) + tid * BH : nullptr;
-    const uint64_t step_d = gridDim.x * d.lddy * (BD / 8), step_h = gridDim.x * d.ldh * (BH / 8), step_r = gridDim.x * d.lddres * (BH / 8);
-    uint64_t ahead = blockIdx.x;
+    const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + first * d.lddy) + tid * BD;
+    const uint8_t* ph = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.h) + first * d.ldh) + tid * BH;
+    const uint8_t* pr = res ? reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.dres) + first * d.lddres) + tid * BH : nullptr;
+    const uint64_t step_d = stride * d.lddy * (BD / 8), step_h = stride * d.ldh * (BH / 8), step_r = stride * d.lddres * (BH / 8);
+    uint64_t ahead = first;
     auto fetch = [&](uint32_t at) {
         if (ahead < d.rows) {
 #pragma unroll
@@ -454,27 +460,32 @@ __global__ void __launch_bounds__(T, CTAS) layernorm_backward_wide_kernel(const 
                     for (uint32_t b = 0; b < BH; b += 16) cp_async<16>(to + off_res + (tid + v * nt) * BH + b, pr + v * nt * BH + b);
                 }
             }
-            ahead += gridDim.x; pd += step_d; ph += step_h;
+            ahead += stride; pd += step_d; ph += step_h;
             if (res) pr += step_r;
         }
         cp_async_commit();
     };
     for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
-    F2 dw[V][4], db[V][4];
+    F2 w[KEEP ? V : 1][4], dw[V][4], db[V][4];
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) if (live[v]) load_vector8(d.w, d.w_type, (tid + v * nt) * 8, 1.f, w[v]);
+    }
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int i = 0; i < 4; ++i) dw[v][i] = db[v][i] = f2(0.f, 0.f);
-    H* pdx = static_cast<H*>(d.dx) + blockIdx.x * d.lddx + tid * 8;
+    H* pdx = static_cast<H*>(d.dx) + first * d.lddx + tid * 8;
     uint32_t it = 0, at = 0;
-    float next_rstd = blockIdx.x < d.rows ? d.rstd[blockIdx.x] : 0.f, next_mean = blockIdx.x < d.rows ? d.mean[blockIdx.x] : 0.f;
-    for (uint64_t row = blockIdx.x; row < d.rows; row += gridDim.x, ++it) {
+    float next_rstd = first < d.rows ? d.rstd[first] : 0.f, next_mean = first < d.rows ? d.mean[first] : 0.f;
+    for (uint64_t row = first; row < d.rows; row += stride, ++it) {
         if (stages >= 4) cp_async_wait<3>(); else if (stages == 3) cp_async_wait<2>(); else if (stages == 2) cp_async_wait<1>(); else cp_async_wait<0>();
         const float rstd = next_rstd, mean = next_mean;
-        if (row + gridDim.x < d.rows) { next_rstd = d.rstd[row + gridDim.x]; next_mean = d.mean[row + gridDim.x]; }
+        if (row + stride < d.rows) { next_rstd = d.rstd[row + stride]; next_mean = d.mean[row + stride]; }
         const uint8_t* stage = ring + at;
-        F2 q[V][4], dots = f2(0.f, 0.f), sums = f2(0.f, 0.f);    // q = w dy; sums of q xh and of q
+        F2 q[V][4], dots = f2(0.f, 0.f), sums = f2(0.f, 0.f);    // q = w dy; sums of q (h - mean) and of q
         Raw8<H> rh[V], rr[V];
+        const F2 mean2 = f2(-mean, -mean), rstd2 = f2(rstd, rstd);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
@@ -482,33 +493,32 @@ __global__ void __launch_bounds__(T, CTAS) layernorm_backward_wide_kernel(const 
             unpack8(*reinterpret_cast<const Raw8<D>*>(stage + g * BD), q[v]);
             rh[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_h + g * BH);
             if (res) rr[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_res + g * BH);
-            F2 h[4], w[4];
+            F2 h[4];
             unpack8(rh[v], h);
-            load_vector8(d.w, d.w_type, g * 8, 1.f, w);
+            if constexpr (!KEEP) load_vector8(d.w, d.w_type, g * 8, 1.f, w[0]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const F2 xh = mul2(add2(h[i], f2(-mean, -mean)), f2(rstd, rstd));
-                dw[v][i] = fma2(q[v][i], xh, dw[v][i]);
+                const F2 c = add2(h[i], mean2);
+                dw[v][i] = fma2(mul2(q[v][i], rstd2), c, dw[v][i]);
                 db[v][i] = add2(db[v][i], q[v][i]);
-                q[v][i] = mul2(q[v][i], w[i]);
+                q[v][i] = mul2(q[v][i], w[KEEP ? v : 0][i]);
                 sums = add2(sums, q[v][i]);
-                dots = fma2(q[v][i], xh, dots);
+                dots = fma2(q[v][i], c, dots);
             }
         }
-        const float2 both = cta_sums(sum_of(sums), sum_of(dots), parts[it & 1]);          // (its barrier: every thread has read this stage)
+        const float2 both = row_sums(sum_of(sums), sum_of(dots), parts[it & 1]);
         fetch(at);
         at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
-        const float shift = both.x * inv_cols, along = both.y * inv_cols;
+        // dx = rstd q - rstd mean(q) - (rstd^3 mean(q (h - mean))) (h - mean)
+        const float shift = rstd * (both.x * inv_cols), along = rstd * (rstd * (rstd * (both.y * inv_cols)));
+        const F2 shift2 = f2(-shift, -shift), along2 = f2(-along, -along);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
             F2 dx[4], h[4];
             unpack8(rh[v], h);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const F2 xh = mul2(add2(h[i], f2(-mean, -mean)), f2(rstd, rstd));
-                dx[i] = mul2(f2(rstd, rstd), fma2(f2(-along, -along), xh, add2(q[v][i], f2(-shift, -shift))));
-            }
+            for (int i = 0; i < 4; ++i) dx[i] = fma2(along2, add2(h[i], mean2), fma2(rstd2, q[v][i], shift2));
             if (res) {
                 unpack8(rr[v], h);
 #pragma unroll
@@ -516,15 +526,41 @@ __global__ void __launch_bounds__(T, CTAS) layernorm_backward_wide_kernel(const 
             }
             store8(pdx + v * nt * 8, dx);
         }
-        pdx += gridDim.x * d.lddx;
+        pdx += stride * d.lddx;
     }
-    if (d.dw || d.db)
+    if (!d.dw && !d.db) return;
+    if (blockDim.y > 1) {                                        // the rows' shares, in order
+        float* other = reinterpret_cast<float*>(rings);
+        cp_async_wait<0>();
+        __syncthreads();
+        if (threadIdx.y)
 #pragma unroll
-        for (int v = 0; v < V; ++v)
-            if (live[v]) {
-                store8(ws + (uint64_t)blockIdx.x * 2 * d.cols + (tid + v * nt) * 8, dw[v]);
-                store8(ws + ((uint64_t)blockIdx.x * 2 + 1) * d.cols + (tid + v * nt) * 8, db[v]);
-            }
+            for (int v = 0; v < V; ++v)
+                if (live[v]) {
+                    store8(other + ((uint64_t)(threadIdx.y - 1) * 2) * d.cols + (tid + v * nt) * 8, dw[v]);
+                    store8(other + ((uint64_t)(threadIdx.y - 1) * 2 + 1) * d.cols + (tid + v * nt) * 8, db[v]);
+                }
+        __syncthreads();
+        if (threadIdx.y) return;
+        for (uint32_t y = 0; y + 1 < blockDim.y; ++y)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+                if (live[v]) {
+                    F2 t[4];
+                    unpack8(*reinterpret_cast<const Raw8<float>*>(other + (uint64_t)y * 2 * d.cols + (tid + v * nt) * 8), t);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) dw[v][i] = add2(dw[v][i], t[i]);
+                    unpack8(*reinterpret_cast<const Raw8<float>*>(other + ((uint64_t)y * 2 + 1) * d.cols + (tid + v * nt) * 8), t);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) db[v][i] = add2(db[v][i], t[i]);
+                }
+    }
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+        if (live[v]) {
+            store8(ws + (uint64_t)blockIdx.x * 2 * d.cols + (tid + v * nt) * 8, dw[v]);
+            store8(ws + ((uint64_t)blockIdx.x * 2 + 1) * d.cols + (tid + v * nt) * 8, db[v]);
+        }
 }
 
 // out[j] = sum over the parts of ws[part][j], 0 <= j < cols for dw and behind them for db, each in a fixed order: 32 columns
@@ -546,27 +582,28 @@ __global__ void __launch_bounds__(1024) layernorm_sum_parts_kernel(const float* 
     if (lane == 0 && blockIdx.x * 32u + warp < cols) out[blockIdx.x * 32u + warp] = v;
 }
 
-template <typename D, typename H, int T, int CTAS>
-cudaError_t launch_backward_wide(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
-    auto kernel = layernorm_backward_wide_kernel<D, H, T, CTAS>;
+template <typename D, typename H, int V, int T>
+cudaError_t launch_backward_wide(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, const Shape& sh, cudaStream_t st) {
+    auto kernel = layernorm_backward_wide_kernel<D, H, V, T>;
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
-    const uint32_t stages = std::max(1u, std::min(4u, std::min(kRingMost, 216u * 1024u / backward_fit(d.cols)) / stage));
-    return launch_chained(kernel, parts, backward_threads(d.cols), stage * stages, st, d, ws, stages);
+    const uint32_t stages = std::max(1u, std::min(4u, kRingMost / sh.rows / stage)), joined = (sh.rows - 1) * 2 * d.cols * 4;
+    return launch_chained(kernel, parts, dim3(sh.threads, sh.rows), std::max(stage * stages * sh.rows, joined), st, d, ws, stages);
 }
 template <typename D, typename H>
 cudaError_t launch_backward_types(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
-    const uint32_t groups = d.cols / 8;
-    if (groups <= 512) return launch_backward_wide<D, H, 256, 2>(d, ws, parts, stage, st);
-    if (groups <= 640) return launch_backward_wide<D, H, 320, 2>(d, ws, parts, stage, st);
-    if (groups <= 1024) return launch_backward_wide<D, H, 512, 1>(d, ws, parts, stage, st);
-    return launch_backward_wide<D, H, 1024, 1>(d, ws, parts, stage, st);
+    const Shape sh = backward_shape(d.cols);
+    if (sh.threads == 512) return launch_backward_wide<D, H, 4, 512>(d, ws, parts, stage, sh, st);
+    if (sh.groups == 5) return launch_backward_wide<D, H, 5, 256>(d, ws, parts, stage, sh, st);
+    if (sh.groups == 4) return launch_backward_wide<D, H, 4, 256>(d, ws, parts, stage, sh, st);
+    if (sh.groups == 3) return launch_backward_wide<D, H, 3, 384>(d, ws, parts, stage, sh, st);
+    return launch_backward_wide<D, H, 2, 512>(d, ws, parts, stage, sh, st);
 }
 cudaError_t launch_layernorm_backward(const cleave_layernorm_backward_t& d, float* ws, cudaStream_t st) {
     const uint32_t parts = layernorm_backward_parts(d.rows, d.cols);
     const uint64_t stage = (uint64_t)d.cols * (type_bytes(d.dy_type) + type_bytes(d.h_type) * (d.dres ? 2u : 1u));
-    const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && stage <= kRingMost && rows_wide(d.dy, d.lddy, d.dy_type) && rows_wide(d.h, d.ldh, d.h_type) &&
+    const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && stage * backward_shape(d.cols).rows <= kRingMost && rows_wide(d.dy, d.lddy, d.dy_type) && rows_wide(d.h, d.ldh, d.h_type) &&
                       rows_wide(d.dx, d.lddx, d.h_type) && (!d.dres || rows_wide(d.dres, d.lddres, d.h_type)) && (uintptr_t)d.w % 16 == 0;
     cudaError_t e = cudaSuccess;
     if (parts && wide) {
