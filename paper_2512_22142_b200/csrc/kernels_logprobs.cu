@@ -127,32 +127,61 @@ template <> struct Floor<__nv_bfloat16> {
     }
 };
 
+// which of a unit's scores reach a bar (bit i: score i): not below it, or with `tie` false above it; a NaN reaches every bar
+__device__ __forceinline__ uint32_t unit_hits(const uint4& w, float bar, bool tie, float) {
+    auto one = [&](uint32_t v, uint32_t bit) { const float x = __uint_as_float(v); return (tie ? x < bar : x <= bar) ? 0u : bit; };
+    return one(w.x, 1u) | one(w.y, 2u) | one(w.z, 4u) | one(w.w, 8u);
+}
+__device__ __forceinline__ uint32_t unit_hits(const uint4& w, float bar, bool tie, __nv_bfloat16) {
+    // (a bar is a bf16 value, or a little below one on the negative side: rounded towards it, it is reached by the same scores)
+    const __nv_bfloat162 b = __bfloat162bfloat162(__float2bfloat16_rz(bar));
+    auto two = [&](uint32_t v, uint32_t bits) {
+        const __nv_bfloat162 x = *reinterpret_cast<const __nv_bfloat162*>(&v);
+        return ~(tie ? __hlt2_mask(x, b) : __hle2_mask(x, b)) & bits;
+    };
+    const uint32_t m = two(w.x, 0x00020001u) | two(w.y, 0x00080004u) | two(w.z, 0x00200010u) | two(w.w, 0x00800040u);
+    return (m | m >> 16) & 0xFFu;
+}
+
 // ---- the best places -----------------------------------------------------------------------------------------
 constexpr uint32_t kRoom = 128;                  // candidates a warp collects before it cuts them to the best
 template <int T>
 struct TopRoom {
-    uint64_t room[T / 32][kRoom];
+    uint32_t room[T / 32][kRoom];                // places
     uint64_t pool[(T / 32 > kPartsMost ? T / 32 : kPartsMost) * CLEAVE_TOP_MOST];      // (each warp's best, or each part's)
-    uint64_t best[CLEAVE_TOP_MOST];
+    uint64_t best[CLEAVE_TOP_MOST], joined[CLEAVE_TOP_MOST];
     uint32_t pooled, held;
 };
-// the warp's n candidates cut to the best k, best first; returns how many there are
-__device__ __forceinline__ uint32_t cut(uint64_t* room, uint32_t n, uint32_t k) {
+// the warp's n places cut to those of the best k candidates, best first; returns how many there are, and in `last` the k-th candidate
+template <typename T>
+__device__ __forceinline__ uint32_t cut(const T* x, uint32_t* room, uint32_t n, uint32_t k, uint64_t& last) {
     const uint32_t lane = threadIdx.x & 31u;
     uint64_t c[kRoom / 32];
     uint32_t rank[kRoom / 32];
     __syncwarp();
 #pragma unroll
-    for (uint32_t i = 0; i < kRoom / 32; ++i) { c[i] = lane + 32 * i < n ? room[lane + 32 * i] : 0; rank[i] = 0; }
-    for (uint32_t j = 0; j < n; ++j) {
-        const uint64_t o = room[j];
-#pragma unroll
-        for (uint32_t i = 0; i < kRoom / 32; ++i) rank[i] += o > c[i];
+    for (uint32_t i = 0; i < kRoom / 32; ++i) {
+        const bool live = lane + 32 * i < n;
+        const uint32_t j = live ? room[lane + 32 * i] : 0u;
+        c[i] = live ? candidate(to_f32(x[j]), j) : 0;
+        rank[i] = 0;
     }
     __syncwarp();
 #pragma unroll
     for (uint32_t i = 0; i < kRoom / 32; ++i)
-        if (c[i] && rank[i] < k) room[rank[i]] = c[i];
+        for (uint32_t l = 0; l < 32; ++l) {
+            const uint64_t o = __shfl_sync(0xFFFFFFFFu, c[i], l);
+#pragma unroll
+            for (uint32_t e = 0; e < kRoom / 32; ++e) rank[e] += o > c[e];
+        }
+    last = 0;
+#pragma unroll
+    for (uint32_t i = 0; i < kRoom / 32; ++i) {
+        if (c[i] && rank[i] < k) room[rank[i]] = place_of(c[i]);
+        if (c[i] && rank[i] == k - 1) last = c[i];
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) last = max(last, (uint64_t)__shfl_xor_sync(0xFFFFFFFFu, last, o));
     __syncwarp();
     return min(n, k);
 }
@@ -167,6 +196,28 @@ __device__ __forceinline__ void pick(const uint64_t* pool, uint32_t n, uint64_t*
         uint32_t rank = 0;
 #pragma unroll 8
         for (uint32_t j = 0; j < n; ++j) rank += pool[j] > c;
+        if (rank < k) best[rank] = c;
+    }
+    __syncthreads();
+}
+
+// the best k of `lists` lists of k candidates each, best first with zeros at their ends, into best[0 .. k): a candidate's rank is its place in
+// its own list and, by bisection, the number of better ones in each other
+template <int T>
+__device__ __forceinline__ void merge(const uint64_t* pool, uint32_t lists, uint64_t* best, uint32_t k) {
+    if (threadIdx.x < k) best[threadIdx.x] = 0;
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < lists * k; e += T) {
+        const uint64_t c = pool[e];
+        const uint32_t own = e / k;
+        uint32_t rank = e - own * k;
+        if (!c) continue;
+        for (uint32_t l = 0; l < lists && rank < k; ++l) {
+            if (l == own) continue;
+            uint32_t lo = 0, hi = k;                             // how many of list l are better than c
+            while (lo < hi) { const uint32_t mid = (lo + hi) / 2; if (pool[l * k + mid] > c) lo = mid + 1; else hi = mid; }
+            rank += lo;
+        }
         if (rank < k) best[rank] = c;
     }
     __syncthreads();
@@ -226,7 +277,7 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
     uint32_t held = 0;
     uint64_t bar = 0;                                            // (candidates above it may be among the best)
     float bar_score = -INFINITY;
-    uint64_t* room = TOP ? top_room->room[warp] : nullptr;
+    uint32_t* room = TOP ? top_room->room[warp] : nullptr;
     auto raise_bar = [&](uint64_t b) {
         if (b > bar) { bar = b; bar_score = score_of(b); }
     };
@@ -238,18 +289,15 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
             if ((uint32_t)__syncthreads_count(mine >= (least | bit)) >= top) least |= bit;
         raise_bar((uint64_t)least << 32);                        // (below every candidate of that score)
     };
-    auto offer = [&](bool live, float v, uint32_t j) {           // one candidate a lane; all lanes of the warp
-        const uint64_t k = candidate(v, j);
-        const bool good = live && k > bar;
-        const uint32_t some = __ballot_sync(0xFFFFFFFFu, good);
-        if (!some) return;
-        if (good) room[held + __popc(some & ((1u << lane) - 1u))] = k;
-        held += __popc(some);
-        if (held > kRoom - 32) {
-            held = cut(room, held, top);
-            if (held == top) raise_bar(room[top - 1] - 1);
-            __syncwarp();
+    auto offer = [&](bool good, uint32_t j) {                    // one place a lane; all lanes of the warp
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, good), n = __popc(some);
+        if (held + n > kRoom) {
+            uint64_t last;
+            held = cut(x, room, held, top, last);
+            if (held == top) raise_bar(last - 1);
         }
+        if (good) room[held + __popc(some & ((1u << lane) - 1u))] = j;
+        held += n;
     };
     // (an equal score counts only where it can stand before the bar's place: a row of few different scores, masked ones most of
     // all, is not offered again and again)
@@ -257,23 +305,16 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
     auto reaches = [&](float v, bool tie) { return !(v < bar_score) && (tie || v != bar_score); };           // (a NaN reaches every bar)
     auto offer_step = [&](const Step& b, uint32_t step) {
         const uint32_t at = begin + step * kStride + tid;
-        uint32_t hits, n, all;
+        uint32_t hits;
         auto count = [&] {
             const bool tie = ties(step);
             hits = 0;
 #pragma unroll
             for (int q = 0; q < kSteps; ++q)
-                if (at + q * kScoreThreads < end)
-#pragma unroll
-                    for (int i = 0; i < V / 2; ++i) {
-                        const float2 p = pair_of(b.w[q], i, T());
-                        hits |= (reaches(p.x, tie) ? 1u << (q * V + 2 * i) : 0u) | (reaches(p.y, tie) ? 2u << (q * V + 2 * i) : 0u);
-                    }
-            n = __popc(hits);
-            all = __reduce_add_sync(0xFFFFFFFFu, n);
+                if (at + q * kScoreThreads < end) hits |= unit_hits(b.w[q], bar_score, tie, T()) << (q * V);
+            return __reduce_add_sync(0xFFFFFFFFu, (uint32_t)__popc(hits));
         };
-        count();
-        if (all > kRoom - 32 - held) {                           // more than the room takes: a bar from the step's own units first
+        if (count() > kRoom - held) {                            // more than the room takes: a bar from the step's own units first
             uint32_t least = 0, most[kSteps];
 #pragma unroll
             for (int q = 0; q < kSteps; ++q) most[q] = score_order(unit_max(b.w[q], T()));
@@ -287,36 +328,16 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
             raise_bar((uint64_t)least << 32);
             count();
         }
-        if (all <= kRoom - 32 - held) {
-            uint32_t to = n;
-#pragma unroll
-            for (uint32_t o = 1; o < 32; o <<= 1) { const uint32_t up = __shfl_up_sync(0xFFFFFFFFu, to, o); if (lane >= o) to += up; }
-            to += held - n;
-            if (hits)
-#pragma unroll
-                for (int q = 0; q < kSteps; ++q)
-#pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        if (hits >> (q * V + i) & 1u) {
-                            const float2 p = pair_of(b.w[q], i / 2, T());
-                            room[to++] = candidate(i & 1 ? p.y : p.x, head + (at + q * kScoreThreads) * V + i);
-                        }
-            held += all;
-            __syncwarp();
-        } else {
-#pragma unroll
-            for (int q = 0; q < kSteps; ++q)
-#pragma unroll
-                for (int i = 0; i < V; ++i) {
-                    const float2 p = pair_of(b.w[q], i / 2, T());
-                    offer(hits >> (q * V + i) & 1u, i & 1 ? p.y : p.x, head + (at + q * kScoreThreads) * V + i);
-                }
+        while (__any_sync(0xFFFFFFFFu, hits != 0)) {             // (once or twice)
+            const uint32_t e = (uint32_t)__ffs((int)hits) - 1, q = e / V;
+            offer(hits != 0, head + (at + q * kScoreThreads) * V + e - q * V);
+            hits &= hits - 1;
         }
     };
     if (TOP) {
         if (tid == 0) top_room->pooled = top_room->held = 0;
         common_bar(max_nan(lone, units_max<T>(even.w)));
-        offer(edge < cols, lone, edge);
+        offer(edge < cols && reaches(lone, true), edge);
     }
     if (edge < cols) {
         raise(a, lone, c);
@@ -374,9 +395,12 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
     if (TOP) {
         const uint32_t all = top_room->held;
         if (all > kRoom) common_bar(seen);                       // (worth its barriers where it leaves less to sort)
-        if (all > THREADS / 32 * CLEAVE_TOP_MOST) held = cut(room, held, top);      // more than the pool has room for
-        for (uint32_t i = lane; i < held; i += 32)
-            if (room[i] > bar) top_room->pool[atomicAdd(&top_room->pooled, 1u)] = room[i];     // (in any order: none are alike)
+        if (all > THREADS / 32 * CLEAVE_TOP_MOST) { uint64_t last; held = cut(x, room, held, top, last); }       // more than the pool has room for
+        __syncwarp();
+        for (uint32_t i = lane; i < held; i += 32) {
+            const uint64_t c = candidate(to_f32(x[room[i]]), room[i]);
+            if (c > bar) top_room->pool[atomicAdd(&top_room->pooled, 1u)] = c;       // (in any order: none are alike)
+        }
         __syncthreads();
         pick<THREADS>(top_room->pool, top_room->pooled, top_room->best, top);
     }
@@ -427,7 +451,7 @@ __global__ void __launch_bounds__(THREADS, TOP ? 1024 / THREADS : 1536 / THREADS
                 const uint32_t at = (uint32_t)__cvta_generic_to_shared(top_room.best);
                 for (uint32_t e = threadIdx.x; e < parts * d.top; e += THREADS) top_room.pool[e] = ld_dsmem_u64(mapa_shared(at, e / d.top) + (e % d.top) * 8);
                 __syncthreads();
-                pick<THREADS>(top_room.pool, parts * d.top, top_room.room[0], d.top);     // (its own `best` may still be read)
+                merge<THREADS>(top_room.pool, parts, top_room.joined, d.top);
             }
         }
         const Stats r = stats_of(a, d.scale, c);
@@ -437,7 +461,7 @@ __global__ void __launch_bounds__(THREADS, TOP ? 1024 / THREADS : 1536 / THREADS
             if (d.logp) d.logp[row] = token < 0 ? 0.f : (r.lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[token]), -r.lse));
         }
         if constexpr (TOP) {
-            const uint64_t* best = parts > 1 ? top_room.room[0] : top_room.best;
+            const uint64_t* best = parts > 1 ? top_room.joined : top_room.best;
             if (threadIdx.x < d.top) {
                 if (d.top_index) d.top_index[row * d.ldti + threadIdx.x] = (int32_t)place_of(best[threadIdx.x]);
                 if (d.top_values) d.top_values[row * d.ldtv + threadIdx.x] = r.lse == -INFINITY ? -INFINITY : fmaf(d.scale, score_of(best[threadIdx.x]), -r.lse);
