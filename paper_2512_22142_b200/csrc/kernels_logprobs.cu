@@ -152,38 +152,51 @@ struct TopRoom {
     uint64_t best[CLEAVE_TOP_MOST], joined[CLEAVE_TOP_MOST];
     uint32_t pooled, held;
 };
-// the warp's n places cut to those of the best k candidates, best first; returns how many there are, and in `last` the k-th candidate
+// Makes room: the warp's n places without those that the bar has passed by now or, where that leaves more than `enough`, those of the best
+// k candidates alone.  Returns how many there are; `last` becomes the k-th candidate where the best were taken, else 0.
 template <typename T>
-__device__ __forceinline__ uint32_t cut(const T* x, uint32_t* room, uint32_t n, uint32_t k, uint64_t& last) {
+__device__ __noinline__ uint32_t cut(const T* x, uint32_t* room, uint32_t n, uint32_t enough, uint32_t k, uint64_t bar, uint64_t& last) {
     const uint32_t lane = threadIdx.x & 31u;
     uint64_t c[kRoom / 32];
-    uint32_t rank[kRoom / 32];
+    uint32_t rank[kRoom / 32], kept = 0;
     __syncwarp();
 #pragma unroll
     for (uint32_t i = 0; i < kRoom / 32; ++i) {
         const bool live = lane + 32 * i < n;
         const uint32_t j = live ? room[lane + 32 * i] : 0u;
         c[i] = live ? candidate(to_f32(x[j]), j) : 0;
-        rank[i] = 0;
+        if (c[i] <= bar) c[i] = 0;
     }
     __syncwarp();
-#pragma unroll
-    for (uint32_t i = 0; i < kRoom / 32; ++i)
-        for (uint32_t l = 0; l < 32; ++l) {
-            const uint64_t o = __shfl_sync(0xFFFFFFFFu, c[i], l);
-#pragma unroll
-            for (uint32_t e = 0; e < kRoom / 32; ++e) rank[e] += o > c[e];
-        }
-    last = 0;
 #pragma unroll
     for (uint32_t i = 0; i < kRoom / 32; ++i) {
-        if (c[i] && rank[i] < k) room[rank[i]] = place_of(c[i]);
-        if (c[i] && rank[i] == k - 1) last = c[i];
+        const uint32_t some = __ballot_sync(0xFFFFFFFFu, c[i] != 0);
+        rank[i] = kept + __popc(some & ((1u << lane) - 1u));
+        kept += __popc(some);
+    }
+    last = 0;
+    if (kept > enough) {
+#pragma unroll
+        for (uint32_t i = 0; i < kRoom / 32; ++i) rank[i] = 0;
+#pragma unroll
+        for (uint32_t i = 0; i < kRoom / 32; ++i)
+            for (uint32_t l = 0; l < 32; ++l) {
+                const uint64_t o = __shfl_sync(0xFFFFFFFFu, c[i], l);
+#pragma unroll
+                for (uint32_t e = 0; e < kRoom / 32; ++e) rank[e] += o > c[e];
+            }
+#pragma unroll
+        for (uint32_t i = 0; i < kRoom / 32; ++i)
+            if (c[i] && rank[i] == k - 1) last = c[i];
+#pragma unroll
+        for (int o = 16; o; o >>= 1) last = max(last, (uint64_t)__shfl_xor_sync(0xFFFFFFFFu, last, o));
+        kept = min(kept, k);
     }
 #pragma unroll
-    for (int o = 16; o; o >>= 1) last = max(last, (uint64_t)__shfl_xor_sync(0xFFFFFFFFu, last, o));
+    for (uint32_t i = 0; i < kRoom / 32; ++i)
+        if (c[i] && rank[i] < kept) room[rank[i]] = place_of(c[i]);
     __syncwarp();
-    return min(n, k);
+    return kept;
 }
 // the best k of a pool of n (zeros do not count) into best[0 .. k), zeros behind them; all threads of the CTA
 template <int T>
@@ -272,7 +285,7 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
     Floor<T> floor;
     floor.set(0.f, far);
     // TOP.  When `top` threads have seen a score of at least v, nothing below v is among the best: the largest such v, to 16 bits, is
-    // the bar, found bit by bit from the threads' largest scores and raised each time the steps have doubled.  What reaches it goes to the
+    // the bar, found bit by bit from the threads' largest scores and raised each time there are four times as many steps.  What reaches it goes to the
     // warp's room; a room that would run over is cut to its best, the last of which is a bar of the warp's own.
     uint32_t held = 0;
     uint64_t bar = 0;                                            // (candidates above it may be among the best)
@@ -293,8 +306,8 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
         const uint32_t some = __ballot_sync(0xFFFFFFFFu, good), n = __popc(some);
         if (held + n > kRoom) {
             uint64_t last;
-            held = cut(x, room, held, top, last);
-            if (held == top) raise_bar(last - 1);
+            held = cut(x, room, held, kRoom - 32, top, bar, last);
+            if (last) raise_bar(last - 1);
         }
         if (good) room[held + __popc(some & ((1u << lane) - 1u))] = j;
         held += n;
@@ -373,7 +386,7 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
                 if (ENT) t2 = fma2(p2, e2, t2);
             }
         }
-        if (TOP && step && (step & (step + 1)) == 0 && step + 1 < steps) common_bar(a.m);          // behind the steps 1, 3, 7, ...
+        if (TOP && step && (step & (step + 1)) == 0 && ((step + 1) & 0x55555555u) && step + 1 < steps) common_bar(a.m);        // behind the steps 3, 15, 63, ...
     };
     for (uint32_t step = 0; step < steps; step += 2) {
         if (step + 1 < steps) fetch(odd, step + 1);
@@ -395,7 +408,7 @@ __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uin
     if (TOP) {
         const uint32_t all = top_room->held;
         if (all > kRoom) common_bar(seen);                       // (worth its barriers where it leaves less to sort)
-        if (all > THREADS / 32 * CLEAVE_TOP_MOST) { uint64_t last; held = cut(x, room, held, top, last); }       // more than the pool has room for
+        if (all > THREADS / 32 * CLEAVE_TOP_MOST) { uint64_t last; held = cut(x, room, held, CLEAVE_TOP_MOST, top, bar, last); }       // more than the pool has room for
         __syncwarp();
         for (uint32_t i = lane; i < held; i += 32) {
             const uint64_t c = candidate(to_f32(x[room[i]]), room[i]);
@@ -471,30 +484,34 @@ __global__ void __launch_bounds__(THREADS, TOP ? 1024 / THREADS : 1536 / THREADS
     if (parts > 1) cluster_arrive_wait();                        // no CTA leaves while another reads its shared memory
 }
 
-// CTAs a row: enough to fill the GPU a few times over, each with 16 KB of scores at least
-uint32_t row_parts(uint64_t rows, uint64_t row_bytes, int sms) {
+// CTAs a row: as many as it takes, at 512 threads each, to fill the SMs once, each with 16 KB of scores at least.  (More would each
+// look for places of their own: the 20 best of 292 x 128864 fp32 with 8 CTAs a row 84 us.)
+uint32_t row_parts(uint64_t rows, uint64_t row_bytes, int sms, uint32_t sm_threads) {
     uint32_t parts = 1;
-    while (parts < kPartsMost && rows * parts < (uint64_t)sms * 8 && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
+    while (parts < kPartsMost && rows * parts * 512 < (uint64_t)sms * sm_threads && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
     return parts;
 }
-// few: less than two CTAs an SM, which then have more threads (16 x 128000 fp32 8 us against 10 with 256); many rows go to
-// CTAs of 128, whose joins cost less (8192 x 50257 with entropy 143 us against 152 with 256).
-struct RowGrid { dim3 cluster, grid; bool few; };
-RowGrid row_grid(uint64_t rows, uint64_t row_bytes, int sms) {
-    const uint32_t parts = row_parts(rows, row_bytes, sms), y = (uint32_t)std::min<uint64_t>(rows, 65535);
-    return {dim3(parts), dim3(parts, y, (unsigned)((rows + y - 1) / y)), rows * parts < 2 * (uint64_t)sms && row_bytes / parts >= 16 * 1024};
+// Threads: as many as fill the SMs (16 x 128000 fp32 8 us with 512, 10 with 256); many rows go to CTAs of 128, whose joins cost
+// less (8192 x 50257 with entropy 143 us against 152 with 256).
+struct RowGrid { dim3 cluster, grid; uint32_t threads; };
+RowGrid row_grid(uint64_t rows, uint64_t row_bytes, int sms, uint32_t sm_threads) {       // sm_threads: what an SM holds of the kernel
+    const uint32_t parts = row_parts(rows, row_bytes, sms, sm_threads), y = (uint32_t)std::min<uint64_t>(rows, 65535);
+    const uint64_t held = (uint64_t)sms * sm_threads / (rows * parts);       // threads a CTA if all are to run at once
+    const uint32_t least = (uint32_t)std::min<uint64_t>(row_bytes / parts / 32, 512);        // two units each at least
+    const uint64_t most = std::min<uint64_t>(held, least);
+    return {dim3(parts), dim3(parts, y, (unsigned)((rows + y - 1) / y)), most >= 512 ? 512u : (most >= 256 ? 256u : 128u)};
 }
 template <typename T, bool ENT, bool TOP>
 cudaError_t launch_logprobs_kernel(const cleave_logprobs_t& d, const RowGrid& g, cudaStream_t st) {
-    return g.few ? launch_chained_clusters(logprobs_kernel<T, ENT, TOP, 512>, g.cluster, g.grid, 512, 0, st, d)
-                 : launch_chained_clusters(logprobs_kernel<T, ENT, TOP, 128>, g.cluster, g.grid, 128, 0, st, d);
+    auto kernel = g.threads == 512 ? logprobs_kernel<T, ENT, TOP, 512> : (g.threads == 256 ? logprobs_kernel<T, ENT, TOP, 256> : logprobs_kernel<T, ENT, TOP, 128>);
+    return launch_chained_clusters(kernel, g.cluster, g.grid, g.threads, 0, st, d);
 }
 template <typename T, bool ENT>
 cudaError_t launch_logprobs_types(const cleave_logprobs_t& d, const RowGrid& g, cudaStream_t st) {
     return d.top ? launch_logprobs_kernel<T, ENT, true>(d, g, st) : launch_logprobs_kernel<T, ENT, false>(d, g, st);
 }
 cudaError_t launch_logprobs(const cleave_logprobs_t& d, int sms, cudaStream_t st) {
-    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms);
+    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms, d.top ? 1024 : 1536);
     if (d.x_type == CLEAVE_T_F32) return d.entropy ? launch_logprobs_types<float, true>(d, g, st) : launch_logprobs_types<float, false>(d, g, st);
     return d.entropy ? launch_logprobs_types<__nv_bfloat16, true>(d, g, st) : launch_logprobs_types<__nv_bfloat16, false>(d, g, st);
 }
@@ -709,10 +726,11 @@ __global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const 
 }
 template <typename T>
 cudaError_t launch_distill_types(const cleave_distill_t& d, const RowGrid& g, cudaStream_t st) {
-    return g.few ? launch_chained_clusters(distill_kernel<T, 512>, g.cluster, g.grid, 512, 0, st, d) : launch_chained_clusters(distill_kernel<T, 128>, g.cluster, g.grid, 128, 0, st, d);
+    auto kernel = g.threads == 512 ? distill_kernel<T, 512> : (g.threads == 256 ? distill_kernel<T, 256> : distill_kernel<T, 128>);
+    return launch_chained_clusters(kernel, g.cluster, g.grid, g.threads, 0, st, d);
 }
 cudaError_t launch_distill(const cleave_distill_t& d, int sms, cudaStream_t st) {
-    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms);
+    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms, 1536);
     return d.x_type == CLEAVE_T_F32 ? launch_distill_types<float>(d, g, st) : launch_distill_types<__nv_bfloat16>(d, g, st);
 }
 template <typename X, typename D, bool WIDE>
