@@ -8,6 +8,7 @@
 //   own    any alignment, up to 8192 columns: neighbouring threads own neighbouring columns, held in registers.
 //   any    what is left: the row is taken again in each pass (it stays in L1 / L2).
 #include <algorithm>
+#include <initializer_list>
 #include <type_traits>
 
 #include "rows.cuh"
@@ -17,7 +18,10 @@ namespace cleave {
 
 // 8 of a vector of weights or biases of columns, or `fill` where there is none
 __device__ __forceinline__ void load_vector8(const void* p, uint32_t type, uint32_t col, float fill, F2 (&v)[4]) {
-    if (type == CLEAVE_T_F32) {
+    if (type != CLEAVE_T_NONE && (((uintptr_t)p + (uint64_t)col * (type == CLEAVE_T_F32 ? 4 : 2)) & 15u)) {       // not on 16 bytes
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = f2(load_as(p, type, col + 2 * i), load_as(p, type, col + 2 * i + 1));
+    } else if (type == CLEAVE_T_F32) {
         Raw8<float> r;
         const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + col);
         r.w[0] = q[0]; r.w[1] = q[1];
@@ -32,6 +36,38 @@ __device__ __forceinline__ void load_vector8(const void* p, uint32_t type, uint3
     }
 }
 __device__ __forceinline__ float sum_of(F2 a) { const float2 h = halves(a); return h.x + h.y; }
+
+// Where the 16-byte lines of a row begin: column (unit - (at + row step) % unit) % unit, alike in all operands.  Rows of one length that
+// lie side by side (or at one distance) in all of them agree whatever that length is; what is before the first line and behind the
+// last whole group of 8 columns, less than 8 each, goes to single threads.
+struct Lines {
+    uint32_t at, step, unit;
+    __device__ __forceinline__ uint32_t head(uint64_t row, uint32_t cols) const { return min(cols, (unit - (at + (uint32_t)(row % unit) * step) % unit) % unit); }
+};
+struct Operand { const void* p; uint64_t ld; uint32_t type; };
+static bool lines_agree(std::initializer_list<Operand> operands, Lines& lines) {
+    lines = {0, 0, 0};
+    for (const bool narrow : {true, false})                      // operands of 1 or 2 bytes say more than those of 4
+        for (const Operand& o : operands)
+            if (o.p && !lines.unit && narrow == (o.type != CLEAVE_T_F32)) {
+                lines.unit = narrow ? 8 : 4;
+                lines.at = (uint32_t)((uintptr_t)o.p / type_bytes(o.type) % lines.unit);
+                lines.step = (uint32_t)(o.ld % lines.unit);
+            }
+    for (const Operand& o : operands) {
+        if (!o.p) continue;
+        const uint32_t unit = o.type == CLEAVE_T_F32 ? 4 : 8;
+        if (((uintptr_t)o.p / type_bytes(o.type) - lines.at) % unit || (o.ld - lines.step) % unit) return false;
+    }
+    return true;
+}
+// the column that thread `tid` of a row has to itself, or none (`cols`)
+__device__ __forceinline__ uint32_t edge_column(uint32_t tid, uint32_t head, uint32_t tail, uint32_t cols) {
+    if (tid < head) return tid;
+    return tid >= 8u && tid - 8u < tail ? cols - tail + (tid - 8u) : cols;
+}
+template <typename T> __device__ __forceinline__ void store_one(T* p, float v) { *p = from_f32<T>(v); }
+__device__ __forceinline__ void store_one(uint8_t* p, float v) { *p = e4m3_nearest(v); }
 
 // ---- forward, any shape ------------------------------------------------------------------------------
 __global__ void __launch_bounds__(kRowThreads) layernorm_any_kernel(const __grid_constant__ cleave_layernorm_t d) {
@@ -130,22 +166,23 @@ __global__ void __launch_bounds__(T) layernorm_own_kernel(const __grid_constant_
 // registers hold no weights, 133); 8 warps with a row each, all registers theirs (8192 x 768 17.0 us; a warp's row at a time without a ring 18.2).
 constexpr int row_warps(int V) { return V <= 2 ? 24 : 16; }
 template <typename X, typename R, typename Y, int V, bool WARP, int T>
-__global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm_wide_kernel(const __grid_constant__ cleave_layernorm_t d, uint32_t stages) {
+__global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm_wide_kernel(const __grid_constant__ cleave_layernorm_t d, uint32_t stages, const Lines lines) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float parts[3][32];
     begin_chained();
     constexpr bool RES = !(sizeof(R) == 1), CODES = sizeof(Y) == 1;
     constexpr uint32_t BX = Bytes8<X>::value, BR = Bytes8<R>::value;
-    const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
+    const uint32_t tid = threadIdx.x, nt = blockDim.x;
     const uint64_t first = WARP ? (uint64_t)blockIdx.x * blockDim.y + threadIdx.y : blockIdx.x;
-    const uint64_t stride = WARP ? (uint64_t)gridDim.x * blockDim.y : gridDim.x;
-    const uint32_t off_r = groups * BX, stage_bytes = off_r + groups * BR;
+    const uint64_t stride = WARP ? (uint64_t)gridDim.x * blockDim.y : gridDim.x;         // (whole units of rows where rows differ: one head for all)
+    const uint32_t head = lines.head(first, d.cols), groups = (d.cols - head) / 8, edge = edge_column(tid, head, d.cols - head - groups * 8, d.cols);
+    const uint32_t off_r = d.cols / 8 * BX, stage_bytes = off_r + d.cols / 8 * BR;
     const float inv_cols = 1.f / (float)d.cols;
     bool live[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) live[v] = tid + v * nt < groups;
-    const uint8_t* px = reinterpret_cast<const uint8_t*>(static_cast<const X*>(d.x) + first * d.ldx) + tid * BX;
-    const uint8_t* pr = reinterpret_cast<const uint8_t*>(d.r) + (RES ? first * d.ldr * (BR / 8) + tid * BR : 0);
+    const uint8_t* px = reinterpret_cast<const uint8_t*>(static_cast<const X*>(d.x) + first * d.ldx + head) + tid * BX;
+    const uint8_t* pr = reinterpret_cast<const uint8_t*>(d.r) + (RES ? (first * d.ldr + head) * (BR / 8) + tid * BR : 0);
     const uint64_t step_x = stride * d.ldx * (BX / 8), step_r = stride * d.ldr * (BR / 8);
     const uint8_t* mine = ring + (WARP ? threadIdx.y * stages * stage_bytes : 0u);
     const uint32_t slot = (uint32_t)__cvta_generic_to_shared(mine);
@@ -170,7 +207,17 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
     F2 w[V][4], b[V][4];
 #pragma unroll
     for (int v = 0; v < V; ++v)
-        if (live[v]) { load_vector8(d.w, d.w_type, (tid + v * nt) * 8, 1.f, w[v]); load_vector8(d.b, d.b_type, (tid + v * nt) * 8, 0.f, b[v]); }
+        if (live[v]) { load_vector8(d.w, d.w_type, head + (tid + v * nt) * 8, 1.f, w[v]); load_vector8(d.b, d.b_type, head + (tid + v * nt) * 8, 0.f, b[v]); }
+    // the thread's single column: its weight and bias, and the next row's value
+    const float edge_w = edge < d.cols && d.w ? load_as(d.w, d.w_type, edge) : 1.f, edge_b = edge < d.cols && d.b ? load_as(d.b, d.b_type, edge) : 0.f;
+    float next_edge = 0.f;
+    auto ask_edge = [&](uint64_t row) {
+        if (edge < d.cols && row < d.rows) {
+            next_edge = to_f32(static_cast<const X*>(d.x)[row * d.ldx + edge]);
+            if constexpr (RES) next_edge += to_f32(static_cast<const R*>(d.r)[row * d.ldr + edge]);
+        }
+    };
+    ask_edge(first);
     auto join = [&](float v, float* p) {                         // sum over the row's threads
         v = warp_sum(v);
         if constexpr (!WARP) {
@@ -180,8 +227,8 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
         }
         return v;
     };
-    Y* py = static_cast<Y*>(d.y) + first * d.ldy + tid * 8;
-    R* ph = RES && d.h ? static_cast<R*>(d.h) + first * d.ldh + tid * 8 : nullptr;
+    Y* py = static_cast<Y*>(d.y) + first * d.ldy + head + tid * 8;
+    R* ph = RES && d.h ? static_cast<R*>(d.h) + first * d.ldh + head + tid * 8 : nullptr;
     uint32_t at = 0;
     for (uint64_t row = first; row < d.rows; row += stride) {
         F2 h[V][4];
@@ -201,7 +248,13 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum = add2(sum, h[v][i]);
         }
-        const float mean = join(sum_of(sum), parts[0]) * inv_cols;
+        float lone = next_edge;
+        if (edge < d.cols) {
+            if constexpr (RES) if (d.h) store_one(static_cast<R*>(d.h) + row * d.ldh + edge, lone);
+            ask_edge(row + stride);
+        }
+        const float mean = join(sum_of(sum) + lone, parts[0]) * inv_cols;
+        if (edge < d.cols) lone -= mean;
         fetch(at);                                               // (this thread has read its groups of this stage)
         at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
 #pragma unroll
@@ -210,12 +263,13 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
 #pragma unroll
             for (int i = 0; i < 4; ++i) { h[v][i] = add2(h[v][i], f2(-mean, -mean)); squares = fma2(h[v][i], h[v][i], squares); }
         }
-        const float rstd = rsqrtf(fmaf(join(sum_of(squares), parts[1]), inv_cols, d.eps));
+        const float rstd = rsqrtf(fmaf(join(fmaf(lone, lone, sum_of(squares)), parts[1]), inv_cols, d.eps));
         if (tid == 0) {
             if (d.mean) d.mean[row] = mean;
             if (d.rstd) d.rstd[row] = rstd;
         }
-        float top = 0.f;
+        if (edge < d.cols) lone = fmaf(lone * rstd, edge_w, edge_b);
+        float top = fabsf(lone);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             if (!live[v]) continue;
@@ -242,7 +296,9 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
                 for (int i = 0; i < 4; ++i) h[v][i] = mul2(h[v][i], f2(sc.y, sc.y));
                 store8(py + v * nt * 8, h[v]);
             }
+            lone *= sc.y;
         }
+        if (edge < d.cols) store_one(static_cast<Y*>(d.y) + row * d.ldy + edge, lone);
         py += stride * d.ldy;
         if (RES && ph) ph += stride * d.ldh;
     }
@@ -254,7 +310,7 @@ constexpr uint32_t kRingMost = 208 * 1024;     // of all rings of a CTA
 constexpr uint32_t kWarpRing = 26 * 1024;       // of one of a CTA's eight warps
 
 template <typename X, typename R, typename Y, int V, bool WARP, int T>
-cudaError_t launch_wide(const cleave_layernorm_t& d, uint32_t threads, int sms, cudaStream_t st) {
+cudaError_t launch_wide(const cleave_layernorm_t& d, uint32_t threads, const Lines& lines, int sms, cudaStream_t st) {
     auto kernel = layernorm_wide_kernel<X, R, Y, V, WARP, T>;
     const uint32_t stage = d.cols / 8 * (Bytes8<X>::value + Bytes8<R>::value);
     static SmemLimit limit;
@@ -262,41 +318,43 @@ cudaError_t launch_wide(const cleave_layernorm_t& d, uint32_t threads, int sms, 
     if (e != cudaSuccess) return e;
     if (WARP) {                                                  // a ring a warp
         const uint32_t stages = std::max(1u, std::min(4u, kWarpRing / stage));
-        return launch_chained(kernel, (unsigned)std::min<uint64_t>((d.rows + 7) / 8, (uint64_t)sms), dim3(32, 8), 8 * stages * stage, st, d, stages);
+        return launch_chained(kernel, (unsigned)std::min<uint64_t>((d.rows + 7) / 8, (uint64_t)sms), dim3(32, 8), 8 * stages * stage, st, d, stages, lines);
     }
     const uint32_t stages = std::max(1u, std::min(4u, kRingBytes / stage)), smem = stage * stages;
     // CTAs that fit an SM by shared memory and registers; each walks the rows in steps of the grid
     const uint32_t fit = std::max(1u, std::min(224u * 1024u / (smem + 2048u), (uint32_t)row_warps(V) * 32u / threads));
-    return launch_chained(kernel, (unsigned)std::min((uint64_t)d.rows, (uint64_t)sms * fit), threads, smem, st, d, stages);
+    uint64_t ctas = (uint64_t)sms * fit;
+    if (lines.step) ctas = std::max<uint64_t>(8, ctas / 8 * 8);  // a CTA's rows begin alike
+    return launch_chained(kernel, (unsigned)std::min((uint64_t)d.rows, ctas), threads, smem, st, d, stages, lines);
 }
 template <typename X, typename R, typename Y>
-cudaError_t launch_sizes(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
+cudaError_t launch_sizes(const cleave_layernorm_t& d, const Lines& lines, int sms, cudaStream_t st) {
     const uint32_t groups = d.cols / 8;
     if (d.cols <= kWarpRowCols) {
-        if (groups <= 32) return launch_wide<X, R, Y, 1, true, 256>(d, 32, sms, st);
-        if (groups <= 64) return launch_wide<X, R, Y, 2, true, 256>(d, 32, sms, st);
-        if (groups <= 96) return launch_wide<X, R, Y, 3, true, 256>(d, 32, sms, st);
-        return launch_wide<X, R, Y, 4, true, 256>(d, 32, sms, st);
+        if (groups <= 32) return launch_wide<X, R, Y, 1, true, 256>(d, 32, lines, sms, st);
+        if (groups <= 64) return launch_wide<X, R, Y, 2, true, 256>(d, 32, lines, sms, st);
+        if (groups <= 96) return launch_wide<X, R, Y, 3, true, 256>(d, 32, lines, sms, st);
+        return launch_wide<X, R, Y, 4, true, 256>(d, 32, lines, sms, st);
     }
-    if (groups <= 512) return launch_wide<X, R, Y, 2, false, 256>(d, (groups + 63) / 64 * 32, sms, st);
+    if (groups <= 512) return launch_wide<X, R, Y, 2, false, 256>(d, (groups + 63) / 64 * 32, lines, sms, st);
     const uint32_t threads = (groups + 127) / 128 * 32;
-    if (groups <= 1024) return launch_wide<X, R, Y, 4, false, 256>(d, threads, sms, st);
-    return launch_wide<X, R, Y, 4, false, 512>(d, threads, sms, st);
+    if (groups <= 1024) return launch_wide<X, R, Y, 4, false, 256>(d, threads, lines, sms, st);
+    return launch_wide<X, R, Y, 4, false, 512>(d, threads, lines, sms, st);
 }
 template <typename X, typename R>
-cudaError_t launch_out(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
-    if (d.y_type == CLEAVE_T_E4M3) return launch_sizes<X, R, uint8_t>(d, sms, st);
-    return d.y_type == CLEAVE_T_F32 ? launch_sizes<X, R, float>(d, sms, st) : launch_sizes<X, R, __nv_bfloat16>(d, sms, st);
+cudaError_t launch_out(const cleave_layernorm_t& d, const Lines& lines, int sms, cudaStream_t st) {
+    if (d.y_type == CLEAVE_T_E4M3) return launch_sizes<X, R, uint8_t>(d, lines, sms, st);
+    return d.y_type == CLEAVE_T_F32 ? launch_sizes<X, R, float>(d, lines, sms, st) : launch_sizes<X, R, __nv_bfloat16>(d, lines, sms, st);
 }
 template <typename X>
-cudaError_t launch_residual(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
-    if (!d.r) return launch_out<X, NoRes>(d, sms, st);
-    return d.r_type == CLEAVE_T_F32 ? launch_out<X, float>(d, sms, st) : launch_out<X, __nv_bfloat16>(d, sms, st);
+cudaError_t launch_residual(const cleave_layernorm_t& d, const Lines& lines, int sms, cudaStream_t st) {
+    if (!d.r) return launch_out<X, NoRes>(d, lines, sms, st);
+    return d.r_type == CLEAVE_T_F32 ? launch_out<X, float>(d, lines, sms, st) : launch_out<X, __nv_bfloat16>(d, lines, sms, st);
 }
 cudaError_t launch_layernorm(const cleave_layernorm_t& d, int sms, cudaStream_t st) {
-    const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && rows_wide(d.x, d.ldx, d.x_type) && rows_wide(d.y, d.ldy, d.y_type) && (!d.r || rows_wide(d.r, d.ldr, d.r_type)) &&
-                      (!d.h || rows_wide(d.h, d.ldh, d.r_type)) && (uintptr_t)d.w % 16 == 0 && (uintptr_t)d.b % 16 == 0;
-    if (wide) return d.x_type == CLEAVE_T_F32 ? launch_residual<float>(d, sms, st) : launch_residual<__nv_bfloat16>(d, sms, st);
+    Lines lines;
+    const bool wide = d.cols >= 64 && d.cols <= 16384 && lines_agree({{d.x, d.ldx, d.x_type}, {d.r, d.ldr, d.r_type}, {d.h, d.ldh, d.r_type}, {d.y, d.ldy, d.y_type}}, lines);
+    if (wide) return d.x_type == CLEAVE_T_F32 ? launch_residual<float>(d, lines, sms, st) : launch_residual<__nv_bfloat16>(d, lines, sms, st);
     if (d.cols <= kOwnCols) {
         const uint32_t threads = own_threads(d.cols);
         const unsigned ctas = (unsigned)std::min<uint64_t>(d.rows, (uint64_t)sms * std::min(24u, 1024u / threads));
@@ -422,27 +480,29 @@ __global__ void __launch_bounds__(T) layernorm_backward_own_kernel(const __grid_
 // V groups of 8 columns a thread, blockDim.y rows at a time, each with a ring of the next rows of (dy, h, dres) in shared memory; the
 // weights (where registers hold them) and the shares of dw and db stay in registers over all rows, and the
 // CTA's rows add theirs at the end.
-template <typename D, typename H, int V, int T>
-__global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws, uint32_t stages) {
+// EDGES: rows that do not begin or end with a line (their threads hold more: 16384 x 5120 152 us in place of 127).
+template <typename D, typename H, int V, int T, bool EDGES>
+__global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws, uint32_t stages, const Lines lines) {
     extern __shared__ __align__(16) uint8_t rings[];
     __shared__ float buffers[16][2][2][32];
     begin_chained();
     constexpr uint32_t BD = Bytes8<D>::value, BH = Bytes8<H>::value;
     constexpr bool KEEP = V < 4 || (V == 4 && T < 512) || (V == 5 && sizeof(H) == 2);
     float (&parts)[2][2][32] = buffers[threadIdx.y];
-    const uint32_t groups = d.cols / 8, tid = threadIdx.x, nt = blockDim.x;
+    const uint32_t tid = threadIdx.x, nt = blockDim.x;
     const bool res = d.dres != nullptr;
-    const uint32_t off_h = groups * BD, off_res = off_h + groups * BH, stage_bytes = off_res + (res ? groups * BH : 0u);
+    const uint64_t first = blockIdx.x + (uint64_t)gridDim.x * threadIdx.y, stride = (uint64_t)gridDim.x * blockDim.y;        // (whole units of rows where rows differ)
+    const uint32_t head = EDGES ? lines.head(first, d.cols) : 0u, groups = (d.cols - head) / 8, edge = EDGES ? edge_column(tid, head, d.cols - head - groups * 8, d.cols) : d.cols;
+    const uint32_t off_h = d.cols / 8 * BD, off_res = off_h + d.cols / 8 * BH, stage_bytes = off_res + (res ? d.cols / 8 * BH : 0u);
     uint8_t* ring = rings + threadIdx.y * stages * stage_bytes;
     const uint32_t ring_base = (uint32_t)__cvta_generic_to_shared(ring);
     const float inv_cols = 1.f / (float)d.cols;
-    const uint64_t first = blockIdx.x + (uint64_t)gridDim.x * threadIdx.y, stride = (uint64_t)gridDim.x * blockDim.y;
     bool live[V];
 #pragma unroll
     for (int v = 0; v < V; ++v) live[v] = tid + v * nt < groups;
-    const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + first * d.lddy) + tid * BD;
-    const uint8_t* ph = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.h) + first * d.ldh) + tid * BH;
-    const uint8_t* pr = res ? reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.dres) + first * d.lddres) + tid * BH : nullptr;
+    const uint8_t* pd = reinterpret_cast<const uint8_t*>(static_cast<const D*>(d.dy) + first * d.lddy + head) + tid * BD;
+    const uint8_t* ph = reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.h) + first * d.ldh + head) + tid * BH;
+    const uint8_t* pr = res ? reinterpret_cast<const uint8_t*>(static_cast<const H*>(d.dres) + first * d.lddres + head) + tid * BH : nullptr;
     const uint64_t step_d = stride * d.lddy * (BD / 8), step_h = stride * d.ldh * (BH / 8), step_r = stride * d.lddres * (BH / 8);
     uint64_t ahead = first;
     auto fetch = [&](uint32_t at) {
@@ -469,13 +529,24 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
     F2 w[KEEP ? V : 1][4], dw[V][4], db[V][4];
     if constexpr (KEEP) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) if (live[v]) load_vector8(d.w, d.w_type, (tid + v * nt) * 8, 1.f, w[v]);
+        for (int v = 0; v < V; ++v) if (live[v]) load_vector8(d.w, d.w_type, head + (tid + v * nt) * 8, 1.f, w[v]);
     }
+    // the thread's single column: its weight, its shares, and the next row's values
+    const float edge_w = EDGES && edge < d.cols && d.w ? load_as(d.w, d.w_type, edge) : 1.f;
+    float edge_dw = 0.f, edge_db = 0.f, next_dy = 0.f, next_h = 0.f, next_res = 0.f;
+    auto ask_edge = [&](uint64_t row) {
+        if (EDGES && edge < d.cols && row < d.rows) {
+            next_dy = to_f32(static_cast<const D*>(d.dy)[row * d.lddy + edge]);
+            next_h = to_f32(static_cast<const H*>(d.h)[row * d.ldh + edge]);
+            if (res) next_res = to_f32(static_cast<const H*>(d.dres)[row * d.lddres + edge]);
+        }
+    };
+    ask_edge(first);
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
         for (int i = 0; i < 4; ++i) dw[v][i] = db[v][i] = f2(0.f, 0.f);
-    H* pdx = static_cast<H*>(d.dx) + first * d.lddx + tid * 8;
+    H* pdx = static_cast<H*>(d.dx) + first * d.lddx + head + tid * 8;
     uint32_t it = 0, at = 0;
     float next_rstd = first < d.rows ? d.rstd[first] : 0.f, next_mean = first < d.rows ? d.mean[first] : 0.f;
     for (uint64_t row = first; row < d.rows; row += stride, ++it) {
@@ -495,7 +566,7 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
             if (res) rr[v] = *reinterpret_cast<const Raw8<H>*>(stage + off_res + g * BH);
             F2 h[4];
             unpack8(rh[v], h);
-            if constexpr (!KEEP) load_vector8(d.w, d.w_type, g * 8, 1.f, w[0]);
+            if constexpr (!KEEP) load_vector8(d.w, d.w_type, head + g * 8, 1.f, w[0]);
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const F2 c = add2(h[i], mean2);
@@ -506,7 +577,16 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
                 dots = fma2(q[v][i], c, dots);
             }
         }
-        const float2 both = row_sums(sum_of(sums), sum_of(dots), parts[it & 1]);
+        float edge_q = 0.f, edge_c = 0.f, edge_res = 0.f;
+        if (EDGES && edge < d.cols) {
+            edge_c = next_h - mean;
+            edge_res = next_res;
+            edge_dw = fmaf(next_dy * rstd, edge_c, edge_dw);
+            edge_db += next_dy;
+            edge_q = next_dy * edge_w;
+            ask_edge(row + stride);
+        }
+        const float2 both = row_sums(sum_of(sums) + edge_q, fmaf(edge_q, edge_c, sum_of(dots)), parts[it & 1]);
         fetch(at);
         at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
         // dx = rstd q - rstd mean(q) - (rstd^3 mean(q (h - mean))) (h - mean)
@@ -526,41 +606,54 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
             }
             store8(pdx + v * nt * 8, dx);
         }
+        if (EDGES && edge < d.cols) store_one(static_cast<H*>(d.dx) + row * d.lddx + edge, fmaf(-along, edge_c, fmaf(rstd, edge_q, -shift)) + edge_res);
         pdx += stride * d.lddx;
     }
     if (!d.dw && !d.db) return;
+    // (a row's columns may begin elsewhere than another's: the shares meet column by column)
+    auto put = [&](float* to) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            if (!live[v]) continue;
+            const uint32_t j = head + (tid + v * nt) * 8;
+            if (((uintptr_t)(to + j) | ((uint64_t)d.cols * 4)) % 16 == 0) {
+                store8(to + j, dw[v]);
+                store8(to + d.cols + j, db[v]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 a = halves(dw[v][i]), b = halves(db[v][i]);
+                    to[j + 2 * i] = a.x; to[j + 2 * i + 1] = a.y;
+                    to[d.cols + j + 2 * i] = b.x; to[d.cols + j + 2 * i + 1] = b.y;
+                }
+            }
+        }
+        if (EDGES && edge < d.cols) { to[edge] = edge_dw; to[d.cols + edge] = edge_db; }
+    };
     if (blockDim.y > 1) {                                        // the rows' shares, in order
         float* other = reinterpret_cast<float*>(rings);
         cp_async_wait<0>();
         __syncthreads();
-        if (threadIdx.y)
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (live[v]) {
-                    store8(other + ((uint64_t)(threadIdx.y - 1) * 2) * d.cols + (tid + v * nt) * 8, dw[v]);
-                    store8(other + ((uint64_t)(threadIdx.y - 1) * 2 + 1) * d.cols + (tid + v * nt) * 8, db[v]);
-                }
+        if (threadIdx.y) put(other + (uint64_t)(threadIdx.y - 1) * 2 * d.cols);
         __syncthreads();
         if (threadIdx.y) return;
-        for (uint32_t y = 0; y + 1 < blockDim.y; ++y)
+        for (uint32_t y = 0; y + 1 < blockDim.y; ++y) {
+            const float* from = other + (uint64_t)y * 2 * d.cols;
 #pragma unroll
-            for (int v = 0; v < V; ++v)
-                if (live[v]) {
-                    F2 t[4];
-                    unpack8(*reinterpret_cast<const Raw8<float>*>(other + (uint64_t)y * 2 * d.cols + (tid + v * nt) * 8), t);
+            for (int v = 0; v < V; ++v) {
+                if (!live[v]) continue;
+                const float* a = from + head + (tid + v * nt) * 8;
+                const float* b = a + d.cols;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) dw[v][i] = add2(dw[v][i], t[i]);
-                    unpack8(*reinterpret_cast<const Raw8<float>*>(other + ((uint64_t)y * 2 + 1) * d.cols + (tid + v * nt) * 8), t);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) db[v][i] = add2(db[v][i], t[i]);
+                for (int i = 0; i < 4; ++i) {
+                    dw[v][i] = add2(dw[v][i], f2(a[2 * i], a[2 * i + 1]));
+                    db[v][i] = add2(db[v][i], f2(b[2 * i], b[2 * i + 1]));
                 }
-    }
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (live[v]) {
-            store8(ws + (uint64_t)blockIdx.x * 2 * d.cols + (tid + v * nt) * 8, dw[v]);
-            store8(ws + ((uint64_t)blockIdx.x * 2 + 1) * d.cols + (tid + v * nt) * 8, db[v]);
+            }
+            if (EDGES && edge < d.cols) { edge_dw += from[edge]; edge_db += from[d.cols + edge]; }
         }
+    }
+    put(ws + (uint64_t)blockIdx.x * 2 * d.cols);
 }
 
 // out[j] = sum over the parts of ws[part][j], 0 <= j < cols for dw and behind them for db, each in a fixed order: 32 columns
@@ -582,33 +675,40 @@ __global__ void __launch_bounds__(1024) layernorm_sum_parts_kernel(const float* 
     if (lane == 0 && blockIdx.x * 32u + warp < cols) out[blockIdx.x * 32u + warp] = v;
 }
 
-template <typename D, typename H, int V, int T>
-cudaError_t launch_backward_wide(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, const Shape& sh, cudaStream_t st) {
-    auto kernel = layernorm_backward_wide_kernel<D, H, V, T>;
+template <typename D, typename H, int V, int T, bool EDGES>
+cudaError_t launch_backward_wide(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, const Shape& sh, const Lines& lines, cudaStream_t st) {
+    auto kernel = layernorm_backward_wide_kernel<D, H, V, T, EDGES>;
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
     if (e != cudaSuccess) return e;
     const uint32_t stages = std::max(1u, std::min(4u, kRingMost / sh.rows / stage)), joined = (sh.rows - 1) * 2 * d.cols * 4;
-    return launch_chained(kernel, parts, dim3(sh.threads, sh.rows), std::max(stage * stages * sh.rows, joined), st, d, ws, stages);
+    return launch_chained(kernel, parts, dim3(sh.threads, sh.rows), std::max(stage * stages * sh.rows, joined), st, d, ws, stages, lines);
+}
+template <typename D, typename H, bool EDGES>
+cudaError_t launch_backward_edges(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, const Lines& lines, cudaStream_t st) {
+    const Shape sh = backward_shape(d.cols);
+    if (sh.threads == 512) return launch_backward_wide<D, H, 4, 512, EDGES>(d, ws, parts, stage, sh, lines, st);
+    if (sh.groups == 5) return launch_backward_wide<D, H, 5, 256, EDGES>(d, ws, parts, stage, sh, lines, st);
+    if (sh.groups == 4) return launch_backward_wide<D, H, 4, 256, EDGES>(d, ws, parts, stage, sh, lines, st);
+    if (sh.groups == 3) return launch_backward_wide<D, H, 3, 384, EDGES>(d, ws, parts, stage, sh, lines, st);
+    return launch_backward_wide<D, H, 2, 512, EDGES>(d, ws, parts, stage, sh, lines, st);
 }
 template <typename D, typename H>
-cudaError_t launch_backward_types(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, cudaStream_t st) {
-    const Shape sh = backward_shape(d.cols);
-    if (sh.threads == 512) return launch_backward_wide<D, H, 4, 512>(d, ws, parts, stage, sh, st);
-    if (sh.groups == 5) return launch_backward_wide<D, H, 5, 256>(d, ws, parts, stage, sh, st);
-    if (sh.groups == 4) return launch_backward_wide<D, H, 4, 256>(d, ws, parts, stage, sh, st);
-    if (sh.groups == 3) return launch_backward_wide<D, H, 3, 384>(d, ws, parts, stage, sh, st);
-    return launch_backward_wide<D, H, 2, 512>(d, ws, parts, stage, sh, st);
+cudaError_t launch_backward_types(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, const Lines& lines, cudaStream_t st) {
+    return lines.at || lines.step || d.cols % 8 ? launch_backward_edges<D, H, true>(d, ws, parts, stage, lines, st) : launch_backward_edges<D, H, false>(d, ws, parts, stage, lines, st);
 }
 cudaError_t launch_layernorm_backward(const cleave_layernorm_backward_t& d, float* ws, cudaStream_t st) {
-    const uint32_t parts = layernorm_backward_parts(d.rows, d.cols);
-    const uint64_t stage = (uint64_t)d.cols * (type_bytes(d.dy_type) + type_bytes(d.h_type) * (d.dres ? 2u : 1u));
-    const bool wide = d.cols % 8 == 0 && d.cols <= 16384 && stage * backward_shape(d.cols).rows <= kRingMost && rows_wide(d.dy, d.lddy, d.dy_type) && rows_wide(d.h, d.ldh, d.h_type) &&
-                      rows_wide(d.dx, d.lddx, d.h_type) && (!d.dres || rows_wide(d.dres, d.lddres, d.h_type)) && (uintptr_t)d.w % 16 == 0;
+    uint32_t parts = layernorm_backward_parts(d.rows, d.cols);
+    const Shape sh = backward_shape(d.cols);
+    const uint64_t stage = (uint64_t)(d.cols / 8) * 8 * (type_bytes(d.dy_type) + type_bytes(d.h_type) * (d.dres ? 2u : 1u));
+    Lines lines;
+    const bool wide = d.cols >= 64 && d.cols <= 16384 && stage * sh.rows <= kRingMost &&
+                      lines_agree({{d.dy, d.lddy, d.dy_type}, {d.h, d.ldh, d.h_type}, {d.dx, d.lddx, d.h_type}, {d.dres, d.lddres, d.h_type}}, lines);
+    if (wide && lines.step && parts * sh.rows % 8 && d.rows > parts) parts = parts / 8 * 8;          // a row's next one begins like it
     cudaError_t e = cudaSuccess;
     if (parts && wide) {
-        if (d.dy_type == CLEAVE_T_F32) e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<float, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<float, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
-        else e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<__nv_bfloat16, float>(d, ws, parts, (uint32_t)stage, st) : launch_backward_types<__nv_bfloat16, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, st);
+        if (d.dy_type == CLEAVE_T_F32) e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<float, float>(d, ws, parts, (uint32_t)stage, lines, st) : launch_backward_types<float, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, lines, st);
+        else e = d.h_type == CLEAVE_T_F32 ? launch_backward_types<__nv_bfloat16, float>(d, ws, parts, (uint32_t)stage, lines, st) : launch_backward_types<__nv_bfloat16, __nv_bfloat16>(d, ws, parts, (uint32_t)stage, lines, st);
     } else if (parts && d.cols <= kOwnCols) {
         const uint32_t threads = own_threads(d.cols);
         e = launch_chained(threads <= 512 ? layernorm_backward_own_kernel<512> : layernorm_backward_own_kernel<1024>, parts, threads, 0, st, d, ws);
