@@ -188,12 +188,14 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
 }
 
 // ---- gradient: sums --------------------------------------------------------------------------------------
-// Places a chunk: 16; 8 where those would make too few CTAs (8192 places of 768 columns 42.6 us against 46, 16384 of 4096 columns 84
-// against 77); more where there would be more than kChunksMost, which bounds the workspace.
+// Places a chunk: the most of 8, 16, 32 or 64 that leave eight CTAs an SM (8192 places of 768 columns 42.6 us with 8, 46 with 16; 16384 of 4096
+// columns 84 with 8, 77 with 16), because each chunk leaves up to two pieces; more where there would be more than kChunksMost, which
+// bounds the workspace.
 constexpr uint32_t kChunksMost = 16 * kPartSms;
 uint32_t sum_chunk(uint64_t n, uint32_t cols) {
-    const uint64_t least = n / 16 * ((cols + 2047u) / 2048u) < 8 * kPartSms ? 8 : 16;
-    return (uint32_t)std::max<uint64_t>(least, (n + kChunksMost - 1) / kChunksMost);
+    uint64_t chunk = 8;
+    while (chunk < 64 && n / (2 * chunk) * ((cols + 2047u) / 2048u) >= 8 * kPartSms) chunk *= 2;
+    return (uint32_t)std::max<uint64_t>(chunk, (n + kChunksMost - 1) / kChunksMost);
 }
 
 struct Ordered {                    // what the order kernel left
@@ -207,18 +209,22 @@ struct Ordered {                    // what the order kernel left
 // rows of dy under way: 128 bytes a thread, and as much of the table's rows where they are added to
 template <typename X, bool ADD> constexpr int kRowsAhead = sizeof(X) == 2 && !ADD ? 8 : 4;
 
-// what a thread holds of a row: 8 columns (wide) or one
+// What a thread holds of a row: 8 columns in a group (wide), or four of `step` columns apart, of which there are `left` more.
+struct Span { uint32_t step, left; };
 template <typename T, bool WIDE> struct Cols;
 template <typename T> struct Cols<T, true> {
     Raw8<T> r;
-    __device__ __forceinline__ void load(const T* p) {
+    __device__ __forceinline__ void load(const T* p, Span) {
 #pragma unroll
         for (int k = 0; k < (int)(sizeof(r.w) / 16); ++k) r.w[k] = reinterpret_cast<const uint4*>(p)[k];
     }
 };
 template <typename T> struct Cols<T, false> {
-    T r;
-    __device__ __forceinline__ void load(const T* p) { r = *p; }
+    T r[4];
+    __device__ __forceinline__ void load(const T* p, Span s) {
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) if (k * s.step < s.left) r[k] = p[k * s.step];
+    }
 };
 template <bool WIDE> struct Acc;
 template <> struct Acc<true> {
@@ -237,22 +243,34 @@ template <> struct Acc<true> {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = mul2(v[i], f2(s, s));
     }
-    template <typename T> __device__ __forceinline__ void store(T* p) const { store8(p, v); }
+    template <typename T> __device__ __forceinline__ void store(T* p, Span) const { store8(p, v); }
 };
 template <> struct Acc<false> {
-    float v;
-    __device__ __forceinline__ void clear() { v = 0.f; }
-    template <typename T> __device__ __forceinline__ void add(const Cols<T, false>& c) { v += to_f32(c.r); }
-    __device__ __forceinline__ void scale(float s) { v *= s; }
-    template <typename T> __device__ __forceinline__ void store(T* p) const { *p = from_f32<T>(v); }
+    float v[4];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = 0.f;
+    }
+    template <typename T> __device__ __forceinline__ void add(const Cols<T, false>& c) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += to_f32(c.r[i]);      // (columns that do not exist: anything, and never stored)
+    }
+    __device__ __forceinline__ void scale(float s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] *= s;
+    }
+    template <typename T> __device__ __forceinline__ void store(T* p, Span s) const {
+#pragma unroll
+        for (uint32_t k = 0; k < 4; ++k) if (k * s.step < s.left) p[k * s.step] = from_f32<T>(v[k]);
+    }
 };
 
 template <typename X, typename D, bool WIDE, bool ADD>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
-    constexpr uint32_t W = WIDE ? 8 : 1;
+    constexpr uint32_t W = WIDE ? 8 : 1, C = WIDE ? 8 : 4;       // a thread's first column after its neighbour's; columns a thread
     constexpr int N = kRowsAhead<X, ADD>;
     begin_chained();
-    const uint32_t lane = threadIdx.x & 31u, columns = gridDim.y * blockDim.x * W, n = (uint32_t)d.n, first = blockIdx.x * o.chunk, most = min(n, first + o.chunk);
+    const uint32_t lane = threadIdx.x & 31u, columns = gridDim.y * blockDim.x * C, n = (uint32_t)d.n, first = blockIdx.x * o.chunk, most = min(n, first + o.chunk);
     // a lane looks at a place: its row, its token, the next place's token (behind the last token's place stands nothing in particular)
     auto look = [&](uint32_t p, uint2& here, uint32_t& next) {
         here = p < most ? o.sorted[p] : make_uint2(0u, 0u);
@@ -267,8 +285,9 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
         return;
     }
     const bool began = first > 0 && ahead == __shfl_sync(0xFFFFFFFFu, here.y, 0);            // the first run began before the chunk
-    for (uint32_t j = (blockIdx.y * blockDim.x + threadIdx.x) * W; j - lane * W < d.cols; j += columns) {       // (a warp stays together)
+    for (uint32_t j = blockIdx.y * blockDim.x * C + threadIdx.x * W; j - lane * W < d.cols; j += columns) {       // (a warp stays together)
         const bool live = j < d.cols;
+        const Span span = {blockDim.x, live ? d.cols - j : 0u};
         const X* dy = static_cast<const X*>(d.dy) + j;
         D* dt = static_cast<D*>(d.dtable) + j;
         Acc<WIDE> acc;
@@ -285,8 +304,8 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
                 for (int k = 0; k < N; ++k) {
                     const uint32_t row = __shfl_sync(0xFFFFFFFFu, here.x, (i + k) & 31u), v = __shfl_sync(0xFFFFFFFFu, here.y, (i + k) & 31u);
                     if (!live || i + k >= count) continue;
-                    x[k].load(dy + (uint64_t)row * d.lddy);
-                    if (ADD && (stops >> (i + k) & 1u)) old[ADD ? k : 0].load(dt + (uint64_t)v * d.lddt);      // (not used where the run's other piece is missing)
+                    x[k].load(dy + (uint64_t)row * d.lddy, span);
+                    if (ADD && (stops >> (i + k) & 1u)) old[ADD ? k : 0].load(dt + (uint64_t)v * d.lddt, span);      // (not used where the run's other piece is missing)
                 }
 #pragma unroll
                 for (int k = 0; k < N; ++k) {
@@ -297,11 +316,11 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
                     if (live) {
                         acc.add(x[k]);
                         if (!open) {
-                            if (before) acc.store(o.parts + (uint64_t)blockIdx.x * 2 * d.cols + j);
+                            if (before) acc.store(o.parts + (uint64_t)blockIdx.x * 2 * d.cols + j, span);
                             else {
                                 acc.scale(d.scale);
                                 if (ADD) acc.add(old[ADD ? k : 0]);
-                                acc.store(dt + (uint64_t)v * d.lddt);
+                                acc.store(dt + (uint64_t)v * d.lddt, span);
                             }
                             acc.clear();
                         }
@@ -310,7 +329,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
                 }
             }
         }
-        if (open && live) acc.store(o.parts + ((uint64_t)blockIdx.x * 2 + (before ? 0 : 1)) * d.cols + j);
+        if (open && live) acc.store(o.parts + ((uint64_t)blockIdx.x * 2 + (before ? 0 : 1)) * d.cols + j, span);
         if (j == 0) o.runs[blockIdx.x] = make_uint2(token, open && !before ? (o.ends[token] - 1) / o.chunk - blockIdx.x + 1 : 0u);
     }
 }
@@ -320,8 +339,8 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
 constexpr uint32_t kLongRun = 16;
 template <typename D, bool WIDE>
 __global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
-    constexpr uint32_t W = WIDE ? 8 : 1;
-    __shared__ __align__(16) float s[8][32 * W];
+    constexpr uint32_t W = WIDE ? 8 : 1, C = WIDE ? 8 : 4;
+    __shared__ __align__(16) float s[8][32 * C];
     begin_chained();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
     uint32_t v = 0, pieces = 0;                                  // of lane k < 8: the run that begins in chunk k
@@ -330,47 +349,48 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_consta
         v = run.x;
         pieces = run.y;
     }
+    auto span_at = [&](uint32_t j) { return Span{32, d.cols - j}; };
     auto add = [&](Acc<WIDE>& acc, uint32_t k, uint32_t begin, uint32_t step, uint32_t end, uint32_t j) {      // pieces of the run of chunk k
         const float* from = o.parts + (uint64_t)(blockIdx.x * 8 + k) * 2 * d.cols + j;
 #pragma unroll 8
         for (uint32_t c = begin; c < end; c += step) {
             Cols<float, WIDE> x;
-            x.load(from + ((uint64_t)c * 2 + (c == 0 ? 1 : 0)) * d.cols);
+            x.load(from + ((uint64_t)c * 2 + (c == 0 ? 1 : 0)) * d.cols, span_at(j));
             acc.add(x);
         }
     };
     auto at = [&](uint32_t token, uint32_t j) { return static_cast<D*>(d.dtable) + (uint64_t)token * d.lddt + j; };
-    auto finish = [&](Acc<WIDE>& acc, const Cols<D, WIDE>& old, D* dt) {
+    auto finish = [&](Acc<WIDE>& acc, const Cols<D, WIDE>& old, uint32_t token, uint32_t j) {
         acc.scale(d.scale);
         if (d.accumulate) acc.add(old);
-        acc.store(dt);
+        acc.store(at(token, j), span_at(j));
     };
     const uint32_t mine = __shfl_sync(0xFFFFFFFFu, pieces, warp), token = __shfl_sync(0xFFFFFFFFu, v, warp);
     if (mine && mine <= kLongRun)
-        for (uint32_t j = (blockIdx.y * 32 + lane) * W; j < d.cols; j += gridDim.y * 32 * W) {
+        for (uint32_t j = blockIdx.y * 32 * C + lane * W; j < d.cols; j += gridDim.y * 32 * C) {
             Acc<WIDE> acc;
             Cols<D, WIDE> old;
             acc.clear();
-            if (d.accumulate) old.load(at(token, j));
+            if (d.accumulate) old.load(at(token, j), span_at(j));
             add(acc, warp, 0, 1, mine, j);
-            finish(acc, old, at(token, j));
+            finish(acc, old, token, j);
         }
     for (uint32_t some = __ballot_sync(0xFFFFFFFFu, pieces > kLongRun); some; some &= some - 1) {
         const uint32_t k = (uint32_t)__ffs((int)some) - 1, many = __shfl_sync(0xFFFFFFFFu, pieces, k), token = __shfl_sync(0xFFFFFFFFu, v, k);
-        for (uint32_t j0 = blockIdx.y * 32 * W; j0 < d.cols; j0 += gridDim.y * 32 * W) {
+        for (uint32_t j0 = blockIdx.y * 32 * C; j0 < d.cols; j0 += gridDim.y * 32 * C) {
             const uint32_t j = j0 + lane * W;
             Acc<WIDE> acc;
             Cols<D, WIDE> old;
             acc.clear();
-            if (d.accumulate && warp == 0 && j < d.cols) old.load(at(token, j));
+            if (d.accumulate && warp == 0 && j < d.cols) old.load(at(token, j), span_at(j));
             if (j < d.cols) add(acc, k, warp, 8, many, j);
-            acc.store(&s[warp][lane * W]);
+            acc.store(&s[warp][lane * W], Span{32, 32 * C});
             __syncthreads();
             if (warp == 0 && j < d.cols) {
                 acc.clear();
 #pragma unroll
-                for (uint32_t w = 0; w < 8; ++w) { Cols<float, WIDE> x; x.load(&s[w][lane * W]); acc.add(x); }
-                finish(acc, old, at(token, j));
+                for (uint32_t w = 0; w < 8; ++w) { Cols<float, WIDE> x; x.load(&s[w][lane * W], Span{32, 32 * C}); acc.add(x); }
+                finish(acc, old, token, j);
             }
             __syncthreads();
         }
@@ -409,7 +429,7 @@ cudaError_t launch_order(const cleave_embedding_backward_t& d, const Ordered& o,
 template <typename X, typename D, bool WIDE>
 cudaError_t launch_sums(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
     if (!o.chunks) return cudaSuccess;
-    const uint32_t units = WIDE ? d.cols / 8 : d.cols, tiles = std::min(65535u, (units + 255) / 256), threads = std::min(256u, ((units + tiles - 1) / tiles + 31) / 32 * 32);
+    const uint32_t units = WIDE ? d.cols / 8 : (d.cols + 3) / 4, tiles = std::min(65535u, (units + 255) / 256), threads = std::min(256u, ((units + tiles - 1) / tiles + 31) / 32 * 32);
     const cudaError_t e = launch_chained(d.accumulate ? embedding_sum_kernel<X, D, WIDE, true> : embedding_sum_kernel<X, D, WIDE, false>, dim3(o.chunks, tiles), threads, 0, st, d, o);
     if (e != cudaSuccess || o.chunks < 2) return e;
     return launch_chained(embedding_join_kernel<D, WIDE>, dim3((o.chunks + 7) / 8, std::min(65535u, (units + 31) / 32)), 256, 0, st, d, o);
