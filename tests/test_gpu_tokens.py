@@ -669,3 +669,49 @@ def test_workspaces_of_calls_on_another_stream_are_not_memory_in_use(cl):
             call(stream)
             torch.cuda.synchronize()
             assert torch.all(kept == 4.0) and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("rows,cols", [(1, 64), (5, 200), (40, 1001), (9, 4104), (300, 776), (3, 9000), (2, 17000)])
+@pytest.mark.parametrize("h_t,dy_t", [("bf16", "bf16"), ("f32", "bf16"), ("bf16", "f32")])
+def test_layernorm_of_operands_that_begin_differently(cl, rows, cols, h_t, dy_t):
+    """Rows that lie differently in each operand leave the same values as rows that lie alike, and these the oracle's."""
+    rng = np.random.default_rng(rows * 3 + cols)
+    x, r = _rand(rng, (rows, cols), DT[dy_t]), _rand(rng, (rows, cols), DT[h_t])
+    w, b = _rand(rng, cols + 3, torch.float32, 0.2) + 1, _rand(rng, cols + 3, torch.float32)
+    one = lambda: torch.empty(rows, device=_dev())  # noqa: E731
+    for wt, bt in ((w[:cols], b[:cols]), (w[1:cols + 1], b[3:])):
+        h64, y64, _, r64 = ref.layernorm(_f64(x), _f64(r), _f64(wt), _f64(bt), float(np.float32(1e-5)))
+        tol = _layernorm_tolerance(h64, _f64(wt), y64, r64, True)
+        for pads in ((0, 0, 0, 0), (1, 2, 3, 5), (7, 0, 7, 0), (8, 16, 8, 0)):
+            y, whole = _room(rows, cols, torch.float32, pads[2], pads[0] % 3)
+            h, _ = _room(rows, cols, DT[h_t], pads[3], pads[1] % 2)
+            mean, rstd = one(), one()
+            cl.layernorm(_lay(x, pads[0], pads[3]), wt, bt, y, residual=_lay(r, pads[1], pads[2]), h=h, mean=mean, rstd=rstd)
+            _close(y, y64, tol, "y")
+            _close(h, h64, U * np.abs(h64), "h")
+            _untouched(whole, cols)
+            dx, whole = _room(rows, cols, DT[h_t], pads[1], pads[2] % 3)
+            dw, db = torch.empty(cols, device=_dev()), torch.empty(cols, device=_dev())
+            cl.layernorm_backward(_lay(x, pads[3], pads[0]), h, wt, mean, rstd, dx, dw, db, dres=_lay(r, pads[0], pads[1]))
+            h_, dy_, m_, s_, w_ = _f64(h), _f64(x), _f64(mean), _f64(rstd), _f64(wt)
+            dx64, dw64, db64 = ref.layernorm_backward(dy_, h_, w_, m_, s_, _f64(r))
+            # (as in test_layernorm_backward)
+            xh, q = np.abs(h_ - m_[:, None]) * s_[:, None], np.abs(dy_ * w_)
+            qx, q1 = (q * xh).mean(axis=1, keepdims=True), q.mean(axis=1, keepdims=True)
+            dtol = s_[:, None] * (4 * U * q + (SUM + 4 * U) * q1 + xh * (SUM + 15 * U) * qx) + 2 * U * np.abs(_f64(r)) + 2 * U * np.abs(dx64)
+            _close(dx, dx64, dtol, "dx")
+            _untouched(whole, cols)
+            _close(dw, dw64, (SUM + 4 * U) * (np.abs(dy_) * xh).sum(axis=0), "dw")
+            _close(db, db64, SUM * np.abs(dy_).sum(axis=0), "db")
+
+
+def test_layernorm_backward_shares_of_rows_that_begin_differently(cl):
+    """Integers, exact in any order: many rows of lengths whose rows begin at every place of a line, and none lost at their ends."""
+    rng = np.random.default_rng(77)
+    for rows, cols in ((700, 65), (3000, 67), (900, 769), (640, 1029), (800, 2051), (500, 4097), (330, 5123), (310, 8195)):
+        dy, h = (_put(rng.integers(-4, 5, size=(rows, cols)), torch.bfloat16) for _ in range(2))
+        one, zero = torch.ones(rows, device=_dev()), torch.zeros(rows, device=_dev())
+        dx, dw, db = torch.empty_like(h), torch.full((cols + 1,), 7.0, device=_dev()), torch.full((cols + 1,), 7.0, device=_dev())
+        cl.layernorm_backward(dy, h, None, zero, one, dx, dw[:cols], db[:cols])
+        assert torch.equal(dw[:cols], (dy.float() * h.float()).sum(0)) and torch.equal(db[:cols], dy.float().sum(0)), (rows, cols)
+        assert float(dw[cols]) == 7.0 and float(db[cols]) == 7.0
