@@ -325,7 +325,8 @@ CLEAVE_API void cleave_destroy(cleave_plan_t* p);
  * What the paper's server computes itself around the distributed GEMMs of a training step (Section
  * 3.2: normalisation, activations and the Adam update stay on the server; Section 4.1: the
  * optimizer's cost C_opt), plus the GEMMs that a server keeps for itself, with everything that
- * follows the product fused into its write-out.
+ * follows the product fused into its write-out, and the two ends of a step on tokens: the table's
+ * rows and their gradient, and the losses of the scores.
  *
  *   - Matrices are row-major with a leading dimension in elements (ld >= columns).  Element types
  *     are CLEAVE_T_*; "type 0" means the operand is absent (and its pointer NULL).
@@ -577,7 +578,7 @@ CLEAVE_API int cleave_layernorm_backward(const cleave_layernorm_backward_t* d, v
  *   top_index, top_values: the `top` places of the largest scores, largest first and of equal ones the lowest place first,
  *   and their log probabilities s x - lse.
  * Every output may be NULL, but not all.  x: bf16 or fp32.  top: 0 to CLEAVE_TOP_MOST and at most cols.
- * A masked place (-infinity) has probability 0.  A row without a score above -2^126 (all places masked, by -infinity or the type's
+ * A score that is not masked has s x within fp32's range.  A masked place (-infinity) has probability 0.  A row without a score above -2^126 (all places masked, by -infinity or the type's
  * lowest value) has lse = -infinity, logp = -infinity, entropy 0, top_values -infinity, and no gradient.  A row
  * that holds a NaN or +infinity has NaN for lse, logp, entropy and top_values (a NaN sorts above all).  The logp of padding is 0. */
 #define CLEAVE_TOP_MOST 64u

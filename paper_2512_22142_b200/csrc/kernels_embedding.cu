@@ -13,7 +13,14 @@
 //   sum      the sorted places are cut into chunks of the same length, whatever the tokens; a CTA adds the rows of a
 //            chunk run by run.  A run that lies inside one chunk is a finished row; the ends of longer runs go to the workspace.
 //   join     the pieces of each longer run are added in order.
-// Bound by the HBM where the whole table is written, by the three launches' latencies where few rows are.
+// Bound by the HBM where the whole table is written, by the three launches' latencies where few rows are.  Measured, with tokens whose
+// frequency falls with their rank: 8192 tokens into the whole of a 50257 x 768 fp32 table 41.7 us (28 of them the zeros and, beside them,
+// the sorting; its bytes take 26), 16384 added to a 32000 x 4096 table 71 us (order 8, sum 48, join 10; its bytes take 44.5).  Lookup of
+// 16384 x 5120 bf16 37 us (6.0 TB/s), of 64 x 4096 4.3.
+//
+// Tried and not kept: zeros beside the sums instead of beside the sorting (82 us for the first of these); a run that ends soon behind its
+// chunk finished there instead of in pieces (77 us for the second: chunks of unlike length); ranges of the vocabulary as owners
+// (one of them has half of the tokens: 77 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -336,9 +343,9 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const __grid_constan
 
 // A CTA looks at 8 chunks for runs that begin in a chunk and go on.  A warp adds the pieces of its chunk's run in order; a run of
 // more than kLongRun pieces is left to all warps (each adds every eighth piece, and the warps' sums are added in order).
-constexpr uint32_t kLongRun = 16;
+constexpr uint32_t kLongRun = 6;
 template <typename D, bool WIDE>
-__global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
+__global__ void __launch_bounds__(256, 6) embedding_join_kernel(const __grid_constant__ cleave_embedding_backward_t d, const __grid_constant__ Ordered o) {
     constexpr uint32_t W = WIDE ? 8 : 1, C = WIDE ? 8 : 4;
     __shared__ __align__(16) float s[8][32 * C];
     begin_chained();
@@ -352,7 +359,7 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const __grid_consta
     auto span_at = [&](uint32_t j) { return Span{32, d.cols - j}; };
     auto add = [&](Acc<WIDE>& acc, uint32_t k, uint32_t begin, uint32_t step, uint32_t end, uint32_t j) {      // pieces of the run of chunk k
         const float* from = o.parts + (uint64_t)(blockIdx.x * 8 + k) * 2 * d.cols + j;
-#pragma unroll 8
+#pragma unroll 4
         for (uint32_t c = begin; c < end; c += step) {
             Cols<float, WIDE> x;
             x.load(from + ((uint64_t)c * 2 + (c == 0 ? 1 : 0)) * d.cols, span_at(j));

@@ -1,12 +1,19 @@
 // Log probabilities of given tokens with entropy and top alternatives, distillation from a teacher's top scores, and the
 // backward passes of both (see cleave.h).
 //
-// Forward: one reading of the scores.  A thread keeps a largest score m and, relative to it, s = sum 2^a and t = sum 2^a a
-// with a = c (x - m), c = scale log2(e); a larger score rescales both.  lse = scale m + ln 2 log2(s), entropy = ln 2 (log2(s) - t / s).
-// The top places go through a threshold that only rises: a score below it is dropped after one comparison (shared by 16
-// bytes of scores), the others are collected by warp and cut to the best `top` when a warp's room is full.
+// Forward: one reading of the scores.  A thread keeps a base and, relative to it, s = sum 2^a and t = sum 2^a a with
+// a = c (x - base), c = scale log2(e).  The base is a score that only a score far above it replaces: then both sums are
+// rescaled.  lse = scale m + ln 2 log2(s) and entropy = ln 2 (log2(s) - t / s), relative to the largest score m.
+// The top places go through a bar that only rises: a score below it is dropped after one comparison (shared by 32 bytes of
+// scores), the places of the others are collected by warp and, where a warp's room is full, cut to those that the bar
+// has not passed, or to the best.
 // A row goes to one CTA, or with few rows to a cluster of them, joined through distributed shared memory.
 // Backward: each element from its score and the row's lse; one reading, one writing.
+//
+// Bound: the forward pass by instruction issue (68 % of the cycles) and exponentials (one an element, half of what the SM has at that
+// rate), then the HBM; few rows by latency; the backward passes by the HBM.  Measured: 8192 x 50257 bf16 with entropy 157 us (5.2 TB/s; 130
+// without entropy), the 20 best of 16 x 128000 fp32 16 us (7 without them), of 2048 rows 220 us; gradient of 8192 x 128000 bf16 636 us
+// (6.6 TB/s; a plain copy runs at 6.4); distillation, loss and gradient, 8192 x 32000 with 64 places 278 us (5.7 TB/s).
 #include <algorithm>
 #include <type_traits>
 
