@@ -371,11 +371,13 @@ cudaError_t launch_layernorm(const cleave_layernorm_t& d, int sms, cudaStream_t 
 // [parts x 2 cols], dw's columns first; each element belongs to one thread), and layernorm_sum_parts_kernel adds the parts in order.
 // The wide form's shape: threads a row, groups of 8 columns a thread, rows that a CTA works on at a time.  What counts is work between two
 // barriers: many groups a thread and few threads (16384 rows of 4096 columns: 4 groups and 128 threads 91 us, 2 groups and 256
-// threads 111, one group and 512 threads 164); up to 1024 columns a row is one warp's.  A CTA an SM, with as many warps as registers allow.
+// threads 111, one group and 512 threads 164); up to 1024 columns a row is one warp's.  A CTA an SM, with as many warps as registers allow
+// (16187 x 2968 bf16 with 3 groups and 12 warps 79 us, 4 groups and 6 warps 93; 8000 x 2600 fp32 90 and 73: its rows spill at 12 warps).
 struct Shape { uint32_t threads, groups, rows; };
-Shape backward_shape(uint32_t cols) {
+Shape backward_shape(uint32_t cols, bool f32) {                  // f32: h is, and takes more registers
     const uint32_t units = (cols + 7) / 8;
-    const uint32_t threads = units <= 640 ? std::min(128u, (units + 127) / 128 * 32) : (units <= 1024 ? 256u : 512u), groups = (units + threads - 1) / threads;
+    const uint32_t threads = units <= 128 ? 32u : (units <= 256 ? 64u : (units <= 384 && f32 ? 96u : (units <= 640 ? 128u : (units <= 1024 ? (units + 127) / 128 * 32 : 512u))));
+    const uint32_t groups = (units + threads - 1) / threads;
     const uint32_t warps = groups <= 2 ? 16 : (groups == 3 ? 12 : 8);
     return {threads, groups, std::max(1u, warps * 32 / threads)};
 }
@@ -490,7 +492,7 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
     __shared__ float buffers[16][2][2][32];
     begin_chained();
     constexpr uint32_t BD = Bytes8<D>::value, BH = Bytes8<H>::value;
-    constexpr bool KEEP = V < 4 || (V == 4 && T < 512) || (V == 5 && sizeof(H) == 2);
+    constexpr bool KEEP = T < 512 ? V < 5 || sizeof(H) == 2 : V < 3;
     float (&parts)[2][2][32] = buffers[threadIdx.y];
     const uint32_t tid = threadIdx.x, nt = blockDim.x;
     const bool res = d.dres != nullptr;
@@ -689,8 +691,8 @@ cudaError_t launch_backward_wide(const cleave_layernorm_backward_t& d, float* ws
 }
 template <typename D, typename H, bool EDGES>
 cudaError_t launch_backward_edges(const cleave_layernorm_backward_t& d, float* ws, uint32_t parts, uint32_t stage, const Lines& lines, cudaStream_t st) {
-    const Shape sh = backward_shape(d.cols);
-    if (sh.threads == 512) return launch_backward_wide<D, H, 4, 512, EDGES>(d, ws, parts, stage, sh, lines, st);
+    const Shape sh = backward_shape(d.cols, sizeof(H) == 4);
+    if (sh.threads == 512) return sh.groups <= 3 ? launch_backward_wide<D, H, 3, 512, EDGES>(d, ws, parts, stage, sh, lines, st) : launch_backward_wide<D, H, 4, 512, EDGES>(d, ws, parts, stage, sh, lines, st);
     if (sh.groups == 5) return launch_backward_wide<D, H, 5, 256, EDGES>(d, ws, parts, stage, sh, lines, st);
     if (sh.groups == 4) return launch_backward_wide<D, H, 4, 256, EDGES>(d, ws, parts, stage, sh, lines, st);
     if (sh.groups == 3) return launch_backward_wide<D, H, 3, 384, EDGES>(d, ws, parts, stage, sh, lines, st);
@@ -702,7 +704,7 @@ cudaError_t launch_backward_types(const cleave_layernorm_backward_t& d, float* w
 }
 cudaError_t launch_layernorm_backward(const cleave_layernorm_backward_t& d, float* ws, cudaStream_t st) {
     uint32_t parts = layernorm_backward_parts(d.rows, d.cols);
-    const Shape sh = backward_shape(d.cols);
+    const Shape sh = backward_shape(d.cols, d.h_type == CLEAVE_T_F32);
     const uint64_t stage = (uint64_t)(d.cols / 8) * 8 * (type_bytes(d.dy_type) + type_bytes(d.h_type) * (d.dres ? 2u : 1u));
     Lines lines;
     const bool wide = d.cols >= 64 && d.cols <= 16384 && stage * sh.rows <= kRingMost &&
