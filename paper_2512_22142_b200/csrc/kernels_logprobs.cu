@@ -244,14 +244,17 @@ __device__ __forceinline__ void merge(const uint64_t* pool, uint32_t lists, uint
 }
 
 // ---- forward ---------------------------------------------------------------------------------------------------
-constexpr int kSteps = 2;                        // units a thread takes at once, and as many again under way
+// Threads an SM: 48 registers each, 64 with top places; units a thread takes at once, with as many again under way: 3, 2 with top places.
+// (8192 x 50257 with entropy 149 us; two units and 1536 threads 152, four and 1024 154.  4096 rows in fp32 126, 134 and 126.  The 20 best of
+// 2048 x 128000 fp32 220 with two units, 273 with three.)
+constexpr int kSumThreads = 1280, kTopThreads = 1024;
 constexpr float kSlack = 8.f;
 
 // The CTA's part (rank `part` of `parts`) of a row: its sums, joined over the CTA (every thread receives them), and with TOP its
 // best `top` candidates in room->best.
 template <typename T, bool ENT, bool TOP, int THREADS>
 __device__ __forceinline__ Sums row_part(const T* x, uint32_t cols, float c, uint32_t part, uint32_t parts, Sums* warps, TopRoom<THREADS>* top_room, uint32_t top) {
-    constexpr int V = kUnit<T>;
+    constexpr int V = kUnit<T>, kSteps = TOP ? 2 : 3;
     constexpr uint32_t kScoreThreads = THREADS;
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5;
     // the row's units stand on 16 bytes; what is before them and behind them (less than a unit each) goes to threads of
@@ -450,7 +453,7 @@ __device__ __forceinline__ uint64_t ld_dsmem_u64(uint32_t at) {
 }
 
 template <typename T, bool ENT, bool TOP, int THREADS>
-__global__ void __launch_bounds__(THREADS, TOP ? 1024 / THREADS : 1536 / THREADS) logprobs_kernel(const __grid_constant__ cleave_logprobs_t d) {
+__global__ void __launch_bounds__(THREADS, TOP ? kTopThreads / THREADS : kSumThreads / THREADS) logprobs_kernel(const __grid_constant__ cleave_logprobs_t d) {
     __shared__ Sums warps[THREADS / 32], whole;
     __shared__ typename std::conditional<TOP, TopRoom<THREADS>, int>::type top_room;
     begin_chained();
@@ -518,7 +521,7 @@ cudaError_t launch_logprobs_types(const cleave_logprobs_t& d, const RowGrid& g, 
     return d.top ? launch_logprobs_kernel<T, ENT, true>(d, g, st) : launch_logprobs_kernel<T, ENT, false>(d, g, st);
 }
 cudaError_t launch_logprobs(const cleave_logprobs_t& d, int sms, cudaStream_t st) {
-    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms, d.top ? 1024 : 1536);
+    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms, d.top ? kTopThreads : kSumThreads);
     if (d.x_type == CLEAVE_T_F32) return d.entropy ? launch_logprobs_types<float, true>(d, g, st) : launch_logprobs_types<float, false>(d, g, st);
     return d.entropy ? launch_logprobs_types<__nv_bfloat16, true>(d, g, st) : launch_logprobs_types<__nv_bfloat16, false>(d, g, st);
 }
@@ -706,7 +709,7 @@ __device__ __forceinline__ float teacher(const cleave_distill_t& d, uint64_t row
     return sum * inv;
 }
 template <typename T, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1536 / THREADS) distill_kernel(const __grid_constant__ cleave_distill_t d) {
+__global__ void __launch_bounds__(THREADS, kSumThreads / THREADS) distill_kernel(const __grid_constant__ cleave_distill_t d) {
     __shared__ Sums warps[THREADS / 32], whole;
     __shared__ float buf[32];
     begin_chained();
@@ -737,7 +740,7 @@ cudaError_t launch_distill_types(const cleave_distill_t& d, const RowGrid& g, cu
     return launch_chained_clusters(kernel, g.cluster, g.grid, g.threads, 0, st, d);
 }
 cudaError_t launch_distill(const cleave_distill_t& d, int sms, cudaStream_t st) {
-    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms, 1536);
+    const RowGrid g = row_grid(d.rows, (uint64_t)d.cols * type_bytes(d.x_type), sms, kSumThreads);
     return d.x_type == CLEAVE_T_F32 ? launch_distill_types<float>(d, g, st) : launch_distill_types<__nv_bfloat16>(d, g, st);
 }
 template <typename X, typename D, bool WIDE>
