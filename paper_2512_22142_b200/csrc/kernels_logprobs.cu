@@ -10,10 +10,11 @@
 // A row goes to one CTA, or with few rows to a cluster of them, joined through distributed shared memory.
 // Backward: each element from its score and the row's lse; one reading, one writing.
 //
-// Bound: the forward pass by instruction issue (68 % of the cycles) and exponentials (one an element, half of what the SM has at that
-// rate), then the HBM; few rows by latency; the backward passes by the HBM.  Measured: 8192 x 50257 bf16 with entropy 157 us (5.2 TB/s; 130
-// without entropy), the 20 best of 16 x 128000 fp32 16 us (7 without them), of 2048 rows 220 us; gradient of 8192 x 128000 bf16 636 us
-// (6.6 TB/s; a plain copy runs at 6.4); distillation, loss and gradient, 8192 x 32000 with 64 places 278 us (5.7 TB/s).
+// Bound: the forward pass by the HBM and, beside it, instruction issue (64 % of the cycles) and exponentials (one an element, half of what
+// the SM has at that rate); few rows by latency; the backward passes by the HBM.  Measured: 8192 x 50257 bf16 with entropy 141 to 155 us with
+// the GPU's clock (5.3 to 5.8 TB/s; 136 without entropy), the 20 best of 16 x 128000 fp32 16 us (6.3 without them), of 2048 rows 220 us;
+// gradient of 8192 x 128000 bf16 636 us (6.6 TB/s; a plain copy runs at 6.4); distillation, loss and gradient, 8192 x 32000 with 64
+// places 267 to 278 us (5.7 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -502,7 +503,7 @@ uint32_t row_parts(uint64_t rows, uint64_t row_bytes, int sms, uint32_t sm_threa
     return parts;
 }
 // Threads: as many as fill the SMs (16 x 128000 fp32 8 us with 512, 10 with 256); many rows go to CTAs of 128, whose joins cost
-// less (8192 x 50257 with entropy 143 us against 152 with 256).
+// less (8192 x 50257 with entropy, two units a thread, 143 us against 152 with 256).
 struct RowGrid { dim3 cluster, grid; uint32_t threads; };
 RowGrid row_grid(uint64_t rows, uint64_t row_bytes, int sms, uint32_t sm_threads) {       // sm_threads: what an SM holds of the kernel
     const uint32_t parts = row_parts(rows, row_bytes, sms, sm_threads), y = (uint32_t)std::min<uint64_t>(rows, 65535);

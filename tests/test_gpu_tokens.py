@@ -715,3 +715,61 @@ def test_layernorm_backward_shares_of_rows_that_begin_differently(cl):
         cl.layernorm_backward(dy, h, None, zero, one, dx, dw[:cols], db[:cols])
         assert torch.equal(dw[:cols], (dy.float() * h.float()).sum(0)) and torch.equal(db[:cols], dy.float().sum(0)), (rows, cols)
         assert float(dw[cols]) == 7.0 and float(db[cols]) == 7.0
+
+
+def test_scores_beyond_32_bits_of_offset(cl):
+    """A matrix of more than 2^31 elements: its last rows leave what the same rows leave by themselves."""
+    rows, vocab, few = 17000, 131072, 5
+    gen = torch.Generator(device=_dev()).manual_seed(1)
+    x = torch.empty(rows, vocab, dtype=torch.bfloat16, device=_dev())
+    for at in range(0, rows, 1000):
+        x[at:at + 1000] = torch.randn(min(1000, rows - at), vocab, generator=gen, device=_dev())
+    t = torch.randint(0, vocab, (rows,), generator=gen, device=_dev())
+    one = lambda n: torch.full((n,), float("nan"), device=_dev())  # noqa: E731
+    logp, lse, h, ti = one(rows), one(rows), one(rows), torch.empty(rows, 5, dtype=torch.int32, device=_dev())
+    cl.token_logprobs(x, t, logp, lse=lse, entropy=h, top_index=ti)
+    assert torch.isfinite(logp).all() and torch.isfinite(lse).all() and torch.isfinite(h).all()
+    up = torch.full((rows,), -1.0, device=_dev())
+    tail, part = x[-few:].clone(), slice(rows - few, rows)
+    logp2, lse2, h2, ti2 = one(few), one(few), one(few), torch.empty(few, 5, dtype=torch.int32, device=_dev())
+    cl.token_logprobs(tail, t[part], logp2, lse=lse2, entropy=h2, top_index=ti2)
+    # (another number of CTAs a row: other sums of the same terms, 64 U of each)
+    for a, b in ((logp[part], logp2), (lse[part], lse2), (h[part], h2)):
+        assert torch.allclose(a, b, rtol=2 * SUM, atol=2 * SUM)
+    assert torch.equal(ti[part], ti2)
+    index, values = torch.randint(0, vocab, (rows, 6), generator=gen, device=_dev()), torch.randn(rows, 6, generator=gen, device=_dev())
+    loss, loss2 = one(rows), one(few)
+    cl.distill(x, index, values, loss)
+    cl.distill(tail, index[part], values[part], loss2)
+    assert torch.isfinite(loss).all() and torch.allclose(loss[part], loss2, rtol=2 * SUM, atol=16 * SUM)
+    want = torch.empty_like(tail)
+    cl.token_logprobs_backward(tail, t[part], lse[part], want, dlogp=up[part])
+    cl.token_logprobs_backward(x, t, lse, x, dlogp=up)
+    assert torch.equal(_bits(x[part]), _bits(want)) and torch.isfinite(x[::1000].float()).all()
+
+
+def test_rows_beyond_32_bits_of_offset(cl):
+    """Layer norm, lookup and gradient over more than 2^31 elements: their last rows are right, and so are whole sums of integers."""
+    rows, cols = 530000, 4104
+    x = torch.ones(rows, cols, dtype=torch.bfloat16, device=_dev())
+    x[:, ::2] = 3.0                                                         # mean 2, variance 1
+    x[-1, :] = torch.arange(cols, device=_dev()) % 7
+    y, mean, rstd = torch.empty_like(x), torch.empty(rows, device=_dev()), torch.empty(rows, device=_dev())
+    cl.layernorm(x, None, None, y, mean=mean, rstd=rstd, eps=0.0)
+    assert torch.all(mean[:-1] == 2) and torch.all((rstd[:-1] - 1).abs() <= 2 * U) and torch.all(y[-3:-1, ::2] == 1) and torch.all(y[-3:-1, 1::2] == -1)
+    last = x[-1].double()
+    assert abs(float(mean[-1] - last.mean())) < 1e-5
+    dw, db, one, zero = torch.empty(cols, device=_dev()), torch.empty(cols, device=_dev()), torch.ones(rows, device=_dev()), torch.zeros(rows, device=_dev())
+    x[-1] = 1.0
+    cl.layernorm_backward(x, x, None, zero, one, y, dw, db)                 # dy = h: dw the sum of squares
+    assert torch.equal(db[1::2], torch.full_like(db[1::2], rows)) and torch.equal(db[::2], torch.full_like(db[::2], 3 * rows - 2))
+    assert torch.equal(dw[::2], torch.full_like(dw[::2], 9 * rows - 8))
+    tokens = torch.arange(rows, device=_dev()) % 3
+    tokens[-1] = 5
+    dt = torch.empty(8, cols, device=_dev())
+    cl.embedding_backward(x, tokens, dt)
+    count = torch.bincount(tokens, minlength=8).float()
+    assert torch.equal(dt[:, 1], count) and torch.equal(dt[5], torch.ones(cols, device=_dev()))
+    assert torch.equal(dt[:3, 0], 3 * count[:3])
+    cl.embedding(tokens, dt[:, :].to(torch.bfloat16), y)
+    assert torch.all(y[-1] == 1) and torch.equal(y[-2, :2].float(), dt[int(tokens[-2]), :2].to(torch.bfloat16).float())
