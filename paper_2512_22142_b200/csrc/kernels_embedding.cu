@@ -15,7 +15,7 @@
 //   join     the pieces of each longer run are added in order.
 // Bound by the HBM where the whole table is written, by the three launches' latencies where few rows are.  Measured, with tokens whose
 // frequency falls with their rank: 8192 tokens into the whole of a 50257 x 768 fp32 table 41.7 us (28 of them the zeros and, beside them,
-// the sorting; its bytes take 26), 16384 added to a 32000 x 4096 table 71 us (order 8, sum 48, join 10; its bytes take 44.5).  Lookup of
+// the sorting; its bytes take 26), 16384 added to a 32000 x 4096 table 69 us (order 8, sum 50, join 9; its bytes take 44.5).  Lookup of
 // 16384 x 5120 bf16 37 us (6.0 TB/s), of 64 x 4096 4.3.
 //
 // Tried and not kept: zeros beside the sums instead of beside the sorting (82 us for the first of these); a run that ends soon behind its
@@ -84,7 +84,6 @@ cudaError_t launch_embedding(const cleave_embedding_t& d, cudaStream_t st) {
 
 // ---- gradient: the tokens' order ------------------------------------------------------------------------
 constexpr uint32_t kOrderThreads = 1024, kOrderWarps = kOrderThreads / 32, kOrderMost = kOrderThreads;        // tokens of the vocabulary a CTA owns at most
-constexpr int kOrderAhead = 8;                   // loads of 32 tokens under way
 
 // log2 of the number of owners: a power of two near the number of SMs, more for a vocabulary beyond 131072
 uint32_t order_owners(uint32_t vocab) {
@@ -113,7 +112,8 @@ __device__ __forceinline__ void fill_zeros(uint8_t* p, uint32_t bytes, uint32_t 
 }
 
 // sorted = (place, v) by v mod owners, v, place; ends[v] = where the places of token v end in it; *count = how many there are
-template <typename ID>
+// AHEAD: loads of 32 tokens that a warp has under way; those of the first are kept for the second reading.
+template <typename ID, int AHEAD>
 __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* ids, uint32_t n, uint32_t vocab, uint32_t bits, uint32_t values, uint32_t* ends, uint32_t* count, uint2* sorted,
                                                                     const __grid_constant__ Zeros z) {
     const uint32_t owners = 1u << bits, low = owners - 1;
@@ -136,18 +136,26 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
     __syncthreads();
     const uint32_t part = ((n + kOrderWarps - 1) / kOrderWarps + 31) / 32 * 32;
     const uint64_t from = (uint64_t)warp * part, to = min((uint64_t)n, from + part);
-    auto load = [&](uint64_t i, ID (&t)[kOrderAhead]) {          // 32 tokens each, in order; -1 behind the warp's part
+    auto load = [&](uint64_t i, int32_t (&t)[AHEAD]) {           // 32 tokens each, in order; -1 for padding and behind the warp's part
+        ID raw[AHEAD];
 #pragma unroll
-        for (int k = 0; k < kOrderAhead; ++k) t[k] = i + 32 * k + lane < to ? ids[i + 32 * k + lane] : (ID)-1;
+        for (int k = 0; k < AHEAD; ++k) raw[k] = i + 32 * k + lane < to ? ids[i + 32 * k + lane] : (ID)-1;
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) t[k] = raw[k] >= 0 && raw[k] < (ID)vocab ? (int32_t)raw[k] : -1;
     };
+    int32_t kept[AHEAD];
+    load(from, kept);
     uint32_t below = 0;
-    for (uint64_t i = from; i < to; i += 32 * kOrderAhead) {
-        ID t[kOrderAhead];
-        load(i, t);
+    for (uint64_t i = from; i < to; i += 32 * AHEAD) {
+        int32_t t[AHEAD];
+        if (i == from) {
 #pragma unroll
-        for (int k = 0; k < kOrderAhead; ++k) {
+            for (int k = 0; k < AHEAD; ++k) t[k] = kept[k];
+        } else load(i, t);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
             const uint32_t v = (uint32_t)t[k], owner = v & low;
-            if (t[k] < 0 || t[k] >= (ID)vocab) continue;
+            if (t[k] < 0) continue;
             if (owner < blockIdx.x) ++below;
             else if (owner == blockIdx.x) atomicAdd(mine + (v >> bits), 1u);
         }
@@ -175,12 +183,15 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
         if (own == values - 1 && blockIdx.x == low) *count = before;
     }
     __syncthreads();
-    for (uint64_t i = from; i < to; i += 32 * kOrderAhead) {
-        ID t[kOrderAhead];
-        load(i, t);
+    for (uint64_t i = from; i < to; i += 32 * AHEAD) {
+        int32_t t[AHEAD];
+        if (i == from) {
 #pragma unroll
-        for (int k = 0; k < kOrderAhead; ++k) {
-            const bool in = t[k] >= 0 && t[k] < (ID)vocab && ((uint32_t)t[k] & low) == blockIdx.x;
+            for (int k = 0; k < AHEAD; ++k) t[k] = kept[k];
+        } else load(i, t);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+            const bool in = t[k] >= 0 && ((uint32_t)t[k] & low) == blockIdx.x;
             const uint32_t some = __ballot_sync(0xFFFFFFFFu, in);
             if (!some) continue;
             if (in) {
@@ -416,11 +427,12 @@ static Space space_of(uint64_t n, uint32_t vocab, uint32_t cols) {
     return s;
 }
 uint64_t embedding_backward_workspace(uint64_t n, uint32_t vocab, uint32_t cols) { return space_of(n, vocab, cols).bytes; }
-template <typename ID>
+template <typename ID, int AHEAD>
 cudaError_t launch_order(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
     const uint32_t bits = order_owners(d.vocab), owners = 1u << bits, values = (uint32_t)(((uint64_t)d.vocab + owners - 1) >> bits);
+    auto kernel = token_order_kernel<ID, AHEAD>;
     static SmemLimit limit;
-    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(token_order_kernel<ID>), kOrderWarps * kOrderMost * 4);
+    const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kOrderWarps * kOrderMost * 4);
     if (e != cudaSuccess) return e;
     Zeros z = {};
     if (!d.accumulate) {
@@ -430,8 +442,13 @@ cudaError_t launch_order(const cleave_embedding_backward_t& d, const Ordered& o,
         z.tasks = z.pieces * rows;
     }
     const uint32_t zeros = (uint32_t)std::min<uint64_t>(2 * kPartSms, (z.tasks + kOrderWarps - 1) / kOrderWarps);
-    return launch_chained(token_order_kernel<ID>, owners + zeros, kOrderThreads, kOrderWarps * values * 4, st, static_cast<const ID*>(d.ids), (uint32_t)d.n, d.vocab, bits, values,
+    return launch_chained(kernel, owners + zeros, kOrderThreads, kOrderWarps * values * 4, st, static_cast<const ID*>(d.ids), (uint32_t)d.n, d.vocab, bits, values,
                           const_cast<uint32_t*>(o.ends), const_cast<uint32_t*>(o.count), const_cast<uint2*>(o.sorted), z);
+}
+// as many loads under way as a warp's part of the tokens has, up to 16 (16384 tokens 8.5 us with 16, 11.7 with 8; 8192 tokens 7.7 and 6.1)
+template <typename ID>
+cudaError_t launch_order_ids(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
+    return d.n <= 32 * 8 * kOrderWarps ? launch_order<ID, 8>(d, o, st) : launch_order<ID, 16>(d, o, st);
 }
 template <typename X, typename D, bool WIDE>
 cudaError_t launch_sums(const cleave_embedding_backward_t& d, const Ordered& o, cudaStream_t st) {
@@ -453,7 +470,7 @@ cudaError_t launch_embedding_backward(const cleave_embedding_backward_t& d, void
     uint32_t* head = reinterpret_cast<uint32_t*>(w);
     Ordered o = {head + 1, head, reinterpret_cast<const uint2*>(w + sp.sorted), reinterpret_cast<uint2*>(w + sp.runs), reinterpret_cast<float*>(w + sp.parts), sum_chunk(d.n, d.cols), 0};
     o.chunks = (uint32_t)((d.n + o.chunk - 1) / o.chunk);
-    const cudaError_t e = d.id_type == CLEAVE_T_I64 ? launch_order<int64_t>(d, o, st) : launch_order<int32_t>(d, o, st);
+    const cudaError_t e = d.id_type == CLEAVE_T_I64 ? launch_order_ids<int64_t>(d, o, st) : launch_order_ids<int32_t>(d, o, st);
     if (e != cudaSuccess) return e;
     if (d.dy_type == CLEAVE_T_F32) return d.dtable_type == CLEAVE_T_F32 ? launch_sums_types<float, float>(d, o, st) : launch_sums_types<float, __nv_bfloat16>(d, o, st);
     return d.dtable_type == CLEAVE_T_F32 ? launch_sums_types<__nv_bfloat16, float>(d, o, st) : launch_sums_types<__nv_bfloat16, __nv_bfloat16>(d, o, st);
