@@ -213,11 +213,12 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
         if (live[v]) { load_vector8(d.w, d.w_type, head + (tid + v * nt) * 8, 1.f, w[v]); load_vector8(d.b, d.b_type, head + (tid + v * nt) * 8, 0.f, b[v]); }
     // the thread's single column: its weight and bias, and the next row's value
     const float edge_w = edge < d.cols && d.w ? load_as(d.w, d.w_type, edge) : 1.f, edge_b = edge < d.cols && d.b ? load_as(d.b, d.b_type, edge) : 0.f;
-    float next_edge = 0.f;
+    X next_x = from_f32<X>(0.f);                                 // (as it is stored: a conversion would wait for the load)
+    typename std::conditional<RES, R, X>::type next_r = from_f32<typename std::conditional<RES, R, X>::type>(0.f);
     auto ask_edge = [&](uint64_t row) {
         if (edge < d.cols && row < d.rows) {
-            next_edge = to_f32(static_cast<const X*>(d.x)[row * d.ldx + edge]);
-            if constexpr (RES) next_edge += to_f32(static_cast<const R*>(d.r)[row * d.ldr + edge]);
+            next_x = static_cast<const X*>(d.x)[row * d.ldx + edge];
+            if constexpr (RES) next_r = static_cast<const R*>(d.r)[row * d.ldr + edge];
         }
     };
     ask_edge(first);
@@ -251,8 +252,10 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
 #pragma unroll
             for (int i = 0; i < 4; ++i) sum = add2(sum, h[v][i]);
         }
-        float lone = next_edge;
+        float lone = 0.f;
         if (edge < d.cols) {
+            lone = to_f32(next_x);
+            if constexpr (RES) lone += to_f32(next_r);
             if constexpr (RES) if (d.h) store_one(static_cast<R*>(d.h) + row * d.ldh + edge, lone);
             ask_edge(row + stride);
         }
@@ -538,12 +541,14 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
     }
     // the thread's single column: its weight, its shares, and the next row's values
     const float edge_w = EDGES && edge < d.cols && d.w ? load_as(d.w, d.w_type, edge) : 1.f;
-    float edge_dw = 0.f, edge_db = 0.f, next_dy = 0.f, next_h = 0.f, next_res = 0.f;
+    float edge_dw = 0.f, edge_db = 0.f;
+    D next_dy = from_f32<D>(0.f);                                // (as they are stored: a conversion would wait for the load)
+    H next_h = from_f32<H>(0.f), next_res = next_h;
     auto ask_edge = [&](uint64_t row) {
         if (EDGES && edge < d.cols && row < d.rows) {
-            next_dy = to_f32(static_cast<const D*>(d.dy)[row * d.lddy + edge]);
-            next_h = to_f32(static_cast<const H*>(d.h)[row * d.ldh + edge]);
-            if (res) next_res = to_f32(static_cast<const H*>(d.dres)[row * d.lddres + edge]);
+            next_dy = static_cast<const D*>(d.dy)[row * d.lddy + edge];
+            next_h = static_cast<const H*>(d.h)[row * d.ldh + edge];
+            if (res) next_res = static_cast<const H*>(d.dres)[row * d.lddres + edge];
         }
     };
     ask_edge(first);
@@ -584,11 +589,12 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
         }
         float edge_q = 0.f, edge_c = 0.f, edge_res = 0.f;
         if (EDGES && edge < d.cols) {
-            edge_c = next_h - mean;
-            edge_res = next_res;
-            edge_dw = fmaf(next_dy * rstd, edge_c, edge_dw);
-            edge_db += next_dy;
-            edge_q = next_dy * edge_w;
+            const float dy = to_f32(next_dy);
+            edge_c = to_f32(next_h) - mean;
+            edge_res = to_f32(next_res);
+            edge_dw = fmaf(dy * rstd, edge_c, edge_dw);
+            edge_db += dy;
+            edge_q = dy * edge_w;
             ask_edge(row + stride);
         }
         const float2 both = row_sums(sum_of(sums) + edge_q, fmaf(edge_q, edge_c, sum_of(dots)), parts[it & 1]);
