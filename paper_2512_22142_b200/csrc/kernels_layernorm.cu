@@ -8,8 +8,8 @@
 //   own    operands that disagree, and short rows, up to 8192 columns: neighbouring threads own neighbouring columns, held in registers.
 //   any    what is left: the row is taken again in each pass (it stays in L1 / L2).
 // Measured: 8192 x 768 with an fp32 residual 16.8 us (4.5 TB/s: 75 MB are read and written in the time of few rows a warp), 8192 x 8192 into E4M3 80 us
-// (5.9 TB/s), one row of 4096 a launch, 4.4 us with the call; backward of 16384 x 5120 with dw and db 128 us (5.2 TB/s, 10 of it the sums of
-// the CTAs' shares).  Rows of odd length: 1899 x 8962 fp32 70 us (3.9 TB/s), backward of 12216 x 3349 99 us (3.3 TB/s).
+// (5.9 TB/s), one row of 4096 a launch, 4.4 us with the call; backward of 16384 x 5120 with dw and db 125 to 131 us (5.1 to 5.4 TB/s, the sums of
+// the CTAs' shares among them).  Rows of odd length: 1899 x 8962 fp32 70 us (3.9 TB/s), backward of 12216 x 3349 93 to 99 us (3.3 to 3.5 TB/s).
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>

@@ -11,10 +11,10 @@
 // Backward: each element from its score and the row's lse; one reading, one writing.
 //
 // Bound: the forward pass by the HBM and, beside it, instruction issue (64 % of the cycles) and exponentials (one an element, half of what
-// the SM has at that rate); few rows by latency; the backward passes by the HBM.  Measured: 8192 x 50257 bf16 with entropy 141 to 155 us with
-// the GPU's clock (5.3 to 5.8 TB/s; 136 without entropy), the 20 best of 16 x 128000 fp32 16 us (6.3 without them), of 2048 rows 220 us;
+// the SM has at that rate); few rows by latency; the backward passes by the HBM.  Measured: 8192 x 50257 bf16 with entropy 141 to 158 us with
+// the GPU's clock (5.2 to 5.8 TB/s; 136 without entropy), the 20 best of 16 x 128000 fp32 16 us (6.3 without them), of 2048 rows 220 us;
 // gradient of 8192 x 128000 bf16 636 us (6.6 TB/s; a plain copy runs at 6.4); distillation, loss and gradient, 8192 x 32000 with 64
-// places 267 to 278 us (5.7 TB/s).
+// places 267 to 281 us (5.7 TB/s).
 #include <algorithm>
 #include <type_traits>
 
