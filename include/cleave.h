@@ -625,7 +625,8 @@ CLEAVE_API int cleave_logprobs_backward(const cleave_logprobs_backward_t* d, voi
  *   loss = sum_k q_k (log q_k - log p_(index_k)), p = softmax(s x) over the whole vocabulary; terms with q_k = 0 are 0
  *   lse as in cleave_logprobs (may be NULL)
  * A row whose places are all empty has loss 0 and no gradient; one whose scores are all masked has loss +infinity, unless
- * its places are empty too, and no gradient.  k: 1 to CLEAVE_DISTILL_MOST. */
+ * its places are empty too, and no gradient.  A NaN among the values of a row's places makes its loss NaN, and its gradient where
+ * dloss is not 0; so does +infinity (of s values) with normalize = 1.  k: 1 to CLEAVE_DISTILL_MOST. */
 #define CLEAVE_DISTILL_MOST 256u
 typedef struct {
     uint64_t rows;

@@ -111,11 +111,12 @@ def logprobs_backward(x, tokens, lse, scale=1.0, dlogp=None, dlse=None, dentropy
 
 
 def teacher(index, values, vocab, scale, normalize):
-    """(q, log q) of one row; empty entries have q = 0"""
-    v = np.where((index >= 0) & (index < vocab), scale * values, -math.inf)
-    if normalize and v.max() > -math.inf:
+    """(q, log q) of one row; empty entries have q = 0, whatever the others hold"""
+    live = (index >= 0) & (index < vocab)
+    v = np.where(live, scale * values, -math.inf)
+    if normalize and v.max() != -math.inf:
         v = v - v.max()
-        v = v - math.log(np.exp(v).sum())
+        v = np.where(live, v - np.log(np.exp(v).sum()), -math.inf)
     return np.exp(v), v
 
 
@@ -127,7 +128,7 @@ def distill(x, index, values, scale=1.0, normalize=True):
         lp, lse[i] = log_softmax(x[i], scale)
         q, log_q = teacher(index[i], values[i], x.shape[1], scale, normalize)
         for j, a, b in zip(index[i], q, log_q):
-            if a > 0:
+            if a != 0:
                 loss[i] += a * (b - lp[j])
                 size[i] += a * (abs(b) + abs(lp[j]))
     return loss, lse, size
@@ -138,12 +139,12 @@ def distill_backward(x, index, values, lse, dloss, scale=1.0, normalize=True):
     dx, size = np.zeros(x.shape), np.zeros(x.shape)
     for i in range(len(x)):
         q, _ = teacher(index[i], values[i], x.shape[1], scale, normalize)
-        if lse[i] == -math.inf or dloss[i] == 0 or not (q > 0).any():
+        if lse[i] == -math.inf or dloss[i] == 0 or not q.any():
             continue
         dx[i] = q.sum() * np.exp(scale * x[i] - lse[i])
         size[i] = dx[i]
         for j, a in zip(index[i], q):
-            if a > 0:
+            if a != 0:
                 dx[i, j] -= a
                 size[i, j] += a
         dx[i] *= scale * dloss[i]

@@ -676,6 +676,7 @@ cudaError_t launch_logprobs_backward(const cleave_logprobs_backward_t& d, int sm
 // ---- distillation ------------------------------------------------------------------------------------------
 // The row's teacher: `take(k, j, q, log_q)` for the entries of this thread's share whose q is not 0, and the sum of q to every thread.
 // Every warp reads the whole row (at most 8 entries a lane), so nothing waits for another warp; the entries are shared out 32 by 32.
+// (Where a value is NaN or +infinity every q is NaN, those of empty entries too: an entry is empty by its place, which is no address.)
 constexpr int kEntries = CLEAVE_DISTILL_MOST / 32;
 template <int THREADS, typename TAKE>
 __device__ __forceinline__ float teacher(const cleave_distill_t& d, uint64_t row, TAKE&& take) {
@@ -706,7 +707,7 @@ __device__ __forceinline__ float teacher(const cleave_distill_t& d, uint64_t row
     const float inv = d.normalize ? 1.f / sum : 1.f, log_sum = d.normalize ? logf(sum) : 0.f;
 #pragma unroll
     for (int i = 0; i < kEntries; ++i)
-        if (i % (THREADS / 32) == warp && e[i] * inv != 0.f) take(lane + 32 * i, (uint32_t)j[i], e[i] * inv, v[i] - log_sum);
+        if (i % (THREADS / 32) == warp && j[i] >= 0 && e[i] * inv != 0.f) take(lane + 32 * i, (uint32_t)j[i], e[i] * inv, v[i] - log_sum);
     return sum * inv;
 }
 template <typename T, int THREADS>

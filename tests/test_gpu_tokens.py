@@ -773,3 +773,48 @@ def test_rows_beyond_32_bits_of_offset(cl):
     assert torch.equal(dt[:3, 0], 3 * count[:3])
     cl.embedding(tokens, dt[:, :].to(torch.bfloat16), y)
     assert torch.all(y[-1] == 1) and torch.equal(y[-2, :2].float(), dt[int(tokens[-2]), :2].to(torch.bfloat16).float())
+
+
+@pytest.mark.parametrize("k", [2, 7, 32, 40, 100, 256])
+@pytest.mark.parametrize("x_t,t_t", [("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_distill_of_a_teacher_with_nan_and_infinities(cl, k, x_t, t_t, normalize):
+    """A NaN or +infinity among a row's values beside empty entries and behind the last one: they stay no places, the row's results are
+    what the formula gives, and other rows' are as without it."""
+    rng = np.random.default_rng(k)
+    rows, vocab, scale = 12, 700, 1.5
+    x = _rand(rng, (rows, vocab), DT[x_t], 2.0)
+    index, values = rng.integers(0, vocab, size=(rows, k)), rng.normal(size=(rows, k))
+    index[:, 1::3] = -1
+    index[3, 1] = vocab
+    plain = torch.tensor(values, dtype=torch.float32).to(DT[t_t]).to(_dev())
+    values[1, 0] = float("nan")
+    values[3, 0] = INF
+    values[4, 0] = 3e38                                                     # infinite once it is scaled
+    values[6, 1] = float("nan")                                             # in an empty entry: it does not matter
+    values[7, 0], values[7, k - 1] = -INF, float("nan")
+    index[8] = -1                                                           # nothing but empty entries
+    values[8] = float("nan")
+    it, vt = torch.tensor(index, device=_dev()), torch.tensor(values, dtype=torch.float32).to(DT[t_t]).to(_dev())
+    dloss = _rand(rng, rows, torch.float32)
+    dloss[3] = 0.0
+    f = lambda: torch.full((rows,), 7.0, device=_dev())  # noqa: E731
+    got = [f(), f(), torch.full_like(x, 7.0)]
+    ref_ = [f(), f(), torch.full_like(x, 7.0)]
+    for (loss, lse, dx), v in ((got, vt), (ref_, plain)):
+        cl.distill(x, it, v, loss, lse=lse, scale=scale, normalize=normalize)
+        cl.distill_backward(x, it, v, lse, dloss, dx, scale=scale, normalize=normalize)
+    v64 = _f64(vt)
+    v64[4, 0] = INF                                                         # (1.5 times 3e38 is, in fp32)
+    with np.errstate(all="ignore"):
+        want, _, _ = ref.distill(_f64(x), index, v64, scale, normalize)
+        want_dx, _ = ref.distill_backward(_f64(x), index, v64, _f64(got[1]), _f64(dloss), scale, normalize)
+    loss, dx = _f64(got[0]), _f64(got[2])
+    broken = [r for r in range(rows) if not np.isfinite(want[r])]
+    assert broken == ([1, 3, 4] if index[7, k - 1] < 0 else [1, 3, 4, 7])
+    assert np.array_equal(loss[broken], want[broken], equal_nan=True)
+    assert not np.isfinite(dx[[r for r in broken if r != 3]]).any() and not np.isfinite(want_dx[[r for r in broken if r != 3]]).any()
+    assert not dx[3].any() and not dx[8].any() and loss[8] == 0
+    assert torch.equal(_bits(got[1]), _bits(ref_[1]))
+    same = [r for r in range(rows) if r not in (1, 3, 4, 7, 8)]
+    assert torch.equal(_bits(got[0][same]), _bits(ref_[0][same])) and torch.equal(_bits(got[2][same]), _bits(ref_[2][same]))
