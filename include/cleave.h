@@ -577,6 +577,8 @@ CLEAVE_API int cleave_layernorm_backward(const cleave_layernorm_backward_t* d, v
  *   lse = log sum_j exp(s x_j)      logp = s x_t - lse for the token t      entropy = -sum_j p_j log p_j
  *   top_index, top_values: the `top` places of the largest scores, largest first and of equal ones the lowest place first,
  *   and their log probabilities s x - lse.
+ * logp and top_values are formed from differences to the largest score, not from the rounded lse: they are as exact at scores of
+ * 30000 as near 0, and not above 0.
  * Every output may be NULL, but not all.  x: bf16 or fp32.  top: 0 to CLEAVE_TOP_MOST and at most cols.
  * A score that is not masked has s x within fp32's range.  A masked place (-infinity) has probability 0.  A row without a score above -2^126 (all places masked, by -infinity or the type's
  * lowest value) has lse = -infinity, logp = -infinity, entropy 0, top_values -infinity, and no gradient.  A row
@@ -600,6 +602,7 @@ CLEAVE_API int cleave_logprobs(const cleave_logprobs_t* d, void* stream);
 
 /* Its backward pass, from the scores and the saved lse (and entropy, where dentropy is given):
  *   dx_j = s (dlogp ([j = t] - p_j) + dlse p_j - dentropy p_j (log p_j + entropy))
+ * p is formed from lse as it is given: in fp32 its relative error is up to 2^-24 |lse|, besides that of the exponent itself.
  * dlogp, dlse, dentropy [device, rows] fp32: each may be NULL (zeros).  dx (bf16 or fp32) may be x's buffer when types and
  * leading dimensions agree.  Cross entropy is dlogp = -1 / (number of tokens); what dlse carries is a penalty on lse. */
 typedef struct {

@@ -66,12 +66,20 @@ __device__ __forceinline__ Sums warp_join(Sums a, float c) {
     return a;
 }
 __device__ __forceinline__ Sums nothing() { return {-INFINITY, 0.f, 0.f, 0.f}; }
-struct Stats { float lse, entropy; };
+// lse, entropy, and what log p is formed from: log p = scale (x - top) - rest.  (From lse, which is rounded at its own size, it would be
+// off by 7e-4 at scores of 30000, and above 0 for a sure token.)
+struct Stats { float lse, entropy, top, rest; };
 __device__ __forceinline__ Stats stats_of(const Sums& a, float scale, float c) {
-    if (a.m <= kMasked) return {-INFINITY, 0.f};
-    if (!(a.m < INFINITY)) return {__uint_as_float(0x7FFFFFFFu), __uint_as_float(0x7FFFFFFFu)};
+    const float nan = __uint_as_float(0x7FFFFFFFu);
+    if (a.m <= kMasked) return {-INFINITY, 0.f, 0.f, 0.f};
+    if (!(a.m < INFINITY)) return {nan, nan, nan, nan};
     const float bits = log2f(a.s);
-    return {fmaf(scale, a.m, kLn2 * bits), fmaxf(kLn2 * (bits - a.t / a.s), 0.f)};
+    // (the largest score's own term is 1: a sum below that is rounding)
+    return {fmaf(scale, a.m, kLn2 * bits), fmaxf(kLn2 * (bits - a.t / a.s), 0.f), a.m, fmaxf(kLn2 * bits, 0.f)};
+}
+__device__ __forceinline__ float log_p(float x, float scale, const Stats& r) {
+    if (r.lse == -INFINITY) return -INFINITY;
+    return fmaf(2.f * scale, 0.5f * x - 0.5f * r.top, -r.rest);      // (halves: the difference of scores of both signs may pass fp32's range)
 }
 
 // ---- 16 bytes of scores ------------------------------------------------------------------------------------
@@ -482,13 +490,13 @@ __global__ void __launch_bounds__(THREADS, TOP ? kTopThreads / THREADS : kSumThr
         if (threadIdx.x == 0) {
             if (d.lse) d.lse[row] = r.lse;
             if (ENT && d.entropy) d.entropy[row] = r.entropy;
-            if (d.logp) d.logp[row] = token < 0 ? 0.f : (r.lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[token]), -r.lse));
+            if (d.logp) d.logp[row] = token < 0 ? 0.f : log_p(to_f32(x[token]), d.scale, r);
         }
         if constexpr (TOP) {
             const uint64_t* best = parts > 1 ? top_room.joined : top_room.best;
             if (threadIdx.x < d.top) {
                 if (d.top_index) d.top_index[row * d.ldti + threadIdx.x] = (int32_t)place_of(best[threadIdx.x]);
-                if (d.top_values) d.top_values[row * d.ldtv + threadIdx.x] = r.lse == -INFINITY ? -INFINITY : fmaf(d.scale, score_of(best[threadIdx.x]), -r.lse);
+                if (d.top_values) d.top_values[row * d.ldtv + threadIdx.x] = log_p(score_of(best[threadIdx.x]), d.scale, r);
             }
         }
     }
@@ -723,15 +731,15 @@ __global__ void __launch_bounds__(THREADS, kSumThreads / THREADS) distill_kernel
     Sums a = row_part<T, false, false, THREADS>(x, d.cols, c, part, parts, warps, nullptr, 0);
     if (parts > 1) a = cluster_join<false>(a, c, part, parts, &whole);
     if (part == 0) {
-        const float lse = stats_of(a, d.scale, c).lse;
+        const Stats r = stats_of(a, d.scale, c);
         float term = 0.f;
         teacher<THREADS>(d, row, [&](uint32_t, uint32_t j, float q, float log_q) {
-            term = fmaf(q, log_q - (lse == -INFINITY ? -INFINITY : fmaf(d.scale, to_f32(x[j]), -lse)), term);
+            term = fmaf(q, log_q - log_p(to_f32(x[j]), d.scale, r), term);
         });
         term = cta_sum(term, buf);
         if (threadIdx.x == 0) {
             d.loss[row] = term;
-            if (d.lse) d.lse[row] = lse;
+            if (d.lse) d.lse[row] = r.lse;
         }
     }
     if (parts > 1) cluster_arrive_wait();

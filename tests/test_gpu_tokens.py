@@ -818,3 +818,44 @@ def test_distill_of_a_teacher_with_nan_and_infinities(cl, k, x_t, t_t, normalize
     assert torch.equal(_bits(got[1]), _bits(ref_[1]))
     same = [r for r in range(rows) if r not in (1, 3, 4, 7, 8)]
     assert torch.equal(_bits(got[0][same]), _bits(ref_[0][same])) and torch.equal(_bits(got[2][same]), _bits(ref_[2][same]))
+
+
+@pytest.mark.parametrize("shift", [0.0, 300.0, 3000.0, 30000.0, -30000.0])
+@pytest.mark.parametrize("vocab", [700, 50257])
+@pytest.mark.parametrize("x_t,scale", [("f32", 0.7), ("bf16", 1.0)])
+def test_log_probabilities_of_rows_far_from_zero(cl, shift, vocab, x_t, scale):
+    """log p = scale (x - largest) - log(sum): its error is that of these two, however large the scores are; never above 0.  A term e^d
+    is off by (4 + 3 |d|) U, their sum by 64 U more; the logarithm by 4 U, the difference and the last sum by U each."""
+    rng = np.random.default_rng(vocab)
+    rows, top, s = 20, 8, float(np.float32(scale))
+    x = rng.normal(size=(rows, vocab)) * 3 + shift
+    x[:6, 5] = shift + 40.0                                                 # sure of one place
+    x[6:9] = shift
+    x[9, 3] = -INF
+    x = torch.tensor(x, dtype=torch.float32).to(DT[x_t]).to(_dev())
+    x64 = _f64(x)
+    tokens = rng.integers(0, vocab, size=rows)
+    tokens[:3], tokens[9] = 5, 3
+    tokens[10:] = x64[10:].argmax(axis=1)
+    w_logp, w_lse, _, w_tv, w_ti = ref.logprobs(x64, tokens, s, top)
+    ed, _, _ = _row_spread(x64, s)
+    rest = w_lse - s * x64.max(axis=1)
+    sums = SUM + (4 + 3 * ed) * U + 4 * U * np.abs(rest)
+    far = lambda at: np.where(np.isfinite(at), np.abs(s * (at - x64.max(axis=1, keepdims=True))), 0.0)  # noqa: E731
+    f = lambda: torch.full((rows,), float("nan"), device=_dev())  # noqa: E731
+    logp, lse, tv = f(), f(), torch.empty(rows, top, device=_dev())
+    cl.token_logprobs(x, torch.tensor(tokens, device=_dev()), logp, lse=lse, top_values=tv, scale=scale)
+    _close(logp, w_logp, sums + 2 * U * far(np.take_along_axis(x64, tokens[:, None], 1))[:, 0], "logp")
+    _close(tv, w_tv, sums[:, None] + 2 * U * far(np.take_along_axis(x64, w_ti, 1)), "top values")
+    assert (logp <= 0).all() and (tv <= 0).all()
+    alone = f()
+    cl.token_logprobs(x, torch.tensor(tokens, device=_dev()), alone, scale=scale)
+    assert torch.allclose(alone, logp, rtol=2 * SUM, atol=2 * SUM)          # (another number of CTAs a row)
+    # a teacher that is as sure: the loss is a difference of logarithms as small as these
+    values = _put(rng.normal(size=(rows, top)), torch.float32)
+    loss = f()
+    cl.distill(x, torch.tensor(w_ti, device=_dev()), values, loss, scale=scale)
+    w_loss, _, size = ref.distill(x64, w_ti, _f64(values), s, True)
+    spread = np.abs(s * _f64(values)).max(axis=1)
+    q_err = SUM + (4 + 6 * spread) * U
+    _close(loss, w_loss, size * (q_err + 4 * U) + sums + q_err + 2 * U * far(np.take_along_axis(x64, w_ti, 1)).max(axis=1), "loss")
