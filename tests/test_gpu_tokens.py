@@ -859,3 +859,30 @@ def test_log_probabilities_of_rows_far_from_zero(cl, shift, vocab, x_t, scale):
     spread = np.abs(s * _f64(values)).max(axis=1)
     q_err = SUM + (4 + 6 * spread) * U
     _close(loss, w_loss, size * (q_err + 4 * U) + sums + q_err + 2 * U * far(np.take_along_axis(x64, w_ti, 1)).max(axis=1), "loss")
+
+
+@pytest.mark.parametrize("cols", [41, 47, 61, 328, 440, 776, 856, 1001, 2568, 4112, 5120, 9224, 16376, 20560])
+@pytest.mark.parametrize("x_t", ["bf16", "f32"])
+@pytest.mark.parametrize("pad", [0, 3])
+def test_layernorm_of_constant_rows_of_any_length(cl, cols, x_t, pad):
+    """The sum of a row of ones is exact and so is its mean, whether or not the length has an exact reciprocal: y is the bias, however
+    small eps is.  A constant dy has no gradient where the normalised values have mean 0."""
+    rng = np.random.default_rng(cols)
+    b = _rand(rng, cols, torch.float32)
+    half, one = torch.full((5, cols), 0.5, device=_dev()), torch.ones(5, cols, dtype=DT[x_t], device=_dev())
+    mean, rstd, scale = (torch.empty(5, device=_dev()) for _ in range(3))
+    for eps in (1e-5, 1e-12):
+        for x, r in ((one, None), (half.to(DT[x_t]), half)):
+            y, _ = _room(5, cols, torch.float32, pad)
+            cl.layernorm(x, None, b, y, residual=r, mean=mean, rstd=rstd, eps=eps)
+            assert torch.all(mean == 1) and torch.equal(y, b.expand(5, -1))
+            assert torch.all((rstd * eps ** 0.5 - 1).abs() < 1e-6)
+        code = torch.empty(5, cols, dtype=torch.float8_e4m3fn, device=_dev())
+        cl.layernorm(one, None, None, code, scale=scale, eps=eps)
+        assert not scale.any() and not code.float().any()
+    h = torch.ones(5, cols, device=_dev())
+    h[:, 1::2] = -1.0
+    h[:, -1] = 0.0 if cols % 2 else -1.0
+    dx, _ = _room(5, cols, torch.float32, pad)
+    cl.layernorm_backward(one, h, None, torch.zeros(5, device=_dev()), torch.full((5,), 1e6, device=_dev()), dx)
+    assert not dx.any()
