@@ -532,7 +532,8 @@ CLEAVE_API int cleave_embedding_backward(const cleave_embedding_backward_t* d, v
 
 /* Layer norm with the residual's addition.  Per row, in fp32:
  *   h = x + r      mean = mean_j h_j      rstd = (mean_j (h_j - mean)^2 + eps)^(-1/2)      y_j = (h_j - mean) rstd w_j + b_j
- * The variance is formed from differences to the mean, never as a difference of squares.  r, h, w, y, the E4M3 codes and their
+ * The variance is formed from differences to the mean, never as a difference of squares; where their squares pass fp32's range
+ * (differences beyond 2^63) rstd is 0.  r, h, w, y, the E4M3 codes and their
  * scale as in cleave_rmsnorm; b (bf16 or fp32) may be absent (zeros), mean and rstd [device, rows] may be NULL. */
 typedef struct {
     uint64_t rows;

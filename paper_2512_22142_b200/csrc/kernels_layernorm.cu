@@ -611,8 +611,8 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
         const float2 both = row_sums(sum_of(sums) + edge_q, fmaf(edge_q, edge_c, sum_of(dots)), parts[it & 1]);
         fetch(at);
         at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
-        // dx = rstd q - rstd mean(q) - (rstd^3 mean(q (h - mean))) (h - mean)
-        const float shift = rstd * inv_cols.mean(both.x), along = rstd * (rstd * (rstd * (both.y * inv_cols.first)));
+        // dx = rstd (q - mean(q) - (rstd (rstd mean(q (h - mean)))) (h - mean)) + dres        (rstd^3 by itself is infinite for small rows)
+        const float shift = inv_cols.mean(both.x), along = rstd * (rstd * (both.y * inv_cols.first));
         const F2 shift2 = f2(-shift, -shift), along2 = f2(-along, -along);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -620,15 +620,18 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
             F2 dx[4], h[4];
             unpack8(rh[v], h);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) dx[i] = fma2(along2, add2(h[i], mean2), fma2(rstd2, q[v][i], shift2));
+            for (int i = 0; i < 4; ++i) dx[i] = fma2(along2, add2(h[i], mean2), add2(q[v][i], shift2));
             if (res) {
                 unpack8(rr[v], h);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) dx[i] = add2(dx[i], h[i]);
+                for (int i = 0; i < 4; ++i) dx[i] = fma2(rstd2, dx[i], h[i]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) dx[i] = mul2(rstd2, dx[i]);
             }
             store8(pdx + v * nt * 8, dx);
         }
-        if (EDGES && edge < d.cols) store_one(static_cast<H*>(d.dx) + row * d.lddx + edge, fmaf(-along, edge_c, fmaf(rstd, edge_q, -shift)) + edge_res);
+        if (EDGES && edge < d.cols) store_one(static_cast<H*>(d.dx) + row * d.lddx + edge, fmaf(rstd, fmaf(-along, edge_c, edge_q - shift), edge_res));
         pdx += stride * d.lddx;
     }
     if (!d.dw && !d.db) return;

@@ -886,3 +886,31 @@ def test_layernorm_of_constant_rows_of_any_length(cl, cols, x_t, pad):
     dx, _ = _room(5, cols, torch.float32, pad)
     cl.layernorm_backward(one, h, None, torch.zeros(5, device=_dev()), torch.full((5,), 1e6, device=_dev()), dx)
     assert not dx.any()
+
+
+@pytest.mark.parametrize("cols", [40, 264, 1000, 1032, 2600, 5120, 9000, 20000])
+@pytest.mark.parametrize("pad", [0, 3])
+@pytest.mark.parametrize("size", [2.0 ** -66, 2.0 ** -40])
+def test_layernorm_of_very_small_rows(cl, cols, pad, size):
+    """With eps = 0 the normalised values do not know the rows' size: y of size h is that of h to the bit (size a power of two), and dx that of
+    h, over the size.  (Squares of 2^-66 are 2^-132: what of them is lost below 2^-149 is 2^-17 of one at most, and 64 U of their sum.)"""
+    rng = np.random.default_rng(cols)
+    h = _lay(_rand(rng, (9, cols), torch.float32), pad)
+    hs = _lay(h * size, pad)
+    dy, w = _lay(100 * _rand(rng, (9, cols), torch.float32), pad), _rand(rng, cols, torch.float32, 0.2) + 1
+    out = []
+    for x in (h, hs):
+        y, mean, rstd = _lay(torch.empty_like(h), pad), torch.empty(9, device=_dev()), torch.empty(9, device=_dev())
+        cl.layernorm(x, None, None, y, mean=mean, rstd=rstd, eps=0.0)
+        dx, dw, db = _lay(torch.empty_like(h), pad), torch.empty(cols, device=_dev()), torch.empty(cols, device=_dev())
+        out.append((y, mean, rstd, dx, dw, db))
+    y, mean, rstd, _, _, _ = out[0]
+    y2, mean2, rstd2, _, _, _ = out[1]
+    lost = 2.0 ** -17
+    assert torch.equal(mean2, mean * size) and ((rstd2.double() * size / rstd - 1).abs() <= lost + SUM).all()
+    assert ((y2 - y).abs() <= (lost + SUM) * y.abs()).all()
+    for x, m, r, (_, _, _, dx, dw, db) in ((h, mean, rstd, out[0]), (hs, mean * size, rstd / size, out[1])):
+        cl.layernorm_backward(dy, x, w, m, r, dx, dw, db)
+    (_, _, _, dx, dw, db), (_, _, _, dx2, dw2, db2) = out
+    assert torch.isfinite(dx).all() and torch.isfinite(dx2).all()
+    assert torch.equal(db2, db) and torch.equal(dw2, dw) and torch.equal(dx2 * size, dx)
