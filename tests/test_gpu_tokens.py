@@ -914,3 +914,94 @@ def test_layernorm_of_very_small_rows(cl, cols, pad, size):
     (_, _, _, dx, dw, db), (_, _, _, dx2, dw2, db2) = out
     assert torch.isfinite(dx).all() and torch.isfinite(dx2).all()
     assert torch.equal(db2, db) and torch.equal(dw2, dw) and torch.equal(dx2 * size, dx)
+
+
+@pytest.mark.parametrize("n,vocab,cols", [(1, 9, 1), (40, 17, 264), (900, 500, 33), (4097, 300, 72), (30000, 3, 24), (2000, 20000, 7)])
+@pytest.mark.parametrize("dy_t,ids,pad,shift", [("bf16", "i32", 3, 1), ("f32", "i64", 5, 3), ("bf16", "i64", 1, 0), ("f32", "i32", 0, 7)])
+def test_embedding_backward_into_a_bf16_table_with_a_pitch(cl, n, vocab, cols, dy_t, ids, pad, shift):
+    """Integers: their sums are exact in fp32 in any order, and each row is rounded to bf16 once; what lies between the rows and before
+    the table stays."""
+    rng = np.random.default_rng(n + cols)
+    tokens = _spread_tokens(rng, n, vocab, "ranks")
+    dy = _lay(_put(rng.integers(-8, 9, size=(n, cols)), DT[dy_t]), pad, shift)
+    t = torch.tensor(tokens, dtype=DT[ids], device=_dev())
+    ok = (t >= 0) & (t < vocab)
+    want = torch.zeros(vocab, cols, dtype=torch.float64, device=_dev()).index_add_(0, t[ok].long(), dy[ok].double()).float()
+    before = _put(rng.integers(-8, 9, size=(vocab, cols)), torch.bfloat16)
+    store = torch.full((shift + vocab * (cols + pad),), 7.0, dtype=torch.bfloat16, device=_dev())
+    whole = store[shift:].view(vocab, cols + pad)
+    dt = whole[:, :cols]
+    for accumulate, result in ((False, want.bfloat16()), (True, (before.float() + 2 * want).bfloat16())):
+        dt.copy_(before)
+        cl.embedding_backward(dy, t, dt, scale=2.0 if accumulate else 1.0, accumulate=accumulate)
+        assert torch.equal(dt, result)
+        _untouched(whole, cols)
+        assert torch.all(store[:shift] == 7.0)
+
+
+@pytest.mark.parametrize("x_t", ["bf16", "f32"])
+def test_scores_of_more_rows_than_a_grid_has(cl, x_t):
+    """65535 rows are a grid's second dimension, what is above goes to the third: rows on both sides, the last one and the first are as
+    by themselves, all of them right, and nothing behind them is written."""
+    rows, vocab, k, behind = 65535 + 7, 41, 5, 3
+    gen = torch.Generator(device=_dev()).manual_seed(2)
+    x = torch.randn(rows, vocab, generator=gen, device=_dev()).mul_(2).to(DT[x_t])
+    t = torch.randint(-1, vocab, (rows,), generator=gen, device=_dev())
+    index, values = torch.randint(-1, vocab, (rows, k), generator=gen, device=_dev()), torch.randn(rows, k, generator=gen, device=_dev())
+    up = torch.randn(rows, generator=gen, device=_dev())
+
+    def outputs(a, b):
+        n = b - a
+        f = lambda *s, d=torch.float32: torch.full((n + behind, *s), 7, dtype=d, device=_dev())  # noqa: E731
+        out = dict(logp=f(), lse=f(), H=f(), lse2=f(), tv=f(k), ti=f(k, d=torch.int32), dx=f(vocab, d=DT[x_t]), loss=f(), lse3=f(), dx2=f(vocab, d=DT[x_t]))
+        o = {q: v[:n] for q, v in out.items()}
+        cl.token_logprobs(x[a:b], t[a:b], o["logp"], lse=o["lse"], entropy=o["H"])
+        cl.token_logprobs(x[a:b], lse=o["lse2"], top_values=o["tv"], top_index=o["ti"])
+        cl.token_logprobs_backward(x[a:b], t[a:b], o["lse"], o["dx"], dlogp=up[a:b], dentropy=up[a:b], entropy=o["H"])
+        cl.distill(x[a:b], index[a:b], values[a:b], o["loss"], lse=o["lse3"])
+        cl.distill_backward(x[a:b], index[a:b], values[a:b], o["lse"], up[a:b], o["dx2"])
+        assert all(torch.all(v[n:] == 7) for v in out.values())
+        return o
+
+    whole = outputs(0, rows)
+    for a, b in ((0, 9), (65530, 65536), (65536, rows), (rows - 1, rows)):
+        for q, v in outputs(a, b).items():
+            assert torch.equal(_bits(whole[q][a:b]), _bits(v)), (q, a)
+    lp = torch.log_softmax(x.double(), 1)
+    assert torch.allclose(whole["lse"].double(), torch.logsumexp(x.double(), 1), rtol=SUM, atol=SUM)
+    assert torch.allclose(whole["logp"].double(), torch.where(t >= 0, lp.gather(1, t.clamp_min(0)[:, None])[:, 0], 0.0), rtol=SUM, atol=SUM)
+    assert torch.equal(whole["ti"].long(), x.double().sort(dim=1, descending=True, stable=True).indices[:, :k])
+
+
+@pytest.mark.parametrize("vocab,k", [(300, 64), (50257, 20), (4097, 1)])
+@pytest.mark.parametrize("x_t", ["bf16", "f32"])
+def test_top_places_are_a_teacher(cl, vocab, k, x_t):
+    """A teacher's best places and their log probabilities, as token_logprobs leaves them, teach a student without normalizing; the teacher
+    itself has nothing left to learn: its loss is 0 and its gradient what the places that are not among the best have of the sum."""
+    rng = np.random.default_rng(vocab + k)
+    rows = 24
+    teacher, student = _scores(rng, rows, vocab, x_t, False), _scores(rng, rows, vocab, x_t, False)
+    student[:, torch.isinf(teacher[0])] = -INF
+    student[:, ~torch.isinf(teacher[0])] = student[:, ~torch.isinf(teacher[0])].clamp_min(-9.0)      # a place that the teacher names is not masked
+    tv, ti = torch.empty(rows, k, device=_dev()), torch.empty(rows, k, dtype=torch.int32, device=_dev())
+    f = lambda: torch.full((rows,), float("nan"), device=_dev())  # noqa: E731
+    cl.token_logprobs(teacher, top_values=tv, top_index=ti)
+    dloss = _rand(rng, rows, torch.float32)
+    at, v64 = ti.cpu().numpy().astype(np.int64), _f64(tv)
+    for x in (student, teacher):
+        loss, lse, dx = f(), f(), torch.empty(rows, vocab, device=_dev())
+        cl.distill(x, ti, tv, loss, lse=lse, normalize=False)
+        cl.distill_backward(x, ti, tv, lse, dloss, dx, normalize=False)
+        x64 = _f64(x)
+        w_loss, _, size = ref.distill(x64, at, v64, 1.0, False)
+        lse_tol, _ = _statistics_tolerance(x64, 1.0)
+        q_err = SUM + (4 + 6 * np.abs(v64).max(axis=1)) * U                 # (as in test_distill)
+        biggest = np.array([np.abs(r[np.isfinite(r)]).max() for r in x64])
+        _close(loss, w_loss, size * (q_err + 4 * U) + lse_tol + q_err + 4 * U * biggest, "loss")
+        want, terms = ref.distill_backward(x64, at, v64, _f64(lse), _f64(dloss), 1.0, False)
+        far = np.where(np.isfinite(x64), np.abs(x64 - _f64(lse)[:, None]), 0.0)
+        _close(dx, want, terms * ((3 * far + 16) * U + q_err[:, None]) + 1e-37, "dx")
+    # (the teacher against itself: each term is the difference of two equal logarithms)
+    assert (np.abs(w_loss) <= 2 * U * (np.abs(v64).max(axis=1) + 1)).all()
+    named = torch.zeros(rows, vocab, dtype=torch.bool, device=_dev()).scatter_(1, ti.long(), True)
+    assert torch.all((dx * dloss[:, None])[~named] >= 0)
