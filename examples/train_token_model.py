@@ -152,15 +152,19 @@ def teacher_of(targets, vocab, k=8):
     return at.to(torch.int32), values.contiguous()
 
 
-def train(steps=60, teacher=False, lr=2e-3, seed=0, **size):
-    """Mean losses of `steps` steps."""
-    model = Model(seed=seed, **size)
+def optimizer(model):
+    """AdamW over all of the model's parameters, in their order."""
     names = list(model.params)
     params = [model.params[k].view(-1) for k in names]
     copies = [None if model.copies[k] is None else model.copies[k].view(-1) for k in names]
-    opt = cl.AdamW(params, [model.grads[k].view(-1) for k in names], [torch.zeros_like(p) for p in params], [torch.zeros_like(p) for p in params],
-                   copies=copies, weight_decay=[model.decay[k] for k in names])
-    losses = []
+    return cl.AdamW(params, [model.grads[k].view(-1) for k in names], [torch.zeros_like(p) for p in params], [torch.zeros_like(p) for p in params],
+                    copies=copies, weight_decay=[model.decay[k] for k in names])
+
+
+def train(steps=60, teacher=False, lr=2e-3, seed=0, **size):
+    """Mean losses of `steps` steps."""
+    model = Model(seed=seed, **size)
+    opt, losses = optimizer(model), []
     for step in range(1, steps + 1):
         tokens, targets = batch(model, step, seed)
         losses.append(model.step(tokens, targets, teacher_of(targets, model.vocab) if teacher else None).mean())

@@ -57,3 +57,34 @@ def test_training_runs(with_teacher):
     from train_token_model import train
     losses = train(steps=6, teacher=with_teacher, seed=1, **SIZE)
     assert len(losses) == 6 and all(v == v and abs(v) < 1e3 for v in losses)
+
+
+@pytest.mark.parametrize("with_teacher", [False, True])
+def test_updates_reach_the_next_step(with_teacher):
+    """The weights after each step are AdamW's of the step's own gradients, to the bit, in the copies that the products read too; the
+    second step's loss and gradients are those of the updated weights (tolerances as in test_a_steps_loss_and_gradients)."""
+    from oracle import ops as ref
+    from train_token_model import Model, batch, optimizer, teacher_of
+    model = Model(seed=6, **SIZE)
+    opt, lr = optimizer(model), 2e-3
+    flat = lambda t: t.detach().float().cpu().numpy().ravel()  # noqa: E731
+    state = {k: (0 * flat(p), 0 * flat(p)) for k, p in model.params.items()}
+    for step in (1, 2):
+        tokens, targets = batch(model, step, 6)
+        teacher = teacher_of(targets, model.vocab) if with_teacher else None
+        want, grads = _torch_step(model, tokens, targets, teacher)
+        got = model.step(tokens, targets, teacher)
+        assert float((got - want).abs().max()) < 0.15
+        for k, g in model.grads.items():
+            off = float((g - grads[k]).norm() / grads[k].norm())
+            assert off < 0.03, f"step {step}, {k}: {off:.4f}"
+        before = {k: (flat(p), flat(model.grads[k])) for k, p in model.params.items()}
+        opt.step(step=step, lr=lr)
+        torch.cuda.synchronize()
+        for k, p in model.params.items():
+            new, m, v = ref.adamw(*before[k], *state[k], lr=lr, beta1=0.9, beta2=0.999, eps=1e-8, step=step, weight_decay=model.decay[k])
+            state[k] = m, v
+            assert (flat(p) == new).all() and (new != before[k][0]).any(), f"step {step}, {k}"
+            if model.copies[k] is not None:
+                assert torch.equal(model.copies[k], p.to(torch.bfloat16)), f"step {step}, {k}"
+    model.check()
