@@ -7,9 +7,10 @@
 //          only, so the ring needs no barrier of its own and the bytes in flight do not depend on registers.
 //   own    operands that disagree, and short rows, up to 8192 columns: neighbouring threads own neighbouring columns, held in registers.
 //   any    what is left: the row is taken again in each pass (it stays in L1 / L2).
-// Measured: 8192 x 768 with an fp32 residual 16.8 us (4.5 TB/s: 75 MB are read and written in the time of few rows a warp), 8192 x 8192 into E4M3 80 us
-// (5.9 TB/s), one row of 4096 a launch, 4.4 us with the call; backward of 16384 x 5120 with dw and db 125 to 131 us (5.1 to 5.4 TB/s, the sums of
-// the CTAs' shares among them).  Rows of odd length: 1899 x 8962 fp32 70 us (3.9 TB/s), backward of 12216 x 3349 93 to 99 us (3.3 to 3.5 TB/s).
+// Measured: 8192 x 768 with an fp32 residual 15.4 us (4.9 TB/s: 75 MB are read and written in the time of few rows a warp), 8192 x 8192 with a bf16 residual
+// into E4M3 81 to 87 us (5.4 to 5.8 TB/s), one row of 4096 a launch, 4.4 us with the call; backward of 16384 x 5120 with dw and db 123 to 125 us
+// (5.4 TB/s, the sums of the CTAs' shares among them), with an fp32 h and bf16 dy 282 us (4.2 TB/s).  Rows of odd length: 1899 x 8962 fp32 with a residual
+// 64 us (4.2 TB/s), backward of 12216 x 3349 bf16 90 us (3.6 TB/s).
 #include <algorithm>
 #include <initializer_list>
 #include <type_traits>
@@ -36,6 +37,33 @@ __device__ __forceinline__ void load_vector8(const void* p, uint32_t type, uint3
     } else {
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = f2(fill, fill);
+    }
+}
+// the same of all of a thread's groups, at the columns col, col + step, ...: every load is asked for before any is unpacked
+// (a choice of type group by group let each group's loads wait for the one's before: 8192 x 768 17.2 us in place of 15.4)
+template <int V>
+__device__ __forceinline__ void load_vectors8(const void* p, uint32_t type, uint32_t col, uint32_t step, const bool (&live)[V], float fill, F2 (&x)[V][4]) {
+    if (type == CLEAVE_T_NONE) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[v][i] = f2(fill, fill);
+    } else if (((uintptr_t)p + (uint64_t)col * (type == CLEAVE_T_F32 ? 4 : 2)) & 15u) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) if (live[v]) load_vector8(p, type, col + v * step, fill, x[v]);
+    } else if (type == CLEAVE_T_F32) {
+        Raw8<float> r[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (live[v]) { const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + col + v * step); r[v].w[0] = q[0]; r[v].w[1] = q[1]; }
+#pragma unroll
+        for (int v = 0; v < V; ++v) unpack8(r[v], x[v]);
+    } else {
+        Raw8<__nv_bfloat16> r[V];
+#pragma unroll
+        for (int v = 0; v < V; ++v) if (live[v]) r[v].w[0] = *reinterpret_cast<const uint4*>(static_cast<const __nv_bfloat16*>(p) + col + v * step);
+#pragma unroll
+        for (int v = 0; v < V; ++v) unpack8(r[v], x[v]);
     }
 }
 __device__ __forceinline__ float sum_of(F2 a) { const float2 h = halves(a); return h.x + h.y; }
@@ -176,10 +204,11 @@ __global__ void __launch_bounds__(T) layernorm_own_kernel(const __grid_constant_
 // ---- forward, wide -----------------------------------------------------------------------------------
 // V groups of 8 columns per thread.  WARP: blockDim (32, 8), a warp per row; otherwise a CTA per row.  A row has a ring of `stages` of the
 // next ones in shared memory, [stage][operand][group] with a thread's groups blockDim.x apart, and weights and biases stay in registers
-// over all rows.  Warps an SM: 24 of two groups, 16 of four (8192 x 8192 into E4M3 80 us; with 1024 threads of two groups, whose
-// registers hold no weights, 133); 8 warps with a row each, all registers theirs (8192 x 768 17.0 us; a warp's row at a time without a ring 18.2).
+// over all rows.  Warps an SM: 24 of two groups, 16 of four (8192 x 8192 with a bf16 residual into E4M3 81 us; with 512 threads of two
+// groups 84); 8 warps with a row each, all registers theirs (8192 x 768 15.4 us; with one row ahead 16.8).
+// EDGES: rows that do not begin or end with a line (their threads hold more: 8192 x 2048 bf16 33 us in place of 26).
 constexpr int row_warps(int V) { return V <= 2 ? 24 : 16; }
-template <typename X, typename R, typename Y, int V, bool WARP, int T>
+template <typename X, typename R, typename Y, int V, bool WARP, int T, bool EDGES>
 __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm_wide_kernel(const __grid_constant__ cleave_layernorm_t d, uint32_t stages, const Lines lines) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float parts[3][32];
@@ -189,7 +218,7 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
     const uint32_t tid = threadIdx.x, nt = blockDim.x;
     const uint64_t first = WARP ? (uint64_t)blockIdx.x * blockDim.y + threadIdx.y : blockIdx.x;
     const uint64_t stride = WARP ? (uint64_t)gridDim.x * blockDim.y : gridDim.x;         // (whole units of rows where rows differ: one head for all)
-    const uint32_t head = lines.head(first, d.cols), groups = (d.cols - head) / 8, edge = edge_column(tid, head, d.cols - head - groups * 8, d.cols);
+    const uint32_t head = EDGES ? lines.head(first, d.cols) : 0u, groups = (d.cols - head) / 8, edge = EDGES ? edge_column(tid, head, d.cols - head - groups * 8, d.cols) : d.cols;
     const uint32_t off_r = d.cols / 8 * BX, stage_bytes = off_r + d.cols / 8 * BR;
     const Reciprocal inv_cols(d.cols);
     bool live[V];
@@ -219,15 +248,14 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
     };
     for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
     F2 w[V][4], b[V][4];
-#pragma unroll
-    for (int v = 0; v < V; ++v)
-        if (live[v]) { load_vector8(d.w, d.w_type, head + (tid + v * nt) * 8, 1.f, w[v]); load_vector8(d.b, d.b_type, head + (tid + v * nt) * 8, 0.f, b[v]); }
+    load_vectors8<V>(d.w, d.w_type, head + tid * 8, nt * 8, live, 1.f, w);
+    load_vectors8<V>(d.b, d.b_type, head + tid * 8, nt * 8, live, 0.f, b);
     // the thread's single column: its weight and bias, and the next row's value
-    const float edge_w = edge < d.cols && d.w ? load_as(d.w, d.w_type, edge) : 1.f, edge_b = edge < d.cols && d.b ? load_as(d.b, d.b_type, edge) : 0.f;
+    const float edge_w = EDGES && edge < d.cols && d.w ? load_as(d.w, d.w_type, edge) : 1.f, edge_b = EDGES && edge < d.cols && d.b ? load_as(d.b, d.b_type, edge) : 0.f;
     X next_x = from_f32<X>(0.f);                                 // (as it is stored: a conversion would wait for the load)
     typename std::conditional<RES, R, X>::type next_r = from_f32<typename std::conditional<RES, R, X>::type>(0.f);
     auto ask_edge = [&](uint64_t row) {
-        if (edge < d.cols && row < d.rows) {
+        if (EDGES && edge < d.cols && row < d.rows) {
             next_x = static_cast<const X*>(d.x)[row * d.ldx + edge];
             if constexpr (RES) next_r = static_cast<const R*>(d.r)[row * d.ldr + edge];
         }
@@ -264,14 +292,14 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
             for (int i = 0; i < 4; ++i) sum = add2(sum, h[v][i]);
         }
         float lone = 0.f;
-        if (edge < d.cols) {
+        if (EDGES && edge < d.cols) {
             lone = to_f32(next_x);
             if constexpr (RES) lone += to_f32(next_r);
             if constexpr (RES) if (d.h) store_one(static_cast<R*>(d.h) + row * d.ldh + edge, lone);
             ask_edge(row + stride);
         }
         const float mean = inv_cols.mean(join(sum_of(sum) + lone, parts[0]));
-        if (edge < d.cols) lone -= mean;
+        if (EDGES && edge < d.cols) lone -= mean;
         fetch(at);                                               // (this thread has read its groups of this stage)
         at = at + stage_bytes == stages * stage_bytes ? 0 : at + stage_bytes;
 #pragma unroll
@@ -285,7 +313,7 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
             if (d.mean) d.mean[row] = mean;
             if (d.rstd) d.rstd[row] = rstd;
         }
-        if (edge < d.cols) lone = fmaf(lone * rstd, edge_w, edge_b);
+        if (EDGES && edge < d.cols) lone = fmaf(lone * rstd, edge_w, edge_b);
         float top = fabsf(lone);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
@@ -315,7 +343,7 @@ __global__ void __launch_bounds__(T, WARP ? 1 : row_warps(V) * 32 / T) layernorm
             }
             lone *= sc.y;
         }
-        if (edge < d.cols) store_one(static_cast<Y*>(d.y) + row * d.ldy + edge, lone);
+        if (EDGES && edge < d.cols) store_one(static_cast<Y*>(d.y) + row * d.ldy + edge, lone);
         py += stride * d.ldy;
         if (RES && ph) ph += stride * d.ldh;
     }
@@ -326,9 +354,9 @@ constexpr uint32_t kRingBytes = 64 * 1024;      // per CTA; three CTAs of 256 th
 constexpr uint32_t kRingMost = 208 * 1024;     // of all rings of a CTA
 constexpr uint32_t kWarpRing = 26 * 1024;       // of one of a CTA's eight warps
 
-template <typename X, typename R, typename Y, int V, bool WARP, int T>
-cudaError_t launch_wide(const cleave_layernorm_t& d, uint32_t threads, const Lines& lines, int sms, cudaStream_t st) {
-    auto kernel = layernorm_wide_kernel<X, R, Y, V, WARP, T>;
+template <typename X, typename R, typename Y, int V, bool WARP, int T, bool EDGES>
+cudaError_t launch_wide_edges(const cleave_layernorm_t& d, uint32_t threads, const Lines& lines, int sms, cudaStream_t st) {
+    auto kernel = layernorm_wide_kernel<X, R, Y, V, WARP, T, EDGES>;
     const uint32_t stage = d.cols / 8 * (Bytes8<X>::value + Bytes8<R>::value);
     static SmemLimit limit;
     const cudaError_t e = limit.raise(reinterpret_cast<const void*>(kernel), kRingMost);
@@ -343,6 +371,11 @@ cudaError_t launch_wide(const cleave_layernorm_t& d, uint32_t threads, const Lin
     uint64_t ctas = (uint64_t)sms * fit;
     if (lines.step) ctas = std::max<uint64_t>(8, ctas / 8 * 8);  // a CTA's rows begin alike
     return launch_chained(kernel, (unsigned)std::min((uint64_t)d.rows, ctas), threads, smem, st, d, stages, lines);
+}
+template <typename X, typename R, typename Y, int V, bool WARP, int T>
+cudaError_t launch_wide(const cleave_layernorm_t& d, uint32_t threads, const Lines& lines, int sms, cudaStream_t st) {
+    return lines.at || lines.step || d.cols % 8 ? launch_wide_edges<X, R, Y, V, WARP, T, true>(d, threads, lines, sms, st)
+                                                : launch_wide_edges<X, R, Y, V, WARP, T, false>(d, threads, lines, sms, st);
 }
 template <typename X, typename R, typename Y>
 cudaError_t launch_sizes(const cleave_layernorm_t& d, const Lines& lines, int sms, cudaStream_t st) {
@@ -384,9 +417,11 @@ cudaError_t launch_layernorm(const cleave_layernorm_t& d, int sms, cudaStream_t 
 // A CTA takes the rows part, part + parts, ...; its shares of dw and db go to row `part` of the workspace (fp32
 // [parts x 2 cols], dw's columns first; each element belongs to one thread), and layernorm_sum_parts_kernel adds the parts in order.
 // The wide form's shape: threads a row, groups of 8 columns a thread, rows that a CTA works on at a time.  What counts is work between two
-// barriers: many groups a thread and few threads (16384 rows of 4096 columns: 4 groups and 128 threads 91 us, 2 groups and 256
-// threads 111, one group and 512 threads 164); up to 1024 columns a row is one warp's.  A CTA an SM, with as many warps as registers allow
-// (16187 x 2968 bf16 with 3 groups and 12 warps 79 us, 4 groups and 6 warps 93; 8000 x 2600 fp32 90 and 73: its rows spill at 12 warps).
+// barriers: many groups a thread and few threads (16384 rows of 4096 columns: 4 groups and 128 threads 95 us, 2 groups and 256
+// threads 99); up to 1024 columns a row is one warp's.  A CTA an SM, with as many warps as registers allow
+// (16187 x 2968 bf16 with 3 groups and 12 warps 79 us, 4 groups and 6 warps 100; 8000 x 2600 with an fp32 h 77 and 62: its rows spill at 12 warps).
+// Not so everywhere: an fp32 h spills at other widths of one to three groups too (up to 768, 1025 to 1536 and 2049 to 2304 columns, 120 to 320 bytes a
+// thread), and every type above 8192 columns, with 512 threads (216 to 944 bytes; rows off lines spill more).
 struct Shape { uint32_t threads, groups, rows; };
 Shape backward_shape(uint32_t cols, bool f32) {                  // f32: h is, and takes more registers
     const uint32_t units = (cols + 7) / 8;
@@ -499,7 +534,7 @@ __global__ void __launch_bounds__(T) layernorm_backward_own_kernel(const __grid_
 // V groups of 8 columns a thread, blockDim.y rows at a time, each with a ring of the next rows of (dy, h, dres) in shared memory; the
 // weights (where registers hold them) and the shares of dw and db stay in registers over all rows, and the
 // CTA's rows add theirs at the end.
-// EDGES: rows that do not begin or end with a line (their threads hold more: 16384 x 5120 152 us in place of 127).
+// EDGES: rows that do not begin or end with a line (their threads hold more: 16384 x 5120 156 us in place of 123).
 template <typename D, typename H, int V, int T, bool EDGES>
 __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __grid_constant__ cleave_layernorm_backward_t d, float* __restrict__ ws, uint32_t stages, const Lines lines) {
     extern __shared__ __align__(16) uint8_t rings[];
@@ -546,10 +581,7 @@ __global__ void __launch_bounds__(T, 1) layernorm_backward_wide_kernel(const __g
     };
     for (uint32_t s = 0; s < stages; ++s) fetch(s * stage_bytes);
     F2 w[KEEP ? V : 1][4], dw[V][4], db[V][4];
-    if constexpr (KEEP) {
-#pragma unroll
-        for (int v = 0; v < V; ++v) if (live[v]) load_vector8(d.w, d.w_type, head + (tid + v * nt) * 8, 1.f, w[v]);
-    }
+    if constexpr (KEEP) load_vectors8<V>(d.w, d.w_type, head + tid * 8, nt * 8, live, 1.f, w);
     // the thread's single column: its weight, its shares, and the next row's values
     const float edge_w = EDGES && edge < d.cols && d.w ? load_as(d.w, d.w_type, edge) : 1.f;
     float edge_dw = 0.f, edge_db = 0.f;
@@ -687,7 +719,7 @@ __global__ void __launch_bounds__(1024) layernorm_sum_parts_kernel(const float* 
     __shared__ float s[32][33];
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, j = blockIdx.x * 32u + lane;
     float* out = blockIdx.y ? db : dw;
-    wait_for_primary();
+    wait_for_primary();                                          // (no early start for what follows: it would land on the SMs unevenly beside the kernel whose sums these are)
     if (!out) return;
     float v = 0.f;
     if (j < cols) {
