@@ -16,7 +16,8 @@
 // Bound by the HBM where the whole table is written, by the three launches' latencies where few rows are.  Measured, with tokens whose
 // frequency falls with their rank: 8192 tokens into the whole of a 50257 x 768 fp32 table 41.7 us (28 of them the zeros and, beside them,
 // the sorting; its bytes take 26), 16384 added to a 32000 x 4096 table 69 us (order 8, sum 50, join 9; its bytes take 44.5).  Lookup of
-// 16384 x 5120 bf16 37 us (6.0 TB/s), of 64 x 4096 4.3.
+// 16384 x 5120 bf16 37 us (6.0 TB/s), of 64 x 4096 4.3; rows off 16 bytes go by single elements (5119 columns, evenly spread tokens, 82 us
+// where 5120 take 51).
 //
 // Tried and not kept: zeros beside the sums instead of beside the sorting (82 us for the first of these); a run that ends soon behind its
 // chunk finished there instead of in pieces (77 us for the second: chunks of unlike length); ranges of the vocabulary as owners
@@ -206,8 +207,8 @@ __global__ void __launch_bounds__(kOrderThreads) token_order_kernel(const ID* id
 }
 
 // ---- gradient: sums --------------------------------------------------------------------------------------
-// Places a chunk: the most of 8, 16, 32 or 64 that leave eight CTAs an SM (8192 places of 768 columns 42.6 us with 8, 46 with 16; 16384 of 4096
-// columns 84 with 8, 77 with 16), because each chunk leaves up to two pieces; more where there would be more than kChunksMost, which
+// Places a chunk: the most of 8, 16, 32 or 64 that leave eight CTAs an SM (8192 places of 768 columns 41.9 us with 8, 44.4 with 16; 16384 of 4096
+// columns 76 with 8, 69 with 16; 2048 of 4096 20.5 and 22.7), because each chunk leaves up to two pieces; more where there would be more than kChunksMost, which
 // bounds the workspace.
 constexpr uint32_t kChunksMost = 16 * kPartSms;
 uint32_t sum_chunk(uint64_t n, uint32_t cols) {

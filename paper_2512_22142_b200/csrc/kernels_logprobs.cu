@@ -11,9 +11,9 @@
 // Backward: each element from its score and the row's lse; one reading, one writing.
 //
 // Bound: the forward pass by the HBM and, beside it, instruction issue (64 % of the cycles) and exponentials (one an element, half of what
-// the SM has at that rate); few rows by latency; the backward passes by the HBM.  Measured: 8192 x 50257 bf16 with entropy 141 to 158 us with
-// the GPU's clock (5.2 to 5.8 TB/s; 136 without entropy), the 20 best of 16 x 128000 fp32 16 us (6.3 without them), of 2048 rows 220 us;
-// gradient of 8192 x 128000 bf16 636 us (6.6 TB/s; a plain copy runs at 6.4); distillation, loss and gradient, 8192 x 32000 with 64
+// the SM has at that rate); few rows by latency; the backward passes by the HBM.  Measured: 8192 x 50257 bf16 with entropy 141 to 158 us from
+// GPU to GPU (5.2 to 5.8 TB/s; without entropy 130 to 136), the 20 best of 16 x 128000 fp32 16 us (6.3 without them), of 2048 rows 220 us;
+// gradient of 8192 x 128000 bf16 628 to 645 us (6.6 TB/s; a plain copy of as many bytes takes 635); distillation, loss and gradient, 8192 x 32000 with 64
 // places 267 to 281 us (5.7 TB/s).
 #include <algorithm>
 #include <type_traits>
@@ -254,8 +254,8 @@ __device__ __forceinline__ void merge(const uint64_t* pool, uint32_t lists, uint
 
 // ---- forward ---------------------------------------------------------------------------------------------------
 // Threads an SM: 48 registers each, 64 with top places; units a thread takes at once, with as many again under way: 3, 2 with top places.
-// (8192 x 50257 with entropy 149 us; two units and 1536 threads 152, four and 1024 154.  4096 rows in fp32 126, 134 and 126.  The 20 best of
-// 2048 x 128000 fp32 220 with two units, 273 with three.)
+// (8192 x 50257 with entropy 143 us; two units and 1536 threads 146, four and 1024 148.  4096 rows in fp32 126, 135 and 126; 600 rows of bf16 17, 20
+// and 23.  The 20 best of 2048 x 128000 fp32 220 with two units, 280 with three.)
 constexpr int kSumThreads = 1280, kTopThreads = 1024;
 constexpr float kSlack = 8.f;
 
@@ -504,16 +504,17 @@ __global__ void __launch_bounds__(THREADS, TOP ? kTopThreads / THREADS : kSumThr
 }
 
 // CTAs a row: as many as it takes, at 512 threads each, to fill the SMs once, each with 16 KB of scores at least.  (More would each
-// look for places of their own: the 20 best of 292 x 128864 fp32 with 8 CTAs a row 84 us.)
+// look for places of their own: the 20 best of 292 x 128864 fp32 take 45 us, with 8 CTAs a row 85.)
 uint32_t row_parts(uint64_t rows, uint64_t row_bytes, int sms, uint32_t sm_threads) {
     uint32_t parts = 1;
     while (parts < kPartsMost && rows * parts * 512 < (uint64_t)sms * sm_threads && row_bytes / (parts * 2) >= 16 * 1024) parts *= 2;
     return parts;
 }
-// Threads: as many as fill the SMs (16 x 128000 fp32 8 us with 512, 10 with 256); many rows go to CTAs of 128, whose joins cost
-// less (8192 x 50257 with entropy, two units a thread, 143 us against 152 with 256).
+// Threads: as many as fill the SMs (16 x 128000 fp32 6.3 us with 512, 8.8 with 256); many rows go to CTAs of 128, whose joins cost
+// less (8192 x 50257 with entropy 143 us against 154 with 256).  An SM holds sm_threads in CTAs of 128 or 256; of 512 without top places
+// it holds 1024, which the rule does not know: 42 rows of 128000 bf16 come in two rounds of CTAs (9.4 us; with 256 threads 6.7).
 struct RowGrid { dim3 cluster, grid; uint32_t threads; };
-RowGrid row_grid(uint64_t rows, uint64_t row_bytes, int sms, uint32_t sm_threads) {       // sm_threads: what an SM holds of the kernel
+RowGrid row_grid(uint64_t rows, uint64_t row_bytes, int sms, uint32_t sm_threads) {
     const uint32_t parts = row_parts(rows, row_bytes, sms, sm_threads), y = (uint32_t)std::min<uint64_t>(rows, 65535);
     const uint64_t held = (uint64_t)sms * sm_threads / (rows * parts);       // threads a CTA if all are to run at once
     const uint32_t least = (uint32_t)std::min<uint64_t>(row_bytes / parts / 32, 512);        // two units each at least
