@@ -1,5 +1,7 @@
 """The oracle of the operators on tokens, pinned: against torch's own functions in 64 bits, and the gradients against
 central differences of the forward passes."""
+import math
+
 import numpy as np
 import pytest
 import torch
@@ -96,3 +98,18 @@ def test_distill_and_its_gradient(normalize):
     if normalize:
         p, q = torch.log_softmax(torch.tensor(x) * 0.5, 1), torch.log_softmax(torch.tensor(t) * 0.5, 1)
         assert np.allclose(ref.distill(x, full, t, 0.5)[0], torch.nn.functional.kl_div(p, q, log_target=True, reduction="none").sum(1).numpy())
+
+
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+@pytest.mark.parametrize("normalize", [True, False])
+def test_a_broken_teacher_leaves_its_empty_entries_empty(bad, normalize):
+    index, values = np.array([3, 5, -1, 9, 2]), np.array([0.5, bad, bad, 0.1, -1.0])
+    q, log_q = ref.teacher(index, values, 9, 1.3, normalize)
+    live = [0, 1, 4]
+    with np.errstate(invalid="ignore"):
+        want = torch.softmax(torch.tensor(1.3 * values[live]), 0) if normalize else torch.exp(torch.tensor(1.3 * values[live]))
+    assert not q[[2, 3]].any() and np.all(log_q[[2, 3]] == -math.inf)
+    np.testing.assert_allclose(q[live], want.numpy(), rtol=1e-12)
+    x = np.linspace(-1, 1, 18).reshape(2, 9)
+    loss, _, _ = ref.distill(x, np.stack([index, [-1, -1, -1, -1, 10]]), np.stack([values, np.full(5, bad)]), 1.3, normalize)
+    assert not math.isfinite(loss[0]) and loss[1] == 0
