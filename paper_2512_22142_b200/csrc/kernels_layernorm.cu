@@ -8,8 +8,8 @@
 //   own    operands that disagree, and short rows, up to 8192 columns: neighbouring threads own neighbouring columns, held in registers.
 //   any    what is left: the row is taken again in each pass (it stays in L1 / L2).
 // Measured: 8192 x 768 with an fp32 residual 15.4 us (4.9 TB/s: 75 MB are read and written in the time of few rows a warp), 8192 x 8192 with a bf16 residual
-// into E4M3 81 to 87 us (5.4 to 5.8 TB/s), one row of 4096 a launch, 4.4 us with the call; backward of 16384 x 5120 with dw and db 123 to 125 us
-// (5.4 TB/s, the sums of the CTAs' shares among them), with an fp32 h and bf16 dy 282 us (4.2 TB/s).  Rows of odd length: 1899 x 8962 fp32 with a residual
+// into E4M3 81 to 87 us (5.4 to 5.8 TB/s), one row of 4096 a launch, 4.4 us with the call; backward of 16384 x 5120 with dw and db 123 to 130 us
+// (5.2 to 5.4 TB/s, the sums of the CTAs' shares among them), with an fp32 h and bf16 dy 282 us (4.2 TB/s).  Rows of odd length: 1899 x 8962 fp32 with a residual
 // 64 us (4.2 TB/s), backward of 12216 x 3349 bf16 90 us (3.6 TB/s).
 #include <algorithm>
 #include <initializer_list>
